@@ -396,6 +396,70 @@ int lr_compact_scratch_bytes(const lr_plan *plan, size_t *bytes_out);
 int lr_compact(lr_plan *plan, const int32_t *keep_off_d, const int32_t *keep_pages_d, const int32_t *keep_valid_d,
                void *k_pool_d, void *v_pool_d, int32_t *new_len_d, int32_t *n_pages_kept_d, void *scratch_d, void *stream);
 
+/* ---- the same on a cache in 8 bits ------------------------------------------ */
+
+/*
+ * A KV cache in 8 bits: half the bytes of the bf16 pools, which is what a verify
+ * pass reads.  (The paper leaves the cache's format open.)  Pages, heads and token
+ * slots as in the bf16 pools, head_dim bytes a row; behind them one scale byte for
+ * every row:
+ *     k_d, v_d              [n_pages][n_kv_heads][16][head_dim] e4m3 codes
+ *     k_scale_d, v_scale_d  [n_pages][n_kv_heads][16] powers of two (e8m0): byte b
+ *                           stands for 2^(b - 127), 255 for NaN
+ * A row's values are its codes times its scale.  As the scales are powers of two,
+ * every such value is a bf16 number (those that would be 2^128 are infinities, as
+ * in fp32): what reads the cache rounds nothing a second time.  The codes 0x7F and 0xFF (e4m3's NaN) and
+ * scales below 3 are never written here; a visible row that has them has
+ * unspecified values.  The four pools are apart from one another; codes are
+ * 16-byte aligned, scales too.  n_pages: pages in each pool.  All pointers are
+ * device pointers of the caller's; the struct is read during the call alone.
+ */
+typedef struct lr_fp8_cache {
+  void *k_d, *v_d;
+  uint8_t *k_scale_d, *v_scale_d;
+  int64_t n_pages;
+} lr_fp8_cache;
+
+/*
+ * Quantises the K and V rows of n_tokens tokens into their slots.  Token t of K is
+ * the n_kv_heads * head_dim contiguous bf16 at k_d + t * k_stride (in elements; a
+ * slice of a joint projection's output has a larger stride than its own width), V
+ * alike.  slots_d[t] = page * 16 + place in the page; a negative slot leaves its
+ * token out.  For each row x: e = the smallest integer >= -124 with
+ * max|x| * 2^-e <= 448, codes = x * 2^-e rounded to nearest even, byte = e + 127;
+ * a row that holds an infinity or a NaN gets codes 0 and byte 255.  Slots named
+ * twice in a call hold bytes of either token.  A slot of n_pages * 16 or more is
+ * skipped and, with status_d (nullable; two int32 that the caller sets to 0),
+ * leaves {LR_EBOUNDS, its token} there.  Strides are multiples of 8 and not below
+ * n_kv_heads * head_dim, k_d and v_d 16-byte aligned, else LR_EINVAL.
+ */
+int lr_fp8_write(lr_ctx *ctx, const lr_fp8_cache *cache, const void *k_d, int64_t k_stride, const void *v_d, int64_t v_stride,
+                 const int64_t *slots_d, int32_t n_tokens, int32_t *status_d, void *stream);
+
+/* The way back: row t of k_d and v_d (bf16, strided as above) becomes the values at
+ * slots_d[t].  A row whose slot is negative is left as it was; one beyond the cache
+ * too, and reported as above.  A slot may be named more than once. */
+int lr_fp8_read(lr_ctx *ctx, const lr_fp8_cache *cache, const int64_t *slots_d, int32_t n_tokens, void *k_d, int64_t k_stride,
+                void *v_d, int64_t v_stride, int32_t *status_d, void *stream);
+
+/*
+ * lr_verify_attention on such a cache (cache->n_pages >= the plan's n_pool_pages,
+ * else LR_EINVAL): same plan, queries, outputs and errors, for a chain or a tree of
+ * draft steps.  Rows of K and V enter as the values they stand for; products are
+ * summed and the softmax is done in fp32.  A row of the cache that a query sees and
+ * that stands for NaN makes the query's output NaN; one that it does not see has no
+ * influence, whatever it holds.  lr_plan_set_attention_path: 0 automatic, 1 CUDA
+ * cores, 2 tensor cores; there is no CTA-pair kernel for this cache (3:
+ * LR_EUNSUPPORTED).
+ */
+int lr_verify_attention_fp8(lr_plan *plan, const void *q_d, const lr_fp8_cache *cache, void *out_d, float *lse_d,
+                            float softmax_scale, void *stream);
+
+/* lr_compact on such a cache: codes and scales move together, bit for bit.  No
+ * scratch.  Errors as for lr_compact. */
+int lr_compact_fp8(lr_plan *plan, const int32_t *keep_off_d, const int32_t *keep_pages_d, const int32_t *keep_valid_d,
+                   const lr_fp8_cache *cache, int32_t *new_len_d, int32_t *n_pages_kept_d, void *stream);
+
 /* ---- whole pass with device buffers --------------------------------------- */
 
 /* The device buffers of one pass, as the three steps take them. */

@@ -426,6 +426,36 @@ def accept_sample(logits_bits: np.ndarray, draft_ids: np.ndarray, cu_draft: np.n
     return n_accept, final_id, p_draft
 
 
+def accept_sample_drafted(logits_bits: np.ndarray, draft_logits_bits: np.ndarray, draft_ids: np.ndarray, cu_draft: np.ndarray,
+                          temperature: float, draft_temperature: float, u_accept: np.ndarray, u_final: np.ndarray):
+    """Rejection sampling of Background, "Speculative Decoding", for drafts that were sampled from a draft model: draft i is accepted
+    with probability min(1, P_i(d_i) / Q_i(d_i)), here iff u_accept[i] Q_i(d_i) < P_i(d_i); at the first rejection the final token
+    is sampled from the normalised max(0, P_i - Q_i), behind a full match from P of the extra row, by inverse CDF with u_final[b].  Where
+    max(0, P - Q) is 0 everywhere the sample comes from P.  A draft id outside the vocabulary has probability 0 in both.
+    Returns (n_accept, final_id, p_draft, q_draft)."""
+    V, n_branch = logits_bits.shape[1], len(cu_draft) - 1
+    n_accept, final_id = np.zeros(n_branch, dtype=np.int32), np.zeros(n_branch, dtype=np.int32)
+    p_draft, q_draft = np.zeros(int(cu_draft[-1])), np.zeros(int(cu_draft[-1]))
+    for b in range(n_branch):
+        d0, L = int(cu_draft[b]), int(cu_draft[b + 1] - cu_draft[b])
+        weights = None
+        for i in range(L):
+            P, Q = target_probs(logits_bits[d0 + b + i], temperature), target_probs(draft_logits_bits[d0 + i], draft_temperature)
+            d = int(draft_ids[d0 + i])
+            if 0 <= d < V:
+                p_draft[d0 + i], q_draft[d0 + i] = P[d], Q[d]
+            if weights is None and not float(u_accept[d0 + i]) * q_draft[d0 + i] < p_draft[d0 + i]:
+                n_accept[b] = i
+                weights = np.maximum(P - Q, 0.0)
+                if not weights.any():
+                    weights = P
+        if weights is None:
+            n_accept[b] = L
+            weights = target_probs(logits_bits[d0 + b + L], temperature)
+        final_id[b] = sample_inverse_cdf(weights, float(u_final[b]))
+    return n_accept, final_id, p_draft, q_draft
+
+
 # ---------------------------------------------------------------------------
 # a3'. compaction of the committed KV (the step after commit)
 # ---------------------------------------------------------------------------
@@ -453,6 +483,46 @@ def compact(keep_off: np.ndarray, keep_pages: np.ndarray, keep_valid: np.ndarray
         new_len[r] = len(seq)
         n_kept[r] = (len(seq) + PAGE - 1) // PAGE
     return new_len, n_kept, k_out, v_out
+
+
+# ---------------------------------------------------------------------------
+# the 8-bit cache
+# ---------------------------------------------------------------------------
+def e4m3_values() -> np.ndarray:
+    """What the 256 e4m3 codes stand for: sign, four exponent bits (bias 7), three fraction bits; no infinities, 0x7F and 0xFF NaN."""
+    code = np.arange(256)
+    e, m = (code >> 3) & 15, code & 7
+    v = np.where(e > 0, np.ldexp(1.0 + m / 8.0, e - 7), np.ldexp(m / 8.0, -6))
+    v = np.where((code & 127) == 127, np.nan, v)
+    return np.where(code & 128, -v, v)
+
+
+def fp8_store(bits: np.ndarray) -> Tuple[np.ndarray, np.ndarray]:
+    """Rows [..., head size] of bf16 bits as the 8-bit cache stores them: codes and scale bytes (uint8).  The scale of a row is 2^e, e the
+    smallest integer >= -124 with max|x| <= 448 2^e; a code is the e4m3 value nearest to x 2^-e, ties to the even code.  A row with an
+    infinity or a NaN: codes 0, byte 255."""
+    x = bf16_bits_to_f64(bits)
+    fine = np.isfinite(x).all(axis=-1)
+    x = np.where(fine[..., None], x, 0.0)
+    top = np.abs(x).max(axis=-1)
+    e = np.full(top.shape, -124)
+    while (top > np.ldexp(448.0, e)).any():
+        e = np.where(top > np.ldexp(448.0, e), e + 1, e)
+    y = np.ldexp(x, -e[..., None])
+    table = e4m3_values()[:127]
+    hi = np.clip(np.searchsorted(table, np.abs(y)), 1, 126)
+    lo = hi - 1
+    below, above = np.abs(y) - table[lo], table[hi] - np.abs(y)
+    code = np.where((below < above) | ((below == above) & (lo % 2 == 0)), lo, hi).astype(np.uint8)
+    code |= (np.signbit(y) * 128).astype(np.uint8)
+    code[~fine] = 0
+    return code, np.where(fine, e + 127, 255).astype(np.uint8)
+
+
+def fp8_load(codes: np.ndarray, scale: np.ndarray) -> np.ndarray:
+    """The values [..., head size] (float64) of stored rows: code times 2^(byte - 127), NaN for byte 255."""
+    v = np.ldexp(e4m3_values()[codes], scale.astype(np.int64)[..., None] - 127)
+    return np.where((scale == 255)[..., None], np.nan, v)
 
 
 def verify_pass(batch, q_bits, k_pool_bits, v_pool_bits, logits_bits, draft_ids, verdict):

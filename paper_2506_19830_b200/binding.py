@@ -58,6 +58,10 @@ class lr_partition_info(C.Structure):
     _fields_ = [(n, C.c_int32) for n in ("n_cta", "n_merge_targets", "n_partial_slots")] + [("longest_load", C.c_int64)]
 
 
+class lr_fp8_cache(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("k_d", "v_d", "k_scale_d", "v_scale_d")] + [("n_pages", C.c_int64)]
+
+
 class lr_pass_host_io(C.Structure):
     _fields_ = [(n, C.c_void_p) for n in (
         "q_h", "logits_h", "draft_ids_h", "verdict_h", "out_h", "n_accept_h", "bonus_id_h", "n_steps_accepted_h",
@@ -109,6 +113,10 @@ def lib() -> C.CDLL:
                                        C.POINTER(i32), C.POINTER(C.c_double)],
             "lr_compact_scratch_bytes": [vp, C.POINTER(sz)],
             "lr_compact": [vp] * 10,
+            "lr_fp8_write": [vp, vp, vp, i64, vp, i64, vp, i32, vp, vp],
+            "lr_fp8_read": [vp, vp, vp, i32, vp, i64, vp, i64, vp, vp],
+            "lr_verify_attention_fp8": [vp, vp, vp, vp, vp, f32, vp],
+            "lr_compact_fp8": [vp] * 8,
             "lr_pass_staging_bytes": [vp, C.POINTER(sz)],
             "lr_verify_pass": [vp, vp, C.c_char_p, f32, vp, vp],
             "lr_verify_pass_host": [vp, C.POINTER(lr_pass_host_io), vp, vp, vp, sz, f32, vp],
@@ -196,6 +204,57 @@ def _stream_ptr(stream: Optional[torch.cuda.Stream]) -> int:
     return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice()) if stream is None else stream.cuda_stream
 
 
+def _stream_on(device: int, stream: Optional[torch.cuda.Stream]) -> int:
+    """The stream given, or the current one of the context's device, which need not be the current device."""
+    return torch._C._cuda_getCurrentRawStream(device) if stream is None else stream.cuda_stream
+
+
+class Fp8Cache:
+    """``lr_fp8_cache`` over four tensors of the caller's: codes [pages, KV heads, 16, head size] (``torch.float8_e4m3fn``) and scales
+    [pages, KV heads, 16] (``torch.float8_e8m0fnu``), of K and of V; ``torch.uint8`` serves for either.  ``empty`` makes them."""
+
+    def __init__(self, k: torch.Tensor, v: torch.Tensor, k_scale: torch.Tensor, v_scale: torch.Tensor):
+        shape = k.shape
+        for t, want, kind in ((k, shape, torch.float8_e4m3fn), (v, shape, torch.float8_e4m3fn), (k_scale, shape[:3], torch.float8_e8m0fnu),
+                              (v_scale, shape[:3], torch.float8_e8m0fnu)):
+            if t.shape != want or len(shape) != 4 or shape[2] != 16 or t.dtype not in (kind, torch.uint8) or not t.is_contiguous() or t.device != k.device:
+                raise ValueError(f"an 8-bit cache is codes [pages, KV heads, 16, head size] and scales [pages, KV heads, 16], contiguous, on one device: "
+                                 f"got {tuple(t.shape)} {t.dtype} on {t.device}")
+        self.k, self.v, self.k_scale, self.v_scale = k, v, k_scale, v_scale
+        self.n_pages, self.heads, self.head_dim, self.device = shape[0], shape[1], shape[3], k.device
+        self._c = lr_fp8_cache(k.data_ptr(), v.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr(), shape[0])
+        self.c = C.addressof(self._c)
+
+    @staticmethod
+    def empty(model, n_pages: int, device="cuda:0") -> "Fp8Cache":
+        """A cache of zeros (scale bytes 127: 2^0)."""
+        shape = (n_pages, int(model.n_kv_heads), 16, int(model.head_dim))
+        codes = [torch.zeros(shape, dtype=torch.uint8, device=device).view(torch.float8_e4m3fn) for _ in range(2)]
+        return Fp8Cache(*codes, *(torch.full(shape[:3], 127, dtype=torch.uint8, device=device).view(torch.float8_e8m0fnu) for _ in range(2)))
+
+
+def _check_cache(cache: Fp8Cache, ctx: "Context") -> None:
+    # what the C side cannot see: how large the tensors behind its pointers are, and where
+    m = ctx.model
+    if cache.heads != m.n_kv_heads or cache.head_dim != m.head_dim or cache.device.index != ctx.device:
+        raise ValueError(f"the cache has {cache.heads} heads of {cache.head_dim} on {cache.device}, the context {m.n_kv_heads} of {m.head_dim} on cuda:{ctx.device}")
+
+
+def _fp8_rows(ctx: "Context", cache: Fp8Cache, k: torch.Tensor, v: torch.Tensor, slots: torch.Tensor, status: Optional[torch.Tensor]) -> int:
+    """Number of tokens, with the tensors found to be what the C side takes them for."""
+    _check_cache(cache, ctx)
+    n, dev = slots.numel(), cache.device
+    for t in (k, v):
+        if t.shape != (n, cache.heads, cache.head_dim) or t.dtype != torch.bfloat16 or t.device != dev or (n and (t.stride(2) != 1 or t.stride(1) != cache.head_dim)):
+            raise ValueError(f"rows are bf16 [{n}, {cache.heads}, {cache.head_dim}] on {dev}, a token's heads side by side: got {tuple(t.shape)} "
+                             f"{t.dtype} strides {t.stride()} on {t.device}")
+    if slots.dtype != torch.int64 or not slots.is_contiguous() or slots.device != dev:
+        raise ValueError(f"slots are contiguous int64 on {dev}")
+    if status is not None and (status.dtype != torch.int32 or status.numel() < 2 or not status.is_contiguous() or status.device != dev):
+        raise ValueError(f"status is two int32 on {dev}")
+    return n
+
+
 class Context:
     """``lr_ctx``: one per (device, model geometry)."""
 
@@ -267,6 +326,23 @@ class Context:
                                                n_branch, logits.shape[0], float(temperature), int(top_k), float(top_p),
                                                _ptr(u_accept), _ptr(u_final), _ptr(n_accept), _ptr(final_id), _ptr(p_draft),
                                                _ptr(n_kept), _ptr(scratch), _stream_ptr(stream)), "lr_accept_sample_filtered")
+
+    def lr_fp8_write(self, cache: Fp8Cache, k: torch.Tensor, v: torch.Tensor, slots: torch.Tensor, status: Optional[torch.Tensor] = None,
+                     stream=None) -> None:
+        """Quantises rows [tokens, KV heads, head size] (bf16; a slice of a joint projection's output will do) into the cache's token
+        slots (int64: page * 16 + place, negative: none); status: two int32 of zeros that a slot beyond the cache sets."""
+        n = _fp8_rows(self, cache, k, v, slots, status)
+        width = cache.heads * cache.head_dim
+        _check(lib().lr_fp8_write(self.handle, cache.c, _ptr(k), k.stride(0) if n > 1 else width, _ptr(v), v.stride(0) if n > 1 else width, _ptr(slots), n,
+                                  _ptr(status), _stream_on(self.device, stream)), "lr_fp8_write")
+
+    def lr_fp8_read(self, cache: Fp8Cache, slots: torch.Tensor, k: torch.Tensor, v: torch.Tensor, status: Optional[torch.Tensor] = None,
+                    stream=None) -> None:
+        """The values at the token slots, into rows as ``lr_fp8_write`` takes them; a row without a slot is left as it was."""
+        n = _fp8_rows(self, cache, k, v, slots, status)
+        width = cache.heads * cache.head_dim
+        _check(lib().lr_fp8_read(self.handle, cache.c, _ptr(slots), n, _ptr(k), k.stride(0) if n > 1 else width, _ptr(v), v.stride(0) if n > 1 else width,
+                                 _ptr(status), _stream_on(self.device, stream)), "lr_fp8_read")
 
     def accept_sample_filtered_scratch(self, n_rows: int) -> torch.Tensor:
         n = C.c_size_t()
@@ -361,6 +437,18 @@ class Plan:
         """Moves the committed tokens (keep lists of ``lr_commit``) densely into the leading kept pages, in place."""
         _check(lib().lr_compact(self.handle, _ptr(keep_off), _ptr(keep_pages), _ptr(keep_valid), _ptr(k_pool), _ptr(v_pool),
                                 _ptr(new_len), _ptr(n_pages_kept), _ptr(scratch), _stream_ptr(stream)), "lr_compact")
+
+    def lr_verify_attention_fp8(self, q, cache: Fp8Cache, out, lse=None, softmax_scale: float = 0.0, stream=None) -> None:
+        """``lr_verify_attention`` over an 8-bit cache."""
+        _check_cache(cache, self.ctx)
+        _check(lib().lr_verify_attention_fp8(self.handle, _ptr(q), cache.c, _ptr(out), _ptr(lse), float(softmax_scale),
+                                             _stream_on(self.ctx.device, stream)), "lr_verify_attention_fp8")
+
+    def lr_compact_fp8(self, keep_off, keep_pages, keep_valid, cache: Fp8Cache, new_len, n_pages_kept, stream=None) -> None:
+        """``lr_compact`` over an 8-bit cache: codes and scales together."""
+        _check_cache(cache, self.ctx)
+        _check(lib().lr_compact_fp8(self.handle, _ptr(keep_off), _ptr(keep_pages), _ptr(keep_valid), cache.c, _ptr(new_len), _ptr(n_pages_kept),
+                                    _stream_on(self.ctx.device, stream)), "lr_compact_fp8")
 
     def lr_poll_status(self, stream=None) -> int:
         d = C.c_int32()

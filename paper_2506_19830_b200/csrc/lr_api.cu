@@ -937,6 +937,121 @@ extern "C" int lr_compact(lr_plan *p, const int32_t *keep_off, const int32_t *ke
                         reinterpret_cast<cudaStream_t>(stream));
 }
 
+// ---- the 8-bit cache ---------------------------------------------------------------
+// Makes the context's device current for the duration of a call.
+namespace {
+class OnDevice {
+ public:
+  explicit OnDevice(const lr_ctx *ctx) : device_(ctx->device) {
+    rc = cuda_fail(cudaGetDevice(&before_), "cudaGetDevice");
+    if (rc == LR_OK && before_ != device_) rc = cuda_fail(cudaSetDevice(device_), "cudaSetDevice");
+  }
+  ~OnDevice() {
+    if (rc == LR_OK && before_ != device_) cudaSetDevice(before_);
+  }
+  OnDevice(const OnDevice &) = delete;
+  int rc;
+
+ private:
+  int device_, before_ = -1;
+};
+}  // namespace
+
+static int check_cache(const lr_fp8_cache *c, const char *who) {
+  if (!c || !c->k_d || !c->v_d || !c->k_scale_d || !c->v_scale_d) {
+    set_error("%s: null cache", who);
+    return LR_EINVAL;
+  }
+  if ((((uintptr_t)c->k_d | (uintptr_t)c->v_d | (uintptr_t)c->k_scale_d | (uintptr_t)c->v_scale_d) & 15) != 0 || c->n_pages < 1) {
+    set_error("%s: the pools of a cache must be 16-byte aligned and have a page at least", who);
+    return LR_EINVAL;
+  }
+  if (c->n_pages > ((int64_t)1 << 40)) {
+    set_error("%s: %lld pages", who, (long long)c->n_pages);
+    return LR_EINVAL;
+  }
+  if (c->k_d == c->v_d || c->k_scale_d == c->v_scale_d) {
+    set_error("%s: K and V share a pool", who);
+    return LR_EINVAL;
+  }
+  return LR_OK;
+}
+
+static int check_plan_cache(const lr_plan *p, const lr_fp8_cache *c, const char *who) {
+  if (int rc = check_cache(c, who)) return rc;
+  if (!p) {
+    set_error("%s: null plan", who);
+    return LR_EINVAL;
+  }
+  if (c->n_pages < p->dev.n_pool_pages) {
+    set_error("%s: the cache has %lld pages, the plan's batch is over %lld", who, (long long)c->n_pages, (long long)p->dev.n_pool_pages);
+    return LR_EINVAL;
+  }
+  return LR_OK;
+}
+
+static int fp8_move(lr_ctx *ctx, const lr_fp8_cache *c, bool write, void *k, int64_t k_stride, void *v, int64_t v_stride, const int64_t *slots,
+                    int32_t n_tokens, int32_t *status, void *stream) {
+  const char *who = write ? "lr_fp8_write" : "lr_fp8_read";
+  if (int rc = check_cache(c, who)) return rc;
+  if (!ctx || n_tokens < 0 || (n_tokens > 0 && (!k || !v || !slots))) {
+    set_error("%s: null argument or negative count", who);
+    return LR_EINVAL;
+  }
+  const int64_t width = (int64_t)ctx->model.n_kv_heads * ctx->model.head_dim;
+  if ((((uintptr_t)k | (uintptr_t)v) & 15) != 0 || ((uintptr_t)slots & 7) != 0 || ((uintptr_t)status & 3) != 0 || (k_stride & 7) != 0 ||
+      (v_stride & 7) != 0 || k_stride < width || v_stride < width) {
+    set_error("%s: rows must be 16-byte aligned with strides that are multiples of 8 and >= %lld, slots 8-byte aligned", who, (long long)width);
+    return LR_EINVAL;
+  }
+  if (n_tokens == 0) return LR_OK;
+  OnDevice on(ctx);
+  if (on.rc != LR_OK) return on.rc;
+  return launch_fp8_move(ctx, *c, write, k, k_stride, v, v_stride, slots, n_tokens, status, reinterpret_cast<cudaStream_t>(stream));
+}
+
+extern "C" int lr_fp8_write(lr_ctx *ctx, const lr_fp8_cache *cache, const void *k, int64_t k_stride, const void *v, int64_t v_stride,
+                            const int64_t *slots, int32_t n_tokens, int32_t *status, void *stream) {
+  return fp8_move(ctx, cache, true, const_cast<void *>(k), k_stride, const_cast<void *>(v), v_stride, slots, n_tokens, status, stream);
+}
+
+extern "C" int lr_fp8_read(lr_ctx *ctx, const lr_fp8_cache *cache, const int64_t *slots, int32_t n_tokens, void *k, int64_t k_stride, void *v,
+                           int64_t v_stride, int32_t *status, void *stream) {
+  return fp8_move(ctx, cache, false, k, k_stride, v, v_stride, slots, n_tokens, status, stream);
+}
+
+extern "C" int lr_verify_attention_fp8(lr_plan *p, const void *q, const lr_fp8_cache *cache, void *out, float *lse, float scale, void *stream) {
+  if (int rc = check_plan_cache(p, cache, "lr_verify_attention_fp8")) return rc;
+  if (!q || !out) {
+    set_error("lr_verify_attention_fp8: null argument");
+    return LR_EINVAL;
+  }
+  if ((((uintptr_t)q | (uintptr_t)out) & 15) != 0 || ((uintptr_t)lse & 3) != 0) {
+    set_error("lr_verify_attention_fp8: q and out must be 16-byte aligned");
+    return LR_EINVAL;
+  }
+  if (!(scale > 0.f)) scale = 1.0f / sqrtf((float)p->dev.head_dim);
+  if (p->attention_path == 3) {
+    set_error("lr_verify_attention_fp8: there is no CTA-pair kernel for an 8-bit cache");
+    return LR_EUNSUPPORTED;
+  }
+  OnDevice on(p->ctx);
+  if (on.rc != LR_OK) return on.rc;
+  return launch_attn_fp8_generic(p, q, *cache, out, lse, scale, reinterpret_cast<cudaStream_t>(stream));
+}
+
+extern "C" int lr_compact_fp8(lr_plan *p, const int32_t *keep_off, const int32_t *keep_pages, const int32_t *keep_valid, const lr_fp8_cache *cache,
+                              int32_t *new_len, int32_t *n_pages_kept, void *stream) {
+  if (int rc = check_plan_cache(p, cache, "lr_compact_fp8")) return rc;
+  if (!keep_off || !keep_pages || !keep_valid || !new_len || !n_pages_kept) {
+    set_error("lr_compact_fp8: null argument");
+    return LR_EINVAL;
+  }
+  OnDevice on(p->ctx);
+  if (on.rc != LR_OK) return on.rc;
+  return launch_compact_fp8(p, keep_off, keep_pages, keep_valid, *cache, new_len, n_pages_kept, reinterpret_cast<cudaStream_t>(stream));
+}
+
 // ---- status --------------------------------------------------------------------
 extern "C" int lr_poll_status(lr_plan *p, void *stream, int32_t *detail) {
   if (!p) {

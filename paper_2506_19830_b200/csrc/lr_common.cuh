@@ -367,6 +367,12 @@ int launch_accept_filtered(lr_ctx *ctx, const void *logits, int64_t stride, cons
                            int32_t *n_kept, void *scratch, cudaStream_t s);
 int launch_compact(lr_plan *p, const int32_t *keep_off, const int32_t *keep_pages, const int32_t *keep_valid, void *k_pool,
                    void *v_pool, int32_t *new_len, int32_t *n_pages_kept, cudaStream_t s);
+// the 8-bit cache
+int launch_fp8_move(lr_ctx *ctx, const lr_fp8_cache &c, bool write, void *k, int64_t k_stride, void *v, int64_t v_stride, const int64_t *slots,
+                    int32_t n_tokens, int32_t *status, cudaStream_t s);
+int launch_attn_fp8_generic(lr_plan *p, const void *q, const lr_fp8_cache &c, void *out, float *lse, float scale, cudaStream_t s);
+int launch_compact_fp8(lr_plan *p, const int32_t *keep_off, const int32_t *keep_pages, const int32_t *keep_valid, const lr_fp8_cache &c,
+                       int32_t *new_len, int32_t *n_pages_kept, cudaStream_t s);
 // after_accept: the launch before it in the stream is a kernel that does not write the verdicts and that lets its successor start
 // only once everything older has finished -- launch_accept's, which waits in its first line.  The verdicts are then read while it
 // still runs.
