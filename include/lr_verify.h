@@ -309,6 +309,38 @@ int lr_accept_sample_filtered(lr_ctx *ctx, const void *logits_d, int64_t row_str
                               void *scratch_d, void *stream);
 
 /*
+ * Stochastic token-level acceptance for drafts that were sampled from a draft
+ * model's distribution (Background, "Speculative Decoding", with a draft model Q).
+ * draft_logits_d: [sum L_b][draft_row_stride] bf16, first `vocab` entries of a row
+ * used; row cu_draft[b] + i is what draft i of branch b was drawn from.  With
+ * P_i = softmax(logits[row0_b + i] / temperature) and
+ * Q_i = softmax(draft_logits[cu_draft[b] + i] / draft_temperature):
+ *     draft i is accepted iff u_accept[cu_draft[b] + i] * Q_i(d_i) < P_i(d_i);
+ *     n_b     = number of drafts accepted before the first rejection;
+ *     final_b = inverse-CDF sample with u_final[b] (smallest v whose cumulative
+ *               weight exceeds u * total) from the weights max(0, P_{n_b} - Q_{n_b}),
+ *               or from P_{L_b} when every draft was accepted.
+ * The emitted tokens are then distributed as the target's.  Where no weight is left
+ * (P <= Q everywhere, which rounding alone can bring about behind a rejection) the
+ * sample comes from P_{n_b}.  A NaN logit counts as -inf; with a logit of +inf the
+ * results are unspecified.  A row of -inf alone has probability 0 everywhere.  The
+ * uniforms, in [0, 1), are inputs.  Arithmetic is fp32 (sums over the weights in 64
+ * bits): a decision whose uniform lies within rounding of its threshold may differ
+ * from an exact evaluation.  p_draft_d, q_draft_d (nullable, [sum L_b]) receive
+ * P_i(d_i) and Q_i(d_i) of every draft; a draft id outside [0, vocab) has 0 in both
+ * and is rejected.  Rows, strides and alignment of both matrices as for
+ * lr_accept_greedy; temperatures > 0; at most 65535 target rows per call.
+ * scratch_d: lr_accept_sample_drafted_scratch_bytes bytes, 8-byte aligned, no
+ * initial contents needed; calls sharing it must not overlap on the device.
+ */
+int lr_accept_sample_drafted_scratch_bytes(const lr_ctx *ctx, int32_t n_rows, size_t *bytes_out);
+int lr_accept_sample_drafted(lr_ctx *ctx, const void *logits_d, int64_t row_stride_elems, const void *draft_logits_d,
+                             int64_t draft_row_stride_elems, const int32_t *draft_ids_d, const int32_t *cu_draft_d,
+                             int32_t n_branch, int32_t n_rows, float temperature, float draft_temperature,
+                             const float *u_accept_d, const float *u_final_d, int32_t *n_accept_d, int32_t *final_id_d,
+                             float *p_draft_d, float *q_draft_d, void *scratch_d, void *stream);
+
+/*
  * lr_accept_greedy without a caller-provided scratch buffer.  (The paper has no
  * counterpart: this is a packaging variant of the call above, same results.)
  *

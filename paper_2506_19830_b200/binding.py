@@ -106,6 +106,8 @@ def lib() -> C.CDLL:
             "lr_accept_sample": [vp, vp, i64, vp, vp, i32, i32, f32, vp, vp, vp, vp, vp, vp, vp],
             "lr_accept_sample_filtered_scratch_bytes": [vp, i32, C.POINTER(sz)],
             "lr_accept_sample_filtered": [vp, vp, i64, vp, vp, i32, i32, f32, i32, f32, vp, vp, vp, vp, vp, vp, vp, vp],
+            "lr_accept_sample_drafted_scratch_bytes": [vp, i32, C.POINTER(sz)],
+            "lr_accept_sample_drafted": [vp, vp, i64, vp, i64, vp, vp, i32, i32, f32, f32, vp, vp, vp, vp, vp, vp, vp, vp],
             "lr_commit": [vp] + [vp] * 10 + [vp],
             "lr_cycle_simulate_sync": [i32, i64, i64, vp, i64, C.POINTER(lr_cycle_stats)],
             "lr_cycle_simulate_async": [i32, i64, i64, vp, i64, C.POINTER(lr_cycle_stats)],
@@ -326,6 +328,22 @@ class Context:
                                                n_branch, logits.shape[0], float(temperature), int(top_k), float(top_p),
                                                _ptr(u_accept), _ptr(u_final), _ptr(n_accept), _ptr(final_id), _ptr(p_draft),
                                                _ptr(n_kept), _ptr(scratch), _stream_ptr(stream)), "lr_accept_sample_filtered")
+
+    def lr_accept_sample_drafted(self, logits: torch.Tensor, draft_logits: torch.Tensor, draft_ids: torch.Tensor, cu_draft: torch.Tensor,
+                                 temperature: float, draft_temperature: float, u_accept: torch.Tensor, u_final: torch.Tensor, n_accept: torch.Tensor,
+                                 final_id: torch.Tensor, scratch: torch.Tensor, p_draft: Optional[torch.Tensor] = None,
+                                 q_draft: Optional[torch.Tensor] = None, stream=None) -> None:
+        """Rejection-sampling acceptance of drafts that a draft model sampled; draft_logits [sum L, >= vocab] are what they were drawn from."""
+        n_branch, n_rows = cu_draft.numel() - 1, logits.shape[0]
+        _check(lib().lr_accept_sample_drafted(self.handle, _ptr(logits), logits.stride(0), _ptr(draft_logits), draft_logits.stride(0), _ptr(draft_ids),
+                                              _ptr(cu_draft), n_branch, n_rows, temperature, draft_temperature, _ptr(u_accept), _ptr(u_final),
+                                              _ptr(n_accept), _ptr(final_id), _ptr(p_draft), _ptr(q_draft), _ptr(scratch),
+                                              _stream_on(self.device, stream)), "lr_accept_sample_drafted")
+
+    def accept_sample_drafted_scratch(self, n_rows: int) -> torch.Tensor:
+        n = C.c_size_t()
+        _check(lib().lr_accept_sample_drafted_scratch_bytes(self.handle, n_rows, C.byref(n)), "lr_accept_sample_drafted_scratch_bytes")
+        return torch.empty((n.value + 7) // 8, dtype=torch.int64, device=f"cuda:{self.device}")
 
     def lr_fp8_write(self, cache: Fp8Cache, k: torch.Tensor, v: torch.Tensor, slots: torch.Tensor, status: Optional[torch.Tensor] = None,
                      stream=None) -> None:

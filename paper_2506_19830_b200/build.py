@@ -10,7 +10,7 @@ CSRC = os.path.join(PKG_DIR, "csrc")
 INCLUDE = os.path.join(os.path.dirname(PKG_DIR), "include")
 LIB_PATH = os.path.join(PKG_DIR, "liblr_verify.so")
 SOURCES = ["lr_api.cu", "accept_greedy.cu", "accept_sample.cu", "accept_filter.cu", "commit.cu", "pass_tail.cu", "compact.cu", "cycle_host.cu", "attn_generic.cu", "attn_tc.cu", "attn_pair.cu",
-           "fp8_cache.cu", "attn_fp8_generic.cu"]
+           "accept_drafted.cu", "fp8_cache.cu", "attn_fp8_generic.cu"]
 
 
 def _nvcc() -> str:

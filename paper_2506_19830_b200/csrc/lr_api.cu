@@ -732,6 +732,25 @@ extern "C" int lr_plan_debug_set_page(lr_plan *p, int32_t page_slot, int32_t new
   return cuda_fail(e, "lr_plan_debug_set_page upload");
 }
 
+// Makes the context's device current for the duration of a call.
+namespace {
+class OnDevice {
+ public:
+  explicit OnDevice(const lr_ctx *ctx) : device_(ctx->device) {
+    rc = cuda_fail(cudaGetDevice(&before_), "cudaGetDevice");
+    if (rc == LR_OK && before_ != device_) rc = cuda_fail(cudaSetDevice(device_), "cudaSetDevice");
+  }
+  ~OnDevice() {
+    if (rc == LR_OK && before_ != device_) cudaSetDevice(before_);
+  }
+  OnDevice(const OnDevice &) = delete;
+  int rc;
+
+ private:
+  int device_, before_ = -1;
+};
+}  // namespace
+
 // ---- steps ---------------------------------------------------------------------
 static int check_attention(const lr_plan *p, const void *q, const void *k, const void *v, const void *out, const float *lse) {
   if (!p || !q || !k || !v || !out) {
@@ -894,6 +913,45 @@ extern "C" int lr_accept_sample_filtered(lr_ctx *ctx, const void *logits, int64_
                                 u_final, n_accept, final_id, p_draft, n_kept, scratch, reinterpret_cast<cudaStream_t>(stream));
 }
 
+extern "C" int lr_accept_sample_drafted_scratch_bytes(const lr_ctx *ctx, int32_t n_rows, size_t *bytes_out) {
+  if (!ctx || !bytes_out || n_rows < 0) {
+    set_error("lr_accept_sample_drafted_scratch_bytes: bad argument");
+    return LR_EINVAL;
+  }
+  *bytes_out = accept_drafted_scratch_bytes(ctx->model.vocab, n_rows);
+  return LR_OK;
+}
+
+extern "C" int lr_accept_sample_drafted(lr_ctx *ctx, const void *logits, int64_t stride, const void *draft_logits, int64_t draft_stride,
+                                        const int32_t *drafts, const int32_t *cu_draft, int32_t n_branch, int32_t n_rows, float temperature,
+                                        float draft_temperature, const float *u_accept, const float *u_final, int32_t *n_accept, int32_t *final_id,
+                                        float *p_draft, float *q_draft, void *scratch, void *stream) {
+  if (!(temperature > 0.f) || !(draft_temperature > 0.f) || temperature > 3.0e38f || draft_temperature > 3.0e38f) {
+    set_error("lr_accept_sample_drafted: temperatures must be positive and finite");
+    return LR_EINVAL;
+  }
+  if (n_branch < 0 || n_rows < n_branch) {
+    set_error("lr_accept_sample_drafted: n_rows %d < n_branch %d", n_rows, n_branch);
+    return LR_EINVAL;
+  }
+  if (!ctx || !logits || !cu_draft || !u_final || !n_accept || !final_id || !scratch ||
+      ((!draft_logits || !drafts || !u_accept) && n_rows > n_branch)) {
+    set_error("lr_accept_sample_drafted: null argument");
+    return LR_EINVAL;
+  }
+  const bool drafter = n_rows > n_branch;  // else its rows are not looked at
+  if (((uintptr_t)logits & 15) != 0 || (stride & 7) != 0 || stride < ctx->model.vocab || ((uintptr_t)scratch & 7) != 0 ||
+      (drafter && (((uintptr_t)draft_logits & 15) != 0 || (draft_stride & 7) != 0 || draft_stride < ctx->model.vocab))) {
+    set_error("lr_accept_sample_drafted: logits must be 16-byte aligned with row strides that are multiples of 8 and >= vocab");
+    return LR_EINVAL;
+  }
+  if (n_branch == 0) return LR_OK;
+  OnDevice on(ctx);
+  if (on.rc != LR_OK) return on.rc;
+  return launch_accept_drafted(ctx, logits, stride, draft_logits, draft_stride, drafts, cu_draft, n_branch, n_rows, temperature, draft_temperature,
+                               u_accept, u_final, n_accept, final_id, p_draft, q_draft, scratch, reinterpret_cast<cudaStream_t>(stream));
+}
+
 static int check_commit(const lr_plan *p, const uint8_t *verdict, const int32_t *n_accept, const CommitOut &o) {
   if (!p || !n_accept || !o.n_steps || !o.survivor || !o.committed || !o.keep_off || !o.keep_pages || !o.keep_valid || !o.free_off ||
       !o.free_pages || (!verdict && p->n_verdicts > 0)) {
@@ -938,25 +996,6 @@ extern "C" int lr_compact(lr_plan *p, const int32_t *keep_off, const int32_t *ke
 }
 
 // ---- the 8-bit cache ---------------------------------------------------------------
-// Makes the context's device current for the duration of a call.
-namespace {
-class OnDevice {
- public:
-  explicit OnDevice(const lr_ctx *ctx) : device_(ctx->device) {
-    rc = cuda_fail(cudaGetDevice(&before_), "cudaGetDevice");
-    if (rc == LR_OK && before_ != device_) rc = cuda_fail(cudaSetDevice(device_), "cudaSetDevice");
-  }
-  ~OnDevice() {
-    if (rc == LR_OK && before_ != device_) cudaSetDevice(before_);
-  }
-  OnDevice(const OnDevice &) = delete;
-  int rc;
-
- private:
-  int device_, before_ = -1;
-};
-}  // namespace
-
 static int check_cache(const lr_fp8_cache *c, const char *who) {
   if (!c || !c->k_d || !c->v_d || !c->k_scale_d || !c->v_scale_d) {
     set_error("%s: null cache", who);

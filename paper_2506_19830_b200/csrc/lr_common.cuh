@@ -365,6 +365,10 @@ int launch_accept_filtered(lr_ctx *ctx, const void *logits, int64_t stride, cons
                            int32_t n_branch, int32_t n_rows, float temperature, int32_t top_k, float top_p,
                            const float *u_accept, const float *u_final, int32_t *n_accept, int32_t *final_id, float *p_draft,
                            int32_t *n_kept, void *scratch, cudaStream_t s);
+size_t accept_drafted_scratch_bytes(int32_t vocab, int32_t n_rows);
+int launch_accept_drafted(lr_ctx *ctx, const void *logits, int64_t stride, const void *draft_logits, int64_t draft_stride, const int32_t *drafts,
+                          const int32_t *cu_draft, int32_t n_branch, int32_t n_rows, float temperature, float draft_temperature, const float *u_accept,
+                          const float *u_final, int32_t *n_accept, int32_t *final_id, float *p_draft, float *q_draft, void *scratch, cudaStream_t s);
 int launch_compact(lr_plan *p, const int32_t *keep_off, const int32_t *keep_pages, const int32_t *keep_valid, void *k_pool,
                    void *v_pool, int32_t *new_len, int32_t *n_pages_kept, cudaStream_t s);
 // the 8-bit cache

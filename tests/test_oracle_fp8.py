@@ -132,3 +132,13 @@ def test_tensors_that_are_no_cache_are_refused():
                  (codes.transpose(0, 1), codes.transpose(0, 1), scale.transpose(0, 1), scale.transpose(0, 1))):
         with pytest.raises(ValueError):
             B.Fp8Cache(*args)
+
+
+def test_drafted_acceptance_is_refused_without_a_device():
+    L = B.lib()
+    good = [None, 16, 104, 16, 104, 16, 16, 1, 3, 1.0, 1.0, 16, 16, 16, 16, None, None, 16, None]
+    for at, bad in ((9, 0.0), (9, float("nan")), (10, -1.0), (10, float("inf")), (7, -1), (7, 4), (1, None)):
+        args = list(good)
+        args[at] = bad
+        assert L.lr_accept_sample_drafted(*args) == -1
+    assert L.lr_accept_sample_drafted(*good) == -1 and "null" in L.lr_last_error().decode()
