@@ -10,7 +10,7 @@ CSRC = os.path.join(PKG_DIR, "csrc")
 INCLUDE = os.path.join(os.path.dirname(PKG_DIR), "include")
 LIB_PATH = os.path.join(PKG_DIR, "liblr_verify.so")
 SOURCES = ["lr_api.cu", "accept_greedy.cu", "accept_sample.cu", "accept_filter.cu", "commit.cu", "pass_tail.cu", "compact.cu", "cycle_host.cu", "attn_generic.cu", "attn_tc.cu", "attn_pair.cu",
-           "accept_drafted.cu", "fp8_cache.cu", "attn_fp8_generic.cu"]
+           "accept_drafted.cu", "fp8_cache.cu", "attn_fp8_generic.cu", "attn_fp8.cu"]
 
 
 def _nvcc() -> str:
@@ -35,7 +35,7 @@ def build_library(force: bool = False, verbose: bool = False) -> str:
     srcs = [os.path.join(CSRC, s) for s in SOURCES if os.path.exists(os.path.join(CSRC, s))]
     cmd = [
         _nvcc(), "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
-        "-shared", "-Xcompiler", "-fPIC", "-I", INCLUDE, "-I", CSRC, "-o", LIB_PATH,
+        "--threads", "0", "-shared", "-Xcompiler", "-fPIC", "-I", INCLUDE, "-I", CSRC, "-o", LIB_PATH,
     ] + (["-Xptxas", "-v"] if verbose else []) + srcs
     res = subprocess.run(cmd, capture_output=True, text=True)
     if res.returncode != 0:

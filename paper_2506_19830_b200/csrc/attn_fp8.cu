@@ -1,0 +1,840 @@
+// Tensor-core nested-prefix attention over the 8-bit cache (head_dim 64 or 128).
+//
+// The plan -- page lists, tiles of 128 keys, M-tiles, pieces, partial results and their merge -- is that of attn_tc.cu, and so are the two
+// streams of a CTA, the issuers and the score buffers in tensor memory.  What is different is how K and V get into shared memory and
+// what the products are made of.
+//
+// Halves.  The products are f16 x f16 -> fp32.  An e4m3 code is an f16 number, and one instruction turns two codes into two halves; a bf16
+// operand would take five.  Scales are powers of two, and only differences of exponents go into a tile: with ref the largest scale byte
+// of the tile's keys, a row enters as code * 2^(byte - ref), exact unless it lies 2^-33 below the largest number of the tile.  2^(ref - 127) itself
+// goes where it costs nothing:
+//   K: into the factor that takes scores to exponents (one number a row and tile);
+//   V: into the exponent of the weights, P 2^(ref - base), where base is the stream's: the accumulator is in units of 2^(base - 127).  When a
+//      tile's ref is more than 2^3 above base the accumulator is scaled down, as when the maximum grows; the row sums take the factor
+//      back out.  A tile far below base (2^-24) sums its weights apart, as keys whose values are all zeros may have any weight.
+//   Q: a row is scaled by a power of two to lie below 4, which goes into the same factor as K's.
+// The weights are f16 as well, 2^6 above the row's reference and at most 2^15: 11 bits instead of bf16's 8, nothing lost above 2^-20 of the
+// largest, and a row whose scores grow by more than 2^6 does its half-tile again.
+//
+// One CTA = 16 warps in four warpgroups, registers moved with setmaxnreg (168 x 256 + 120 x 128 + 56 x 128 <= 128 x 512):
+//   warps 8-11  converters.  No staging: a thread loads its codes (16 bytes of eight keys of a tile; four with head size 64) straight into registers,
+//               two tiles (four) ahead -- 32 KB in flight an SM -- turns them into halves and stores them as the swizzled operand.  Through
+//               shared memory they would cross it twice more, and it is as busy as the tensor cores: 32 KB of a tile written and
+//               read by the products, and Q read again for every 64 keys.  A warp has the tile's 128 scale bytes in one word a lane, so that
+//               ref is one reduction and a key's byte one shuffle.  Slots that hold no valid token become zeros, whatever they held.
+//   warps 12, 13  MMA issuers of stream 0 and 1.
+//   warps 0-3, 4-7  softmax of stream 0 and 1, one thread per query row; they also turn the rows of Q into halves.
+//
+// A visible row that stands for NaN: K's becomes NaN as an operand, and with it the row's sum.  V's becomes zeros, for a weight of 0 times NaN
+// would reach rows that do not see it; the converters note such keys per tile, and a row that sees one multiplies its result by NaN.
+#include <cuda.h>
+
+#include <algorithm>
+
+#include "attn_mma.cuh"
+#include "fp8_cache.cuh"
+
+namespace lr {
+
+namespace {
+
+constexpr int kHalfBytes = 16384;  // 128 rows or keys x 64 channels
+constexpr int kAtomBytes = 1024;   // 8 keys x 64 channels, one 128-byte-swizzle atom
+constexpr int kMaxStages = 10;
+constexpr int kThreads = 512;
+constexpr int kInfos = 16;         // tiles whose scales are published ahead of their products; more than the ring can hold
+constexpr float kGrow = 6.0f;      // log2: how far the scores of a row may rise above its reference exponent
+constexpr float kHead = 6.0f;      // log2: weights are kept this much above what they are
+constexpr int kRise = 3;           // log2: ... and V's tiles this much above the accumulator's unit: 6 + 6 + 3 = 15, f16 ends at 16
+constexpr int kApart = 24;         // log2: a tile of V this far below the unit sums its weights apart
+
+template <int kD>
+struct Shape {
+  static_assert(kD == 64 || kD == 128, "head sizes of the tensor-core path");
+  static constexpr int kHalves = kD / 64;
+  static constexpr int kTileBytes = kHalves * kHalfBytes;   // as in attn_tc.cu
+  static constexpr int kGroupBytes = kHalves * kAtomBytes;
+  static constexpr int kStages = kD == 128 ? 5 : 10;
+  static constexpr int kCols = kD / 16;                     // converter threads side by side in a row, 16 channels each
+  static constexpr int kGroups = 128 / kCols;               // groups of four keys that the converters have at a time
+  static constexpr int kRounds = 32 / kGroups;              // ... and how many times for a tile
+  static constexpr int kChunks = 4 * kRounds;               // 16-byte chunks of a tile that a thread has
+  static constexpr int kAhead = 16 / kChunks;               // tiles that it has in registers
+};
+
+struct Info {  // of a tile: the largest scale bytes of its keys; whether some visible row of V stands for NaN
+  int32_t k_ref, v_ref, v_nan;
+};
+
+struct __align__(16) Ctrl {
+  TcCtaHead head;         // this CTA's record
+  uint64_t kv_full[kMaxStages], kv_empty[kMaxStages];
+  uint64_t q_full, q_empty;
+  uint64_t s_full[2][2], p_full[2][2], o_done[2];  // [stream][half]
+  uint64_t epi_done, drain[2];
+  uint64_t xch;           // stream 1 -> stream 0: its sums are published and its accumulator is final
+  uint64_t info_full[kInfos];
+  uint32_t tmem_base;
+  int abort_flag;
+  uint64_t wait_limit_ns;
+  Info info[kInfos];
+  uint8_t v_nan[kInfos][32];  // four keys a byte
+  float xch_m[128], xch_l[128], xch_unit[128];  // stream 1's rows, for the in-CTA combination
+};
+constexpr int kCtrlBytes = 3 << 10;
+static_assert(sizeof(Ctrl) <= kCtrlBytes, "Ctrl must fit behind the tiles");
+template <int kD>
+constexpr int kSmemBytes = (2 + Shape<kD>::kStages) * Shape<kD>::kTileBytes + kCtrlBytes;  // Q, the ring; the base must be 1024-aligned
+static_assert(kSmemBytes<64> <= 227 * 1024 && kSmemBytes<128> <= 227 * 1024, "shared memory per CTA");
+
+// Instruction descriptors: D fp32, A and B f16 (format 0), M = 128; QK: N = 64 keys, both operands K-major; PV: N = head size, B N-major.
+constexpr uint32_t kIdescBase = (1u << 4) | (8u << 24);
+constexpr uint32_t kIdescQK = kIdescBase | ((64u >> 3) << 17);
+template <int kD>
+constexpr uint32_t kIdescPV = kIdescBase | (((uint32_t)kD >> 3) << 17) | (1u << 16);
+
+__device__ __forceinline__ uint32_t pack_f16(float lo, float hi) {
+  uint32_t r;
+  asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+  return r;
+}
+__device__ __forceinline__ uint32_t mul_f16x2(uint32_t a, uint32_t b) {
+  uint32_t r;
+  asm("mul.rn.f16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+  return r;
+}
+__device__ __forceinline__ float pow2(int e) { return __uint_as_float((uint32_t)(min(max(e, -126), 127) + 127) << 23); }
+__device__ __forceinline__ uint4 ld_codes(const uint8_t *p) {
+  uint4 v;
+  asm volatile("ld.global.nc.L1::no_allocate.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p));
+  return v;
+}
+__device__ __forceinline__ void st_shared(uint32_t addr, uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
+  asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(addr), "r"(a), "r"(b), "r"(c), "r"(d) : "memory");
+}
+
+// P = exp2(sc * s - m + bias) for 64 scores, as halves over the first half of the score buffer; returns their fp32 sum.  With kMax also the
+// maximum of the raw scores.
+template <bool kMax>
+__device__ __forceinline__ float exp_half(const uint32_t (&v)[64], uint32_t addr, float sc, float neg, float &raw_max) {
+  const float2 s2 = make_float2(sc, sc), n2 = make_float2(neg, neg);
+  float2 acc0 = make_float2(0.f, 0.f), acc1 = make_float2(0.f, 0.f);
+  float m0 = -INFINITY, m1 = -INFINITY;
+  uint32_t pk[32];
+#pragma unroll
+  for (int i = 0; i < 64; i += 4) {
+    float2 y0 = ffma2(make_float2(bits_f(v[i]), bits_f(v[i + 1])), s2, n2);
+    float2 y1 = ffma2(make_float2(bits_f(v[i + 2]), bits_f(v[i + 3])), s2, n2);
+    if (kMax) m0 = max3(m0, bits_f(v[i]), bits_f(v[i + 1]));
+    y0.x = ex2(y0.x);
+    y0.y = ex2(y0.y);
+    if (kMax) m1 = max3(m1, bits_f(v[i + 2]), bits_f(v[i + 3]));
+    y1.x = ex2(y1.x);
+    y1.y = ex2(y1.y);
+    acc0 = fadd2(acc0, y0);
+    acc1 = fadd2(acc1, y1);
+    pk[i >> 1] = pack_f16(y0.x, y0.y);
+    pk[(i >> 1) + 1] = pack_f16(y1.x, y1.y);
+  }
+  tmem_st32(addr, pk);
+  if (kMax) raw_max = fmaxf(m0, m1);
+  acc0 = fadd2(acc0, acc1);
+  return acc0.x + acc0.y;
+}
+
+// Whether the row sees a key of the tile whose row of V stands for NaN.  pages: null where it sees all keys.
+__device__ __noinline__ bool sees_nan(const uint8_t *nan4, const TcPage *pages, RowInfo ri) {
+  bool seen = false;
+  for (int p = 0; p < kPagesPerTile; ++p) {
+    const uint32_t w = *reinterpret_cast<const volatile uint32_t *>(nan4 + 4 * p);  // a byte of it: four keys
+    const uint32_t keys = (w & 15u) | ((w >> 4) & 0xF0u) | ((w >> 8) & 0xF00u) | ((w >> 12) & 0xF000u);
+    const int n = pages != nullptr ? page_n_ok(pages[p].meta, ri) : kPage;
+    seen = seen || (keys & ((1u << n) - 1u)) != 0u;
+  }
+  return seen;
+}
+
+// A row of Q, scaled by a power of two to lie below 4, as halves into the channel halves [h0, h1) of its M-tile; returns the exponent taken out.
+template <int kD>
+__device__ __noinline__ int convert_q(const uint16_t *__restrict__ q, int64_t q_index, uint32_t tile, int r, int h0, int h1) {
+  uint4 x[kD / 8];
+#pragma unroll
+  for (int i = 0; i < kD / 8; ++i) x[i] = q_index >= 0 ? __ldg(reinterpret_cast<const uint4 *>(q + q_index * kD) + i) : make_uint4(0, 0, 0, 0);
+  uint32_t top = 0;
+#pragma unroll
+  for (int i = 0; i < kD / 8; ++i)
+    top = __vmaxu2(top, __vmaxu2(__vmaxu2(x[i].x & 0x7FFF7FFFu, x[i].y & 0x7FFF7FFFu), __vmaxu2(x[i].z & 0x7FFF7FFFu, x[i].w & 0x7FFF7FFFu)));
+  top = max(top & 0xFFFFu, top >> 16);
+  const int e = top < 0x7F80u ? min(max((int)(top >> 7) - 127, -126), 126) : 0;
+  const float by = pow2(-e);
+#pragma unroll
+  for (int i = 0; i < kD / 8; ++i) {
+    if (i / 8 < h0 || i / 8 >= h1) continue;
+    const uint32_t w[4] = {x[i].x, x[i].y, x[i].z, x[i].w};
+    uint32_t o[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) o[j] = pack_f16(bits_f(w[j] << 16) * by, bits_f(w[j] & 0xFFFF0000u) * by);
+    st_shared(tile + (i / 8) * kHalfBytes + r * 128 + (((i & 7) ^ (r & 7)) << 4), o[0], o[1], o[2], o[3]);
+  }
+  return e;
+}
+
+// The store epilogue of a softmax thread: row r of the accumulator at o_addr times `self` (and, when the CTA's two streams worked on the same
+// rows, of the other stream's at o_other times `other`) goes out as bf16 (slot < 0) or as an fp32 partial.  Not inlined: its two row
+// buffers must not weigh on the register allocation of the sweep.
+template <int kD>
+__device__ __noinline__ void store_rows(uint32_t o_addr, uint32_t o_other, int slot, float self, float other, bool other_live, float m_out, float l_out, int r,
+                                        int64_t q_index, uint16_t *__restrict__ out, float *__restrict__ lse, float *__restrict__ partial_o,
+                                        float *__restrict__ partial_ml) {
+  const bool any_other = __any_sync(0xFFFFFFFFu, other_live);
+  if (slot < 0) {
+    const float inv = 1.0f / l_out;
+    self *= inv;
+    other *= inv;
+  }
+#pragma unroll
+  for (int hf = 0; hf < kD / 64; ++hf) {
+    uint32_t o[64];
+    tmem_ld64(o_addr + hf * 64, o);
+    tc_wait_ld();
+#pragma unroll
+    for (int c = 0; c < 64; ++c) o[c] = __float_as_uint(bits_f(o[c]) * self);
+    if (any_other) {  // the loads are warp-wide; a row whose other stream saw nothing keeps its own values
+#pragma unroll
+      for (int part = 0; part < 2; ++part) {
+        uint32_t p[32];
+        tmem_ld32(o_other + hf * 64 + part * 32, p);
+        tc_wait_ld();
+        if (other_live) {
+#pragma unroll
+          for (int c = 0; c < 32; ++c) o[part * 32 + c] = __float_as_uint(fmaf(bits_f(p[c]), other, bits_f(o[part * 32 + c])));
+        }
+      }
+    }
+    if (q_index >= 0) {
+      if (slot < 0) {
+        uint4 *dst = reinterpret_cast<uint4 *>(out + q_index * kD + hf * 64);
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+          dst[j] = make_uint4(pack_bf16(bits_f(o[8 * j]), bits_f(o[8 * j + 1])), pack_bf16(bits_f(o[8 * j + 2]), bits_f(o[8 * j + 3])),
+                              pack_bf16(bits_f(o[8 * j + 4]), bits_f(o[8 * j + 5])), pack_bf16(bits_f(o[8 * j + 6]), bits_f(o[8 * j + 7])));
+      } else {
+        // chunk-major: 16-byte chunk k of row r at [slot][k][r], so a warp's store is 512 contiguous bytes
+        uint4 *dst = reinterpret_cast<uint4 *>(partial_o) + ((int64_t)slot * (kD / 4) + hf * 16) * 128 + r;
+#pragma unroll
+        for (int j = 0; j < 16; ++j) dst[j * 128] = make_uint4(o[4 * j], o[4 * j + 1], o[4 * j + 2], o[4 * j + 3]);
+      }
+    }
+  }
+  if (q_index < 0) return;
+  if (slot >= 0) {
+    // a sum that is not a number must not look like that of a row that saw nothing: the merge asks whether the sum is above 0
+    const bool nan = l_out != l_out;
+    *reinterpret_cast<float2 *>(partial_ml + ((int64_t)slot * 128 + r) * 2) = nan ? make_float2(l_out, 1.0f) : make_float2(m_out, l_out);
+  } else if (lse != nullptr) {
+    lse[q_index] = (m_out + log2f(l_out)) * 0.6931471805599453f;
+  }
+}
+
+struct Fp8Pools {
+  const uint8_t *k, *v, *k_scale, *v_scale;
+};
+
+// What a converter thread has of one tile of K or V on its way.
+template <int kD>
+struct Fetched {
+  uint4 codes[Shape<kD>::kChunks];
+  uint32_t word, v_word;  // scale bytes of keys 4 lane .. 4 lane + 3; with a tile of K also V's
+  int32_t valid;          // tokens of the page those keys lie in
+};
+
+// the largest scale byte of the tile, of valid keys that do not stand for NaN; `bytes`: this lane's four, those of no valid token cleared
+__device__ __forceinline__ int tile_ref(uint32_t bytes) {
+  const uint32_t w = bytes & ~__vcmpeq4(bytes, 0xFFFFFFFFu), t = __vmaxu4(w, w >> 16);
+  return (int)max(__reduce_max_sync(0xFFFFFFFFu, max(t & 0xFFu, (t >> 8) & 0xFFu)), 1u);
+}
+__device__ __forceinline__ uint32_t valid_bytes(int valid, int lane) {  // of the four keys of this lane's word
+  const int n = valid - (lane & 3) * 4;
+  return n >= 4 ? 0xFFFFFFFFu : n <= 0 ? 0u : (1u << (8 * n)) - 1u;
+}
+
+template <int kD>
+__global__ void __launch_bounds__(kThreads, 1)
+attn_fp8_kernel(DevBatch d, DevTcPlan tc, const uint16_t *__restrict__ q, Fp8Pools in, uint16_t *__restrict__ out, float *__restrict__ lse,
+                float scale_log2) {
+  using Sh = Shape<kD>;
+  constexpr int kTileBytes = Sh::kTileBytes, kGroupBytes = Sh::kGroupBytes, kStages = Sh::kStages, kHalves = Sh::kHalves;
+  extern __shared__ __align__(1024) unsigned char smem[];
+  if ((smem_u32(smem) & 1023u) != 0u) {  // the swizzled tiles need a 1024-byte aligned base
+    if (threadIdx.x == 0) {
+      d.status[0] = kDevBounds;
+      d.status[1] = 260;
+    }
+    return;
+  }
+  unsigned char *q_smem = smem;                    // two M-tiles
+  unsigned char *kv_smem = smem + 2 * kTileBytes;  // kStages tiles
+  Ctrl *ctrl = reinterpret_cast<Ctrl *>(kv_smem + kStages * kTileBytes);
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+
+  // the plan is uploaded by copies, so it may be read in front of the wait for the kernel before
+  const TcCtaHead *head = tc.heads + blockIdx.x;
+  const int piece0 = head->piece0, piece1 = head->piece1;
+  if (warp == 8 && lane < (int)(sizeof(TcCtaHead) / 16))
+    reinterpret_cast<uint4 *>(&ctrl->head)[lane] = __ldg(reinterpret_cast<const uint4 *>(head) + lane);
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < kStages; ++s) {
+      mbar_init(&ctrl->kv_full[s], 4);   // one arrival per converter warp
+      mbar_init(&ctrl->kv_empty[s], 2);  // one per MMA issuer
+    }
+    mbar_init(&ctrl->q_full, 256);
+    mbar_init(&ctrl->q_empty, 2);
+    for (int s = 0; s < 2; ++s) {
+      for (int h = 0; h < 2; ++h) {
+        mbar_init(&ctrl->s_full[s][h], 1);
+        mbar_init(&ctrl->p_full[s][h], 128);
+      }
+      mbar_init(&ctrl->o_done[s], 1);
+      mbar_init(&ctrl->drain[s], 1);
+    }
+    mbar_init(&ctrl->epi_done, 256);
+    mbar_init(&ctrl->xch, 128);
+    for (int i = 0; i < kInfos; ++i) mbar_init(&ctrl->info_full[i], 1);
+    ctrl->abort_flag = 0;
+    ctrl->wait_limit_ns = (uint64_t)tc.wait_limit_us * 1000ull;
+    fence_barrier_init();
+  }
+  if (warp == 12) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&ctrl->tmem_base)), "r"(512u)
+                 : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = *reinterpret_cast<volatile uint32_t *>(&ctrl->tmem_base);
+  asm volatile("griddepcontrol.wait;" ::: "memory");  // queries and cache may come from the kernel launched just before
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+
+  const int T = tc.tokens_per_mtile;
+
+  if (warp >= 12) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
+    if (warp < 14) {
+      // ======================= MMA issuer of stream s ====================================
+      // Both issuers walk every ring position of a piece in order: a position this stream uses is consumed by its MMAs (released by a
+      // tcgen05.commit), one it does not use is released with a plain arrive once it has landed.
+      const TcCtaHead *head = &ctrl->head;
+      const int s = __shfl_sync(0xFFFFFFFFu, warp, 0) - 12;
+      uint32_t ring_base = 0, waited = 0, p_cnt = 0, pc_idx = 0;
+      bool ok = true;
+      const uint32_t q_addr = smem_u32(q_smem), kv_addr = smem_u32(kv_smem);
+      const uint32_t tmem_u = __shfl_sync(0xFFFFFFFFu, tmem, 0);
+      const uint32_t s_tmem = tmem_u + s * 128, o_tmem = tmem_u + 256 + s * 128;
+      // Descriptors differ from a base only in the start-address field (units of 16 bytes).
+      const uint64_t qdesc0 = make_desc(q_addr, 16, 1024), kdesc0 = make_desc(kv_addr, 16, kGroupBytes),
+                     vdesc0 = make_desc(kv_addr, kAtomBytes, kGroupBytes);
+      auto issue_qk = [&](int m, uint32_t stage, int half) {  // S_s[half] = Q_m K^T over 64 of the 128 keys
+        const uint64_t a = qdesc0 + (uint64_t)(m * (kTileBytes >> 4)),
+                       b = kdesc0 + (uint64_t)(stage * (kTileBytes >> 4) + half * (8 * kGroupBytes >> 4));
+#pragma unroll
+        for (int h = 0; h < kHalves; ++h)
+#pragma unroll
+          for (int kk = 0; kk < 4; ++kk)
+            mma_ss(s_tmem + half * 64, a + (uint64_t)(h * (kHalfBytes >> 4) + kk * 2), b + (uint64_t)(h * (kAtomBytes >> 4) + kk * 2),
+                   kIdescQK, (h | kk) != 0);
+      };
+      auto issue_pv = [&](uint32_t stage, int half, bool acc) {  // O_s (+)= P_s[half] V over 64 of the 128 keys
+        const uint64_t b = vdesc0 + (uint64_t)(stage * (kTileBytes >> 4) + half * (8 * kGroupBytes >> 4));
+#pragma unroll
+        for (int k4 = 0; k4 < 4; ++k4)
+          mma_ts(o_tmem, s_tmem + half * 64 + k4 * 8, b + (uint64_t)(k4 * (2 * kGroupBytes >> 4)), kIdescPV<kD>, acc || k4 != 0);
+      };
+      for (int pc = piece0; pc < piece1 && ok; ++pc, ++pc_idx) {
+        const TcPiece pi = pc == piece0 ? head->first : tc.pieces[pc];
+        const int n = pi.tile_end - pi.tile_begin, mode = pi.n_mt;
+        const RingOrder ord(n, mode);
+        const int my_units = mode == 2 ? n : (n - s + 1) / 2;
+        const int m_tile = mode == 2 ? s : 0;
+        auto need = [&](uint32_t pos, int code) -> bool {  // waits, in ring order, until absolute ring position `pos` has landed
+          while (waited <= pos) {
+            if (!wait_bar(&ctrl->kv_full[waited % kStages], (waited / kStages) & 1u, ctrl, d.status, code)) return false;
+            if (waited < pos && elect_one()) mbar_arrive(&ctrl->kv_empty[waited % kStages]);
+            ++waited;
+          }
+          return true;
+        };
+        auto release = [&](uint32_t pos) { tc_commit(&ctrl->kv_empty[pos % kStages]); };  // arrives when the MMAs that read the stage retire
+        ok = wait_bar(&ctrl->q_full, pc_idx & 1u, ctrl, d.status, 270);
+        if (!ok) break;
+        if (my_units > 0) {
+          const uint32_t pos = ring_base + ord.pos_k(mode == 2 ? 0 : s);
+          ok = need(pos, 271);
+          if (!ok) break;
+          tc_fence_after();
+          if (elect_one()) {
+            issue_qk(m_tile, pos % kStages, 0);
+            tc_commit(&ctrl->s_full[s][0]);
+            issue_qk(m_tile, pos % kStages, 1);
+            tc_commit(&ctrl->s_full[s][1]);
+            release(pos);
+            if (my_units == 1) tc_commit(&ctrl->q_empty);  // last QK of the piece: this stream is done with the Q buffers
+          }
+          __syncwarp();
+        } else {
+          if (elect_one()) mbar_arrive(&ctrl->q_empty);
+          // nothing to issue in this piece: still observe the previous piece's epilogue phase, so that the parity
+          // wait of a later piece never finds this issuer two phases behind
+          if (pc_idx > 0) {
+            ok = wait_bar(&ctrl->epi_done, (pc_idx - 1) & 1u, ctrl, d.status, 278);
+            if (!ok) break;
+          }
+        }
+        for (int j = 0; j < my_units && ok; ++j) {
+          const int t = mode == 2 ? j : 2 * j + s;
+          const uint32_t pos_v = ring_base + ord.pos_v(t), sV = pos_v % kStages;
+          ok = need(pos_v, 272);
+          if (!ok) break;
+          const bool has_next = j + 1 < my_units;
+          uint32_t pos_k = 0;
+          if (has_next) {
+            pos_k = ring_base + ord.pos_k(mode == 2 ? j + 1 : 2 * (j + 1) + s);
+            ok = need(pos_k, 276);
+            if (!ok) break;
+          }
+          if (j == 0 && pc_idx > 0) {  // the epilogue of the previous piece has read O_0 and O_1
+            ok = wait_bar(&ctrl->epi_done, (pc_idx - 1) & 1u, ctrl, d.status, 273);
+            if (!ok) break;
+          }
+#pragma unroll 1
+          for (int half = 0; half < 2; ++half) {
+            // P of this half is in place: O += P V, then the buffer takes the scores of the next tile's half
+            ok = wait_bar(&ctrl->p_full[s][half], p_cnt & 1u, ctrl, d.status, 274 + s);
+            if (!ok) break;
+            tc_fence_after();
+            if (elect_one()) {
+              issue_pv(sV, half, (j | half) != 0);
+              tc_commit(&ctrl->o_done[s]);
+              if (half == 1) release(pos_v);
+              if (has_next) {
+                issue_qk(m_tile, pos_k % kStages, half);
+                tc_commit(&ctrl->s_full[s][half]);
+                if (half == 1) {
+                  release(pos_k);
+                  if (j + 2 == my_units) tc_commit(&ctrl->q_empty);  // last QK of the piece
+                }
+              }
+            }
+            __syncwarp();
+          }
+          ++p_cnt;
+        }
+        if (!ok) break;
+        ring_base += 2u * (uint32_t)n;
+        if (waited < ring_base) {  // positions of the piece this stream never touched (the tail of the other stream's tiles)
+          ok = need(ring_base - 1, 277);
+          if (!ok) break;
+          if (elect_one()) mbar_arrive(&ctrl->kv_empty[(ring_base - 1) % kStages]);
+        }
+      }
+      if (!ok && elect_one()) {
+        // let every MMA already issued retire before tensor memory is released (a commit covers what its own thread issued)
+        tc_commit(&ctrl->drain[s]);
+        const uint64_t t0 = global_ns();
+        while (!mbar_try_wait(&ctrl->drain[s], 0))
+          if (global_ns() - t0 > kDrainLimitNs) break;
+      }
+      __syncwarp();
+    }
+  } else if (warp >= 8) {
+    // ======================= converters ==================================================
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 120;");
+    const TcCtaHead *head = &ctrl->head;
+    constexpr int kCols = Sh::kCols, kGroups = Sh::kGroups, kRounds = Sh::kRounds, kAhead = Sh::kAhead;
+    const int ct = threadIdx.x - 256, col = ct % kCols, grp = ct / kCols;  // 16 channels of keys (round * kGroups + grp) * 4 .. + 3
+    // Both channel halves of a key (or, with head size 64, keys four apart) have their 16-byte units at the same places of the banks: half of the
+    // lanes store their two units the other way round.
+    const int first = kD == 128 ? col >> 2 : grp & 1;
+    uint32_t ring = 0, tiles = 0;  // ring positions and tiles of K so far
+    bool ok = true;
+    for (int pc = piece0; pc < piece1 && ok; ++pc) {
+      const TcPiece pi = pc == piece0 ? head->first : tc.pieces[pc];
+      const TcReq rq = pc == piece0 ? head->first_req : tc.reqs[pi.req];
+      const int n = pi.tile_end - pi.tile_begin, n_pos = 2 * n;
+      const RingOrder ord(n, pi.n_mt);
+      const TcPage *pages = tc.pages + rq.page_off + pi.tile_begin * kPagesPerTile + (lane >> 2);  // of this lane's word
+      auto page_at = [&](int i) -> TcPage {
+        bool is_v;
+        const int t = ord.step(min(i, n_pos - 1), is_v);
+        const int2 w = __ldg(reinterpret_cast<const int2 *>(pages + t * kPagesPerTile));
+        return TcPage{w.x, (uint32_t)w.y};
+      };
+      auto fetch = [&](Fetched<kD> &f, int i, TcPage pg) {  // asks for the tile of position i
+        bool is_v;
+        ord.step(i, is_v);
+        f.valid = (int)(pg.meta & 31u);
+        if (f.valid > 0 && (pg.page < 0 || pg.page >= d.n_pool_pages)) {  // never fetch outside the pool
+          d.status[0] = kDevBounds;
+          d.status[1] = 200;
+          pg.page = 0;
+        }
+        const int32_t row = (pg.page * d.n_kv_heads + pi.kv_head) * kPage;  // rows of the pools are numbered within 32 bits (tc_plan_structure)
+        f.word = f.v_word = 0u;
+        if (f.valid > 0) {
+          f.word = __ldg(reinterpret_cast<const uint32_t *>((is_v ? in.v_scale : in.k_scale) + row) + (lane & 3));
+          if (!is_v) f.v_word = __ldg(reinterpret_cast<const uint32_t *>(in.v_scale + row) + (lane & 3));
+        }
+        const uint8_t *pool = is_v ? in.v : in.k;
+#pragma unroll
+        for (int u = 0; u < kRounds; ++u) {
+          const int from = ((u * kGroups + grp) >> 2) * 4;  // a lane whose word lies in the page of this thread's keys
+          const int64_t at = __shfl_sync(0xFFFFFFFFu, row, from) + (grp & 3) * 4;
+          const bool there = __shfl_sync(0xFFFFFFFFu, f.valid, from) > 0;
+#pragma unroll
+          for (int j = 0; j < 4; ++j) f.codes[u * 4 + j] = there ? ld_codes(pool + (at + j) * kD + col * 16) : make_uint4(0, 0, 0, 0);
+        }
+      };
+      auto convert = [&](Fetched<kD> &f, int i) -> bool {  // the tile of position i into its stage
+        bool is_v;
+        const int t = ord.step(i, is_v);
+        const uint32_t live = valid_bytes(f.valid, lane);
+        const uint32_t bytes = f.word & live;
+        const int ref = tile_ref(bytes);
+        if (!is_v) {
+          const uint32_t v_bytes = f.v_word & live, nan = __vcmpeq4(v_bytes, 0xFFFFFFFFu);
+          const int v_ref = tile_ref(v_bytes);
+          const bool any = __any_sync(0xFFFFFFFFu, nan != 0u);
+          if (warp == 8) {
+            const uint32_t at = (tiles + (uint32_t)t) % kInfos;
+            if (any) ctrl->v_nan[at][lane] = (uint8_t)((nan & 1u) | ((nan >> 7) & 2u) | ((nan >> 14) & 4u) | ((nan >> 21) & 8u));
+            __syncwarp();
+            if (lane == 0) {
+              ctrl->info[at] = Info{ref, v_ref, any ? 1 : 0};
+              mbar_arrive(&ctrl->info_full[at]);
+            }
+          }
+        }
+        const uint32_t stage = ring % kStages;
+        if (!wait_bar(&ctrl->kv_empty[stage], ((ring / kStages) & 1u) ^ 1u, ctrl, d.status, 210)) return false;
+        const bool whole = pi.tile_begin + t < rq.n_dense_tiles;
+        const uint32_t tile = smem_u32(kv_smem) + stage * kTileBytes + (kD == 128 ? (col >> 2) * kAtomBytes : 0);
+#pragma unroll
+        for (int u = 0; u < kRounds; ++u) {
+          const int key4 = u * kGroups + grp;  // four keys
+          const uint32_t b4 = __shfl_sync(0xFFFFFFFFu, bytes, key4);
+          uint32_t l4 = 0xFFFFFFFFu;
+          if (!whole) l4 = __shfl_sync(0xFFFFFFFFu, live, key4);
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            const uint32_t b = (b4 >> (8 * j)) & 0xFFu;
+            float by = __uint_as_float((uint32_t)max((int)b - ref + 127, 0) << 23);
+            if (b == kFp8NanScale) by = is_v ? 0.f : __uint_as_float(0x7FC00000u);
+            const uint32_t by2 = pack_f16(by, by);
+            uint4 c = f.codes[u * 4 + j];
+            if (!whole && ((l4 >> (8 * j)) & 1u) == 0u) c = make_uint4(0, 0, 0, 0);
+            const uint32_t lo0 = mul_f16x2(fp8_half2(c.x & 0xFFFFu), by2), lo1 = mul_f16x2(fp8_half2(c.x >> 16), by2);
+            const uint32_t lo2 = mul_f16x2(fp8_half2(c.y & 0xFFFFu), by2), lo3 = mul_f16x2(fp8_half2(c.y >> 16), by2);
+            const uint32_t hi0 = mul_f16x2(fp8_half2(c.z & 0xFFFFu), by2), hi1 = mul_f16x2(fp8_half2(c.z >> 16), by2);
+            const uint32_t hi2 = mul_f16x2(fp8_half2(c.w & 0xFFFFu), by2), hi3 = mul_f16x2(fp8_half2(c.w >> 16), by2);
+            const int key = key4 * 4 + j, r = key & 7;
+            const uint32_t line = tile + (key >> 3) * kGroupBytes + r * 128;
+            const uint32_t a0 = line + ((((col & 3) * 2) ^ r) << 4), a1 = line + ((((col & 3) * 2 + 1) ^ r) << 4);
+            if (first) {
+              st_shared(a1, hi0, hi1, hi2, hi3);
+              st_shared(a0, lo0, lo1, lo2, lo3);
+            } else {
+              st_shared(a0, lo0, lo1, lo2, lo3);
+              st_shared(a1, hi0, hi1, hi2, hi3);
+            }
+          }
+        }
+        fence_proxy_async();
+        __syncwarp();
+        // (the test hook of lr_plan_debug_set_phantom_bytes: a stage that is never full)
+        if (lane == 0 && !(tc.phantom_tx_bytes != 0u && blockIdx.x == 0 && ring == 0)) mbar_arrive(&ctrl->kv_full[stage]);
+        ++ring;
+        return true;
+      };
+      Fetched<kD> f[kAhead];
+      TcPage pg[kAhead + 1];
+#pragma unroll
+      for (int a = 0; a <= kAhead; ++a) pg[a] = page_at(a);
+#pragma unroll
+      for (int a = 0; a < kAhead; ++a)
+        if (a < n_pos) fetch(f[a], a, pg[a]);
+      TcPage next = pg[kAhead];
+      for (int i0 = 0; i0 < n_pos && ok; i0 += kAhead) {
+#pragma unroll
+        for (int a = 0; a < kAhead; ++a) {
+          const int i = i0 + a;
+          if (i < n_pos && ok) {
+            ok = convert(f[a], i);
+            if (ok && i + kAhead < n_pos) {
+              fetch(f[a], i + kAhead, next);
+              next = page_at(i + kAhead + 1);
+            }
+          }
+        }
+      }
+      tiles += (uint32_t)n;
+    }
+  } else {
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 168;");
+    // ======================= softmax warpgroups ======================================
+    const int s = warp >> 2;        // stream
+    const int quarter = warp & 3;   // tensor-memory lane quarter this warp may access
+    const int r = quarter * 32 + lane;  // row within the M-tile
+    const uint32_t lane_base = tmem + ((uint32_t)(quarter * 32) << 16);
+    const uint32_t s_addr = lane_base + s * 128, o_addr = lane_base + 256 + s * 128;
+    uint32_t s_cnt = 0, o_cnt = 0;  // tiles / half-units of this stream so far
+    uint32_t x_cnt = 0;             // pieces so far in which the two streams were combined
+    uint32_t tiles = 0;             // tiles of both streams so far
+    bool ok = true;
+    for (int pc = piece0; pc < piece1; ++pc) {
+      const TcPiece pi = pc == piece0 ? head->first : tc.pieces[pc];
+      const TcReq rq = pc == piece0 ? head->first_req : tc.reqs[pi.req];
+      const int n = pi.tile_end - pi.tile_begin, mode = pi.n_mt;
+      const int my_units = mode == 2 ? n : (n - s + 1) / 2;
+      const RowInfo ri = row_info(d, tc, rq, T, mode == 2 ? pi.mtile0 + s : pi.mtile0, r, pi.kv_head);
+      float sc_row = 0.f;
+      if (ok) {
+        // the queries, once the products of the piece before no longer read the buffers; with one M-tile each stream stores its part
+        ok = wait_bar(&ctrl->q_empty, ((uint32_t)(pc - piece0) & 1u) ^ 1u, ctrl, d.status, 245);
+        if (ok) {
+          const int h0 = mode == 2 || kHalves == 2 ? (mode == 2 ? 0 : s) : 0, h1 = mode == 2 ? kHalves : kHalves == 2 ? s + 1 : 1 - s;
+          sc_row = scale_log2 * pow2(convert_q<kD>(q, ri.q_index, smem_u32(q_smem) + (mode == 2 ? s : 0) * kTileBytes, r, h0, h1));
+          fence_proxy_async();
+          mbar_arrive(&ctrl->q_full);
+        }
+      }
+      if (ok && my_units > 0) {
+        float m_used = -INFINITY, l = 0.f;
+        int base = 0;
+        bool s_ready = false, nan_v = false;
+        // O *= alpha.  The PV product of the previous half-unit must have retired first; the one before
+        // it has (its commit precedes the s_full this thread has just seen), so o_done has completed done_needed or
+        // done_needed - 1 phases and the parity says which, whether or not this thread has looked at the earlier ones.
+        auto rescale_o = [&](float alpha, uint32_t done_needed) -> bool {
+          if (!wait_bar(&ctrl->o_done[s], (done_needed - 1) & 1u, ctrl, d.status, 235 + s)) return false;
+          tc_fence_after();
+#pragma unroll
+          for (int ch = 0; ch < kD / 32; ++ch) {
+            uint32_t o[32];
+            tmem_ld32(o_addr + ch * 32, o);
+            tc_wait_ld();
+#pragma unroll
+            for (int c = 0; c < 32; ++c) o[c] = __float_as_uint(bits_f(o[c]) * alpha);
+            tmem_st32(o_addr + ch * 32, o);
+          }
+          tc_wait_st();
+          return true;
+        };
+        // A warp whose 32 rows are all padding only keeps the barriers' counts: what it leaves as weights multiplies into rows
+        // of O that nobody reads.
+        const bool idle = __all_sync(0xFFFFFFFFu, ri.q_index < 0);
+        if (idle) {
+          for (int u = 0; u < 2 * my_units && ok; ++u) {
+            ok = wait_bar(&ctrl->s_full[s][u & 1], (s_cnt + (uint32_t)(u >> 1)) & 1u, ctrl, d.status, 230 + s);
+            if (ok && u + 1 == 2 * my_units) ok = wait_bar(&ctrl->o_done[s], (o_cnt + (uint32_t)u - 1) & 1u, ctrl, d.status, 237 + s);
+            if (ok) mbar_arrive(&ctrl->p_full[s][u & 1]);
+          }
+          s_cnt += (uint32_t)my_units;
+        }
+        for (int j = 0; j < my_units && ok && !idle; ++j) {
+          const int local = mode == 2 ? j : 2 * j + s, t = pi.tile_begin + local;
+          const uint32_t at = (tiles + (uint32_t)local) % kInfos;
+          const bool masked = t >= rq.n_dense_tiles;
+          int n_ok[kPagesPerTile];
+          if (masked) {
+            const uint4 *mp = reinterpret_cast<const uint4 *>(tc.pages + rq.page_off + t * kPagesPerTile);
+#pragma unroll
+            for (int jj = 0; jj < 4; ++jj) {
+              const uint4 w = __ldg(mp + jj);
+              n_ok[2 * jj] = page_n_ok(w.y, ri);
+              n_ok[2 * jj + 1] = page_n_ok(w.w, ri);
+            }
+          }
+          if (!s_ready) {
+            ok = wait_bar(&ctrl->info_full[at], ((tiles + (uint32_t)local) / kInfos) & 1u, ctrl, d.status, 248) &&
+                 wait_bar(&ctrl->s_full[s][0], s_cnt & 1u, ctrl, d.status, 230 + s);
+            if (!ok) break;
+          }
+          const Info info = ctrl->info[at];
+          const float sc = sc_row * pow2(info.k_ref - 127);
+          if (info.v_nan) nan_v = sees_nan(ctrl->v_nan[at], masked ? tc.pages + rq.page_off + t * kPagesPerTile : nullptr, ri) || nan_v;
+          if (j == 0) {
+            base = info.v_ref;
+          } else if (info.v_ref > base + kRise) {
+            ok = rescale_o(pow2(base - info.v_ref), o_cnt + (uint32_t)(2 * j));
+            if (!ok) break;
+            base = info.v_ref;
+          }
+          const int off = info.v_ref - base;
+          const float bias = (float)off + kHead;
+#pragma unroll 1  // one copy of the sweep: the unrolled pair is slower (instruction fetch)
+          for (int half = 0; half < 2; ++half) {
+            const uint32_t sh_addr = s_addr + half * 64;
+            const uint32_t g = o_cnt + (uint32_t)(2 * j + half);  // half-units of this stream before this one
+            const bool first = (j | half) == 0;
+            if (half == 1 && !s_ready) {
+              ok = wait_bar(&ctrl->s_full[s][1], s_cnt & 1u, ctrl, d.status, 230 + s);
+              if (!ok) break;
+            }
+            tc_fence_after();
+            uint32_t v[64];
+            tmem_ld64(sh_addr, v);
+            tc_wait_ld();
+            // the scores after these (and what is known of their tile) are looked for under the exponentials: a test costs over 100 cycles even
+            // when it succeeds
+            uint32_t next_ready;
+            if (half == 0) {
+              next_ready = mbar_test_wait(&ctrl->s_full[s][1], s_cnt & 1u);
+            } else {
+              const uint32_t next = tiles + (uint32_t)local + (mode == 2 ? 1u : 2u);
+              next_ready = mbar_test_wait2(&ctrl->s_full[s][0], (s_cnt + 1u) & 1u, &ctrl->info_full[next % kInfos], (next / kInfos) & 1u) == 3u;
+            }
+            if (masked) mask_half(v, n_ok + 4 * half);
+            float sum = 0.f, mx, raw;
+            // Fast path: exponentials against the running reference exponent; the maximum of the 64 scores is computed beside them and only
+            // checked afterwards.
+            bool fast = __all_sync(0xFFFFFFFFu, m_used > -INFINITY);
+            if (fast) {
+              sum = exp_half<true>(v, sh_addr, sc, bias - m_used, raw);
+              mx = raw * sc;
+              if (__any_sync(0xFFFFFFFFu, mx > m_used + kGrow)) fast = false;  // beyond what a half holds: once more
+            } else {
+              mx = max_half(v) * sc;
+            }
+            if (!fast) {
+              const bool grow = mx > m_used + kGrow || m_used == -INFINITY;
+              const float alpha = grow && m_used > -INFINITY ? ex2(m_used - mx) : 1.0f;
+              if (grow) {
+                l *= alpha;
+                m_used = mx;
+              }
+              if (!first && __any_sync(0xFFFFFFFFu, alpha != 1.0f)) {
+                ok = rescale_o(alpha, g);
+                if (!ok) break;
+              }
+              tc_wait_st();
+              sum = exp_half<false>(v, sh_addr, sc, (m_used == -INFINITY) ? 0.f : bias - m_used, raw);
+            }
+            if (off >= -kApart) {
+              l = fmaf(sum, pow2(-off - (int)kHead), l);
+            } else {  // (the scores themselves are gone from tensor memory, but not from the registers)
+              float apart = 0.f;
+#pragma unroll
+              for (int i = 0; i < 64; ++i) apart += ex2(fmaf(bits_f(v[i]), sc, m_used == -INFINITY ? 0.f : -m_used));
+              l += apart;
+            }
+            tc_wait_st();
+            tc_fence_before();
+            s_ready = __all_sync(0xFFFFFFFFu, next_ready) != 0;
+            // The wait at the end must not find o_done two phases back (one parity for both): the last arrive comes
+            // after the product before has been seen to retire.
+            if (half == 1 && j + 1 == my_units) {
+              ok = wait_bar(&ctrl->o_done[s], (g - 1) & 1u, ctrl, d.status, 237 + s);
+              if (!ok) break;
+            }
+            mbar_arrive(&ctrl->p_full[s][half]);
+          }
+          ++s_cnt;
+        }
+        if (ok) {
+          // epilogue: wait for the last PV of this stream, then normalise and store
+          o_cnt += 2u * (uint32_t)my_units;
+          ok = wait_bar(&ctrl->o_done[s], (o_cnt - 1) & 1u, ctrl, d.status, 240 + s);
+        }
+        // what the accumulator's numbers are worth; NaN for a row that sees a row of V that is
+        const float unit = nan_v ? __uint_as_float(0x7FC00000u) : exp2f((float)(base - 127) - kHead);
+        // The two streams of a one-M-tile piece hold partial results of the same rows (even and odd tiles).
+        // Stream 1 publishes its sums; stream 0 reads them and stream 1's accumulator -- the same tensor-memory
+        // lanes, so the thread of row r can load both -- and writes one combined result.
+        const bool pair = mode == 1 && n >= 2;
+        float m_out = m_used, l_out = l, self = unit, other = 0.0f;
+        bool writer = true, other_live = false;
+        if (ok && pair) {
+          if (s == 1) {
+            ctrl->xch_m[r] = m_used;
+            ctrl->xch_l[r] = l;
+            ctrl->xch_unit[r] = unit;
+            tc_fence_before();
+            mbar_arrive(&ctrl->xch);
+            writer = false;
+          } else {
+            ok = wait_bar(&ctrl->xch, x_cnt & 1u, ctrl, d.status, 242);
+            if (ok) {
+              tc_fence_after();
+              const float om = ctrl->xch_m[r], ol = ctrl->xch_l[r];
+              other_live = ol != 0.f;  // a stream that saw no key of the row has a sum of 0
+              m_out = fmaxf(m_used, om);
+              const float w_self = l != 0.f ? ex2(m_used - m_out) : 0.f, w_other = other_live ? ex2(om - m_out) : 0.f;
+              self = l != 0.f ? unit * w_self : 0.f;
+              other = other_live ? ctrl->xch_unit[r] * w_other : 0.f;
+              l_out = w_self * l + w_other * ol;
+            }
+          }
+        }
+        if (pair) ++x_cnt;
+        if (ok && writer && !idle) {
+          tc_fence_after();
+          store_rows<kD>(o_addr, lane_base + 256 + (1 - s) * 128, pi.slot[pair ? 0 : s], self, other, other_live, m_out, l_out, r, ri.q_index, out, lse,
+                         tc.partial_o, tc.partial_ml);
+          tc_fence_before();
+        }
+      }
+      // One arrival per thread and piece.  A stream with units in this piece cannot get here before the previous
+      // piece's phase is complete (its PV products were issued behind a wait for it); a stream with none must look
+      // itself, or its arrival would be counted into the previous phase while the other stream is still storing.
+      if (my_units == 0 && pc > piece0 && ok) ok = wait_bar(&ctrl->epi_done, (uint32_t)(pc - piece0 - 1) & 1u, ctrl, d.status, 243);
+      mbar_arrive(&ctrl->epi_done);
+      tiles += (uint32_t)n;
+    }
+  }
+
+  tc_fence_before();
+  __syncthreads();
+  if (warp == 12) {
+    tc_fence_after();
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512u) : "memory");
+  }
+}
+
+template <int kD, int kBatch>
+__global__ void __launch_bounds__(256, kMergeCtas<kBatch>)
+attn_fp8_merge_kernel(DevBatch d, DevTcPlan tc, uint16_t *__restrict__ out, float *__restrict__ lse) {
+  merge_cta<kD, kBatch>(d, tc, blockIdx.x, blockIdx.y, out, lse);
+}
+
+template <int kD>
+int launch(lr_plan *p, const uint16_t *q, const Fp8Pools &in, uint16_t *out, float *lse, float scale_log2, cudaStream_t s) {
+  const DevTcPlan &tc = p->tc;
+  p->ctx->launches++;
+  if (int rc = cuda_fail(launch_dependent(attn_fp8_kernel<kD>, dim3((unsigned)tc.n_cta), dim3(kThreads), kSmemBytes<kD>, s, p->dev, tc, q, in, out, lse,
+                                          scale_log2),
+                         "attn_fp8_kernel launch"))
+    return rc;
+  if (tc.n_targets == 0) return LR_OK;
+  p->ctx->launches++;  // the merge grid is set up while the attention grid drains
+  return cuda_fail(launch_dependent(tc.most_slots <= 4 ? attn_fp8_merge_kernel<kD, 4> : attn_fp8_merge_kernel<kD, 8>, dim3((unsigned)tc.n_targets, kD / 8),
+                                    dim3(256), 0, s, p->dev, tc, out, lse),
+                   "attn_fp8_merge_kernel launch");
+}
+
+}  // namespace
+
+int init_attn_fp8_kernel() {
+  if (int rc = cuda_fail(cudaFuncSetAttribute(attn_fp8_kernel<128>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemBytes<128>),
+                         "attn_fp8_kernel<128> shared-memory attribute"))
+    return rc;
+  return cuda_fail(cudaFuncSetAttribute(attn_fp8_kernel<64>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemBytes<64>),
+                   "attn_fp8_kernel<64> shared-memory attribute");
+}
+
+int launch_attn_fp8(lr_plan *p, const void *q, const lr_fp8_cache &c, void *out, float *lse, float scale, cudaStream_t s) {
+  const Fp8Pools in = {reinterpret_cast<const uint8_t *>(c.k_d), reinterpret_cast<const uint8_t *>(c.v_d), c.k_scale_d, c.v_scale_d};
+  return (p->dev.head_dim == 128 ? launch<128> : launch<64>)(p, reinterpret_cast<const uint16_t *>(q), in, reinterpret_cast<uint16_t *>(out), lse,
+                                                             scale * 1.4426950408889634f, s);
+}
+
+}  // namespace lr

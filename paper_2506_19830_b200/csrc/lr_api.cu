@@ -311,6 +311,7 @@ extern "C" int lr_create(lr_ctx **out, const lr_model *m, int device) {
   if (int rc = init_commit_kernel()) { delete c; return rc; }
   if (int rc = init_attn_tc_kernel()) { delete c; return rc; }
   if (int rc = init_attn_pair_kernel()) { delete c; return rc; }
+  if (int rc = init_attn_fp8_kernel()) { delete c; return rc; }
   if (int rc = init_accept_filter_kernels()) { delete c; return rc; }
   SideStream side;
   if (int rc = make_side(side)) { delete c; return rc; }
@@ -1074,8 +1075,14 @@ extern "C" int lr_verify_attention_fp8(lr_plan *p, const void *q, const lr_fp8_c
     set_error("lr_verify_attention_fp8: there is no CTA-pair kernel for an 8-bit cache");
     return LR_EUNSUPPORTED;
   }
+  const bool use_tc = p->attention_path == 2 || (p->attention_path == 0 && p->tc_ok);
+  if (use_tc && !p->tc_ok) {
+    set_error("lr_verify_attention_fp8: the tensor-core path does not support this shape");
+    return LR_EUNSUPPORTED;
+  }
   OnDevice on(p->ctx);
   if (on.rc != LR_OK) return on.rc;
+  if (use_tc) return launch_attn_fp8(p, q, *cache, out, lse, scale, reinterpret_cast<cudaStream_t>(stream));
   return launch_attn_fp8_generic(p, q, *cache, out, lse, scale, reinterpret_cast<cudaStream_t>(stream));
 }
 

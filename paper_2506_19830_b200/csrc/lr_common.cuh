@@ -333,6 +333,7 @@ int cuda_fail(cudaError_t e, const char *what);
 int init_commit_kernel();
 int init_attn_tc_kernel();
 int init_attn_pair_kernel();
+int init_attn_fp8_kernel();
 int init_accept_filter_kernels();
 
 int launch_attn_pair(lr_plan *p, const void *q, const void *k, const void *v, void *out, float *lse, float scale,
@@ -374,6 +375,7 @@ int launch_compact(lr_plan *p, const int32_t *keep_off, const int32_t *keep_page
 // the 8-bit cache
 int launch_fp8_move(lr_ctx *ctx, const lr_fp8_cache &c, bool write, void *k, int64_t k_stride, void *v, int64_t v_stride, const int64_t *slots,
                     int32_t n_tokens, int32_t *status, cudaStream_t s);
+int launch_attn_fp8(lr_plan *p, const void *q, const lr_fp8_cache &c, void *out, float *lse, float scale, cudaStream_t s);
 int launch_attn_fp8_generic(lr_plan *p, const void *q, const lr_fp8_cache &c, void *out, float *lse, float scale, cudaStream_t s);
 int launch_compact_fp8(lr_plan *p, const int32_t *keep_off, const int32_t *keep_pages, const int32_t *keep_valid, const lr_fp8_cache &c,
                        int32_t *new_len, int32_t *n_pages_kept, cudaStream_t s);

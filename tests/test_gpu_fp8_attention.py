@@ -14,7 +14,7 @@ from paper_2506_19830_b200 import runner as R
 
 pytestmark = pytest.mark.gpu
 DEV = "cuda:0"
-PATHS = [B.PATH_GENERIC]
+PATHS = [B.PATH_GENERIC, B.PATH_TENSOR_CORE]
 
 
 def stored(w, seed=0):
