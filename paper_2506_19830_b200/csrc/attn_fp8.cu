@@ -16,7 +16,7 @@
 // The weights are f16 as well, 2^6 above the row's reference and at most 2^15: 11 bits instead of bf16's 8, nothing lost above 2^-20 of the
 // largest, and a row whose scores grow by more than 2^6 does its half-tile again.
 //
-// One CTA = 16 warps in four warpgroups, registers moved with setmaxnreg (168 x 256 + 120 x 128 + 56 x 128 <= 128 x 512):
+// One CTA = 16 warps in four warpgroups, registers moved with setmaxnreg (176 x 256 + 80 x 128 + 72 x 128 <= 128 x 512):
 //   warps 8-11  converters.  No staging: a thread loads its codes (16 bytes of eight keys of a tile; four with head size 64) straight into registers,
 //               two tiles (four) ahead -- 32 KB in flight an SM -- turns them into halves and stores them as the swizzled operand.  Through
 //               shared memory they would cross it twice more, and it is as busy as the tensor cores: 32 KB of a tile written and
@@ -40,7 +40,7 @@ namespace {
 
 constexpr int kHalfBytes = 16384;  // 128 rows or keys x 64 channels
 constexpr int kAtomBytes = 1024;   // 8 keys x 64 channels, one 128-byte-swizzle atom
-constexpr int kMaxStages = 10;
+constexpr int kMaxStages = 8;
 constexpr int kThreads = 512;
 constexpr int kInfos = 16;         // tiles whose scales are published ahead of their products; more than the ring can hold
 constexpr float kGrow = 6.0f;      // log2: how far the scores of a row may rise above its reference exponent
@@ -54,12 +54,14 @@ struct Shape {
   static constexpr int kHalves = kD / 64;
   static constexpr int kTileBytes = kHalves * kHalfBytes;   // as in attn_tc.cu
   static constexpr int kGroupBytes = kHalves * kAtomBytes;
-  static constexpr int kStages = kD == 128 ? 5 : 10;
+  static constexpr int kStages = kD == 128 ? 4 : 8;
   static constexpr int kCols = kD / 16;                     // converter threads side by side in a row, 16 channels each
   static constexpr int kGroups = 128 / kCols;               // groups of four keys that the converters have at a time
   static constexpr int kRounds = 32 / kGroups;              // ... and how many times for a tile
   static constexpr int kChunks = 4 * kRounds;               // 16-byte chunks of a tile that a thread has
-  static constexpr int kAhead = 16 / kChunks;               // tiles that it has in registers
+  static constexpr int kCodeBytes = 128 * kD;               // a tile as it comes
+  static constexpr int kSlots = kD == 128 ? 2 : 6;          // of them on their way
+  static constexpr int kDeepSlots = kD == 128 ? 4 : 6;      // ... where no piece of the CTA has a second M-tile: its place in Q's buffer
 };
 
 struct Info {  // of a tile: the largest scale bytes of its keys; whether some visible row of V stands for NaN
@@ -84,7 +86,7 @@ struct __align__(16) Ctrl {
 constexpr int kCtrlBytes = 3 << 10;
 static_assert(sizeof(Ctrl) <= kCtrlBytes, "Ctrl must fit behind the tiles");
 template <int kD>
-constexpr int kSmemBytes = (2 + Shape<kD>::kStages) * Shape<kD>::kTileBytes + kCtrlBytes;  // Q, the ring; the base must be 1024-aligned
+constexpr int kSmemBytes = (2 + Shape<kD>::kStages) * Shape<kD>::kTileBytes + Shape<kD>::kSlots * Shape<kD>::kCodeBytes + kCtrlBytes;  // the base must be 1024-aligned
 static_assert(kSmemBytes<64> <= 227 * 1024 && kSmemBytes<128> <= 227 * 1024, "shared memory per CTA");
 
 // Instruction descriptors: D fp32, A and B f16 (format 0), M = 128; QK: N = 64 keys, both operands K-major; PV: N = head size, B N-major.
@@ -98,15 +100,24 @@ __device__ __forceinline__ uint32_t pack_f16(float lo, float hi) {
   asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
   return r;
 }
-__device__ __forceinline__ uint32_t mul_f16x2(uint32_t a, uint32_t b) {
-  uint32_t r;
-  asm("mul.rn.f16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
-  return r;
-}
 __device__ __forceinline__ float pow2(int e) { return __uint_as_float((uint32_t)(min(max(e, -126), 127) + 127) << 23); }
-__device__ __forceinline__ uint4 ld_codes(const uint8_t *p) {
+__device__ __forceinline__ void copy_codes(uint32_t dst, const uint8_t *src) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
+}
+__device__ __forceinline__ uint4 ld_shared(uint32_t addr) {
   uint4 v;
-  asm volatile("ld.global.nc.L1::no_allocate.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p));
+  asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(addr) : "memory");
+  return v;
+}
+// (asm so that these stay where they are written, tiles ahead of their use)
+__device__ __forceinline__ uint32_t ld_word(const uint8_t *p) {
+  uint32_t v;
+  asm volatile("ld.global.nc.u32 %0, [%1];" : "=r"(v) : "l"(p));
+  return v;
+}
+__device__ __forceinline__ int2 ld_pair(const void *p) {
+  int2 v;
+  asm volatile("ld.global.nc.v2.s32 {%0, %1}, [%2];" : "=r"(v.x), "=r"(v.y) : "l"(p));
   return v;
 }
 __device__ __forceinline__ void st_shared(uint32_t addr, uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
@@ -240,22 +251,32 @@ struct Fp8Pools {
   const uint8_t *k, *v, *k_scale, *v_scale;
 };
 
-// What a converter thread has of one tile of K or V on its way.
-template <int kD>
-struct Fetched {
-  uint4 codes[Shape<kD>::kChunks];
+// What a converter lane knows of a tile of K or V.
+struct TileWords {
   uint32_t word, v_word;  // scale bytes of keys 4 lane .. 4 lane + 3; with a tile of K also V's
-  int32_t valid;          // tokens of the page those keys lie in
+  uint32_t meta;          // of the page those keys lie in
 };
 
+__device__ __forceinline__ uint32_t valid_bytes(int valid, int lane) {  // of the four keys of this lane's word
+  const int n = valid - (lane & 3) * 4;
+  return n >= 4 ? 0xFFFFFFFFu : n <= 0 ? 0u : (1u << (8 * n)) - 1u;
+}
 // the largest scale byte of the tile, of valid keys that do not stand for NaN; `bytes`: this lane's four, those of no valid token cleared
 __device__ __forceinline__ int tile_ref(uint32_t bytes) {
   const uint32_t w = bytes & ~__vcmpeq4(bytes, 0xFFFFFFFFu), t = __vmaxu4(w, w >> 16);
   return (int)max(__reduce_max_sync(0xFFFFFFFFu, max(t & 0xFFu, (t >> 8) & 0xFFu)), 1u);
 }
-__device__ __forceinline__ uint32_t valid_bytes(int valid, int lane) {  // of the four keys of this lane's word
-  const int n = valid - (lane & 3) * 4;
-  return n >= 4 ? 0xFFFFFFFFu : n <= 0 ? 0u : (1u << (8 * n)) - 1u;
+// 2^(byte - ref) of two keys, as halves; `nan`: what a byte of 255 gives
+__device__ __forceinline__ uint32_t factors(uint32_t b0, uint32_t b1, int ref, float nan) {
+  const float f0 = __uint_as_float((uint32_t)max((int)b0 - ref + 127, 0) << 23), f1 = __uint_as_float((uint32_t)max((int)b1 - ref + 127, 0) << 23);
+  return pack_f16(b0 == kFp8NanScale ? nan : f0, b1 == kFp8NanScale ? nan : f1);
+}
+// four codes times a key's factor, as four halves
+__device__ __forceinline__ void halves4(uint32_t c, uint32_t by, uint32_t &lo, uint32_t &hi) {
+  asm("{\n\t.reg .b16 a, b;\n\t.reg .b32 x, y;\n\tmov.b32 {a, b}, %2;\n\t"
+      "cvt.rn.f16x2.e4m3x2 x, a;\n\tcvt.rn.f16x2.e4m3x2 y, b;\n\tmul.rn.f16x2 %0, x, %3;\n\tmul.rn.f16x2 %1, y, %3;\n\t}"
+      : "=r"(lo), "=r"(hi)
+      : "r"(c), "r"(by));
 }
 
 template <int kD>
@@ -274,7 +295,8 @@ attn_fp8_kernel(DevBatch d, DevTcPlan tc, const uint16_t *__restrict__ q, Fp8Poo
   }
   unsigned char *q_smem = smem;                    // two M-tiles
   unsigned char *kv_smem = smem + 2 * kTileBytes;  // kStages tiles
-  Ctrl *ctrl = reinterpret_cast<Ctrl *>(kv_smem + kStages * kTileBytes);
+  unsigned char *code_smem = kv_smem + kStages * kTileBytes;  // kSlots tiles of codes
+  Ctrl *ctrl = reinterpret_cast<Ctrl *>(code_smem + Sh::kSlots * Sh::kCodeBytes);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
 
   // the plan is uploaded by copies, so it may be read in front of the wait for the kernel before
@@ -319,7 +341,7 @@ attn_fp8_kernel(DevBatch d, DevTcPlan tc, const uint16_t *__restrict__ q, Fp8Poo
   const int T = tc.tokens_per_mtile;
 
   if (warp >= 12) {
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
     if (warp < 14) {
       // ======================= MMA issuer of stream s ====================================
       // Both issuers walk every ring position of a piece in order: a position this stream uses is consumed by its MMAs (released by a
@@ -448,56 +470,87 @@ attn_fp8_kernel(DevBatch d, DevTcPlan tc, const uint16_t *__restrict__ q, Fp8Poo
     }
   } else if (warp >= 8) {
     // ======================= converters ==================================================
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 120;");
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 80;");
     const TcCtaHead *head = &ctrl->head;
-    constexpr int kCols = Sh::kCols, kGroups = Sh::kGroups, kRounds = Sh::kRounds, kAhead = Sh::kAhead;
+    constexpr int kCols = Sh::kCols, kGroups = Sh::kGroups, kRounds = Sh::kRounds;
     const int ct = threadIdx.x - 256, col = ct % kCols, grp = ct / kCols;  // 16 channels of keys (round * kGroups + grp) * 4 .. + 3
-    // Both channel halves of a key (or, with head size 64, keys four apart) have their 16-byte units at the same places of the banks: half of the
-    // lanes store their two units the other way round.
-    const int first = kD == 128 ? col >> 2 : grp & 1;
+    // Eight neighbouring lanes store to two lines at a time whose 16-byte units lie in the same banks (both channel halves of a key, or with head size 64
+    // keys four apart); half of them take their four keys in the order 1, 0, 3, 2, which brings the units of the two lines apart.
+    const int odd = kD == 128 ? col >> 2 : grp & 1;
+    const uint32_t line0 = smem_u32(kv_smem) + (kD == 128 ? (col >> 2) * kAtomBytes : 0) + (grp >> 1) * kGroupBytes;
+    uint32_t off[4];  // of the first of the two units of each key
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const int r = (grp & 1) * 4 + (j ^ odd);
+      off[j] = line0 + r * 128 + ((((col & 3) * 2) ^ r) << 4);
+    }
+    const int32_t k_off = (grp & 3) * 4 * kD + col * 16;  // within the page of the keys
+    // This thread's part of the slots: it alone copies and reads them, so that nothing but its own copies has to be waited for.
+    const uint32_t mine = smem_u32(code_smem) + ct * 16, mine_deep = smem_u32(q_smem) + kTileBytes + ct * 16;
+    auto slot_at = [&](int slot) -> uint32_t {
+      return slot < Sh::kSlots ? mine + slot * Sh::kCodeBytes : mine_deep + (slot - Sh::kSlots) * Sh::kCodeBytes;
+    };
+    bool deep = Sh::kDeepSlots > Sh::kSlots;
+    if constexpr (Sh::kDeepSlots > Sh::kSlots)
+      for (int pc = piece0; pc < piece1; ++pc) deep = deep && (pc == piece0 ? head->first.n_mt : tc.pieces[pc].n_mt) == 1;
+    const int ahead = deep ? Sh::kDeepSlots : Sh::kSlots;  // tiles on their way
     uint32_t ring = 0, tiles = 0;  // ring positions and tiles of K so far
     bool ok = true;
     for (int pc = piece0; pc < piece1 && ok; ++pc) {
       const TcPiece pi = pc == piece0 ? head->first : tc.pieces[pc];
       const TcReq rq = pc == piece0 ? head->first_req : tc.reqs[pi.req];
       const int n = pi.tile_end - pi.tile_begin, n_pos = 2 * n;
+      const int n_whole = rq.n_dense_tiles - pi.tile_begin;  // tiles of the piece without slots of no valid token
       const RingOrder ord(n, pi.n_mt);
       const TcPage *pages = tc.pages + rq.page_off + pi.tile_begin * kPagesPerTile + (lane >> 2);  // of this lane's word
-      auto page_at = [&](int i) -> TcPage {
+      auto page_at = [&](int i) -> int2 {
         bool is_v;
         const int t = ord.step(min(i, n_pos - 1), is_v);
-        const int2 w = __ldg(reinterpret_cast<const int2 *>(pages + t * kPagesPerTile));
-        return TcPage{w.x, (uint32_t)w.y};
+        return ld_pair(pages + t * kPagesPerTile);
       };
-      auto fetch = [&](Fetched<kD> &f, int i, TcPage pg) {  // asks for the tile of position i
-        bool is_v;
-        ord.step(i, is_v);
-        f.valid = (int)(pg.meta & 31u);
-        if (f.valid > 0 && (pg.page < 0 || pg.page >= d.n_pool_pages)) {  // never fetch outside the pool
+      auto row_of = [&](int32_t page) -> int32_t {  // the first row of a page; rows of the pools are numbered within 32 bits (tc_plan_structure)
+        if (page < 0 || page >= d.n_pool_pages) {  // never fetch outside the pool
           d.status[0] = kDevBounds;
           d.status[1] = 200;
-          pg.page = 0;
+          page = 0;
         }
-        const int32_t row = (pg.page * d.n_kv_heads + pi.kv_head) * kPage;  // rows of the pools are numbered within 32 bits (tc_plan_structure)
-        f.word = f.v_word = 0u;
-        if (f.valid > 0) {
-          f.word = __ldg(reinterpret_cast<const uint32_t *>((is_v ? in.v_scale : in.k_scale) + row) + (lane & 3));
-          if (!is_v) f.v_word = __ldg(reinterpret_cast<const uint32_t *>(in.v_scale + row) + (lane & 3));
+        return (page * d.n_kv_heads + pi.kv_head) * kPage;
+      };
+      auto words_at = [&](int i, int2 pg) -> TileWords {
+        bool is_v;
+        ord.step(min(i, n_pos - 1), is_v);
+        const int32_t row = row_of(pg.x);
+        TileWords w;
+        w.meta = (uint32_t)pg.y;
+        w.word = ld_word((is_v ? in.v_scale : in.k_scale) + row + (lane & 3) * 4);
+        w.v_word = is_v ? 0u : ld_word(in.v_scale + row + (lane & 3) * 4);
+        return w;
+      };
+      auto fetch = [&](int i, int slot, int2 pg) {  // asks for the codes of the tile of position i
+        bool is_v;
+        ord.step(i, is_v);
+        const int32_t row = row_of(pg.x);
+        if ((lane & 3) == 0) {  // its scale bytes are read a position ahead of their use, which is enough from L2
+          asm volatile("prefetch.global.L2 [%0];" ::"l"((is_v ? in.v_scale : in.k_scale) + row));
+          if (!is_v) asm volatile("prefetch.global.L2 [%0];" ::"l"(in.v_scale + row));
         }
-        const uint8_t *pool = is_v ? in.v : in.k;
+        const uint8_t *pool = (is_v ? in.v : in.k) + k_off;
+        const uint32_t to = slot_at(slot);
 #pragma unroll
         for (int u = 0; u < kRounds; ++u) {
-          const int from = ((u * kGroups + grp) >> 2) * 4;  // a lane whose word lies in the page of this thread's keys
-          const int64_t at = __shfl_sync(0xFFFFFFFFu, row, from) + (grp & 3) * 4;
-          const bool there = __shfl_sync(0xFFFFFFFFu, f.valid, from) > 0;
-#pragma unroll
-          for (int j = 0; j < 4; ++j) f.codes[u * 4 + j] = there ? ld_codes(pool + (at + j) * kD + col * 16) : make_uint4(0, 0, 0, 0);
+          // (a lane whose word lies in the page of this thread's keys; an absent page of the last tile reads page 0 and is cleared below)
+          const uint8_t *at = pool + (int64_t)__shfl_sync(0xFFFFFFFFu, row, ((u * kGroups + grp) >> 2) * 4) * kD;
+          const uint8_t *even = at + odd * kD, *other = at - odd * kD;
+          copy_codes(to + (u * 4) * 2048, even);
+          copy_codes(to + (u * 4 + 1) * 2048, other + kD);
+          copy_codes(to + (u * 4 + 2) * 2048, even + 2 * kD);
+          copy_codes(to + (u * 4 + 3) * 2048, other + 3 * kD);
         }
       };
-      auto convert = [&](Fetched<kD> &f, int i) -> bool {  // the tile of position i into its stage
+      auto convert = [&](TileWords f, int i, int slot) -> bool {  // the tile of position i into its stage
         bool is_v;
         const int t = ord.step(i, is_v);
-        const uint32_t live = valid_bytes(f.valid, lane);
+        const uint32_t live = valid_bytes((int)(f.meta & 31u), lane);
         const uint32_t bytes = f.word & live;
         const int ref = tile_ref(bytes);
         if (!is_v) {
@@ -514,38 +567,36 @@ attn_fp8_kernel(DevBatch d, DevTcPlan tc, const uint16_t *__restrict__ q, Fp8Poo
             }
           }
         }
+        // the factors of this lane's four keys, which other lanes ask for
+        const float nan_is = is_v ? 0.f : __uint_as_float(0x7FC00000u);
+        const uint32_t f01 = factors(bytes & 0xFFu, (bytes >> 8) & 0xFFu, ref, nan_is), f23 = factors((bytes >> 16) & 0xFFu, bytes >> 24, ref, nan_is);
         const uint32_t stage = ring % kStages;
         if (!wait_bar(&ctrl->kv_empty[stage], ((ring / kStages) & 1u) ^ 1u, ctrl, d.status, 210)) return false;
-        const bool whole = pi.tile_begin + t < rq.n_dense_tiles;
-        const uint32_t tile = smem_u32(kv_smem) + stage * kTileBytes + (kD == 128 ? (col >> 2) * kAtomBytes : 0);
+        const uint32_t to = stage * kTileBytes, from = slot_at(slot);
+        const bool clear = is_v && t >= n_whole;  // (K's scores of slots that hold no valid token are never looked at)
 #pragma unroll
         for (int u = 0; u < kRounds; ++u) {
-          const int key4 = u * kGroups + grp;  // four keys
-          const uint32_t b4 = __shfl_sync(0xFFFFFFFFu, bytes, key4);
-          uint32_t l4 = 0xFFFFFFFFu;
-          if (!whole) l4 = __shfl_sync(0xFFFFFFFFu, live, key4);
+          uint4 c[4];
+#pragma unroll
+          for (int j = 0; j < 4; ++j) c[j] = ld_shared(from + (u * 4 + j) * 2048);
+          if (clear) {
+            const uint32_t l4 = __shfl_sync(0xFFFFFFFFu, live, u * kGroups + grp);
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+              if (((l4 >> (8 * (j ^ odd))) & 1u) == 0u) c[j] = make_uint4(0, 0, 0, 0);
+          }
+          const uint32_t by[2] = {__shfl_sync(0xFFFFFFFFu, f01, u * kGroups + grp), __shfl_sync(0xFFFFFFFFu, f23, u * kGroups + grp)};
 #pragma unroll
           for (int j = 0; j < 4; ++j) {
-            const uint32_t b = (b4 >> (8 * j)) & 0xFFu;
-            float by = __uint_as_float((uint32_t)max((int)b - ref + 127, 0) << 23);
-            if (b == kFp8NanScale) by = is_v ? 0.f : __uint_as_float(0x7FC00000u);
-            const uint32_t by2 = pack_f16(by, by);
-            uint4 c = f.codes[u * 4 + j];
-            if (!whole && ((l4 >> (8 * j)) & 1u) == 0u) c = make_uint4(0, 0, 0, 0);
-            const uint32_t lo0 = mul_f16x2(fp8_half2(c.x & 0xFFFFu), by2), lo1 = mul_f16x2(fp8_half2(c.x >> 16), by2);
-            const uint32_t lo2 = mul_f16x2(fp8_half2(c.y & 0xFFFFu), by2), lo3 = mul_f16x2(fp8_half2(c.y >> 16), by2);
-            const uint32_t hi0 = mul_f16x2(fp8_half2(c.z & 0xFFFFu), by2), hi1 = mul_f16x2(fp8_half2(c.z >> 16), by2);
-            const uint32_t hi2 = mul_f16x2(fp8_half2(c.w & 0xFFFFu), by2), hi3 = mul_f16x2(fp8_half2(c.w >> 16), by2);
-            const int key = key4 * 4 + j, r = key & 7;
-            const uint32_t line = tile + (key >> 3) * kGroupBytes + r * 128;
-            const uint32_t a0 = line + ((((col & 3) * 2) ^ r) << 4), a1 = line + ((((col & 3) * 2 + 1) ^ r) << 4);
-            if (first) {
-              st_shared(a1, hi0, hi1, hi2, hi3);
-              st_shared(a0, lo0, lo1, lo2, lo3);
-            } else {
-              st_shared(a0, lo0, lo1, lo2, lo3);
-              st_shared(a1, hi0, hi1, hi2, hi3);
-            }
+            const uint32_t x = __byte_perm(by[j >> 1], 0u, ((j & 1) != 0) != (odd != 0) ? 0x3232 : 0x1010);
+            uint32_t h[8];
+            halves4(c[j].x, x, h[0], h[1]);
+            halves4(c[j].y, x, h[2], h[3]);
+            halves4(c[j].z, x, h[4], h[5]);
+            halves4(c[j].w, x, h[6], h[7]);
+            const uint32_t a = off[j] + to + u * (kGroups / 2) * kGroupBytes;
+            st_shared(a, h[0], h[1], h[2], h[3]);
+            st_shared(a ^ 16u, h[4], h[5], h[6], h[7]);
           }
         }
         fence_proxy_async();
@@ -555,31 +606,33 @@ attn_fp8_kernel(DevBatch d, DevTcPlan tc, const uint16_t *__restrict__ q, Fp8Poo
         ++ring;
         return true;
       };
-      Fetched<kD> f[kAhead];
-      TcPage pg[kAhead + 1];
-#pragma unroll
-      for (int a = 0; a <= kAhead; ++a) pg[a] = page_at(a);
-#pragma unroll
-      for (int a = 0; a < kAhead; ++a)
-        if (a < n_pos) fetch(f[a], a, pg[a]);
-      TcPage next = pg[kAhead];
-      for (int i0 = 0; i0 < n_pos && ok; i0 += kAhead) {
-#pragma unroll
-        for (int a = 0; a < kAhead; ++a) {
-          const int i = i0 + a;
-          if (i < n_pos && ok) {
-            ok = convert(f[a], i);
-            if (ok && i + kAhead < n_pos) {
-              fetch(f[a], i + kAhead, next);
-              next = page_at(i + kAhead + 1);
-            }
-          }
-        }
+      for (int a = 0; a < ahead; ++a) {
+        if (a < n_pos) fetch(a, a, page_at(a));
+        asm volatile("cp.async.commit_group;" ::: "memory");
       }
+      TileWords nxt = words_at(0, page_at(0));
+      int2 near = page_at(1);
+      int slot = 0;
+      for (int i = 0; i < n_pos; ++i) {
+        // Loads into registers are all asked for here and looked at a position later: a warp has few counters to wait for loads with, and a wait
+        // for an old one that shares a counter with a new one is a wait for both.
+        const TileWords cur = nxt;
+        nxt = words_at(i + 1, near);
+        near = page_at(i + 2);
+        const int2 far = page_at(i + ahead);
+        if (deep) asm volatile("cp.async.wait_group %0;" ::"n"(Sh::kDeepSlots - 1) : "memory");
+        else asm volatile("cp.async.wait_group %0;" ::"n"(Sh::kSlots - 1) : "memory");
+        ok = convert(cur, i, slot);
+        if (!ok) break;
+        if (i + ahead < n_pos) fetch(i + ahead, slot, far);
+        asm volatile("cp.async.commit_group;" ::: "memory");
+        slot = slot + 1 == ahead ? 0 : slot + 1;
+      }
+      asm volatile("cp.async.wait_group 0;" ::: "memory");  // (after an abort some are still on their way)
       tiles += (uint32_t)n;
     }
   } else {
-    asm volatile("setmaxnreg.inc.sync.aligned.u32 168;");
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 176;");
     // ======================= softmax warpgroups ======================================
     const int s = warp >> 2;        // stream
     const int quarter = warp & 3;   // tensor-memory lane quarter this warp may access
