@@ -16,7 +16,7 @@
 // The weights are f16 as well, 2^6 above the row's reference and at most 2^15: 11 bits instead of bf16's 8, nothing lost above 2^-20 of the
 // largest, and a row whose scores grow by more than 2^6 does its half-tile again.
 //
-// One CTA = 16 warps in four warpgroups, registers moved with setmaxnreg (176 x 256 + 80 x 128 + 72 x 128 <= 128 x 512):
+// One CTA = 16 warps in four warpgroups, registers moved with setmaxnreg (176 x 256 + 80 x 256 = 128 x 512):
 //   warps 8-11  converters.  No staging: a thread loads its codes (16 bytes of eight keys of a tile; four with head size 64) straight into registers,
 //               two tiles (four) ahead -- 32 KB in flight an SM -- turns them into halves and stores them as the swizzled operand.  Through
 //               shared memory they would cross it twice more, and it is as busy as the tensor cores: 32 KB of a tile written and
@@ -38,33 +38,32 @@ namespace lr {
 
 namespace {
 
-constexpr int kHalfBytes = 16384;  // 128 rows or keys x 64 channels
+constexpr int kHalfBytes = 16384;  // 128 rows of Q x 64 channels
 constexpr int kAtomBytes = 1024;   // 8 keys x 64 channels, one 128-byte-swizzle atom
-constexpr int kMaxStages = 8;
+constexpr int kMaxStages = 16;
 constexpr int kThreads = 512;
-constexpr int kInfos = 16;         // tiles whose scales are published ahead of their products; more than the ring can hold
+constexpr int kTeams = 6;          // converter warps, each with half-tiles of its own
+constexpr int kInfos = 16;         // half-tiles whose scales are published ahead of their products; more than the ring can hold
 constexpr float kGrow = 6.0f;      // log2: how far the scores of a row may rise above its reference exponent
 constexpr float kHead = 6.0f;      // log2: weights are kept this much above what they are
-constexpr int kRise = 3;           // log2: ... and V's tiles this much above the accumulator's unit: 6 + 6 + 3 = 15, f16 ends at 16
-constexpr int kApart = 24;         // log2: a tile of V this far below the unit sums its weights apart
+constexpr int kRise = 3;           // log2: ... and V's half-tiles this much above the accumulator's unit: 6 + 6 + 3 = 15, f16 ends at 16
+constexpr int kApart = 24;         // log2: V this far below the unit has its weights summed apart
 
 template <int kD>
 struct Shape {
   static_assert(kD == 64 || kD == 128, "head sizes of the tensor-core path");
-  static constexpr int kHalves = kD / 64;
-  static constexpr int kTileBytes = kHalves * kHalfBytes;   // as in attn_tc.cu
-  static constexpr int kGroupBytes = kHalves * kAtomBytes;
-  static constexpr int kStages = kD == 128 ? 4 : 8;
-  static constexpr int kCols = kD / 16;                     // converter threads side by side in a row, 16 channels each
-  static constexpr int kGroups = 128 / kCols;               // groups of four keys that the converters have at a time
-  static constexpr int kRounds = 32 / kGroups;              // ... and how many times for a tile
-  static constexpr int kChunks = 4 * kRounds;               // 16-byte chunks of a tile that a thread has
-  static constexpr int kCodeBytes = 128 * kD;               // a tile as it comes
-  static constexpr int kSlots = kD == 128 ? 2 : 6;          // of them on their way
-  static constexpr int kDeepSlots = kD == 128 ? 4 : 6;      // ... where no piece of the CTA has a second M-tile: its place in Q's buffer
+  static constexpr int kHalves = kD / 64;                   // 64-channel halves of a row (one 128-byte swizzle line each)
+  static constexpr int kQBytes = kHalves * kHalfBytes;      // an M-tile of Q: [halves][128 rows][128 B]
+  static constexpr int kGroupBytes = kHalves * kAtomBytes;  // the atoms of one 8-key group
+  static constexpr int kStageBytes = 8 * kGroupBytes;       // 64 keys as halves: [8 groups][halves][8 keys][128 B]
+  static constexpr int kStages = kD == 128 ? 7 : 16;
+  static constexpr int kCols = kD / 16;                     // lanes side by side in a row, 16 channels each
+  static constexpr int kGroups = 32 / kCols;                // groups of four keys that a warp has at a time
+  static constexpr int kRounds = 16 / kGroups;              // ... and how many times for a half-tile
+  static constexpr int kCodeBytes = 64 * kD;                // a half-tile as it comes
 };
 
-struct Info {  // of a tile: the largest scale bytes of its keys; whether some visible row of V stands for NaN
+struct Info {  // of a half-tile: the largest scale bytes of its keys; whether some valid row of V stands for NaN
   int32_t k_ref, v_ref, v_nan;
 };
 
@@ -80,20 +79,71 @@ struct __align__(16) Ctrl {
   int abort_flag;
   uint64_t wait_limit_ns;
   Info info[kInfos];
-  uint8_t v_nan[kInfos][32];  // four keys a byte
+  uint8_t v_nan[kInfos][16];  // four keys a byte
   float xch_m[128], xch_l[128], xch_unit[128];  // stream 1's rows, for the in-CTA combination
 };
 constexpr int kCtrlBytes = 3 << 10;
 static_assert(sizeof(Ctrl) <= kCtrlBytes, "Ctrl must fit behind the tiles");
 template <int kD>
-constexpr int kSmemBytes = (2 + Shape<kD>::kStages) * Shape<kD>::kTileBytes + Shape<kD>::kSlots * Shape<kD>::kCodeBytes + kCtrlBytes;  // the base must be 1024-aligned
+constexpr int kSmemBytes = 2 * Shape<kD>::kQBytes + Shape<kD>::kStages * Shape<kD>::kStageBytes + kTeams * Shape<kD>::kCodeBytes + kCtrlBytes;  // the base must be 1024-aligned
 static_assert(kSmemBytes<64> <= 227 * 1024 && kSmemBytes<128> <= 227 * 1024, "shared memory per CTA");
+
+// ---- ring order ----------------------------------------------------------------------
+// The ring holds half-tiles (64 keys of K or of V).  Within a piece of n tiles they come in the order the issuers first touch them.  With la = tiles of K
+// issued ahead of the first PV (1 for two M-tiles, 2 for the even/odd split): both halves of K(0..min(la,n)-1), then for every u with u + la < n
+// V(u)a, K(u+la)a, V(u)b, K(u+la)b, then what is left of V.
+struct HalfOrder {
+  int la, la_c, np;  // np = number of (V, K) pairs
+  __device__ __forceinline__ HalfOrder(int n, int mode) : la(mode == 2 ? 1 : 2) {
+    la_c = min(la, n);
+    np = max(0, n - la);
+  }
+  __device__ __forceinline__ int k(int t, int half) const { return t < la ? 2 * t + half : 2 * la_c + 4 * (t - la) + 2 * half + 1; }
+  __device__ __forceinline__ int v(int u, int half) const { return u < np ? 2 * la_c + 4 * u + 2 * half : 2 * la_c + 4 * np + 2 * (u - np) + half; }
+  // place i of the 4n of a piece -> tile, half, and whether it is V's
+  __device__ __forceinline__ int at(int i, int &half, bool &is_v) const {
+    half = i & 1;
+    is_v = false;
+    if (i < 2 * la_c) return i >> 1;
+    i -= 2 * la_c;
+    if (i < 4 * np) {
+      half = (i >> 1) & 1;
+      is_v = !(i & 1);
+      return (i >> 2) + (is_v ? 0 : la);
+    }
+    i -= 4 * np;
+    half = i & 1;
+    is_v = true;
+    return np + (i >> 1);
+  }
+};
 
 // Instruction descriptors: D fp32, A and B f16 (format 0), M = 128; QK: N = 64 keys, both operands K-major; PV: N = head size, B N-major.
 constexpr uint32_t kIdescBase = (1u << 4) | (8u << 24);
 constexpr uint32_t kIdescQK = kIdescBase | ((64u >> 3) << 17);
 template <int kD>
 constexpr uint32_t kIdescPV = kIdescBase | (((uint32_t)kD >> 3) << 17) | (1u << 16);
+
+// Five roles share an SM's instruction cache, and warps that wait for instructions were what bounded a version of this kernel that had everything
+// unrolled: what is long is in a loop, and what is rare out of the way.  The bounded wait of a whole warp (as wait_bar):
+__device__ __forceinline__ bool wait(uint64_t *bar, uint32_t parity, Ctrl *ctrl, int32_t *status, int code) {
+  if (__builtin_expect(__all_sync(0xFFFFFFFFu, mbar_test_wait(bar, parity)), 1)) return true;
+  const uint64_t t0 = global_ns();
+  for (uint32_t i = 0;; ++i) {
+    if (__all_sync(0xFFFFFFFFu, mbar_try_wait(bar, parity))) return true;
+    if ((i & 31u) == 31u) {
+      const bool out = global_ns() - t0 > ctrl->wait_limit_ns;
+      if (__any_sync(0xFFFFFFFFu, out || *reinterpret_cast<volatile int *>(&ctrl->abort_flag))) {
+        if (out) {
+          *reinterpret_cast<volatile int *>(&ctrl->abort_flag) = 1;
+          status[0] = kDevTimeout;
+          status[1] = code;
+        }
+        return false;
+      }
+    }
+  }
+}
 
 __device__ __forceinline__ uint32_t pack_f16(float lo, float hi) {
   uint32_t r;
@@ -124,9 +174,7 @@ __device__ __forceinline__ void st_shared(uint32_t addr, uint32_t a, uint32_t b,
   asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(addr), "r"(a), "r"(b), "r"(c), "r"(d) : "memory");
 }
 
-// P = exp2(sc * s - m + bias) for 64 scores, as halves over the first half of the score buffer; returns their fp32 sum.  With kMax also the
-// maximum of the raw scores.
-template <bool kMax>
+// P = exp2(sc * s + neg) for 64 scores, as halves over the first half of the score buffer; returns their fp32 sum and the maximum of the raw scores.
 __device__ __forceinline__ float exp_half(const uint32_t (&v)[64], uint32_t addr, float sc, float neg, float &raw_max) {
   const float2 s2 = make_float2(sc, sc), n2 = make_float2(neg, neg);
   float2 acc0 = make_float2(0.f, 0.f), acc1 = make_float2(0.f, 0.f);
@@ -136,10 +184,10 @@ __device__ __forceinline__ float exp_half(const uint32_t (&v)[64], uint32_t addr
   for (int i = 0; i < 64; i += 4) {
     float2 y0 = ffma2(make_float2(bits_f(v[i]), bits_f(v[i + 1])), s2, n2);
     float2 y1 = ffma2(make_float2(bits_f(v[i + 2]), bits_f(v[i + 3])), s2, n2);
-    if (kMax) m0 = max3(m0, bits_f(v[i]), bits_f(v[i + 1]));
+    m0 = max3(m0, bits_f(v[i]), bits_f(v[i + 1]));
     y0.x = ex2(y0.x);
     y0.y = ex2(y0.y);
-    if (kMax) m1 = max3(m1, bits_f(v[i + 2]), bits_f(v[i + 3]));
+    m1 = max3(m1, bits_f(v[i + 2]), bits_f(v[i + 3]));
     y1.x = ex2(y1.x);
     y1.y = ex2(y1.y);
     acc0 = fadd2(acc0, y0);
@@ -148,15 +196,15 @@ __device__ __forceinline__ float exp_half(const uint32_t (&v)[64], uint32_t addr
     pk[(i >> 1) + 1] = pack_f16(y1.x, y1.y);
   }
   tmem_st32(addr, pk);
-  if (kMax) raw_max = fmaxf(m0, m1);
+  raw_max = fmaxf(m0, m1);
   acc0 = fadd2(acc0, acc1);
   return acc0.x + acc0.y;
 }
 
-// Whether the row sees a key of the tile whose row of V stands for NaN.  pages: null where it sees all keys.
+// Whether the row sees a key of the half-tile whose row of V stands for NaN.  pages: null where it sees all keys.
 __device__ __noinline__ bool sees_nan(const uint8_t *nan4, const TcPage *pages, RowInfo ri) {
   bool seen = false;
-  for (int p = 0; p < kPagesPerTile; ++p) {
+  for (int p = 0; p < kPagesPerTile / 2; ++p) {
     const uint32_t w = *reinterpret_cast<const volatile uint32_t *>(nan4 + 4 * p);  // a byte of it: four keys
     const uint32_t keys = (w & 15u) | ((w >> 4) & 0xF0u) | ((w >> 8) & 0xF00u) | ((w >> 12) & 0xF000u);
     const int n = pages != nullptr ? page_n_ok(pages[p].meta, ri) : kPage;
@@ -251,20 +299,14 @@ struct Fp8Pools {
   const uint8_t *k, *v, *k_scale, *v_scale;
 };
 
-// What a converter lane knows of a tile of K or V.
-struct TileWords {
-  uint32_t word, v_word;  // scale bytes of keys 4 lane .. 4 lane + 3; with a tile of K also V's
-  uint32_t meta;          // of the page those keys lie in
-};
-
 __device__ __forceinline__ uint32_t valid_bytes(int valid, int lane) {  // of the four keys of this lane's word
   const int n = valid - (lane & 3) * 4;
   return n >= 4 ? 0xFFFFFFFFu : n <= 0 ? 0u : (1u << (8 * n)) - 1u;
 }
-// the largest scale byte of the tile, of valid keys that do not stand for NaN; `bytes`: this lane's four, those of no valid token cleared
-__device__ __forceinline__ int tile_ref(uint32_t bytes) {
+// the largest of four scale bytes, but for those of rows that stand for NaN
+__device__ __forceinline__ uint32_t top_byte(uint32_t bytes) {
   const uint32_t w = bytes & ~__vcmpeq4(bytes, 0xFFFFFFFFu), t = __vmaxu4(w, w >> 16);
-  return (int)max(__reduce_max_sync(0xFFFFFFFFu, max(t & 0xFFu, (t >> 8) & 0xFFu)), 1u);
+  return max(t & 0xFFu, (t >> 8) & 0xFFu);
 }
 // 2^(byte - ref) of two keys, as halves; `nan`: what a byte of 255 gives
 __device__ __forceinline__ uint32_t factors(uint32_t b0, uint32_t b1, int ref, float nan) {
@@ -284,7 +326,7 @@ __global__ void __launch_bounds__(kThreads, 1)
 attn_fp8_kernel(DevBatch d, DevTcPlan tc, const uint16_t *__restrict__ q, Fp8Pools in, uint16_t *__restrict__ out, float *__restrict__ lse,
                 float scale_log2) {
   using Sh = Shape<kD>;
-  constexpr int kTileBytes = Sh::kTileBytes, kGroupBytes = Sh::kGroupBytes, kStages = Sh::kStages, kHalves = Sh::kHalves;
+  constexpr int kQBytes = Sh::kQBytes, kStageBytes = Sh::kStageBytes, kGroupBytes = Sh::kGroupBytes, kStages = Sh::kStages, kHalves = Sh::kHalves;
   extern __shared__ __align__(1024) unsigned char smem[];
   if ((smem_u32(smem) & 1023u) != 0u) {  // the swizzled tiles need a 1024-byte aligned base
     if (threadIdx.x == 0) {
@@ -293,10 +335,10 @@ attn_fp8_kernel(DevBatch d, DevTcPlan tc, const uint16_t *__restrict__ q, Fp8Poo
     }
     return;
   }
-  unsigned char *q_smem = smem;                    // two M-tiles
-  unsigned char *kv_smem = smem + 2 * kTileBytes;  // kStages tiles
-  unsigned char *code_smem = kv_smem + kStages * kTileBytes;  // kSlots tiles of codes
-  Ctrl *ctrl = reinterpret_cast<Ctrl *>(code_smem + Sh::kSlots * Sh::kCodeBytes);
+  unsigned char *q_smem = smem;                  // two M-tiles
+  unsigned char *kv_smem = smem + 2 * kQBytes;   // kStages half-tiles
+  unsigned char *code_smem = kv_smem + kStages * kStageBytes;  // a half-tile of codes for each converter
+  Ctrl *ctrl = reinterpret_cast<Ctrl *>(code_smem + kTeams * Sh::kCodeBytes);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
 
   // the plan is uploaded by copies, so it may be read in front of the wait for the kernel before
@@ -306,7 +348,7 @@ attn_fp8_kernel(DevBatch d, DevTcPlan tc, const uint16_t *__restrict__ q, Fp8Poo
     reinterpret_cast<uint4 *>(&ctrl->head)[lane] = __ldg(reinterpret_cast<const uint4 *>(head) + lane);
   if (threadIdx.x == 0) {
     for (int s = 0; s < kStages; ++s) {
-      mbar_init(&ctrl->kv_full[s], 4);   // one arrival per converter warp
+      mbar_init(&ctrl->kv_full[s], 1);
       mbar_init(&ctrl->kv_empty[s], 2);  // one per MMA issuer
     }
     mbar_init(&ctrl->q_full, 256);
@@ -340,25 +382,23 @@ attn_fp8_kernel(DevBatch d, DevTcPlan tc, const uint16_t *__restrict__ q, Fp8Poo
 
   const int T = tc.tokens_per_mtile;
 
-  if (warp >= 12) {
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
-    if (warp < 14) {
+  if (warp >= 8) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 80;");
+    const TcCtaHead *head = &ctrl->head;
+    if (warp == 12 || warp == 13) {
       // ======================= MMA issuer of stream s ====================================
       // Both issuers walk every ring position of a piece in order: a position this stream uses is consumed by its MMAs (released by a
       // tcgen05.commit), one it does not use is released with a plain arrive once it has landed.
-      const TcCtaHead *head = &ctrl->head;
       const int s = __shfl_sync(0xFFFFFFFFu, warp, 0) - 12;
       uint32_t ring_base = 0, waited = 0, p_cnt = 0, pc_idx = 0;
       bool ok = true;
-      const uint32_t q_addr = smem_u32(q_smem), kv_addr = smem_u32(kv_smem);
       const uint32_t tmem_u = __shfl_sync(0xFFFFFFFFu, tmem, 0);
       const uint32_t s_tmem = tmem_u + s * 128, o_tmem = tmem_u + 256 + s * 128;
       // Descriptors differ from a base only in the start-address field (units of 16 bytes).
-      const uint64_t qdesc0 = make_desc(q_addr, 16, 1024), kdesc0 = make_desc(kv_addr, 16, kGroupBytes),
-                     vdesc0 = make_desc(kv_addr, kAtomBytes, kGroupBytes);
-      auto issue_qk = [&](int m, uint32_t stage, int half) {  // S_s[half] = Q_m K^T over 64 of the 128 keys
-        const uint64_t a = qdesc0 + (uint64_t)(m * (kTileBytes >> 4)),
-                       b = kdesc0 + (uint64_t)(stage * (kTileBytes >> 4) + half * (8 * kGroupBytes >> 4));
+      const uint64_t qdesc0 = make_desc(smem_u32(q_smem), 16, 1024), kdesc0 = make_desc(smem_u32(kv_smem), 16, kGroupBytes),
+                     vdesc0 = make_desc(smem_u32(kv_smem), kAtomBytes, kGroupBytes);
+      auto issue_qk = [&](int m, uint32_t stage, int half) {  // S_s[half] = Q_m K^T over 64 keys
+        const uint64_t a = qdesc0 + (uint64_t)(m * (kQBytes >> 4)), b = kdesc0 + (uint64_t)(stage * (kStageBytes >> 4));
 #pragma unroll
         for (int h = 0; h < kHalves; ++h)
 #pragma unroll
@@ -366,8 +406,8 @@ attn_fp8_kernel(DevBatch d, DevTcPlan tc, const uint16_t *__restrict__ q, Fp8Poo
             mma_ss(s_tmem + half * 64, a + (uint64_t)(h * (kHalfBytes >> 4) + kk * 2), b + (uint64_t)(h * (kAtomBytes >> 4) + kk * 2),
                    kIdescQK, (h | kk) != 0);
       };
-      auto issue_pv = [&](uint32_t stage, int half, bool acc) {  // O_s (+)= P_s[half] V over 64 of the 128 keys
-        const uint64_t b = vdesc0 + (uint64_t)(stage * (kTileBytes >> 4) + half * (8 * kGroupBytes >> 4));
+      auto issue_pv = [&](uint32_t stage, int half, bool acc) {  // O_s (+)= P_s[half] V over 64 keys
+        const uint64_t b = vdesc0 + (uint64_t)(stage * (kStageBytes >> 4));
 #pragma unroll
         for (int k4 = 0; k4 < 4; ++k4)
           mma_ts(o_tmem, s_tmem + half * 64 + k4 * 8, b + (uint64_t)(k4 * (2 * kGroupBytes >> 4)), kIdescPV<kD>, acc || k4 != 0);
@@ -375,76 +415,70 @@ attn_fp8_kernel(DevBatch d, DevTcPlan tc, const uint16_t *__restrict__ q, Fp8Poo
       for (int pc = piece0; pc < piece1 && ok; ++pc, ++pc_idx) {
         const TcPiece pi = pc == piece0 ? head->first : tc.pieces[pc];
         const int n = pi.tile_end - pi.tile_begin, mode = pi.n_mt;
-        const RingOrder ord(n, mode);
+        const HalfOrder ord(n, mode);
         const int my_units = mode == 2 ? n : (n - s + 1) / 2;
         const int m_tile = mode == 2 ? s : 0;
         auto need = [&](uint32_t pos, int code) -> bool {  // waits, in ring order, until absolute ring position `pos` has landed
           while (waited <= pos) {
-            if (!wait_bar(&ctrl->kv_full[waited % kStages], (waited / kStages) & 1u, ctrl, d.status, code)) return false;
+            if (!wait(&ctrl->kv_full[waited % kStages], (waited / kStages) & 1u, ctrl, d.status, code)) return false;
             if (waited < pos && elect_one()) mbar_arrive(&ctrl->kv_empty[waited % kStages]);
             ++waited;
           }
           return true;
         };
         auto release = [&](uint32_t pos) { tc_commit(&ctrl->kv_empty[pos % kStages]); };  // arrives when the MMAs that read the stage retire
-        ok = wait_bar(&ctrl->q_full, pc_idx & 1u, ctrl, d.status, 270);
+        ok = wait(&ctrl->q_full, pc_idx & 1u, ctrl, d.status, 270);
         if (!ok) break;
         if (my_units > 0) {
-          const uint32_t pos = ring_base + ord.pos_k(mode == 2 ? 0 : s);
-          ok = need(pos, 271);
-          if (!ok) break;
-          tc_fence_after();
-          if (elect_one()) {
-            issue_qk(m_tile, pos % kStages, 0);
-            tc_commit(&ctrl->s_full[s][0]);
-            issue_qk(m_tile, pos % kStages, 1);
-            tc_commit(&ctrl->s_full[s][1]);
-            release(pos);
-            if (my_units == 1) tc_commit(&ctrl->q_empty);  // last QK of the piece: this stream is done with the Q buffers
+#pragma unroll 1
+          for (int half = 0; half < 2; ++half) {
+            const uint32_t pos = ring_base + ord.k(mode == 2 ? 0 : s, half);
+            ok = need(pos, 271);
+            if (!ok) break;
+            tc_fence_after();
+            if (elect_one()) {
+              issue_qk(m_tile, pos % kStages, half);
+              tc_commit(&ctrl->s_full[s][half]);
+              release(pos);
+              if (half == 1 && my_units == 1) tc_commit(&ctrl->q_empty);  // last QK of the piece: this stream is done with the Q buffers
+            }
+            __syncwarp();
           }
-          __syncwarp();
+          if (!ok) break;
         } else {
           if (elect_one()) mbar_arrive(&ctrl->q_empty);
           // nothing to issue in this piece: still observe the previous piece's epilogue phase, so that the parity
           // wait of a later piece never finds this issuer two phases behind
           if (pc_idx > 0) {
-            ok = wait_bar(&ctrl->epi_done, (pc_idx - 1) & 1u, ctrl, d.status, 278);
+            ok = wait(&ctrl->epi_done, (pc_idx - 1) & 1u, ctrl, d.status, 278);
             if (!ok) break;
           }
         }
         for (int j = 0; j < my_units && ok; ++j) {
           const int t = mode == 2 ? j : 2 * j + s;
-          const uint32_t pos_v = ring_base + ord.pos_v(t), sV = pos_v % kStages;
-          ok = need(pos_v, 272);
-          if (!ok) break;
           const bool has_next = j + 1 < my_units;
-          uint32_t pos_k = 0;
-          if (has_next) {
-            pos_k = ring_base + ord.pos_k(mode == 2 ? j + 1 : 2 * (j + 1) + s);
-            ok = need(pos_k, 276);
-            if (!ok) break;
-          }
           if (j == 0 && pc_idx > 0) {  // the epilogue of the previous piece has read O_0 and O_1
-            ok = wait_bar(&ctrl->epi_done, (pc_idx - 1) & 1u, ctrl, d.status, 273);
+            ok = wait(&ctrl->epi_done, (pc_idx - 1) & 1u, ctrl, d.status, 273);
             if (!ok) break;
           }
 #pragma unroll 1
           for (int half = 0; half < 2; ++half) {
+            const uint32_t pos_v = ring_base + ord.v(t, half), pos_k = ring_base + ord.k(t + (mode == 2 ? 1 : 2), half);
+            ok = need(pos_v, 272) && (!has_next || need(pos_k, 276));
+            if (!ok) break;
             // P of this half is in place: O += P V, then the buffer takes the scores of the next tile's half
-            ok = wait_bar(&ctrl->p_full[s][half], p_cnt & 1u, ctrl, d.status, 274 + s);
+            ok = wait(&ctrl->p_full[s][half], p_cnt & 1u, ctrl, d.status, 274 + s);
             if (!ok) break;
             tc_fence_after();
             if (elect_one()) {
-              issue_pv(sV, half, (j | half) != 0);
+              issue_pv(pos_v % kStages, half, (j | half) != 0);
               tc_commit(&ctrl->o_done[s]);
-              if (half == 1) release(pos_v);
+              release(pos_v);
               if (has_next) {
                 issue_qk(m_tile, pos_k % kStages, half);
                 tc_commit(&ctrl->s_full[s][half]);
-                if (half == 1) {
-                  release(pos_k);
-                  if (j + 2 == my_units) tc_commit(&ctrl->q_empty);  // last QK of the piece
-                }
+                release(pos_k);
+                if (half == 1 && j + 2 == my_units) tc_commit(&ctrl->q_empty);  // last QK of the piece
               }
             }
             __syncwarp();
@@ -452,7 +486,7 @@ attn_fp8_kernel(DevBatch d, DevTcPlan tc, const uint16_t *__restrict__ q, Fp8Poo
           ++p_cnt;
         }
         if (!ok) break;
-        ring_base += 2u * (uint32_t)n;
+        ring_base += 4u * (uint32_t)n;
         if (waited < ring_base) {  // positions of the piece this stream never touched (the tail of the other stream's tiles)
           ok = need(ring_base - 1, 277);
           if (!ok) break;
@@ -467,169 +501,161 @@ attn_fp8_kernel(DevBatch d, DevTcPlan tc, const uint16_t *__restrict__ q, Fp8Poo
           if (global_ns() - t0 > kDrainLimitNs) break;
       }
       __syncwarp();
-    }
-  } else if (warp >= 8) {
-    // ======================= converters ==================================================
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 80;");
-    const TcCtaHead *head = &ctrl->head;
-    constexpr int kCols = Sh::kCols, kGroups = Sh::kGroups, kRounds = Sh::kRounds;
-    const int ct = threadIdx.x - 256, col = ct % kCols, grp = ct / kCols;  // 16 channels of keys (round * kGroups + grp) * 4 .. + 3
-    // Eight neighbouring lanes store to two lines at a time whose 16-byte units lie in the same banks (both channel halves of a key, or with head size 64
-    // keys four apart); half of them take their four keys in the order 1, 0, 3, 2, which brings the units of the two lines apart.
-    const int odd = kD == 128 ? col >> 2 : grp & 1;
-    const uint32_t line0 = smem_u32(kv_smem) + (kD == 128 ? (col >> 2) * kAtomBytes : 0) + (grp >> 1) * kGroupBytes;
-    uint32_t off[4];  // of the first of the two units of each key
+    } else {
+      // ======================= converters ==================================================
+      constexpr int kCols = Sh::kCols, kGroups = Sh::kGroups, kRounds = Sh::kRounds;
+      const int team = warp < 12 ? warp - 8 : warp - 10;
+      const int col = lane % kCols, grp = lane / kCols;  // 16 channels of keys (round * kGroups + grp) * 4 .. + 3
+      // Eight neighbouring lanes store to two lines at a time whose 16-byte units lie in the same banks (both channel halves of a key, or with head size 64
+      // keys four apart); half of them take their four keys in the order 1, 0, 3, 2, which brings the units of the two lines apart.
+      const int odd = kD == 128 ? col >> 2 : grp & 1;
+      uint32_t off[4];  // in a stage: of the first of the two units of each key
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const int r = (grp & 1) * 4 + (j ^ odd);
-      off[j] = line0 + r * 128 + ((((col & 3) * 2) ^ r) << 4);
-    }
-    const int32_t k_off = (grp & 3) * 4 * kD + col * 16;  // within the page of the keys
-    // This thread's part of the slots: it alone copies and reads them, so that nothing but its own copies has to be waited for.
-    const uint32_t mine = smem_u32(code_smem) + ct * 16, mine_deep = smem_u32(q_smem) + kTileBytes + ct * 16;
-    auto slot_at = [&](int slot) -> uint32_t {
-      return slot < Sh::kSlots ? mine + slot * Sh::kCodeBytes : mine_deep + (slot - Sh::kSlots) * Sh::kCodeBytes;
-    };
-    bool deep = Sh::kDeepSlots > Sh::kSlots;
-    if constexpr (Sh::kDeepSlots > Sh::kSlots)
-      for (int pc = piece0; pc < piece1; ++pc) deep = deep && (pc == piece0 ? head->first.n_mt : tc.pieces[pc].n_mt) == 1;
-    const int ahead = deep ? Sh::kDeepSlots : Sh::kSlots;  // tiles on their way
-    uint32_t ring = 0, tiles = 0;  // ring positions and tiles of K so far
-    bool ok = true;
-    for (int pc = piece0; pc < piece1 && ok; ++pc) {
-      const TcPiece pi = pc == piece0 ? head->first : tc.pieces[pc];
-      const TcReq rq = pc == piece0 ? head->first_req : tc.reqs[pi.req];
-      const int n = pi.tile_end - pi.tile_begin, n_pos = 2 * n;
-      const int n_whole = rq.n_dense_tiles - pi.tile_begin;  // tiles of the piece without slots of no valid token
-      const RingOrder ord(n, pi.n_mt);
-      const TcPage *pages = tc.pages + rq.page_off + pi.tile_begin * kPagesPerTile + (lane >> 2);  // of this lane's word
-      auto page_at = [&](int i) -> int2 {
-        bool is_v;
-        const int t = ord.step(min(i, n_pos - 1), is_v);
-        return ld_pair(pages + t * kPagesPerTile);
+      for (int j = 0; j < 4; ++j) {
+        const int r = (grp & 1) * 4 + (j ^ odd);
+        off[j] = smem_u32(kv_smem) + (kD == 128 ? (col >> 2) * kAtomBytes : 0) + (grp >> 1) * kGroupBytes + r * 128 + ((((col & 3) * 2) ^ r) << 4);
+      }
+      const int32_t k_off = (grp & 3) * 4 * kD + col * 16;  // within the page of the keys
+      // A lane alone copies and reads its part of the warp's codes, so that nothing but its own copies has to be waited for; a part
+      // is asked for again as soon as it has been read, a whole half-tile's work ahead.
+      const uint32_t mine = smem_u32(code_smem) + team * Sh::kCodeBytes + lane * 16;
+
+      // the ring positions of this warp: every kTeams-th of the CTA's
+      struct Place {
+        int32_t info;    // number of the half-tile among the CTA's
+        int32_t kv_head;
+        bool is_v, whole, there;  // whole: no slot without a valid token
       };
-      auto row_of = [&](int32_t page) -> int32_t {  // the first row of a page; rows of the pools are numbered within 32 bits (tc_plan_structure)
+      int pc = piece0, x = team;  // of the position that comes after the next one
+      TcPiece pi = head->first;
+      TcReq rq = head->first_req;
+      int32_t tiles0 = 0;  // tiles of the pieces before
+      auto place = [&](int2 &entry) -> Place {  // ... and the page of this lane's word, asked for here
+        while (pc < piece1 && x >= 4 * (pi.tile_end - pi.tile_begin)) {
+          x -= 4 * (pi.tile_end - pi.tile_begin);
+          tiles0 += pi.tile_end - pi.tile_begin;
+          if (++pc < piece1) {
+            pi = tc.pieces[pc];
+            rq = tc.reqs[pi.req];
+          }
+        }
+        Place p;
+        p.there = pc < piece1;
+        if (!p.there) return p;
+        int half;
+        const int t = HalfOrder(pi.tile_end - pi.tile_begin, pi.n_mt).at(x, half, p.is_v);
+        p.info = (tiles0 + t) * 2 + half;
+        p.kv_head = pi.kv_head;
+        p.whole = pi.tile_begin + t < rq.n_dense_tiles;
+        entry = ld_pair(tc.pages + rq.page_off + (pi.tile_begin + t) * kPagesPerTile + half * 4 + ((lane >> 2) & 3));
+        x += kTeams;
+        return p;
+      };
+      auto row_of = [&](int32_t page, int32_t kv_head) -> int32_t {  // the first row of a page; rows of the pools are numbered within 32 bits (tc_plan_structure)
         if (page < 0 || page >= d.n_pool_pages) {  // never fetch outside the pool
           d.status[0] = kDevBounds;
           d.status[1] = 200;
           page = 0;
         }
-        return (page * d.n_kv_heads + pi.kv_head) * kPage;
+        return (page * d.n_kv_heads + kv_head) * kPage;
       };
-      auto words_at = [&](int i, int2 pg) -> TileWords {
-        bool is_v;
-        ord.step(min(i, n_pos - 1), is_v);
-        const int32_t row = row_of(pg.x);
-        TileWords w;
-        w.meta = (uint32_t)pg.y;
-        w.word = ld_word((is_v ? in.v_scale : in.k_scale) + row + (lane & 3) * 4);
-        w.v_word = is_v ? 0u : ld_word(in.v_scale + row + (lane & 3) * 4);
-        return w;
+      // lanes 0-15: the scale bytes of keys 4 lane .. 4 lane + 3; beside those of K, lanes 16-31 have V's of the same keys
+      auto word_at = [&](const Place &p, int32_t row) -> uint32_t {
+        return ld_word((p.is_v || lane >= 16 ? in.v_scale : in.k_scale) + row + (lane & 3) * 4);
       };
-      auto fetch = [&](int i, int slot, int2 pg) {  // asks for the codes of the tile of position i
-        bool is_v;
-        ord.step(i, is_v);
-        const int32_t row = row_of(pg.x);
-        if ((lane & 3) == 0) {  // its scale bytes are read a position ahead of their use, which is enough from L2
-          asm volatile("prefetch.global.L2 [%0];" ::"l"((is_v ? in.v_scale : in.k_scale) + row));
-          if (!is_v) asm volatile("prefetch.global.L2 [%0];" ::"l"(in.v_scale + row));
-        }
-        const uint8_t *pool = (is_v ? in.v : in.k) + k_off;
-        const uint32_t to = slot_at(slot);
+      auto fetch = [&](const Place &p, int32_t row, int u) {  // part u of the codes
+        // (a lane whose word lies in the page of this lane's keys; an absent page of the last tile reads page 0 and is cleared below)
+        const uint8_t *at = (p.is_v ? in.v : in.k) + k_off + (int64_t)__shfl_sync(0xFFFFFFFFu, row, ((u * kGroups + grp) >> 2) * 4) * kD;
+        const uint8_t *even = at + odd * kD, *other = at - odd * kD;
+        copy_codes(mine + u * 2048, even);
+        copy_codes(mine + u * 2048 + 512, other + kD);
+        copy_codes(mine + u * 2048 + 1024, even + 2 * kD);
+        copy_codes(mine + u * 2048 + 1536, other + 3 * kD);
+      };
+      bool ok = true;
+      int2 e_nxt = make_int2(0, 0), e_after = make_int2(0, 0);
+      Place nxt = place(e_nxt);
+      int32_t row = 0;
+      uint32_t word = 0, meta = 0;
+      if (nxt.there) {
+        row = row_of(e_nxt.x, nxt.kv_head);
+        meta = (uint32_t)e_nxt.y;
+        word = word_at(nxt, row);
+      }
 #pragma unroll
-        for (int u = 0; u < kRounds; ++u) {
-          // (a lane whose word lies in the page of this thread's keys; an absent page of the last tile reads page 0 and is cleared below)
-          const uint8_t *at = pool + (int64_t)__shfl_sync(0xFFFFFFFFu, row, ((u * kGroups + grp) >> 2) * 4) * kD;
-          const uint8_t *even = at + odd * kD, *other = at - odd * kD;
-          copy_codes(to + (u * 4) * 2048, even);
-          copy_codes(to + (u * 4 + 1) * 2048, other + kD);
-          copy_codes(to + (u * 4 + 2) * 2048, even + 2 * kD);
-          copy_codes(to + (u * 4 + 3) * 2048, other + 3 * kD);
+      for (int u = 0; u < kRounds; ++u) {
+        if (nxt.there) fetch(nxt, row, u);
+        asm volatile("cp.async.commit_group;" ::: "memory");
+      }
+      Place after = nxt;
+      if (nxt.there) after = place(e_after);
+      for (uint32_t ring = (uint32_t)team; nxt.there; ring += kTeams) {
+        // Loads into registers are asked for here and looked at a half-tile later.
+        const Place cur = nxt;
+        const uint32_t cur_word = word, cur_meta = meta;
+        nxt = after;
+        if (nxt.there) {
+          row = row_of(e_after.x, nxt.kv_head);
+          meta = (uint32_t)e_after.y;
+          word = word_at(nxt, row);
+          after = place(e_after);
         }
-      };
-      auto convert = [&](TileWords f, int i, int slot) -> bool {  // the tile of position i into its stage
-        bool is_v;
-        const int t = ord.step(i, is_v);
-        const uint32_t live = valid_bytes((int)(f.meta & 31u), lane);
-        const uint32_t bytes = f.word & live;
-        const int ref = tile_ref(bytes);
-        if (!is_v) {
-          const uint32_t v_bytes = f.v_word & live, nan = __vcmpeq4(v_bytes, 0xFFFFFFFFu);
-          const int v_ref = tile_ref(v_bytes);
+        const uint32_t live = valid_bytes((int)(cur_meta & 31u), lane), bytes = cur_word & live, top = top_byte(bytes);
+        const int ref = (int)max(__reduce_max_sync(0xFFFFFFFFu, lane < 16 ? top : 0u), 1u);
+        const uint32_t stage = ring % kStages;
+        ok = wait(&ctrl->kv_empty[stage], ((ring / kStages) & 1u) ^ 1u, ctrl, d.status, 210);
+        if (!ok) break;
+        if (!cur.is_v) {  // what the softmax has to know of this half-tile, V's scales among it
+          const int v_ref = (int)max(__reduce_max_sync(0xFFFFFFFFu, lane >= 16 ? top : 0u), 1u);
+          const uint32_t nan = lane >= 16 ? __vcmpeq4(bytes, 0xFFFFFFFFu) : 0u;
           const bool any = __any_sync(0xFFFFFFFFu, nan != 0u);
-          if (warp == 8) {
-            const uint32_t at = (tiles + (uint32_t)t) % kInfos;
-            if (any) ctrl->v_nan[at][lane] = (uint8_t)((nan & 1u) | ((nan >> 7) & 2u) | ((nan >> 14) & 4u) | ((nan >> 21) & 8u));
-            __syncwarp();
-            if (lane == 0) {
-              ctrl->info[at] = Info{ref, v_ref, any ? 1 : 0};
-              mbar_arrive(&ctrl->info_full[at]);
-            }
+          const uint32_t at = (uint32_t)cur.info % kInfos;
+          if (any && lane >= 16) ctrl->v_nan[at][lane - 16] = (uint8_t)((nan & 1u) | ((nan >> 7) & 2u) | ((nan >> 14) & 4u) | ((nan >> 21) & 8u));
+          __syncwarp();
+          if (lane == 0) {
+            ctrl->info[at] = Info{ref, v_ref, any ? 1 : 0};
+            mbar_arrive(&ctrl->info_full[at]);
           }
         }
         // the factors of this lane's four keys, which other lanes ask for
-        const float nan_is = is_v ? 0.f : __uint_as_float(0x7FC00000u);
+        const float nan_is = cur.is_v ? 0.f : __uint_as_float(0x7FC00000u);
         const uint32_t f01 = factors(bytes & 0xFFu, (bytes >> 8) & 0xFFu, ref, nan_is), f23 = factors((bytes >> 16) & 0xFFu, bytes >> 24, ref, nan_is);
-        const uint32_t stage = ring % kStages;
-        if (!wait_bar(&ctrl->kv_empty[stage], ((ring / kStages) & 1u) ^ 1u, ctrl, d.status, 210)) return false;
-        const uint32_t to = stage * kTileBytes, from = slot_at(slot);
-        const bool clear = is_v && t >= n_whole;  // (K's scores of slots that hold no valid token are never looked at)
-#pragma unroll
+        const uint32_t to = stage * kStageBytes;
+        const bool clear = cur.is_v && !cur.whole;  // (K's scores of slots that hold no valid token are never looked at)
+#pragma unroll 1
         for (int u = 0; u < kRounds; ++u) {
+          asm volatile("cp.async.wait_group %0;" ::"n"(kRounds - 1) : "memory");
           uint4 c[4];
 #pragma unroll
-          for (int j = 0; j < 4; ++j) c[j] = ld_shared(from + (u * 4 + j) * 2048);
+          for (int j = 0; j < 4; ++j) c[j] = ld_shared(mine + u * 2048 + j * 512);
+          const uint32_t by[2] = {__shfl_sync(0xFFFFFFFFu, f01, u * kGroups + grp), __shfl_sync(0xFFFFFFFFu, f23, u * kGroups + grp)};
           if (clear) {
             const uint32_t l4 = __shfl_sync(0xFFFFFFFFu, live, u * kGroups + grp);
 #pragma unroll
             for (int j = 0; j < 4; ++j)
               if (((l4 >> (8 * (j ^ odd))) & 1u) == 0u) c[j] = make_uint4(0, 0, 0, 0);
           }
-          const uint32_t by[2] = {__shfl_sync(0xFFFFFFFFu, f01, u * kGroups + grp), __shfl_sync(0xFFFFFFFFu, f23, u * kGroups + grp)};
 #pragma unroll
           for (int j = 0; j < 4; ++j) {
-            const uint32_t x = __byte_perm(by[j >> 1], 0u, ((j & 1) != 0) != (odd != 0) ? 0x3232 : 0x1010);
+            const uint32_t f = __byte_perm(by[j >> 1], 0u, ((j & 1) != 0) != (odd != 0) ? 0x3232 : 0x1010);
             uint32_t h[8];
-            halves4(c[j].x, x, h[0], h[1]);
-            halves4(c[j].y, x, h[2], h[3]);
-            halves4(c[j].z, x, h[4], h[5]);
-            halves4(c[j].w, x, h[6], h[7]);
+            halves4(c[j].x, f, h[0], h[1]);
+            halves4(c[j].y, f, h[2], h[3]);
+            halves4(c[j].z, f, h[4], h[5]);
+            halves4(c[j].w, f, h[6], h[7]);
             const uint32_t a = off[j] + to + u * (kGroups / 2) * kGroupBytes;
             st_shared(a, h[0], h[1], h[2], h[3]);
             st_shared(a ^ 16u, h[4], h[5], h[6], h[7]);
           }
+          if (nxt.there) fetch(nxt, row, u);
+          asm volatile("cp.async.commit_group;" ::: "memory");
         }
         fence_proxy_async();
         __syncwarp();
         // (the test hook of lr_plan_debug_set_phantom_bytes: a stage that is never full)
         if (lane == 0 && !(tc.phantom_tx_bytes != 0u && blockIdx.x == 0 && ring == 0)) mbar_arrive(&ctrl->kv_full[stage]);
-        ++ring;
-        return true;
-      };
-      for (int a = 0; a < ahead; ++a) {
-        if (a < n_pos) fetch(a, a, page_at(a));
-        asm volatile("cp.async.commit_group;" ::: "memory");
-      }
-      TileWords nxt = words_at(0, page_at(0));
-      int2 near = page_at(1);
-      int slot = 0;
-      for (int i = 0; i < n_pos; ++i) {
-        // Loads into registers are all asked for here and looked at a position later: a warp has few counters to wait for loads with, and a wait
-        // for an old one that shares a counter with a new one is a wait for both.
-        const TileWords cur = nxt;
-        nxt = words_at(i + 1, near);
-        near = page_at(i + 2);
-        const int2 far = page_at(i + ahead);
-        if (deep) asm volatile("cp.async.wait_group %0;" ::"n"(Sh::kDeepSlots - 1) : "memory");
-        else asm volatile("cp.async.wait_group %0;" ::"n"(Sh::kSlots - 1) : "memory");
-        ok = convert(cur, i, slot);
-        if (!ok) break;
-        if (i + ahead < n_pos) fetch(i + ahead, slot, far);
-        asm volatile("cp.async.commit_group;" ::: "memory");
-        slot = slot + 1 == ahead ? 0 : slot + 1;
       }
       asm volatile("cp.async.wait_group 0;" ::: "memory");  // (after an abort some are still on their way)
-      tiles += (uint32_t)n;
     }
   } else {
     asm volatile("setmaxnreg.inc.sync.aligned.u32 176;");
@@ -652,10 +678,10 @@ attn_fp8_kernel(DevBatch d, DevTcPlan tc, const uint16_t *__restrict__ q, Fp8Poo
       float sc_row = 0.f;
       if (ok) {
         // the queries, once the products of the piece before no longer read the buffers; with one M-tile each stream stores its part
-        ok = wait_bar(&ctrl->q_empty, ((uint32_t)(pc - piece0) & 1u) ^ 1u, ctrl, d.status, 245);
+        ok = wait(&ctrl->q_empty, ((uint32_t)(pc - piece0) & 1u) ^ 1u, ctrl, d.status, 245);
         if (ok) {
           const int h0 = mode == 2 || kHalves == 2 ? (mode == 2 ? 0 : s) : 0, h1 = mode == 2 ? kHalves : kHalves == 2 ? s + 1 : 1 - s;
-          sc_row = scale_log2 * pow2(convert_q<kD>(q, ri.q_index, smem_u32(q_smem) + (mode == 2 ? s : 0) * kTileBytes, r, h0, h1));
+          sc_row = scale_log2 * pow2(convert_q<kD>(q, ri.q_index, smem_u32(q_smem) + (mode == 2 ? s : 0) * kQBytes, r, h0, h1));
           fence_proxy_async();
           mbar_arrive(&ctrl->q_full);
         }
@@ -668,9 +694,9 @@ attn_fp8_kernel(DevBatch d, DevTcPlan tc, const uint16_t *__restrict__ q, Fp8Poo
         // it has (its commit precedes the s_full this thread has just seen), so o_done has completed done_needed or
         // done_needed - 1 phases and the parity says which, whether or not this thread has looked at the earlier ones.
         auto rescale_o = [&](float alpha, uint32_t done_needed) -> bool {
-          if (!wait_bar(&ctrl->o_done[s], (done_needed - 1) & 1u, ctrl, d.status, 235 + s)) return false;
+          if (!wait(&ctrl->o_done[s], (done_needed - 1) & 1u, ctrl, d.status, 235 + s)) return false;
           tc_fence_after();
-#pragma unroll
+#pragma unroll 1
           for (int ch = 0; ch < kD / 32; ++ch) {
             uint32_t o[32];
             tmem_ld32(o_addr + ch * 32, o);
@@ -687,15 +713,14 @@ attn_fp8_kernel(DevBatch d, DevTcPlan tc, const uint16_t *__restrict__ q, Fp8Poo
         const bool idle = __all_sync(0xFFFFFFFFu, ri.q_index < 0);
         if (idle) {
           for (int u = 0; u < 2 * my_units && ok; ++u) {
-            ok = wait_bar(&ctrl->s_full[s][u & 1], (s_cnt + (uint32_t)(u >> 1)) & 1u, ctrl, d.status, 230 + s);
-            if (ok && u + 1 == 2 * my_units) ok = wait_bar(&ctrl->o_done[s], (o_cnt + (uint32_t)u - 1) & 1u, ctrl, d.status, 237 + s);
+            ok = wait(&ctrl->s_full[s][u & 1], (s_cnt + (uint32_t)(u >> 1)) & 1u, ctrl, d.status, 230 + s);
+            if (ok && u + 1 == 2 * my_units) ok = wait(&ctrl->o_done[s], (o_cnt + (uint32_t)u - 1) & 1u, ctrl, d.status, 237 + s);
             if (ok) mbar_arrive(&ctrl->p_full[s][u & 1]);
           }
           s_cnt += (uint32_t)my_units;
         }
         for (int j = 0; j < my_units && ok && !idle; ++j) {
           const int local = mode == 2 ? j : 2 * j + s, t = pi.tile_begin + local;
-          const uint32_t at = (tiles + (uint32_t)local) % kInfos;
           const bool masked = t >= rq.n_dense_tiles;
           int n_ok[kPagesPerTile];
           if (masked) {
@@ -707,78 +732,70 @@ attn_fp8_kernel(DevBatch d, DevTcPlan tc, const uint16_t *__restrict__ q, Fp8Poo
               n_ok[2 * jj + 1] = page_n_ok(w.w, ri);
             }
           }
-          if (!s_ready) {
-            ok = wait_bar(&ctrl->info_full[at], ((tiles + (uint32_t)local) / kInfos) & 1u, ctrl, d.status, 248) &&
-                 wait_bar(&ctrl->s_full[s][0], s_cnt & 1u, ctrl, d.status, 230 + s);
-            if (!ok) break;
-          }
-          const Info info = ctrl->info[at];
-          const float sc = sc_row * pow2(info.k_ref - 127);
-          if (info.v_nan) nan_v = sees_nan(ctrl->v_nan[at], masked ? tc.pages + rq.page_off + t * kPagesPerTile : nullptr, ri) || nan_v;
-          if (j == 0) {
-            base = info.v_ref;
-          } else if (info.v_ref > base + kRise) {
-            ok = rescale_o(pow2(base - info.v_ref), o_cnt + (uint32_t)(2 * j));
-            if (!ok) break;
-            base = info.v_ref;
-          }
-          const int off = info.v_ref - base;
-          const float bias = (float)off + kHead;
 #pragma unroll 1  // one copy of the sweep: the unrolled pair is slower (instruction fetch)
           for (int half = 0; half < 2; ++half) {
             const uint32_t sh_addr = s_addr + half * 64;
             const uint32_t g = o_cnt + (uint32_t)(2 * j + half);  // half-units of this stream before this one
+            const uint32_t at = (tiles + (uint32_t)local) * 2 + half;  // half-tiles of both streams before this one
             const bool first = (j | half) == 0;
-            if (half == 1 && !s_ready) {
-              ok = wait_bar(&ctrl->s_full[s][1], s_cnt & 1u, ctrl, d.status, 230 + s);
+            if (!s_ready) {
+              ok = wait(&ctrl->info_full[at % kInfos], (at / kInfos) & 1u, ctrl, d.status, 248) &&
+                   wait(&ctrl->s_full[s][half], s_cnt & 1u, ctrl, d.status, 230 + s);
               if (!ok) break;
             }
             tc_fence_after();
+            const Info info = ctrl->info[at % kInfos];
+            if (info.v_nan)
+              nan_v = sees_nan(ctrl->v_nan[at % kInfos], masked ? tc.pages + rq.page_off + t * kPagesPerTile + half * 4 : nullptr, ri) || nan_v;
             uint32_t v[64];
             tmem_ld64(sh_addr, v);
+            float alpha = 1.0f;  // what O has to be multiplied by before this half's product
+            if (first) base = info.v_ref;
+            if (info.v_ref > base + kRise) {
+              alpha = pow2(base - info.v_ref);
+              base = info.v_ref;
+            }
+            const float sc = sc_row * pow2(info.k_ref - 127);
+            const int off = info.v_ref - base;
+            const float bias = (float)off + kHead;
+            bool apart = off < -kApart;  // the sums first, of weights as they are
             tc_wait_ld();
-            // the scores after these (and what is known of their tile) are looked for under the exponentials: a test costs over 100 cycles even
+            // the scores after these (and what is known of their keys) are looked for under the exponentials: a test costs over 100 cycles even
             // when it succeeds
-            uint32_t next_ready;
-            if (half == 0) {
-              next_ready = mbar_test_wait(&ctrl->s_full[s][1], s_cnt & 1u);
-            } else {
-              const uint32_t next = tiles + (uint32_t)local + (mode == 2 ? 1u : 2u);
-              next_ready = mbar_test_wait2(&ctrl->s_full[s][0], (s_cnt + 1u) & 1u, &ctrl->info_full[next % kInfos], (next / kInfos) & 1u) == 3u;
-            }
+            const uint32_t next = half == 0 ? at + 1u : (tiles + (uint32_t)local + (mode == 2 ? 1u : 2u)) * 2u;
+            const uint32_t next_ready = mbar_test_wait2(&ctrl->s_full[s][half ^ 1], (s_cnt + (uint32_t)half) & 1u, &ctrl->info_full[next % kInfos],
+                                                        (next / kInfos) & 1u) == 3u;
             if (masked) mask_half(v, n_ok + 4 * half);
-            float sum = 0.f, mx, raw;
-            // Fast path: exponentials against the running reference exponent; the maximum of the 64 scores is computed beside them and only
-            // checked afterwards.
-            bool fast = __all_sync(0xFFFFFFFFu, m_used > -INFINITY);
-            if (fast) {
-              sum = exp_half<true>(v, sh_addr, sc, bias - m_used, raw);
-              mx = raw * sc;
-              if (__any_sync(0xFFFFFFFFu, mx > m_used + kGrow)) fast = false;  // beyond what a half holds: once more
-            } else {
-              mx = max_half(v) * sc;
-            }
-            if (!fast) {
-              const bool grow = mx > m_used + kGrow || m_used == -INFINITY;
-              const float alpha = grow && m_used > -INFINITY ? ex2(m_used - mx) : 1.0f;
-              if (grow) {
-                l *= alpha;
-                m_used = mx;
+            // Exponentials against the running reference exponent, the maximum of the 64 scores beside them.  Where that is beyond what a half holds
+            // (and on a row's first keys) they are done again with the reference moved to it.
+            for (;;) {
+              float raw;
+              const float sum = exp_half(v, sh_addr, sc, m_used == -INFINITY ? 0.f : (apart ? 0.f : bias) - m_used, raw), mx = raw * sc;
+              const bool grow = mx > m_used + kGrow;  // (a row that has seen nothing: by any score)
+              if (__any_sync(0xFFFFFFFFu, grow)) {
+                if (grow) {
+                  if (m_used > -INFINITY) {
+                    const float down = ex2(m_used - mx);
+                    alpha *= down;
+                    l *= down;
+                  }
+                  m_used = mx;
+                }
+                tc_wait_st();
+                continue;
               }
-              if (!first && __any_sync(0xFFFFFFFFu, alpha != 1.0f)) {
-                ok = rescale_o(alpha, g);
-                if (!ok) break;
+              if (apart) {
+                l += sum;
+                apart = false;
+                tc_wait_st();
+                continue;
               }
-              tc_wait_st();
-              sum = exp_half<false>(v, sh_addr, sc, (m_used == -INFINITY) ? 0.f : bias - m_used, raw);
+              if (off >= -kApart) l = fmaf(sum, pow2(-off - (int)kHead), l);
+              break;
             }
-            if (off >= -kApart) {
-              l = fmaf(sum, pow2(-off - (int)kHead), l);
-            } else {  // (the scores themselves are gone from tensor memory, but not from the registers)
-              float apart = 0.f;
-#pragma unroll
-              for (int i = 0; i < 64; ++i) apart += ex2(fmaf(bits_f(v[i]), sc, m_used == -INFINITY ? 0.f : -m_used));
-              l += apart;
+            if (!first && __any_sync(0xFFFFFFFFu, alpha != 1.0f)) {
+              ok = rescale_o(alpha, g);
+              if (!ok) break;
             }
             tc_wait_st();
             tc_fence_before();
@@ -786,7 +803,7 @@ attn_fp8_kernel(DevBatch d, DevTcPlan tc, const uint16_t *__restrict__ q, Fp8Poo
             // The wait at the end must not find o_done two phases back (one parity for both): the last arrive comes
             // after the product before has been seen to retire.
             if (half == 1 && j + 1 == my_units) {
-              ok = wait_bar(&ctrl->o_done[s], (g - 1) & 1u, ctrl, d.status, 237 + s);
+              ok = wait(&ctrl->o_done[s], (g - 1) & 1u, ctrl, d.status, 237 + s);
               if (!ok) break;
             }
             mbar_arrive(&ctrl->p_full[s][half]);
@@ -796,7 +813,7 @@ attn_fp8_kernel(DevBatch d, DevTcPlan tc, const uint16_t *__restrict__ q, Fp8Poo
         if (ok) {
           // epilogue: wait for the last PV of this stream, then normalise and store
           o_cnt += 2u * (uint32_t)my_units;
-          ok = wait_bar(&ctrl->o_done[s], (o_cnt - 1) & 1u, ctrl, d.status, 240 + s);
+          ok = wait(&ctrl->o_done[s], (o_cnt - 1) & 1u, ctrl, d.status, 240 + s);
         }
         // what the accumulator's numbers are worth; NaN for a row that sees a row of V that is
         const float unit = nan_v ? __uint_as_float(0x7FC00000u) : exp2f((float)(base - 127) - kHead);
@@ -815,7 +832,7 @@ attn_fp8_kernel(DevBatch d, DevTcPlan tc, const uint16_t *__restrict__ q, Fp8Poo
             mbar_arrive(&ctrl->xch);
             writer = false;
           } else {
-            ok = wait_bar(&ctrl->xch, x_cnt & 1u, ctrl, d.status, 242);
+            ok = wait(&ctrl->xch, x_cnt & 1u, ctrl, d.status, 242);
             if (ok) {
               tc_fence_after();
               const float om = ctrl->xch_m[r], ol = ctrl->xch_l[r];
@@ -839,7 +856,7 @@ attn_fp8_kernel(DevBatch d, DevTcPlan tc, const uint16_t *__restrict__ q, Fp8Poo
       // One arrival per thread and piece.  A stream with units in this piece cannot get here before the previous
       // piece's phase is complete (its PV products were issued behind a wait for it); a stream with none must look
       // itself, or its arrival would be counted into the previous phase while the other stream is still storing.
-      if (my_units == 0 && pc > piece0 && ok) ok = wait_bar(&ctrl->epi_done, (uint32_t)(pc - piece0 - 1) & 1u, ctrl, d.status, 243);
+      if (my_units == 0 && pc > piece0 && ok) ok = wait(&ctrl->epi_done, (uint32_t)(pc - piece0 - 1) & 1u, ctrl, d.status, 243);
       mbar_arrive(&ctrl->epi_done);
       tiles += (uint32_t)n;
     }

@@ -1,5 +1,5 @@
 // What the single-CTA tensor-core attention kernels share (attn_tc.cu, attn_fp8.cu): mbarriers and tcgen05 in inline PTX, the bounded
-// waits, the order of the ring of tiles, and which keys a query row sees.
+// waits, and which keys a query row sees.
 #pragma once
 
 #include <cuda.h>
@@ -181,28 +181,7 @@ __device__ __forceinline__ bool wait_bar(uint64_t *bar, uint32_t parity, Ctrl *c
   return __all_sync(0xFFFFFFFFu, wait_bar_lane(bar, parity, ctrl, status, code)) != 0;
 }
 
-// ---- ring order ----------------------------------------------------------------------
-// Within a piece of n tiles the producer emits K and V tiles in the order the MMA issuers first
-// touch them.  With la = K tiles issued ahead of the first PV (1 for two M-tiles, 2 for the
-// even/odd split): K(0..min(la,n)-1), then for u = 0..n-1: V(u), and K(u+la) while u+la < n.
-struct RingOrder {
-  int n, la, la_c, np;  // np = number of (V, K) pairs
-  __device__ __forceinline__ RingOrder(int n_, int mode) : n(n_), la(mode == 2 ? 1 : 2) {
-    la_c = min(la, n);
-    np = max(0, n - la);
-  }
-  __device__ __forceinline__ int pos_k(int t) const { return t < la ? t : la_c + 2 * (t - la) + 1; }
-  __device__ __forceinline__ int pos_v(int u) const { return u < np ? la_c + 2 * u : la_c + 2 * np + (u - np); }
-  // step i (= ring position within the piece) of the 2n steps -> tile, and whether it is a V tile
-  __device__ __forceinline__ int step(int i, bool &is_v) const {
-    if (i < la_c) { is_v = false; return i; }
-    const int j = i - la_c;
-    if (j < 2 * np) { is_v = !(j & 1); return (j >> 1) + ((j & 1) ? la : 0); }
-    is_v = true;
-    return np + (j - 2 * np);
-  }
-};
-
+// ---- which keys a row sees ------------------------------------------------------------
 struct RowInfo {
   int depth;       // depth-first number of the node the row's branch continues (on a chain: segments it sees); -1 for padding rows
   int branch;      // local branch index within the request; -1 for padding rows

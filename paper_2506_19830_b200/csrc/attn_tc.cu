@@ -144,6 +144,28 @@ constexpr uint32_t kIdescQK = kIdescBase | ((64u >> 3) << 17);
 template <int kD>
 constexpr uint32_t kIdescPV = kIdescBase | (((uint32_t)kD >> 3) << 17) | (1u << 16);
 
+// ---- ring order ----------------------------------------------------------------------
+// Within a piece of n tiles the producer emits K and V tiles in the order the MMA issuers first
+// touch them.  With la = K tiles issued ahead of the first PV (1 for two M-tiles, 2 for the
+// even/odd split): K(0..min(la,n)-1), then for u = 0..n-1: V(u), and K(u+la) while u+la < n.
+struct RingOrder {
+  int n, la, la_c, np;  // np = number of (V, K) pairs
+  __device__ __forceinline__ RingOrder(int n_, int mode) : n(n_), la(mode == 2 ? 1 : 2) {
+    la_c = min(la, n);
+    np = max(0, n - la);
+  }
+  __device__ __forceinline__ int pos_k(int t) const { return t < la ? t : la_c + 2 * (t - la) + 1; }
+  __device__ __forceinline__ int pos_v(int u) const { return u < np ? la_c + 2 * u : la_c + 2 * np + (u - np); }
+  // step i (= ring position within the piece) of the 2n steps -> tile, and whether it is a V tile
+  __device__ __forceinline__ int step(int i, bool &is_v) const {
+    if (i < la_c) { is_v = false; return i; }
+    const int j = i - la_c;
+    if (j < 2 * np) { is_v = !(j & 1); return (j >> 1) + ((j & 1) ? la : 0); }
+    is_v = true;
+    return np + (j - 2 * np);
+  }
+};
+
 // The weights of a half as they go to tensor memory; with several terms 16 columns (32 weights) at a time, so that no more
 // than these sit in registers beside the scores (which a redo needs again).  Column c of a term holds the weights 2c and 2c + 1.  With three
 // terms each is the leading eight bits of what the terms before it leave: cut off, not rounded, which takes one
