@@ -4,29 +4,30 @@
 // streams of a CTA, the issuers and the score buffers in tensor memory.  What is different is how K and V get into shared memory and
 // what the products are made of.
 //
-// Halves.  The products are f16 x f16 -> fp32.  An e4m3 code is an f16 number, and one instruction turns two codes into two halves; a bf16
-// operand would take five.  Scales are powers of two, and only differences of exponents go into a tile: with ref the largest scale byte
-// of the tile's keys, a row enters as code * 2^(byte - ref), exact unless it lies 2^-33 below the largest number of the tile.  2^(ref - 127) itself
-// goes where it costs nothing:
-//   K: into the factor that takes scores to exponents (one number a row and tile);
-//   V: into the exponent of the weights, P 2^(ref - base), where base is the stream's: the accumulator is in units of 2^(base - 127).  When a
-//      tile's ref is more than 2^3 above base the accumulator is scaled down, as when the maximum grows; the row sums take the factor
-//      back out.  A tile far below base (2^-24) sums its weights apart, as keys whose values are all zeros may have any weight.
-//   Q: a row is scaled by a power of two to lie below 4, which goes into the same factor as K's.
-// The weights are f16 as well, 2^6 above the row's reference and at most 2^15: 11 bits instead of bf16's 8, nothing lost above 2^-20 of the
+// Scores.  S = Q K^T is an e4m3 x e4m3 product: K goes from the cache into shared memory as it is, by TMA.  Q comes in two terms, hi = the e4m3
+// numbers nearest to the row (scaled by a power of two to just fit) and lo = what that leaves: bf16 has eight bits, each term holds four, so the
+// two are the row itself wherever it is above 2^-10 of its largest number, and off by 2^-19 of that elsewhere.  Two products at twice f16's rate
+// take what one would.  A key's scale multiplies its column of S, before masks and maximum.
+//
+// Weights and V are f16.  One instruction turns two codes into two halves; a bf16 operand would take five.  Scales being powers of two, only differences
+// of exponents go into a tile: with ref the largest scale byte of a half-tile's keys, a row of V enters as code * 2^(byte - ref), exact unless it lies
+// 2^-33 below the largest number of the half-tile.  2^(ref - 127) itself goes into the exponent of the weights, P 2^(ref - base), where base is the
+// stream's: the accumulator is in units of 2^(base - 127).  When ref is more than 2^3 above base the accumulator is scaled down, as when the maximum
+// grows; the row sums take the factor back out.  A half-tile far below base (2^-24) sums its weights apart, as keys whose values are all zeros
+// may have any weight.  Weights lie 2^6 above what they are and reach 2^15 at most: 11 bits instead of bf16's 8, nothing lost above 2^-20 of the
 // largest, and a row whose scores grow by more than 2^6 does its half-tile again.
 //
 // One CTA = 16 warps in four warpgroups, registers moved with setmaxnreg (176 x 256 + 80 x 256 = 128 x 512):
-//   warps 8-11  converters.  No staging: a thread loads its codes (16 bytes of eight keys of a tile; four with head size 64) straight into registers,
-//               two tiles (four) ahead -- 32 KB in flight an SM -- turns them into halves and stores them as the swizzled operand.  Through
-//               shared memory they would cross it twice more, and it is as busy as the tensor cores: 32 KB of a tile written and
-//               read by the products, and Q read again for every 64 keys.  A warp has the tile's 128 scale bytes in one word a lane, so that
-//               ref is one reduction and a key's byte one shuffle.  Slots that hold no valid token become zeros, whatever they held.
+//   warp 14      producer: per tile of 128 keys 8 boxes of K (a page each), the keys' scales as fp32, ref of V's half-tiles.
+//   warps 8-11, 15  converters: the codes of a half-tile of V (64 keys) by asynchronous copies into a buffer of the warp's own, the next one's taking the
+//                place of each part as it is read; halves into the ring as the swizzled operand.  A warp has the half-tile's scale bytes in one word
+//                a lane, so that ref is one reduction and a key's factor one shuffle.  Slots that hold no valid token become zeros, whatever they held.
 //   warps 12, 13  MMA issuers of stream 0 and 1.
-//   warps 0-3, 4-7  softmax of stream 0 and 1, one thread per query row; they also turn the rows of Q into halves.
+//   warps 0-3, 4-7  softmax of stream 0 and 1, one thread per query row; they also turn the rows of Q into their two terms.
+// All of it shares an SM's instruction cache; a version with everything unrolled and in line, K converted to halves as well, took three times as long.
 //
-// A visible row that stands for NaN: K's becomes NaN as an operand, and with it the row's sum.  V's becomes zeros, for a weight of 0 times NaN
-// would reach rows that do not see it; the converters note such keys per tile, and a row that sees one multiplies its result by NaN.
+// A visible row that stands for NaN: K's has a scale of NaN, and with it the row's sum is.  V's becomes zeros, for a weight of 0 times NaN
+// would reach rows that do not see it; the producer notes such keys per tile, and a row that sees one multiplies its result by NaN.
 #include <cuda.h>
 
 #include <algorithm>
@@ -38,12 +39,14 @@ namespace lr {
 
 namespace {
 
-constexpr int kHalfBytes = 16384;  // 128 rows of Q x 64 channels
-constexpr int kAtomBytes = 1024;   // 8 keys x 64 channels, one 128-byte-swizzle atom
-constexpr int kMaxStages = 16;
+constexpr int kAtomBytes = 1024;   // 8 keys of V x 64 channels as halves, one 128-byte-swizzle atom
+constexpr int kMaxK = 8, kMaxV = 8;
 constexpr int kThreads = 512;
-constexpr int kTeams = 6;          // converter warps, each with half-tiles of its own
-constexpr int kInfos = 16;         // half-tiles whose scales are published ahead of their products; more than the ring can hold
+constexpr int kTeams = 5;          // converter warps, each with half-tiles of its own
+// Tiles whose scales are published ahead of their products.  The producer writes those of tile x + kInfos once the stage of K that it takes is
+// free, which tile x + kInfos - kKStages / 2 had; from x + 3 on, that tells that no softmax thread will look at x again (an issuer asks for or
+// skips x + 3 behind the weights of its last half-tile up to x).
+constexpr int kInfos = 8;
 constexpr float kGrow = 6.0f;      // log2: how far the scores of a row may rise above its reference exponent
 constexpr float kHead = 6.0f;      // log2: weights are kept this much above what they are
 constexpr int kRise = 3;           // log2: ... and V's half-tiles this much above the accumulator's unit: 6 + 6 + 3 = 15, f16 ends at 16
@@ -52,24 +55,27 @@ constexpr int kApart = 24;         // log2: V this far below the unit has its we
 template <int kD>
 struct Shape {
   static_assert(kD == 64 || kD == 128, "head sizes of the tensor-core path");
-  static constexpr int kHalves = kD / 64;                   // 64-channel halves of a row (one 128-byte swizzle line each)
-  static constexpr int kQBytes = kHalves * kHalfBytes;      // an M-tile of Q: [halves][128 rows][128 B]
-  static constexpr int kGroupBytes = kHalves * kAtomBytes;  // the atoms of one 8-key group
-  static constexpr int kStageBytes = 8 * kGroupBytes;       // 64 keys as halves: [8 groups][halves][8 keys][128 B]
-  static constexpr int kStages = kD == 128 ? 7 : 16;
+  static constexpr int kHalves = kD / 64;                   // 64-channel halves of a row of V (one 128-byte swizzle line each)
+  static constexpr int kTermBytes = 128 * kD;               // a term of an M-tile of Q: 128 rows of kD bytes
+  static constexpr int kQBytes = 2 * kTermBytes;
+  static constexpr int kCodeBytes = 64 * kD;                // a half-tile (64 keys) as it comes
+  static constexpr int kGroupBytes = kHalves * kAtomBytes;  // the atoms of 8 keys of V
+  static constexpr int kVBytes = 8 * kGroupBytes;           // a half-tile of V as halves: [8 groups][halves][8 keys][128 B]
+  static constexpr int kKStages = kD == 128 ? 4 : 8, kVStages = kD == 128 ? 5 : 8;
   static constexpr int kCols = kD / 16;                     // lanes side by side in a row, 16 channels each
   static constexpr int kGroups = 32 / kCols;                // groups of four keys that a warp has at a time
   static constexpr int kRounds = 16 / kGroups;              // ... and how many times for a half-tile
-  static constexpr int kCodeBytes = 64 * kD;                // a half-tile as it comes
 };
 
-struct Info {  // of a half-tile: the largest scale bytes of its keys; whether some valid row of V stands for NaN
-  int32_t k_ref, v_ref, v_nan;
+struct Info {  // of a tile: largest scale bytes of V's half-tiles; whether some valid row of V stands for NaN; the keys' scales
+  float k_scale[128];
+  int32_t v_ref[2], v_nan, pad;
 };
 
 struct __align__(16) Ctrl {
   TcCtaHead head;         // this CTA's record
-  uint64_t kv_full[kMaxStages], kv_empty[kMaxStages];
+  Info info[kInfos];
+  uint64_t k_full[kMaxK], k_empty[kMaxK], v_full[kMaxV], v_empty[kMaxV];
   uint64_t q_full, q_empty;
   uint64_t s_full[2][2], p_full[2][2], o_done[2];  // [stream][half]
   uint64_t epi_done, drain[2];
@@ -78,51 +84,51 @@ struct __align__(16) Ctrl {
   uint32_t tmem_base;
   int abort_flag;
   uint64_t wait_limit_ns;
-  Info info[kInfos];
-  uint8_t v_nan[kInfos][16];  // four keys a byte
+  uint8_t v_nan[kInfos][32];  // four keys a byte
   float xch_m[128], xch_l[128], xch_unit[128];  // stream 1's rows, for the in-CTA combination
 };
-constexpr int kCtrlBytes = 3 << 10;
+constexpr int kCtrlBytes = 7 << 10;
 static_assert(sizeof(Ctrl) <= kCtrlBytes, "Ctrl must fit behind the tiles");
 template <int kD>
-constexpr int kSmemBytes = 2 * Shape<kD>::kQBytes + Shape<kD>::kStages * Shape<kD>::kStageBytes + kTeams * Shape<kD>::kCodeBytes + kCtrlBytes;  // the base must be 1024-aligned
+constexpr int kSmemBytes = 2 * Shape<kD>::kQBytes + Shape<kD>::kKStages * Shape<kD>::kCodeBytes + Shape<kD>::kVStages * Shape<kD>::kVBytes +
+                           kTeams * Shape<kD>::kCodeBytes + kCtrlBytes;  // the base must be 1024-aligned
+static_assert(kInfos - Shape<64>::kKStages / 2 >= 3 && kInfos - Shape<128>::kKStages / 2 >= 3, "see kInfos");
+// A converter at position r has filled position r - kTeams, whose stage position r - kTeams - kVStages had been released from.  Releases are in order, so
+// with no more teams than stages the release before the one it waits for has happened, and the parity of the barrier means what it looks for.
+static_assert(kTeams <= Shape<64>::kVStages && kTeams <= Shape<128>::kVStages, "a converter must not be two phases of a stage ahead");
 static_assert(kSmemBytes<64> <= 227 * 1024 && kSmemBytes<128> <= 227 * 1024, "shared memory per CTA");
 
-// ---- ring order ----------------------------------------------------------------------
-// The ring holds half-tiles (64 keys of K or of V).  Within a piece of n tiles they come in the order the issuers first touch them.  With la = tiles of K
-// issued ahead of the first PV (1 for two M-tiles, 2 for the even/odd split): both halves of K(0..min(la,n)-1), then for every u with u + la < n
-// V(u)a, K(u+la)a, V(u)b, K(u+la)b, then what is left of V.
-struct HalfOrder {
-  int la, la_c, np;  // np = number of (V, K) pairs
-  __device__ __forceinline__ HalfOrder(int n, int mode) : la(mode == 2 ? 1 : 2) {
-    la_c = min(la, n);
-    np = max(0, n - la);
-  }
-  __device__ __forceinline__ int k(int t, int half) const { return t < la ? 2 * t + half : 2 * la_c + 4 * (t - la) + 2 * half + 1; }
-  __device__ __forceinline__ int v(int u, int half) const { return u < np ? 2 * la_c + 4 * u + 2 * half : 2 * la_c + 4 * np + 2 * (u - np) + half; }
-  // place i of the 4n of a piece -> tile, half, and whether it is V's
-  __device__ __forceinline__ int at(int i, int &half, bool &is_v) const {
-    half = i & 1;
-    is_v = false;
-    if (i < 2 * la_c) return i >> 1;
-    i -= 2 * la_c;
-    if (i < 4 * np) {
-      half = (i >> 1) & 1;
-      is_v = !(i & 1);
-      return (i >> 2) + (is_v ? 0 : la);
-    }
-    i -= 4 * np;
-    half = i & 1;
-    is_v = true;
-    return np + (i >> 1);
-  }
-};
-
-// Instruction descriptors: D fp32, A and B f16 (format 0), M = 128; QK: N = 64 keys, both operands K-major; PV: N = head size, B N-major.
+// Instruction descriptors: D fp32, M = 128; QK: A and B e4m3 (format 0 of kind::f8f6f4), N = 64 keys, both operands K-major; PV: A and B f16 (format 0
+// of kind::f16), N = head size, B N-major.
 constexpr uint32_t kIdescBase = (1u << 4) | (8u << 24);
 constexpr uint32_t kIdescQK = kIdescBase | ((64u >> 3) << 17);
 template <int kD>
 constexpr uint32_t kIdescPV = kIdescBase | (((uint32_t)kD >> 3) << 17) | (1u << 16);
+
+__device__ __forceinline__ void mma_f8(uint32_t d_tmem, uint64_t adesc, uint64_t bdesc, uint32_t idesc, uint32_t acc) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
+      "tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], %1, %2, %3, p;\n\t}" ::"r"(d_tmem),
+      "l"(adesc), "l"(bdesc), "r"(idesc), "r"(acc)
+      : "memory");
+}
+// Descriptor of a K-major operand of rows of kD bytes: the swizzle spans a row (128 or 64 bytes), groups of eight rows lie one after another.
+template <int kD>
+__device__ __forceinline__ uint64_t make_row_desc(uint32_t addr) {
+  return (uint64_t)((addr & 0x3FFFFu) >> 4) | ((uint64_t)1 << 16) | ((uint64_t)(8 * kD >> 4) << 32) | (1ull << 46) |
+         ((uint64_t)(kD == 128 ? 2 : 4) << 61);
+}
+// the place of 16-byte unit u of row r in such an operand
+template <int kD>
+__device__ __forceinline__ uint32_t row_unit(int r, int u) {
+  return (uint32_t)(r * kD + ((u ^ (kD == 128 ? r & 7 : (r >> 1) & 3)) << 4));
+}
+
+__device__ __forceinline__ void tma_load_2d(uint32_t dst, const CUtensorMap *map, int32_t x, int32_t y, uint64_t *bar) {
+  asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4}], [%2];" ::"r"(dst), "l"(map),
+               "r"(smem_u32(bar)), "r"(x), "r"(y)
+               : "memory");
+}
 
 // Five roles share an SM's instruction cache, and warps that wait for instructions were what bounded a version of this kernel that had everything
 // unrolled: what is long is in a loop, and what is rare out of the way.  The bounded wait of a whole warp (as wait_bar):
@@ -148,6 +154,18 @@ __device__ __forceinline__ bool wait(uint64_t *bar, uint32_t parity, Ctrl *ctrl,
 __device__ __forceinline__ uint32_t pack_f16(float lo, float hi) {
   uint32_t r;
   asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+  return r;
+}
+__device__ __forceinline__ void mul2(uint32_t &a, uint32_t &b, float x, float y) {  // a *= x, b *= y
+  asm("{\n\t.reg .b64 r, t;\n\tmov.b64 r, {%0, %1};\n\tmov.b64 t, {%2, %3};\n\tmul.rn.f32x2 r, r, t;\n\tmov.b64 {%0, %1}, r;\n\t}"
+      : "+r"(a), "+r"(b)
+      : "f"(x), "f"(y));
+}
+__device__ __forceinline__ uint32_t pack_e4m3(float a, float b, float c, float d) {
+  uint32_t r;
+  asm("{\n\t.reg .b16 lo, hi;\n\tcvt.rn.satfinite.e4m3x2.f32 lo, %2, %1;\n\tcvt.rn.satfinite.e4m3x2.f32 hi, %4, %3;\n\tmov.b32 %0, {lo, hi};\n\t}"
+      : "=r"(r)
+      : "f"(a), "f"(b), "f"(c), "f"(d));
   return r;
 }
 __device__ __forceinline__ float pow2(int e) { return __uint_as_float((uint32_t)(min(max(e, -126), 127) + 127) << 23); }
@@ -201,10 +219,10 @@ __device__ __forceinline__ float exp_half(const uint32_t (&v)[64], uint32_t addr
   return acc0.x + acc0.y;
 }
 
-// Whether the row sees a key of the half-tile whose row of V stands for NaN.  pages: null where it sees all keys.
+// Whether the row sees a key of the tile whose row of V stands for NaN.  pages: null where it sees all keys.
 __device__ __noinline__ bool sees_nan(const uint8_t *nan4, const TcPage *pages, RowInfo ri) {
   bool seen = false;
-  for (int p = 0; p < kPagesPerTile / 2; ++p) {
+  for (int p = 0; p < kPagesPerTile; ++p) {
     const uint32_t w = *reinterpret_cast<const volatile uint32_t *>(nan4 + 4 * p);  // a byte of it: four keys
     const uint32_t keys = (w & 15u) | ((w >> 4) & 0xF0u) | ((w >> 8) & 0xF00u) | ((w >> 12) & 0xF000u);
     const int n = pages != nullptr ? page_n_ok(pages[p].meta, ri) : kPage;
@@ -213,9 +231,10 @@ __device__ __noinline__ bool sees_nan(const uint8_t *nan4, const TcPage *pages, 
   return seen;
 }
 
-// A row of Q, scaled by a power of two to lie below 4, as halves into the channel halves [h0, h1) of its M-tile; returns the exponent taken out.
+// A row of Q, scaled by a power of two to lie within 448, as its two e4m3 terms (those of [t0, t1) are stored); returns 2 to the exponent taken out, or NaN for
+// a row that is not finite (its scores are no numbers either).
 template <int kD>
-__device__ __noinline__ int convert_q(const uint16_t *__restrict__ q, int64_t q_index, uint32_t tile, int r, int h0, int h1) {
+__device__ __noinline__ float convert_q(const uint16_t *__restrict__ q, int64_t q_index, uint32_t tile, int r, int t0, int t1) {
   uint4 x[kD / 8];
 #pragma unroll
   for (int i = 0; i < kD / 8; ++i) x[i] = q_index >= 0 ? __ldg(reinterpret_cast<const uint4 *>(q + q_index * kD) + i) : make_uint4(0, 0, 0, 0);
@@ -224,18 +243,24 @@ __device__ __noinline__ int convert_q(const uint16_t *__restrict__ q, int64_t q_
   for (int i = 0; i < kD / 8; ++i)
     top = __vmaxu2(top, __vmaxu2(__vmaxu2(x[i].x & 0x7FFF7FFFu, x[i].y & 0x7FFF7FFFu), __vmaxu2(x[i].z & 0x7FFF7FFFu, x[i].w & 0x7FFF7FFFu)));
   top = max(top & 0xFFFFu, top >> 16);
-  const int e = top < 0x7F80u ? min(max((int)(top >> 7) - 127, -126), 126) : 0;
+  const int e = min(max((int)(top >> 7) - 135 + ((top & 0x7Fu) > 0x60u ? 1 : 0), -126), 120);  // as lr_fp8_write
   const float by = pow2(-e);
 #pragma unroll
-  for (int i = 0; i < kD / 8; ++i) {
-    if (i / 8 < h0 || i / 8 >= h1) continue;
-    const uint32_t w[4] = {x[i].x, x[i].y, x[i].z, x[i].w};
-    uint32_t o[4];
+  for (int u = 0; u < kD / 16; ++u) {
+    const uint32_t w[8] = {x[2 * u].x, x[2 * u].y, x[2 * u].z, x[2 * u].w, x[2 * u + 1].x, x[2 * u + 1].y, x[2 * u + 1].z, x[2 * u + 1].w};
+    uint32_t hi[4], lo[4];
 #pragma unroll
-    for (int j = 0; j < 4; ++j) o[j] = pack_f16(bits_f(w[j] << 16) * by, bits_f(w[j] & 0xFFFF0000u) * by);
-    st_shared(tile + (i / 8) * kHalfBytes + r * 128 + (((i & 7) ^ (r & 7)) << 4), o[0], o[1], o[2], o[3]);
+    for (int j = 0; j < 4; ++j) {
+      const float a = bits_f(w[2 * j] << 16) * by, b = bits_f(w[2 * j] & 0xFFFF0000u) * by, c = bits_f(w[2 * j + 1] << 16) * by,
+                  d = bits_f(w[2 * j + 1] & 0xFFFF0000u) * by;
+      hi[j] = pack_e4m3(a, b, c, d);
+      const float2 ab = fp8_float2(hi[j] & 0xFFFFu), cd = fp8_float2(hi[j] >> 16);
+      lo[j] = pack_e4m3(a - ab.x, b - ab.y, c - cd.x, d - cd.y);
+    }
+    if (t0 == 0) st_shared(tile + row_unit<kD>(r, u), hi[0], hi[1], hi[2], hi[3]);
+    if (t1 == 2) st_shared(tile + Shape<kD>::kTermBytes + row_unit<kD>(r, u), lo[0], lo[1], lo[2], lo[3]);
   }
-  return e;
+  return top < 0x7F80u ? pow2(e) : __uint_as_float(0x7FC00000u);
 }
 
 // The store epilogue of a softmax thread: row r of the accumulator at o_addr times `self` (and, when the CTA's two streams worked on the same
@@ -295,8 +320,8 @@ __device__ __noinline__ void store_rows(uint32_t o_addr, uint32_t o_other, int s
   }
 }
 
-struct Fp8Pools {
-  const uint8_t *k, *v, *k_scale, *v_scale;
+struct Fp8Pools {  // K's codes are behind a tensor map
+  const uint8_t *v, *k_scale, *v_scale;
 };
 
 __device__ __forceinline__ uint32_t valid_bytes(int valid, int lane) {  // of the four keys of this lane's word
@@ -308,10 +333,10 @@ __device__ __forceinline__ uint32_t top_byte(uint32_t bytes) {
   const uint32_t w = bytes & ~__vcmpeq4(bytes, 0xFFFFFFFFu), t = __vmaxu4(w, w >> 16);
   return max(t & 0xFFu, (t >> 8) & 0xFFu);
 }
-// 2^(byte - ref) of two keys, as halves; `nan`: what a byte of 255 gives
-__device__ __forceinline__ uint32_t factors(uint32_t b0, uint32_t b1, int ref, float nan) {
+// 2^(byte - ref) of two keys, as halves; 0 for a row that stands for NaN
+__device__ __forceinline__ uint32_t factors(uint32_t b0, uint32_t b1, int ref) {
   const float f0 = __uint_as_float((uint32_t)max((int)b0 - ref + 127, 0) << 23), f1 = __uint_as_float((uint32_t)max((int)b1 - ref + 127, 0) << 23);
-  return pack_f16(b0 == kFp8NanScale ? nan : f0, b1 == kFp8NanScale ? nan : f1);
+  return pack_f16(b0 == kFp8NanScale ? 0.f : f0, b1 == kFp8NanScale ? 0.f : f1);
 }
 // four codes times a key's factor, as four halves
 __device__ __forceinline__ void halves4(uint32_t c, uint32_t by, uint32_t &lo, uint32_t &hi) {
@@ -323,10 +348,11 @@ __device__ __forceinline__ void halves4(uint32_t c, uint32_t by, uint32_t &lo, u
 
 template <int kD>
 __global__ void __launch_bounds__(kThreads, 1)
-attn_fp8_kernel(DevBatch d, DevTcPlan tc, const uint16_t *__restrict__ q, Fp8Pools in, uint16_t *__restrict__ out, float *__restrict__ lse,
+attn_fp8_kernel(const __grid_constant__ CUtensorMap k_map, DevBatch d, DevTcPlan tc, const uint16_t *__restrict__ q, Fp8Pools in, uint16_t *__restrict__ out, float *__restrict__ lse,
                 float scale_log2) {
   using Sh = Shape<kD>;
-  constexpr int kQBytes = Sh::kQBytes, kStageBytes = Sh::kStageBytes, kGroupBytes = Sh::kGroupBytes, kStages = Sh::kStages, kHalves = Sh::kHalves;
+  constexpr int kQBytes = Sh::kQBytes, kTermBytes = Sh::kTermBytes, kCodeBytes = Sh::kCodeBytes, kVBytes = Sh::kVBytes, kGroupBytes = Sh::kGroupBytes;
+  constexpr int kKStages = Sh::kKStages, kVStages = Sh::kVStages;
   extern __shared__ __align__(1024) unsigned char smem[];
   if ((smem_u32(smem) & 1023u) != 0u) {  // the swizzled tiles need a 1024-byte aligned base
     if (threadIdx.x == 0) {
@@ -335,21 +361,28 @@ attn_fp8_kernel(DevBatch d, DevTcPlan tc, const uint16_t *__restrict__ q, Fp8Poo
     }
     return;
   }
-  unsigned char *q_smem = smem;                  // two M-tiles
-  unsigned char *kv_smem = smem + 2 * kQBytes;   // kStages half-tiles
-  unsigned char *code_smem = kv_smem + kStages * kStageBytes;  // a half-tile of codes for each converter
-  Ctrl *ctrl = reinterpret_cast<Ctrl *>(code_smem + kTeams * Sh::kCodeBytes);
+  unsigned char *q_smem = smem;                // two M-tiles
+  unsigned char *k_smem = q_smem + 2 * kQBytes;  // kKStages half-tiles of codes
+  unsigned char *v_smem = k_smem + kKStages * kCodeBytes;  // kVStages half-tiles of halves
+  unsigned char *code_smem = v_smem + kVStages * kVBytes;  // a half-tile of V's codes for each converter
+  Ctrl *ctrl = reinterpret_cast<Ctrl *>(code_smem + kTeams * kCodeBytes);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
 
   // the plan is uploaded by copies, so it may be read in front of the wait for the kernel before
   const TcCtaHead *head = tc.heads + blockIdx.x;
   const int piece0 = head->piece0, piece1 = head->piece1;
-  if (warp == 8 && lane < (int)(sizeof(TcCtaHead) / 16))
-    reinterpret_cast<uint4 *>(&ctrl->head)[lane] = __ldg(reinterpret_cast<const uint4 *>(head) + lane);
+  if (warp == 14) {
+    if (lane < (int)(sizeof(TcCtaHead) / 16)) reinterpret_cast<uint4 *>(&ctrl->head)[lane] = __ldg(reinterpret_cast<const uint4 *>(head) + lane);
+    if (elect_one()) asm volatile("prefetch.tensormap [%0];" ::"l"(&k_map) : "memory");
+  }
   if (threadIdx.x == 0) {
-    for (int s = 0; s < kStages; ++s) {
-      mbar_init(&ctrl->kv_full[s], 1);
-      mbar_init(&ctrl->kv_empty[s], 2);  // one per MMA issuer
+    for (int s = 0; s < kKStages; ++s) {
+      mbar_init(&ctrl->k_full[s], 1);
+      mbar_init(&ctrl->k_empty[s], 2);  // one arrival per MMA issuer
+    }
+    for (int s = 0; s < kVStages; ++s) {
+      mbar_init(&ctrl->v_full[s], 1);
+      mbar_init(&ctrl->v_empty[s], 2);
     }
     mbar_init(&ctrl->q_full, 256);
     mbar_init(&ctrl->q_empty, 2);
@@ -385,61 +418,72 @@ attn_fp8_kernel(DevBatch d, DevTcPlan tc, const uint16_t *__restrict__ q, Fp8Poo
   if (warp >= 8) {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 80;");
     const TcCtaHead *head = &ctrl->head;
+    // the page a table names, or page 0 in its place: never fetch outside the pool
+    auto page_in_pool = [&](int32_t page) -> int32_t {
+      if (page >= 0 && page < d.n_pool_pages) return page;
+      d.status[0] = kDevBounds;
+      d.status[1] = 200;
+      return 0;
+    };
     if (warp == 12 || warp == 13) {
       // ======================= MMA issuer of stream s ====================================
-      // Both issuers walk every ring position of a piece in order: a position this stream uses is consumed by its MMAs (released by a
+      // Both issuers walk every position of both rings in order: a half-tile this stream uses is consumed by its MMAs (released by a
       // tcgen05.commit), one it does not use is released with a plain arrive once it has landed.
       const int s = __shfl_sync(0xFFFFFFFFu, warp, 0) - 12;
-      uint32_t ring_base = 0, waited = 0, p_cnt = 0, pc_idx = 0;
+      uint32_t base = 0, k_seen = 0, v_seen = 0, p_cnt = 0, pc_idx = 0;  // base: half-tiles of the pieces before
       bool ok = true;
       const uint32_t tmem_u = __shfl_sync(0xFFFFFFFFu, tmem, 0);
       const uint32_t s_tmem = tmem_u + s * 128, o_tmem = tmem_u + 256 + s * 128;
       // Descriptors differ from a base only in the start-address field (units of 16 bytes).
-      const uint64_t qdesc0 = make_desc(smem_u32(q_smem), 16, 1024), kdesc0 = make_desc(smem_u32(kv_smem), 16, kGroupBytes),
-                     vdesc0 = make_desc(smem_u32(kv_smem), kAtomBytes, kGroupBytes);
-      auto issue_qk = [&](int m, uint32_t stage, int half) {  // S_s[half] = Q_m K^T over 64 keys
-        const uint64_t a = qdesc0 + (uint64_t)(m * (kQBytes >> 4)), b = kdesc0 + (uint64_t)(stage * (kStageBytes >> 4));
+      const uint64_t qdesc0 = make_row_desc<kD>(smem_u32(q_smem)), kdesc0 = make_row_desc<kD>(smem_u32(k_smem)),
+                     vdesc0 = make_desc(smem_u32(v_smem), kAtomBytes, kGroupBytes);
+      auto issue_qk = [&](int m, uint32_t stage, int half) {  // S_s[half] = (hi + lo) of Q_m times K^T over 64 keys
+        const uint64_t a = qdesc0 + (uint64_t)(m * (kQBytes >> 4)), b = kdesc0 + (uint64_t)(stage * (kCodeBytes >> 4));
 #pragma unroll
-        for (int h = 0; h < kHalves; ++h)
+        for (int term = 0; term < 2; ++term)
 #pragma unroll
-          for (int kk = 0; kk < 4; ++kk)
-            mma_ss(s_tmem + half * 64, a + (uint64_t)(h * (kHalfBytes >> 4) + kk * 2), b + (uint64_t)(h * (kAtomBytes >> 4) + kk * 2),
-                   kIdescQK, (h | kk) != 0);
+          for (int kk = 0; kk < kD / 32; ++kk)
+            mma_f8(s_tmem + half * 64, a + (uint64_t)(term * (kTermBytes >> 4) + kk * 2), b + (uint64_t)(kk * 2), kIdescQK, (term | kk) != 0);
       };
       auto issue_pv = [&](uint32_t stage, int half, bool acc) {  // O_s (+)= P_s[half] V over 64 keys
-        const uint64_t b = vdesc0 + (uint64_t)(stage * (kStageBytes >> 4));
+        const uint64_t b = vdesc0 + (uint64_t)(stage * (kVBytes >> 4));
 #pragma unroll
         for (int k4 = 0; k4 < 4; ++k4)
           mma_ts(o_tmem, s_tmem + half * 64 + k4 * 8, b + (uint64_t)(k4 * (2 * kGroupBytes >> 4)), kIdescPV<kD>, acc || k4 != 0);
       };
+      // waits, in ring order, until position `pos` has landed; positions on the way belong to the other stream and are released here
+      auto need_k = [&](uint32_t pos) -> bool {
+        for (; k_seen <= pos; ++k_seen) {
+          if (!wait(&ctrl->k_full[k_seen % kKStages], (k_seen / kKStages) & 1u, ctrl, d.status, 271)) return false;
+          if (k_seen < pos && elect_one()) mbar_arrive(&ctrl->k_empty[k_seen % kKStages]);
+        }
+        return true;
+      };
+      auto need_v = [&](uint32_t pos) -> bool {
+        for (; v_seen <= pos; ++v_seen) {
+          if (!wait(&ctrl->v_full[v_seen % kVStages], (v_seen / kVStages) & 1u, ctrl, d.status, 272)) return false;
+          if (v_seen < pos && elect_one()) mbar_arrive(&ctrl->v_empty[v_seen % kVStages]);
+        }
+        return true;
+      };
       for (int pc = piece0; pc < piece1 && ok; ++pc, ++pc_idx) {
         const TcPiece pi = pc == piece0 ? head->first : tc.pieces[pc];
         const int n = pi.tile_end - pi.tile_begin, mode = pi.n_mt;
-        const HalfOrder ord(n, mode);
-        const int my_units = mode == 2 ? n : (n - s + 1) / 2;
+        const int my_units = mode == 2 ? n : (n - s + 1) / 2, step = mode == 2 ? 2 : 4;  // half-tiles from a tile of this stream to its next
         const int m_tile = mode == 2 ? s : 0;
-        auto need = [&](uint32_t pos, int code) -> bool {  // waits, in ring order, until absolute ring position `pos` has landed
-          while (waited <= pos) {
-            if (!wait(&ctrl->kv_full[waited % kStages], (waited / kStages) & 1u, ctrl, d.status, code)) return false;
-            if (waited < pos && elect_one()) mbar_arrive(&ctrl->kv_empty[waited % kStages]);
-            ++waited;
-          }
-          return true;
-        };
-        auto release = [&](uint32_t pos) { tc_commit(&ctrl->kv_empty[pos % kStages]); };  // arrives when the MMAs that read the stage retire
+        uint32_t pos = base + (mode == 2 ? 0u : 2u * s);  // of the stream's tile
         ok = wait(&ctrl->q_full, pc_idx & 1u, ctrl, d.status, 270);
         if (!ok) break;
         if (my_units > 0) {
 #pragma unroll 1
           for (int half = 0; half < 2; ++half) {
-            const uint32_t pos = ring_base + ord.k(mode == 2 ? 0 : s, half);
-            ok = need(pos, 271);
+            ok = need_k(pos + half);
             if (!ok) break;
             tc_fence_after();
             if (elect_one()) {
-              issue_qk(m_tile, pos % kStages, half);
+              issue_qk(m_tile, (pos + half) % kKStages, half);
               tc_commit(&ctrl->s_full[s][half]);
-              release(pos);
+              tc_commit(&ctrl->k_empty[(pos + half) % kKStages]);
               if (half == 1 && my_units == 1) tc_commit(&ctrl->q_empty);  // last QK of the piece: this stream is done with the Q buffers
             }
             __syncwarp();
@@ -447,37 +491,31 @@ attn_fp8_kernel(DevBatch d, DevTcPlan tc, const uint16_t *__restrict__ q, Fp8Poo
           if (!ok) break;
         } else {
           if (elect_one()) mbar_arrive(&ctrl->q_empty);
-          // nothing to issue in this piece: still observe the previous piece's epilogue phase, so that the parity
-          // wait of a later piece never finds this issuer two phases behind
-          if (pc_idx > 0) {
-            ok = wait(&ctrl->epi_done, (pc_idx - 1) & 1u, ctrl, d.status, 278);
-            if (!ok) break;
-          }
         }
-        for (int j = 0; j < my_units && ok; ++j) {
-          const int t = mode == 2 ? j : 2 * j + s;
+        if (pc_idx > 0) {  // the epilogue of the previous piece has read O_0 and O_1 (a stream with nothing to do here looks too, so that the parity
+                           // never is two phases behind)
+          ok = wait(&ctrl->epi_done, (pc_idx - 1) & 1u, ctrl, d.status, 273);
+          if (!ok) break;
+        }
+        for (int j = 0; j < my_units && ok; ++j, pos += step) {
           const bool has_next = j + 1 < my_units;
-          if (j == 0 && pc_idx > 0) {  // the epilogue of the previous piece has read O_0 and O_1
-            ok = wait(&ctrl->epi_done, (pc_idx - 1) & 1u, ctrl, d.status, 273);
-            if (!ok) break;
-          }
 #pragma unroll 1
           for (int half = 0; half < 2; ++half) {
-            const uint32_t pos_v = ring_base + ord.v(t, half), pos_k = ring_base + ord.k(t + (mode == 2 ? 1 : 2), half);
-            ok = need(pos_v, 272) && (!has_next || need(pos_k, 276));
+            const uint32_t pos_v = pos + half, pos_k = pos_v + step;
+            ok = need_v(pos_v) && (!has_next || need_k(pos_k));
             if (!ok) break;
             // P of this half is in place: O += P V, then the buffer takes the scores of the next tile's half
             ok = wait(&ctrl->p_full[s][half], p_cnt & 1u, ctrl, d.status, 274 + s);
             if (!ok) break;
             tc_fence_after();
             if (elect_one()) {
-              issue_pv(pos_v % kStages, half, (j | half) != 0);
+              issue_pv(pos_v % kVStages, half, (j | half) != 0);
               tc_commit(&ctrl->o_done[s]);
-              release(pos_v);
+              tc_commit(&ctrl->v_empty[pos_v % kVStages]);
               if (has_next) {
-                issue_qk(m_tile, pos_k % kStages, half);
+                issue_qk(m_tile, pos_k % kKStages, half);
                 tc_commit(&ctrl->s_full[s][half]);
-                release(pos_k);
+                tc_commit(&ctrl->k_empty[pos_k % kKStages]);
                 if (half == 1 && j + 2 == my_units) tc_commit(&ctrl->q_empty);  // last QK of the piece
               }
             }
@@ -486,11 +524,17 @@ attn_fp8_kernel(DevBatch d, DevTcPlan tc, const uint16_t *__restrict__ q, Fp8Poo
           ++p_cnt;
         }
         if (!ok) break;
-        ring_base += 4u * (uint32_t)n;
-        if (waited < ring_base) {  // positions of the piece this stream never touched (the tail of the other stream's tiles)
-          ok = need(ring_base - 1, 277);
+        // half-tiles of the piece behind the last of this stream
+        base += 2u * (uint32_t)n;
+        if (k_seen < base) {
+          ok = need_k(base - 1);
           if (!ok) break;
-          if (elect_one()) mbar_arrive(&ctrl->kv_empty[(ring_base - 1) % kStages]);
+          if (elect_one()) mbar_arrive(&ctrl->k_empty[(base - 1) % kKStages]);
+        }
+        if (v_seen < base) {
+          ok = need_v(base - 1);
+          if (!ok) break;
+          if (elect_one()) mbar_arrive(&ctrl->v_empty[(base - 1) % kVStages]);
         }
       }
       if (!ok && elect_one()) {
@@ -501,10 +545,78 @@ attn_fp8_kernel(DevBatch d, DevTcPlan tc, const uint16_t *__restrict__ q, Fp8Poo
           if (global_ns() - t0 > kDrainLimitNs) break;
       }
       __syncwarp();
+    } else if (warp == 14) {
+      // ======================= producer ====================================================
+      uint32_t tiles = 0, ring = 0;
+      bool ok = true;
+      for (int pc = piece0; pc < piece1 && ok; ++pc) {
+        const TcPiece pi = pc == piece0 ? head->first : tc.pieces[pc];
+        const TcReq rq = pc == piece0 ? head->first_req : tc.reqs[pi.req];
+        const int n = pi.tile_end - pi.tile_begin;
+        const TcPage *pages = tc.pages + rq.page_off + pi.tile_begin * kPagesPerTile + (lane >> 2);  // of the keys 4 lane .. 4 lane + 3
+        auto row_of = [&](int2 e) -> int32_t {  // first row of a page; rows of the pools are numbered within 32 bits (tc_plan_structure)
+          return (page_in_pool(e.x) * d.n_kv_heads + pi.kv_head) * kPage;
+        };
+        // A tile's page entries are asked for two tiles ahead, its scale bytes one.
+        int2 e = ld_pair(pages), e_next = ld_pair(pages + min(1, n - 1) * kPagesPerTile);
+        int32_t row = row_of(e);
+        uint32_t k_word = ld_word(in.k_scale + row + (lane & 3) * 4), v_word = ld_word(in.v_scale + row + (lane & 3) * 4);
+        for (int t = 0; t < n && ok; ++t, ++tiles) {
+          const uint32_t live = valid_bytes(e.y & 31, lane), kb = k_word & live, vb = v_word & live;
+          const int32_t my_row = row;
+          e = e_next;
+          row = row_of(e);
+          k_word = ld_word(in.k_scale + row + (lane & 3) * 4);
+          v_word = ld_word(in.v_scale + row + (lane & 3) * 4);
+          e_next = ld_pair(pages + min(t + 2, n - 1) * kPagesPerTile);
+          ok = wait(&ctrl->k_empty[ring % kKStages], ((ring / kKStages) & 1u) ^ 1u, ctrl, d.status, 210);
+          if (!ok) break;
+#pragma unroll
+          for (int half = 0; half < 2; ++half, ++ring) {
+            const uint32_t stage = ring % kKStages;
+            if (half == 1) {
+              ok = wait(&ctrl->k_empty[stage], ((ring / kKStages) & 1u) ^ 1u, ctrl, d.status, 211);
+              if (!ok) break;
+            }
+            if (lane == 0)
+              mbar_arrive_expect_tx(&ctrl->k_full[stage], (uint32_t)kCodeBytes + ((blockIdx.x == 0 && ring == 0) ? tc.phantom_tx_bytes : 0u));
+            __syncwarp();
+            // one box per page, absent pages of the last tile included (page 0 in their place: nobody looks at these scores)
+            if ((lane >> 4) == half && (lane & 3) == 0)
+              tma_load_2d(smem_u32(k_smem) + stage * kCodeBytes + ((lane >> 2) & 3) * (kPage * kD), &k_map, 0, my_row, &ctrl->k_full[stage]);
+            if (half == 0) {
+              Info &info = ctrl->info[tiles % kInfos];
+              // (a byte of a slot without a valid token is 0 here)
+              reinterpret_cast<float4 *>(info.k_scale)[lane] =
+                  make_float4(fp8_scale(kb & 0xFFu), fp8_scale((kb >> 8) & 0xFFu), fp8_scale((kb >> 16) & 0xFFu), fp8_scale(kb >> 24));
+              const uint32_t top = top_byte(vb), nan = __vcmpeq4(vb, 0xFFFFFFFFu);
+              const uint32_t ref0 = __reduce_max_sync(0xFFFFFFFFu, lane < 16 ? top : 0u), ref1 = __reduce_max_sync(0xFFFFFFFFu, lane >= 16 ? top : 0u);
+              const bool any = __any_sync(0xFFFFFFFFu, nan != 0u);
+              if (any) ctrl->v_nan[tiles % kInfos][lane] = (uint8_t)((nan & 1u) | ((nan >> 7) & 2u) | ((nan >> 14) & 4u) | ((nan >> 21) & 8u));
+              if (lane == 0) {
+                info.v_ref[0] = (int)max(ref0, 1u);
+                info.v_ref[1] = (int)max(ref1, 1u);
+                info.v_nan = any ? 1 : 0;
+              }
+              __syncwarp();
+              if (lane == 0) mbar_arrive(&ctrl->info_full[tiles % kInfos]);
+            }
+          }
+        }
+      }
+      if (!ok) {
+        // give the copies already in flight a bounded time to land before the CTA exits
+        for (uint32_t back = 1; back <= (uint32_t)kKStages && back <= ring; ++back) {
+          const uint32_t j = ring - back;
+          const uint64_t t0 = global_ns();
+          while (!mbar_try_wait(&ctrl->k_full[j % kKStages], (j / kKStages) & 1u))
+            if (global_ns() - t0 > kDrainLimitNs) break;
+        }
+      }
     } else {
-      // ======================= converters ==================================================
+      // ======================= converters of V ===============================================
       constexpr int kCols = Sh::kCols, kGroups = Sh::kGroups, kRounds = Sh::kRounds;
-      const int team = warp < 12 ? warp - 8 : warp - 10;
+      const int team = warp < 12 ? warp - 8 : 4;
       const int col = lane % kCols, grp = lane / kCols;  // 16 channels of keys (round * kGroups + grp) * 4 .. + 3
       // Eight neighbouring lanes store to two lines at a time whose 16-byte units lie in the same banks (both channel halves of a key, or with head size 64
       // keys four apart); half of them take their four keys in the order 1, 0, 3, 2, which brings the units of the two lines apart.
@@ -513,115 +625,76 @@ attn_fp8_kernel(DevBatch d, DevTcPlan tc, const uint16_t *__restrict__ q, Fp8Poo
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
         const int r = (grp & 1) * 4 + (j ^ odd);
-        off[j] = smem_u32(kv_smem) + (kD == 128 ? (col >> 2) * kAtomBytes : 0) + (grp >> 1) * kGroupBytes + r * 128 + ((((col & 3) * 2) ^ r) << 4);
+        off[j] = smem_u32(v_smem) + (kD == 128 ? (col >> 2) * kAtomBytes : 0) + (grp >> 1) * kGroupBytes + r * 128 + ((((col & 3) * 2) ^ r) << 4);
       }
       const int32_t k_off = (grp & 3) * 4 * kD + col * 16;  // within the page of the keys
       // A lane alone copies and reads its part of the warp's codes, so that nothing but its own copies has to be waited for; a part
       // is asked for again as soon as it has been read, a whole half-tile's work ahead.
-      const uint32_t mine = smem_u32(code_smem) + team * Sh::kCodeBytes + lane * 16;
+      const uint32_t mine = smem_u32(code_smem) + team * kCodeBytes + lane * 16;
 
-      // the ring positions of this warp: every kTeams-th of the CTA's
-      struct Place {
-        int32_t info;    // number of the half-tile among the CTA's
-        int32_t kv_head;
-        bool is_v, whole, there;  // whole: no slot without a valid token
+      // the half-tiles of this warp: every kTeams-th of the CTA's
+      int pc = piece0, x = team, n_half = 0, n_whole = 0, kv_head = 0;  // of the half-tile that comes after the next one: its number within the piece
+      const TcPage *pages = nullptr;
+      auto open = [&]() {
+        const TcPiece pi = pc == piece0 ? head->first : tc.pieces[pc];
+        const TcReq rq = pc == piece0 ? head->first_req : tc.reqs[pi.req];
+        n_half = 2 * (pi.tile_end - pi.tile_begin);
+        n_whole = 2 * (rq.n_dense_tiles - pi.tile_begin);  // half-tiles without slots of no valid token
+        kv_head = pi.kv_head;
+        pages = tc.pages + rq.page_off + pi.tile_begin * kPagesPerTile + ((lane >> 2) & 3);  // of the keys 4 lane .. 4 lane + 3 (lanes 16-31: again)
       };
-      int pc = piece0, x = team;  // of the position that comes after the next one
-      TcPiece pi = head->first;
-      TcReq rq = head->first_req;
-      int32_t tiles0 = 0;  // tiles of the pieces before
-      auto place = [&](int2 &entry) -> Place {  // ... and the page of this lane's word, asked for here
-        while (pc < piece1 && x >= 4 * (pi.tile_end - pi.tile_begin)) {
-          x -= 4 * (pi.tile_end - pi.tile_begin);
-          tiles0 += pi.tile_end - pi.tile_begin;
-          if (++pc < piece1) {
-            pi = tc.pieces[pc];
-            rq = tc.reqs[pi.req];
-          }
-        }
+      // moves on by kTeams half-tiles; the page of this lane's keys (asked for here), the KV head, and whether V has to be cleared there
+      struct Place {
+        int2 entry;
+        int32_t kv_head;
+        bool there, clear;
+      };
+      auto place = [&]() -> Place {
         Place p;
+        while (pc < piece1 && x >= n_half) {
+          x -= n_half;
+          if (++pc < piece1) open();
+        }
         p.there = pc < piece1;
-        if (!p.there) return p;
-        int half;
-        const int t = HalfOrder(pi.tile_end - pi.tile_begin, pi.n_mt).at(x, half, p.is_v);
-        p.info = (tiles0 + t) * 2 + half;
-        p.kv_head = pi.kv_head;
-        p.whole = pi.tile_begin + t < rq.n_dense_tiles;
-        entry = ld_pair(tc.pages + rq.page_off + (pi.tile_begin + t) * kPagesPerTile + half * 4 + ((lane >> 2) & 3));
+        p.kv_head = kv_head;
+        p.clear = x >= n_whole;
+        p.entry = make_int2(0, 0);
+        if (p.there) p.entry = ld_pair(pages + x * (kPagesPerTile / 2));
         x += kTeams;
         return p;
       };
-      auto row_of = [&](int32_t page, int32_t kv_head) -> int32_t {  // the first row of a page; rows of the pools are numbered within 32 bits (tc_plan_structure)
-        if (page < 0 || page >= d.n_pool_pages) {  // never fetch outside the pool
-          d.status[0] = kDevBounds;
-          d.status[1] = 200;
-          page = 0;
-        }
-        return (page * d.n_kv_heads + kv_head) * kPage;
-      };
-      // lanes 0-15: the scale bytes of keys 4 lane .. 4 lane + 3; beside those of K, lanes 16-31 have V's of the same keys
-      auto word_at = [&](const Place &p, int32_t row) -> uint32_t {
-        return ld_word((p.is_v || lane >= 16 ? in.v_scale : in.k_scale) + row + (lane & 3) * 4);
-      };
-      auto fetch = [&](const Place &p, int32_t row, int u) {  // part u of the codes
-        // (a lane whose word lies in the page of this lane's keys; an absent page of the last tile reads page 0 and is cleared below)
-        const uint8_t *at = (p.is_v ? in.v : in.k) + k_off + (int64_t)__shfl_sync(0xFFFFFFFFu, row, ((u * kGroups + grp) >> 2) * 4) * kD;
+      auto fetch = [&](int32_t row, int u) {  // part u of the codes of the pages with those rows
+        // (a lane whose row is that of the page of this lane's keys; an absent page of the last tile reads page 0 and is cleared below)
+        const uint8_t *at = in.v + k_off + (int64_t)__shfl_sync(0xFFFFFFFFu, row, ((u * kGroups + grp) >> 2) * 4) * kD;
         const uint8_t *even = at + odd * kD, *other = at - odd * kD;
         copy_codes(mine + u * 2048, even);
         copy_codes(mine + u * 2048 + 512, other + kD);
         copy_codes(mine + u * 2048 + 1024, even + 2 * kD);
         copy_codes(mine + u * 2048 + 1536, other + 3 * kD);
       };
-      bool ok = true;
-      int2 e_nxt = make_int2(0, 0), e_after = make_int2(0, 0);
-      Place nxt = place(e_nxt);
-      int32_t row = 0;
-      uint32_t word = 0, meta = 0;
-      if (nxt.there) {
-        row = row_of(e_nxt.x, nxt.kv_head);
-        meta = (uint32_t)e_nxt.y;
-        word = word_at(nxt, row);
-      }
+      open();
+      Place nxt = place();
+      int32_t row = (page_in_pool(nxt.entry.x) * d.n_kv_heads + nxt.kv_head) * kPage;  // rows of the pools are numbered within 32 bits (tc_plan_structure)
+      uint32_t word = ld_word(in.v_scale + row + (lane & 3) * 4);
 #pragma unroll
       for (int u = 0; u < kRounds; ++u) {
-        if (nxt.there) fetch(nxt, row, u);
+        if (nxt.there) fetch(row, u);
         asm volatile("cp.async.commit_group;" ::: "memory");
       }
-      Place after = nxt;
-      if (nxt.there) after = place(e_after);
+      Place after = place();
       for (uint32_t ring = (uint32_t)team; nxt.there; ring += kTeams) {
         // Loads into registers are asked for here and looked at a half-tile later.
-        const Place cur = nxt;
-        const uint32_t cur_word = word, cur_meta = meta;
+        const uint32_t live = valid_bytes(nxt.entry.y & 31, lane), bytes = word & live;
+        const bool clear = nxt.clear;
         nxt = after;
-        if (nxt.there) {
-          row = row_of(e_after.x, nxt.kv_head);
-          meta = (uint32_t)e_after.y;
-          word = word_at(nxt, row);
-          after = place(e_after);
-        }
-        const uint32_t live = valid_bytes((int)(cur_meta & 31u), lane), bytes = cur_word & live, top = top_byte(bytes);
-        const int ref = (int)max(__reduce_max_sync(0xFFFFFFFFu, lane < 16 ? top : 0u), 1u);
-        const uint32_t stage = ring % kStages;
-        ok = wait(&ctrl->kv_empty[stage], ((ring / kStages) & 1u) ^ 1u, ctrl, d.status, 210);
-        if (!ok) break;
-        if (!cur.is_v) {  // what the softmax has to know of this half-tile, V's scales among it
-          const int v_ref = (int)max(__reduce_max_sync(0xFFFFFFFFu, lane >= 16 ? top : 0u), 1u);
-          const uint32_t nan = lane >= 16 ? __vcmpeq4(bytes, 0xFFFFFFFFu) : 0u;
-          const bool any = __any_sync(0xFFFFFFFFu, nan != 0u);
-          const uint32_t at = (uint32_t)cur.info % kInfos;
-          if (any && lane >= 16) ctrl->v_nan[at][lane - 16] = (uint8_t)((nan & 1u) | ((nan >> 7) & 2u) | ((nan >> 14) & 4u) | ((nan >> 21) & 8u));
-          __syncwarp();
-          if (lane == 0) {
-            ctrl->info[at] = Info{ref, v_ref, any ? 1 : 0};
-            mbar_arrive(&ctrl->info_full[at]);
-          }
-        }
+        row = (page_in_pool(nxt.entry.x) * d.n_kv_heads + nxt.kv_head) * kPage;
+        word = ld_word(in.v_scale + row + (lane & 3) * 4);
+        after = place();
+        const int ref = (int)max(__reduce_max_sync(0xFFFFFFFFu, top_byte(bytes)), 1u);  // (what the producer publishes)
         // the factors of this lane's four keys, which other lanes ask for
-        const float nan_is = cur.is_v ? 0.f : __uint_as_float(0x7FC00000u);
-        const uint32_t f01 = factors(bytes & 0xFFu, (bytes >> 8) & 0xFFu, ref, nan_is), f23 = factors((bytes >> 16) & 0xFFu, bytes >> 24, ref, nan_is);
-        const uint32_t to = stage * kStageBytes;
-        const bool clear = cur.is_v && !cur.whole;  // (K's scores of slots that hold no valid token are never looked at)
+        const uint32_t f01 = factors(bytes & 0xFFu, (bytes >> 8) & 0xFFu, ref), f23 = factors((bytes >> 16) & 0xFFu, bytes >> 24, ref);
+        const uint32_t stage = ring % kVStages, to = stage * kVBytes;
+        if (!wait(&ctrl->v_empty[stage], ((ring / kVStages) & 1u) ^ 1u, ctrl, d.status, 212)) break;
 #pragma unroll 1
         for (int u = 0; u < kRounds; ++u) {
           asm volatile("cp.async.wait_group %0;" ::"n"(kRounds - 1) : "memory");
@@ -635,6 +708,7 @@ attn_fp8_kernel(DevBatch d, DevTcPlan tc, const uint16_t *__restrict__ q, Fp8Poo
             for (int j = 0; j < 4; ++j)
               if (((l4 >> (8 * (j ^ odd))) & 1u) == 0u) c[j] = make_uint4(0, 0, 0, 0);
           }
+          const uint32_t at = to + u * (kGroups / 2) * kGroupBytes;
 #pragma unroll
           for (int j = 0; j < 4; ++j) {
             const uint32_t f = __byte_perm(by[j >> 1], 0u, ((j & 1) != 0) != (odd != 0) ? 0x3232 : 0x1010);
@@ -643,17 +717,15 @@ attn_fp8_kernel(DevBatch d, DevTcPlan tc, const uint16_t *__restrict__ q, Fp8Poo
             halves4(c[j].y, f, h[2], h[3]);
             halves4(c[j].z, f, h[4], h[5]);
             halves4(c[j].w, f, h[6], h[7]);
-            const uint32_t a = off[j] + to + u * (kGroups / 2) * kGroupBytes;
-            st_shared(a, h[0], h[1], h[2], h[3]);
-            st_shared(a ^ 16u, h[4], h[5], h[6], h[7]);
+            st_shared(off[j] + at, h[0], h[1], h[2], h[3]);
+            st_shared((off[j] + at) ^ 16u, h[4], h[5], h[6], h[7]);
           }
-          if (nxt.there) fetch(nxt, row, u);
+          if (nxt.there) fetch(row, u);
           asm volatile("cp.async.commit_group;" ::: "memory");
         }
         fence_proxy_async();
         __syncwarp();
-        // (the test hook of lr_plan_debug_set_phantom_bytes: a stage that is never full)
-        if (lane == 0 && !(tc.phantom_tx_bytes != 0u && blockIdx.x == 0 && ring == 0)) mbar_arrive(&ctrl->kv_full[stage]);
+        if (lane == 0) mbar_arrive(&ctrl->v_full[stage]);
       }
       asm volatile("cp.async.wait_group 0;" ::: "memory");  // (after an abort some are still on their way)
     }
@@ -680,8 +752,7 @@ attn_fp8_kernel(DevBatch d, DevTcPlan tc, const uint16_t *__restrict__ q, Fp8Poo
         // the queries, once the products of the piece before no longer read the buffers; with one M-tile each stream stores its part
         ok = wait(&ctrl->q_empty, ((uint32_t)(pc - piece0) & 1u) ^ 1u, ctrl, d.status, 245);
         if (ok) {
-          const int h0 = mode == 2 || kHalves == 2 ? (mode == 2 ? 0 : s) : 0, h1 = mode == 2 ? kHalves : kHalves == 2 ? s + 1 : 1 - s;
-          sc_row = scale_log2 * pow2(convert_q<kD>(q, ri.q_index, smem_u32(q_smem) + (mode == 2 ? s : 0) * kQBytes, r, h0, h1));
+          sc_row = scale_log2 * convert_q<kD>(q, ri.q_index, smem_u32(q_smem) + (mode == 2 ? s : 0) * kQBytes, r, mode == 2 ? 0 : s, mode == 2 ? 2 : s + 1);
           fence_proxy_async();
           mbar_arrive(&ctrl->q_full);
         }
@@ -690,6 +761,7 @@ attn_fp8_kernel(DevBatch d, DevTcPlan tc, const uint16_t *__restrict__ q, Fp8Poo
         float m_used = -INFINITY, l = 0.f;
         int base = 0;
         bool s_ready = false, nan_v = false;
+        uint32_t nan_at = kInfos;  // place of a tile in which some row of V stands for NaN
         // O *= alpha.  The PV product of the previous half-unit must have retired first; the one before
         // it has (its commit precedes the s_full this thread has just seen), so o_done has completed done_needed or
         // done_needed - 1 phases and the parity says which, whether or not this thread has looked at the earlier ones.
@@ -736,41 +808,45 @@ attn_fp8_kernel(DevBatch d, DevTcPlan tc, const uint16_t *__restrict__ q, Fp8Poo
           for (int half = 0; half < 2; ++half) {
             const uint32_t sh_addr = s_addr + half * 64;
             const uint32_t g = o_cnt + (uint32_t)(2 * j + half);  // half-units of this stream before this one
-            const uint32_t at = (tiles + (uint32_t)local) * 2 + half;  // half-tiles of both streams before this one
+            const uint32_t at = tiles + (uint32_t)local;  // tiles of both streams before this one
             const bool first = (j | half) == 0;
             if (!s_ready) {
-              ok = wait(&ctrl->info_full[at % kInfos], (at / kInfos) & 1u, ctrl, d.status, 248) &&
-                   wait(&ctrl->s_full[s][half], s_cnt & 1u, ctrl, d.status, 230 + s);
+              ok = wait(&ctrl->info_full[at % kInfos], (at / kInfos) & 1u, ctrl, d.status, 248) && wait(&ctrl->s_full[s][half], s_cnt & 1u, ctrl, d.status, 230 + s);
               if (!ok) break;
             }
             tc_fence_after();
-            const Info info = ctrl->info[at % kInfos];
-            if (info.v_nan)
-              nan_v = sees_nan(ctrl->v_nan[at % kInfos], masked ? tc.pages + rq.page_off + t * kPagesPerTile + half * 4 : nullptr, ri) || nan_v;
             uint32_t v[64];
             tmem_ld64(sh_addr, v);
+            const Info &info = ctrl->info[at % kInfos];
+            const int v_ref = info.v_ref[half];
+            if (info.v_nan) nan_at = at % kInfos;
             float alpha = 1.0f;  // what O has to be multiplied by before this half's product
-            if (first) base = info.v_ref;
-            if (info.v_ref > base + kRise) {
-              alpha = pow2(base - info.v_ref);
-              base = info.v_ref;
+            if (first) base = v_ref;
+            if (v_ref > base + kRise) {
+              alpha = pow2(base - v_ref);
+              base = v_ref;
             }
-            const float sc = sc_row * pow2(info.k_ref - 127);
-            const int off = info.v_ref - base;
+            const int off = v_ref - base;
             const float bias = (float)off + kHead;
             bool apart = off < -kApart;  // the sums first, of weights as they are
             tc_wait_ld();
             // the scores after these (and what is known of their keys) are looked for under the exponentials: a test costs over 100 cycles even
             // when it succeeds
-            const uint32_t next = half == 0 ? at + 1u : (tiles + (uint32_t)local + (mode == 2 ? 1u : 2u)) * 2u;
+            const uint32_t next = at + (half == 0 ? 0u : mode == 2 ? 1u : 2u);
             const uint32_t next_ready = mbar_test_wait2(&ctrl->s_full[s][half ^ 1], (s_cnt + (uint32_t)half) & 1u, &ctrl->info_full[next % kInfos],
                                                         (next / kInfos) & 1u) == 3u;
+#pragma unroll
+            for (int i = 0; i < 64; i += 4) {
+              const float4 ks = *reinterpret_cast<const float4 *>(info.k_scale + half * 64 + i);
+              mul2(v[i], v[i + 1], ks.x, ks.y);
+              mul2(v[i + 2], v[i + 3], ks.z, ks.w);
+            }
             if (masked) mask_half(v, n_ok + 4 * half);
             // Exponentials against the running reference exponent, the maximum of the 64 scores beside them.  Where that is beyond what a half holds
             // (and on a row's first keys) they are done again with the reference moved to it.
             for (;;) {
               float raw;
-              const float sum = exp_half(v, sh_addr, sc, m_used == -INFINITY ? 0.f : (apart ? 0.f : bias) - m_used, raw), mx = raw * sc;
+              const float sum = exp_half(v, sh_addr, sc_row, m_used == -INFINITY ? 0.f : (apart ? 0.f : bias) - m_used, raw), mx = raw * sc_row;
               const bool grow = mx > m_used + kGrow;  // (a row that has seen nothing: by any score)
               if (__any_sync(0xFFFFFFFFu, grow)) {
                 if (grow) {
@@ -805,6 +881,10 @@ attn_fp8_kernel(DevBatch d, DevTcPlan tc, const uint16_t *__restrict__ q, Fp8Poo
             if (half == 1 && j + 1 == my_units) {
               ok = wait(&ctrl->o_done[s], (g - 1) & 1u, ctrl, d.status, 237 + s);
               if (!ok) break;
+            }
+            if (nan_at < kInfos) {  // (before the arrival: what it looks at may be replaced behind it)
+              nan_v = sees_nan(ctrl->v_nan[nan_at], masked ? tc.pages + rq.page_off + t * kPagesPerTile : nullptr, ri) || nan_v;
+              nan_at = kInfos;
             }
             mbar_arrive(&ctrl->p_full[s][half]);
           }
@@ -876,12 +956,41 @@ attn_fp8_merge_kernel(DevBatch d, DevTcPlan tc, uint16_t *__restrict__ out, floa
   merge_cta<kD, kBatch>(d, tc, blockIdx.x, blockIdx.y, out, lse);
 }
 
+typedef CUresult (*EncodeTiledFn)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *, const cuuint64_t *,
+                                  const cuuint32_t *, const cuuint32_t *, CUtensorMapInterleave, CUtensorMapSwizzle,
+                                  CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+
+// K's codes as rows of head_dim bytes; a box is one page of one KV head, 16 rows.  Made for every call: it takes a fraction of a microsecond.
+int encode_k(lr_ctx *ctx, const void *codes, int64_t n_pages, CUtensorMap *map) {
+  if (!ctx->tmap_encode) {
+    void *fn = nullptr;
+    cudaDriverEntryPointQueryResult qres;
+    cudaError_t e = cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &fn, cudaEnableDefault, &qres);
+    if (e != cudaSuccess || qres != cudaDriverEntryPointSuccess || !fn) {
+      set_error("cuTensorMapEncodeTiled is not available from the driver");
+      return LR_ECUDA;
+    }
+    ctx->tmap_encode = fn;
+  }
+  const lr_model &m = ctx->model;
+  const cuuint64_t dims[2] = {(cuuint64_t)m.head_dim, (cuuint64_t)n_pages * m.n_kv_heads * kPage}, strides[1] = {(cuuint64_t)m.head_dim};
+  const cuuint32_t box[2] = {(cuuint32_t)m.head_dim, kPage}, estr[2] = {1, 1};
+  const CUresult r = reinterpret_cast<EncodeTiledFn>(ctx->tmap_encode)(
+      map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<void *>(codes), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+      m.head_dim == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B, CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  if (r != CUDA_SUCCESS) {
+    set_error("cuTensorMapEncodeTiled failed with CUresult %d", (int)r);
+    return LR_ECUDA;
+  }
+  return LR_OK;
+}
+
 template <int kD>
-int launch(lr_plan *p, const uint16_t *q, const Fp8Pools &in, uint16_t *out, float *lse, float scale_log2, cudaStream_t s) {
+int launch(lr_plan *p, const CUtensorMap &k_map, const uint16_t *q, const Fp8Pools &in, uint16_t *out, float *lse, float scale_log2, cudaStream_t s) {
   const DevTcPlan &tc = p->tc;
   p->ctx->launches++;
-  if (int rc = cuda_fail(launch_dependent(attn_fp8_kernel<kD>, dim3((unsigned)tc.n_cta), dim3(kThreads), kSmemBytes<kD>, s, p->dev, tc, q, in, out, lse,
-                                          scale_log2),
+  if (int rc = cuda_fail(launch_dependent(attn_fp8_kernel<kD>, dim3((unsigned)tc.n_cta), dim3(kThreads), kSmemBytes<kD>, s, k_map, p->dev, tc, q, in, out,
+                                          lse, scale_log2),
                          "attn_fp8_kernel launch"))
     return rc;
   if (tc.n_targets == 0) return LR_OK;
@@ -902,8 +1011,10 @@ int init_attn_fp8_kernel() {
 }
 
 int launch_attn_fp8(lr_plan *p, const void *q, const lr_fp8_cache &c, void *out, float *lse, float scale, cudaStream_t s) {
-  const Fp8Pools in = {reinterpret_cast<const uint8_t *>(c.k_d), reinterpret_cast<const uint8_t *>(c.v_d), c.k_scale_d, c.v_scale_d};
-  return (p->dev.head_dim == 128 ? launch<128> : launch<64>)(p, reinterpret_cast<const uint16_t *>(q), in, reinterpret_cast<uint16_t *>(out), lse,
+  alignas(64) CUtensorMap k_map;
+  if (int rc = encode_k(p->ctx, c.k_d, p->dev.n_pool_pages, &k_map)) return rc;
+  const Fp8Pools in = {reinterpret_cast<const uint8_t *>(c.v_d), c.k_scale_d, c.v_scale_d};
+  return (p->dev.head_dim == 128 ? launch<128> : launch<64>)(p, k_map, reinterpret_cast<const uint16_t *>(q), in, reinterpret_cast<uint16_t *>(out), lse,
                                                              scale * 1.4426950408889634f, s);
 }
 

@@ -74,3 +74,20 @@ def test_single_tokens(d, prefix, q, path):
     rng = np.random.default_rng(prefix + d)
     w = _finish("token", 11, Model(10, 2, d, 16), [{"P": prefix, "segs": [], "branches": [(0, q, q, q)]} for _ in range(3)], rng, 0.3, 0.6, False, True, "nan")
     check(w, path, REL_LARGE)
+
+
+@pytest.mark.parametrize("cfg,branches", [(3, [0, 5, 15]), (4, [0, 5]), (5, [0, 20, 40])])
+def test_large_configurations_on_the_tensor_cores(cfg, branches):
+    """Two M-tiles a piece, several pieces a CTA, results merged from many."""
+    w = make_config(cfg, with_logits=False)
+    check(w, B.PATH_TENSOR_CORE, branches=[b for b in branches if b < w.batch.n_branch])
+
+
+@pytest.mark.parametrize("seed", range(12))
+def test_both_sides_of_the_grouping_switch(seed):
+    check(make_random_mid(seed), B.PATH_TENSOR_CORE, REL_LARGE)
+
+
+@pytest.mark.parametrize("W,size", [(2, "tiny"), (3, "tiny"), (2, "layer")])
+def test_full_trees(W, size):
+    check(make_tree(W, 2, size=size, with_logits=False), B.PATH_TENSOR_CORE, REL_LARGE)
