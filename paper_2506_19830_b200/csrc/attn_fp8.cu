@@ -19,7 +19,7 @@
 //
 // One CTA = 16 warps in four warpgroups, registers moved with setmaxnreg (176 x 256 + 80 x 256 = 128 x 512):
 //   warp 14      producer: per tile of 128 keys 8 boxes of K (a page each), the keys' scales as fp32, ref of V's half-tiles.
-//   warps 8-11, 15  converters: the codes of a half-tile of V (64 keys) by asynchronous copies into a buffer of the warp's own, the next one's taking the
+//   warps 8-11  converters: the codes of a half-tile of V (64 keys) by asynchronous copies into a buffer of the warp's own, the next one's taking the
 //                place of each part as it is read; halves into the ring as the swizzled operand.  A warp has the half-tile's scale bytes in one word
 //                a lane, so that ref is one reduction and a key's factor one shuffle.  Slots that hold no valid token become zeros, whatever they held.
 //   warps 12, 13  MMA issuers of stream 0 and 1.
@@ -42,11 +42,11 @@ namespace {
 constexpr int kAtomBytes = 1024;   // 8 keys of V x 64 channels as halves, one 128-byte-swizzle atom
 constexpr int kMaxK = 8, kMaxV = 8;
 constexpr int kThreads = 512;
-constexpr int kTeams = 5;          // converter warps, each with half-tiles of its own
-// Tiles whose scales are published ahead of their products.  The producer writes those of tile x + kInfos once the stage of K that it takes is
-// free, which tile x + kInfos - kKStages / 2 had; from x + 3 on, that tells that no softmax thread will look at x again (an issuer asks for or
-// skips x + 3 behind the weights of its last half-tile up to x).
-constexpr int kInfos = 8;
+constexpr int kTeams = 4;          // converter warps, each with half-tiles of its own
+// Half-tiles whose scales are published ahead of their products.  A converter writes those of half-tile x + kInfos once the stage of K that it takes is
+// free, which half-tile x + kInfos - kKStages had; from x + 6 (three tiles) on, that tells that no softmax thread will look at x again: an issuer
+// asks for or skips x + 6 behind the weights of its last half-tile up to x.
+constexpr int kInfos = 16;
 constexpr float kGrow = 6.0f;      // log2: how far the scores of a row may rise above its reference exponent
 constexpr float kHead = 6.0f;      // log2: weights are kept this much above what they are
 constexpr int kRise = 3;           // log2: ... and V's half-tiles this much above the accumulator's unit: 6 + 6 + 3 = 15, f16 ends at 16
@@ -61,15 +61,16 @@ struct Shape {
   static constexpr int kCodeBytes = 64 * kD;                // a half-tile (64 keys) as it comes
   static constexpr int kGroupBytes = kHalves * kAtomBytes;  // the atoms of 8 keys of V
   static constexpr int kVBytes = 8 * kGroupBytes;           // a half-tile of V as halves: [8 groups][halves][8 keys][128 B]
-  static constexpr int kKStages = kD == 128 ? 4 : 8, kVStages = kD == 128 ? 5 : 8;
+  static constexpr int kKStages = kD == 128 ? 4 : 8, kVStages = kD == 128 ? 4 : 8;
   static constexpr int kCols = kD / 16;                     // lanes side by side in a row, 16 channels each
   static constexpr int kGroups = 32 / kCols;                // groups of four keys that a warp has at a time
   static constexpr int kRounds = 16 / kGroups;              // ... and how many times for a half-tile
 };
 
-struct Info {  // of a tile: largest scale bytes of V's half-tiles; whether some valid row of V stands for NaN; the keys' scales
-  float k_scale[128];
-  int32_t v_ref[2], v_nan, pad;
+struct Info {  // of a half-tile: the keys' scales, the largest scale byte of V, whether some valid row of V stands for NaN (and which: four keys a byte)
+  float k_scale[64];
+  int32_t v_ref, v_nan, pad[2];
+  uint8_t nan4[16];
 };
 
 struct __align__(16) Ctrl {
@@ -84,7 +85,7 @@ struct __align__(16) Ctrl {
   uint32_t tmem_base;
   int abort_flag;
   uint64_t wait_limit_ns;
-  uint8_t v_nan[kInfos][32];  // four keys a byte
+  int32_t *status;        // the plan's
   float xch_m[128], xch_l[128], xch_unit[128];  // stream 1's rows, for the in-CTA combination
 };
 constexpr int kCtrlBytes = 7 << 10;
@@ -92,10 +93,12 @@ static_assert(sizeof(Ctrl) <= kCtrlBytes, "Ctrl must fit behind the tiles");
 template <int kD>
 constexpr int kSmemBytes = 2 * Shape<kD>::kQBytes + Shape<kD>::kKStages * Shape<kD>::kCodeBytes + Shape<kD>::kVStages * Shape<kD>::kVBytes +
                            kTeams * Shape<kD>::kCodeBytes + kCtrlBytes;  // the base must be 1024-aligned
-static_assert(kInfos - Shape<64>::kKStages / 2 >= 3 && kInfos - Shape<128>::kKStages / 2 >= 3, "see kInfos");
-// A converter at position r has filled position r - kTeams, whose stage position r - kTeams - kVStages had been released from.  Releases are in order, so
-// with no more teams than stages the release before the one it waits for has happened, and the parity of the barrier means what it looks for.
-static_assert(kTeams <= Shape<64>::kVStages && kTeams <= Shape<128>::kVStages, "a converter must not be two phases of a stage ahead");
+static_assert(kInfos - Shape<64>::kKStages >= 6 && kInfos - Shape<128>::kKStages >= 6, "see kInfos");
+// A converter at position r of a ring has filled position r - kTeams, whose stage position r - kTeams - stages had been released from.  Releases are in
+// order, so with no more teams than stages the release before the one it waits for has happened, and the parity of the barrier means what it
+// looks for.
+static_assert(kTeams <= Shape<64>::kVStages && kTeams <= Shape<128>::kVStages && kTeams <= Shape<64>::kKStages && kTeams <= Shape<128>::kKStages,
+              "a converter must not be two phases of a stage ahead");
 static_assert(kSmemBytes<64> <= 227 * 1024 && kSmemBytes<128> <= 227 * 1024, "shared memory per CTA");
 
 // Instruction descriptors: D fp32, M = 128; QK: A and B e4m3 (format 0 of kind::f8f6f4), N = 64 keys, both operands K-major; PV: A and B f16 (format 0
@@ -130,25 +133,53 @@ __device__ __forceinline__ void tma_load_2d(uint32_t dst, const CUtensorMap *map
                : "memory");
 }
 
-// Five roles share an SM's instruction cache, and warps that wait for instructions were what bounded a version of this kernel that had everything
-// unrolled: what is long is in a loop, and what is rare out of the way.  The bounded wait of a whole warp (as wait_bar):
-__device__ __forceinline__ bool wait(uint64_t *bar, uint32_t parity, Ctrl *ctrl, int32_t *status, int code) {
-  if (__builtin_expect(__all_sync(0xFFFFFFFFu, mbar_test_wait(bar, parity)), 1)) return true;
-  const uint64_t t0 = global_ns();
+// Five roles share an SM's instruction cache (2048 instructions of it are fast), and warps that wait for instructions are what bounds a version of this
+// kernel that has everything in line: what is rare is in functions of its own, for each role (which have registers of different numbers) apart.
+// The bounded wait of a whole warp (as wait_bar):
+__device__ __forceinline__ bool test_bar(uint32_t bar, uint32_t parity) {
+  uint32_t ok;
+  asm volatile("{\n\t.reg .pred p;\n\tmbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n\tselp.b32 %0, 1, 0, p;\n\t}" : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
+  return ok != 0u;
+}
+extern __shared__ __align__(1024) unsigned char smem[];
+template <int kD>
+__device__ __forceinline__ Ctrl *ctrl_at() {
+  return reinterpret_cast<Ctrl *>(smem + kSmemBytes<kD> - kCtrlBytes);
+}
+template <int kD>
+__device__ __forceinline__ bool wait_long(uint32_t bar, uint32_t parity, int code) {
+  Ctrl *ctrl = ctrl_at<kD>();
+  uint64_t t0 = 0;
   for (uint32_t i = 0;; ++i) {
-    if (__all_sync(0xFFFFFFFFu, mbar_try_wait(bar, parity))) return true;
+    uint32_t got;
+    asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, %3;\n\tselp.b32 %0, 1, 0, p;\n\t}"
+                 : "=r"(got)
+                 : "r"(bar), "r"(parity), "r"(20000u)  // suspend for at most 20 us per try
+                 : "memory");
+    if (__all_sync(0xFFFFFFFFu, got != 0u)) return true;
+    if (i == 0) t0 = global_ns();
     if ((i & 31u) == 31u) {
       const bool out = global_ns() - t0 > ctrl->wait_limit_ns;
       if (__any_sync(0xFFFFFFFFu, out || *reinterpret_cast<volatile int *>(&ctrl->abort_flag))) {
         if (out) {
           *reinterpret_cast<volatile int *>(&ctrl->abort_flag) = 1;
-          status[0] = kDevTimeout;
-          status[1] = code;
+          ctrl->status[0] = kDevTimeout;
+          ctrl->status[1] = code;
         }
         return false;
       }
     }
   }
+}
+template <int kD, int kRole>
+__device__ __noinline__ bool wait_call(uint32_t bar, uint32_t parity, int code) { return wait_long<kD>(bar, parity, code); }
+// kRole: 0 softmax, 1 the others
+template <int kD, int kRole>
+__device__ __forceinline__ bool wait(uint64_t *bar, uint32_t parity, int code) {
+  const uint32_t at = smem_u32(bar);
+  if (__all_sync(0xFFFFFFFFu, test_bar(at, parity))) return true;
+  if constexpr (kRole == 2) return wait_long<kD>(at, parity, code);
+  else return wait_call<kD, kRole>(at, parity, code);
 }
 
 __device__ __forceinline__ uint32_t pack_f16(float lo, float hi) {
@@ -192,7 +223,8 @@ __device__ __forceinline__ void st_shared(uint32_t addr, uint32_t a, uint32_t b,
   asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(addr), "r"(a), "r"(b), "r"(c), "r"(d) : "memory");
 }
 
-// P = exp2(sc * s + neg) for 64 scores, as halves over the first half of the score buffer; returns their fp32 sum and the maximum of the raw scores.
+// P = exp2(sc * s + neg) for 64 scores, as halves over the first half of the score buffer; returns their fp32 sum and, worked out in the shadow of the
+// exponentials (which a quarter of an SM does four of a cycle: 512 cycles), the maximum of the scores.
 __device__ __forceinline__ float exp_half(const uint32_t (&v)[64], uint32_t addr, float sc, float neg, float &raw_max) {
   const float2 s2 = make_float2(sc, sc), n2 = make_float2(neg, neg);
   float2 acc0 = make_float2(0.f, 0.f), acc1 = make_float2(0.f, 0.f);
@@ -218,11 +250,40 @@ __device__ __forceinline__ float exp_half(const uint32_t (&v)[64], uint32_t addr
   acc0 = fadd2(acc0, acc1);
   return acc0.x + acc0.y;
 }
+// the scores of 64 keys times the keys' scales
+__device__ __forceinline__ void scale_half(uint32_t (&v)[64], const float *k_scale) {
+#pragma unroll
+  for (int i = 0; i < 64; i += 4) {
+    const float4 ks = *reinterpret_cast<const float4 *>(k_scale + i);
+    mul2(v[i], v[i + 1], ks.x, ks.y);
+    mul2(v[i + 2], v[i + 3], ks.z, ks.w);
+  }
+}
 
-// Whether the row sees a key of the tile whose row of V stands for NaN.  pages: null where it sees all keys.
+// O *= alpha.  The PV product of the previous half-unit must have retired first; the one before it has (its commit precedes the s_full this thread has just
+// seen), so o_done has completed done_needed or done_needed - 1 phases and the parity says which, whether or not this thread has looked at the
+// earlier ones.
+template <int kD>
+__device__ __noinline__ bool rescale_rows(uint32_t o_addr, float alpha, uint64_t *o_done, uint32_t done_needed, int code) {
+  if (!wait<kD, 2>(o_done, (done_needed - 1) & 1u, code)) return false;
+  tc_fence_after();
+#pragma unroll 1
+  for (int ch = 0; ch < kD / 32; ++ch) {
+    uint32_t o[32];
+    tmem_ld32(o_addr + ch * 32, o);
+    tc_wait_ld();
+#pragma unroll
+    for (int c = 0; c < 32; ++c) o[c] = __float_as_uint(bits_f(o[c]) * alpha);
+    tmem_st32(o_addr + ch * 32, o);
+  }
+  tc_wait_st();
+  return true;
+}
+
+// Whether the row sees a key of the half-tile whose row of V stands for NaN.  pages: null where it sees all keys.
 __device__ __noinline__ bool sees_nan(const uint8_t *nan4, const TcPage *pages, RowInfo ri) {
   bool seen = false;
-  for (int p = 0; p < kPagesPerTile; ++p) {
+  for (int p = 0; p < kPagesPerTile / 2; ++p) {
     const uint32_t w = *reinterpret_cast<const volatile uint32_t *>(nan4 + 4 * p);  // a byte of it: four keys
     const uint32_t keys = (w & 15u) | ((w >> 4) & 0xF0u) | ((w >> 8) & 0xF00u) | ((w >> 12) & 0xF000u);
     const int n = pages != nullptr ? page_n_ok(pages[p].meta, ri) : kPage;
@@ -353,7 +414,6 @@ attn_fp8_kernel(const __grid_constant__ CUtensorMap k_map, DevBatch d, DevTcPlan
   using Sh = Shape<kD>;
   constexpr int kQBytes = Sh::kQBytes, kTermBytes = Sh::kTermBytes, kCodeBytes = Sh::kCodeBytes, kVBytes = Sh::kVBytes, kGroupBytes = Sh::kGroupBytes;
   constexpr int kKStages = Sh::kKStages, kVStages = Sh::kVStages;
-  extern __shared__ __align__(1024) unsigned char smem[];
   if ((smem_u32(smem) & 1023u) != 0u) {  // the swizzled tiles need a 1024-byte aligned base
     if (threadIdx.x == 0) {
       d.status[0] = kDevBounds;
@@ -365,13 +425,13 @@ attn_fp8_kernel(const __grid_constant__ CUtensorMap k_map, DevBatch d, DevTcPlan
   unsigned char *k_smem = q_smem + 2 * kQBytes;  // kKStages half-tiles of codes
   unsigned char *v_smem = k_smem + kKStages * kCodeBytes;  // kVStages half-tiles of halves
   unsigned char *code_smem = v_smem + kVStages * kVBytes;  // a half-tile of V's codes for each converter
-  Ctrl *ctrl = reinterpret_cast<Ctrl *>(code_smem + kTeams * kCodeBytes);
+  Ctrl *ctrl = ctrl_at<kD>();
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
 
   // the plan is uploaded by copies, so it may be read in front of the wait for the kernel before
   const TcCtaHead *head = tc.heads + blockIdx.x;
   const int piece0 = head->piece0, piece1 = head->piece1;
-  if (warp == 14) {
+  if (warp == 8) {
     if (lane < (int)(sizeof(TcCtaHead) / 16)) reinterpret_cast<uint4 *>(&ctrl->head)[lane] = __ldg(reinterpret_cast<const uint4 *>(head) + lane);
     if (elect_one()) asm volatile("prefetch.tensormap [%0];" ::"l"(&k_map) : "memory");
   }
@@ -399,6 +459,7 @@ attn_fp8_kernel(const __grid_constant__ CUtensorMap k_map, DevBatch d, DevTcPlan
     for (int i = 0; i < kInfos; ++i) mbar_init(&ctrl->info_full[i], 1);
     ctrl->abort_flag = 0;
     ctrl->wait_limit_ns = (uint64_t)tc.wait_limit_us * 1000ull;
+    ctrl->status = d.status;
     fence_barrier_init();
   }
   if (warp == 12) {
@@ -439,7 +500,7 @@ attn_fp8_kernel(const __grid_constant__ CUtensorMap k_map, DevBatch d, DevTcPlan
                      vdesc0 = make_desc(smem_u32(v_smem), kAtomBytes, kGroupBytes);
       auto issue_qk = [&](int m, uint32_t stage, int half) {  // S_s[half] = (hi + lo) of Q_m times K^T over 64 keys
         const uint64_t a = qdesc0 + (uint64_t)(m * (kQBytes >> 4)), b = kdesc0 + (uint64_t)(stage * (kCodeBytes >> 4));
-#pragma unroll
+#pragma unroll 1
         for (int term = 0; term < 2; ++term)
 #pragma unroll
           for (int kk = 0; kk < kD / 32; ++kk)
@@ -454,74 +515,61 @@ attn_fp8_kernel(const __grid_constant__ CUtensorMap k_map, DevBatch d, DevTcPlan
       // waits, in ring order, until position `pos` has landed; positions on the way belong to the other stream and are released here
       auto need_k = [&](uint32_t pos) -> bool {
         for (; k_seen <= pos; ++k_seen) {
-          if (!wait(&ctrl->k_full[k_seen % kKStages], (k_seen / kKStages) & 1u, ctrl, d.status, 271)) return false;
+          if (!wait<kD, 1>(&ctrl->k_full[k_seen % kKStages], (k_seen / kKStages) & 1u, 271)) return false;
           if (k_seen < pos && elect_one()) mbar_arrive(&ctrl->k_empty[k_seen % kKStages]);
         }
         return true;
       };
       auto need_v = [&](uint32_t pos) -> bool {
         for (; v_seen <= pos; ++v_seen) {
-          if (!wait(&ctrl->v_full[v_seen % kVStages], (v_seen / kVStages) & 1u, ctrl, d.status, 272)) return false;
+          if (!wait<kD, 1>(&ctrl->v_full[v_seen % kVStages], (v_seen / kVStages) & 1u, 272)) return false;
           if (v_seen < pos && elect_one()) mbar_arrive(&ctrl->v_empty[v_seen % kVStages]);
         }
         return true;
       };
       for (int pc = piece0; pc < piece1 && ok; ++pc, ++pc_idx) {
-        const TcPiece pi = pc == piece0 ? head->first : tc.pieces[pc];
-        const int n = pi.tile_end - pi.tile_begin, mode = pi.n_mt;
+        const TcPiece *pi = pc == piece0 ? &head->first : tc.pieces + pc;
+        const int n = pi->tile_end - pi->tile_begin, mode = pi->n_mt;
         const int my_units = mode == 2 ? n : (n - s + 1) / 2, step = mode == 2 ? 2 : 4;  // half-tiles from a tile of this stream to its next
         const int m_tile = mode == 2 ? s : 0;
-        uint32_t pos = base + (mode == 2 ? 0u : 2u * s);  // of the stream's tile
-        ok = wait(&ctrl->q_full, pc_idx & 1u, ctrl, d.status, 270);
+        const uint32_t pos = base + (mode == 2 ? 0u : 2u * s);  // of the stream's first tile
+        ok = wait<kD, 1>(&ctrl->q_full, pc_idx & 1u, 270);
         if (!ok) break;
-        if (my_units > 0) {
-#pragma unroll 1
-          for (int half = 0; half < 2; ++half) {
-            ok = need_k(pos + half);
-            if (!ok) break;
-            tc_fence_after();
-            if (elect_one()) {
-              issue_qk(m_tile, (pos + half) % kKStages, half);
-              tc_commit(&ctrl->s_full[s][half]);
-              tc_commit(&ctrl->k_empty[(pos + half) % kKStages]);
-              if (half == 1 && my_units == 1) tc_commit(&ctrl->q_empty);  // last QK of the piece: this stream is done with the Q buffers
-            }
-            __syncwarp();
-          }
-          if (!ok) break;
-        } else {
+        if (my_units == 0) {
           if (elect_one()) mbar_arrive(&ctrl->q_empty);
+          // a stream with nothing to do here looks at the epilogue before too, so that the parity never is two phases behind
+          if (pc_idx > 0) ok = wait<kD, 1>(&ctrl->epi_done, (pc_idx - 1) & 1u, 273);
         }
-        if (pc_idx > 0) {  // the epilogue of the previous piece has read O_0 and O_1 (a stream with nothing to do here looks too, so that the parity
-                           // never is two phases behind)
-          ok = wait(&ctrl->epi_done, (pc_idx - 1) & 1u, ctrl, d.status, 273);
-          if (!ok) break;
-        }
-        for (int j = 0; j < my_units && ok; ++j, pos += step) {
-          const bool has_next = j + 1 < my_units;
+        // step j: O += P V of tile j, and the scores of tile j + 1 into the buffers that its weights leave; step -1 has scores alone
+        for (int j = my_units > 0 ? -1 : 0; j < my_units && ok; ++j) {
+          const bool has_pv = j >= 0, has_qk = j + 1 < my_units;
+          if (j == 0 && pc_idx > 0) {  // the epilogue of the previous piece has read O_0 and O_1
+            ok = wait<kD, 1>(&ctrl->epi_done, (pc_idx - 1) & 1u, 273);
+            if (!ok) break;
+          }
 #pragma unroll 1
           for (int half = 0; half < 2; ++half) {
-            const uint32_t pos_v = pos + half, pos_k = pos_v + step;
-            ok = need_v(pos_v) && (!has_next || need_k(pos_k));
-            if (!ok) break;
-            // P of this half is in place: O += P V, then the buffer takes the scores of the next tile's half
-            ok = wait(&ctrl->p_full[s][half], p_cnt & 1u, ctrl, d.status, 274 + s);
+            const uint32_t pos_v = pos + j * step + half, pos_k = pos_v + step;
+            ok = (!has_pv || need_v(pos_v)) && (!has_qk || need_k(pos_k));
+            if (ok && has_pv) ok = wait<kD, 1>(&ctrl->p_full[s][half], p_cnt & 1u, 274 + s);  // P of this half is in place
             if (!ok) break;
             tc_fence_after();
             if (elect_one()) {
-              issue_pv(pos_v % kVStages, half, (j | half) != 0);
-              tc_commit(&ctrl->o_done[s]);
-              tc_commit(&ctrl->v_empty[pos_v % kVStages]);
-              if (has_next) {
+              if (has_pv) {
+                issue_pv(pos_v % kVStages, half, (j | half) != 0);
+                tc_commit(&ctrl->o_done[s]);
+                tc_commit(&ctrl->v_empty[pos_v % kVStages]);
+              }
+              if (has_qk) {
                 issue_qk(m_tile, pos_k % kKStages, half);
                 tc_commit(&ctrl->s_full[s][half]);
                 tc_commit(&ctrl->k_empty[pos_k % kKStages]);
-                if (half == 1 && j + 2 == my_units) tc_commit(&ctrl->q_empty);  // last QK of the piece
+                if (half == 1 && j + 2 == my_units) tc_commit(&ctrl->q_empty);  // last QK of the piece: this stream is done with the Q buffers
               }
             }
             __syncwarp();
           }
-          ++p_cnt;
+          if (has_pv) ++p_cnt;
         }
         if (!ok) break;
         // half-tiles of the piece behind the last of this stream
@@ -545,78 +593,10 @@ attn_fp8_kernel(const __grid_constant__ CUtensorMap k_map, DevBatch d, DevTcPlan
           if (global_ns() - t0 > kDrainLimitNs) break;
       }
       __syncwarp();
-    } else if (warp == 14) {
-      // ======================= producer ====================================================
-      uint32_t tiles = 0, ring = 0;
-      bool ok = true;
-      for (int pc = piece0; pc < piece1 && ok; ++pc) {
-        const TcPiece pi = pc == piece0 ? head->first : tc.pieces[pc];
-        const TcReq rq = pc == piece0 ? head->first_req : tc.reqs[pi.req];
-        const int n = pi.tile_end - pi.tile_begin;
-        const TcPage *pages = tc.pages + rq.page_off + pi.tile_begin * kPagesPerTile + (lane >> 2);  // of the keys 4 lane .. 4 lane + 3
-        auto row_of = [&](int2 e) -> int32_t {  // first row of a page; rows of the pools are numbered within 32 bits (tc_plan_structure)
-          return (page_in_pool(e.x) * d.n_kv_heads + pi.kv_head) * kPage;
-        };
-        // A tile's page entries are asked for two tiles ahead, its scale bytes one.
-        int2 e = ld_pair(pages), e_next = ld_pair(pages + min(1, n - 1) * kPagesPerTile);
-        int32_t row = row_of(e);
-        uint32_t k_word = ld_word(in.k_scale + row + (lane & 3) * 4), v_word = ld_word(in.v_scale + row + (lane & 3) * 4);
-        for (int t = 0; t < n && ok; ++t, ++tiles) {
-          const uint32_t live = valid_bytes(e.y & 31, lane), kb = k_word & live, vb = v_word & live;
-          const int32_t my_row = row;
-          e = e_next;
-          row = row_of(e);
-          k_word = ld_word(in.k_scale + row + (lane & 3) * 4);
-          v_word = ld_word(in.v_scale + row + (lane & 3) * 4);
-          e_next = ld_pair(pages + min(t + 2, n - 1) * kPagesPerTile);
-          ok = wait(&ctrl->k_empty[ring % kKStages], ((ring / kKStages) & 1u) ^ 1u, ctrl, d.status, 210);
-          if (!ok) break;
-#pragma unroll
-          for (int half = 0; half < 2; ++half, ++ring) {
-            const uint32_t stage = ring % kKStages;
-            if (half == 1) {
-              ok = wait(&ctrl->k_empty[stage], ((ring / kKStages) & 1u) ^ 1u, ctrl, d.status, 211);
-              if (!ok) break;
-            }
-            if (lane == 0)
-              mbar_arrive_expect_tx(&ctrl->k_full[stage], (uint32_t)kCodeBytes + ((blockIdx.x == 0 && ring == 0) ? tc.phantom_tx_bytes : 0u));
-            __syncwarp();
-            // one box per page, absent pages of the last tile included (page 0 in their place: nobody looks at these scores)
-            if ((lane >> 4) == half && (lane & 3) == 0)
-              tma_load_2d(smem_u32(k_smem) + stage * kCodeBytes + ((lane >> 2) & 3) * (kPage * kD), &k_map, 0, my_row, &ctrl->k_full[stage]);
-            if (half == 0) {
-              Info &info = ctrl->info[tiles % kInfos];
-              // (a byte of a slot without a valid token is 0 here)
-              reinterpret_cast<float4 *>(info.k_scale)[lane] =
-                  make_float4(fp8_scale(kb & 0xFFu), fp8_scale((kb >> 8) & 0xFFu), fp8_scale((kb >> 16) & 0xFFu), fp8_scale(kb >> 24));
-              const uint32_t top = top_byte(vb), nan = __vcmpeq4(vb, 0xFFFFFFFFu);
-              const uint32_t ref0 = __reduce_max_sync(0xFFFFFFFFu, lane < 16 ? top : 0u), ref1 = __reduce_max_sync(0xFFFFFFFFu, lane >= 16 ? top : 0u);
-              const bool any = __any_sync(0xFFFFFFFFu, nan != 0u);
-              if (any) ctrl->v_nan[tiles % kInfos][lane] = (uint8_t)((nan & 1u) | ((nan >> 7) & 2u) | ((nan >> 14) & 4u) | ((nan >> 21) & 8u));
-              if (lane == 0) {
-                info.v_ref[0] = (int)max(ref0, 1u);
-                info.v_ref[1] = (int)max(ref1, 1u);
-                info.v_nan = any ? 1 : 0;
-              }
-              __syncwarp();
-              if (lane == 0) mbar_arrive(&ctrl->info_full[tiles % kInfos]);
-            }
-          }
-        }
-      }
-      if (!ok) {
-        // give the copies already in flight a bounded time to land before the CTA exits
-        for (uint32_t back = 1; back <= (uint32_t)kKStages && back <= ring; ++back) {
-          const uint32_t j = ring - back;
-          const uint64_t t0 = global_ns();
-          while (!mbar_try_wait(&ctrl->k_full[j % kKStages], (j / kKStages) & 1u))
-            if (global_ns() - t0 > kDrainLimitNs) break;
-        }
-      }
-    } else {
-      // ======================= converters of V ===============================================
+    } else if (warp < 12) {
+      // ======================= converters ====================================================
       constexpr int kCols = Sh::kCols, kGroups = Sh::kGroups, kRounds = Sh::kRounds;
-      const int team = warp < 12 ? warp - 8 : 4;
+      const int team = warp - 8;
       const int col = lane % kCols, grp = lane / kCols;  // 16 channels of keys (round * kGroups + grp) * 4 .. + 3
       // Eight neighbouring lanes store to two lines at a time whose 16-byte units lie in the same banks (both channel halves of a key, or with head size 64
       // keys four apart); half of them take their four keys in the order 1, 0, 3, 2, which brings the units of the two lines apart.
@@ -633,36 +613,8 @@ attn_fp8_kernel(const __grid_constant__ CUtensorMap k_map, DevBatch d, DevTcPlan
       const uint32_t mine = smem_u32(code_smem) + team * kCodeBytes + lane * 16;
 
       // the half-tiles of this warp: every kTeams-th of the CTA's
-      int pc = piece0, x = team, n_half = 0, n_whole = 0, kv_head = 0;  // of the half-tile that comes after the next one: its number within the piece
+      int pc = piece0 - 1, x = team, n_half = 0, n_whole = 0, kv_head = 0;  // x: the one asked for next, its number within piece pc
       const TcPage *pages = nullptr;
-      auto open = [&]() {
-        const TcPiece pi = pc == piece0 ? head->first : tc.pieces[pc];
-        const TcReq rq = pc == piece0 ? head->first_req : tc.reqs[pi.req];
-        n_half = 2 * (pi.tile_end - pi.tile_begin);
-        n_whole = 2 * (rq.n_dense_tiles - pi.tile_begin);  // half-tiles without slots of no valid token
-        kv_head = pi.kv_head;
-        pages = tc.pages + rq.page_off + pi.tile_begin * kPagesPerTile + ((lane >> 2) & 3);  // of the keys 4 lane .. 4 lane + 3 (lanes 16-31: again)
-      };
-      // moves on by kTeams half-tiles; the page of this lane's keys (asked for here), the KV head, and whether V has to be cleared there
-      struct Place {
-        int2 entry;
-        int32_t kv_head;
-        bool there, clear;
-      };
-      auto place = [&]() -> Place {
-        Place p;
-        while (pc < piece1 && x >= n_half) {
-          x -= n_half;
-          if (++pc < piece1) open();
-        }
-        p.there = pc < piece1;
-        p.kv_head = kv_head;
-        p.clear = x >= n_whole;
-        p.entry = make_int2(0, 0);
-        if (p.there) p.entry = ld_pair(pages + x * (kPagesPerTile / 2));
-        x += kTeams;
-        return p;
-      };
       auto fetch = [&](int32_t row, int u) {  // part u of the codes of the pages with those rows
         // (a lane whose row is that of the page of this lane's keys; an absent page of the last tile reads page 0 and is cleared below)
         const uint8_t *at = in.v + k_off + (int64_t)__shfl_sync(0xFFFFFFFFu, row, ((u * kGroups + grp) >> 2) * 4) * kD;
@@ -672,60 +624,130 @@ attn_fp8_kernel(const __grid_constant__ CUtensorMap k_map, DevBatch d, DevTcPlan
         copy_codes(mine + u * 2048 + 1024, even + 2 * kD);
         copy_codes(mine + u * 2048 + 1536, other + 3 * kD);
       };
-      open();
-      Place nxt = place();
-      int32_t row = (page_in_pool(nxt.entry.x) * d.n_kv_heads + nxt.kv_head) * kPage;  // rows of the pools are numbered within 32 bits (tc_plan_structure)
-      uint32_t word = ld_word(in.v_scale + row + (lane & 3) * 4);
-#pragma unroll
-      for (int u = 0; u < kRounds; ++u) {
-        if (nxt.there) fetch(row, u);
-        asm volatile("cp.async.commit_group;" ::: "memory");
-      }
-      Place after = place();
-      for (uint32_t ring = (uint32_t)team; nxt.there; ring += kTeams) {
-        // Loads into registers are asked for here and looked at a half-tile later.
-        const uint32_t live = valid_bytes(nxt.entry.y & 31, lane), bytes = word & live;
-        const bool clear = nxt.clear;
-        nxt = after;
-        row = (page_in_pool(nxt.entry.x) * d.n_kv_heads + nxt.kv_head) * kPage;
-        word = ld_word(in.v_scale + row + (lane & 3) * 4);
-        after = place();
-        const int ref = (int)max(__reduce_max_sync(0xFFFFFFFFu, top_byte(bytes)), 1u);  // (what the producer publishes)
-        // the factors of this lane's four keys, which other lanes ask for
-        const uint32_t f01 = factors(bytes & 0xFFu, (bytes >> 8) & 0xFFu, ref), f23 = factors((bytes >> 16) & 0xFFu, bytes >> 24, ref);
+      // Loads into registers are looked at a half-tile later: the page entries of one, the scale bytes of the one before it, whose codes of K and V are asked
+      // for, and the one before that, whose V is converted.
+      int2 e = make_int2(0, 0);
+      int e_head = -1;                // KV head of the half-tile whose page entries are on their way, -1: there is none
+      uint32_t k_word = 0, word = 0, meta = 0;  // scale bytes of keys 4 lane .. 4 lane + 3 (lanes 16-31: again) and valid tokens of their page, of the one before
+      bool e_clear = false, word_clear = false;  // whether it has slots without a valid token
+      bool words = false, ok = true;
+      uint32_t asked = (uint32_t)team;  // ring position of K asked for next
+#pragma unroll 1
+      for (uint32_t ring = (uint32_t)team;;) {
+        const bool there = words, clear = word_clear;
+        const uint32_t live = valid_bytes((int)(meta & 31u), lane), bytes = word & live;
+        words = e_head >= 0;
+        int32_t row = 0;
+        if (words) {
+          row = (page_in_pool(e.x) * d.n_kv_heads + e_head) * kPage;  // rows of the pools are numbered within 32 bits (tc_plan_structure)
+          meta = (uint32_t)e.y;
+          word = ld_word(in.v_scale + row + (lane & 3) * 4);
+          k_word = ld_word(in.k_scale + row + (lane & 3) * 4);
+          word_clear = e_clear;
+        }
+        while (pc < piece1 && x >= n_half) {
+          x -= n_half;
+          if (++pc >= piece1) break;
+          const TcPiece *pi = pc == piece0 ? &head->first : tc.pieces + pc;
+          const TcReq *rq = pc == piece0 ? &head->first_req : tc.reqs + pi->req;
+          n_half = 2 * (pi->tile_end - pi->tile_begin);
+          n_whole = 2 * (rq->n_dense_tiles - pi->tile_begin);  // half-tiles without slots of no valid token
+          kv_head = pi->kv_head;
+          pages = tc.pages + rq->page_off + pi->tile_begin * kPagesPerTile + ((lane >> 2) & 3);
+        }
+        e_head = -1;
+        if (pc < piece1) {
+          e = ld_pair(pages + x * (kPagesPerTile / 2));
+          e_head = kv_head;
+          e_clear = x >= n_whole;
+          x += kTeams;
+        }
         const uint32_t stage = ring % kVStages, to = stage * kVBytes;
-        if (!wait(&ctrl->v_empty[stage], ((ring / kVStages) & 1u) ^ 1u, ctrl, d.status, 212)) break;
+        uint32_t f01 = 0, f23 = 0;
+        if (there) {
+          const int ref = (int)max(__reduce_max_sync(0xFFFFFFFFu, top_byte(bytes)), 1u);
+          // the factors of this lane's four keys, which other lanes ask for
+          f01 = factors(bytes & 0xFFu, (bytes >> 8) & 0xFFu, ref);
+          f23 = factors((bytes >> 16) & 0xFFu, bytes >> 24, ref);
+          ok = wait<kD, 1>(&ctrl->v_empty[stage], ((ring / kVStages) & 1u) ^ 1u, 212);
+          if (!ok) break;
+        }
 #pragma unroll 1
         for (int u = 0; u < kRounds; ++u) {
-          asm volatile("cp.async.wait_group %0;" ::"n"(kRounds - 1) : "memory");
-          uint4 c[4];
+          if (there) {
+            asm volatile("cp.async.wait_group %0;" ::"n"(kRounds - 1) : "memory");
+            uint4 c[4];
 #pragma unroll
-          for (int j = 0; j < 4; ++j) c[j] = ld_shared(mine + u * 2048 + j * 512);
-          const uint32_t by[2] = {__shfl_sync(0xFFFFFFFFu, f01, u * kGroups + grp), __shfl_sync(0xFFFFFFFFu, f23, u * kGroups + grp)};
-          if (clear) {
-            const uint32_t l4 = __shfl_sync(0xFFFFFFFFu, live, u * kGroups + grp);
+            for (int j = 0; j < 4; ++j) c[j] = ld_shared(mine + u * 2048 + j * 512);
+            const uint32_t by[2] = {__shfl_sync(0xFFFFFFFFu, f01, u * kGroups + grp), __shfl_sync(0xFFFFFFFFu, f23, u * kGroups + grp)};
+            if (clear) {
+              const uint32_t l4 = __shfl_sync(0xFFFFFFFFu, live, u * kGroups + grp);
 #pragma unroll
-            for (int j = 0; j < 4; ++j)
-              if (((l4 >> (8 * (j ^ odd))) & 1u) == 0u) c[j] = make_uint4(0, 0, 0, 0);
+              for (int j = 0; j < 4; ++j)
+                if (((l4 >> (8 * (j ^ odd))) & 1u) == 0u) c[j] = make_uint4(0, 0, 0, 0);
+            }
+            const uint32_t at = to + u * (kGroups / 2) * kGroupBytes;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+              const uint32_t f = __byte_perm(by[j >> 1], 0u, ((j & 1) != 0) != (odd != 0) ? 0x3232 : 0x1010);
+              uint32_t h[8];
+              halves4(c[j].x, f, h[0], h[1]);
+              halves4(c[j].y, f, h[2], h[3]);
+              halves4(c[j].z, f, h[4], h[5]);
+              halves4(c[j].w, f, h[6], h[7]);
+              st_shared(off[j] + at, h[0], h[1], h[2], h[3]);
+              st_shared((off[j] + at) ^ 16u, h[4], h[5], h[6], h[7]);
+            }
           }
-          const uint32_t at = to + u * (kGroups / 2) * kGroupBytes;
-#pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            const uint32_t f = __byte_perm(by[j >> 1], 0u, ((j & 1) != 0) != (odd != 0) ? 0x3232 : 0x1010);
-            uint32_t h[8];
-            halves4(c[j].x, f, h[0], h[1]);
-            halves4(c[j].y, f, h[2], h[3]);
-            halves4(c[j].z, f, h[4], h[5]);
-            halves4(c[j].w, f, h[6], h[7]);
-            st_shared(off[j] + at, h[0], h[1], h[2], h[3]);
-            st_shared((off[j] + at) ^ 16u, h[4], h[5], h[6], h[7]);
-          }
-          if (nxt.there) fetch(row, u);
+          if (words) fetch(row, u);
           asm volatile("cp.async.commit_group;" ::: "memory");
         }
-        fence_proxy_async();
-        __syncwarp();
-        if (lane == 0) mbar_arrive(&ctrl->v_full[stage]);
+        if (there) {
+          fence_proxy_async();
+          __syncwarp();
+          if (lane == 0) mbar_arrive(&ctrl->v_full[stage]);
+          ring += kTeams;
+        }
+        if (words) {
+          // K of the next half-tile, and what the softmax has to know of its keys, V's scales among it
+          const uint32_t k_stage = asked % kKStages;
+          ok = wait<kD, 1>(&ctrl->k_empty[k_stage], ((asked / kKStages) & 1u) ^ 1u, 210);
+          if (!ok) break;
+          if (lane == 0)
+            mbar_arrive_expect_tx(&ctrl->k_full[k_stage], (uint32_t)kCodeBytes + ((blockIdx.x == 0 && asked == 0) ? tc.phantom_tx_bytes : 0u));
+          __syncwarp();
+          // one box per page, absent pages of the last tile included (page 0 in their place: nobody looks at these scores)
+          if (lane < 16 && (lane & 3) == 0)
+            tma_load_2d(smem_u32(k_smem) + k_stage * kCodeBytes + (lane >> 2) * (kPage * kD), &k_map, 0, row, &ctrl->k_full[k_stage]);
+          Info &info = ctrl->info[asked % kInfos];
+          const uint32_t now = valid_bytes((int)(meta & 31u), lane), kb = k_word & now, vb = word & now, nan = __vcmpeq4(vb, 0xFFFFFFFFu);
+          const uint32_t v_ref = max(__reduce_max_sync(0xFFFFFFFFu, top_byte(vb)), 1u);
+          const bool any = __any_sync(0xFFFFFFFFu, nan != 0u);
+          if (lane < 16) {  // (a byte of a slot without a valid token is 0 here: its scores are not looked at)
+            float4 f;
+            f.x = __uint_as_float((kb & 0xFFu) << 23);
+            f.y = __uint_as_float((kb << 15) & 0x7F800000u);
+            f.z = __uint_as_float((kb << 7) & 0x7F800000u);
+            f.w = __uint_as_float((kb >> 1) & 0x7F800000u);
+            reinterpret_cast<float4 *>(info.k_scale)[lane] = f;
+            if (any) info.nan4[lane] = (uint8_t)((nan & 1u) | ((nan >> 7) & 2u) | ((nan >> 14) & 4u) | ((nan >> 21) & 8u));
+          }
+          if (lane == 0) *reinterpret_cast<int2 *>(&info.v_ref) = make_int2((int)v_ref, any ? 1 : 0);
+          __syncwarp();
+          if (lane == 0) mbar_arrive(&ctrl->info_full[asked % kInfos]);
+          asked += kTeams;
+        }
+        if (!words && e_head < 0) break;
+      }
+      if (!ok) {
+        // give the copies of K already in flight a bounded time to land before the CTA exits
+        for (int back = 0; back < kKStages; ++back) {
+          if (asked < (uint32_t)kTeams + (uint32_t)team) break;
+          asked -= kTeams;
+          const uint64_t t0 = global_ns();
+          while (!mbar_try_wait(&ctrl->k_full[asked % kKStages], (asked / kKStages) & 1u))
+            if (global_ns() - t0 > kDrainLimitNs) break;
+        }
       }
       asm volatile("cp.async.wait_group 0;" ::: "memory");  // (after an abort some are still on their way)
     }
@@ -750,7 +772,7 @@ attn_fp8_kernel(const __grid_constant__ CUtensorMap k_map, DevBatch d, DevTcPlan
       float sc_row = 0.f;
       if (ok) {
         // the queries, once the products of the piece before no longer read the buffers; with one M-tile each stream stores its part
-        ok = wait(&ctrl->q_empty, ((uint32_t)(pc - piece0) & 1u) ^ 1u, ctrl, d.status, 245);
+        ok = wait<kD, 0>(&ctrl->q_empty, ((uint32_t)(pc - piece0) & 1u) ^ 1u, 245);
         if (ok) {
           sc_row = scale_log2 * convert_q<kD>(q, ri.q_index, smem_u32(q_smem) + (mode == 2 ? s : 0) * kQBytes, r, mode == 2 ? 0 : s, mode == 2 ? 2 : s + 1);
           fence_proxy_async();
@@ -758,68 +780,36 @@ attn_fp8_kernel(const __grid_constant__ CUtensorMap k_map, DevBatch d, DevTcPlan
         }
       }
       if (ok && my_units > 0) {
-        float m_used = -INFINITY, l = 0.f;
+        float m_used = -INFINITY, l = 0.f;  // the row's reference exponent and sum
         int base = 0;
         bool s_ready = false, nan_v = false;
-        uint32_t nan_at = kInfos;  // place of a tile in which some row of V stands for NaN
-        // O *= alpha.  The PV product of the previous half-unit must have retired first; the one before
-        // it has (its commit precedes the s_full this thread has just seen), so o_done has completed done_needed or
-        // done_needed - 1 phases and the parity says which, whether or not this thread has looked at the earlier ones.
-        auto rescale_o = [&](float alpha, uint32_t done_needed) -> bool {
-          if (!wait(&ctrl->o_done[s], (done_needed - 1) & 1u, ctrl, d.status, 235 + s)) return false;
-          tc_fence_after();
-#pragma unroll 1
-          for (int ch = 0; ch < kD / 32; ++ch) {
-            uint32_t o[32];
-            tmem_ld32(o_addr + ch * 32, o);
-            tc_wait_ld();
-#pragma unroll
-            for (int c = 0; c < 32; ++c) o[c] = __float_as_uint(bits_f(o[c]) * alpha);
-            tmem_st32(o_addr + ch * 32, o);
-          }
-          tc_wait_st();
-          return true;
-        };
         // A warp whose 32 rows are all padding only keeps the barriers' counts: what it leaves as weights multiplies into rows
         // of O that nobody reads.
         const bool idle = __all_sync(0xFFFFFFFFu, ri.q_index < 0);
         if (idle) {
           for (int u = 0; u < 2 * my_units && ok; ++u) {
-            ok = wait(&ctrl->s_full[s][u & 1], (s_cnt + (uint32_t)(u >> 1)) & 1u, ctrl, d.status, 230 + s);
-            if (ok && u + 1 == 2 * my_units) ok = wait(&ctrl->o_done[s], (o_cnt + (uint32_t)u - 1) & 1u, ctrl, d.status, 237 + s);
+            ok = wait<kD, 0>(&ctrl->s_full[s][u & 1], (s_cnt + (uint32_t)(u >> 1)) & 1u, 230 + s);
+            if (ok && u + 1 == 2 * my_units) ok = wait<kD, 0>(&ctrl->o_done[s], (o_cnt + (uint32_t)u - 1) & 1u, 237 + s);
             if (ok) mbar_arrive(&ctrl->p_full[s][u & 1]);
           }
           s_cnt += (uint32_t)my_units;
         }
         for (int j = 0; j < my_units && ok && !idle; ++j) {
           const int local = mode == 2 ? j : 2 * j + s, t = pi.tile_begin + local;
-          const bool masked = t >= rq.n_dense_tiles;
-          int n_ok[kPagesPerTile];
-          if (masked) {
-            const uint4 *mp = reinterpret_cast<const uint4 *>(tc.pages + rq.page_off + t * kPagesPerTile);
-#pragma unroll
-            for (int jj = 0; jj < 4; ++jj) {
-              const uint4 w = __ldg(mp + jj);
-              n_ok[2 * jj] = page_n_ok(w.y, ri);
-              n_ok[2 * jj + 1] = page_n_ok(w.w, ri);
-            }
-          }
+          const TcPage *pages = t >= rq.n_dense_tiles ? tc.pages + rq.page_off + t * kPagesPerTile : nullptr;
 #pragma unroll 1  // one copy of the sweep: the unrolled pair is slower (instruction fetch)
           for (int half = 0; half < 2; ++half) {
             const uint32_t sh_addr = s_addr + half * 64;
+            const uint32_t at = (tiles + (uint32_t)local) * 2u + half;  // half-tiles of both streams before this one
+            const Info &info = ctrl->info[at % kInfos];
             const uint32_t g = o_cnt + (uint32_t)(2 * j + half);  // half-units of this stream before this one
-            const uint32_t at = tiles + (uint32_t)local;  // tiles of both streams before this one
-            const bool first = (j | half) == 0;
             if (!s_ready) {
-              ok = wait(&ctrl->info_full[at % kInfos], (at / kInfos) & 1u, ctrl, d.status, 248) && wait(&ctrl->s_full[s][half], s_cnt & 1u, ctrl, d.status, 230 + s);
+              ok = wait<kD, 0>(&ctrl->info_full[at % kInfos], (at / kInfos) & 1u, 248) && wait<kD, 0>(&ctrl->s_full[s][half], s_cnt & 1u, 230 + s);
               if (!ok) break;
             }
             tc_fence_after();
-            uint32_t v[64];
-            tmem_ld64(sh_addr, v);
-            const Info &info = ctrl->info[at % kInfos];
-            const int v_ref = info.v_ref[half];
-            if (info.v_nan) nan_at = at % kInfos;
+            const int v_ref = info.v_ref;
+            const bool first = (j | half) == 0;
             float alpha = 1.0f;  // what O has to be multiplied by before this half's product
             if (first) base = v_ref;
             if (v_ref > base + kRise) {
@@ -827,27 +817,31 @@ attn_fp8_kernel(const __grid_constant__ CUtensorMap k_map, DevBatch d, DevTcPlan
               base = v_ref;
             }
             const int off = v_ref - base;
-            const float bias = (float)off + kHead;
-            bool apart = off < -kApart;  // the sums first, of weights as they are
+            uint32_t v[64];
+            tmem_ld64(sh_addr, v);
             tc_wait_ld();
             // the scores after these (and what is known of their keys) are looked for under the exponentials: a test costs over 100 cycles even
             // when it succeeds
-            const uint32_t next = at + (half == 0 ? 0u : mode == 2 ? 1u : 2u);
-            const uint32_t next_ready = mbar_test_wait2(&ctrl->s_full[s][half ^ 1], (s_cnt + (uint32_t)half) & 1u, &ctrl->info_full[next % kInfos],
-                                                        (next / kInfos) & 1u) == 3u;
+            const uint32_t next = at + (half == 0 || mode == 2 ? 1u : 3u);
+            const uint32_t next_ready = mbar_test_wait2(&ctrl->s_full[s][half ^ 1], (s_cnt + (uint32_t)half) & 1u, &ctrl->info_full[next % kInfos], (next / kInfos) & 1u) == 3u;
+            scale_half(v, info.k_scale);
+            if (pages != nullptr) {
+              int n_ok[kPagesPerTile / 2];
 #pragma unroll
-            for (int i = 0; i < 64; i += 4) {
-              const float4 ks = *reinterpret_cast<const float4 *>(info.k_scale + half * 64 + i);
-              mul2(v[i], v[i + 1], ks.x, ks.y);
-              mul2(v[i + 2], v[i + 3], ks.z, ks.w);
+              for (int p = 0; p < kPagesPerTile / 2; ++p) n_ok[p] = page_n_ok(__ldg(&pages[half * 4 + p].meta), ri);
+              mask_half(v, n_ok);
             }
-            if (masked) mask_half(v, n_ok + 4 * half);
-            // Exponentials against the running reference exponent, the maximum of the 64 scores beside them.  Where that is beyond what a half holds
-            // (and on a row's first keys) they are done again with the reference moved to it.
+            // Exponentials against the running reference exponent.  Where the maximum is beyond what a half holds (and on a row's first keys) they are done
+            // again with the reference moved to it; values far below the accumulator's unit have their weights summed apart, as they are.
+            bool apart = off < -kApart;
             for (;;) {
               float raw;
-              const float sum = exp_half(v, sh_addr, sc_row, m_used == -INFINITY ? 0.f : (apart ? 0.f : bias) - m_used, raw), mx = raw * sc_row;
+              const float sum = exp_half(v, sh_addr, sc_row, m_used == -INFINITY ? 0.f : (apart ? 0.f : (float)off + kHead) - m_used, raw), mx = raw * sc_row;
               const bool grow = mx > m_used + kGrow;  // (a row that has seen nothing: by any score)
+              if (!apart && !__any_sync(0xFFFFFFFFu, grow)) {
+                if (off >= -kApart) l = fmaf(sum, pow2(-off - (int)kHead), l);
+                break;
+              }
               if (__any_sync(0xFFFFFFFFu, grow)) {
                 if (grow) {
                   if (m_used > -INFINITY) {
@@ -857,20 +851,14 @@ attn_fp8_kernel(const __grid_constant__ CUtensorMap k_map, DevBatch d, DevTcPlan
                   }
                   m_used = mx;
                 }
-                tc_wait_st();
-                continue;
-              }
-              if (apart) {
+              } else {
                 l += sum;
                 apart = false;
-                tc_wait_st();
-                continue;
               }
-              if (off >= -kApart) l = fmaf(sum, pow2(-off - (int)kHead), l);
-              break;
+              tc_wait_st();
             }
             if (!first && __any_sync(0xFFFFFFFFu, alpha != 1.0f)) {
-              ok = rescale_o(alpha, g);
+              ok = rescale_rows<kD>(o_addr, alpha, &ctrl->o_done[s], g, 235 + s);
               if (!ok) break;
             }
             tc_wait_st();
@@ -879,13 +867,11 @@ attn_fp8_kernel(const __grid_constant__ CUtensorMap k_map, DevBatch d, DevTcPlan
             // The wait at the end must not find o_done two phases back (one parity for both): the last arrive comes
             // after the product before has been seen to retire.
             if (half == 1 && j + 1 == my_units) {
-              ok = wait(&ctrl->o_done[s], (g - 1) & 1u, ctrl, d.status, 237 + s);
+              ok = wait<kD, 0>(&ctrl->o_done[s], (g - 1) & 1u, 237 + s);
               if (!ok) break;
             }
-            if (nan_at < kInfos) {  // (before the arrival: what it looks at may be replaced behind it)
-              nan_v = sees_nan(ctrl->v_nan[nan_at], masked ? tc.pages + rq.page_off + t * kPagesPerTile : nullptr, ri) || nan_v;
-              nan_at = kInfos;
-            }
+            // (before the arrival: what it looks at may be replaced behind it)
+            if (info.v_nan) nan_v = sees_nan(info.nan4, pages == nullptr ? nullptr : pages + half * 4, ri) || nan_v;
             mbar_arrive(&ctrl->p_full[s][half]);
           }
           ++s_cnt;
@@ -893,7 +879,7 @@ attn_fp8_kernel(const __grid_constant__ CUtensorMap k_map, DevBatch d, DevTcPlan
         if (ok) {
           // epilogue: wait for the last PV of this stream, then normalise and store
           o_cnt += 2u * (uint32_t)my_units;
-          ok = wait(&ctrl->o_done[s], (o_cnt - 1) & 1u, ctrl, d.status, 240 + s);
+          ok = wait<kD, 0>(&ctrl->o_done[s], (o_cnt - 1) & 1u, 240 + s);
         }
         // what the accumulator's numbers are worth; NaN for a row that sees a row of V that is
         const float unit = nan_v ? __uint_as_float(0x7FC00000u) : exp2f((float)(base - 127) - kHead);
@@ -912,7 +898,7 @@ attn_fp8_kernel(const __grid_constant__ CUtensorMap k_map, DevBatch d, DevTcPlan
             mbar_arrive(&ctrl->xch);
             writer = false;
           } else {
-            ok = wait(&ctrl->xch, x_cnt & 1u, ctrl, d.status, 242);
+            ok = wait<kD, 0>(&ctrl->xch, x_cnt & 1u, 242);
             if (ok) {
               tc_fence_after();
               const float om = ctrl->xch_m[r], ol = ctrl->xch_l[r];
@@ -936,7 +922,7 @@ attn_fp8_kernel(const __grid_constant__ CUtensorMap k_map, DevBatch d, DevTcPlan
       // One arrival per thread and piece.  A stream with units in this piece cannot get here before the previous
       // piece's phase is complete (its PV products were issued behind a wait for it); a stream with none must look
       // itself, or its arrival would be counted into the previous phase while the other stream is still storing.
-      if (my_units == 0 && pc > piece0 && ok) ok = wait(&ctrl->epi_done, (uint32_t)(pc - piece0 - 1) & 1u, ctrl, d.status, 243);
+      if (my_units == 0 && pc > piece0 && ok) ok = wait<kD, 0>(&ctrl->epi_done, (uint32_t)(pc - piece0 - 1) & 1u, 243);
       mbar_arrive(&ctrl->epi_done);
       tiles += (uint32_t)n;
     }
