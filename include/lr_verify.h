@@ -478,9 +478,13 @@ int lr_fp8_read(lr_ctx *ctx, const lr_fp8_cache *cache, const int64_t *slots_d, 
  * lr_verify_attention on such a cache (cache->n_pages >= the plan's n_pool_pages,
  * else LR_EINVAL): same plan, queries, outputs and errors, for a chain or a tree of
  * draft steps.  Rows of K and V enter as the values they stand for; products are
- * summed and the softmax is done in fp32.  A row of the cache that a query sees and
- * that stands for NaN makes the query's output NaN; one that it does not see has no
- * influence, whatever it holds.  lr_plan_set_attention_path: 0 automatic, 1 CUDA
+ * summed and the softmax is done in fp32.  The rows of tokens are such as
+ * lr_fp8_write leaves; slots that hold no token of the plan may hold anything.  A
+ * row that stands for NaN (byte 255, codes 0) makes the output of a query that sees
+ * it NaN and does not touch the others.  The tensor cores take softmax weights as
+ * halves, in units of the largest scale of V: a key's part of an output is off by
+ * at most 2^-11 of itself or 2^-23 of the largest number of V among the request's
+ * tokens (of that KV head).  lr_plan_set_attention_path: 0 automatic, 1 CUDA
  * cores, 2 tensor cores; there is no CTA-pair kernel for this cache (3:
  * LR_EUNSUPPORTED).
  */

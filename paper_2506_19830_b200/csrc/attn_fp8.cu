@@ -17,17 +17,17 @@
 // may have any weight.  Weights lie 2^6 above what they are and reach 2^15 at most: 11 bits instead of bf16's 8, nothing lost above 2^-20 of the
 // largest, and a row whose scores grow by more than 2^6 does its half-tile again.
 //
-// One CTA = 16 warps in four warpgroups, registers moved with setmaxnreg (176 x 256 + 80 x 256 = 128 x 512):
-//   warp 14      producer: per tile of 128 keys 8 boxes of K (a page each), the keys' scales as fp32, ref of V's half-tiles.
-//   warps 8-11  converters: the codes of a half-tile of V (64 keys) by asynchronous copies into a buffer of the warp's own, the next one's taking the
-//                place of each part as it is read; halves into the ring as the swizzled operand.  A warp has the half-tile's scale bytes in one word
-//                a lane, so that ref is one reduction and a key's factor one shuffle.  Slots that hold no valid token become zeros, whatever they held.
+// One CTA = 16 warps in four warpgroups, registers moved with setmaxnreg (168 x 256 + 88 x 256 = 128 x 512):
+//   warps 8-11  converters, each with every fourth half-tile (64 keys): the codes of V by asynchronous copies into a buffer of the warp's own, the next
+//                one's taking the place of each part as it is read; halves into the ring as the swizzled operand.  A warp has the half-tile's scale
+//                bytes in one word a lane, so that ref is one reduction and a key's factor one shuffle.  Slots that hold no valid token become
+//                zeros, whatever they held.  A warp also asks for K of its half-tiles, 4 boxes of a page each, and publishes the keys' scales and ref.
 //   warps 13, 14  MMA issuers of stream 0 and 1 (not 12: with few queries the rows that live are those of the warps that share its quarter of the SM).
 //   warps 0-3, 4-7  softmax of stream 0 and 1, one thread per query row; they also turn the rows of Q into their two terms.
 // All of it shares an SM's instruction cache; a version with everything unrolled and in line, K converted to halves as well, took three times as long.
 //
 // A visible row that stands for NaN: K's has a scale of NaN, and with it the row's sum is.  V's becomes zeros, for a weight of 0 times NaN
-// would reach rows that do not see it; the producer notes such keys per tile, and a row that sees one multiplies its result by NaN.
+// would reach rows that do not see it; the converter notes such keys per half-tile, and a row that sees one multiplies its result by NaN.
 #include <cuda.h>
 
 #include <algorithm>
@@ -39,14 +39,13 @@ namespace lr {
 
 namespace {
 
-constexpr int kHalfBytes = 16384;  // 128 rows of Q x 64 channels
-constexpr int kAtomBytes = 1024;   // 8 keys x 64 channels, one 128-byte-swizzle atom
-constexpr int kMaxStages = 16;
+constexpr int kAtomBytes = 1024;   // 8 keys of V x 64 channels as halves, one 128-byte-swizzle atom
+constexpr int kMaxK = 8, kMaxV = 8;
 constexpr int kThreads = 512;
-constexpr int kTeams = 6;          // converter warps, each with half-tiles of its own
-// Half-tiles whose scales are published ahead of their products.  A converter writes those of half-tile x + kInfos once the stage that its K takes is free; an
-// issuer releases the stage of K of x + 4 behind the weights of its last half-tile up to x at the earliest, and between the two lie more half-tiles than
-// the ring has stages.
+constexpr int kTeams = 4;          // converter warps, each with half-tiles of its own
+// Half-tiles whose scales are published ahead of their products.  A converter writes those of half-tile x + kInfos once the stage of K that it takes is
+// free, which half-tile x + kInfos - kKStages had; from x + 6 (three tiles) on, that tells that no softmax thread will look at x again: an issuer
+// asks for or skips x + 6 behind the weights of its last half-tile up to x.
 constexpr int kInfos = 16;
 constexpr float kLift = 3.0f;      // log2: a row's reference exponent is set this much above its maximum so far,
 constexpr float kGrow = 11.0f;     // log2: ... scores may rise this much above it,
@@ -57,25 +56,28 @@ constexpr int kApart = 24;         // log2: V this far below the unit has its we
 template <int kD>
 struct Shape {
   static_assert(kD == 64 || kD == 128, "head sizes of the tensor-core path");
-  static constexpr int kHalves = kD / 64;                   // 64-channel halves of a row (one 128-byte swizzle line each)
-  static constexpr int kQBytes = kHalves * kHalfBytes;      // an M-tile of Q: [halves][128 rows][128 B]
-  static constexpr int kGroupBytes = kHalves * kAtomBytes;  // the atoms of one 8-key group
-  static constexpr int kStageBytes = 8 * kGroupBytes;       // 64 keys as halves: [8 groups][halves][8 keys][128 B]
-  static constexpr int kStages = kD == 128 ? 7 : 8;
+  static constexpr int kHalves = kD / 64;                   // 64-channel halves of a row of V (one 128-byte swizzle line each)
+  static constexpr int kTermBytes = 128 * kD;               // a term of an M-tile of Q: 128 rows of kD bytes
+  static constexpr int kQBytes = 2 * kTermBytes;
+  static constexpr int kCodeBytes = 64 * kD;                // a half-tile (64 keys) as it comes
+  static constexpr int kGroupBytes = kHalves * kAtomBytes;  // the atoms of 8 keys of V
+  static constexpr int kVBytes = 8 * kGroupBytes;           // a half-tile of V as halves: [8 groups][halves][8 keys][128 B]
+  static constexpr int kKStages = kD == 128 ? 4 : 8, kVStages = kD == 128 ? 4 : 8;
   static constexpr int kCols = kD / 16;                     // lanes side by side in a row, 16 channels each
   static constexpr int kGroups = 32 / kCols;                // groups of four keys that a warp has at a time
   static constexpr int kRounds = 16 / kGroups;              // ... and how many times for a half-tile
-  static constexpr int kCodeBytes = 64 * kD;                // a half-tile as it comes
 };
 
-struct Info {  // of a half-tile: 2 to the power of the largest scale of its keys, V's largest scale byte, whether some valid row of V stands for NaN
-  float k_scale;
-  int32_t v_ref, v_nan;
+struct Info {  // of a half-tile: the keys' scales, the largest scale byte of V, whether some valid row of V stands for NaN (and which: four keys a byte)
+  float k_scale[64];
+  int32_t v_ref, v_nan, pad[2];
+  uint8_t nan4[16];
 };
 
 struct __align__(16) Ctrl {
   TcCtaHead head;         // this CTA's record
-  uint64_t kv_full[kMaxStages], kv_empty[kMaxStages];
+  Info info[kInfos];
+  uint64_t k_full[kMaxK], k_empty[kMaxK], v_full[kMaxV], v_empty[kMaxV];
   uint64_t q_full, q_empty;
   uint64_t s_full[2][2], p_full[2][2], o_done[2];  // [stream][half]
   uint64_t epi_done, drain[2];
@@ -85,55 +87,52 @@ struct __align__(16) Ctrl {
   int abort_flag;
   uint64_t wait_limit_ns;
   int32_t *status;        // the plan's
-  Info info[kInfos];
-  uint8_t nan4[kInfos][16];  // four keys a byte
   float xch_m[128], xch_l[128], xch_unit[128];  // stream 1's rows, for the in-CTA combination
 };
-constexpr int kCtrlBytes = 3 << 10;
+constexpr int kCtrlBytes = 7 << 10;
 static_assert(sizeof(Ctrl) <= kCtrlBytes, "Ctrl must fit behind the tiles");
 template <int kD>
-constexpr int kSmemBytes = 2 * Shape<kD>::kQBytes + Shape<kD>::kStages * Shape<kD>::kStageBytes + kTeams * Shape<kD>::kCodeBytes + kCtrlBytes;  // the base must be 1024-aligned
-static_assert(kSmemBytes<64> <= 227 * 1024 && kSmemBytes<128> <= 227 * 1024, "shared memory per CTA");
-// A converter at position r of the ring has filled position r - kTeams, whose stage position r - kTeams - kStages had been released from.  Releases are in
+constexpr int kSmemBytes = 2 * Shape<kD>::kQBytes + Shape<kD>::kKStages * Shape<kD>::kCodeBytes + Shape<kD>::kVStages * Shape<kD>::kVBytes +
+                           kTeams * Shape<kD>::kCodeBytes + kCtrlBytes;  // the base must be 1024-aligned
+static_assert(kInfos - Shape<64>::kKStages >= 6 && kInfos - Shape<128>::kKStages >= 6, "see kInfos");
+// A converter at position r of a ring has filled position r - kTeams, whose stage position r - kTeams - stages had been released from.  Releases are in
 // order, so with no more teams than stages the release before the one it waits for has happened, and the parity of the barrier means what it
 // looks for.
-static_assert(kTeams <= Shape<64>::kStages && kTeams <= Shape<128>::kStages, "a converter must not be two phases of a stage ahead");
+static_assert(kTeams <= Shape<64>::kVStages && kTeams <= Shape<128>::kVStages && kTeams <= Shape<64>::kKStages && kTeams <= Shape<128>::kKStages,
+              "a converter must not be two phases of a stage ahead");
+static_assert(kSmemBytes<64> <= 227 * 1024 && kSmemBytes<128> <= 227 * 1024, "shared memory per CTA");
 
-// ---- ring order ----------------------------------------------------------------------
-// The ring holds half-tiles (64 keys of K or of V).  Within a piece of n tiles they come in the order the issuers first touch them.  With la = tiles of K
-// issued ahead of the first PV (1 for two M-tiles, 2 for the even/odd split): both halves of K(0..min(la,n)-1), then for every u with u + la < n
-// V(u)a, K(u+la)a, V(u)b, K(u+la)b, then what is left of V.
-struct HalfOrder {
-  int la, la_c, np;  // np = number of (V, K) pairs
-  __device__ __forceinline__ HalfOrder(int n, int mode) : la(mode == 2 ? 1 : 2) {
-    la_c = min(la, n);
-    np = max(0, n - la);
-  }
-  __device__ __forceinline__ int k(int t, int half) const { return t < la ? 2 * t + half : 2 * la_c + 4 * (t - la) + 2 * half + 1; }
-  __device__ __forceinline__ int v(int u, int half) const { return u < np ? 2 * la_c + 4 * u + 2 * half : 2 * la_c + 4 * np + 2 * (u - np) + half; }
-  // place i of the 4n of a piece -> tile, half, and whether it is V's
-  __device__ __forceinline__ int at(int i, int &half, bool &is_v) const {
-    half = i & 1;
-    is_v = false;
-    if (i < 2 * la_c) return i >> 1;
-    i -= 2 * la_c;
-    if (i < 4 * np) {
-      half = (i >> 1) & 1;
-      is_v = !(i & 1);
-      return (i >> 2) + (is_v ? 0 : la);
-    }
-    i -= 4 * np;
-    half = i & 1;
-    is_v = true;
-    return np + (i >> 1);
-  }
-};
-
-// Instruction descriptors: D fp32, A and B f16 (format 0), M = 128; QK: N = 64 keys, both operands K-major; PV: N = head size, B N-major.
+// Instruction descriptors: D fp32, M = 128; QK: A and B e4m3 (format 0 of kind::f8f6f4), N = 64 keys, both operands K-major; PV: A and B f16 (format 0
+// of kind::f16), N = head size, B N-major.
 constexpr uint32_t kIdescBase = (1u << 4) | (8u << 24);
 constexpr uint32_t kIdescQK = kIdescBase | ((64u >> 3) << 17);
 template <int kD>
 constexpr uint32_t kIdescPV = kIdescBase | (((uint32_t)kD >> 3) << 17) | (1u << 16);
+
+__device__ __forceinline__ void mma_f8(uint32_t d_tmem, uint64_t adesc, uint64_t bdesc, uint32_t idesc, uint32_t acc) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
+      "tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], %1, %2, %3, p;\n\t}" ::"r"(d_tmem),
+      "l"(adesc), "l"(bdesc), "r"(idesc), "r"(acc)
+      : "memory");
+}
+// Descriptor of a K-major operand of rows of kD bytes: the swizzle spans a row (128 or 64 bytes), groups of eight rows lie one after another.
+template <int kD>
+__device__ __forceinline__ uint64_t make_row_desc(uint32_t addr) {
+  return (uint64_t)((addr & 0x3FFFFu) >> 4) | ((uint64_t)1 << 16) | ((uint64_t)(8 * kD >> 4) << 32) | (1ull << 46) |
+         ((uint64_t)(kD == 128 ? 2 : 4) << 61);
+}
+// the place of 16-byte unit u of row r in such an operand
+template <int kD>
+__device__ __forceinline__ uint32_t row_unit(int r, int u) {
+  return (uint32_t)(r * kD + ((u ^ (kD == 128 ? r & 7 : (r >> 1) & 3)) << 4));
+}
+
+__device__ __forceinline__ void tma_load_2d(uint32_t dst, const CUtensorMap *map, int32_t x, int32_t y, uint64_t *bar) {
+  asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4}], [%2];" ::"r"(dst), "l"(map),
+               "r"(smem_u32(bar)), "r"(x), "r"(y)
+               : "memory");
+}
 
 // Five roles share an SM's instruction cache (2048 instructions of it are fast), and warps that wait for instructions are what bounds a version of this
 // kernel that has everything in line: what is rare is in functions of its own, for each role (which have registers of different numbers) apart.
@@ -192,6 +191,30 @@ __device__ __forceinline__ uint32_t pack_f16(float lo, float hi) {
   asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
   return r;
 }
+__device__ __forceinline__ float4 ld_shared_f4(uint32_t addr) {
+  float4 v;
+  asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(addr) : "memory");
+  return v;
+}
+__device__ __forceinline__ int2 ld_shared_i2(uint32_t addr) {
+  int2 v;
+  asm volatile("ld.shared.v2.s32 {%0, %1}, [%2];" : "=r"(v.x), "=r"(v.y) : "r"(addr) : "memory");
+  return v;
+}
+__device__ __forceinline__ float2 fmul2(float2 a, float2 b) {
+  float2 d;
+  asm("{\n\t.reg .b64 ra, rb, rd;\n\tmov.b64 ra, {%2, %3};\n\tmov.b64 rb, {%4, %5};\n\tmul.rn.f32x2 rd, ra, rb;\n\tmov.b64 {%0, %1}, rd;\n\t}"
+      : "=f"(d.x), "=f"(d.y)
+      : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+  return d;
+}
+__device__ __forceinline__ uint32_t pack_e4m3(float a, float b, float c, float d) {
+  uint32_t r;
+  asm("{\n\t.reg .b16 lo, hi;\n\tcvt.rn.satfinite.e4m3x2.f32 lo, %2, %1;\n\tcvt.rn.satfinite.e4m3x2.f32 hi, %4, %3;\n\tmov.b32 %0, {lo, hi};\n\t}"
+      : "=r"(r)
+      : "f"(a), "f"(b), "f"(c), "f"(d));
+  return r;
+}
 __device__ __forceinline__ float pow2(int e) { return __uint_as_float((uint32_t)(min(max(e, -126), 127) + 127) << 23); }
 __device__ __forceinline__ void copy_codes(uint32_t dst, const uint8_t *src) {
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
@@ -216,33 +239,32 @@ __device__ __forceinline__ void st_shared(uint32_t addr, uint32_t a, uint32_t b,
   asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(addr), "r"(a), "r"(b), "r"(c), "r"(d) : "memory");
 }
 
-// P = exp2(sc * s + neg) for 64 scores, as halves over the first half of the score buffer; returns their fp32 sum and, worked out in the shadow of the
-// exponentials (which a quarter of an SM does four of a cycle: 512 cycles), the maximum of the scores.
-__device__ __forceinline__ float exp_half(const uint32_t (&v)[64], uint32_t addr, float sc, float neg, float &raw_max) {
-  const float2 s2 = make_float2(sc, sc), n2 = make_float2(neg, neg);
+// P = exp2(t) for 64 exponents, as halves over the first half of the score buffer; returns their fp32 sum and, worked out in the shadow of the
+// exponentials, the largest t.
+__device__ __forceinline__ float exp_half(const uint32_t (&t)[64], uint32_t addr, float &t_max) {
   float2 acc0 = make_float2(0.f, 0.f), acc1 = make_float2(0.f, 0.f);
   float m0 = -INFINITY, m1 = -INFINITY;
   uint32_t pk[32];
 #pragma unroll
   for (int i = 0; i < 64; i += 4) {
-    float2 y0 = ffma2(make_float2(bits_f(v[i]), bits_f(v[i + 1])), s2, n2);
-    float2 y1 = ffma2(make_float2(bits_f(v[i + 2]), bits_f(v[i + 3])), s2, n2);
-    m0 = max3(m0, bits_f(v[i]), bits_f(v[i + 1]));
-    y0.x = ex2(y0.x);
-    y0.y = ex2(y0.y);
-    m1 = max3(m1, bits_f(v[i + 2]), bits_f(v[i + 3]));
-    y1.x = ex2(y1.x);
-    y1.y = ex2(y1.y);
+    float2 y0, y1;
+    m0 = max3(m0, bits_f(t[i]), bits_f(t[i + 1]));
+    y0.x = ex2(bits_f(t[i]));
+    y0.y = ex2(bits_f(t[i + 1]));
+    m1 = max3(m1, bits_f(t[i + 2]), bits_f(t[i + 3]));
+    y1.x = ex2(bits_f(t[i + 2]));
+    y1.y = ex2(bits_f(t[i + 3]));
     acc0 = fadd2(acc0, y0);
     acc1 = fadd2(acc1, y1);
     pk[i >> 1] = pack_f16(y0.x, y0.y);
     pk[(i >> 1) + 1] = pack_f16(y1.x, y1.y);
   }
   tmem_st32(addr, pk);
-  raw_max = fmaxf(m0, m1);
+  t_max = fmaxf(m0, m1);
   acc0 = fadd2(acc0, acc1);
   return acc0.x + acc0.y;
 }
+
 // O *= alpha.  The PV product of the previous half-unit must have retired first; the one before it has (its commit precedes the s_full this thread has just
 // seen), so o_done has completed done_needed or done_needed - 1 phases and the parity says which, whether or not this thread has looked at the
 // earlier ones.
@@ -275,9 +297,10 @@ __device__ __noinline__ bool sees_nan(const uint8_t *nan4, const TcPage *pages, 
   return seen;
 }
 
-// A row of Q, scaled by a power of two to lie below 4, as halves into the channel halves [h0, h1) of its M-tile; returns 2 to the exponent taken out.
+// A row of Q, scaled by a power of two to lie within 448, as its two e4m3 terms (those of [t0, t1) are stored); returns 2 to the exponent taken out, or NaN for
+// a row that is not finite (its scores are no numbers either).
 template <int kD>
-__device__ __noinline__ float convert_q(const uint16_t *__restrict__ q, int64_t q_index, uint32_t tile, int r, int h0, int h1) {
+__device__ __noinline__ float convert_q(const uint16_t *__restrict__ q, int64_t q_index, uint32_t tile, int r, int t0, int t1) {
   uint4 x[kD / 8];
 #pragma unroll
   for (int i = 0; i < kD / 8; ++i) x[i] = q_index >= 0 ? __ldg(reinterpret_cast<const uint4 *>(q + q_index * kD) + i) : make_uint4(0, 0, 0, 0);
@@ -286,18 +309,24 @@ __device__ __noinline__ float convert_q(const uint16_t *__restrict__ q, int64_t 
   for (int i = 0; i < kD / 8; ++i)
     top = __vmaxu2(top, __vmaxu2(__vmaxu2(x[i].x & 0x7FFF7FFFu, x[i].y & 0x7FFF7FFFu), __vmaxu2(x[i].z & 0x7FFF7FFFu, x[i].w & 0x7FFF7FFFu)));
   top = max(top & 0xFFFFu, top >> 16);
-  const int e = top < 0x7F80u ? min(max((int)(top >> 7) - 127, -126), 126) : 0;
+  const int e = min(max((int)(top >> 7) - 135 + ((top & 0x7Fu) > 0x60u ? 1 : 0), -126), 120);  // as lr_fp8_write
   const float by = pow2(-e);
 #pragma unroll
-  for (int i = 0; i < kD / 8; ++i) {
-    if (i / 8 < h0 || i / 8 >= h1) continue;
-    const uint32_t w[4] = {x[i].x, x[i].y, x[i].z, x[i].w};
-    uint32_t o[4];
+  for (int u = 0; u < kD / 16; ++u) {
+    const uint32_t w[8] = {x[2 * u].x, x[2 * u].y, x[2 * u].z, x[2 * u].w, x[2 * u + 1].x, x[2 * u + 1].y, x[2 * u + 1].z, x[2 * u + 1].w};
+    uint32_t hi[4], lo[4];
 #pragma unroll
-    for (int j = 0; j < 4; ++j) o[j] = pack_f16(bits_f(w[j] << 16) * by, bits_f(w[j] & 0xFFFF0000u) * by);
-    st_shared(tile + (i / 8) * kHalfBytes + r * 128 + (((i & 7) ^ (r & 7)) << 4), o[0], o[1], o[2], o[3]);
+    for (int j = 0; j < 4; ++j) {
+      const float a = bits_f(w[2 * j] << 16) * by, b = bits_f(w[2 * j] & 0xFFFF0000u) * by, c = bits_f(w[2 * j + 1] << 16) * by,
+                  d = bits_f(w[2 * j + 1] & 0xFFFF0000u) * by;
+      hi[j] = pack_e4m3(a, b, c, d);
+      const float2 ab = fp8_float2(hi[j] & 0xFFFFu), cd = fp8_float2(hi[j] >> 16);
+      lo[j] = pack_e4m3(a - ab.x, b - ab.y, c - cd.x, d - cd.y);
+    }
+    if (t0 == 0) st_shared(tile + row_unit<kD>(r, u), hi[0], hi[1], hi[2], hi[3]);
+    if (t1 == 2) st_shared(tile + Shape<kD>::kTermBytes + row_unit<kD>(r, u), lo[0], lo[1], lo[2], lo[3]);
   }
-  return pow2(e);
+  return top < 0x7F80u ? pow2(e) : __uint_as_float(0x7FC00000u);
 }
 
 // The store epilogue of a softmax thread: row r of the accumulator at o_addr times `self` (and, when the CTA's two streams worked on the same
@@ -357,8 +386,8 @@ __device__ __noinline__ void store_rows(uint32_t o_addr, uint32_t o_other, int s
   }
 }
 
-struct Fp8Pools {
-  const uint8_t *k, *v, *k_scale, *v_scale;
+struct Fp8Pools {  // K's codes are behind a tensor map
+  const uint8_t *v, *k_scale, *v_scale;
 };
 
 __device__ __forceinline__ uint32_t valid_bytes(int valid, int lane) {  // of the four keys of this lane's word
@@ -370,11 +399,10 @@ __device__ __forceinline__ uint32_t top_byte(uint32_t bytes) {
   const uint32_t w = bytes & ~__vcmpeq4(bytes, 0xFFFFFFFFu), t = __vmaxu4(w, w >> 16);
   return max(t & 0xFFu, (t >> 8) & 0xFFu);
 }
-// 2^(byte - ref) of two keys, as halves; of a row that stands for NaN: of K NaN, of V 0
-__device__ __forceinline__ uint32_t factors(uint32_t b0, uint32_t b1, int ref, int is_v) {
+// 2^(byte - ref) of two keys, as halves; 0 for a row that stands for NaN
+__device__ __forceinline__ uint32_t factors(uint32_t b0, uint32_t b1, int ref) {
   const float f0 = __uint_as_float((uint32_t)max((int)b0 - ref + 127, 0) << 23), f1 = __uint_as_float((uint32_t)max((int)b1 - ref + 127, 0) << 23);
-  const float nan = is_v ? 0.f : __uint_as_float(0x7FC00000u);
-  return pack_f16(b0 == kFp8NanScale ? nan : f0, b1 == kFp8NanScale ? nan : f1);
+  return pack_f16(b0 == kFp8NanScale ? 0.f : f0, b1 == kFp8NanScale ? 0.f : f1);
 }
 // four codes times a key's factor, as four halves
 __device__ __forceinline__ void halves4(uint32_t c, uint32_t by, uint32_t &lo, uint32_t &hi) {
@@ -386,10 +414,11 @@ __device__ __forceinline__ void halves4(uint32_t c, uint32_t by, uint32_t &lo, u
 
 template <int kD>
 __global__ void __launch_bounds__(kThreads, 1)
-attn_fp8_kernel(DevBatch d, DevTcPlan tc, const uint16_t *__restrict__ q, Fp8Pools in, uint16_t *__restrict__ out, float *__restrict__ lse,
+attn_fp8_kernel(const __grid_constant__ CUtensorMap k_map, DevBatch d, DevTcPlan tc, const uint16_t *__restrict__ q, Fp8Pools in, uint16_t *__restrict__ out, float *__restrict__ lse,
                 float scale_log2) {
   using Sh = Shape<kD>;
-  constexpr int kQBytes = Sh::kQBytes, kStageBytes = Sh::kStageBytes, kGroupBytes = Sh::kGroupBytes, kStages = Sh::kStages, kHalves = Sh::kHalves;
+  constexpr int kQBytes = Sh::kQBytes, kTermBytes = Sh::kTermBytes, kCodeBytes = Sh::kCodeBytes, kVBytes = Sh::kVBytes, kGroupBytes = Sh::kGroupBytes;
+  constexpr int kKStages = Sh::kKStages, kVStages = Sh::kVStages;
   if ((smem_u32(smem) & 1023u) != 0u) {  // the swizzled tiles need a 1024-byte aligned base
     if (threadIdx.x == 0) {
       d.status[0] = kDevBounds;
@@ -397,21 +426,28 @@ attn_fp8_kernel(DevBatch d, DevTcPlan tc, const uint16_t *__restrict__ q, Fp8Poo
     }
     return;
   }
-  unsigned char *q_smem = smem;                  // two M-tiles
-  unsigned char *kv_smem = smem + 2 * kQBytes;   // kStages half-tiles
-  unsigned char *code_smem = kv_smem + kStages * kStageBytes;  // a half-tile of codes for each converter
+  unsigned char *q_smem = smem;                // two M-tiles
+  unsigned char *k_smem = q_smem + 2 * kQBytes;  // kKStages half-tiles of codes
+  unsigned char *v_smem = k_smem + kKStages * kCodeBytes;  // kVStages half-tiles of halves
+  unsigned char *code_smem = v_smem + kVStages * kVBytes;  // a half-tile of V's codes for each converter
   Ctrl *ctrl = ctrl_at<kD>();
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
 
   // the plan is uploaded by copies, so it may be read in front of the wait for the kernel before
   const TcCtaHead *head = tc.heads + blockIdx.x;
   const int piece0 = head->piece0, piece1 = head->piece1;
-  if (warp == 8 && lane < (int)(sizeof(TcCtaHead) / 16))
-    reinterpret_cast<uint4 *>(&ctrl->head)[lane] = __ldg(reinterpret_cast<const uint4 *>(head) + lane);
+  if (warp == 8) {
+    if (lane < (int)(sizeof(TcCtaHead) / 16)) reinterpret_cast<uint4 *>(&ctrl->head)[lane] = __ldg(reinterpret_cast<const uint4 *>(head) + lane);
+    if (elect_one()) asm volatile("prefetch.tensormap [%0];" ::"l"(&k_map) : "memory");
+  }
   if (threadIdx.x == 0) {
-    for (int s = 0; s < kStages; ++s) {
-      mbar_init(&ctrl->kv_full[s], 1);
-      mbar_init(&ctrl->kv_empty[s], 2);  // one arrival per MMA issuer
+    for (int s = 0; s < kKStages; ++s) {
+      mbar_init(&ctrl->k_full[s], 1);
+      mbar_init(&ctrl->k_empty[s], 2);  // one arrival per MMA issuer
+    }
+    for (int s = 0; s < kVStages; ++s) {
+      mbar_init(&ctrl->v_full[s], 1);
+      mbar_init(&ctrl->v_empty[s], 2);
     }
     mbar_init(&ctrl->q_full, 256);
     mbar_init(&ctrl->q_empty, 2);
@@ -446,7 +482,7 @@ attn_fp8_kernel(DevBatch d, DevTcPlan tc, const uint16_t *__restrict__ q, Fp8Poo
   const int T = tc.tokens_per_mtile;
 
   if (warp >= 8) {
-    asm volatile("setmaxnreg.dec.sync.aligned.u32 80;");
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 88;");
     const TcCtaHead *head = &ctrl->head;
     // the page a table names, or page 0 in its place: never fetch outside the pool
     auto page_in_pool = [&](int32_t page) -> int32_t {
@@ -460,42 +496,48 @@ attn_fp8_kernel(DevBatch d, DevTcPlan tc, const uint16_t *__restrict__ q, Fp8Poo
       // Both issuers walk every position of both rings in order: a half-tile this stream uses is consumed by its MMAs (released by a
       // tcgen05.commit), one it does not use is released with a plain arrive once it has landed.
       const int s = __shfl_sync(0xFFFFFFFFu, warp, 0) - 13;
-      uint32_t base = 0, seen = 0, p_cnt = 0, pc_idx = 0;  // base: ring positions of the pieces before
+      uint32_t base = 0, k_seen = 0, v_seen = 0, p_cnt = 0, pc_idx = 0;  // base: half-tiles of the pieces before
       bool ok = true;
       const uint32_t tmem_u = __shfl_sync(0xFFFFFFFFu, tmem, 0);
       const uint32_t s_tmem = tmem_u + s * 128, o_tmem = tmem_u + 256 + s * 128;
       // Descriptors differ from a base only in the start-address field (units of 16 bytes).
-      const uint64_t qdesc0 = make_desc(smem_u32(q_smem), 16, 1024), kdesc0 = make_desc(smem_u32(kv_smem), 16, kGroupBytes),
-                     vdesc0 = make_desc(smem_u32(kv_smem), kAtomBytes, kGroupBytes);
-      auto issue_qk = [&](int m, uint32_t stage, int half) {  // S_s[half] = Q_m K^T over 64 keys
-        const uint64_t a = qdesc0 + (uint64_t)(m * (kQBytes >> 4)), b = kdesc0 + (uint64_t)(stage * (kStageBytes >> 4));
+      const uint64_t qdesc0 = make_row_desc<kD>(smem_u32(q_smem)), kdesc0 = make_row_desc<kD>(smem_u32(k_smem)),
+                     vdesc0 = make_desc(smem_u32(v_smem), kAtomBytes, kGroupBytes);
+      auto issue_qk = [&](int m, uint32_t stage, int half) {  // S_s[half] = (hi + lo) of Q_m times K^T over 64 keys
+        const uint64_t a = qdesc0 + (uint64_t)(m * (kQBytes >> 4)), b = kdesc0 + (uint64_t)(stage * (kCodeBytes >> 4));
+#pragma unroll 1
+        for (int term = 0; term < 2; ++term)
 #pragma unroll
-        for (int h = 0; h < kHalves; ++h)
-#pragma unroll
-          for (int kk = 0; kk < 4; ++kk)
-            mma_ss(s_tmem + half * 64, a + (uint64_t)(h * (kHalfBytes >> 4) + kk * 2), b + (uint64_t)(h * (kAtomBytes >> 4) + kk * 2),
-                   kIdescQK, (h | kk) != 0);
+          for (int kk = 0; kk < kD / 32; ++kk)
+            mma_f8(s_tmem + half * 64, a + (uint64_t)(term * (kTermBytes >> 4) + kk * 2), b + (uint64_t)(kk * 2), kIdescQK, (term | kk) != 0);
       };
       auto issue_pv = [&](uint32_t stage, int half, bool acc) {  // O_s (+)= P_s[half] V over 64 keys
-        const uint64_t b = vdesc0 + (uint64_t)(stage * (kStageBytes >> 4));
+        const uint64_t b = vdesc0 + (uint64_t)(stage * (kVBytes >> 4));
 #pragma unroll
         for (int k4 = 0; k4 < 4; ++k4)
           mma_ts(o_tmem, s_tmem + half * 64 + k4 * 8, b + (uint64_t)(k4 * (2 * kGroupBytes >> 4)), kIdescPV<kD>, acc || k4 != 0);
       };
       // waits, in ring order, until position `pos` has landed; positions on the way belong to the other stream and are released here
-      auto need = [&](uint32_t pos) -> bool {
-        for (; seen <= pos; ++seen) {
-          if (!wait<kD, 1>(&ctrl->kv_full[seen % kStages], (seen / kStages) & 1u, 271)) return false;
-          if (seen < pos && elect_one()) mbar_arrive(&ctrl->kv_empty[seen % kStages]);
+      auto need_k = [&](uint32_t pos) -> bool {
+        for (; k_seen <= pos; ++k_seen) {
+          if (!wait<kD, 1>(&ctrl->k_full[k_seen % kKStages], (k_seen / kKStages) & 1u, 271)) return false;
+          if (k_seen < pos && elect_one()) mbar_arrive(&ctrl->k_empty[k_seen % kKStages]);
+        }
+        return true;
+      };
+      auto need_v = [&](uint32_t pos) -> bool {
+        for (; v_seen <= pos; ++v_seen) {
+          if (!wait<kD, 1>(&ctrl->v_full[v_seen % kVStages], (v_seen / kVStages) & 1u, 272)) return false;
+          if (v_seen < pos && elect_one()) mbar_arrive(&ctrl->v_empty[v_seen % kVStages]);
         }
         return true;
       };
       for (int pc = piece0; pc < piece1 && ok; ++pc, ++pc_idx) {
         const TcPiece *pi = pc == piece0 ? &head->first : tc.pieces + pc;
         const int n = pi->tile_end - pi->tile_begin, mode = pi->n_mt;
-        const int my_units = mode == 2 ? n : (n - s + 1) / 2;
-        const HalfOrder ord(n, mode);
+        const int my_units = mode == 2 ? n : (n - s + 1) / 2, step = mode == 2 ? 2 : 4;  // half-tiles from a tile of this stream to its next
         const int m_tile = mode == 2 ? s : 0;
+        const uint32_t pos = base + (mode == 2 ? 0u : 2u * s);  // of the stream's first tile
         ok = wait<kD, 1>(&ctrl->q_full, pc_idx & 1u, 270);
         if (!ok) break;
         if (my_units == 0) {
@@ -515,22 +557,21 @@ attn_fp8_kernel(DevBatch d, DevTcPlan tc, const uint16_t *__restrict__ q, Fp8Poo
           for (int half = 0; half < 2; ++half) {
             opaque(j);
             const bool has_pv = j >= 0, has_qk = j + 1 < my_units;
-            const int t = mode == 2 ? j : 2 * j + s;
-            const uint32_t pos_v = base + ord.v(t, half), pos_k = base + ord.k(t + (mode == 2 ? 1 : 2), half);
-            ok = (!has_pv || need(pos_v)) && (!has_qk || need(pos_k));
+            const uint32_t pos_v = pos + j * step + half, pos_k = pos_v + step;
+            ok = (!has_pv || need_v(pos_v)) && (!has_qk || need_k(pos_k));
             if (ok && has_pv) ok = wait<kD, 1>(&ctrl->p_full[s][half], p_cnt & 1u, 274 + s);  // P of this half is in place
             if (!ok) break;
             tc_fence_after();
             if (elect_one()) {
               if (has_pv) {
-                issue_pv(pos_v % kStages, half, (j | half) != 0);
+                issue_pv(pos_v % kVStages, half, (j | half) != 0);
                 tc_commit(&ctrl->o_done[s]);
-                tc_commit(&ctrl->kv_empty[pos_v % kStages]);
+                tc_commit(&ctrl->v_empty[pos_v % kVStages]);
               }
               if (has_qk) {
-                issue_qk(m_tile, pos_k % kStages, half);
+                issue_qk(m_tile, pos_k % kKStages, half);
                 tc_commit(&ctrl->s_full[s][half]);
-                tc_commit(&ctrl->kv_empty[pos_k % kStages]);
+                tc_commit(&ctrl->k_empty[pos_k % kKStages]);
                 if (half == 1 && j + 2 == my_units) tc_commit(&ctrl->q_empty);  // last QK of the piece: this stream is done with the Q buffers
               }
             }
@@ -539,11 +580,17 @@ attn_fp8_kernel(DevBatch d, DevTcPlan tc, const uint16_t *__restrict__ q, Fp8Poo
           if (j >= 0) ++p_cnt;
         }
         if (!ok) break;
-        base += 4u * (uint32_t)n;
-        if (seen < base) {  // positions of the piece behind the last of this stream
-          ok = need(base - 1);
+        // half-tiles of the piece behind the last of this stream
+        base += 2u * (uint32_t)n;
+        if (k_seen < base) {
+          ok = need_k(base - 1);
           if (!ok) break;
-          if (elect_one()) mbar_arrive(&ctrl->kv_empty[(base - 1) % kStages]);
+          if (elect_one()) mbar_arrive(&ctrl->k_empty[(base - 1) % kKStages]);
+        }
+        if (v_seen < base) {
+          ok = need_v(base - 1);
+          if (!ok) break;
+          if (elect_one()) mbar_arrive(&ctrl->v_empty[(base - 1) % kVStages]);
         }
       }
       if (!ok && elect_one()) {
@@ -554,10 +601,10 @@ attn_fp8_kernel(DevBatch d, DevTcPlan tc, const uint16_t *__restrict__ q, Fp8Poo
           if (global_ns() - t0 > kDrainLimitNs) break;
       }
       __syncwarp();
-    } else {
+    } else if (warp < 12) {
       // ======================= converters ====================================================
       constexpr int kCols = Sh::kCols, kGroups = Sh::kGroups, kRounds = Sh::kRounds;
-      const int team = warp < 13 ? warp - 8 : 5;
+      const int team = warp - 8;
       const int col = lane % kCols, grp = lane / kCols;  // 16 channels of keys (round * kGroups + grp) * 4 .. + 3
       // Eight neighbouring lanes store to two lines at a time whose 16-byte units lie in the same banks (both channel halves of a key, or with head size 64
       // keys four apart); half of them take their four keys in the order 1, 0, 3, 2, which brings the units of the two lines apart.
@@ -566,90 +613,74 @@ attn_fp8_kernel(DevBatch d, DevTcPlan tc, const uint16_t *__restrict__ q, Fp8Poo
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
         const int r = (grp & 1) * 4 + (j ^ odd);
-        off[j] = smem_u32(kv_smem) + (kD == 128 ? (col >> 2) * kAtomBytes : 0) + (grp >> 1) * kGroupBytes + r * 128 + ((((col & 3) * 2) ^ r) << 4);
+        off[j] = smem_u32(v_smem) + (kD == 128 ? (col >> 2) * kAtomBytes : 0) + (grp >> 1) * kGroupBytes + r * 128 + ((((col & 3) * 2) ^ r) << 4);
       }
       const int32_t k_off = (grp & 3) * 4 * kD + col * 16;  // within the page of the keys
       // A lane alone copies and reads its part of the warp's codes, so that nothing but its own copies has to be waited for; a part
       // is asked for again as soon as it has been read, a whole half-tile's work ahead.
-      const uint32_t mine = smem_u32(code_smem) + team * Sh::kCodeBytes + lane * 16;
+      const uint32_t mine = smem_u32(code_smem) + team * kCodeBytes + lane * 16;
 
-      // the ring positions of this warp: every kTeams-th of the CTA's
-      int pc = piece0 - 1, x = team, n4 = 0, n_dense = 0, kv_head = 0, mode = 0, tiles = 0;  // x: the one asked for next, its number within piece pc
+      // the half-tiles of this warp: every kTeams-th of the CTA's
+      int pc = piece0 - 1, x = team, n_half = 0, n_whole = 0, kv_head = 0;  // x: the one asked for next, its number within piece pc
       const TcPage *pages = nullptr;
-      auto fetch = [&](int32_t row, int is_v, int u) {  // part u of the codes of the pages with those rows
+      auto fetch = [&](int32_t row, int u) {  // part u of the codes of the pages with those rows
         // (a lane whose row is that of the page of this lane's keys; an absent page of the last tile reads page 0 and is cleared below)
-        const uint8_t *at = (is_v ? in.v : in.k) + k_off + (int64_t)__shfl_sync(0xFFFFFFFFu, row, ((u * kGroups + grp) >> 2) * 4) * kD;
+        const uint8_t *at = in.v + k_off + (int64_t)__shfl_sync(0xFFFFFFFFu, row, ((u * kGroups + grp) >> 2) * 4) * kD;
         const uint8_t *even = at + odd * kD, *other = at - odd * kD;
         copy_codes(mine + u * 2048, even);
         copy_codes(mine + u * 2048 + 512, other + kD);
         copy_codes(mine + u * 2048 + 1024, even + 2 * kD);
         copy_codes(mine + u * 2048 + 1536, other + 3 * kD);
       };
-      // Loads into registers are looked at a half-tile later: the page entries of one, the scale bytes of the one before it, whose codes are asked for, and the
-      // one before that, which is converted.  Of each: the number of the half-tile among the CTA's (-1: there is none), whether it is V's, and
-      // whether it has slots without a valid token.
+      // Loads into registers are looked at a half-tile later: the page entries of one, the scale bytes of the one before it, whose codes of K and V are asked
+      // for, and the one before that, whose V is converted.
       int2 e = make_int2(0, 0);
-      int e_at = -1, e_v = 0, e_clear = 0, e_head = 0;
-      int w_at = -1, w_v = 0, w_clear = 0;
-      uint32_t word = 0, meta = 0;  // scale bytes of keys 4 lane .. 4 lane + 3; beside those of K, lanes 16-31 have V's of the same keys
+      int e_head = -1;                // KV head of the half-tile whose page entries are on their way, -1: there is none
+      uint32_t k_word = 0, word = 0, meta = 0;  // scale bytes of keys 4 lane .. 4 lane + 3 (lanes 16-31: again) and valid tokens of their page, of the one before
+      bool e_clear = false, word_clear = false;  // whether it has slots without a valid token
+      bool words = false, ok = true;
+      uint32_t asked = (uint32_t)team;  // ring position of K asked for next
 #pragma unroll 1
       for (uint32_t ring = (uint32_t)team;;) {
-        const int at = w_at, is_v = w_v, clear = w_v & w_clear;  // (K's scores of slots that hold no valid token are never looked at)
+        const bool there = words, clear = word_clear;
         const uint32_t live = valid_bytes((int)(meta & 31u), lane), bytes = word & live;
+        words = e_head >= 0;
         int32_t row = 0;
-        w_at = e_at;
-        w_v = e_v;
-        w_clear = e_clear;
-        if (w_at >= 0) {
+        if (words) {
           row = (page_in_pool(e.x) * d.n_kv_heads + e_head) * kPage;  // rows of the pools are numbered within 32 bits (tc_plan_structure)
           meta = (uint32_t)e.y;
-          word = ld_word((w_v || lane >= 16 ? in.v_scale : in.k_scale) + row + (lane & 3) * 4);
+          word = ld_word(in.v_scale + row + (lane & 3) * 4);
+          k_word = ld_word(in.k_scale + row + (lane & 3) * 4);
+          word_clear = e_clear;
         }
-        while (pc < piece1 && x >= n4) {
-          x -= n4;
-          tiles += n4 >> 2;
+        while (pc < piece1 && x >= n_half) {
+          x -= n_half;
           if (++pc >= piece1) break;
           const TcPiece *pi = pc == piece0 ? &head->first : tc.pieces + pc;
           const TcReq *rq = pc == piece0 ? &head->first_req : tc.reqs + pi->req;
-          n4 = 4 * (pi->tile_end - pi->tile_begin);
-          n_dense = rq->n_dense_tiles - pi->tile_begin;
+          n_half = 2 * (pi->tile_end - pi->tile_begin);
+          n_whole = 2 * (rq->n_dense_tiles - pi->tile_begin);  // half-tiles without slots of no valid token
           kv_head = pi->kv_head;
-          mode = pi->n_mt;
           pages = tc.pages + rq->page_off + pi->tile_begin * kPagesPerTile + ((lane >> 2) & 3);
         }
-        e_at = -1;
+        e_head = -1;
         if (pc < piece1) {
-          int half;
-          bool v;
-          const int t = HalfOrder(n4 >> 2, mode).at(x, half, v);
-          e = ld_pair(pages + t * kPagesPerTile + half * (kPagesPerTile / 2));
-          e_at = (tiles + t) * 2 + half;
-          e_v = v;
-          e_clear = t >= n_dense;
+          e = ld_pair(pages + x * (kPagesPerTile / 2));
           e_head = kv_head;
+          e_clear = x >= n_whole;
           x += kTeams;
         }
-        const uint32_t stage = ring % kStages, to = stage * kStageBytes;
+        const uint32_t stage = ring % kVStages, to = stage * kVBytes;
         uint32_t f01 = 0, f23 = 0;
-        if (at >= 0) {
-          const uint32_t top = top_byte(bytes), ref = max(__reduce_max_sync(0xFFFFFFFFu, lane < 16 ? top : 0u), 1u);
+        if (there) {
+          const int ref = (int)max(__reduce_max_sync(0xFFFFFFFFu, top_byte(bytes)), 1u);
           // the factors of this lane's four keys, which other lanes ask for
-          f01 = factors(bytes & 0xFFu, (bytes >> 8) & 0xFFu, (int)ref, is_v);
-          f23 = factors((bytes >> 16) & 0xFFu, bytes >> 24, (int)ref, is_v);
-          if (!wait<kD, 1>(&ctrl->kv_empty[stage], ((ring / kStages) & 1u) ^ 1u, 210)) break;
-          if (!is_v) {  // what the softmax has to know of this half-tile, V's scales among it
-            const uint32_t v_ref = max(__reduce_max_sync(0xFFFFFFFFu, lane >= 16 ? top : 0u), 1u), slot = (uint32_t)at % kInfos;
-            const uint32_t nan = lane >= 16 ? __vcmpeq4(bytes, 0xFFFFFFFFu) : 0u;
-            const bool any = __any_sync(0xFFFFFFFFu, nan != 0u);
-            if (any && lane >= 16) ctrl->nan4[slot][lane - 16] = (uint8_t)((nan & 1u) | ((nan >> 7) & 2u) | ((nan >> 14) & 4u) | ((nan >> 21) & 8u));
-            __syncwarp();
-            if (lane == 0) {
-              ctrl->info[slot] = Info{__uint_as_float(ref << 23), (int)v_ref, any ? 1 : 0};
-              mbar_arrive(&ctrl->info_full[slot]);
-            }
-          }
+          f01 = factors(bytes & 0xFFu, (bytes >> 8) & 0xFFu, ref);
+          f23 = factors((bytes >> 16) & 0xFFu, bytes >> 24, ref);
+          ok = wait<kD, 1>(&ctrl->v_empty[stage], ((ring / kVStages) & 1u) ^ 1u, 212);
+          if (!ok) break;
         }
-        int conv = at >= 0, ask = w_at >= 0, wipe = clear;
+        int conv = there ? 1 : 0, ask = words ? 1 : 0, wipe = clear ? 1 : 0;
 #pragma unroll 1
         for (int u = 0; u < kRounds; ++u) {
           opaque(conv);
@@ -667,7 +698,7 @@ attn_fp8_kernel(DevBatch d, DevTcPlan tc, const uint16_t *__restrict__ q, Fp8Poo
               for (int j = 0; j < 4; ++j)
                 if (((l4 >> (8 * (j ^ odd))) & 1u) == 0u) c[j] = make_uint4(0, 0, 0, 0);
             }
-            const uint32_t into = to + u * (kGroups / 2) * kGroupBytes;
+            const uint32_t at = to + u * (kGroups / 2) * kGroupBytes;
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
               const uint32_t f = __byte_perm(by[j >> 1], 0u, ((j & 1) != 0) != (odd != 0) ? 0x3232 : 0x1010);
@@ -676,26 +707,64 @@ attn_fp8_kernel(DevBatch d, DevTcPlan tc, const uint16_t *__restrict__ q, Fp8Poo
               halves4(c[j].y, f, h[2], h[3]);
               halves4(c[j].z, f, h[4], h[5]);
               halves4(c[j].w, f, h[6], h[7]);
-              st_shared(off[j] + into, h[0], h[1], h[2], h[3]);
-              st_shared((off[j] + into) ^ 16u, h[4], h[5], h[6], h[7]);
+              st_shared(off[j] + at, h[0], h[1], h[2], h[3]);
+              st_shared((off[j] + at) ^ 16u, h[4], h[5], h[6], h[7]);
             }
           }
-          if (ask) fetch(row, w_v, u);
+          if (ask) fetch(row, u);
           asm volatile("cp.async.commit_group;" ::: "memory");
         }
-        if (at >= 0) {
+        if (there) {
           fence_proxy_async();
           __syncwarp();
-          // (the test hook of lr_plan_debug_set_phantom_bytes: a stage that is never full)
-          if (lane == 0 && !(tc.phantom_tx_bytes != 0u && blockIdx.x == 0 && ring == 0)) mbar_arrive(&ctrl->kv_full[stage]);
+          if (lane == 0) mbar_arrive(&ctrl->v_full[stage]);
           ring += kTeams;
         }
-        if (w_at < 0 && e_at < 0) break;
+        if (words) {
+          // K of the next half-tile, and what the softmax has to know of its keys, V's scales among it
+          const uint32_t k_stage = asked % kKStages;
+          ok = wait<kD, 1>(&ctrl->k_empty[k_stage], ((asked / kKStages) & 1u) ^ 1u, 210);
+          if (!ok) break;
+          if (lane == 0)
+            mbar_arrive_expect_tx(&ctrl->k_full[k_stage], (uint32_t)kCodeBytes + ((blockIdx.x == 0 && asked == 0) ? tc.phantom_tx_bytes : 0u));
+          __syncwarp();
+          // one box per page, absent pages of the last tile included (page 0 in their place: nobody looks at these scores)
+          if (lane < 16 && (lane & 3) == 0)
+            tma_load_2d(smem_u32(k_smem) + k_stage * kCodeBytes + (lane >> 2) * (kPage * kD), &k_map, 0, row, &ctrl->k_full[k_stage]);
+          Info &info = ctrl->info[asked % kInfos];
+          const uint32_t now = valid_bytes((int)(meta & 31u), lane), kb = k_word & now, vb = word & now, nan = __vcmpeq4(vb, 0xFFFFFFFFu);
+          const uint32_t v_ref = max(__reduce_max_sync(0xFFFFFFFFu, top_byte(vb)), 1u);
+          const bool any = __any_sync(0xFFFFFFFFu, nan != 0u);
+          if (lane < 16) {  // (a byte of a slot without a valid token is 0 here: its scores are not looked at)
+            float4 f;
+            f.x = __uint_as_float((kb & 0xFFu) << 23);
+            f.y = __uint_as_float((kb << 15) & 0x7F800000u);
+            f.z = __uint_as_float((kb << 7) & 0x7F800000u);
+            f.w = __uint_as_float((kb >> 1) & 0x7F800000u);
+            reinterpret_cast<float4 *>(info.k_scale)[lane] = f;
+            if (any) info.nan4[lane] = (uint8_t)((nan & 1u) | ((nan >> 7) & 2u) | ((nan >> 14) & 4u) | ((nan >> 21) & 8u));
+          }
+          if (lane == 0) *reinterpret_cast<int2 *>(&info.v_ref) = make_int2((int)v_ref, any ? 1 : 0);
+          __syncwarp();
+          if (lane == 0) mbar_arrive(&ctrl->info_full[asked % kInfos]);
+          asked += kTeams;
+        }
+        if (!words && e_head < 0) break;
+      }
+      if (!ok) {
+        // give the copies of K already in flight a bounded time to land before the CTA exits
+        for (int back = 0; back < kKStages; ++back) {
+          if (asked < (uint32_t)kTeams + (uint32_t)team) break;
+          asked -= kTeams;
+          const uint64_t t0 = global_ns();
+          while (!mbar_try_wait(&ctrl->k_full[asked % kKStages], (asked / kKStages) & 1u))
+            if (global_ns() - t0 > kDrainLimitNs) break;
+        }
       }
       asm volatile("cp.async.wait_group 0;" ::: "memory");  // (after an abort some are still on their way)
     }
   } else {
-    asm volatile("setmaxnreg.inc.sync.aligned.u32 176;");
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 168;");
     // ======================= softmax warpgroups ======================================
     const int s = warp >> 2;        // stream
     const int quarter = warp & 3;   // tensor-memory lane quarter this warp may access
@@ -717,9 +786,7 @@ attn_fp8_kernel(DevBatch d, DevTcPlan tc, const uint16_t *__restrict__ q, Fp8Poo
         // the queries, once the products of the piece before no longer read the buffers; with one M-tile each stream stores its part
         ok = wait<kD, 0>(&ctrl->q_empty, ((uint32_t)(pc - piece0) & 1u) ^ 1u, 245);
         if (ok) {
-          // (with head size 64 and one M-tile stream 0 stores all of it)
-          const int h0 = mode == 2 ? 0 : kHalves == 2 ? s : 0, h1 = mode == 2 ? kHalves : kHalves == 2 ? s + 1 : 1 - s;
-          sc_row = scale_log2 * convert_q<kD>(q, ri.q_index, smem_u32(q_smem) + (mode == 2 ? s : 0) * kQBytes, r, h0, h1);
+          sc_row = scale_log2 * convert_q<kD>(q, ri.q_index, smem_u32(q_smem) + (mode == 2 ? s : 0) * kQBytes, r, mode == 2 ? 0 : s, mode == 2 ? 2 : s + 1);
           fence_proxy_async();
           mbar_arrive(&ctrl->q_full);
         }
@@ -748,64 +815,91 @@ attn_fp8_kernel(DevBatch d, DevTcPlan tc, const uint16_t *__restrict__ q, Fp8Poo
             opaque(half);
             const uint32_t sh_addr = s_addr + half * 64;
             const uint32_t at = (tiles + (uint32_t)local) * 2u + half;  // half-tiles of both streams before this one
-            const Info &info = ctrl->info[at % kInfos];
+            const uint32_t info = smem_u32(&ctrl->info[at % kInfos]);
             const uint32_t g = o_cnt + (uint32_t)(2 * j + half);  // half-units of this stream before this one
+            const bool first = (j | half) == 0;
             if (!s_ready) {
-              ok = wait<kD, 0>(&ctrl->info_full[at % kInfos], (at / kInfos) & 1u, 248) && wait<kD, 0>(&ctrl->s_full[s][half], s_cnt & 1u, 230 + s);
+              // (in this order: a warp need not have looked at what the slot of `info` held before, and its parity says something only once the
+              // phase before is over, as it is when the scores are there)
+              ok = wait<kD, 0>(&ctrl->s_full[s][half], s_cnt & 1u, 230 + s) && wait<kD, 0>(&ctrl->info_full[at % kInfos], (at / kInfos) & 1u, 248);
               if (!ok) break;
             }
             tc_fence_after();
-            const int v_ref = info.v_ref;
-            const float sc = sc_row * info.k_scale;
-            const bool first = (j | half) == 0;
-            float alpha = 1.0f;  // what O has to be multiplied by before this half's product
-            if (first) base = v_ref;
-            if (v_ref > base + kRise) {
-              alpha = pow2(base - v_ref);
-              base = v_ref;
-            }
-            const int off = v_ref - base;
             uint32_t v[64];
             tmem_ld64(sh_addr, v);
+            const int2 of_v = ld_shared_i2(info + 256);  // largest scale byte, whether some row stands for NaN
+            float alpha = 1.0f;  // what O has to be multiplied by before this half's product
+            bool moved = false;  // ... in some row of the warp
+            if (first) base = of_v.x + 1;
+            if (of_v.x > base + kRise) {
+              alpha = pow2(base - (of_v.x + 1));
+              base = of_v.x + 1;
+              moved = true;
+            }
+            const int off = of_v.x - base;
+            bool apart = off < -kApart;  // values far below the accumulator's unit: the sum first, of weights as they are
+            float bias = apart ? 0.f : (float)off + kHead, neg = m_used == -INFINITY ? 0.f : bias - m_used;
             tc_wait_ld();
             // the scores after these (and what is known of their keys) are looked for under the exponentials: a test costs over 100 cycles even
             // when it succeeds
             const uint32_t next = at + (half == 0 || mode == 2 ? 1u : 3u);
             const uint32_t next_ready = mbar_test_wait2(&ctrl->s_full[s][half ^ 1], (s_cnt + (uint32_t)half) & 1u, &ctrl->info_full[next % kInfos], (next / kInfos) & 1u) == 3u;
+#pragma unroll
+            for (int i = 0; i < 64; i += 4) {  // the exponents, in log2: score * (key's scale * row's factor) + neg
+              const float4 ks = ld_shared_f4(info + i * 4);
+              const float2 row = make_float2(sc_row, sc_row), n2 = make_float2(neg, neg);
+              const float2 t0 = ffma2(make_float2(bits_f(v[i]), bits_f(v[i + 1])), fmul2(make_float2(ks.x, ks.y), row), n2);
+              const float2 t1 = ffma2(make_float2(bits_f(v[i + 2]), bits_f(v[i + 3])), fmul2(make_float2(ks.z, ks.w), row), n2);
+              v[i] = __float_as_uint(t0.x);
+              v[i + 1] = __float_as_uint(t0.y);
+              v[i + 2] = __float_as_uint(t1.x);
+              v[i + 3] = __float_as_uint(t1.y);
+            }
             if (pages != nullptr) {
               int n_ok[kPagesPerTile / 2];
 #pragma unroll
               for (int p = 0; p < kPagesPerTile / 2; ++p) n_ok[p] = page_n_ok(__ldg(&pages[half * 4 + p].meta), ri);
               mask_half(v, n_ok);
             }
-            // Exponentials against the running reference exponent.  Where the maximum is beyond what a half holds (and on a row's first keys) they are done
-            // again with the reference moved to it; values far below the accumulator's unit have their weights summed apart, as they are.
-            bool apart = off < -kApart;
             for (;;) {
-              float raw;
-              const float sum = exp_half(v, sh_addr, sc, m_used == -INFINITY ? 0.f : (apart ? 0.f : (float)off + kHead) - m_used, raw), mx = raw * sc;
-              // (a row that has seen nothing: by any score)
-              const bool grow = mx > m_used + kGrow;
-              if (!apart && !__any_sync(0xFFFFFFFFu, grow)) {
+              float t_max;
+              const float sum = exp_half(v, sh_addr, t_max);
+              // beyond what a half holds, or a row's first keys: again, with the reference moved
+              const bool grow = t_max > kGrow + bias || (m_used == -INFINITY && t_max > -INFINITY);
+              const bool grows = __any_sync(0xFFFFFFFFu, grow);
+              if (!grows && !apart) {
                 if (off >= -kApart) l = fmaf(sum, pow2(-off - (int)kHead), l);
                 break;
               }
-              if (__any_sync(0xFFFFFFFFu, grow)) {
+              float shift = 0.f;
+              if (grows) {
                 if (grow) {
+                  const float to = t_max - neg + kLift;
                   if (m_used > -INFINITY) {
-                    const float down = ex2(m_used - (mx + kLift));
+                    const float down = ex2(m_used - to);
                     alpha *= down;
                     l *= down;
                   }
-                  m_used = mx + kLift;
+                  m_used = to;
+                  shift = bias - to - neg;
                 }
+                moved = !first;
               } else {
                 l += sum;
                 apart = false;
+                shift = (float)off + kHead;
+                bias = shift;
+              }
+              neg += shift;
+#pragma unroll
+              for (int i = 0; i < 64; i += 2) {
+                const float2 t = fadd2(make_float2(bits_f(v[i]), bits_f(v[i + 1])), make_float2(shift, shift));
+                v[i] = __float_as_uint(t.x);
+                v[i + 1] = __float_as_uint(t.y);
               }
               tc_wait_st();
             }
-            if (!first && __any_sync(0xFFFFFFFFu, alpha != 1.0f)) {
+            if (moved) {
               ok = rescale_rows<kD>(o_addr, alpha, &ctrl->o_done[s], g, 235 + s);
               if (!ok) break;
             }
@@ -819,7 +913,7 @@ attn_fp8_kernel(DevBatch d, DevTcPlan tc, const uint16_t *__restrict__ q, Fp8Poo
               if (!ok) break;
             }
             // (before the arrival: what it looks at may be replaced behind it)
-            if (info.v_nan) nan_v = sees_nan(ctrl->nan4[at % kInfos], pages == nullptr ? nullptr : pages + half * 4, ri) || nan_v;
+            if (of_v.y) nan_v = sees_nan(ctrl->info[at % kInfos].nan4, pages == nullptr ? nullptr : pages + half * 4, ri) || nan_v;
             mbar_arrive(&ctrl->p_full[s][half]);
           }
           ++s_cnt;
@@ -890,11 +984,41 @@ attn_fp8_merge_kernel(DevBatch d, DevTcPlan tc, uint16_t *__restrict__ out, floa
   merge_cta<kD, kBatch>(d, tc, blockIdx.x, blockIdx.y, out, lse);
 }
 
+typedef CUresult (*EncodeTiledFn)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *, const cuuint64_t *,
+                                  const cuuint32_t *, const cuuint32_t *, CUtensorMapInterleave, CUtensorMapSwizzle,
+                                  CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+
+// K's codes as rows of head_dim bytes; a box is one page of one KV head, 16 rows.  Made for every call: it takes a fraction of a microsecond.
+int encode_k(lr_ctx *ctx, const void *codes, int64_t n_pages, CUtensorMap *map) {
+  if (!ctx->tmap_encode) {
+    void *fn = nullptr;
+    cudaDriverEntryPointQueryResult qres;
+    cudaError_t e = cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &fn, cudaEnableDefault, &qres);
+    if (e != cudaSuccess || qres != cudaDriverEntryPointSuccess || !fn) {
+      set_error("cuTensorMapEncodeTiled is not available from the driver");
+      return LR_ECUDA;
+    }
+    ctx->tmap_encode = fn;
+  }
+  const lr_model &m = ctx->model;
+  const cuuint64_t dims[2] = {(cuuint64_t)m.head_dim, (cuuint64_t)n_pages * m.n_kv_heads * kPage}, strides[1] = {(cuuint64_t)m.head_dim};
+  const cuuint32_t box[2] = {(cuuint32_t)m.head_dim, kPage}, estr[2] = {1, 1};
+  const CUresult r = reinterpret_cast<EncodeTiledFn>(ctx->tmap_encode)(
+      map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<void *>(codes), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+      m.head_dim == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B, CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  if (r != CUDA_SUCCESS) {
+    set_error("cuTensorMapEncodeTiled failed with CUresult %d", (int)r);
+    return LR_ECUDA;
+  }
+  return LR_OK;
+}
+
 template <int kD>
-int launch(lr_plan *p, const uint16_t *q, const Fp8Pools &in, uint16_t *out, float *lse, float scale_log2, cudaStream_t s) {
+int launch(lr_plan *p, const CUtensorMap &k_map, const uint16_t *q, const Fp8Pools &in, uint16_t *out, float *lse, float scale_log2, cudaStream_t s) {
   const DevTcPlan &tc = p->tc;
   p->ctx->launches++;
-  if (int rc = cuda_fail(launch_dependent(attn_fp8_kernel<kD>, dim3((unsigned)tc.n_cta), dim3(kThreads), kSmemBytes<kD>, s, p->dev, tc, q, in, out, lse, scale_log2),
+  if (int rc = cuda_fail(launch_dependent(attn_fp8_kernel<kD>, dim3((unsigned)tc.n_cta), dim3(kThreads), kSmemBytes<kD>, s, k_map, p->dev, tc, q, in, out,
+                                          lse, scale_log2),
                          "attn_fp8_kernel launch"))
     return rc;
   if (tc.n_targets == 0) return LR_OK;
@@ -915,8 +1039,10 @@ int init_attn_fp8_kernel() {
 }
 
 int launch_attn_fp8(lr_plan *p, const void *q, const lr_fp8_cache &c, void *out, float *lse, float scale, cudaStream_t s) {
-  const Fp8Pools in = {reinterpret_cast<const uint8_t *>(c.k_d), reinterpret_cast<const uint8_t *>(c.v_d), c.k_scale_d, c.v_scale_d};
-  return (p->dev.head_dim == 128 ? launch<128> : launch<64>)(p, reinterpret_cast<const uint16_t *>(q), in, reinterpret_cast<uint16_t *>(out), lse,
+  alignas(64) CUtensorMap k_map;
+  if (int rc = encode_k(p->ctx, c.k_d, p->dev.n_pool_pages, &k_map)) return rc;
+  const Fp8Pools in = {reinterpret_cast<const uint8_t *>(c.v_d), c.k_scale_d, c.v_scale_d};
+  return (p->dev.head_dim == 128 ? launch<128> : launch<64>)(p, k_map, reinterpret_cast<const uint16_t *>(q), in, reinterpret_cast<uint16_t *>(out), lse,
                                                              scale * 1.4426950408889634f, s);
 }
 
