@@ -88,8 +88,11 @@ struct __align__(16) Ctrl {
   uint64_t wait_limit_ns;
   int32_t *status;        // the plan's
   float xch_m[128], xch_l[128], xch_unit[128];  // stream 1's rows, for the in-CTA combination
+  // What the rows of Q were divided by, of two pieces in turn: the queries of a piece are written when both streams have asked for the last scores of the piece
+  // before, and a stream asks for its first behind the weights of the one before that, which its threads had to know this for.
+  float q_unit[2][2][128];
 };
-constexpr int kCtrlBytes = 7 << 10;
+constexpr int kCtrlBytes = 9 << 10;
 static_assert(sizeof(Ctrl) <= kCtrlBytes, "Ctrl must fit behind the tiles");
 template <int kD>
 constexpr int kSmemBytes = 2 * Shape<kD>::kQBytes + Shape<kD>::kKStages * Shape<kD>::kCodeBytes + Shape<kD>::kVStages * Shape<kD>::kVBytes +
@@ -238,6 +241,9 @@ __device__ __forceinline__ int2 ld_pair(const void *p) {
 __device__ __forceinline__ void st_shared(uint32_t addr, uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
   asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(addr), "r"(a), "r"(b), "r"(c), "r"(d) : "memory");
 }
+__device__ __forceinline__ void st_shared2(uint32_t addr, uint32_t a, uint32_t b) {
+  asm volatile("st.shared.v2.b32 [%0], {%1, %2};" ::"r"(addr), "r"(a), "r"(b) : "memory");
+}
 
 // P = exp2(t) for 64 exponents, as halves over the first half of the score buffer; returns their fp32 sum and, worked out in the shadow of the
 // exponentials, the largest t.
@@ -297,36 +303,59 @@ __device__ __noinline__ bool sees_nan(const uint8_t *nan4, const TcPage *pages, 
   return seen;
 }
 
-// A row of Q, scaled by a power of two to lie within 448, as its two e4m3 terms (those of [t0, t1) are stored); returns 2 to the exponent taken out, or NaN for
-// a row that is not finite (its scores are no numbers either).
+// Rows r0 .. r0 + n - 1 of a tile (q_index of row r0 + i: in lane i0 + i), each scaled by a power of two to lie within 448, as their two e4m3 terms; 2 to the
+// exponent taken out goes to unit[row], NaN for a row that is not finite (its scores are no numbers either).  The rows come by asynchronous copies into
+// the place of their terms (bf16 is as long as the two) and are converted where they lie, a row's channels across lanes.  Registers for 32 rows in flight
+// there are none, and with a row to a thread this took 17,000 cycles at the start of every piece, a third of a short call.
 template <int kD>
-__device__ __noinline__ float convert_q(const uint16_t *__restrict__ q, int64_t q_index, uint32_t tile, int r, int t0, int t1) {
-  uint4 x[kD / 8];
-#pragma unroll
-  for (int i = 0; i < kD / 8; ++i) x[i] = q_index >= 0 ? __ldg(reinterpret_cast<const uint4 *>(q + q_index * kD) + i) : make_uint4(0, 0, 0, 0);
-  uint32_t top = 0;
-#pragma unroll
-  for (int i = 0; i < kD / 8; ++i)
-    top = __vmaxu2(top, __vmaxu2(__vmaxu2(x[i].x & 0x7FFF7FFFu, x[i].y & 0x7FFF7FFFu), __vmaxu2(x[i].z & 0x7FFF7FFFu, x[i].w & 0x7FFF7FFFu)));
-  top = max(top & 0xFFFFu, top >> 16);
-  const int e = min(max((int)(top >> 7) - 135 + ((top & 0x7Fu) > 0x60u ? 1 : 0), -126), 120);  // as lr_fp8_write
-  const float by = pow2(-e);
-#pragma unroll
-  for (int u = 0; u < kD / 16; ++u) {
-    const uint32_t w[8] = {x[2 * u].x, x[2 * u].y, x[2 * u].z, x[2 * u].w, x[2 * u + 1].x, x[2 * u + 1].y, x[2 * u + 1].z, x[2 * u + 1].w};
-    uint32_t hi[4], lo[4];
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const float a = bits_f(w[2 * j] << 16) * by, b = bits_f(w[2 * j] & 0xFFFF0000u) * by, c = bits_f(w[2 * j + 1] << 16) * by,
-                  d = bits_f(w[2 * j + 1] & 0xFFFF0000u) * by;
-      hi[j] = pack_e4m3(a, b, c, d);
-      const float2 ab = fp8_float2(hi[j] & 0xFFFFu), cd = fp8_float2(hi[j] >> 16);
-      lo[j] = pack_e4m3(a - ab.x, b - ab.y, c - cd.x, d - cd.y);
-    }
-    if (t0 == 0) st_shared(tile + row_unit<kD>(r, u), hi[0], hi[1], hi[2], hi[3]);
-    if (t1 == 2) st_shared(tile + Shape<kD>::kTermBytes + row_unit<kD>(r, u), lo[0], lo[1], lo[2], lo[3]);
+__device__ __noinline__ void convert_q(const uint16_t *__restrict__ q, int64_t q_index, uint32_t tile, float *unit, int r0, int n, int i0) {
+  constexpr int kLanes = kD / 8, kRows = 32 / kLanes;  // lanes to a row, 8 channels each; rows at a time
+  const int lane = threadIdx.x & 31, sub = lane / kLanes, c = lane % kLanes;
+  const uint32_t raw = tile + (r0 + sub) * kD + (c % (kLanes / 2)) * 16 + (c / (kLanes / 2)) * Shape<kD>::kTermBytes;
+#pragma unroll 1
+  for (int p = 0; p < n; p += kRows) {
+    const int64_t index = __shfl_sync(0xFFFFFFFFu, q_index, (i0 + p + sub) & 31);
+    if (p + sub < n) copy_codes(raw + p * kD, reinterpret_cast<const uint8_t *>(q + index * kD + c * 8));
   }
-  return top < 0x7F80u ? pow2(e) : __uint_as_float(0x7FC00000u);
+  asm volatile("cp.async.wait_all;" ::: "memory");
+  __syncwarp();
+#pragma unroll 1
+  for (int p0 = 0; p0 < n; p0 += 2 * kRows) {  // two of the warp's rows (or four, or eight) at a time, for their latencies' sake
+    uint32_t w[2][4], top[2];
+#pragma unroll
+    for (int b = 0; b < 2; ++b) {
+      const int p = p0 + b * kRows;
+      const uint4 x = p + sub < n ? ld_shared(raw + p * kD) : make_uint4(0, 0, 0, 0);
+      w[b][0] = x.x, w[b][1] = x.y, w[b][2] = x.z, w[b][3] = x.w;
+      const uint32_t t = __vmaxu2(__vmaxu2(x.x & 0x7FFF7FFFu, x.y & 0x7FFF7FFFu), __vmaxu2(x.z & 0x7FFF7FFFu, x.w & 0x7FFF7FFFu));
+      top[b] = max(t & 0xFFFFu, t >> 16);
+    }
+#pragma unroll
+    for (int m = kLanes / 2; m > 0; m >>= 1)
+#pragma unroll
+      for (int b = 0; b < 2; ++b) top[b] = max(top[b], __shfl_xor_sync(0xFFFFFFFFu, top[b], m));
+    __syncwarp();  // the rows have been read
+#pragma unroll
+    for (int b = 0; b < 2; ++b) {
+      const int p = p0 + b * kRows, e = min(max((int)(top[b] >> 7) - 135 + ((top[b] & 0x7Fu) > 0x60u ? 1 : 0), -126), 120);  // as lr_fp8_write
+      const float by = pow2(-e);
+      uint32_t hi[2], lo[2];
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        const uint32_t w0 = w[b][2 * j], w1 = w[b][2 * j + 1];
+        const float x0 = bits_f(w0 << 16) * by, x1 = bits_f(w0 & 0xFFFF0000u) * by, x2 = bits_f(w1 << 16) * by, x3 = bits_f(w1 & 0xFFFF0000u) * by;
+        hi[j] = pack_e4m3(x0, x1, x2, x3);
+        const float2 h0 = fp8_float2(hi[j] & 0xFFFFu), h1 = fp8_float2(hi[j] >> 16);
+        lo[j] = pack_e4m3(x0 - h0.x, x1 - h0.y, x2 - h1.x, x3 - h1.y);
+      }
+      if (p + sub < n) {
+        const uint32_t at = tile + row_unit<kD>(r0 + p + sub, c >> 1) + (c & 1) * 8;
+        st_shared2(at, hi[0], hi[1]);
+        st_shared2(at + Shape<kD>::kTermBytes, lo[0], lo[1]);
+        if (c == 0) unit[r0 + p + sub] = top[b] < 0x7F80u ? pow2(e) : __uint_as_float(0x7FC00000u);
+      }
+    }
+  }
 }
 
 // The store epilogue of a softmax thread: row r of the accumulator at o_addr times `self` (and, when the CTA's two streams worked on the same
@@ -342,37 +371,34 @@ __device__ __noinline__ void store_rows(uint32_t o_addr, uint32_t o_other, int s
     self *= inv;
     other *= inv;
   }
-#pragma unroll
-  for (int hf = 0; hf < kD / 64; ++hf) {
-    uint32_t o[64];
-    tmem_ld64(o_addr + hf * 64, o);
+#pragma unroll 1
+  for (int ch = 0; ch < kD / 32; ++ch) {
+    uint32_t o[32];
+    tmem_ld32(o_addr + ch * 32, o);
     tc_wait_ld();
 #pragma unroll
-    for (int c = 0; c < 64; ++c) o[c] = __float_as_uint(bits_f(o[c]) * self);
+    for (int c = 0; c < 32; ++c) o[c] = __float_as_uint(bits_f(o[c]) * self);
     if (any_other) {  // the loads are warp-wide; a row whose other stream saw nothing keeps its own values
+      uint32_t p[32];
+      tmem_ld32(o_other + ch * 32, p);
+      tc_wait_ld();
+      if (other_live) {
 #pragma unroll
-      for (int part = 0; part < 2; ++part) {
-        uint32_t p[32];
-        tmem_ld32(o_other + hf * 64 + part * 32, p);
-        tc_wait_ld();
-        if (other_live) {
-#pragma unroll
-          for (int c = 0; c < 32; ++c) o[part * 32 + c] = __float_as_uint(fmaf(bits_f(p[c]), other, bits_f(o[part * 32 + c])));
-        }
+        for (int c = 0; c < 32; ++c) o[c] = __float_as_uint(fmaf(bits_f(p[c]), other, bits_f(o[c])));
       }
     }
     if (q_index >= 0) {
       if (slot < 0) {
-        uint4 *dst = reinterpret_cast<uint4 *>(out + q_index * kD + hf * 64);
+        uint4 *dst = reinterpret_cast<uint4 *>(out + q_index * kD + ch * 32);
 #pragma unroll
-        for (int j = 0; j < 8; ++j)
+        for (int j = 0; j < 4; ++j)
           dst[j] = make_uint4(pack_bf16(bits_f(o[8 * j]), bits_f(o[8 * j + 1])), pack_bf16(bits_f(o[8 * j + 2]), bits_f(o[8 * j + 3])),
                               pack_bf16(bits_f(o[8 * j + 4]), bits_f(o[8 * j + 5])), pack_bf16(bits_f(o[8 * j + 6]), bits_f(o[8 * j + 7])));
       } else {
         // chunk-major: 16-byte chunk k of row r at [slot][k][r], so a warp's store is 512 contiguous bytes
-        uint4 *dst = reinterpret_cast<uint4 *>(partial_o) + ((int64_t)slot * (kD / 4) + hf * 16) * 128 + r;
+        uint4 *dst = reinterpret_cast<uint4 *>(partial_o) + ((int64_t)slot * (kD / 4) + ch * 8) * 128 + r;
 #pragma unroll
-        for (int j = 0; j < 16; ++j) dst[j * 128] = make_uint4(o[4 * j], o[4 * j + 1], o[4 * j + 2], o[4 * j + 3]);
+        for (int j = 0; j < 8; ++j) dst[j * 128] = make_uint4(o[4 * j], o[4 * j + 1], o[4 * j + 2], o[4 * j + 3]);
       }
     }
   }
@@ -783,12 +809,17 @@ attn_fp8_kernel(const __grid_constant__ CUtensorMap k_map, DevBatch d, DevTcPlan
       const RowInfo ri = row_info(d, tc, rq, T, mode == 2 ? pi.mtile0 + s : pi.mtile0, r, pi.kv_head);
       float sc_row = 0.f;
       if (ok) {
-        // the queries, once the products of the piece before no longer read the buffers; with one M-tile each stream stores its part
+        // the queries, once the products of the piece before no longer read the buffers; of one M-tile each stream takes half of every warp's rows.
+        // Padding is left as it is: what comes of it reaches rows that nobody reads.
         ok = wait<kD, 0>(&ctrl->q_empty, ((uint32_t)(pc - piece0) & 1u) ^ 1u, 245);
         if (ok) {
-          sc_row = scale_log2 * convert_q<kD>(q, ri.q_index, smem_u32(q_smem) + (mode == 2 ? s : 0) * kQBytes, r, mode == 2 ? 0 : s, mode == 2 ? 2 : s + 1);
+          const int live = __popc(__ballot_sync(0xFFFFFFFFu, ri.q_index >= 0)), i0 = mode == 2 ? 0 : s * 16;  // (live rows come first)
+          float *unit = ctrl->q_unit[(pc - piece0) & 1][mode == 2 ? s : 0];
+          convert_q<kD>(q, ri.q_index, smem_u32(q_smem) + (mode == 2 ? s : 0) * kQBytes, unit, quarter * 32 + i0, min(live - i0, mode == 2 ? 32 : 16), i0);
           fence_proxy_async();
           mbar_arrive(&ctrl->q_full);
+          ok = wait<kD, 0>(&ctrl->q_full, (uint32_t)(pc - piece0) & 1u, 246);
+          if (ok && ri.q_index >= 0) sc_row = scale_log2 * unit[r];
         }
       }
       if (ok && my_units > 0) {
@@ -861,7 +892,7 @@ attn_fp8_kernel(const __grid_constant__ CUtensorMap k_map, DevBatch d, DevTcPlan
               for (int p = 0; p < kPagesPerTile / 2; ++p) n_ok[p] = page_n_ok(__ldg(&pages[half * 4 + p].meta), ri);
               mask_half(v, n_ok);
             }
-            for (;;) {
+            for (;;) {  // three times at most: a row's reference moves once, the sum apart is taken once
               float t_max;
               const float sum = exp_half(v, sh_addr, t_max);
               // beyond what a half holds, or a row's first keys: again, with the reference moved
@@ -871,7 +902,7 @@ attn_fp8_kernel(const __grid_constant__ CUtensorMap k_map, DevBatch d, DevTcPlan
                 if (off >= -kApart) l = fmaf(sum, pow2(-off - (int)kHead), l);
                 break;
               }
-              float shift = 0.f;
+              float down_by = 0.f, up_by = 0.f;  // in two steps: the first leaves exactly 0 at the largest, however large that was, so that this ends
               if (grows) {
                 if (grow) {
                   const float to = t_max - neg + kLift;
@@ -881,19 +912,19 @@ attn_fp8_kernel(const __grid_constant__ CUtensorMap k_map, DevBatch d, DevTcPlan
                     l *= down;
                   }
                   m_used = to;
-                  shift = bias - to - neg;
+                  down_by = t_max;
+                  up_by = bias - kLift;
                 }
                 moved = !first;
               } else {
                 l += sum;
                 apart = false;
-                shift = (float)off + kHead;
-                bias = shift;
+                up_by = (float)off + kHead;
+                bias = up_by;
               }
-              neg += shift;
 #pragma unroll
               for (int i = 0; i < 64; i += 2) {
-                const float2 t = fadd2(make_float2(bits_f(v[i]), bits_f(v[i + 1])), make_float2(shift, shift));
+                const float2 t = fadd2(fadd2(make_float2(bits_f(v[i]), bits_f(v[i + 1])), make_float2(-down_by, -down_by)), make_float2(up_by, up_by));
                 v[i] = __float_as_uint(t.x);
                 v[i + 1] = __float_as_uint(t.y);
               }

@@ -163,6 +163,31 @@ def test_large_queries_over_small_keys_and_the_reverse(by, path):
     compare(w, store_pools(t.k_pool, t.v_pool), path)
 
 
+@pytest.mark.parametrize("path", PATHS)
+@pytest.mark.parametrize("by", [24, 40, 90])
+@pytest.mark.parametrize("how", ["falling", "steps", "one large"])
+def test_scores_beyond_what_fp32_tells_apart(how, by, path):
+    """Queries 2^by times as large: the weights are 1 for one key, and the output is its V, of whichever size."""
+    w = chain([900, 170], seed=18)
+    b, t, rng = w.batch, w.tensors, np.random.default_rng(19)
+    at = tokens(b)
+    v = bf16_to_f32(t.v_pool)
+    with np.errstate(all="ignore"):
+        v[at[:, 0], :, at[:, 1]] *= np.exp2(np.round(SIZES[how](len(at), rng) / 4)).astype(np.float32)[:, None, None]
+        t.v_pool[:] = bf16_round(v)
+        t.q[:] = bf16_round(bf16_to_f32(t.q) * np.float32(2.0 ** by))
+    pools = store_pools(t.k_pool, t.v_pool)
+    k, v = as_bf16(pools[0], pools[2]), as_bf16(pools[1], pools[3])
+    o_ref, l_ref, weights = O.verify_attention(b, t.q, k, v, return_weights=True)
+    assert min(x.max() for x in weights.values()) > 1 - 2.0 ** -20  # (else the input would have to be another)
+    limit = bound(w, k, v, o_ref)
+    out, lse = run_stored(w, pools, path)
+    got = bf16_to_f32(R.bf16_bits(out)).astype(np.float64)
+    assert (np.abs(got - o_ref) <= limit).all()
+    # scores: D products and sums in fp32, Q to 2^-19 of its largest
+    assert (np.abs(lse.cpu().numpy() - l_ref) <= 2.0 ** -16 * np.abs(l_ref)).all()
+
+
 # ---- ways of calling it ------------------------------------------------------------------------------------------------------
 @pytest.mark.parametrize("path", PATHS)
 def test_a_softmax_scale_of_the_callers(path):
