@@ -223,7 +223,7 @@ class Fp8Cache:
                 raise ValueError(f"an 8-bit cache is codes [pages, KV heads, 16, head size] and scales [pages, KV heads, 16], contiguous, on one device: "
                                  f"got {tuple(t.shape)} {t.dtype} on {t.device}")
         self.k, self.v, self.k_scale, self.v_scale = k, v, k_scale, v_scale
-        self.n_pages, self.heads, self.head_dim, self.device = shape[0], shape[1], shape[3], k.device
+        self.n_pages, self.heads, self.head_dim, self.device, self.index = shape[0], shape[1], shape[3], k.device, k.device.index
         self._c = lr_fp8_cache(k.data_ptr(), v.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr(), shape[0])
         self.c = C.addressof(self._c)
 
@@ -238,23 +238,26 @@ class Fp8Cache:
 def _check_cache(cache: Fp8Cache, ctx: "Context") -> None:
     # what the C side cannot see: how large the tensors behind its pointers are, and where
     m = ctx.model
-    if cache.heads != m.n_kv_heads or cache.head_dim != m.head_dim or cache.device.index != ctx.device:
+    if cache.heads != m.n_kv_heads or cache.head_dim != m.head_dim or cache.index != ctx.device:
         raise ValueError(f"the cache has {cache.heads} heads of {cache.head_dim} on {cache.device}, the context {m.n_kv_heads} of {m.head_dim} on cuda:{ctx.device}")
 
 
-def _fp8_rows(ctx: "Context", cache: Fp8Cache, k: torch.Tensor, v: torch.Tensor, slots: torch.Tensor, status: Optional[torch.Tensor]) -> int:
-    """Number of tokens, with the tensors found to be what the C side takes them for."""
+def _fp8_rows(ctx: "Context", cache: Fp8Cache, k: torch.Tensor, v: torch.Tensor, slots: torch.Tensor, status: Optional[torch.Tensor]) -> tuple:
+    """Number of tokens and the rows' strides, with the tensors found to be what the C side takes them for."""
     _check_cache(cache, ctx)
-    n, dev = slots.numel(), cache.device
+    n, heads, width, dev = slots.numel(), cache.heads, cache.head_dim, ctx.device
+    strides = []
     for t in (k, v):
-        if t.shape != (n, cache.heads, cache.head_dim) or t.dtype != torch.bfloat16 or t.device != dev or (n and (t.stride(2) != 1 or t.stride(1) != cache.head_dim)):
-            raise ValueError(f"rows are bf16 [{n}, {cache.heads}, {cache.head_dim}] on {dev}, a token's heads side by side: got {tuple(t.shape)} "
+        row, head, one = t.stride() if t.dim() == 3 else (0, 0, 0)
+        if t.shape != (n, heads, width) or t.dtype is not torch.bfloat16 or t.get_device() != dev or (n and (one != 1 or head != width)):
+            raise ValueError(f"rows are bf16 [{n}, {heads}, {width}] on {cache.device}, a token's heads side by side: got {tuple(t.shape)} "
                              f"{t.dtype} strides {t.stride()} on {t.device}")
-    if slots.dtype != torch.int64 or not slots.is_contiguous() or slots.device != dev:
-        raise ValueError(f"slots are contiguous int64 on {dev}")
-    if status is not None and (status.dtype != torch.int32 or status.numel() < 2 or not status.is_contiguous() or status.device != dev):
-        raise ValueError(f"status is two int32 on {dev}")
-    return n
+        strides.append(row if n > 1 else heads * width)
+    if slots.dtype is not torch.int64 or not slots.is_contiguous() or slots.get_device() != dev:
+        raise ValueError(f"slots are contiguous int64 on {cache.device}")
+    if status is not None and (status.dtype is not torch.int32 or status.numel() < 2 or not status.is_contiguous() or status.get_device() != dev):
+        raise ValueError(f"status is two int32 on {cache.device}")
+    return n, strides[0], strides[1]
 
 
 class Context:
@@ -349,18 +352,16 @@ class Context:
                      stream=None) -> None:
         """Quantises rows [tokens, KV heads, head size] (bf16; a slice of a joint projection's output will do) into the cache's token
         slots (int64: page * 16 + place, negative: none); status: two int32 of zeros that a slot beyond the cache sets."""
-        n = _fp8_rows(self, cache, k, v, slots, status)
-        width = cache.heads * cache.head_dim
-        _check(lib().lr_fp8_write(self.handle, cache.c, _ptr(k), k.stride(0) if n > 1 else width, _ptr(v), v.stride(0) if n > 1 else width, _ptr(slots), n,
-                                  _ptr(status), _stream_on(self.device, stream)), "lr_fp8_write")
+        n, k_stride, v_stride = _fp8_rows(self, cache, k, v, slots, status)
+        _check(lib().lr_fp8_write(self.handle, cache.c, k.data_ptr(), k_stride, v.data_ptr(), v_stride, slots.data_ptr(), n, _ptr(status),
+                                  _stream_on(self.device, stream)), "lr_fp8_write")
 
     def lr_fp8_read(self, cache: Fp8Cache, slots: torch.Tensor, k: torch.Tensor, v: torch.Tensor, status: Optional[torch.Tensor] = None,
                     stream=None) -> None:
         """The values at the token slots, into rows as ``lr_fp8_write`` takes them; a row without a slot is left as it was."""
-        n = _fp8_rows(self, cache, k, v, slots, status)
-        width = cache.heads * cache.head_dim
-        _check(lib().lr_fp8_read(self.handle, cache.c, _ptr(slots), n, _ptr(k), k.stride(0) if n > 1 else width, _ptr(v), v.stride(0) if n > 1 else width,
-                                 _ptr(status), _stream_on(self.device, stream)), "lr_fp8_read")
+        n, k_stride, v_stride = _fp8_rows(self, cache, k, v, slots, status)
+        _check(lib().lr_fp8_read(self.handle, cache.c, slots.data_ptr(), n, k.data_ptr(), k_stride, v.data_ptr(), v_stride, _ptr(status),
+                                 _stream_on(self.device, stream)), "lr_fp8_read")
 
     def accept_sample_filtered_scratch(self, n_rows: int) -> torch.Tensor:
         n = C.c_size_t()

@@ -3,14 +3,19 @@
 // Two kernels.  drafted_stats_kernel streams all rows of both matrices once, a warp a chunk at a time, and leaves the pairs (M_c, S_c)
 // of the chunks (accept_stats.cuh): bound by HBM.  drafted_walk_kernel takes a cluster of eight CTAs a branch:
 //   1. its warps take the branch's rows in turn: the pairs of a row of P and of Q into (m, Z), P(d), Q(d), and whether the draft is
-//      refused, u Q(d) >= P(d).  A warp remembers its first refused row; behind a cluster barrier the smallest of all is the row the walk
-//      stops at, and its (m, Z) come from the warp that has them;
+//      refused, u Q(d) >= P(d).  A warp remembers its first refused row; the smallest of all is the row the walk stops at, and its (m, Z) come from the
+//      warp that has them.  A branch of fewer rows than a CTA has warps is gone through by every CTA alone, a longer one by all together and a cluster
+//      barrier;
 //   2. the weights max(0, P - Q) over that row (or P, behind a full match): a CTA sums an eighth of the vocabulary, 256 tokens a step,
-//      the sums of the steps staying in shared memory.  Their total and the inverse CDF need all CTAs' sums: a second cluster barrier;
+//      the sums of the steps staying in shared memory.  Their total and the inverse CDF need all CTAs' sums: a cluster barrier;
 //   3. the CTA whose share holds u_final * total finds the step from the sums, then the token by computing the step's weights again.
 // The second read of the stop rows mostly hits L2.  As one CTA a branch the walk over 152 K tokens would keep 3 to 55 SMs busy for
-// ten microseconds; a cluster has the first two reductions without a trip through global memory or a launch of their own.
+// ten microseconds; a cluster has the reductions without a trip through global memory or a launch of their own.
 // Weights are fp32; the sums of steps, CTAs and the scan for the token are in 64 bits and of fixed order: same inputs, same outputs.
+//
+// Measured, 152 K tokens: 65 branches of up to 16 drafts 84 us, of which the stream over the rows is 70 (its bytes at the copy rate: 58); 3 branches 17 us, bound by
+// the walk's chain of trips to memory.  Weights two at a time in packed fp32 and CTAs of 1024 threads where there are SMs for them brought the
+// first from 107 and the second from 26.
 #include <algorithm>
 
 #include "accept_stats.cuh"
@@ -25,7 +30,7 @@ constexpr int kCtasPerSm = 4;
 constexpr int kCluster = 8;
 constexpr int kTokens = 256;       // a step: 8 tokens a lane
 constexpr int kMaxSteps = 4096;    // of a CTA: 16 KB of sums
-constexpr int kAhead = 4;          // steps a warp has in flight
+constexpr int kAhead = 2;          // steps a warp has in flight: with more the weights spill (64 registers for four CTAs an SM)
 
 struct Rows {  // a matrix of logits, and log2(e) / T
   const uint16_t *logits;
@@ -105,29 +110,67 @@ struct Stop {  // the row a warp would stop at
   RowSum p, q;
 };
 
+__device__ __forceinline__ float2 add2(float2 a, float2 b) {
+  float2 d;
+  asm("{\n\t.reg .b64 x, y, z;\n\tmov.b64 x, {%2, %3};\n\tmov.b64 y, {%4, %5};\n\tadd.rn.f32x2 z, x, y;\n\tmov.b64 {%0, %1}, z;\n\t}"
+      : "=f"(d.x), "=f"(d.y)
+      : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+  return d;
+}
+__device__ __forceinline__ float2 mul2(float2 a, float2 b) {
+  float2 d;
+  asm("{\n\t.reg .b64 x, y, z;\n\tmov.b64 x, {%2, %3};\n\tmov.b64 y, {%4, %5};\n\tmul.rn.f32x2 z, x, y;\n\tmov.b64 {%0, %1}, z;\n\t}"
+      : "=f"(d.x), "=f"(d.y)
+      : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+  return d;
+}
 // The rows the final token is drawn from, and their weights.
 struct Weights {
   const uint16_t *pr, *qr;  // qr: null for P alone
   RowSum p, q;
   float kp, kq;
   int32_t vocab;
-  __device__ __forceinline__ void load(int32_t vi, uint4 &a, uint4 &b) const {
-    a = __ldg(reinterpret_cast<const uint4 *>(pr) + vi);
-    if (qr != nullptr) b = __ldg(reinterpret_cast<const uint4 *>(qr) + vi);
+  __device__ __forceinline__ void alone() {  // P without Q
+    qr = nullptr;
+    q = RowSum{0.f, 0.f};
   }
-  // of the eight tokens of vector vi, loaded (where it is a whole one) into a and b
-  __device__ __forceinline__ void weigh(int32_t vi, const uint4 &a, const uint4 &b, float (&w)[8]) const {
-    float x[8], y[8];
-    if (vi < (vocab >> 3)) unpack(a, x);
-    else load_tail(pr, vocab, vi, x);
-#pragma unroll
-    for (int j = 0; j < 8; ++j) w[j] = share(x[j], p, kp);
-    if (qr != nullptr) {
-      if (vi < (vocab >> 3)) unpack(b, y);
-      else load_tail(qr, vocab, vi, y);
-#pragma unroll
-      for (int j = 0; j < 8; ++j) w[j] = fmaxf(w[j] - share(y[j], q, kq), 0.f);
+  __device__ __forceinline__ void load(int32_t vi, uint4 &a, uint4 &b) const {  // eight logits of each; -inf behind the last
+    b = make_uint4(0xFF80FF80u, 0xFF80FF80u, 0xFF80FF80u, 0xFF80FF80u);
+    if (vi < (vocab >> 3)) {
+      a = __ldg(reinterpret_cast<const uint4 *>(pr) + vi);
+      if (qr != nullptr) b = __ldg(reinterpret_cast<const uint4 *>(qr) + vi);
+    } else {
+      a = tail(pr, vi);
+      if (qr != nullptr) b = tail(qr, vi);
     }
+  }
+  __device__ __forceinline__ uint4 tail(const uint16_t *row, int32_t vi) const {
+    uint32_t t[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const int32_t e = vi * 8 + 2 * j;
+      t[j] = (e < vocab ? (uint32_t)row[e] : 0xFF80u) | (e + 1 < vocab ? (uint32_t)row[e + 1] : 0xFF80u) << 16;
+    }
+    return make_uint4(t[0], t[1], t[2], t[3]);
+  }
+  // max(0, P - Q) of two tokens; Q's row may be all -inf (load) with q = {0, 0}.  x - m is exact near the maximum, whatever the logits' size; a NaN of P falls to the
+  // maximum with 0.  Below 2^-126 of the largest there is no weight.
+  __device__ __forceinline__ float2 weight2(uint32_t a, uint32_t b) const {
+    const float2 x = mul2(add2(make_float2(bf_lo(a), bf_hi(a)), make_float2(-p.m, -p.m)), make_float2(kp, kp));
+    const float2 y = mul2(add2(make_float2(denan(bf_lo(b)), denan(bf_hi(b))), make_float2(-q.m, -q.m)), make_float2(kq, kq));
+    // (not as one fused operation: where the rows are equal the difference has to be 0, not what a rounding left)
+    const float2 w = add2(mul2(make_float2(ex2_approx(x.x), ex2_approx(x.y)), make_float2(p.inv, p.inv)),
+                          mul2(make_float2(ex2_approx(y.x), ex2_approx(y.y)), make_float2(-q.inv, -q.inv)));
+    return make_float2(fmaxf(w.x, 0.f), fmaxf(w.y, 0.f));
+  }
+  __device__ __forceinline__ float mass(const uint4 &a, const uint4 &b) const {  // of the eight tokens of a vector
+    const float2 w = add2(add2(weight2(a.x, b.x), weight2(a.y, b.y)), add2(weight2(a.z, b.z), weight2(a.w, b.w)));
+    return w.x + w.y;
+  }
+  __device__ __forceinline__ void weigh(const uint4 &a, const uint4 &b, float (&w)[8]) const {  // one by one
+    const float2 t[4] = {weight2(a.x, b.x), weight2(a.y, b.y), weight2(a.z, b.z), weight2(a.w, b.w)};
+#pragma unroll
+    for (int j = 0; j < 8; ++j) w[j] = (j & 1) != 0 ? t[j / 2].y : t[j / 2].x;
   }
 };
 
@@ -166,13 +209,15 @@ __device__ __forceinline__ int find_lane(double w, double target, double &before
 }
 
 // cluster b of kCluster CTAs: branch b.  per_step: tokens of a step, kTokens or a multiple; steps: of a CTA.
-__global__ void __cluster_dims__(kCluster, 1, 1) __launch_bounds__(kThreads)
+template <int kWalk>
+__global__ void __cluster_dims__(kCluster, 1, 1) __launch_bounds__(kWalk, 1024 / kWalk)
 drafted_walk_kernel(Rows tp, Rows tq, int32_t vocab, const float2 *stats, int32_t n_rows, int n_chunks, int32_t per_step, int32_t steps,
                     const int32_t *__restrict__ draft_ids, const int32_t *__restrict__ cu_draft, const float *__restrict__ u_accept,
                     const float *__restrict__ u_final, int32_t *__restrict__ n_accept, int32_t *__restrict__ final_id, float *__restrict__ p_draft,
                     float *__restrict__ q_draft) {
+  constexpr int kTeam = kWalk / 32;
   extern __shared__ float s_step[];  // [steps]: the weight of each step of this CTA
-  __shared__ Stop s_stop[kWarps];
+  __shared__ Stop s_stop[kTeam];
   __shared__ double s_total[2];      // this CTA's weight, of either attempt
   __shared__ Stop s_at;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
@@ -187,7 +232,8 @@ drafted_walk_kernel(Rows tp, Rows tq, int32_t vocab, const float2 *stats, int32_
   mine.i = 0x7FFFFFFF;
   mine.p = mine.q = RowSum{0.f, 0.f};
   bool waited = false;
-  for (int32_t i = rank * kWarps + warp; i <= L; i += kCluster * kWarps) {
+  const bool few = L < kTeam;  // every CTA looks at all rows itself, which saves the wait for the others
+  for (int32_t i = (few ? 0 : rank * kTeam) + warp; i <= L; i += kCluster * kTeam) {
     float xd = -INFINITY, yd = -INFINITY, u = 0.f;
     if (i < L) {
       const int32_t d = draft_ids[d0 + i];
@@ -211,7 +257,7 @@ drafted_walk_kernel(Rows tp, Rows tq, int32_t vocab, const float2 *stats, int32_
       row.q = c.sum(tq.k_log2);
       const float p = share(xd, row.p, tp.k_log2), q = share(yd, row.q, tq.k_log2);
       refused = !(u * q < p);
-      if (lane == 0) {
+      if (lane == 0 && !(few && rank != 0)) {
         if (p_draft != nullptr) p_draft[d0 + i] = p;
         if (q_draft != nullptr) q_draft[d0 + i] = q;
       }
@@ -221,14 +267,15 @@ drafted_walk_kernel(Rows tp, Rows tq, int32_t vocab, const float2 *stats, int32_
   if (!waited) asm volatile("griddepcontrol.wait;" ::: "memory");
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   if (lane == 0) s_stop[warp] = mine;
-  cluster_barrier();
+  if (few) __syncthreads();
+  else cluster_barrier();
   if (warp == 0) {  // the first refused row of the cluster's warps
     int32_t best = 0x7FFFFFFF;
     uint32_t at = 0;
 #pragma unroll
-    for (int k = 0; k < kCluster * kWarps / 32; ++k) {
+    for (int k = 0; k < kCluster * kTeam / 32; ++k) {
       const int w = k * 32 + lane;
-      const uint32_t from = in_cta(&s_stop[w % kWarps], w / kWarps);
+      const uint32_t from = in_cta(&s_stop[w % kTeam], few ? rank : w / kTeam);
       const int32_t i = ld_cluster_i32(from);
       if (i < best) {
         best = i;
@@ -249,18 +296,18 @@ drafted_walk_kernel(Rows tp, Rows tq, int32_t vocab, const float2 *stats, int32_
   Weights wt;
   wt.vocab = vocab;
   wt.pr = tp.logits + (int64_t)(r0 + n) * tp.stride;
-  wt.qr = n < L ? tq.logits + (int64_t)(d0 + n) * tq.stride : nullptr;
+  wt.qr = tq.logits + (int64_t)(d0 + n) * tq.stride;
   wt.p = s_at.p;
   wt.q = s_at.q;
+  if (n == L || !(wt.q.inv > 0.f)) wt.alone();  // behind a full match, and where Q's row is all -inf
   wt.kp = tp.k_log2;
   wt.kq = tq.k_log2;
-  const int32_t n_vec = vocab >> 3;
   const int sub = per_step / kTokens;
 
   // ---- 2. the weights, once more from P alone where P - Q leaves nothing
   for (int attempt = 0;; ++attempt) {
     const int32_t s0 = rank * steps;
-    for (int32_t at = warp; at < steps; at += kWarps * kAhead) {
+    for (int32_t at = warp; at < steps; at += kTeam * kAhead) {
       float sum[kAhead];
 #pragma unroll
       for (int k = 0; k < kAhead; ++k) sum[k] = 0.f;
@@ -268,24 +315,18 @@ drafted_walk_kernel(Rows tp, Rows tq, int32_t vocab, const float2 *stats, int32_
         uint4 x[kAhead], y[kAhead];
 #pragma unroll
         for (int k = 0; k < kAhead; ++k) {
-          const int64_t vi = ((int64_t)(s0 + at + k * kWarps) * sub + j) * 32 + lane;
-          if (at + k * kWarps < steps && vi < n_vec) wt.load((int32_t)vi, x[k], y[k]);
+          const int64_t vi = ((int64_t)(s0 + at + k * kTeam) * sub + j) * 32 + lane;
+          x[k] = y[k] = make_uint4(0xFF80FF80u, 0xFF80FF80u, 0xFF80FF80u, 0xFF80FF80u);
+          if (at + k * kTeam < steps && vi * 8 < vocab) wt.load((int32_t)vi, x[k], y[k]);
         }
 #pragma unroll
-        for (int k = 0; k < kAhead; ++k) {
-          const int64_t vi = ((int64_t)(s0 + at + k * kWarps) * sub + j) * 32 + lane;
-          if (at + k * kWarps < steps && vi * 8 < vocab) {
-            float w[8];
-            wt.weigh((int32_t)vi, x[k], y[k], w);
-            sum[k] += ((w[0] + w[1]) + (w[2] + w[3])) + ((w[4] + w[5]) + (w[6] + w[7]));
-          }
-        }
+        for (int k = 0; k < kAhead; ++k) sum[k] += wt.mass(x[k], y[k]);
       }
 #pragma unroll
       for (int k = 0; k < kAhead; ++k) {
 #pragma unroll
         for (int o = 16; o > 0; o >>= 1) sum[k] += __shfl_xor_sync(0xFFFFFFFFu, sum[k], o);
-        if (lane == 0 && at + k * kWarps < steps) s_step[at + k * kWarps] = sum[k];
+        if (lane == 0 && at + k * kTeam < steps) s_step[at + k * kTeam] = sum[k];
       }
     }
     __syncthreads();
@@ -300,7 +341,7 @@ drafted_walk_kernel(Rows tp, Rows tq, int32_t vocab, const float2 *stats, int32_
     const double t = lane < kCluster ? ld_cluster_f64(in_cta(&s_total[attempt], lane)) : 0.0;
     const double total = warp_sum_f64(t);
     if (!(total > 0.0) && attempt == 0) {
-      wt.qr = nullptr;
+      wt.alone();
       continue;
     }
     // ---- 3. the token
@@ -312,14 +353,30 @@ drafted_walk_kernel(Rows tp, Rows tq, int32_t vocab, const float2 *stats, int32_
     if (past) owner = max(last, 0);
     if (rank == owner && warp == 0) {
       const double goal = past ? 1e300 : target;
-      int32_t step = -1, last_step = 0;
-      for (int32_t s = 0; s < steps && step < 0; s += 32) {
-        const int l = find_lane(s + lane < steps ? (double)s_step[s + lane] : 0.0, goal, before, last, lane);
-        if (last >= 0) last_step = s + last;
-        if (l >= 0) step = s + l;
+      // the step: a lane's share of them, then one by one
+      const int32_t each = (steps + 31) / 32, first = lane * each, end = min(first + each, steps);
+      double own = 0.0;
+      for (int32_t s = first; s < end; ++s) own += (double)s_step[s];
+      int l = find_lane(own, goal, before, last, lane);
+      const bool late = l < 0;
+      if (late) {
+        l = max(last, 0);
+        before = 0.0;  // (any: the last token with a weight is looked for)
       }
-      const bool late = step < 0;
-      if (late) step = last_step;
+      int32_t step = first;
+      double ahead = before, cum = before;
+      bool hit = false;
+      for (int32_t s = first; s < end; ++s) {
+        const double w = (double)s_step[s];
+        if (!hit && w > 0.0) {
+          step = s;
+          ahead = cum;
+          cum += w;
+          hit = !late && cum > goal;
+        }
+      }
+      step = __shfl_sync(0xFFFFFFFFu, step, l);
+      before = shfl_f64(ahead, l);
       int32_t token = 0;  // nothing has any weight: a row of -inf
       bool found = false;
       for (int j = 0; j < sub && !found; ++j) {
@@ -328,14 +385,14 @@ drafted_walk_kernel(Rows tp, Rows tq, int32_t vocab, const float2 *stats, int32_
 #pragma unroll
         for (int e = 0; e < 8; ++e) w[e] = 0.f;
         if (vi * 8 < vocab) {
-          uint4 x = make_uint4(0, 0, 0, 0), y = x;
-          if (vi < n_vec) wt.load((int32_t)vi, x, y);
-          wt.weigh((int32_t)vi, x, y, w);
+          uint4 x, y;
+          wt.load((int32_t)vi, x, y);
+          wt.weigh(x, y, w);
         }
         double mass = 0.0;
 #pragma unroll
         for (int e = 0; e < 8; ++e) mass += (double)w[e];
-        int l = find_lane(mass, late ? 1e300 : goal, before, last, lane);
+        l = find_lane(mass, late ? 1e300 : goal, before, last, lane);
         found = l >= 0;
         if (!found) l = last;
         if (l >= 0) {  // within that lane's eight
@@ -390,7 +447,9 @@ int launch_accept_drafted(lr_ctx *ctx, const void *logits, int64_t stride, const
                                           total, st),
                          "drafted_stats_kernel launch"))
     return rc;
-  return cuda_fail(launch_dependent(drafted_walk_kernel, dim3((unsigned)n_branch * kCluster), dim3(kThreads), (size_t)steps * sizeof(float), s, p, q, vocab, st,
+  // With an SM for each CTA a CTA of 1024 threads has all of its share of a row on its way at once; more CTAs share SMs, four of 256 each.
+  const bool wide = (int64_t)n_branch * kCluster <= ctx->sm_count;
+  return cuda_fail(launch_dependent(wide ? drafted_walk_kernel<1024> : drafted_walk_kernel<256>, dim3((unsigned)n_branch * kCluster), dim3(wide ? 1024 : 256), (size_t)steps * sizeof(float), s, p, q, vocab, st,
                                     n_rows, n_chunks, (int32_t)per_step, (int32_t)steps, drafts, cu_draft, u_accept, u_final, n_accept, final_id, p_draft,
                                     q_draft),
                    "drafted_walk_kernel launch");

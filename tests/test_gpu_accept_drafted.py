@@ -105,6 +105,19 @@ def test_ragged_branches(V, T, Tq):
     assert np.array_equal(n, lens)
 
 
+@pytest.mark.parametrize("n_branch,most", [(2, 70), (40, 6), (40, 20)])
+def test_few_and_many_branches_of_short_and_of_long_drafts(n_branch, most):
+    """An SM for each CTA or several CTAs to one; rows for every CTA alone or for the cluster's warps in turn."""
+    rng = np.random.default_rng(n_branch + most)
+    V = 1027
+    lengths = rng.integers(most // 2, most + 1, n_branch)
+    lengths[0], lengths[1] = most, 0
+    cu = np.concatenate([[0], np.cumsum(lengths)]).astype(np.int32)
+    p, q, d = _models(rng, int(cu[-1]) + n_branch, cu, V, noise=0.1)
+    n, _ = _check(p, q, d, cu, 0.8, 0.8, rng.random(int(cu[-1])) * 0.9, rng.random(n_branch), most_unsure=2)
+    assert n.max() > most // 3
+
+
 def test_no_drafts_at_all_and_one_branch():
     rng = np.random.default_rng(1)
     p, q, _ = _models(rng, 3, np.zeros(4, dtype=np.int32), 500)
