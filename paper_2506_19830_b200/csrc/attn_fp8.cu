@@ -81,6 +81,7 @@ struct __align__(16) Ctrl {
   uint64_t q_full, q_empty;
   uint64_t s_full[2][2], p_full[2][2], o_done[2];  // [stream][half]
   uint64_t epi_done, drain[2];
+  uint64_t join;          // stream 0's warps among each other, in pieces whose keys they share
   uint64_t xch;           // stream 1 -> stream 0: its sums are published and its accumulator is final
   uint64_t info_full[kInfos];
   uint32_t tmem_base;
@@ -94,9 +95,11 @@ struct __align__(16) Ctrl {
 };
 constexpr int kCtrlBytes = 9 << 10;
 static_assert(sizeof(Ctrl) <= kCtrlBytes, "Ctrl must fit behind the tiles");
+constexpr int kJoinRow = 36;  // floats: 32 channels of a row, and four so that rows start in different banks
+constexpr int kJoinBytes = 4 * 32 * kJoinRow * 4;
 template <int kD>
 constexpr int kSmemBytes = 2 * Shape<kD>::kQBytes + Shape<kD>::kKStages * Shape<kD>::kCodeBytes + Shape<kD>::kVStages * Shape<kD>::kVBytes +
-                           kTeams * Shape<kD>::kCodeBytes + kCtrlBytes;  // the base must be 1024-aligned
+                           kTeams * Shape<kD>::kCodeBytes + kJoinBytes + kCtrlBytes;  // the base must be 1024-aligned
 static_assert(kInfos - Shape<64>::kKStages >= 6 && kInfos - Shape<128>::kKStages >= 6, "see kInfos");
 // A converter at position r of a ring has filled position r - kTeams, whose stage position r - kTeams - stages had been released from.  Releases are in
 // order, so with no more teams than stages the release before the one it waits for has happened, and the parity of the barrier means what it
@@ -291,12 +294,16 @@ __device__ __noinline__ bool rescale_rows(uint32_t o_addr, float alpha, uint64_t
   return true;
 }
 
+// Which of the 16 keys of a half-tile's page have a row of V that stands for NaN.
+__device__ __forceinline__ uint32_t nan_keys(const uint8_t *nan4, int page) {
+  const uint32_t w = *reinterpret_cast<const volatile uint32_t *>(nan4 + 4 * page);  // a byte of it: four keys
+  return (w & 15u) | ((w >> 4) & 0xF0u) | ((w >> 8) & 0xF00u) | ((w >> 12) & 0xF000u);
+}
 // Whether the row sees a key of the half-tile whose row of V stands for NaN.  pages: null where it sees all keys.
 __device__ __noinline__ bool sees_nan(const uint8_t *nan4, const TcPage *pages, RowInfo ri) {
   bool seen = false;
   for (int p = 0; p < kPagesPerTile / 2; ++p) {
-    const uint32_t w = *reinterpret_cast<const volatile uint32_t *>(nan4 + 4 * p);  // a byte of it: four keys
-    const uint32_t keys = (w & 15u) | ((w >> 4) & 0xF0u) | ((w >> 8) & 0xF00u) | ((w >> 12) & 0xF000u);
+    const uint32_t keys = nan_keys(nan4, p);
     const int n = pages != nullptr ? page_n_ok(pages[p].meta, ri) : kPage;
     seen = seen || (keys & ((1u << n) - 1u)) != 0u;
   }
@@ -412,6 +419,85 @@ __device__ __noinline__ void store_rows(uint32_t o_addr, uint32_t o_other, int s
   }
 }
 
+// The end of a piece whose keys the four warps of a stream have shared: row `lane` of each holds the sums over its keys (and those of stream 1).  Called by stream 0's
+// warps.  m, l: the row's reference exponent and sum in this warp, joined with stream 1's.
+template <int kD>
+__device__ __noinline__ bool join_rows(uint32_t o_addr, uint32_t o_other, int slot, float self, float other, bool other_live, float m, float l, int quarter, int64_t q_index,
+                                       uint32_t &joins, uint16_t *__restrict__ out, float *__restrict__ lse, float *__restrict__ partial_o, float *__restrict__ partial_ml) {
+  Ctrl *ctrl = ctrl_at<kD>();
+  const int lane = threadIdx.x & 31;
+  float *part = reinterpret_cast<float *>(reinterpret_cast<unsigned char *>(ctrl) - kJoinBytes);
+  const bool any_other = __any_sync(0xFFFFFFFFu, other_live);
+  // (a thread's own entries of these have been read by then: stream 1's)
+  ctrl->xch_m[quarter * 32 + lane] = m;
+  ctrl->xch_l[quarter * 32 + lane] = l;
+  mbar_arrive(&ctrl->join);
+  if (!wait<kD, 2>(&ctrl->join, joins++ & 1u, 249)) return false;
+  float m_all = -INFINITY, l_all = 0.f;
+#pragma unroll
+  for (int k = 0; k < 4; ++k) m_all = fmaxf(m_all, ctrl->xch_m[k * 32 + lane]);
+#pragma unroll
+  for (int k = 0; k < 4; ++k)
+    if (ctrl->xch_l[k * 32 + lane] != 0.f) l_all += ex2(ctrl->xch_m[k * 32 + lane] - m_all) * ctrl->xch_l[k * 32 + lane];  // (a warp that saw no key of the row has a sum of 0)
+  const float by = l != 0.f ? ex2(m - m_all) * (slot < 0 ? 1.0f / l_all : 1.0f) : 0.f;
+  self = l != 0.f ? self * by : 0.f;
+  other = l != 0.f ? other * by : 0.f;
+  const int row = quarter * 8 + lane / 4, c = (lane % 4) * 8;  // what this thread adds up
+  const int64_t row_index = __shfl_sync(0xFFFFFFFFu, q_index, row);
+#pragma unroll 1
+  for (int ch = 0; ch < kD / 32; ++ch) {
+    uint32_t o[32];
+    tmem_ld32(o_addr + ch * 32, o);
+    tc_wait_ld();
+#pragma unroll
+    for (int i = 0; i < 32; ++i) o[i] = __float_as_uint(self != 0.f ? bits_f(o[i]) * self : 0.f);
+    if (any_other) {
+      uint32_t p[32];
+      tmem_ld32(o_other + ch * 32, p);
+      tc_wait_ld();
+      if (other_live) {
+#pragma unroll
+        for (int i = 0; i < 32; ++i) o[i] = __float_as_uint(fmaf(bits_f(p[i]), other, bits_f(o[i])));
+      }
+    }
+    float4 *mine = reinterpret_cast<float4 *>(part + (quarter * 32 + lane) * kJoinRow);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) mine[i] = make_float4(bits_f(o[4 * i]), bits_f(o[4 * i + 1]), bits_f(o[4 * i + 2]), bits_f(o[4 * i + 3]));
+    mbar_arrive(&ctrl->join);
+    if (!wait<kD, 2>(&ctrl->join, joins++ & 1u, 249)) return false;
+    float t[8];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const float4 *from = reinterpret_cast<const float4 *>(part + (k * 32 + row) * kJoinRow + c);
+      const float4 a = from[0], b = from[1];
+      const float x[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+#pragma unroll
+      for (int i = 0; i < 8; ++i) t[i] = k == 0 ? x[i] : t[i] + x[i];
+    }
+    if (row_index >= 0) {
+      if (slot < 0) {
+        *reinterpret_cast<uint4 *>(out + row_index * kD + ch * 32 + c) =
+            make_uint4(pack_bf16(t[0], t[1]), pack_bf16(t[2], t[3]), pack_bf16(t[4], t[5]), pack_bf16(t[6], t[7]));
+      } else {
+        float4 *dst = reinterpret_cast<float4 *>(partial_o) + ((int64_t)slot * (kD / 4) + ch * 8 + c / 4) * 128 + row;
+        dst[0] = make_float4(t[0], t[1], t[2], t[3]);
+        dst[128] = make_float4(t[4], t[5], t[6], t[7]);
+      }
+    }
+    mbar_arrive(&ctrl->join);  // before the next channels take the place of these
+    if (!wait<kD, 2>(&ctrl->join, joins++ & 1u, 249)) return false;
+  }
+  if (quarter == 0 && q_index >= 0) {
+    if (slot >= 0) {
+      const bool nan = l_all != l_all;  // as in store_rows
+      *reinterpret_cast<float2 *>(partial_ml + ((int64_t)slot * 128 + lane) * 2) = nan ? make_float2(l_all, 1.0f) : make_float2(m_all, l_all);
+    } else if (lse != nullptr) {
+      lse[q_index] = (m_all + log2f(l_all)) * 0.6931471805599453f;
+    }
+  }
+  return true;
+}
+
 struct Fp8Pools {  // K's codes are behind a tensor map
   const uint8_t *v, *k_scale, *v_scale;
 };
@@ -487,6 +573,7 @@ attn_fp8_kernel(const __grid_constant__ CUtensorMap k_map, DevBatch d, DevTcPlan
     }
     mbar_init(&ctrl->epi_done, 256);
     mbar_init(&ctrl->xch, 128);
+    mbar_init(&ctrl->join, 128);
     for (int i = 0; i < kInfos; ++i) mbar_init(&ctrl->info_full[i], 1);
     ctrl->abort_flag = 0;
     ctrl->wait_limit_ns = (uint64_t)tc.wait_limit_us * 1000ull;
@@ -799,6 +886,7 @@ attn_fp8_kernel(const __grid_constant__ CUtensorMap k_map, DevBatch d, DevTcPlan
     const uint32_t s_addr = lane_base + s * 128, o_addr = lane_base + 256 + s * 128;
     uint32_t s_cnt = 0, o_cnt = 0;  // tiles / half-units of this stream so far
     uint32_t x_cnt = 0;             // pieces so far in which the two streams were combined
+    uint32_t joins = 0;             // phases of ctrl->join so far
     uint32_t tiles = 0;             // tiles of both streams so far
     bool ok = true;
     for (int pc = piece0; pc < piece1; ++pc) {
@@ -806,7 +894,8 @@ attn_fp8_kernel(const __grid_constant__ CUtensorMap k_map, DevBatch d, DevTcPlan
       const TcReq rq = pc == piece0 ? head->first_req : tc.reqs[pi.req];
       const int n = pi.tile_end - pi.tile_begin, mode = pi.n_mt;
       const int my_units = mode == 2 ? n : (n - s + 1) / 2;
-      const RowInfo ri = row_info(d, tc, rq, T, mode == 2 ? pi.mtile0 + s : pi.mtile0, r, pi.kv_head);
+      const bool split = mode == 1 && n >= 2 && min(T, rq.n_q - pi.mtile0 * T) * d.group <= 32;
+      const RowInfo ri = row_info(d, tc, rq, T, mode == 2 ? pi.mtile0 + s : pi.mtile0, split ? lane : r, pi.kv_head);
       float sc_row = 0.f;
       if (ok) {
         // the queries, once the products of the piece before no longer read the buffers; of one M-tile each stream takes half of every warp's rows.
@@ -829,7 +918,110 @@ attn_fp8_kernel(const __grid_constant__ CUtensorMap k_map, DevBatch d, DevTcPlan
         // A warp whose 32 rows are all padding only keeps the barriers' counts: what it leaves as weights multiplies into rows
         // of O that nobody reads.
         const bool idle = __all_sync(0xFFFFFFFFu, ri.q_index < 0);
-        if (idle) {
+        if (split) {  // as below, for the warp's 16 keys of a half-tile
+#pragma unroll 1
+          for (int u = 0; u < 2 * my_units; ++u) {
+            const int j = u >> 1, half = u & 1, local = 2 * j + s, t = pi.tile_begin + local;
+            const uint32_t sh_addr = s_addr + half * 64, at = (tiles + (uint32_t)local) * 2u + half, info = smem_u32(&ctrl->info[at % kInfos]), g = o_cnt + (uint32_t)u;
+            if (!s_ready) {
+              ok = wait<kD, 0>(&ctrl->s_full[s][half], (s_cnt + (uint32_t)j) & 1u, 230 + s) && wait<kD, 0>(&ctrl->info_full[at % kInfos], (at / kInfos) & 1u, 248);
+              if (!ok) break;
+            }
+            tc_fence_after();
+            uint32_t v[16];
+            tmem_ld16(sh_addr + quarter * 16, v);
+            const int2 of_v = ld_shared_i2(info + 256);
+            const int n_ok = t >= rq.n_dense_tiles ? page_n_ok(__ldg(&tc.pages[rq.page_off + t * kPagesPerTile + half * 4 + quarter].meta), ri) : kPage;
+            float alpha = 1.0f;
+            bool moved = false;
+            if (u == 0) base = of_v.x + 1;
+            if (of_v.x > base + kRise) {
+              alpha = pow2(base - (of_v.x + 1));
+              base = of_v.x + 1;
+              moved = true;
+            }
+            const int off = of_v.x - base;
+            bool apart = off < -kApart;
+            float bias = apart ? 0.f : (float)off + kHead, neg = m_used == -INFINITY ? 0.f : bias - m_used;
+            tc_wait_ld();
+            const uint32_t next = at + (half == 0 ? 1u : 3u);
+            const uint32_t next_ready =
+                mbar_test_wait2(&ctrl->s_full[s][half ^ 1], (s_cnt + (uint32_t)(j + half)) & 1u, &ctrl->info_full[next % kInfos], (next / kInfos) & 1u) == 3u;
+#pragma unroll
+            for (int i = 0; i < 16; i += 4) {
+              const float4 ks = ld_shared_f4(info + quarter * 64 + i * 4);
+              const float2 row = make_float2(sc_row, sc_row), n2 = make_float2(neg, neg);
+              const float2 t0 = ffma2(make_float2(bits_f(v[i]), bits_f(v[i + 1])), fmul2(make_float2(ks.x, ks.y), row), n2);
+              const float2 t1 = ffma2(make_float2(bits_f(v[i + 2]), bits_f(v[i + 3])), fmul2(make_float2(ks.z, ks.w), row), n2);
+              v[i] = __float_as_uint(n_ok > i ? t0.x : -INFINITY);
+              v[i + 1] = __float_as_uint(n_ok > i + 1 ? t0.y : -INFINITY);
+              v[i + 2] = __float_as_uint(n_ok > i + 2 ? t1.x : -INFINITY);
+              v[i + 3] = __float_as_uint(n_ok > i + 3 ? t1.y : -INFINITY);
+            }
+            const uint32_t none[8] = {0, 0, 0, 0, 0, 0, 0, 0};  // the other warps' keys
+#pragma unroll
+            for (int k = 1; k < 4; ++k) tmem_st8(sh_addr + ((quarter + k) & 3) * 8, none);
+            for (;;) {
+              float t_max = max3(bits_f(v[0]), bits_f(v[1]), bits_f(v[2])), sum = 0.f;
+              uint32_t pk[8];
+#pragma unroll
+              for (int i = 3; i < 15; i += 2) t_max = max3(t_max, bits_f(v[i]), bits_f(v[i + 1]));
+              t_max = fmaxf(t_max, bits_f(v[15]));
+              float2 acc = make_float2(0.f, 0.f);
+#pragma unroll
+              for (int i = 0; i < 16; i += 2) {
+                const float2 y = make_float2(ex2(bits_f(v[i])), ex2(bits_f(v[i + 1])));
+                acc = fadd2(acc, y);
+                pk[i >> 1] = pack_f16(y.x, y.y);
+              }
+              sum = acc.x + acc.y;
+              tmem_st8(sh_addr + quarter * 8, pk);
+              const bool grow = t_max > kGrow + bias || (m_used == -INFINITY && t_max > -INFINITY);
+              const bool grows = __any_sync(0xFFFFFFFFu, grow);
+              if (!grows && !apart) {
+                if (off >= -kApart) l = fmaf(sum, pow2(-off - (int)kHead), l);
+                break;
+              }
+              float down_by = 0.f, up_by = 0.f;
+              if (grows) {
+                if (grow) {
+                  const float to = t_max - neg + kLift;
+                  if (m_used > -INFINITY) {
+                    const float down = ex2(m_used - to);
+                    alpha *= down;
+                    l *= down;
+                  }
+                  m_used = to;
+                  down_by = t_max;
+                  up_by = bias - kLift;
+                }
+                moved = u != 0;
+              } else {
+                l += sum;
+                apart = false;
+                up_by = (float)off + kHead;
+                bias = up_by;
+              }
+#pragma unroll
+              for (int i = 0; i < 16; ++i) v[i] = __float_as_uint((bits_f(v[i]) - down_by) + up_by);
+              tc_wait_st();
+            }
+            if (moved) {
+              ok = rescale_rows<kD>(o_addr, alpha, &ctrl->o_done[s], g, 235 + s);
+              if (!ok) break;
+            }
+            tc_wait_st();
+            tc_fence_before();
+            s_ready = __all_sync(0xFFFFFFFFu, next_ready) != 0;
+            if (u + 1 == 2 * my_units) {
+              ok = wait<kD, 0>(&ctrl->o_done[s], (g - 1) & 1u, 237 + s);
+              if (!ok) break;
+            }
+            if (of_v.y) nan_v = nan_v || (nan_keys(ctrl->info[at % kInfos].nan4, quarter) & ((1u << n_ok) - 1u)) != 0u;
+            mbar_arrive(&ctrl->p_full[s][half]);
+          }
+          s_cnt += (uint32_t)my_units;
+        } else if (idle) {
           for (int u = 0; u < 2 * my_units && ok; ++u) {
             ok = wait<kD, 0>(&ctrl->s_full[s][u & 1], (s_cnt + (uint32_t)(u >> 1)) & 1u, 230 + s);
             if (ok && u + 1 == 2 * my_units) ok = wait<kD, 0>(&ctrl->o_done[s], (o_cnt + (uint32_t)u - 1) & 1u, 237 + s);
@@ -838,7 +1030,7 @@ attn_fp8_kernel(const __grid_constant__ CUtensorMap k_map, DevBatch d, DevTcPlan
           s_cnt += (uint32_t)my_units;
         }
 #pragma unroll 1
-        for (int j = 0; j < my_units && ok && !idle; ++j) {
+        for (int j = 0; j < my_units && ok && !idle && !split; ++j) {
           const int local = mode == 2 ? j : 2 * j + s, t = pi.tile_begin + local;
           const TcPage *pages = t >= rq.n_dense_tiles ? tc.pages + rq.page_off + t * kPagesPerTile : nullptr;
 #pragma unroll 1  // one copy of the sweep: the unrolled pair is slower (instruction fetch)
@@ -985,7 +1177,11 @@ attn_fp8_kernel(const __grid_constant__ CUtensorMap k_map, DevBatch d, DevTcPlan
           }
         }
         if (pair) ++x_cnt;
-        if (ok && writer && !idle) {
+        if (ok && writer && split) {
+          tc_fence_after();
+          ok = join_rows<kD>(o_addr, lane_base + 256 + 128, pi.slot[0], self, other, other_live, m_out, l_out, quarter, ri.q_index, joins, out, lse, tc.partial_o, tc.partial_ml);
+          tc_fence_before();
+        } else if (ok && writer && !idle) {
           tc_fence_after();
           store_rows<kD>(o_addr, lane_base + 256 + (1 - s) * 128, pi.slot[pair ? 0 : s], self, other, other_live, m_out, l_out, r, ri.q_index, out, lse,
                          tc.partial_o, tc.partial_ml);

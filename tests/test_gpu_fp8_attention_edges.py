@@ -54,10 +54,52 @@ def compare(w, pools, path):
     assert np.abs(lse.cpu().numpy() - l_ref).max() <= LSE_ABS
 
 
+# ---- queries that fit the rows of one warp: its four neighbours share the keys -----------------------------------------------
+def few_rows(d, hq, h, q, seed, n_req=10):
+    """Requests whose pieces have several tiles each, with one, a few and the most rows there may be; some with draft steps of their own."""
+    rng = np.random.default_rng(seed)
+    reqs = []
+    for i in range(n_req):
+        p = int(rng.integers(300, 2400))
+        reqs.append({"P": p, "segs": [], "branches": [(0, q, q, q)]} if i % 2 else {"P": p, "segs": [21], "branches": [(0, max(q - 1, 1), max(q - 1, 1), 1), (1, 1, 1, 1)]})
+    return _finish("few", 11, Model(hq, h, d, 16), reqs, rng, 0.3, 0.6, False, True, "nan")
+
+
+@pytest.mark.parametrize("d,hq,h,q", [(64, 8, 8, 1), (64, 32, 8, 8), (128, 8, 8, 1), (128, 40, 8, 6), (128, 16, 2, 4), (128, 32, 8, 9)])
+def test_few_rows_over_many_tiles(d, hq, h, q):
+    check(few_rows(d, hq, h, q, d + q), B.PATH_TENSOR_CORE, REL_LARGE)
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("how", ["rising", "falling", "steps", "any", "half zeros"])
+def test_few_rows_over_values_of_very_different_sizes(how, d):
+    w = few_rows(d, 8, 4, 2, 21, n_req=4)
+    t, at = w.tensors, tokens(w.batch)
+    v = bf16_to_f32(t.v_pool)
+    with np.errstate(all="ignore"):
+        v[at[:, 0], :, at[:, 1]] *= np.exp2(np.round(SIZES[how](len(at), np.random.default_rng(1)))).astype(np.float32)[:, None, None]
+        t.v_pool[:] = bf16_round(v)
+    compare(w, store_pools(t.k_pool, t.v_pool), B.PATH_TENSOR_CORE)
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("how", ["rising", "falling", "steps", "any", "late"])
+def test_few_rows_over_scores_that_grow_fall_and_jump(how, d):
+    w = few_rows(d, 8, 4, 2, 22, n_req=4)
+    b, t, rng = w.batch, w.tensors, np.random.default_rng(23)
+    at = tokens(b)
+    axis, k = rng.choice([-1.0, 1.0], d), bf16_to_f32(t.k_pool)
+    want = SCORES[how](len(at), rng)
+    k[at[:, 0], :, at[:, 1]] = (0.2 * rng.standard_normal((len(at), b.model.n_kv_heads, d)) + (want / np.sqrt(d))[:, None, None] * axis).astype(np.float32)
+    t.k_pool[:] = bf16_round(k)
+    t.q[:] = bf16_round((axis + 0.2 * rng.standard_normal(t.q.shape)).astype(np.float32))
+    compare(w, store_pools(t.k_pool, t.v_pool), B.PATH_TENSOR_CORE)
+
+
 # ---- rows that stand for NaN -------------------------------------------------------------------------------------------------
 @pytest.mark.parametrize("path", PATHS)
 @pytest.mark.parametrize("which", ["k", "v"])
-@pytest.mark.parametrize("make", [lambda: make_random_small(9001), lambda: make_random_tree(9104), lambda: chain([300, 1, 640]), lambda: chain([129, 2000], 64),
+@pytest.mark.parametrize("make", [lambda: make_random_small(9001), lambda: make_random_tree(9104), lambda: chain([300, 1, 640]), lambda: chain([129, 2000], 64), lambda: few_rows(128, 8, 8, 2, 24, n_req=6), lambda: few_rows(64, 8, 8, 2, 25, n_req=6),
                                   lambda: make_tree(2, 2, size="tiny", with_logits=False)])
 def test_rows_that_stand_for_nan_reach_those_who_see_them(make, which, path):
     w = make()
