@@ -524,7 +524,8 @@ __device__ __forceinline__ void halves4(uint32_t c, uint32_t by, uint32_t &lo, u
       : "r"(c), "r"(by));
 }
 
-template <int kD>
+// kFew: some piece has few enough rows to share its keys among the warps; the code for that costs the other pieces 2 % (instruction fetch)
+template <int kD, bool kFew>
 __global__ void __launch_bounds__(kThreads, 1)
 attn_fp8_kernel(const __grid_constant__ CUtensorMap k_map, DevBatch d, DevTcPlan tc, const uint16_t *__restrict__ q, Fp8Pools in, uint16_t *__restrict__ out, float *__restrict__ lse,
                 float scale_log2) {
@@ -894,7 +895,7 @@ attn_fp8_kernel(const __grid_constant__ CUtensorMap k_map, DevBatch d, DevTcPlan
       const TcReq rq = pc == piece0 ? head->first_req : tc.reqs[pi.req];
       const int n = pi.tile_end - pi.tile_begin, mode = pi.n_mt;
       const int my_units = mode == 2 ? n : (n - s + 1) / 2;
-      const bool split = mode == 1 && n >= 2 && min(T, rq.n_q - pi.mtile0 * T) * d.group <= 32;
+      const bool split = kFew && shares_keys(pi, rq, T, d.group);
       const RowInfo ri = row_info(d, tc, rq, T, mode == 2 ? pi.mtile0 + s : pi.mtile0, split ? lane : r, pi.kv_head);
       float sc_row = 0.f;
       if (ok) {
@@ -918,7 +919,7 @@ attn_fp8_kernel(const __grid_constant__ CUtensorMap k_map, DevBatch d, DevTcPlan
         // A warp whose 32 rows are all padding only keeps the barriers' counts: what it leaves as weights multiplies into rows
         // of O that nobody reads.
         const bool idle = __all_sync(0xFFFFFFFFu, ri.q_index < 0);
-        if (split) {  // as below, for the warp's 16 keys of a half-tile
+        if (kFew && split) {  // as below, for the warp's 16 keys of a half-tile
 #pragma unroll 1
           for (int u = 0; u < 2 * my_units; ++u) {
             const int j = u >> 1, half = u & 1, local = 2 * j + s, t = pi.tile_begin + local;
@@ -1177,7 +1178,7 @@ attn_fp8_kernel(const __grid_constant__ CUtensorMap k_map, DevBatch d, DevTcPlan
           }
         }
         if (pair) ++x_cnt;
-        if (ok && writer && split) {
+        if (kFew && ok && writer && split) {
           tc_fence_after();
           ok = join_rows<kD>(o_addr, lane_base + 256 + 128, pi.slot[0], self, other, other_live, m_out, l_out, quarter, ri.q_index, joins, out, lse, tc.partial_o, tc.partial_ml);
           tc_fence_before();
@@ -1244,7 +1245,7 @@ template <int kD>
 int launch(lr_plan *p, const CUtensorMap &k_map, const uint16_t *q, const Fp8Pools &in, uint16_t *out, float *lse, float scale_log2, cudaStream_t s) {
   const DevTcPlan &tc = p->tc;
   p->ctx->launches++;
-  if (int rc = cuda_fail(launch_dependent(attn_fp8_kernel<kD>, dim3((unsigned)tc.n_cta), dim3(kThreads), kSmemBytes<kD>, s, k_map, p->dev, tc, q, in, out,
+  if (int rc = cuda_fail(launch_dependent(p->tc_few_rows ? attn_fp8_kernel<kD, true> : attn_fp8_kernel<kD, false>, dim3((unsigned)tc.n_cta), dim3(kThreads), kSmemBytes<kD>, s, k_map, p->dev, tc, q, in, out,
                                           lse, scale_log2),
                          "attn_fp8_kernel launch"))
     return rc;
@@ -1258,11 +1259,11 @@ int launch(lr_plan *p, const CUtensorMap &k_map, const uint16_t *q, const Fp8Poo
 }  // namespace
 
 int init_attn_fp8_kernel() {
-  if (int rc = cuda_fail(cudaFuncSetAttribute(attn_fp8_kernel<128>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemBytes<128>),
-                         "attn_fp8_kernel<128> shared-memory attribute"))
-    return rc;
-  return cuda_fail(cudaFuncSetAttribute(attn_fp8_kernel<64>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemBytes<64>),
-                   "attn_fp8_kernel<64> shared-memory attribute");
+  cudaError_t e = cudaFuncSetAttribute(attn_fp8_kernel<128, false>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemBytes<128>);
+  if (e == cudaSuccess) e = cudaFuncSetAttribute(attn_fp8_kernel<128, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemBytes<128>);
+  if (e == cudaSuccess) e = cudaFuncSetAttribute(attn_fp8_kernel<64, false>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemBytes<64>);
+  if (e == cudaSuccess) e = cudaFuncSetAttribute(attn_fp8_kernel<64, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemBytes<64>);
+  return cuda_fail(e, "attn_fp8_kernel shared-memory attribute");
 }
 
 int launch_attn_fp8(lr_plan *p, const void *q, const lr_fp8_cache &c, void *out, float *lse, float scale, cudaStream_t s) {

@@ -1315,6 +1315,8 @@ void tc_plan_tables(const lr_batch *b, const int32_t *req_br_off, const int32_t 
 
 void tc_bind_device_plan(const TcHostPlan &h, unsigned char *image_base, unsigned char *scratch_base, lr_plan *p) {
   p->tc_ok = h.ok;
+  p->tc_few_rows = false;
+  for (const TcPiece &pi : h.all.pieces) p->tc_few_rows |= shares_keys(pi, h.lists[pi.req].rq, h.tokens_per_mtile, p->dev.group);
   p->tc_pieces = (int)h.all.pieces.size();
   p->o_tc_pages = h.o_pages;
   p->o_tc_heads[0] = h.all.o_heads;

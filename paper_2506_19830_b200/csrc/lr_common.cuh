@@ -80,6 +80,11 @@ struct TcReq {           // one page list: what one group of M-tiles of a reques
   int32_t n_dense_tiles;  // leading tiles made only of full prefix pages (no masking needed)
   int32_t pad[3];
 };
+// Whether a piece's queries fit the rows of one warp: the 8-bit kernel then has them in all four of a stream's, which share the keys.
+__host__ __device__ inline bool shares_keys(const TcPiece &p, const TcReq &rq, int tokens_per_mtile, int group) {
+  const int left = rq.n_q - p.mtile0 * tokens_per_mtile;
+  return p.n_mt == 1 && p.tile_end - p.tile_begin >= 2 && (left < tokens_per_mtile ? left : tokens_per_mtile) * group <= 32;
+}
 struct TcTarget {
   int32_t req, kv_head, mtile;
   int32_t slot_begin, n_slots;  // partial slots to merge (n_slots >= 2)
@@ -181,6 +186,7 @@ struct lr_plan {
   lr::SmallPass small;
   lr::DevPairPlan pr;
   bool tc_ok;             // shape allows the tensor-core path
+  bool tc_few_rows;       // some piece of it shares_keys
   // The CTA-pair plan is built and uploaded when its path is first selected.  Its tables have a part of the workspace to
   // themselves, so that launches that were captured or queued find them whatever has run since; partial results share
   // theirs with the single-CTA path's (the two never run at the same time).
