@@ -2,7 +2,8 @@
 
 Host bookkeeping only -- which physical pages a request owns, a free list, where new tokens go -- around the
 library calls that do the work: ``lr_plan_create``, ``lr_verify_attention``, ``lr_accept_greedy``, ``lr_commit``
-and ``lr_compact``.  The models are not here: the caller hands in, per cycle, the K/V of the drafted steps and of
+and ``lr_compact``, or, with the cache in 8 bits, ``lr_fp8_write``, ``lr_verify_attention_fp8``, ``lr_compact_fp8`` and ``lr_fp8_read``; drafts that a
+model sampled are accepted by ``lr_accept_sample_drafted``.  The models are not here: the caller hands in, per cycle, the K/V of the drafted steps and of
 every branch's tail, the queries, the logits and the step verdicts, as a serving engine would after running its
 draft model, target model and verifier.
 
@@ -13,7 +14,7 @@ prefix span needs.
 from __future__ import annotations
 
 from dataclasses import dataclass
-from typing import List, Sequence, Tuple
+from typing import List, Optional, Sequence, Tuple
 
 import numpy as np
 import torch
@@ -40,6 +41,16 @@ class RequestInput:
     parents: Sequence[int] = ()  # multi-branch drafting: the step each draft step continues (0 = prefix); empty = chain
 
 
+@dataclass
+class SampledDrafts:
+    """What a cycle's acceptance needs when a draft model sampled the drafts: its rows, and a uniform number a draft and a branch."""
+    logits: np.ndarray  # uint16 [sum n_draft, vocab] bf16 bits: row i is what draft i was drawn from
+    temperature: float
+    draft_temperature: float
+    u_accept: np.ndarray  # [sum n_draft]
+    u_final: np.ndarray  # [n_branch]
+
+
 class _HostBatch:
     """The fields ``binding.HostBatch`` reads."""
 
@@ -49,12 +60,19 @@ class _HostBatch:
 
 
 class PagedCycleEngine:
-    def __init__(self, model, n_pool_pages: int, device: str = "cuda:0"):
-        self.model, self.device = model, device
+    def __init__(self, model, n_pool_pages: int, device: str = "cuda:0", kv_dtype: str = "bf16"):
+        """kv_dtype: "bf16", or "fp8" for a cache of half the size (e4m3 codes, a power of two a row)."""
+        if kv_dtype not in ("bf16", "fp8"):
+            raise ValueError(f"kv_dtype is 'bf16' or 'fp8', not {kv_dtype!r}")
+        self.model, self.device, self.n_pool_pages = model, device, n_pool_pages
         self.ctx = B.Context(model, torch.device(device).index or 0)
-        shape = (n_pool_pages, model.n_kv_heads, PAGE, model.head_dim)
-        self.k_pool = torch.zeros(shape, dtype=torch.bfloat16, device=device)
-        self.v_pool = torch.zeros(shape, dtype=torch.bfloat16, device=device)
+        self.cache: Optional[B.Fp8Cache] = None
+        if kv_dtype == "fp8":
+            self.cache = B.Fp8Cache.empty(model, n_pool_pages, torch.device("cuda", self.ctx.device))
+        else:
+            shape = (n_pool_pages, model.n_kv_heads, PAGE, model.head_dim)
+            self.k_pool = torch.zeros(shape, dtype=torch.bfloat16, device=device)
+            self.v_pool = torch.zeros(shape, dtype=torch.bfloat16, device=device)
         self.free: List[int] = list(range(n_pool_pages - 1, -1, -1))  # a stack: pop() hands out the lowest first
         self.pages: List[List[int]] = []
         self.length: List[int] = []
@@ -71,10 +89,16 @@ class PagedCycleEngine:
         n = len(k_bits)
         if n == 0:
             return
+        if self.cache is not None:
+            self.ctx.lr_fp8_write(self.cache, R.bf16_tensor(k_bits, self.device), R.bf16_tensor(v_bits, self.device), self._slots(pages, n))
+            return
         idx_page = torch.tensor([pages[t // PAGE] for t in range(n)], device=self.device)
         idx_slot = torch.arange(n, device=self.device) % PAGE
         self.k_pool[idx_page, :, idx_slot, :] = R.bf16_tensor(k_bits, self.device)
         self.v_pool[idx_page, :, idx_slot, :] = R.bf16_tensor(v_bits, self.device)
+
+    def _slots(self, pages: List[int], n: int) -> torch.Tensor:
+        return torch.tensor([pages[t // PAGE] * PAGE + t % PAGE for t in range(n)], dtype=torch.int64, device=self.device)
 
     def add_request(self, k_bits: np.ndarray, v_bits: np.ndarray) -> int:
         """A new request whose context so far is the given tokens; returns its index."""
@@ -85,17 +109,23 @@ class PagedCycleEngine:
         return len(self.pages) - 1
 
     def sequence(self, r: int) -> Tuple[np.ndarray, np.ndarray]:
-        """The committed tokens of request r, gathered from its pages: two uint16 arrays [length, H_kv, D]."""
+        """The committed tokens of request r, gathered from its pages: two uint16 arrays [length, H_kv, D] (of an 8-bit cache: the values its rows
+        stand for)."""
         n = self.length[r]
+        if self.cache is not None:
+            k, v = (torch.empty((n, self.model.n_kv_heads, self.model.head_dim), dtype=torch.bfloat16, device=self.device) for _ in range(2))
+            self.ctx.lr_fp8_read(self.cache, self._slots(self.pages[r], n), k, v)
+            return R.bf16_bits(k), R.bf16_bits(v)
         idx_page = torch.tensor([self.pages[r][t // PAGE] for t in range(n)], device=self.device, dtype=torch.long)
         idx_slot = torch.arange(n, device=self.device) % PAGE
         return R.bf16_bits(self.k_pool[idx_page, :, idx_slot, :]), R.bf16_bits(self.v_pool[idx_page, :, idx_slot, :])
 
     # ---- one cycle ------------------------------------------------------------------------------------------
     def run_cycle(self, reqs: Sequence[RequestInput], q_bits: np.ndarray, logits_bits: np.ndarray, draft_ids: np.ndarray,
-                  verdict: np.ndarray) -> dict:
+                  verdict: np.ndarray, sampled: Optional[SampledDrafts] = None) -> dict:
         """Verify, commit and compact one cycle for every request (``reqs[r]`` belongs to request r; queries, logits
-        rows, drafts and verdicts are packed in request, branch order as the C ABI wants them)."""
+        rows, drafts and verdicts are packed in request, branch order as the C ABI wants them).  Drafts are accepted greedily, or
+        against the draft model's own rows where `sampled` is given; "bonus_id" is then the token sampled behind the accepted ones."""
         assert len(reqs) == len(self.pages)
         page_ids: List[int] = []
         req_span_off, span_len, span_slot, seg_parent = [0], [], [], []
@@ -130,7 +160,7 @@ class PagedCycleEngine:
                 cu_q.append(cu_q[-1] + b.q_len)
         i32 = lambda a: np.asarray(a, dtype=np.int32)  # noqa: E731
         batch = _HostBatch(self.model, req_span_off=i32(req_span_off), span_len=i32(span_len), span_slot=i32(span_slot),
-                           cu_q=i32(cu_q), page_ids=i32(page_ids), n_pool_pages=self.k_pool.shape[0],
+                           cu_q=i32(cu_q), page_ids=i32(page_ids), n_pool_pages=self.n_pool_pages,
                            seg_parent=i32(seg_parent) if tree else None, **{k: i32(v) for k, v in br.items()})
         n_req, n_branch, n_slots = len(reqs), len(br["br_req"]), len(page_ids)
         plan = B.Plan(self.ctx, batch)
@@ -138,8 +168,13 @@ class PagedCycleEngine:
         q = R.bf16_tensor(q_bits, dev)
         vocab = logits_bits.shape[1]
         stride = (vocab + 7) // 8 * 8
-        logits = torch.zeros((logits_bits.shape[0], stride), dtype=torch.bfloat16, device=dev)
-        logits[:, :vocab] = R.bf16_tensor(logits_bits, dev)
+
+        def rows(bits: np.ndarray) -> torch.Tensor:
+            t = torch.zeros((bits.shape[0], stride), dtype=torch.bfloat16, device=dev)
+            t[:, :vocab] = R.bf16_tensor(bits, dev)
+            return t[:, :vocab]
+
+        logits = rows(logits_bits)
         cu_draft = torch.from_numpy(np.concatenate([[0], np.cumsum(br["br_n_draft"])]).astype(np.int32)).to(dev)
         out = torch.empty((cu_q[-1], self.model.n_q_heads, self.model.head_dim), dtype=torch.bfloat16, device=dev)
         n_accept, bonus = torch.empty(n_branch, **i32t), torch.empty(n_branch, **i32t)
@@ -148,12 +183,24 @@ class PagedCycleEngine:
         keep_pages, keep_valid, free_pages = (torch.empty(n_slots, **i32t) for _ in range(3))
         new_len, n_kept = torch.empty(n_req, **i32t), torch.empty(n_req, **i32t)
         v = verdict if len(verdict) else np.zeros(1, dtype=np.uint8)
-        plan.lr_verify_attention(q, self.k_pool, self.v_pool, out, None, 0.0, None)
-        self.ctx.lr_accept_greedy(logits[:, :vocab], torch.from_numpy(i32(draft_ids)).to(dev), cu_draft, n_accept, bonus,
-                                  B.Context.accept_scratch(logits_bits.shape[0], dev), None, None)
+        if self.cache is not None:
+            plan.lr_verify_attention_fp8(q, self.cache, out)
+        else:
+            plan.lr_verify_attention(q, self.k_pool, self.v_pool, out, None, 0.0, None)
+        drafts = torch.from_numpy(i32(draft_ids)).to(dev)
+        if sampled is not None:
+            f32 = lambda a: torch.from_numpy(np.ascontiguousarray(a, dtype=np.float32)).to(dev)  # noqa: E731
+            self.ctx.lr_accept_sample_drafted(logits, rows(sampled.logits), drafts, cu_draft, sampled.temperature, sampled.draft_temperature,
+                                              f32(sampled.u_accept), f32(sampled.u_final), n_accept, bonus,
+                                              self.ctx.accept_sample_drafted_scratch(logits_bits.shape[0]))
+        else:
+            self.ctx.lr_accept_greedy(logits, drafts, cu_draft, n_accept, bonus, B.Context.accept_scratch(logits_bits.shape[0], dev), None, None)
         plan.lr_commit(torch.from_numpy(np.ascontiguousarray(v, dtype=np.uint8)).to(dev), n_accept, steps, surv, clen,
                        keep_off, keep_pages, keep_valid, free_off, free_pages, None)
-        plan.lr_compact(keep_off, keep_pages, keep_valid, self.k_pool, self.v_pool, new_len, n_kept, plan.compact_scratch(), None)
+        if self.cache is not None:
+            plan.lr_compact_fp8(keep_off, keep_pages, keep_valid, self.cache, new_len, n_kept)
+        else:
+            plan.lr_compact(keep_off, keep_pages, keep_valid, self.k_pool, self.v_pool, new_len, n_kept, plan.compact_scratch(), None)
         status = plan.lr_poll_status()  # synchronises the stream
         if status != 0:
             raise RuntimeError(f"device status {status} after the cycle")
