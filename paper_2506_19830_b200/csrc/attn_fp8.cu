@@ -239,9 +239,9 @@ __device__ __forceinline__ uint4 ld_shared(uint32_t addr) {
   return v;
 }
 // (asm so that these stay where they are written, tiles ahead of their use)
-__device__ __forceinline__ uint32_t ld_word(const uint8_t *p) {
+__device__ __forceinline__ uint32_t ld_word(const uint8_t *p) {  // four scales, as ld_scale
   uint32_t v;
-  asm volatile("ld.global.nc.u32 %0, [%1];" : "=r"(v) : "l"(p));
+  asm volatile("ld.global.cg.u32 %0, [%1];" : "=r"(v) : "l"(p));
   return v;
 }
 __device__ __forceinline__ int2 ld_pair(const void *p) {

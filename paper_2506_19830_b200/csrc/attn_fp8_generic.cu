@@ -90,8 +90,8 @@ attn_fp8_generic_kernel(DevBatch d, const uint16_t *__restrict__ q, const uint8_
             a1 = fmaf(qq[4 * j + 3], y.y, a1);
           }
         }
-        s = (a0 + a1) * (fp8_scale(kscale[at]) * scale_log2);
-        vs = fp8_scale(vscale[at]);
+        s = (a0 + a1) * (fp8_scale(ld_scale(kscale + at)) * scale_log2);
+        vs = fp8_scale(ld_scale(vscale + at));
       }
       const float bm = warp_max(s);  // (a NaN score is not the largest: it comes back through the sum)
       const float m_new = fmaxf(m, bm);

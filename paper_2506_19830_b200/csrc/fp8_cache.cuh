@@ -16,6 +16,14 @@ __device__ __forceinline__ float fp8_scale(uint32_t byte) {
   return __uint_as_float(byte == kFp8NanScale ? 0x7FC00000u : byte == 0u ? 0x00400000u : byte << 23);
 }
 
+// A scale byte, from L2: a line of them holds those of other sequences' tokens too, so that a kernel on another stream may have brought it into this SM's L1 before
+// the kernel in front of this one wrote there.
+__device__ __forceinline__ uint32_t ld_scale(const uint8_t *p) {
+  uint32_t v;
+  asm volatile("ld.global.cg.u8 %0, [%1];" : "=r"(v) : "l"(p));
+  return v;
+}
+
 // two e4m3 codes (low byte first) as halves: exact
 __device__ __forceinline__ uint32_t fp8_half2(uint32_t two) {
   uint32_t h;
