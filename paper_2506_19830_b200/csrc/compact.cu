@@ -9,7 +9,7 @@
 // thousand integers, in L2 after the first reader); tokens in front of the first partly filled page stay where they are.
 //
 // The same sweep serves the 8-bit cache, whose rows have half the bytes: the CTA that owns the first columns of a head moves that
-// head's scale bytes too.
+// head's scale bytes too, each with its row (in rounds of their own, behind the rows' or in another CTA, 0.5 and 1.2 us more for 16 requests).
 //
 // Bytes moved: 2 (K, V) x H_kv x D x 2 B per displaced token, read and written once.  Bound by the chain of dependent
 // reads (list bounds, counts, page ids, data), not by bandwidth.  One launch; as three (scan, gather to a staging area,
@@ -29,14 +29,15 @@ constexpr int kScan = kThreads * kPerThread;   // pages per step
 constexpr int kRows = 8;                       // 16-byte vectors a thread holds per round
 
 // What a CTA moves at a time: rows of vec_per_row elements, of which it has 1 << shift from column c0 on.  Rounds of kThreads * kRows
-// elements, in token order, over the pages first .. n_here - 1 of a step.
-template <typename Vec>
-__device__ __forceinline__ void move_rounds(const DevBatch &d, Vec *pool, int vec_per_row, int shift, int c0, int h, const int32_t *__restrict__ keep_pages,
+// elements, in token order, over the pages first .. n_here - 1 of a step.  kScales: the thread of a row's first element takes its scale byte along.
+template <bool kScales>
+__device__ __forceinline__ void move_rounds(const DevBatch &d, uint4 *pool, uint8_t *scale, int vec_per_row, int shift, int c0, int h, const int32_t *__restrict__ keep_pages,
                                             const int32_t *s_off, int i0, int base, int first, int n_here) {
   const int tid = threadIdx.x;
   const int total = ((n_here - first) * kPage) << shift;
   for (int at = 0; at < total; at += kThreads * kRows) {
-    Vec v[kRows];
+    uint4 v[kRows];
+    uint8_t byte[kRows];
     int64_t to[kRows];
 #pragma unroll
     for (int u = 0; u < kRows; ++u) {
@@ -63,13 +64,18 @@ __device__ __forceinline__ void move_rounds(const DevBatch &d, Vec *pool, int ve
         d.status[1] = code;
         continue;
       }
-      v[u] = pool[((src_page * d.n_kv_heads + h) * kPage + t) * vec_per_row + c];
+      const int64_t from = (src_page * d.n_kv_heads + h) * kPage + t;
+      v[u] = pool[from * vec_per_row + c];
+      if (kScales && c == 0) byte[u] = scale[from];
       to[u] = ((dst_page * d.n_kv_heads + h) * kPage + k % kPage) * vec_per_row + c;
     }
     __syncthreads();  // the round is in registers
 #pragma unroll
     for (int u = 0; u < kRows; ++u)
-      if (to[u] >= 0) pool[to[u]] = v[u];
+      if (to[u] >= 0) {
+        pool[to[u]] = v[u];
+        if (kScales && (to[u] & (vec_per_row - 1)) == 0) scale[to[u] >> (31 - __clz(vec_per_row))] = byte[u];  // (4 or 8 to a row)
+      }
   }
 }
 
@@ -86,7 +92,9 @@ compact_kernel(DevBatch d, const int32_t *__restrict__ keep_off, const int32_t *
   const int r = blockIdx.y, tid = threadIdx.x, lane = tid & 31, wid = tid >> 5;
   const int vec_per_row = d.head_dim / (kScales ? 16 : 8), slices = vec_per_row >> shift;
   const int slice = blockIdx.x % slices, h = blockIdx.x / slices / sides;
-  uint4 *pool = blockIdx.x / slices % sides ? v_pool : k_pool;
+  const bool of_v = blockIdx.x / slices % sides != 0;
+  uint4 *pool = of_v ? v_pool : k_pool;
+  uint8_t *scale = of_v ? v_scale : k_scale;
   asm volatile("griddepcontrol.wait;" ::: "memory");  // the keep list comes from the kernel launched just before
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");  // the next layer's grid may be set up meanwhile
   const int i0 = keep_off[r], i1 = keep_off[r + 1];
@@ -142,9 +150,7 @@ compact_kernel(DevBatch d, const int32_t *__restrict__ keep_off, const int32_t *
       for (int w = 0; w < kThreads / 32; ++w) first = min(first, warp_first[w]);
     }
     moved = moved || first < n_here;
-    move_rounds(d, pool, vec_per_row, shift, slice << shift, h, keep_pages, s_off, i0, base, first, n_here);
-    if constexpr (kScales)
-      if (slice == 0) move_rounds(d, blockIdx.x / slices % sides ? v_scale : k_scale, 1, 0, 0, h, keep_pages, s_off, i0, base, first, n_here);
+    move_rounds<kScales>(d, pool, scale, vec_per_row, shift, slice << shift, h, keep_pages, s_off, i0, base, first, n_here);
     __syncthreads();  // s_off is free again
   }
   if (blockIdx.x == 0 && tid == 0) {
