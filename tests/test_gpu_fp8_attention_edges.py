@@ -421,3 +421,45 @@ def test_a_wait_that_runs_out_is_reported_and_the_context_stays_usable():
     check_attention(out, None, O.verify_attention(b, w.tensors.q, k, v)[0], None)
     plan.close()
     ctx.close()
+
+
+@pytest.mark.parametrize("path", PATHS)
+def test_a_cache_whose_bytes_pass_32_bits(path):
+    """The batch's pages lie in the last of 270,000: rows written, attended to, compacted and read there."""
+    w = chain([200, 37], seed=30)
+    b, t = w.batch, w.tensors
+    n, used = 270_000, int(b.n_pool_pages)
+    at = tokens(b)
+    k_rows, v_rows = (x[at[:, 0], :, at[:, 1]] for x in (t.k_pool, t.v_pool))
+    pools = store_pools(t.k_pool, t.v_pool)
+    k, v = as_bf16(pools[0], pools[2]), as_bf16(pools[1], pools[3])
+    o_ref, l_ref = O.verify_attention(b, t.q, k, v)
+    n_accept = np.asarray(b.br_n_draft, dtype=np.int32)
+    c = O.commit(b, t.verdict, n_accept)
+    want = O.compact(c["keep_off"], c["keep_pages"], c["keep_valid"], k, v)
+    b.page_ids = b.page_ids + (n - used)
+    b.n_pool_pages = n
+    ctx = B.Context(b.model, 0)
+    plan = B.Plan(ctx, b)
+    plan.lr_plan_set_attention_path(path)
+    cache = B.Fp8Cache.empty(b.model, n, DEV)
+    slots = torch.from_numpy((at[:, 0] + (n - used)) * 16 + at[:, 1]).to(DEV)
+    ctx.lr_fp8_write(cache, R.bf16_tensor(k_rows, DEV), R.bf16_tensor(v_rows, DEV), slots)
+    q = R.bf16_tensor(t.q, DEV)
+    out, lse = torch.zeros_like(q), torch.zeros(q.shape[:2], device=DEV)
+    plan.lr_verify_attention_fp8(q, cache, out, lse)
+    i32 = lambda a: torch.from_numpy(np.ascontiguousarray(a, dtype=np.int32)).to(DEV)  # noqa: E731
+    new_len, kept = (torch.zeros(b.n_req, dtype=torch.int32, device=DEV) for _ in range(2))
+    plan.lr_compact_fp8(i32(c["keep_off"]), i32(c["keep_pages"] + (n - used)), i32(c["keep_valid"]), cache, new_len, kept)
+    assert plan.lr_poll_status() == 0
+    check_attention(out, lse, o_ref, l_ref, None, REL_LARGE)
+    assert np.array_equal(new_len.cpu().numpy(), want[0]) and np.array_equal(kept.cpu().numpy(), want[1])
+    for r in range(b.n_req):
+        pages = c["keep_pages"][c["keep_off"][r]:c["keep_off"][r + 1]]
+        place = np.array([int(pages[i // 16]) * 16 + i % 16 for i in range(int(want[0][r]))], dtype=np.int64)
+        back = [torch.zeros((len(place), b.model.n_kv_heads, b.model.head_dim), dtype=torch.bfloat16, device=DEV) for _ in range(2)]
+        ctx.lr_fp8_read(cache, torch.from_numpy(place + (n - used) * 16).to(DEV), *back)
+        for got, ref in zip(back, want[2:]):
+            assert np.array_equal(R.bf16_bits(got), ref[place // 16, :, place % 16])
+    plan.close()
+    ctx.close()
