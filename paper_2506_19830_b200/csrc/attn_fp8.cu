@@ -191,7 +191,7 @@ __device__ __forceinline__ bool wait_long(uint32_t bar, uint32_t parity, int cod
 }
 template <int kD, int kRole>
 __device__ __noinline__ bool wait_call(uint32_t bar, uint32_t parity, int code) { return wait_long<kD>(bar, parity, code); }
-// kRole: 0 softmax, 1 the others
+// kRole: 0 softmax, 1 the others (whose registers are fewer: a call is compiled for either), 2 within a function that is one already
 template <int kD, int kRole>
 __device__ __forceinline__ bool wait(uint64_t *bar, uint32_t parity, int code) {
   const uint32_t at = smem_u32(bar);
