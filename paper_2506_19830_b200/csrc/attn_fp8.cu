@@ -31,7 +31,7 @@
 // warps of a scheduler need 1,024: all roles share an SM's instruction cache, of which 2,048 instructions are fast, and code that runs once a
 // half-tile comes at some eight cycles an instruction.  So loops are rolled, what is rare is in functions, and what runs once a piece is short.  A version
 // with everything unrolled and in line, K converted to halves as well, took three times as long.
-// Measured: 224 query rows over 32 K keys 83 us (31 for the products), a serving batch of 16 requests 208 us (65), 8 trees of 64-wide heads 151 us (28),
+// Measured: 96 query tokens of 32 heads over 32 K keys 83 us (31 for the products), a serving batch of 16 requests 207 us (65), 8 trees of 64-wide heads 151 us (28),
 // one token over 250 keys 11.4 us; 64 single tokens over 1024 keys each 79 us with head size 128 (93 without sharing the keys), 62 us with 64 (83).
 //
 // A visible row that stands for NaN: K's has a scale of NaN, and with it the row's sum is.  V's becomes zeros, for a weight of 0 times NaN
