@@ -246,18 +246,19 @@ def _fp8_rows(ctx: "Context", cache: Fp8Cache, k: torch.Tensor, v: torch.Tensor,
     """Number of tokens and the rows' strides, with the tensors found to be what the C side takes them for."""
     _check_cache(cache, ctx)
     n, heads, width, dev = slots.numel(), cache.heads, cache.head_dim, ctx.device
-    strides = []
-    for t in (k, v):
-        row, head, one = t.stride() if t.dim() == 3 else (0, 0, 0)
-        if t.shape != (n, heads, width) or t.dtype is not torch.bfloat16 or t.get_device() != dev or (n and (one != 1 or head != width)):
-            raise ValueError(f"rows are bf16 [{n}, {heads}, {width}] on {cache.device}, a token's heads side by side: got {tuple(t.shape)} "
-                             f"{t.dtype} strides {t.stride()} on {t.device}")
-        strides.append(row if n > 1 else heads * width)
+    strides = ()
+    if k.shape == v.shape == (n, heads, width) and k.dtype is v.dtype is torch.bfloat16 and k.get_device() == v.get_device() == dev:
+        (k_row, k_head, k_one), (v_row, v_head, v_one) = k.stride(), v.stride()
+        if n == 0 or (k_one == v_one == 1 and k_head == v_head == width):
+            strides = (k_row, v_row) if n > 1 else (heads * width, heads * width)
+    if not strides:
+        raise ValueError(f"rows are bf16 [{n}, {heads}, {width}] on {cache.device}, a token's heads side by side: got " +
+                         " and ".join(f"{tuple(t.shape)} {t.dtype} strides {t.stride()} on {t.device}" for t in (k, v)))
     if slots.dtype is not torch.int64 or not slots.is_contiguous() or slots.get_device() != dev:
         raise ValueError(f"slots are contiguous int64 on {cache.device}")
     if status is not None and (status.dtype is not torch.int32 or status.numel() < 2 or not status.is_contiguous() or status.get_device() != dev):
         raise ValueError(f"status is two int32 on {cache.device}")
-    return n, strides[0], strides[1]
+    return n, *strides
 
 
 class Context:
