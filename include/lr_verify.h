@@ -481,12 +481,17 @@ int lr_fp8_read(lr_ctx *ctx, const lr_fp8_cache *cache, const int64_t *slots_d, 
  * summed and the softmax is done in fp32.  The rows of tokens are such as
  * lr_fp8_write leaves; slots that hold no token of the plan may hold anything.  A
  * row that stands for NaN (byte 255, codes 0) makes the output of a query that sees
- * it NaN and does not touch the others.  The tensor cores take softmax weights as
- * halves, in units of the largest scale of V: a key's part of an output is off by
- * at most 2^-11 of itself or 2^-23 of the largest number of V among the request's
- * tokens (of that KV head).  lr_plan_set_attention_path: 0 automatic, 1 CUDA
- * cores, 2 tensor cores; there is no CTA-pair kernel for this cache (3:
- * LR_EUNSUPPORTED).
+ * it NaN and does not touch the others.
+ *
+ * The tensor cores take Q as two 8-bit terms, whose sum is Q but for channels below
+ * 2^-13 of their row's largest.  A row whose scores could be off by more than 2^-10
+ * for that (as exponents of 2; it takes a channel some thousand times the others) is
+ * worked out on the CUDA cores from Q as it is: same results as any, in 200 times
+ * the time.  They take softmax weights as halves, in units of the largest scale of
+ * V: a key's part of an output is off by at most 2^-11 of itself or 2^-23 of the
+ * largest number of V among the request's tokens (of that KV head).
+ * lr_plan_set_attention_path: 0 automatic, 1 CUDA cores, 2 tensor cores; there is no
+ * CTA-pair kernel for this cache (3: LR_EUNSUPPORTED).
  */
 int lr_verify_attention_fp8(lr_plan *plan, const void *q_d, const lr_fp8_cache *cache, void *out_d, float *lse_d,
                             float softmax_scale, void *stream);

@@ -4,10 +4,12 @@
 // streams of a CTA, the issuers and the score buffers in tensor memory.  What is different is how K and V get into shared memory and
 // what the products are made of.
 //
-// Scores.  S = Q K^T is an e4m3 x e4m3 product: K goes from the cache into shared memory as it is, by TMA.  Q comes in two terms, hi = the e4m3
-// numbers nearest to the row (scaled by a power of two to just fit) and lo = what that leaves: bf16 has eight bits, each term holds four, so the
-// two are the row itself wherever it is above 2^-10 of its largest number, and off by 2^-19 of that elsewhere.  Two products at twice f16's rate
-// take what one would.  A key's scale multiplies its column of S, before masks and maximum.
+// Scores.  S = Q K^T is a product of 8-bit numbers: K goes from the cache into shared memory as it is, by TMA.  Q comes in two terms, hi = the e4m3
+// numbers nearest to the row (scaled by a power of two to lie within 448) and lo = the e5m2 numbers nearest to what that leaves.  bf16 has eight bits: from 2^-6 on
+// hi holds four of them and lo, whose three bits with a sign tell apart the 17 multiples of the last bit that may be left, the others, so there the two are Q itself.
+// Below, they leave 2^-14 at most: 2^-21.8 of the row's largest number.  With a key's codes of 448 at most that bounds what a row's scores can be off by; a row
+// where it is above kScoreTol, one with a channel a thousand times the others, is gone through again on the CUDA cores with Q as it is (exact_rows).  Both terms as
+// e4m3 would leave 2^-10.  Two products at twice f16's rate take what one would.  A key's scale multiplies its column of S, before masks and maximum.
 //
 // Weights and V are f16.  One instruction turns two codes into two halves; a bf16 operand would take five.  Scales being powers of two, only differences
 // of exponents go into a tile: with ref the largest scale byte of a half-tile's keys, a row of V enters as code * 2^(byte - ref), exact unless it lies
@@ -60,6 +62,9 @@ constexpr float kGrow = 11.0f;     // log2: ... scores may rise this much above 
 constexpr float kHead = 2.0f;      // log2: ... weights are kept this much above what they are,
 constexpr int kRise = 2;           // log2: ... and V's half-tiles may be this much above the accumulator's unit: 11 + 2 + 2 = 15, f16 ends at 16
 constexpr int kApart = 24;         // log2: V this far below the unit has its weights summed apart
+constexpr float kScoreTol = 0x1p-10f;  // log2: a row whose scores the terms of Q might put off by more is gone through again with Q as it is.  2^-10 is 7e-4 of a
+                                       // weight or a log-sum, a third of what the framework's attention is held to
+constexpr float kTermsLeave = 0x1p-14f;  // of a channel of Q, scaled to lie within 448: below 2^-6 at most, above nothing
 
 template <int kD>
 struct Shape {
@@ -76,10 +81,20 @@ struct Shape {
   static constexpr int kRounds = 16 / kGroups;              // ... and how many times for a half-tile
 };
 
-struct Info {  // of a half-tile: the keys' scales, the largest scale byte of V, whether some valid row of V stands for NaN (and which: four keys a byte)
+struct Info {  // of a half-tile: the keys' scales, the largest scale bytes of V and of K, whether some valid row of V stands for NaN (and which: four keys a byte)
   float k_scale[64];
-  int32_t v_ref, v_nan, pad[2];
+  int32_t v_ref, v_nan, k_ref, pad;
   uint8_t nan4[16];
+};
+
+struct Plain {  // what exact_rows needs of the call
+  const uint16_t *q;
+  const uint8_t *k, *v, *k_scale, *v_scale;
+  uint16_t *out;
+  float *lse, *partial_o, *partial_ml;
+  int64_t n_pool_pages;
+  int32_t n_kv_heads;
+  float scale_log2;
 };
 
 struct __align__(16) Ctrl {
@@ -95,13 +110,16 @@ struct __align__(16) Ctrl {
   uint32_t tmem_base;
   int abort_flag;
   uint64_t wait_limit_ns;
+  uint64_t alive_ns;      // when a warp was last seen at work that may take longer than a wait (exact_rows)
   int32_t *status;        // the plan's
+  Plain plain;
+  uint8_t xch_exact[128];
   float xch_m[128], xch_l[128], xch_unit[128];  // stream 1's rows, for the in-CTA combination
-  // What the rows of Q were divided by, of two pieces in turn: the queries of a piece are written when both streams have asked for the last scores of the piece
+  // What the rows of Q were divided by and (in such units) what their terms may be off by, summed over the channels, of two pieces in turn: the queries of a piece are written when both streams have asked for the last scores of the piece
   // before, and a stream asks for its first behind the weights of the one before that, which its threads had to know this for.
-  float q_unit[2][2][128];
+  float2 q_unit[2][2][128];
 };
-constexpr int kCtrlBytes = 9 << 10;
+constexpr int kCtrlBytes = 11 << 10;
 static_assert(sizeof(Ctrl) <= kCtrlBytes, "Ctrl must fit behind the tiles");
 constexpr int kJoinRow = 36;  // floats: 32 channels of a row, and four so that rows start in different banks
 constexpr int kJoinBytes = 4 * 32 * kJoinRow * 4;
@@ -116,10 +134,10 @@ static_assert(kTeams <= Shape<64>::kVStages && kTeams <= Shape<128>::kVStages &&
               "a converter must not be two phases of a stage ahead");
 static_assert(kSmemBytes<64> <= 227 * 1024 && kSmemBytes<128> <= 227 * 1024, "shared memory per CTA");
 
-// Instruction descriptors: D fp32, M = 128; QK: A and B e4m3 (format 0 of kind::f8f6f4), N = 64 keys, both operands K-major; PV: A and B f16 (format 0
-// of kind::f16), N = head size, B N-major.
+// Instruction descriptors: D fp32, M = 128; QK: A e4m3 or e5m2 (formats 0 and 1 of kind::f8f6f4), B e4m3, N = 64 keys, both operands K-major; PV: A and B f16
+// (format 0 of kind::f16), N = head size, B N-major.
 constexpr uint32_t kIdescBase = (1u << 4) | (8u << 24);
-constexpr uint32_t kIdescQK = kIdescBase | ((64u >> 3) << 17);
+constexpr uint32_t kIdescQK = kIdescBase | ((64u >> 3) << 17), kAIsE5M2 = 1u << 7;
 template <int kD>
 constexpr uint32_t kIdescPV = kIdescBase | (((uint32_t)kD >> 3) << 17) | (1u << 16);
 
@@ -177,7 +195,8 @@ __device__ __forceinline__ bool wait_long(uint32_t bar, uint32_t parity, int cod
     if (__all_sync(0xFFFFFFFFu, got != 0u)) return true;
     if (i == 0) t0 = global_ns();
     if ((i & 31u) == 31u) {
-      const bool out = global_ns() - t0 > ctrl->wait_limit_ns;
+      const uint64_t since = max(t0, *reinterpret_cast<volatile uint64_t *>(&ctrl->alive_ns)), now = global_ns();
+      const bool out = now > since && now - since > ctrl->wait_limit_ns;
       if (__any_sync(0xFFFFFFFFu, out || *reinterpret_cast<volatile int *>(&ctrl->abort_flag))) {
         if (out) {
           *reinterpret_cast<volatile int *>(&ctrl->abort_flag) = 1;
@@ -210,9 +229,9 @@ __device__ __forceinline__ float4 ld_shared_f4(uint32_t addr) {
   asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(addr) : "memory");
   return v;
 }
-__device__ __forceinline__ int2 ld_shared_i2(uint32_t addr) {
-  int2 v;
-  asm volatile("ld.shared.v2.s32 {%0, %1}, [%2];" : "=r"(v.x), "=r"(v.y) : "r"(addr) : "memory");
+__device__ __forceinline__ int4 ld_shared_i4(uint32_t addr) {
+  int4 v;
+  asm volatile("ld.shared.v4.s32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(addr) : "memory");
   return v;
 }
 __device__ __forceinline__ float2 fmul2(float2 a, float2 b) {
@@ -225,6 +244,13 @@ __device__ __forceinline__ float2 fmul2(float2 a, float2 b) {
 __device__ __forceinline__ uint32_t pack_e4m3(float a, float b, float c, float d) {
   uint32_t r;
   asm("{\n\t.reg .b16 lo, hi;\n\tcvt.rn.satfinite.e4m3x2.f32 lo, %2, %1;\n\tcvt.rn.satfinite.e4m3x2.f32 hi, %4, %3;\n\tmov.b32 %0, {lo, hi};\n\t}"
+      : "=r"(r)
+      : "f"(a), "f"(b), "f"(c), "f"(d));
+  return r;
+}
+__device__ __forceinline__ uint32_t pack_e5m2(float a, float b, float c, float d) {
+  uint32_t r;
+  asm("{\n\t.reg .b16 lo, hi;\n\tcvt.rn.satfinite.e5m2x2.f32 lo, %2, %1;\n\tcvt.rn.satfinite.e5m2x2.f32 hi, %4, %3;\n\tmov.b32 %0, {lo, hi};\n\t}"
       : "=r"(r)
       : "f"(a), "f"(b), "f"(c), "f"(d));
   return r;
@@ -318,12 +344,13 @@ __device__ __noinline__ bool sees_nan(const uint8_t *nan4, const TcPage *pages, 
   return seen;
 }
 
-// Rows r0 .. r0 + n - 1 of a tile (q_index of row r0 + i: in lane i0 + i), each scaled by a power of two to lie within 448, as their two e4m3 terms; 2 to the
-// exponent taken out goes to unit[row], NaN for a row that is not finite (its scores are no numbers either).  The rows come by asynchronous copies into
+// Rows r0 .. r0 + n - 1 of a tile (q_index of row r0 + i: in lane i0 + i), each scaled by a power of two to lie within 448, as their two terms, e4m3 and e5m2; 2 to the
+// exponent taken out goes to unit[row], NaN for a row that is not finite (its scores are no numbers either), and beside it what the terms may leave of all its
+// channels together.  The rows come by asynchronous copies into
 // the place of their terms (bf16 is as long as the two) and are converted where they lie, a row's channels across lanes.  Registers for 32 rows in flight
 // there are none, and with a row to a thread this took 17,000 cycles at the start of every piece, a third of a short call.
 template <int kD>
-__device__ __noinline__ void convert_q(const uint16_t *__restrict__ q, int64_t q_index, uint32_t tile, float *unit, int r0, int n, int i0) {
+__device__ __noinline__ void convert_q(const uint16_t *__restrict__ q, int64_t q_index, uint32_t tile, float2 *unit, int r0, int n, int i0) {
   constexpr int kLanes = kD / 8, kRows = 32 / kLanes;  // lanes to a row, 8 channels each; rows at a time
   const int lane = threadIdx.x & 31, sub = lane / kLanes, c = lane % kLanes;
   const uint32_t raw = tile + (r0 + sub) * kD + (c % (kLanes / 2)) * 16 + (c / (kLanes / 2)) * Shape<kD>::kTermBytes;
@@ -350,6 +377,7 @@ __device__ __noinline__ void convert_q(const uint16_t *__restrict__ q, int64_t q
 #pragma unroll
       for (int b = 0; b < 2; ++b) top[b] = max(top[b], __shfl_xor_sync(0xFFFFFFFFu, top[b], m));
     __syncwarp();  // the rows have been read
+    uint32_t small = 0;  // how many channels of this lane's two rows are below 2^-6 or just above: 16 bits each
 #pragma unroll
     for (int b = 0; b < 2; ++b) {
       const int p = p0 + b * kRows, e = min(max((int)(top[b] >> 7) - 135 + ((top[b] & 0x7Fu) > 0x60u ? 1 : 0), -126), 120);  // as lr_fp8_write
@@ -361,14 +389,22 @@ __device__ __noinline__ void convert_q(const uint16_t *__restrict__ q, int64_t q
         const float x0 = bits_f(w0 << 16) * by, x1 = bits_f(w0 & 0xFFFF0000u) * by, x2 = bits_f(w1 << 16) * by, x3 = bits_f(w1 & 0xFFFF0000u) * by;
         hi[j] = pack_e4m3(x0, x1, x2, x3);
         const float2 h0 = fp8_float2(hi[j] & 0xFFFFu), h1 = fp8_float2(hi[j] >> 16);
-        lo[j] = pack_e4m3(x0 - h0.x, x1 - h0.y, x2 - h1.x, x3 - h1.y);
+        lo[j] = pack_e5m2(x0 - h0.x, x1 - h0.y, x2 - h1.x, x3 - h1.y);
+        small += __popc(~((hi[j] & 0x7F7F7F7Fu) + 0x77777777u) & 0x80808080u) << (16 * b);  // codes below 9, where 8 is 2^-6
       }
       if (p + sub < n) {
         const uint32_t at = tile + row_unit<kD>(r0 + p + sub, c >> 1) + (c & 1) * 8;
         st_shared2(at, hi[0], hi[1]);
         st_shared2(at + Shape<kD>::kTermBytes, lo[0], lo[1]);
-        if (c == 0) unit[r0 + p + sub] = top[b] < 0x7F80u ? pow2(e) : __uint_as_float(0x7FC00000u);
+        if (c == 0) unit[r0 + p + sub] = make_float2(top[b] < 0x7F80u ? pow2(e) : __uint_as_float(0x7FC00000u), 0.f);
       }
+    }
+    if (__any_sync(0xFFFFFFFFu, small != 0u)) {
+#pragma unroll
+      for (int m = kLanes / 2; m > 0; m >>= 1) small += __shfl_xor_sync(0xFFFFFFFFu, small, m);
+#pragma unroll
+      for (int b = 0; b < 2; ++b)
+        if (c == 0 && p0 + b * kRows + sub < n) unit[r0 + p0 + b * kRows + sub].y = kTermsLeave * (float)((small >> (16 * b)) & 0xFFFFu);
     }
   }
 }
@@ -506,9 +542,119 @@ __device__ __noinline__ bool join_rows(uint32_t o_addr, uint32_t o_other, int sl
   return true;
 }
 
-struct Fp8Pools {  // K's codes are behind a tensor map
-  const uint8_t *v, *k_scale, *v_scale;
+struct Fp8Pools {  // (K's codes are behind a tensor map too)
+  const uint8_t *k, *v, *k_scale, *v_scale;
 };
+
+// Rows of a piece whose scores the terms of Q might put off by more than kScoreTol, one after another by a whole warp on the CUDA cores, with Q as it is: what
+// store_rows or join_rows would have left for them.  `rows`: the lanes whose rows they are, ri theirs; row0: of lane 0's row in the M-tile.  As attn_fp8_generic.cu, from
+// which it differs in the order of keys alone; that kernel has all of an SM's warps for it.
+template <int kD>
+__device__ __noinline__ void exact_rows(uint32_t rows, RowInfo ri, const TcPage *__restrict__ pages, int n_tiles, int n_dense, int kv_head, int slot, int row0) {
+  constexpr int kEach = kD / 32;  // output channels of a lane
+  Ctrl *ctrl = ctrl_at<kD>();
+  const Plain in = ctrl->plain;
+  const int lane = threadIdx.x & 31;
+  for (; rows != 0u; rows &= rows - 1u) {
+    const int i = __ffs(rows) - 1;
+    RowInfo one;
+    one.depth = __shfl_sync(0xFFFFFFFFu, ri.depth, i);
+    one.branch = __shfl_sync(0xFFFFFFFFu, ri.branch, i);
+    one.limit = __shfl_sync(0xFFFFFFFFu, ri.limit, i);
+    one.q_index = __shfl_sync(0xFFFFFFFFu, ri.q_index, i);
+    const uint4 *qp = reinterpret_cast<const uint4 *>(in.q + one.q_index * kD);
+    float m = -INFINITY, l = 0.f, acc[kEach];
+#pragma unroll
+    for (int e = 0; e < kEach; ++e) acc[e] = 0.f;
+#pragma unroll 1
+    for (int t = 0; t < 4 * n_tiles; ++t) {  // two pages, a key a lane
+      if (lane == 0 && (t & 255) == 0) *reinterpret_cast<volatile uint64_t *>(&ctrl->alive_ns) = global_ns();
+      const int2 e = ld_pair(pages + 2 * t + (lane >> 4));
+      const int n_ok = (t >> 2) < n_dense ? kPage : page_n_ok((uint32_t)e.y, one);
+      const bool valid = (lane & 15) < n_ok;
+      const unsigned live = __ballot_sync(0xFFFFFFFFu, valid);
+      if (live == 0u) continue;
+      // (the page named, or page 0 in its place, as for the products)
+      const int64_t page = e.x >= 0 && e.x < in.n_pool_pages ? e.x : 0, at = (page * in.n_kv_heads + kv_head) * kPage + (lane & 15);
+      if (valid && page != e.x) {
+        ctrl->status[0] = kDevBounds;
+        ctrl->status[1] = 200;
+      }
+      float s = -INFINITY, vs = 0.f;
+      if (valid) {
+        const uint4 *kp = reinterpret_cast<const uint4 *>(in.k + at * kD);
+        float a0 = 0.f, a1 = 0.f;
+        uint4 code[kD / 16];
+#pragma unroll
+        for (int c = 0; c < kD / 16; ++c) code[c] = __ldcg(kp + c);
+#pragma unroll
+        for (int c = 0; c < kD / 16; ++c) {
+          const uint4 kk = code[c], qa = __ldg(qp + 2 * c), qb = __ldg(qp + 2 * c + 1);
+          const uint32_t w[4] = {kk.x, kk.y, kk.z, kk.w}, x[8] = {qa.x, qa.y, qa.z, qa.w, qb.x, qb.y, qb.z, qb.w};
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            const float2 y0 = fp8_float2(w[j] & 0xFFFFu), y1 = fp8_float2(w[j] >> 16);
+            a0 = fmaf(bits_f(x[2 * j] << 16), y0.x, a0);
+            a1 = fmaf(bits_f(x[2 * j] & 0xFFFF0000u), y0.y, a1);
+            a0 = fmaf(bits_f(x[2 * j + 1] << 16), y1.x, a0);
+            a1 = fmaf(bits_f(x[2 * j + 1] & 0xFFFF0000u), y1.y, a1);
+          }
+        }
+        s = (a0 + a1) * (fp8_scale(ld_scale(in.k_scale + at)) * in.scale_log2);
+        vs = fp8_scale(ld_scale(in.v_scale + at));
+      }
+      float m_new = s;  // (a score that is no number is not the largest: it comes back through the sum)
+#pragma unroll
+      for (int o = 16; o > 0; o >>= 1) m_new = fmaxf(m_new, __shfl_xor_sync(0xFFFFFFFFu, m_new, o));
+      m_new = fmaxf(m, m_new);
+      const float ref = m_new > -INFINITY ? m_new : 0.f, down = m > -INFINITY ? exp2f(m - ref) : 0.f, p = valid ? exp2f(s - ref) : 0.f;
+      float sum = p;
+#pragma unroll
+      for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, o);
+      l = fmaf(l, down, sum);
+      m = m_new;
+#pragma unroll
+      for (int e2 = 0; e2 < kEach; ++e2) acc[e2] *= down;
+      const float weight = valid ? p * vs : 0.f;
+#pragma unroll 1
+      for (int j0 = 0; j0 < 32; j0 += 8) {
+        if (((live >> j0) & 0xFFu) == 0u) continue;
+        uint32_t c[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {  // a key the row does not see: zeros, whatever is there
+          const uint8_t *vp = in.v + (int64_t)__shfl_sync(0xFFFFFFFFu, (long long)at, j0 + j) * kD + lane * kEach;
+          c[j] = 0u;
+          if ((live >> (j0 + j)) & 1u) c[j] = kEach == 4 ? __ldcg(reinterpret_cast<const uint32_t *>(vp)) : (uint32_t)__ldcg(reinterpret_cast<const uint16_t *>(vp));
+        }
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          const float w = __shfl_sync(0xFFFFFFFFu, weight, j0 + j);
+          const float2 y = fp8_float2(c[j] & 0xFFFFu);
+          acc[0] = fmaf(w, y.x, acc[0]);
+          acc[1] = fmaf(w, y.y, acc[1]);
+          if constexpr (kEach == 4) {
+            const float2 z = fp8_float2(c[j] >> 16);
+            acc[2] = fmaf(w, z.x, acc[2]);
+            acc[3] = fmaf(w, z.y, acc[3]);
+          }
+        }
+      }
+    }
+    if (slot < 0) {
+      const float inv = 1.0f / l;
+#pragma unroll
+      for (int e = 0; e < kEach; e += 2)
+        *reinterpret_cast<uint32_t *>(in.out + one.q_index * kD + lane * kEach + e) = pack_bf16(acc[e] * inv, acc[e + 1] * inv);
+      if (lane == 0 && in.lse != nullptr) in.lse[one.q_index] = (m + log2f(l)) * 0.6931471805599453f;
+    } else {
+      const int r = row0 + i;
+      float *dst = in.partial_o + (((int64_t)slot * (kD / 4) + lane * kEach / 4) * 128 + r) * 4 + (lane * kEach) % 4;
+#pragma unroll
+      for (int e = 0; e < kEach; e += 2) *reinterpret_cast<float2 *>(dst + e) = make_float2(acc[e], acc[e + 1]);
+      if (lane == 0) *reinterpret_cast<float2 *>(in.partial_ml + ((int64_t)slot * 128 + r) * 2) = l != l ? make_float2(l, 1.0f) : make_float2(m, l);  // as in store_rows
+    }
+  }
+}
 
 __device__ __forceinline__ uint32_t valid_bytes(int valid, int lane) {  // of the four keys of this lane's word
   const int n = valid - (lane & 3) * 4;
@@ -585,10 +731,12 @@ attn_fp8_kernel(const __grid_constant__ CUtensorMap k_map, DevBatch d, DevTcPlan
     mbar_init(&ctrl->join, 128);
     for (int i = 0; i < kInfos; ++i) mbar_init(&ctrl->info_full[i], 1);
     ctrl->abort_flag = 0;
+    ctrl->alive_ns = 0;
     ctrl->wait_limit_ns = (uint64_t)tc.wait_limit_us * 1000ull;
     ctrl->status = d.status;
     fence_barrier_init();
   }
+  if (threadIdx.x == 32) ctrl->plain = Plain{q, in.k, in.v, in.k_scale, in.v_scale, out, lse, tc.partial_o, tc.partial_ml, d.n_pool_pages, d.n_kv_heads, scale_log2};
   if (warp == 12) {
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&ctrl->tmem_base)), "r"(512u)
                  : "memory");
@@ -631,7 +779,7 @@ attn_fp8_kernel(const __grid_constant__ CUtensorMap k_map, DevBatch d, DevTcPlan
         for (int term = 0; term < 2; ++term)
 #pragma unroll
           for (int kk = 0; kk < kD / 32; ++kk)
-            mma_f8(s_tmem + half * 64, a + (uint64_t)(term * (kTermBytes >> 4) + kk * 2), b + (uint64_t)(kk * 2), kIdescQK, (term | kk) != 0);
+            mma_f8(s_tmem + half * 64, a + (uint64_t)(term * (kTermBytes >> 4) + kk * 2), b + (uint64_t)(kk * 2), kIdescQK | (term != 0 ? kAIsE5M2 : 0u), (term | kk) != 0);
       };
       auto issue_pv = [&](uint32_t stage, int half, bool acc) {  // O_s (+)= P_s[half] V over 64 keys
         const uint64_t b = vdesc0 + (uint64_t)(stage * (kVBytes >> 4));
@@ -855,7 +1003,7 @@ attn_fp8_kernel(const __grid_constant__ CUtensorMap k_map, DevBatch d, DevTcPlan
             tma_load_2d(smem_u32(k_smem) + k_stage * kCodeBytes + (lane >> 2) * (kPage * kD), &k_map, 0, row, &ctrl->k_full[k_stage]);
           Info &info = ctrl->info[asked % kInfos];
           const uint32_t now = valid_bytes((int)(meta & 31u), lane), kb = k_word & now, vb = word & now, nan = __vcmpeq4(vb, 0xFFFFFFFFu);
-          const uint32_t v_ref = max(__reduce_max_sync(0xFFFFFFFFu, top_byte(vb)), 1u);
+          const uint32_t v_ref = max(__reduce_max_sync(0xFFFFFFFFu, top_byte(vb)), 1u), k_ref = __reduce_max_sync(0xFFFFFFFFu, top_byte(kb));
           const bool any = __any_sync(0xFFFFFFFFu, nan != 0u);
           if (lane < 16) {  // (a byte of a slot without a valid token is 0 here: its scores are not looked at)
             float4 f;
@@ -866,7 +1014,7 @@ attn_fp8_kernel(const __grid_constant__ CUtensorMap k_map, DevBatch d, DevTcPlan
             reinterpret_cast<float4 *>(info.k_scale)[lane] = f;
             if (any) info.nan4[lane] = (uint8_t)((nan & 1u) | ((nan >> 7) & 2u) | ((nan >> 14) & 4u) | ((nan >> 21) & 8u));
           }
-          if (lane == 0) *reinterpret_cast<int2 *>(&info.v_ref) = make_int2((int)v_ref, any ? 1 : 0);
+          if (lane == 0) *reinterpret_cast<int4 *>(&info.v_ref) = make_int4((int)v_ref, any ? 1 : 0, (int)k_ref, 0);
           __syncwarp();
           if (lane == 0) mbar_arrive(&ctrl->info_full[asked % kInfos]);
           asked += kTeams;
@@ -905,24 +1053,27 @@ attn_fp8_kernel(const __grid_constant__ CUtensorMap k_map, DevBatch d, DevTcPlan
       const int my_units = mode == 2 ? n : (n - s + 1) / 2;
       const bool split = kFew && shares_keys(pi, rq, T, d.group);
       const RowInfo ri = row_info(d, tc, rq, T, mode == 2 ? pi.mtile0 + s : pi.mtile0, split ? lane : r, pi.kv_head);
-      float sc_row = 0.f;
+      float sc_row = 0.f, q_off = 0.f;  // q_off: what the terms of Q leave of the row, times what its scores are multiplied by
       if (ok) {
         // the queries, once the products of the piece before no longer read the buffers; of one M-tile each stream takes half of every warp's rows.
         // Padding is left as it is: what comes of it reaches rows that nobody reads.
         ok = wait<kD, 0>(&ctrl->q_empty, ((uint32_t)(pc - piece0) & 1u) ^ 1u, 245);
         if (ok) {
           const int live = __popc(__ballot_sync(0xFFFFFFFFu, ri.q_index >= 0)), i0 = mode == 2 ? 0 : s * 16;  // (live rows come first)
-          float *unit = ctrl->q_unit[(pc - piece0) & 1][mode == 2 ? s : 0];
+          float2 *unit = ctrl->q_unit[(pc - piece0) & 1][mode == 2 ? s : 0];
           convert_q<kD>(q, ri.q_index, smem_u32(q_smem) + (mode == 2 ? s : 0) * kQBytes, unit, quarter * 32 + i0, min(live - i0, mode == 2 ? 32 : 16), i0);
           fence_proxy_async();
           mbar_arrive(&ctrl->q_full);
           ok = wait<kD, 0>(&ctrl->q_full, (uint32_t)(pc - piece0) & 1u, 246);
-          if (ok && ri.q_index >= 0) sc_row = scale_log2 * unit[r];
+          if (ok && ri.q_index >= 0) {
+            sc_row = scale_log2 * unit[r].x;
+            q_off = sc_row * unit[r].y;
+          }
         }
       }
       if (ok && my_units > 0) {
         float m_used = -INFINITY, l = 0.f;  // the row's reference exponent and sum
-        int base = 0;
+        int base = 0, k_top = 0;  // k_top: the largest scale byte of K so far
         bool s_ready = false, nan_v = false;
         // A warp whose 32 rows are all padding only keeps the barriers' counts: what it leaves as weights multiplies into rows
         // of O that nobody reads.
@@ -939,7 +1090,8 @@ attn_fp8_kernel(const __grid_constant__ CUtensorMap k_map, DevBatch d, DevTcPlan
             tc_fence_after();
             uint32_t v[16];
             tmem_ld16(sh_addr + quarter * 16, v);
-            const int2 of_v = ld_shared_i2(info + 256);
+            const int4 of_v = ld_shared_i4(info + 256);
+            k_top = max(k_top, of_v.z);
             const int n_ok = t >= rq.n_dense_tiles ? page_n_ok(__ldg(&tc.pages[rq.page_off + t * kPagesPerTile + half * 4 + quarter].meta), ri) : kPage;
             float alpha = 1.0f;
             bool moved = false;
@@ -1059,7 +1211,8 @@ attn_fp8_kernel(const __grid_constant__ CUtensorMap k_map, DevBatch d, DevTcPlan
             tc_fence_after();
             uint32_t v[64];
             tmem_ld64(sh_addr, v);
-            const int2 of_v = ld_shared_i2(info + 256);  // largest scale byte, whether some row stands for NaN
+            const int4 of_v = ld_shared_i4(info + 256);  // largest scale byte, whether some row stands for NaN; K's largest scale byte
+            k_top = max(k_top, of_v.z);
             float alpha = 1.0f;  // what O has to be multiplied by before this half's product
             bool moved = false;  // ... in some row of the warp
             if (first) base = of_v.x + 1;
@@ -1157,6 +1310,8 @@ attn_fp8_kernel(const __grid_constant__ CUtensorMap k_map, DevBatch d, DevTcPlan
         }
         // what the accumulator's numbers are worth; NaN for a row that sees a row of V that is
         const float unit = nan_v ? __uint_as_float(0x7FC00000u) : exp2f((float)(base - 127) - kHead);
+        // A key's codes are 448 at most: no score of the row is off by more than this.
+        bool exact = q_off * 448.0f * pow2(k_top - 127) > kScoreTol;
         // The two streams of a one-M-tile piece hold partial results of the same rows (even and odd tiles).
         // Stream 1 publishes its sums; stream 0 reads them and stream 1's accumulator -- the same tensor-memory
         // lanes, so the thread of row r can load both -- and writes one combined result.
@@ -1168,6 +1323,7 @@ attn_fp8_kernel(const __grid_constant__ CUtensorMap k_map, DevBatch d, DevTcPlan
             ctrl->xch_m[r] = m_used;
             ctrl->xch_l[r] = l;
             ctrl->xch_unit[r] = unit;
+            ctrl->xch_exact[r] = exact;
             tc_fence_before();
             mbar_arrive(&ctrl->xch);
             writer = false;
@@ -1182,19 +1338,28 @@ attn_fp8_kernel(const __grid_constant__ CUtensorMap k_map, DevBatch d, DevTcPlan
               self = l != 0.f ? unit * w_self : 0.f;
               other = other_live ? ctrl->xch_unit[r] * w_other : 0.f;
               l_out = w_self * l + w_other * ol;
+              exact = exact || ctrl->xch_exact[r] != 0;
             }
           }
         }
         if (pair) ++x_cnt;
+        const int64_t q_index = exact ? -1 : ri.q_index;
         if (kFew && ok && writer && split) {
           tc_fence_after();
-          ok = join_rows<kD>(o_addr, lane_base + 256 + 128, pi.slot[0], self, other, other_live, m_out, l_out, quarter, ri.q_index, joins, out, lse, tc.partial_o, tc.partial_ml);
+          ok = join_rows<kD>(o_addr, lane_base + 256 + 128, pi.slot[0], self, other, other_live, m_out, l_out, quarter, q_index, joins, out, lse, tc.partial_o, tc.partial_ml);
           tc_fence_before();
         } else if (ok && writer && !idle) {
           tc_fence_after();
-          store_rows<kD>(o_addr, lane_base + 256 + (1 - s) * 128, pi.slot[pair ? 0 : s], self, other, other_live, m_out, l_out, r, ri.q_index, out, lse,
+          store_rows<kD>(o_addr, lane_base + 256 + (1 - s) * 128, pi.slot[pair ? 0 : s], self, other, other_live, m_out, l_out, r, q_index, out, lse,
                          tc.partial_o, tc.partial_ml);
           tc_fence_before();
+        }
+        if (ok && writer) {
+          uint32_t again = __ballot_sync(0xFFFFFFFFu, exact && ri.q_index >= 0);
+          if (split) again &= 0x11111111u << quarter;  // the four warps have the same rows
+          if (again != 0u)
+            exact_rows<kD>(again, ri, tc.pages + rq.page_off + pi.tile_begin * kPagesPerTile, n, rq.n_dense_tiles - pi.tile_begin, pi.kv_head, pi.slot[pair ? 0 : s],
+                           split ? 0 : quarter * 32);
         }
       }
       // One arrival per thread and piece.  A stream with units in this piece cannot get here before the previous
@@ -1277,7 +1442,7 @@ int init_attn_fp8_kernel() {
 int launch_attn_fp8(lr_plan *p, const void *q, const lr_fp8_cache &c, void *out, float *lse, float scale, cudaStream_t s) {
   alignas(64) CUtensorMap k_map;
   if (int rc = encode_k(p->ctx, c.k_d, p->dev.n_pool_pages, &k_map)) return rc;
-  const Fp8Pools in = {reinterpret_cast<const uint8_t *>(c.v_d), c.k_scale_d, c.v_scale_d};
+  const Fp8Pools in = {reinterpret_cast<const uint8_t *>(c.k_d), reinterpret_cast<const uint8_t *>(c.v_d), c.k_scale_d, c.v_scale_d};
   return (p->dev.head_dim == 128 ? launch<128> : launch<64>)(p, k_map, reinterpret_cast<const uint16_t *>(q), in, reinterpret_cast<uint16_t *>(out), lse,
                                                              scale * 1.4426950408889634f, s);
 }
