@@ -57,7 +57,7 @@ constexpr int kTeams = 4;          // converter warps, each with half-tiles of i
 // free, which half-tile x + kInfos - kKStages had; from x + 6 (three tiles) on, that tells that no softmax thread will look at x again: an issuer
 // asks for or skips x + 6 behind the weights of its last half-tile up to x.
 constexpr int kInfos = 16;
-constexpr float kLift = 3.0f;      // log2: a row's reference exponent is set this much above its maximum so far,
+constexpr float kLift = 2.0f;      // log2: a row's reference exponent is set this much above its maximum so far,
 constexpr float kGrow = 11.0f;     // log2: ... scores may rise this much above it,
 constexpr float kHead = 2.0f;      // log2: ... weights are kept this much above what they are,
 constexpr int kRise = 2;           // log2: ... and V's half-tiles may be this much above the accumulator's unit: 11 + 2 + 2 = 15, f16 ends at 16
