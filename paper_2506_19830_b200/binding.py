@@ -261,6 +261,45 @@ def _fp8_rows(ctx: "Context", cache: Fp8Cache, k: torch.Tensor, v: torch.Tensor,
     return n, *strides
 
 
+def _flat(t: Optional[torch.Tensor], kind: torch.dtype, n: int, dev: int) -> bool:
+    """Whether the C side may take t for n numbers of that kind side by side (None is its own affair)."""
+    return t is None or (t.dtype is kind and t.numel() >= n and t.is_contiguous() and t.get_device() == dev)
+
+
+def _logit_rows(t: Optional[torch.Tensor], n: int, vocab: int, dev: int) -> bool:
+    return t is None or (t.dtype is torch.bfloat16 and t.dim() == 2 and t.shape[0] >= n and t.shape[1] >= vocab and t.stride(1) == 1 and t.get_device() == dev)
+
+
+def _refuse(where: str, dev: int, **wanted) -> None:
+    """The first of the tensors that is not what it has to be: name=(whether it is, the tensor, what it has to be)."""
+    for name, (fine, t, want) in wanted.items():
+        if not fine:
+            raise ValueError(f"{where}: {name} is {want} on device {dev}: got {tuple(t.shape)} {t.dtype} strides {t.stride()} on {t.device}")
+
+
+def _check_drafted(ctx: "Context", logits, draft_logits, draft_ids, cu_draft, u_accept, u_final, n_accept, final_id, p_draft, q_draft, scratch,
+                   scratch_bytes: int) -> tuple:
+    """(branches, target rows) of a drafted acceptance, its tensors found to be what the C side takes them for: it sees neither how long they are nor of which kind."""
+    dev, vocab, where = ctx.device, ctx.model.vocab, "lr_accept_sample_drafted"
+    _refuse(where, dev, cu_draft=(_flat(cu_draft, torch.int32, 1, dev), cu_draft, "int32 [branches + 1]"),
+            logits=(_logit_rows(logits, 0, vocab, dev), logits, f"bf16 [rows, >= {vocab}], a row's logits side by side,"))
+    n_branch, n_rows = cu_draft.numel() - 1, logits.shape[0]
+    n = n_rows - n_branch  # drafts
+    if n < 0:
+        raise ValueError(f"{where}: {n_branch} branches have a row of logits each at least, not {n_rows} together")
+    fine = [_flat(draft_ids, torch.int32, n, dev), _flat(u_accept, torch.float32, n, dev), _flat(u_final, torch.float32, n_branch, dev),
+            _flat(n_accept, torch.int32, n_branch, dev), _flat(final_id, torch.int32, n_branch, dev), _flat(p_draft, torch.float32, n, dev),
+            _flat(q_draft, torch.float32, n, dev), n == 0 or _logit_rows(draft_logits, n, vocab, dev),
+            scratch is None or (scratch.is_contiguous() and scratch.get_device() == dev and scratch.numel() * scratch.element_size() >= scratch_bytes)]
+    if not all(fine):
+        names = ("draft_ids", "u_accept", "u_final", "n_accept", "final_id", "p_draft", "q_draft", "draft_logits", "scratch")
+        tensors = (draft_ids, u_accept, u_final, n_accept, final_id, p_draft, q_draft, draft_logits, scratch)
+        want = (f"int32 [{n}]", f"float32 [{n}]", f"float32 [{n_branch}]", f"int32 [{n_branch}]", f"int32 [{n_branch}]", f"float32 [{n}]", f"float32 [{n}]",
+                f"bf16 [{n}, >= {vocab}], a row's logits side by side,", f"{scratch_bytes} bytes")
+        _refuse(where, dev, **dict(zip(names, zip(fine, tensors, want))))
+    return n_branch, n_rows
+
+
 class Context:
     """``lr_ctx``: one per (device, model geometry)."""
 
@@ -338,16 +377,20 @@ class Context:
                                  final_id: torch.Tensor, scratch: torch.Tensor, p_draft: Optional[torch.Tensor] = None,
                                  q_draft: Optional[torch.Tensor] = None, stream=None) -> None:
         """Rejection-sampling acceptance of drafts that a draft model sampled; draft_logits [sum L, >= vocab] are what they were drawn from."""
-        n_branch, n_rows = cu_draft.numel() - 1, logits.shape[0]
+        n_branch, n_rows = _check_drafted(self, logits, draft_logits, draft_ids, cu_draft, u_accept, u_final, n_accept, final_id, p_draft, q_draft, scratch,
+                                          self._drafted_scratch_bytes(logits.shape[0]))
         _check(lib().lr_accept_sample_drafted(self.handle, _ptr(logits), logits.stride(0), _ptr(draft_logits), draft_logits.stride(0), _ptr(draft_ids),
                                               _ptr(cu_draft), n_branch, n_rows, temperature, draft_temperature, _ptr(u_accept), _ptr(u_final),
                                               _ptr(n_accept), _ptr(final_id), _ptr(p_draft), _ptr(q_draft), _ptr(scratch),
                                               _stream_on(self.device, stream)), "lr_accept_sample_drafted")
 
-    def accept_sample_drafted_scratch(self, n_rows: int) -> torch.Tensor:
+    def _drafted_scratch_bytes(self, n_rows: int) -> int:
         n = C.c_size_t()
         _check(lib().lr_accept_sample_drafted_scratch_bytes(self.handle, n_rows, C.byref(n)), "lr_accept_sample_drafted_scratch_bytes")
-        return torch.empty((n.value + 7) // 8, dtype=torch.int64, device=f"cuda:{self.device}")
+        return n.value
+
+    def accept_sample_drafted_scratch(self, n_rows: int) -> torch.Tensor:
+        return torch.empty((self._drafted_scratch_bytes(n_rows) + 7) // 8, dtype=torch.int64, device=f"cuda:{self.device}")
 
     def lr_fp8_write(self, cache: Fp8Cache, k: torch.Tensor, v: torch.Tensor, slots: torch.Tensor, status: Optional[torch.Tensor] = None,
                      stream=None) -> None:
