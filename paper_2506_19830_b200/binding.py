@@ -300,6 +300,35 @@ def _check_drafted(ctx: "Context", logits, draft_logits, draft_ids, cu_draft, u_
     return n_branch, n_rows
 
 
+# (These run before every launch, where each look at a tensor takes a twentieth of a microsecond: all of them in one expression, and who is at fault only then.)
+def _check_attention(ctx: "Context", n_q_rows: int, q, out, lse) -> None:
+    m, dev = ctx.model, ctx.device
+    n = n_q_rows * m.n_q_heads
+    if (q is not None and out is not None and lse is not None and q.dtype is out.dtype is torch.bfloat16 and lse.dtype is torch.float32
+            and q.get_device() == out.get_device() == lse.get_device() == dev and q.is_contiguous() and out.is_contiguous() and lse.is_contiguous()
+            and q.numel() >= n * m.head_dim <= out.numel() and lse.numel() >= n):
+        return
+    shape = f"[{n_q_rows}, {m.n_q_heads}"
+    _refuse("lr_verify_attention_fp8", dev, q=(_flat(q, torch.bfloat16, n * m.head_dim, dev), q, f"contiguous bf16 {shape}, {m.head_dim}]"),
+            out=(_flat(out, torch.bfloat16, n * m.head_dim, dev), out, f"contiguous bf16 {shape}, {m.head_dim}]"),
+            lse=(_flat(lse, torch.float32, n, dev), lse, f"contiguous float32 {shape}]"))
+
+
+def _check_compact(ctx: "Context", n_req: int, keep_off, keep_pages, keep_valid, new_len, n_pages_kept) -> None:
+    # (how much of the lists there is to read the offsets say, which are on the device)
+    dev, i32 = ctx.device, torch.int32
+    some = keep_off is not None and keep_pages is not None and keep_valid is not None and new_len is not None and n_pages_kept is not None
+    if (some and keep_off.dtype is keep_pages.dtype is keep_valid.dtype is new_len.dtype is n_pages_kept.dtype is i32
+            and keep_off.get_device() == keep_pages.get_device() == keep_valid.get_device() == new_len.get_device() == n_pages_kept.get_device() == dev
+            and keep_off.is_contiguous() and keep_pages.is_contiguous() and keep_valid.is_contiguous() and new_len.is_contiguous() and n_pages_kept.is_contiguous()
+            and keep_off.numel() > n_req <= new_len.numel() and n_pages_kept.numel() >= n_req and keep_valid.numel() >= keep_pages.numel()):
+        return
+    _refuse("lr_compact_fp8", dev, keep_off=(_flat(keep_off, i32, n_req + 1, dev), keep_off, f"int32 [{n_req + 1}]"),
+            keep_pages=(_flat(keep_pages, i32, 0, dev), keep_pages, "int32 [page slots]"),
+            keep_valid=(_flat(keep_valid, i32, 0 if keep_pages is None else keep_pages.numel(), dev), keep_valid, "int32, as long as keep_pages,"),
+            new_len=(_flat(new_len, i32, n_req, dev), new_len, f"int32 [{n_req}]"), n_pages_kept=(_flat(n_pages_kept, i32, n_req, dev), n_pages_kept, f"int32 [{n_req}]"))
+
+
 class Context:
     """``lr_ctx``: one per (device, model geometry)."""
 
@@ -448,6 +477,7 @@ class Plan:
         self.n_req = self.host.c.n_req
         self.n_branch = self.host.c.n_branch
         self.n_page_slots = self.host.c.n_page_slots
+        self.n_q_rows = int(batch.cu_q[-1])
 
     def close(self):
         if self.handle:
@@ -504,12 +534,14 @@ class Plan:
     def lr_verify_attention_fp8(self, q, cache: Fp8Cache, out, lse=None, softmax_scale: float = 0.0, stream=None) -> None:
         """``lr_verify_attention`` over an 8-bit cache."""
         _check_cache(cache, self.ctx)
+        _check_attention(self.ctx, self.n_q_rows, q, out, lse)
         _check(lib().lr_verify_attention_fp8(self.handle, _ptr(q), cache.c, _ptr(out), _ptr(lse), float(softmax_scale),
                                              _stream_on(self.ctx.device, stream)), "lr_verify_attention_fp8")
 
     def lr_compact_fp8(self, keep_off, keep_pages, keep_valid, cache: Fp8Cache, new_len, n_pages_kept, stream=None) -> None:
         """``lr_compact`` over an 8-bit cache: codes and scales together."""
         _check_cache(cache, self.ctx)
+        _check_compact(self.ctx, self.n_req, keep_off, keep_pages, keep_valid, new_len, n_pages_kept)
         _check(lib().lr_compact_fp8(self.handle, _ptr(keep_off), _ptr(keep_pages), _ptr(keep_valid), cache.c, _ptr(new_len), _ptr(n_pages_kept),
                                     _stream_on(self.ctx.device, stream)), "lr_compact_fp8")
 

@@ -5,7 +5,7 @@ from types import SimpleNamespace
 import pytest
 import torch
 
-from lr_workloads import Model
+from lr_workloads import Model, make_config
 from paper_2506_19830_b200 import binding as B
 
 V = 100
@@ -68,4 +68,67 @@ def test_drafted_acceptance_refuses_before_it_launches():
     call(drafted("cuda:0"))
     torch.cuda.synchronize()
     assert ctx.launch_count == 2
+    ctx.close()
+
+
+def attention(rows, m, dev="cpu"):
+    q = torch.zeros((rows, m.n_q_heads, m.head_dim), dtype=torch.bfloat16, device=dev)
+    return dict(q=q, out=torch.zeros_like(q), lse=torch.zeros(q.shape[:2], device=dev))
+
+
+def wrong_attention(rows, m, dev):
+    good, wide = attention(rows, m, dev), torch.zeros((rows, 2 * m.n_q_heads, m.head_dim), dtype=torch.bfloat16, device=dev)
+    return [(name, t) for name in ("q", "out") for t in (good[name][:-1], good[name].half(), good[name].float(), wide[:, :m.n_q_heads], good[name][:, :, ::2])] + \
+           [("lse", t) for t in (good["lse"][:-1], good["lse"].double(), good["lse"].bfloat16(), torch.zeros((rows, 2 * m.n_q_heads), device=dev)[:, ::2])]
+
+
+def compaction(n_req, slots, dev="cpu"):
+    i32 = lambda n: torch.zeros(n, dtype=torch.int32, device=dev)  # noqa: E731
+    return dict(keep_off=i32(n_req + 1), keep_pages=i32(slots), keep_valid=i32(slots), new_len=i32(n_req), n_pages_kept=i32(n_req))
+
+
+def wrong_compaction(n_req, slots, dev):
+    good = compaction(n_req, slots, dev)
+    return [(name, t) for name in good for t in ((good[name].long(), torch.zeros(2 * slots + 4, dtype=torch.int32, device=dev)[::2]) +
+                                                 (() if name == "keep_pages" else (good[name][:-1],)))]
+
+
+def test_attention_and_compaction_take_tensors_for_what_they_are():
+    m = Model(8, 2, 64, V)
+    ctx = SimpleNamespace(model=m, device=-1)
+    good, keep = attention(5, m), compaction(3, 17)
+    B._check_attention(ctx, 5, **good)
+    B._check_attention(ctx, 5, good["q"].view(5, -1), good["out"].view(-1), None)
+    B._check_attention(ctx, 4, **good)  # rows behind the last are left alone
+    B._check_compact(ctx, 3, **keep)
+    for name, t in wrong_attention(5, m, "cpu"):
+        with pytest.raises(ValueError, match=f"lr_verify_attention_fp8: {name}"):
+            B._check_attention(ctx, 5, **dict(good, **{name: t}))
+    for name, t in wrong_compaction(3, 17, "cpu"):
+        with pytest.raises(ValueError, match=f"lr_compact_fp8: {name}"):
+            B._check_compact(ctx, 3, **dict(keep, **{name: t}))
+    elsewhere = SimpleNamespace(model=m, device=0)
+    for call in (lambda: B._check_attention(elsewhere, 5, **good), lambda: B._check_compact(elsewhere, 3, **keep)):
+        with pytest.raises(ValueError):
+            call()
+
+
+@pytest.mark.gpu
+def test_attention_and_compaction_refuse_before_they_launch():
+    w = make_config(2, with_logits=False)
+    b, dev = w.batch, "cuda:0"
+    ctx = B.Context(b.model, 0)
+    plan, cache = B.Plan(ctx, b), B.Fp8Cache.empty(b.model, b.n_pool_pages)
+    rows = int(b.cu_q[-1])
+    for name, t in wrong_attention(rows, b.model, dev) + [(n, attention(rows, b.model)[n]) for n in ("q", "out", "lse")]:
+        a = dict(attention(rows, b.model, dev), **{name: t})
+        with pytest.raises(ValueError, match=f"lr_verify_attention_fp8: {name}"):
+            plan.lr_verify_attention_fp8(a["q"], cache, a["out"], a["lse"])
+    here = compaction(b.n_req, b.n_page_slots)
+    for name, t in wrong_compaction(b.n_req, b.n_page_slots, dev) + list(here.items()):
+        a = dict(compaction(b.n_req, b.n_page_slots, dev), **{name: t})
+        with pytest.raises(ValueError, match="lr_compact_fp8: "):
+            plan.lr_compact_fp8(a["keep_off"], a["keep_pages"], a["keep_valid"], cache, a["new_len"], a["n_pages_kept"])
+    assert ctx.launch_count == 0
+    plan.close()
     ctx.close()
