@@ -78,7 +78,7 @@ attn_fp8_generic_kernel(DevBatch d, const uint16_t *__restrict__ q, const uint8_
         float a0 = 0.f, a1 = 0.f;
 #pragma unroll
         for (int c = 0; c < D / 16; ++c) {
-          const uint4 kk = __ldg(kp + c);
+          const uint4 kk = __ldcg(kp + c);
           const uint32_t w[4] = {kk.x, kk.y, kk.z, kk.w};
           const float *qq = &sq[warp][c * 16];
 #pragma unroll
@@ -110,11 +110,11 @@ attn_fp8_generic_kernel(DevBatch d, const uint16_t *__restrict__ q, const uint8_
         if (!((live >> j) & 1u)) continue;
         const uint8_t *vp = vpool + aj * D + lane * EPL;
         if constexpr (EPL == 2) {
-          const float2 x = fp8_float2(__ldg(reinterpret_cast<const uint16_t *>(vp)));
+          const float2 x = fp8_float2(__ldcg(reinterpret_cast<const uint16_t *>(vp)));
           acc[0] = fmaf(pj, x.x, acc[0]);
           acc[1] = fmaf(pj, x.y, acc[1]);
         } else {
-          const uint32_t vv = __ldg(reinterpret_cast<const uint32_t *>(vp));
+          const uint32_t vv = __ldcg(reinterpret_cast<const uint32_t *>(vp));
           const float2 x = fp8_float2(vv & 0xFFFFu), y = fp8_float2(vv >> 16);
           acc[0] = fmaf(pj, x.x, acc[0]);
           acc[1] = fmaf(pj, x.y, acc[1]);

@@ -16,7 +16,7 @@
 // scatter) with the bytes read and written twice, one layer of 8 ragged requests took 16.3 us on a B200, this takes 4.1.
 #include <algorithm>
 
-#include "lr_common.cuh"
+#include "fp8_cache.cuh"
 
 namespace lr {
 
@@ -37,7 +37,7 @@ __device__ __forceinline__ void move_rounds(const DevBatch &d, uint4 *pool, uint
   const int total = ((n_here - first) * kPage) << shift;
   for (int at = 0; at < total; at += kThreads * kRows) {
     uint4 v[kRows];
-    uint8_t byte[kRows];
+    uint32_t byte[kRows];
     int64_t to[kRows];
 #pragma unroll
     for (int u = 0; u < kRows; ++u) {
@@ -65,8 +65,12 @@ __device__ __forceinline__ void move_rounds(const DevBatch &d, uint4 *pool, uint
         continue;
       }
       const int64_t from = (src_page * d.n_kv_heads + h) * kPage + t;
-      v[u] = pool[from * vec_per_row + c];
-      if (kScales && c == 0) byte[u] = scale[from];
+      if constexpr (kScales) {
+        v[u] = __ldcg(pool + from * vec_per_row + c);
+        if (c == 0) byte[u] = ld_scale(scale + from);
+      } else {
+        v[u] = pool[from * vec_per_row + c];
+      }
       to[u] = ((dst_page * d.n_kv_heads + h) * kPage + k % kPage) * vec_per_row + c;
     }
     __syncthreads();  // the round is in registers
@@ -74,7 +78,7 @@ __device__ __forceinline__ void move_rounds(const DevBatch &d, uint4 *pool, uint
     for (int u = 0; u < kRows; ++u)
       if (to[u] >= 0) {
         pool[to[u]] = v[u];
-        if (kScales && (to[u] & (vec_per_row - 1)) == 0) scale[to[u] >> (31 - __clz(vec_per_row))] = byte[u];  // (4 or 8 to a row)
+        if (kScales && (to[u] & (vec_per_row - 1)) == 0) scale[to[u] >> (31 - __clz(vec_per_row))] = (uint8_t)byte[u];  // (4 or 8 to a row)
       }
   }
 }

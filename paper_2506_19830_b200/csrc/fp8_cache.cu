@@ -125,7 +125,7 @@ fp8_read_kernel(Fp8Rows w, uint16_t *__restrict__ k, uint16_t *__restrict__ v, c
 #pragma unroll
   for (int side = 0; side < 2; ++side)
 #pragma unroll
-    for (int h = 0; h < 2; ++h) c[side][h] = __ldg(reinterpret_cast<const uint2 *>((side != 0 ? v_pool : k_pool) + r.at * kD) + part + h * kLanes);
+    for (int h = 0; h < 2; ++h) c[side][h] = __ldcg(reinterpret_cast<const uint2 *>((side != 0 ? v_pool : k_pool) + r.at * kD) + part + h * kLanes);
   const float by[2] = {fp8_scale(ld_scale(k_scale + r.at)), fp8_scale(ld_scale(v_scale + r.at))};
 #pragma unroll
   for (int side = 0; side < 2; ++side)

@@ -16,8 +16,9 @@ __device__ __forceinline__ float fp8_scale(uint32_t byte) {
   return __uint_as_float(byte == kFp8NanScale ? 0x7FC00000u : byte == 0u ? 0x00400000u : byte << 23);
 }
 
-// A scale byte, from L2: a line of them holds those of other sequences' tokens too, so that a kernel on another stream may have brought it into this SM's L1 before
-// the kernel in front of this one wrote there.
+// What a kernel reads of the cache it reads from L2 (this, __ldcg, copies that pass L1 by), whichever kernel it is.  Its blocks are there before the kernel in front of
+// it has ended, which may be the one that writes the rows: the read-only path is for what does not change while a grid lives.  And 32 bytes of scales hold
+// those of two heads, or of two pages, which may be another sequence's: a kernel on another stream may have brought them into this SM's L1 before they were written.
 __device__ __forceinline__ uint32_t ld_scale(const uint8_t *p) {
   uint32_t v;
   asm volatile("ld.global.cg.u8 %0, [%1];" : "=r"(v) : "l"(p));
