@@ -272,18 +272,21 @@ drafted_walk_kernel(Rows tp, Rows tq, int32_t vocab, const float2 *stats, int32_
   if (warp == 0) {  // the first refused row of the cluster's warps
     int32_t best = 0x7FFFFFFF;
     uint32_t at = 0;
+    const int warps = few ? kTeam : kCluster * kTeam;  // of this CTA alone, or of all
 #pragma unroll
     for (int k = 0; k < kCluster * kTeam / 32; ++k) {
       const int w = k * 32 + lane;
-      const uint32_t from = in_cta(&s_stop[w % kTeam], few ? rank : w / kTeam);
-      const int32_t i = ld_cluster_i32(from);
-      if (i < best) {
-        best = i;
-        at = from;
+      if (w < warps) {
+        const uint32_t from = in_cta(&s_stop[w % kTeam], few ? rank : w / kTeam);
+        const int32_t i = ld_cluster_i32(from);
+        if (i < best) {
+          best = i;
+          at = from;
+        }
       }
     }
     const int32_t n = __reduce_min_sync(0xFFFFFFFFu, best);
-    if (best == n) {  // one lane: rows are apart
+    if (best == n) {  // one lane: a row is one warp's, and a warp is looked at once
       s_at.i = n;
       s_at.p.m = ld_cluster_f32(at + 4);
       s_at.p.inv = ld_cluster_f32(at + 8);
