@@ -435,8 +435,8 @@ int launch_accept_drafted(lr_ctx *ctx, const void *logits, int64_t stride, const
   }
   const int32_t vocab = ctx->model.vocab;
   const int chunk = chunk_steps(vocab), n_chunks = (int)(((int64_t)vocab + (int64_t)chunk * kStep - 1) / ((int64_t)chunk * kStep));
-  const Rows p = {reinterpret_cast<const uint16_t *>(logits), stride, 1.4426950408889634f / temperature};
-  const Rows q = {reinterpret_cast<const uint16_t *>(draft_logits), draft_stride, 1.4426950408889634f / draft_temperature};
+  const Rows p = {reinterpret_cast<const uint16_t *>(logits), stride, log2_scale(temperature)};
+  const Rows q = {reinterpret_cast<const uint16_t *>(draft_logits), draft_stride, log2_scale(draft_temperature)};
   auto *st = reinterpret_cast<float2 *>(scratch);
   const uint32_t total = ((uint32_t)n_rows + (uint32_t)(n_rows - n_branch)) * (uint32_t)n_chunks;  // at most 2 * 65535 * kMaxChunks
   const unsigned grid = std::min((total + kWarps - 1) / kWarps, (uint32_t)(ctx->sm_count * kCtasPerSm));

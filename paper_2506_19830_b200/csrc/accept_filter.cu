@@ -1226,7 +1226,7 @@ int launch_accept_filtered(lr_ctx *ctx, const void *logits, int64_t stride, cons
                            const float *u_accept, const float *u_final, int32_t *n_accept, int32_t *final_id, float *p_draft,
                            int32_t *n_kept, void *scratch, cudaStream_t s) {
   const int32_t vocab = ctx->model.vocab;
-  const float k_log2 = 1.4426950408889634f / temperature;
+  const float k_log2 = log2_scale(temperature);
   const ScratchLayout L = filter_layout(vocab, n_rows);
   unsigned char *base = reinterpret_cast<unsigned char *>(scratch);
   auto *lg = reinterpret_cast<const uint16_t *>(logits);

@@ -273,7 +273,7 @@ int launch_accept_sample(lr_ctx *ctx, const void *logits, int64_t stride, const 
     set_error("lr_accept_sample: more than 65535 logits rows in one call");
     return LR_EUNSUPPORTED;
   }
-  const float k_log2 = 1.4426950408889634f / temperature;
+  const float k_log2 = log2_scale(temperature);
   auto *lg = reinterpret_cast<const uint16_t *>(logits);
   auto *st = reinterpret_cast<float2 *>(scratch);
   const uint32_t total = (uint32_t)n_rows * n_chunks;  // at most 65535 * kMaxChunks

@@ -49,8 +49,14 @@ __device__ __forceinline__ uint4 ld_stream(const uint4 *p) {
   return v;
 }
 
-// The pair of a chunk, by one warp: this lane starts at vector v0 of the row rp, and the warp takes `steps` steps.
-__device__ __forceinline__ float2 chunk_pair(const uint16_t *rp, int32_t vocab, int32_t v0, int steps, float k_log2) {
+// Where m log2(e) / T is this large nothing but a row's largest logits has any weight: two bf16 numbers that differ do so by 2^-8 of the larger at least, an exponent of
+// -2^22 there.  What `off` below is rounded by is all that is left of it, and passes the range of the exponential from 2^31 on: such logits are counted, in a second
+// pass over the chunk that has them.  (As a branch in the first, 4 % of its time.)
+constexpr float kCold = 0x1p30f;
+
+// The pair of a chunk, by one warp: this lane starts at vector v0 of the row rp, and the warp takes `steps` steps.  worst: the largest magnitude that `off` had.
+template <bool kCounts>
+__device__ __forceinline__ float2 chunk_pair_as(const uint16_t *rp, int32_t vocab, int32_t v0, int steps, float k_log2, float &worst) {
   const int32_t n_vec = vocab >> 3, rem = vocab & 7;
   constexpr uint32_t kNegInf2 = 0xFF80FF80u;
   // Of this lane's share of the chunk: the maximum, an exponent near -m * k_log2 and the sum of 2^(x * k_log2 + off).  `off` is
@@ -89,6 +95,14 @@ __device__ __forceinline__ float2 chunk_pair(const uint16_t *rp, int32_t vocab, 
     const float mn = fmaxf(m, fmaxf(bf_lo(mx), bf_hi(mx)));
     const float off_before = off;
     off = mn > -INFINITY ? -mn * k_log2 : 0.f;
+    if (!kCounts) worst = fmaxf(worst, fabsf(off));
+    if (kCounts && fabsf(off) >= kCold) {
+      if (m < mn) sum = 0.f;
+      m = mn;
+#pragma unroll
+      for (int i = 0; i < kVec * 4; ++i) sum += (bf_lo(x[i]) == mn ? 1.f : 0.f) + (bf_hi(x[i]) == mn ? 1.f : 0.f);
+      continue;
+    }
     float a0 = 0.f, a1 = 0.f, a2 = 0.f, a3 = 0.f;
 #pragma unroll
     for (int i = 0; i < kVec * 4; i += 2) {
@@ -104,9 +118,19 @@ __device__ __forceinline__ float2 chunk_pair(const uint16_t *rp, int32_t vocab, 
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) M = fmaxf(M, __shfl_xor_sync(0xFFFFFFFFu, M, o));
   float S = m > -INFINITY ? sum * ex2_approx(-fmaf(M, k_log2, off)) : 0.f;
+  if (kCounts && fabsf(off) >= kCold) S = m == M ? sum : 0.f;
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) S += __shfl_xor_sync(0xFFFFFFFFu, S, o);
   return make_float2(M, S);
+}
+__device__ __noinline__ float2 chunk_pair_cold(const uint16_t *rp, int32_t vocab, int32_t v0, int steps, float k_log2) {
+  float none = 0.f;
+  return chunk_pair_as<true>(rp, vocab, v0, steps, k_log2, none);
+}
+__device__ __forceinline__ float2 chunk_pair(const uint16_t *rp, int32_t vocab, int32_t v0, int steps, float k_log2) {
+  float worst = 0.f;
+  const float2 pair = chunk_pair_as<false>(rp, vocab, v0, steps, k_log2, worst);
+  return __any_sync(0xFFFFFFFFu, worst >= kCold) ? chunk_pair_cold(rp, vocab, v0, steps, k_log2) : pair;
 }
 
 // steps of kStep logits per chunk

@@ -332,6 +332,8 @@ inline cudaError_t launch_dependent(void (*kernel)(KArgs...), dim3 grid, dim3 bl
   cfg.numAttrs = 1;
   return cudaLaunchKernelEx(&cfg, kernel, static_cast<KArgs>(args)...);
 }
+// log2(e) / T, as far as fp32 goes (it ends below T = 2^-127.5: an infinity would make a row's largest logit, less itself, a NaN)
+inline float log2_scale(float temperature) { return fminf(1.4426950408889634f / temperature, 3.402823466e38f); }
 int cuda_fail(cudaError_t e, const char *what);
 
 // kernels (each file exposes launchers)
