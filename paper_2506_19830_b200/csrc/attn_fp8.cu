@@ -12,13 +12,14 @@
 // e4m3 would leave 2^-10.  Two products at twice f16's rate take what one would.  A key's scale multiplies its column of S, before masks and maximum.
 //
 // Weights and V are f16.  One instruction turns two codes into two halves; a bf16 operand would take five.  Scales being powers of two, only differences
-// of exponents go into a tile: with ref the largest scale byte of a half-tile's keys, a row of V enters as code * 2^(byte - ref), exact unless it lies
-// 2^-33 below the largest number of the half-tile.  2^(ref - 127) itself goes into the exponent of the weights, P 2^(ref - base), where base is the
-// stream's: the accumulator is in units of 2^(base - 127).  When ref is more than 2^3 above base the accumulator is scaled down, as when the maximum
-// grows; the row sums take the factor back out.  A half-tile far below base (2^-24) sums its weights apart, as keys whose values are all zeros
-// may have any weight.  Weights lie 2^6 above what they are and reach 2^15 at most: 11 bits instead of bf16's 8, nothing lost above 2^-20 of the
-// largest, and a row whose scores grow by more than 2^6 does its half-tile again.
-//
+// of exponents go into a tile: with ref the largest scale byte of a half-tile's keys, a row of V enters as code * 2^(byte - ref).  That is exact for rows down to
+// 2^-15 of ref's scale; below, the factor still is to 2^-24, the products are multiples of 2^-24 (of 448 at the most), and a row further down becomes zeros: 2^-24 of the
+// largest number.  2^(ref - 127) itself goes into the exponent of the weights, P 2^(ref - base), where base is the stream's: the accumulator is in units of
+// 2^(base - 127).  base is set one above the first ref; when a ref is more than kRise above it the accumulator is scaled down, as when the maximum
+// grows; the row sums take the factor back out.  A half-tile more than kApart below base sums its weights apart, as keys whose values are all zeros
+// may have any weight.  Weights lie 2^kHead above what they are; a row's reference is 2^kLift above its maximum, and a half-tile whose scores are more than 2^kGrow
+// above the reference is done again: 2^15 at most, and eleven bits down to 2^-14.  Below, a weight is a multiple of 2^-24, off by 2^-25 at most.  That is 2^-25 x 448 x 2^(base - 127 - kHead)
+// of an output whose row sum is 2^-kLift, the least it can be; the largest number of V is above 224 x 2^(base - 1 - 127), so 2^(kLift - kHead - 23) of it.
 // One CTA = 16 warps in four warpgroups, registers moved with setmaxnreg (168 x 256 + 88 x 256 = 128 x 512):
 //   warps 8-11  converters, each with every fourth half-tile (64 keys): the codes of V by asynchronous copies into a buffer of the warp's own, the next
 //                one's taking the place of each part as it is read; halves into the ring as the swizzled operand.  A warp has the half-tile's scale
@@ -33,8 +34,9 @@
 // warps of a scheduler need 1,024: all roles share an SM's instruction cache, of which 2,048 instructions are fast, and code that runs once a
 // half-tile comes at some eight cycles an instruction.  So loops are rolled, what is rare is in functions, and what runs once a piece is short.  A version
 // with everything unrolled and in line, K converted to halves as well, took three times as long.
-// Measured: 96 query tokens of 32 heads over 32 K keys 83 us (31 for the products), a serving batch of 16 requests 207 us (65), 8 trees of 64-wide heads 151 us (28),
-// one token over 250 keys 11.4 us; 64 single tokens over 1024 keys each 79 us with head size 128 (93 without sharing the keys), 62 us with 64 (83).
+// Measured: 96 query tokens of 32 heads over 32 K keys 87 us (31 for the products), a serving batch of 16 requests 214 to 226 us (65), 8 trees of 64-wide heads 154 us (28),
+// one token over 250 keys 11.7 us; 64 single tokens over 1024 keys each 84 us with head size 128 (93 without sharing the keys), 64 us with 64 (83).  Looking for rows that
+// the terms of Q fall short of takes 1 to 2 % of it, 6 of the last; with every row gone through again the first takes 23 ms.
 //
 // A visible row that stands for NaN: K's has a scale of NaN, and with it the row's sum is.  V's becomes zeros, for a weight of 0 times NaN
 // would reach rows that do not see it; the converter notes such keys per half-tile, and a row that sees one multiplies its result by NaN.
@@ -92,8 +94,12 @@ struct Plain {  // what exact_rows needs of the call
   const uint8_t *k, *v, *k_scale, *v_scale;
   uint16_t *out;
   float *lse, *partial_o, *partial_ml;
+  const TcPage *pages;
+  const TcRow *rows;
+  const TcPiece *pieces;
+  const TcReq *reqs;
   int64_t n_pool_pages;
-  int32_t n_kv_heads;
+  int32_t n_q_heads, n_kv_heads, group, tokens_per_mtile;
   float scale_log2;
 };
 
@@ -113,7 +119,7 @@ struct __align__(16) Ctrl {
   uint64_t alive_ns;      // when a warp was last seen at work that may take longer than a wait (exact_rows)
   int32_t *status;        // the plan's
   Plain plain;
-  uint8_t xch_exact[128];
+  int32_t xch_k;          // stream 1's largest scale byte of K
   float xch_m[128], xch_l[128], xch_unit[128];  // stream 1's rows, for the in-CTA combination
   // What the rows of Q were divided by and (in such units) what their terms may be off by, summed over the channels, of two pieces in turn: the queries of a piece are written when both streams have asked for the last scores of the piece
   // before, and a stream asks for its first behind the weights of the one before that, which its threads had to know this for.
@@ -126,6 +132,8 @@ constexpr int kJoinBytes = 4 * 32 * kJoinRow * 4;
 template <int kD>
 constexpr int kSmemBytes = 2 * Shape<kD>::kQBytes + Shape<kD>::kKStages * Shape<kD>::kCodeBytes + Shape<kD>::kVStages * Shape<kD>::kVBytes +
                            kTeams * Shape<kD>::kCodeBytes + kJoinBytes + kCtrlBytes;  // the base must be 1024-aligned
+static_assert(kGrow + kHead + kRise <= 15.0f, "the largest weight as a half");
+static_assert(kLift <= kHead, "what a key's part of an output may be off by, 2^-23 of the largest number of V: see above");
 static_assert(kInfos - Shape<64>::kKStages >= 6 && kInfos - Shape<128>::kKStages >= 6, "see kInfos");
 // A converter at position r of a ring has filled position r - kTeams, whose stage position r - kTeams - stages had been released from.  Releases are in
 // order, so with no more teams than stages the release before the one it waits for has happened, and the parity of the barrier means what it
@@ -390,13 +398,15 @@ __device__ __noinline__ void convert_q(const uint16_t *__restrict__ q, int64_t q
         hi[j] = pack_e4m3(x0, x1, x2, x3);
         const float2 h0 = fp8_float2(hi[j] & 0xFFFFu), h1 = fp8_float2(hi[j] >> 16);
         lo[j] = pack_e5m2(x0 - h0.x, x1 - h0.y, x2 - h1.x, x3 - h1.y);
-        small += __popc(~((hi[j] & 0x7F7F7F7Fu) + 0x77777777u) & 0x80808080u) << (16 * b);  // codes below 9, where 8 is 2^-6
       }
       if (p + sub < n) {
         const uint32_t at = tile + row_unit<kD>(r0 + p + sub, c >> 1) + (c & 1) * 8;
         st_shared2(at, hi[0], hi[1]);
         st_shared2(at + Shape<kD>::kTermBytes, lo[0], lo[1]);
         if (c == 0) unit[r0 + p + sub] = make_float2(top[b] < 0x7F80u ? pow2(e) : __uint_as_float(0x7FC00000u), 0.f);
+        // codes below 9, where 8 is 2^-6
+        const uint32_t few0 = ~((hi[0] & 0x7F7F7F7Fu) + 0x77777777u) & 0x80808080u, few1 = ~((hi[1] & 0x7F7F7F7Fu) + 0x77777777u) & 0x80808080u;
+        small += __popc(few0 | few1 >> 1) << (16 * b);
       }
     }
     if (__any_sync(0xFFFFFFFFu, small != 0u)) {
@@ -546,22 +556,28 @@ struct Fp8Pools {  // (K's codes are behind a tensor map too)
   const uint8_t *k, *v, *k_scale, *v_scale;
 };
 
-// Rows of a piece whose scores the terms of Q might put off by more than kScoreTol, one after another by a whole warp on the CUDA cores, with Q as it is: what
-// store_rows or join_rows would have left for them.  `rows`: the lanes whose rows they are, ri theirs; row0: of lane 0's row in the M-tile.  As attn_fp8_generic.cu, from
-// which it differs in the order of keys alone; that kernel has all of an SM's warps for it.
+// Rows whose scores the terms of Q might put off by more than kScoreTol, one after another by a whole warp on the CUDA cores, with Q as it is: what store_rows or
+// join_rows would have left for them.  rows: the lanes whose rows they are; s: the stream; split: whether four warps have the same rows.  As
+// attn_fp8_generic.cu, from which it differs in the order of keys alone; that kernel has all of an SM's warps for it.
 template <int kD>
-__device__ __noinline__ void exact_rows(uint32_t rows, RowInfo ri, const TcPage *__restrict__ pages, int n_tiles, int n_dense, int kv_head, int slot, int row0) {
+__device__ __noinline__ void exact_rows(uint32_t rows, int pc, int s, bool split) {
   constexpr int kEach = kD / 32;  // output channels of a lane
   Ctrl *ctrl = ctrl_at<kD>();
-  const Plain in = ctrl->plain;
-  const int lane = threadIdx.x & 31;
+  const Plain &in = ctrl->plain;
+  const int lane = threadIdx.x & 31, row0 = split ? 0 : ((threadIdx.x >> 5) & 3) * 32;
+  const TcPiece pi = in.pieces[pc];
+  const TcReq rq = in.reqs[pi.req];
+  const int n_tiles = pi.tile_end - pi.tile_begin, n_dense = rq.n_dense_tiles - pi.tile_begin, kv_head = pi.kv_head, slot = pi.slot[pi.n_mt == 2 ? s : 0];
+  const TcPage *pages = in.pages + rq.page_off + pi.tile_begin * kPagesPerTile;
+#pragma unroll 1
   for (; rows != 0u; rows &= rows - 1u) {
     const int i = __ffs(rows) - 1;
-    RowInfo one;
-    one.depth = __shfl_sync(0xFFFFFFFFu, ri.depth, i);
-    one.branch = __shfl_sync(0xFFFFFFFFu, ri.branch, i);
-    one.limit = __shfl_sync(0xFFFFFFFFu, ri.limit, i);
-    one.q_index = __shfl_sync(0xFFFFFFFFu, ri.q_index, i);
+    DevBatch d;
+    d.group = in.group;
+    d.n_q_heads = in.n_q_heads;
+    DevTcPlan tc;
+    tc.rows = in.rows;
+    const RowInfo one = row_info(d, tc, rq, in.tokens_per_mtile, pi.n_mt == 2 ? pi.mtile0 + s : pi.mtile0, row0 + i, kv_head);
     const uint4 *qp = reinterpret_cast<const uint4 *>(in.q + one.q_index * kD);
     float m = -INFINITY, l = 0.f, acc[kEach];
 #pragma unroll
@@ -589,7 +605,7 @@ __device__ __noinline__ void exact_rows(uint32_t rows, RowInfo ri, const TcPage 
         for (int c = 0; c < kD / 16; ++c) code[c] = __ldcg(kp + c);
 #pragma unroll
         for (int c = 0; c < kD / 16; ++c) {
-          const uint4 kk = code[c], qa = __ldg(qp + 2 * c), qb = __ldg(qp + 2 * c + 1);
+          const uint4 kk = code[c], qa = qp[2 * c], qb = qp[2 * c + 1];
           const uint32_t w[4] = {kk.x, kk.y, kk.z, kk.w}, x[8] = {qa.x, qa.y, qa.z, qa.w, qb.x, qb.y, qb.z, qb.w};
 #pragma unroll
           for (int j = 0; j < 4; ++j) {
@@ -736,7 +752,9 @@ attn_fp8_kernel(const __grid_constant__ CUtensorMap k_map, DevBatch d, DevTcPlan
     ctrl->status = d.status;
     fence_barrier_init();
   }
-  if (threadIdx.x == 32) ctrl->plain = Plain{q, in.k, in.v, in.k_scale, in.v_scale, out, lse, tc.partial_o, tc.partial_ml, d.n_pool_pages, d.n_kv_heads, scale_log2};
+  if (threadIdx.x == 32)
+    ctrl->plain = Plain{q, in.k, in.v, in.k_scale, in.v_scale, out, lse, tc.partial_o, tc.partial_ml, tc.pages, tc.rows, tc.pieces, tc.reqs, d.n_pool_pages,
+                        d.n_q_heads, d.n_kv_heads, d.group, tc.tokens_per_mtile, scale_log2};
   if (warp == 12) {
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&ctrl->tmem_base)), "r"(512u)
                  : "memory");
@@ -1053,7 +1071,7 @@ attn_fp8_kernel(const __grid_constant__ CUtensorMap k_map, DevBatch d, DevTcPlan
       const int my_units = mode == 2 ? n : (n - s + 1) / 2;
       const bool split = kFew && shares_keys(pi, rq, T, d.group);
       const RowInfo ri = row_info(d, tc, rq, T, mode == 2 ? pi.mtile0 + s : pi.mtile0, split ? lane : r, pi.kv_head);
-      float sc_row = 0.f, q_off = 0.f;  // q_off: what the terms of Q leave of the row, times what its scores are multiplied by
+      float sc_row = 0.f;
       if (ok) {
         // the queries, once the products of the piece before no longer read the buffers; of one M-tile each stream takes half of every warp's rows.
         // Padding is left as it is: what comes of it reaches rows that nobody reads.
@@ -1065,10 +1083,7 @@ attn_fp8_kernel(const __grid_constant__ CUtensorMap k_map, DevBatch d, DevTcPlan
           fence_proxy_async();
           mbar_arrive(&ctrl->q_full);
           ok = wait<kD, 0>(&ctrl->q_full, (uint32_t)(pc - piece0) & 1u, 246);
-          if (ok && ri.q_index >= 0) {
-            sc_row = scale_log2 * unit[r].x;
-            q_off = sc_row * unit[r].y;
-          }
+          if (ok && ri.q_index >= 0) sc_row = scale_log2 * unit[r].x;
         }
       }
       if (ok && my_units > 0) {
@@ -1310,8 +1325,6 @@ attn_fp8_kernel(const __grid_constant__ CUtensorMap k_map, DevBatch d, DevTcPlan
         }
         // what the accumulator's numbers are worth; NaN for a row that sees a row of V that is
         const float unit = nan_v ? __uint_as_float(0x7FC00000u) : exp2f((float)(base - 127) - kHead);
-        // A key's codes are 448 at most: no score of the row is off by more than this.
-        bool exact = q_off * 448.0f * pow2(k_top - 127) > kScoreTol;
         // The two streams of a one-M-tile piece hold partial results of the same rows (even and odd tiles).
         // Stream 1 publishes its sums; stream 0 reads them and stream 1's accumulator -- the same tensor-memory
         // lanes, so the thread of row r can load both -- and writes one combined result.
@@ -1323,7 +1336,7 @@ attn_fp8_kernel(const __grid_constant__ CUtensorMap k_map, DevBatch d, DevTcPlan
             ctrl->xch_m[r] = m_used;
             ctrl->xch_l[r] = l;
             ctrl->xch_unit[r] = unit;
-            ctrl->xch_exact[r] = exact;
+            if (r == 0) ctrl->xch_k = k_top;
             tc_fence_before();
             mbar_arrive(&ctrl->xch);
             writer = false;
@@ -1338,12 +1351,16 @@ attn_fp8_kernel(const __grid_constant__ CUtensorMap k_map, DevBatch d, DevTcPlan
               self = l != 0.f ? unit * w_self : 0.f;
               other = other_live ? ctrl->xch_unit[r] * w_other : 0.f;
               l_out = w_self * l + w_other * ol;
-              exact = exact || ctrl->xch_exact[r] != 0;
+              k_top = max(k_top, ctrl->xch_k);
             }
           }
         }
         if (pair) ++x_cnt;
-        const int64_t q_index = exact ? -1 : ri.q_index;
+        // A key's codes are 448 at most: no score of the row is off by more than this.  (What the terms leave is looked up here: one more register through the sweep, or
+        // more for exact_rows to be given, costs short pieces 5 %.)
+        uint32_t again = __ballot_sync(0xFFFFFFFFu, writer && ri.q_index >= 0 &&
+                                                        sc_row * ctrl->q_unit[(pc - piece0) & 1][mode == 2 ? s : 0][r].y * 448.0f * pow2(k_top - 127) > kScoreTol);
+        const int64_t q_index = (again >> lane) & 1u ? -1 : ri.q_index;
         if (kFew && ok && writer && split) {
           tc_fence_after();
           ok = join_rows<kD>(o_addr, lane_base + 256 + 128, pi.slot[0], self, other, other_live, m_out, l_out, quarter, q_index, joins, out, lse, tc.partial_o, tc.partial_ml);
@@ -1354,13 +1371,8 @@ attn_fp8_kernel(const __grid_constant__ CUtensorMap k_map, DevBatch d, DevTcPlan
                          tc.partial_o, tc.partial_ml);
           tc_fence_before();
         }
-        if (ok && writer) {
-          uint32_t again = __ballot_sync(0xFFFFFFFFu, exact && ri.q_index >= 0);
-          if (split) again &= 0x11111111u << quarter;  // the four warps have the same rows
-          if (again != 0u)
-            exact_rows<kD>(again, ri, tc.pages + rq.page_off + pi.tile_begin * kPagesPerTile, n, rq.n_dense_tiles - pi.tile_begin, pi.kv_head, pi.slot[pair ? 0 : s],
-                           split ? 0 : quarter * 32);
-        }
+        if (split) again &= 0x11111111u << quarter;  // the four warps have the same rows
+        if (ok && writer && again != 0u) exact_rows<kD>(again, pc, s, split);
       }
       // One arrival per thread and piece.  A stream with units in this piece cannot get here before the previous
       // piece's phase is complete (its PV products were issued behind a wait for it); a stream with none must look
