@@ -223,7 +223,8 @@ class Fp8Cache:
                 raise ValueError(f"an 8-bit cache is codes [pages, KV heads, 16, head size] and scales [pages, KV heads, 16], contiguous, on one device: "
                                  f"got {tuple(t.shape)} {t.dtype} on {t.device}")
         self.k, self.v, self.k_scale, self.v_scale = k, v, k_scale, v_scale
-        self.n_pages, self.heads, self.head_dim, self.device, self.index = shape[0], shape[1], shape[3], k.device, k.device.index
+        self.n_pages, self.heads, self.head_dim, self.device = shape[0], shape[1], shape[3], k.device
+        self.kind = (self.heads, self.head_dim, k.device.index)  # what a context has to have, too
         self._c = lr_fp8_cache(k.data_ptr(), v.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr(), shape[0])
         self.c = C.addressof(self._c)
 
@@ -237,8 +238,8 @@ class Fp8Cache:
 
 def _check_cache(cache: Fp8Cache, ctx: "Context") -> None:
     # what the C side cannot see: how large the tensors behind its pointers are, and where
-    m = ctx.model
-    if cache.heads != m.n_kv_heads or cache.head_dim != m.head_dim or cache.index != ctx.device:
+    if cache.kind != ctx.cache_kind:
+        m = ctx.model
         raise ValueError(f"the cache has {cache.heads} heads of {cache.head_dim} on {cache.device}, the context {m.n_kv_heads} of {m.head_dim} on cuda:{ctx.device}")
 
 
@@ -301,20 +302,22 @@ def _check_drafted(ctx: "Context", logits, draft_logits, draft_ids, cu_draft, u_
 
 
 # (These run before every launch, where each look at a tensor takes a twentieth of a microsecond: all of them in one expression, and who is at fault only then.)
-def _check_attention(ctx: "Context", n_q_rows: int, q, out, lse) -> None:
+def _check_attention(ctx: "Context", n_q_rows: int, q, out, lse) -> tuple:
+    """The addresses of the tensors of an attention call, found to be what the C side takes them for."""
     m, dev = ctx.model, ctx.device
     n = n_q_rows * m.n_q_heads
     if (q is not None and out is not None and lse is not None and q.dtype is out.dtype is torch.bfloat16 and lse.dtype is torch.float32
             and q.get_device() == out.get_device() == lse.get_device() == dev and q.is_contiguous() and out.is_contiguous() and lse.is_contiguous()
             and q.numel() >= n * m.head_dim <= out.numel() and lse.numel() >= n):
-        return
+        return q.data_ptr(), out.data_ptr(), lse.data_ptr()
     shape = f"[{n_q_rows}, {m.n_q_heads}"
     _refuse("lr_verify_attention_fp8", dev, q=(_flat(q, torch.bfloat16, n * m.head_dim, dev), q, f"contiguous bf16 {shape}, {m.head_dim}]"),
             out=(_flat(out, torch.bfloat16, n * m.head_dim, dev), out, f"contiguous bf16 {shape}, {m.head_dim}]"),
             lse=(_flat(lse, torch.float32, n, dev), lse, f"contiguous float32 {shape}]"))
+    return _ptr(q), _ptr(out), _ptr(lse)
 
 
-def _check_compact(ctx: "Context", n_req: int, keep_off, keep_pages, keep_valid, new_len, n_pages_kept) -> None:
+def _check_compact(ctx: "Context", n_req: int, keep_off, keep_pages, keep_valid, new_len, n_pages_kept) -> tuple:
     # (how much of the lists there is to read the offsets say, which are on the device)
     dev, i32 = ctx.device, torch.int32
     some = keep_off is not None and keep_pages is not None and keep_valid is not None and new_len is not None and n_pages_kept is not None
@@ -322,11 +325,12 @@ def _check_compact(ctx: "Context", n_req: int, keep_off, keep_pages, keep_valid,
             and keep_off.get_device() == keep_pages.get_device() == keep_valid.get_device() == new_len.get_device() == n_pages_kept.get_device() == dev
             and keep_off.is_contiguous() and keep_pages.is_contiguous() and keep_valid.is_contiguous() and new_len.is_contiguous() and n_pages_kept.is_contiguous()
             and keep_off.numel() > n_req <= new_len.numel() and n_pages_kept.numel() >= n_req and keep_valid.numel() >= keep_pages.numel()):
-        return
+        return keep_off.data_ptr(), keep_pages.data_ptr(), keep_valid.data_ptr(), new_len.data_ptr(), n_pages_kept.data_ptr()
     _refuse("lr_compact_fp8", dev, keep_off=(_flat(keep_off, i32, n_req + 1, dev), keep_off, f"int32 [{n_req + 1}]"),
             keep_pages=(_flat(keep_pages, i32, 0, dev), keep_pages, "int32 [page slots]"),
             keep_valid=(_flat(keep_valid, i32, 0 if keep_pages is None else keep_pages.numel(), dev), keep_valid, "int32, as long as keep_pages,"),
             new_len=(_flat(new_len, i32, n_req, dev), new_len, f"int32 [{n_req}]"), n_pages_kept=(_flat(n_pages_kept, i32, n_req, dev), n_pages_kept, f"int32 [{n_req}]"))
+    return _ptr(keep_off), _ptr(keep_pages), _ptr(keep_valid), _ptr(new_len), _ptr(n_pages_kept)
 
 
 class Context:
@@ -335,6 +339,7 @@ class Context:
     def __init__(self, model, device: int = 0):
         self.model = model
         self.device = device
+        self.cache_kind = (int(model.n_kv_heads), int(model.head_dim), device)
         h = C.c_void_p()
         m = _model_struct(model)
         _check(lib().lr_create(C.byref(h), C.byref(m), device), "lr_create")
@@ -534,16 +539,16 @@ class Plan:
     def lr_verify_attention_fp8(self, q, cache: Fp8Cache, out, lse=None, softmax_scale: float = 0.0, stream=None) -> None:
         """``lr_verify_attention`` over an 8-bit cache."""
         _check_cache(cache, self.ctx)
-        _check_attention(self.ctx, self.n_q_rows, q, out, lse)
-        _check(lib().lr_verify_attention_fp8(self.handle, _ptr(q), cache.c, _ptr(out), _ptr(lse), float(softmax_scale),
-                                             _stream_on(self.ctx.device, stream)), "lr_verify_attention_fp8")
+        q_at, out_at, lse_at = _check_attention(self.ctx, self.n_q_rows, q, out, lse)
+        _check(lib().lr_verify_attention_fp8(self.handle, q_at, cache.c, out_at, lse_at, float(softmax_scale), _stream_on(self.ctx.device, stream)),
+               "lr_verify_attention_fp8")
 
     def lr_compact_fp8(self, keep_off, keep_pages, keep_valid, cache: Fp8Cache, new_len, n_pages_kept, stream=None) -> None:
         """``lr_compact`` over an 8-bit cache: codes and scales together."""
         _check_cache(cache, self.ctx)
-        _check_compact(self.ctx, self.n_req, keep_off, keep_pages, keep_valid, new_len, n_pages_kept)
-        _check(lib().lr_compact_fp8(self.handle, _ptr(keep_off), _ptr(keep_pages), _ptr(keep_valid), cache.c, _ptr(new_len), _ptr(n_pages_kept),
-                                    _stream_on(self.ctx.device, stream)), "lr_compact_fp8")
+        off_at, pages_at, valid_at, len_at, kept_at = _check_compact(self.ctx, self.n_req, keep_off, keep_pages, keep_valid, new_len, n_pages_kept)
+        _check(lib().lr_compact_fp8(self.handle, off_at, pages_at, valid_at, cache.c, len_at, kept_at, _stream_on(self.ctx.device, stream)),
+               "lr_compact_fp8")
 
     def lr_poll_status(self, stream=None) -> int:
         d = C.c_int32()
