@@ -459,8 +459,8 @@ typedef struct lr_fp8_cache {
  * alike.  slots_d[t] = page * 16 + place in the page; a negative slot leaves its
  * token out.  For each row x: e = the smallest integer >= -124 with
  * max|x| * 2^-e <= 448, codes = x * 2^-e rounded to nearest even, byte = e + 127;
- * a row that holds an infinity or a NaN gets codes 0 and byte 255.  Slots named
- * twice in a call hold bytes of either token.  A slot of n_pages * 16 or more is
+ * a row that holds an infinity or a NaN gets codes 0 and byte 255.  A slot named
+ * twice in a call holds bytes of both tokens, in any mixture.  A slot of n_pages * 16 or more is
  * skipped and, with status_d (nullable; two int32 that the caller sets to 0),
  * leaves {LR_EBOUNDS, its token} there.  Strides are multiples of 8 and not below
  * n_kv_heads * head_dim, k_d and v_d 16-byte aligned, else LR_EINVAL.

@@ -18,8 +18,10 @@
 // 2^(base - 127).  base is set one above the first ref; when a ref is more than kRise above it the accumulator is scaled down, as when the maximum
 // grows; the row sums take the factor back out.  A half-tile more than kApart below base sums its weights apart, as keys whose values are all zeros
 // may have any weight.  Weights lie 2^kHead above what they are; a row's reference is 2^kLift above its maximum, and a half-tile whose scores are more than 2^kGrow
-// above the reference is done again: 2^15 at most, and eleven bits down to 2^-14.  Below, a weight is a multiple of 2^-24, off by 2^-25 at most.  That is 2^-25 x 448 x 2^(base - 127 - kHead)
-// of an output whose row sum is 2^-kLift, the least it can be; the largest number of V is above 224 x 2^(base - 1 - 127), so 2^(kLift - kHead - 23) of it.
+// above the reference is done again: 2^15 at most, and eleven bits down to 2^-14.  Below, a weight is a multiple of 2^-24, off by 2^-25 at most.  In an output whose row
+// sum is 2^-kLift, the least it can be, that is 2^(kLift - 25) x 448 x 2^(base - 127 - kHead); the largest number of V is above 224 x 2^(base - 1 - 127), so it is
+// 2^(kLift - kHead - 23) of that.
+//
 // One CTA = 16 warps in four warpgroups, registers moved with setmaxnreg (168 x 256 + 88 x 256 = 128 x 512):
 //   warps 8-11  converters, each with every fourth half-tile (64 keys): the codes of V by asynchronous copies into a buffer of the warp's own, the next
 //                one's taking the place of each part as it is read; halves into the ring as the swizzled operand.  A warp has the half-tile's scale
