@@ -586,7 +586,7 @@ __device__ __noinline__ void exact_rows(uint32_t rows, int pc, int s, bool split
     for (int e = 0; e < kEach; ++e) acc[e] = 0.f;
 #pragma unroll 1
     for (int t = 0; t < 4 * n_tiles; ++t) {  // two pages, a key a lane
-      if (lane == 0 && (t & 255) == 0) *reinterpret_cast<volatile uint64_t *>(&ctrl->alive_ns) = global_ns();
+      if (lane == 0 && (t & 63) == 0) *reinterpret_cast<volatile uint64_t *>(&ctrl->alive_ns) = global_ns();
       const int2 e = ld_pair(pages + 2 * t + (lane >> 4));
       const int n_ok = (t >> 2) < n_dense ? kPage : page_n_ok((uint32_t)e.y, one);
       const bool valid = (lane & 15) < n_ok;

@@ -139,3 +139,29 @@ def test_such_rows_leave_the_same_bits_every_time():
     pools, _, _ = stored(w)
     got = [(R.bf16_bits(o), l.cpu().numpy().view(np.uint32)) for o, l in (run(w, pools, B.PATH_TENSOR_CORE) for _ in range(5))]
     assert all(np.array_equal(a, b) for g in got[1:] for a, b in zip(g, got[0]))
+
+
+def test_waits_for_such_rows_do_not_run_out():
+    """Going through the rows of a piece again takes longer than any wait may: who waits for it meanwhile sees that it goes on."""
+    w = with_outliers(chain([1024] * 220, 128, hq=4, h=1, q=64, seed=46), 20, 11)
+    b = w.batch
+    pools, k, v = stored(w)
+    ctx = B.Context(b.model, 0)
+    plan = B.Plan(ctx, b)
+    plan.lr_plan_set_attention_path(B.PATH_TENSOR_CORE)
+    assert plan.lr_plan_describe()["n_pieces"] > plan.lr_plan_describe()["n_cta"]  # some CTA has one piece behind another
+    q, cache = R.bf16_tensor(w.tensors.q, DEV), on_device(pools)
+    out, lse = torch.zeros_like(q), torch.zeros(q.shape[:2], device=DEV)
+    plan.lr_plan_debug_set_wait_limit(3000)
+    start, end = (torch.cuda.Event(enable_timing=True) for _ in range(2))
+    start.record()
+    plan.lr_verify_attention_fp8(q, cache, out, lse)
+    end.record()
+    assert plan.lr_poll_status() == 0
+    assert start.elapsed_time(end) > 6.0  # ms: twice the limit
+    some = [0, 57, 219]
+    rows = np.concatenate([np.arange(b.cu_q[i], b.cu_q[i + 1]) for i in some])
+    o_ref, l_ref = O.verify_attention(b, w.tensors.q, k, v, branches=some)
+    check_attention(out, lse, o_ref, l_ref, rows, REL_LARGE)
+    plan.close()
+    ctx.close()
