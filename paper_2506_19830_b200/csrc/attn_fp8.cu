@@ -123,8 +123,9 @@ struct __align__(16) Ctrl {
   Plain plain;
   int32_t xch_k;          // stream 1's largest scale byte of K
   float xch_m[128], xch_l[128], xch_unit[128];  // stream 1's rows, for the in-CTA combination
-  // What the rows of Q were divided by and (in such units) what their terms may be off by, summed over the channels, of two pieces in turn: the queries of a piece are written when both streams have asked for the last scores of the piece
-  // before, and a stream asks for its first behind the weights of the one before that, which its threads had to know this for.
+  // What the rows of Q were divided by and (in such units) what their terms may be off by, summed over the channels, of two pieces in turn: the queries of a piece are
+  // written when both streams have asked for the last scores of the piece before, and a stream asks for its first behind the weights of the one before that, which its
+  // threads had to know this for.
   float2 q_unit[2][2][128];
 };
 constexpr int kCtrlBytes = 11 << 10;
