@@ -501,6 +501,136 @@ int lr_verify_attention_fp8(lr_plan *plan, const void *q_d, const lr_fp8_cache *
 int lr_compact_fp8(lr_plan *plan, const int32_t *keep_off_d, const int32_t *keep_pages_d, const int32_t *keep_valid_d,
                    const lr_fp8_cache *cache, int32_t *new_len_d, int32_t *n_pages_kept_d, void *stream);
 
+/* ---- the same on a cache in 4 bits ------------------------------------------ */
+
+/*
+ * A KV cache in 4 bits: 68 bytes for a row of 128 channels, which take 256 in bf16.
+ * Pages, heads and token slots as in the bf16 pools, head_dim / 2 bytes a row; a
+ * scale byte for every 32 channels:
+ *     k_d, v_d              [n_pages][n_kv_heads][16][head_dim / 2] e2m1 codes
+ *     k_scale_d, v_scale_d  [n_pages][n_kv_heads][16][head_dim / 32] powers of two
+ *                           (e8m0): byte b stands for 2^(b - 127), 255 for NaN
+ * A code is 0, 1/2, 1, 3/2, 2, 3, 4 or 6 with a sign.  The codes of channels 8w .. 8w + 7
+ * are the 32-bit word w of a row: bits 4j .. 4j + 3 hold channel 8w + 2j for j < 4 and
+ * channel 8w + 2 (j - 4) + 1 above, so that neighbouring channels lie 16 bits apart.
+ * A channel's value is its code times its group's scale: a bf16 number (those that would
+ * be 2^128 are infinities), so what reads the cache rounds nothing a second time.  A row
+ * with a scale of 255 stands for NaN as a whole.  Scales of 0 are never written here; a
+ * visible row that has one has unspecified values.  The four pools are apart from one
+ * another and 16-byte aligned.  n_pages: pages in each pool.  All pointers are device
+ * pointers of the caller's; the struct is read during the call alone.
+ */
+typedef struct lr_fp4_cache {
+  void *k_d, *v_d;
+  uint8_t *k_scale_d, *v_scale_d;
+  int64_t n_pages;
+} lr_fp4_cache;
+
+/*
+ * lr_fp8_write and lr_fp8_read for such a cache: the same rows, strides, slots, status
+ * and errors.  For each group x of 32 channels: e = the smallest integer >= -126 with
+ * max|x| * 2^-e <= 6, codes = x * 2^-e rounded to nearest (ties to an even code), byte =
+ * e + 127; a row that holds an infinity or a NaN gets codes 0 and bytes 255.
+ */
+int lr_fp4_write(lr_ctx *ctx, const lr_fp4_cache *cache, const void *k_d, int64_t k_stride, const void *v_d, int64_t v_stride,
+                 const int64_t *slots_d, int32_t n_tokens, int32_t *status_d, void *stream);
+int lr_fp4_read(lr_ctx *ctx, const lr_fp4_cache *cache, const int64_t *slots_d, int32_t n_tokens, void *k_d, int64_t k_stride,
+                void *v_d, int64_t v_stride, int32_t *status_d, void *stream);
+
+/*
+ * lr_verify_attention on such a cache (cache->n_pages >= the plan's n_pool_pages, else
+ * LR_EINVAL): same plan, queries, outputs and errors, for a chain or a tree of draft
+ * steps.  Q, and K and V as the values they stand for, enter the products as bf16, which
+ * they are; numbers of K and V below 2^-117 count as 0.  Products are summed and the
+ * softmax is done in fp32; its weights enter the second product as bf16.  Slots that hold
+ * no token of the plan may hold anything.  A row of K or V that stands for NaN makes
+ * output and log-sum of a query that sees it NaN and does not touch the others.
+ * lr_plan_set_attention_path: 0 automatic, 1 CUDA cores, 2 tensor cores; there is no
+ * CTA-pair kernel for this cache (3: LR_EUNSUPPORTED).
+ */
+int lr_verify_attention_fp4(lr_plan *plan, const void *q_d, const lr_fp4_cache *cache, void *out_d, float *lse_d,
+                            float softmax_scale, void *stream);
+
+/* lr_compact on such a cache: codes and scales move together, bit for bit.  No
+ * scratch.  Errors as for lr_compact. */
+int lr_compact_fp4(lr_plan *plan, const int32_t *keep_off_d, const int32_t *keep_pages_d, const int32_t *keep_valid_d,
+                   const lr_fp4_cache *cache, int32_t *new_len_d, int32_t *n_pages_kept_d, void *stream);
+
+/* ---- a cache of any kind: rotary positions, pages ------------------------------ */
+
+/* The pools of one layer.  LR_KV_BF16: k_d and v_d as in "Data layout", no scales;
+ * LR_KV_FP8, LR_KV_FP4: as lr_fp8_cache and lr_fp4_cache. */
+enum { LR_KV_BF16 = 0, LR_KV_FP8 = 1, LR_KV_FP4 = 2 };
+typedef struct lr_kv_cache {
+  int32_t kind;
+  void *k_d, *v_d;
+  uint8_t *k_scale_d, *v_scale_d;
+  int64_t n_pages;
+} lr_kv_cache;
+
+/*
+ * Rotary positions.  Of a head's channels the first rot_dim (even) are turned in pairs:
+ * (i, i + rot_dim / 2), or (2i, 2i + 1) if interleaved.  A pair at position p becomes
+ *     (a cos - b sin, a sin + b cos) * amplitude   at the angle p * f_i,
+ * f_i = base^(-2i / rot_dim), stretched for contexts longer than `original` tokens:
+ *     LR_ROPE_PLAIN   f
+ *     LR_ROPE_LINEAR  f / factor
+ *     LR_ROPE_SMOOTH  f (1 - w) + f / factor w; w falls linearly from 1, where a pair turns
+ *                     `lo` times over the original length, to 0 at `hi` times
+ *     LR_ROPE_PARTS   the same with w rising linearly with i from the pair that turns `hi`
+ *                     times to the one that turns `lo` times, rounded down and up to whole
+ *                     numbers and kept within 0 and rot_dim - 1
+ * amplitude 0 selects 1, with LR_ROPE_PARTS 0.1 ln(factor) + 1.  The angles are worked out
+ * in 64 bits, so that far positions keep them.
+ */
+enum { LR_ROPE_PLAIN = 0, LR_ROPE_LINEAR = 1, LR_ROPE_PARTS = 2, LR_ROPE_SMOOTH = 3 };
+#define LR_ROPE_MAX_DIM 128
+typedef struct lr_rope_spec {
+  int32_t rot_dim, interleaved, scaling;
+  double base, factor, original, lo, hi, amplitude;
+} lr_rope_spec;
+typedef struct lr_rope lr_rope; /* host memory alone: serves any device and any number of calls */
+
+/* LR_EINVAL: rot_dim odd or outside 2 .. LR_ROPE_MAX_DIM, base not above 1, and where the scaling uses
+ * them factor below 1, original below 1, 0 < lo < hi violated; anything that is not finite. */
+int lr_rope_create(lr_rope **out, const lr_rope_spec *spec);
+int lr_rope_destroy(lr_rope *rope);
+/* f_i, rot_dim / 2 of them, in radians a position, and the amplitude (either nullable). */
+int lr_rope_frequencies(const lr_rope *rope, double *radians_h, double *amplitude_h);
+
+/*
+ * What lies between a layer's joint projection and attention, in one pass over its output:
+ * the queries turned, the keys turned and written with their values into the slots of the
+ * cache.  Token t stands at positions_d[t] (negative ones turn the other way).
+ *   q_d, q_out_d   nullable together.  Rows of n_q_heads * head_dim bf16 at q_d + t * q_stride
+ *                  go to q_out_d[t][n_q_heads][head_dim], as attention takes them; they may
+ *                  be the same memory where q_stride is n_q_heads * head_dim, else they are
+ *                  apart
+ *   k_d, v_d       as in lr_fp8_write; slots too, with the same status: a negative slot
+ *                  leaves K and V of its token out (its query is turned all the same)
+ *   rope           nullable: nothing is turned.  rot_dim above head_dim: LR_EINVAL
+ * Turned in fp32, then rounded once, to bf16 or to the codes of the cache (scales as the
+ * writes of the two caches choose them, from the turned numbers).  Strides are multiples of 8
+ * and not below the rows' width, rows 16-byte aligned.  positions_d may be null where rope is.
+ */
+int lr_rope_write(lr_ctx *ctx, const lr_rope *rope, const lr_kv_cache *cache, const int32_t *positions_d, const void *q_d, int64_t q_stride,
+                  void *q_out_d, const void *k_d, int64_t k_stride, const void *v_d, int64_t v_stride, const int64_t *slots_d, int32_t n_tokens,
+                  int32_t *status_d, void *stream);
+
+/*
+ * Copies whole pages, K, V and scales bit for bit: pair i's page src_pages_d[i] of
+ * src_h[c] becomes page dst_pages_d[i] of dst_h[c], for every layer c < n_caches (host
+ * arrays, read during the call alone; src_h and dst_h may be the same).  All caches are of one
+ * kind.  This is how a sequence is forked, as a page belongs to one sequence, and how
+ * pages are taken out of a cache and put back.  A pair with a negative page on
+ * either side is left out; one with a page beyond its cache too and, with status_d
+ * (nullable; two int32 that the caller sets to 0), leaves {LR_EBOUNDS, its pair} there.
+ * A page named as a destination twice, or in the same pools as a source and a destination
+ * of different pairs, holds bytes of either in any mixture.
+ */
+int lr_copy_pages(lr_ctx *ctx, const lr_kv_cache *src_h, const lr_kv_cache *dst_h, int32_t n_caches, const int32_t *src_pages_d,
+                  const int32_t *dst_pages_d, int32_t n_pairs, int32_t *status_d, void *stream);
+
 /* ---- whole pass with device buffers --------------------------------------- */
 
 /* The device buffers of one pass, as the three steps take them. */

@@ -525,6 +525,86 @@ def fp8_load(codes: np.ndarray, scale: np.ndarray) -> np.ndarray:
     return np.where((scale == 255)[..., None], np.nan, v)
 
 
+E2M1 = np.array([0.0, 0.5, 1.0, 1.5, 2.0, 3.0, 4.0, 6.0])
+FP4_GROUP = 32
+
+
+def fp4_store(bits: np.ndarray) -> Tuple[np.ndarray, np.ndarray]:
+    """bf16 rows [..., head size] as the 4-bit cache holds them: code bytes [..., head size / 2] and scale bytes [..., head size / 32]."""
+    return fp4_store_values(bf16_bits_to_f64(bits))
+
+
+def fp4_store_values(x: np.ndarray) -> Tuple[np.ndarray, np.ndarray]:
+    """fp4_store of rows in 64 bits.
+
+    For each group of 32 channels: the smallest e >= -126 with max|x| <= 6 * 2^e; codes are x / 2^e rounded to the nearest e2m1 number, ties to the even code; the
+    byte is e + 127.  A row that is not finite has codes 0 and bytes 255."""
+    x = np.asarray(x, dtype=np.float64)
+    fine = np.isfinite(x).all(axis=-1)
+    g = np.where(fine[..., None], x, 0.0).reshape(*x.shape[:-1], x.shape[-1] // FP4_GROUP, FP4_GROUP)
+    top = np.abs(g).max(axis=-1)
+    m, x2 = np.frexp(top)  # top = m 2^x2, 1/2 <= m < 1, and 6 = 3/4 2^3
+    e = np.maximum(np.where(m > 0.75, x2 - 2, x2 - 3), -126).astype(np.int64)
+    y = (g / np.exp2(e.astype(np.float64))[..., None]).reshape(x.shape)
+    between = (E2M1[1:] + E2M1[:-1]) / 2
+    a = np.abs(y)
+    code = np.searchsorted(between, a)  # of two as near the lower one
+    code += (code % 2 == 1) & (a == between[np.minimum(code, 6)])
+    code = (code + 8 * np.signbit(y)).astype(np.uint32)
+    code[~fine] = 0
+    word = np.zeros((*x.shape[:-1], x.shape[-1] // 8), dtype=np.uint32)
+    for c in range(8):
+        word |= code[..., c::8] << np.uint32(4 * (c // 2) + 16 * (c % 2))
+    byte = np.where(fine[..., None], e + 127, 255).astype(np.uint8)
+    return np.ascontiguousarray(word).astype("<u4").view(np.uint8).reshape(*x.shape[:-1], x.shape[-1] // 2), byte
+
+
+def fp4_load(codes: np.ndarray, scale: np.ndarray) -> np.ndarray:
+    """What stored rows stand for, in 64 bits [..., head size]; a row with a byte of 255 is NaN."""
+    word = np.ascontiguousarray(codes).view("<u4").reshape(*codes.shape[:-1], codes.shape[-1] // 4)
+    out = np.empty((*codes.shape[:-1], 2 * codes.shape[-1]))
+    for c in range(8):
+        nibble = (word >> np.uint32(4 * (c // 2) + 16 * (c % 2))) & np.uint32(15)
+        out[..., c::8] = np.where(nibble > 7, -1.0, 1.0) * E2M1[nibble & 7]
+    by = np.repeat(np.exp2(scale.astype(np.float64) - 127.0), FP4_GROUP, axis=-1)
+    return np.where((scale == 255).any(axis=-1)[..., None], np.nan, out * by)
+
+
+def rope_frequencies(rot: int, base: float, scaling: str = "none", factor: float = 1.0, original: float = 0.0, lo: float = 1.0, hi: float = 32.0):
+    """(radians a position of every pair, amplitude): base^(-2 i / rot), those that turn seldom over the original length slowed down."""
+    f = [base ** (-2.0 * i / rot) for i in range(rot // 2)]
+    if scaling == "linear":
+        return np.array([x / factor for x in f]), 1.0
+    if scaling == "smooth":
+        out = []
+        for x in f:
+            turns = original * x / (2.0 * math.pi)
+            kept = 1.0 if turns >= hi else 0.0 if turns <= lo else (turns - lo) / (hi - lo)
+            out.append(kept * x + (1.0 - kept) * x / factor)
+        return np.array(out), 1.0
+    if scaling == "parts":
+        where = [rot * math.log(original / (2.0 * math.pi * turns)) / (2.0 * math.log(base)) for turns in (hi, lo)]
+        first, last = max(math.floor(where[0]), 0), min(math.ceil(where[1]), rot - 1)
+        out = []
+        for i, x in enumerate(f):
+            stretched = min(max((i - first) / max(last - first, 0.001), 0.0), 1.0)
+            out.append(x * (1.0 - stretched) + x / factor * stretched)
+        return np.array(out), 0.1 * math.log(factor) + 1.0
+    return np.array(f), 1.0
+
+
+def rope(x: np.ndarray, positions: np.ndarray, radians: np.ndarray, amplitude: float = 1.0, interleaved: bool = False) -> np.ndarray:
+    """Rows [tokens, heads, head size] in 64 bits, the first 2 len(radians) channels of a head turned to their token's position."""
+    y, n = np.array(x, dtype=np.float64), len(radians)
+    for t, p in enumerate(positions):
+        for i, f in enumerate(radians):
+            a, b = (2 * i, 2 * i + 1) if interleaved else (i, i + n)
+            c, s = math.cos(int(p) * f) * amplitude, math.sin(int(p) * f) * amplitude
+            u, v = x[t, :, a].astype(np.float64), x[t, :, b].astype(np.float64)
+            y[t, :, a], y[t, :, b] = u * c - v * s, u * s + v * c
+    return y
+
+
 def verify_pass(batch, q_bits, k_pool_bits, v_pool_bits, logits_bits, draft_ids, verdict):
     """All three steps in order, as one pass."""
     o, lse = verify_attention(batch, q_bits, k_pool_bits, v_pool_bits)

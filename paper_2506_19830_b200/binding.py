@@ -21,6 +21,7 @@ LR_OK = 0
 STATUS_NAMES = {0: "LR_OK", -1: "LR_EINVAL", -2: "LR_EUNSUPPORTED", -3: "LR_ECUDA", -4: "LR_ETIMEOUT", -5: "LR_EBOUNDS",
                 -6: "LR_ENOMEM"}
 
+KV_BF16, KV_FP8, KV_FP4 = 0, 1, 2  # LR_KV_*
 PATH_AUTO, PATH_GENERIC, PATH_TENSOR_CORE, PATH_PAIR = 0, 1, 2, 3
 ACCEPT_STATIC_MAX_ROWS = 4096  # LR_ACCEPT_STATIC_MAX_ROWS
 COMMIT_MAX_REQUESTS = 4096  # LR_COMMIT_MAX_REQUESTS
@@ -60,6 +61,18 @@ class lr_partition_info(C.Structure):
 
 class lr_fp8_cache(C.Structure):
     _fields_ = [(n, C.c_void_p) for n in ("k_d", "v_d", "k_scale_d", "v_scale_d")] + [("n_pages", C.c_int64)]
+
+
+class lr_fp4_cache(C.Structure):
+    _fields_ = lr_fp8_cache._fields_
+
+
+class lr_kv_cache(C.Structure):
+    _fields_ = [("kind", C.c_int32)] + lr_fp8_cache._fields_
+
+
+class lr_rope_spec(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("rot_dim", "interleaved", "scaling")] + [(n, C.c_double) for n in ("base", "factor", "original", "lo", "hi", "amplitude")]
 
 
 class lr_pass_host_io(C.Structure):
@@ -119,6 +132,15 @@ def lib() -> C.CDLL:
             "lr_fp8_read": [vp, vp, vp, i32, vp, i64, vp, i64, vp, vp],
             "lr_verify_attention_fp8": [vp, vp, vp, vp, vp, f32, vp],
             "lr_compact_fp8": [vp] * 8,
+            "lr_fp4_write": [vp, vp, vp, i64, vp, i64, vp, i32, vp, vp],
+            "lr_fp4_read": [vp, vp, vp, i32, vp, i64, vp, i64, vp, vp],
+            "lr_verify_attention_fp4": [vp, vp, vp, vp, vp, f32, vp],
+            "lr_compact_fp4": [vp] * 8,
+            "lr_rope_create": [C.POINTER(vp), C.POINTER(lr_rope_spec)],
+            "lr_rope_destroy": [vp],
+            "lr_rope_frequencies": [vp, vp, C.POINTER(C.c_double)],
+            "lr_rope_write": [vp, vp, vp, vp, vp, i64, vp, vp, i64, vp, i64, vp, i32, vp, vp],
+            "lr_copy_pages": [vp, vp, vp, i32, vp, vp, i32, vp, vp],
             "lr_pass_staging_bytes": [vp, C.POINTER(sz)],
             "lr_verify_pass": [vp, vp, C.c_char_p, f32, vp, vp],
             "lr_verify_pass_host": [vp, C.POINTER(lr_pass_host_io), vp, vp, vp, sz, f32, vp],
@@ -227,6 +249,8 @@ class Fp8Cache:
         self.kind = (self.heads, self.head_dim, k.device.index)  # what a context has to have, too
         self._c = lr_fp8_cache(k.data_ptr(), v.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr(), shape[0])
         self.c = C.addressof(self._c)
+        self.kv = lr_kv_cache(KV_FP8, *(getattr(self._c, n) for n, _ in lr_fp8_cache._fields_))
+        self.any = C.addressof(self.kv)
 
     @staticmethod
     def empty(model, n_pages: int, device="cuda:0") -> "Fp8Cache":
@@ -236,14 +260,90 @@ class Fp8Cache:
         return Fp8Cache(*codes, *(torch.full(shape[:3], 127, dtype=torch.uint8, device=device).view(torch.float8_e8m0fnu) for _ in range(2)))
 
 
-def _check_cache(cache: Fp8Cache, ctx: "Context") -> None:
+class Fp4Cache:
+    """``lr_fp4_cache`` over four tensors of the caller's: code bytes [pages, KV heads, 16, head size / 2] (``torch.uint8``) and scales
+    [pages, KV heads, 16, head size / 32] (``torch.float8_e8m0fnu`` or ``torch.uint8``), of K and of V.  ``empty`` makes them."""
+
+    def __init__(self, k: torch.Tensor, v: torch.Tensor, k_scale: torch.Tensor, v_scale: torch.Tensor):
+        shape = k.shape
+        for t, want, kinds in ((k, shape, (torch.uint8,)), (v, shape, (torch.uint8,)), (k_scale, shape[:3] + (shape[-1] // 16,), (torch.float8_e8m0fnu, torch.uint8)),
+                               (v_scale, shape[:3] + (shape[-1] // 16,), (torch.float8_e8m0fnu, torch.uint8))):
+            if t.shape != want or len(shape) != 4 or shape[2] != 16 or shape[3] % 16 != 0 or t.dtype not in kinds or not t.is_contiguous() or t.device != k.device:
+                raise ValueError(f"a 4-bit cache is code bytes [pages, KV heads, 16, head size / 2] and scales [pages, KV heads, 16, head size / 32], contiguous, on one device: "
+                                 f"got {tuple(t.shape)} {t.dtype} on {t.device}")
+        self.k, self.v, self.k_scale, self.v_scale = k, v, k_scale, v_scale
+        self.n_pages, self.heads, self.head_dim, self.device = shape[0], shape[1], 2 * shape[3], k.device
+        self.kind = (self.heads, self.head_dim, k.device.index)
+        self._c = lr_fp4_cache(k.data_ptr(), v.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr(), shape[0])
+        self.c = C.addressof(self._c)
+        self.kv = lr_kv_cache(KV_FP4, *(getattr(self._c, n) for n, _ in lr_fp8_cache._fields_))
+        self.any = C.addressof(self.kv)
+
+    @staticmethod
+    def empty(model, n_pages: int, device="cuda:0") -> "Fp4Cache":
+        """A cache of zeros (scale bytes 127: 2^0)."""
+        shape = (n_pages, int(model.n_kv_heads), 16, int(model.head_dim))
+        codes = [torch.zeros(shape[:3] + (shape[3] // 2,), dtype=torch.uint8, device=device) for _ in range(2)]
+        return Fp4Cache(*codes, *(torch.full(shape[:3] + (shape[3] // 32,), 127, dtype=torch.uint8, device=device).view(torch.float8_e8m0fnu) for _ in range(2)))
+
+
+class Bf16Cache:
+    """The bf16 pools [pages, KV heads, 16, head size] of K and of V, as the calls on a cache of any kind take them."""
+
+    def __init__(self, k: torch.Tensor, v: torch.Tensor):
+        for t in (k, v):
+            if t.shape != k.shape or t.dim() != 4 or t.shape[2] != 16 or t.dtype is not torch.bfloat16 or not t.is_contiguous() or t.device != k.device:
+                raise ValueError(f"a bf16 cache is two pools [pages, KV heads, 16, head size], contiguous, on one device: got {tuple(t.shape)} {t.dtype} on {t.device}")
+        self.k, self.v = k, v
+        self.n_pages, self.heads, self.head_dim, self.device = k.shape[0], k.shape[1], k.shape[3], k.device
+        self.kind = (self.heads, self.head_dim, k.device.index)
+        self.kv = lr_kv_cache(KV_BF16, k.data_ptr(), v.data_ptr(), None, None, k.shape[0])
+        self.any = C.addressof(self.kv)
+
+
+class Rope:
+    """``lr_rope``: rotary positions of the first ``rot_dim`` channels of a head.  scaling: "none", "linear", "parts" or "smooth", with its factor and,
+    for the latter two, the original length and the turns over it between which frequencies pass from stretched (``lo``) to kept (``hi``)."""
+
+    SCALINGS = ("none", "linear", "parts", "smooth")
+
+    def __init__(self, rot_dim: int, base: float = 10000.0, interleaved: bool = False, scaling: str = "none", factor: float = 1.0, original: float = 0.0,
+                 lo: float = 1.0, hi: Optional[float] = None, amplitude: float = 0.0):
+        if scaling not in self.SCALINGS:
+            raise ValueError(f"scaling is one of {self.SCALINGS}, not {scaling!r}")
+        hi = (4.0 if scaling == "smooth" else 32.0) if hi is None else hi
+        self.handle = None
+        h = C.c_void_p()
+        spec = lr_rope_spec(rot_dim, int(interleaved), self.SCALINGS.index(scaling), base, factor, original, lo, hi, amplitude)
+        _check(lib().lr_rope_create(C.byref(h), C.byref(spec)), "lr_rope_create")
+        self.handle, self.rot_dim = h, rot_dim
+
+    def frequencies(self) -> tuple:
+        """(radians a position of every pair, float64 [rot_dim / 2]; amplitude)."""
+        f, amplitude = np.empty(self.rot_dim // 2), C.c_double()
+        _check(lib().lr_rope_frequencies(self.handle, _addr(f), C.byref(amplitude)), "lr_rope_frequencies")
+        return f, amplitude.value
+
+    def close(self):
+        if self.handle:
+            lib().lr_rope_destroy(self.handle)
+            self.handle = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+
+def _check_cache(cache, ctx: "Context") -> None:
     # what the C side cannot see: how large the tensors behind its pointers are, and where
     if cache.kind != ctx.cache_kind:
         m = ctx.model
         raise ValueError(f"the cache has {cache.heads} heads of {cache.head_dim} on {cache.device}, the context {m.n_kv_heads} of {m.head_dim} on cuda:{ctx.device}")
 
 
-def _fp8_rows(ctx: "Context", cache: Fp8Cache, k: torch.Tensor, v: torch.Tensor, slots: torch.Tensor, status: Optional[torch.Tensor]) -> tuple:
+def _cache_rows(ctx: "Context", cache, k: torch.Tensor, v: torch.Tensor, slots: torch.Tensor, status: Optional[torch.Tensor]) -> tuple:
     """Number of tokens and the rows' strides, with the tensors found to be what the C side takes them for."""
     _check_cache(cache, ctx)
     n, heads, width, dev = slots.numel(), cache.heads, cache.head_dim, ctx.device
@@ -301,8 +401,33 @@ def _check_drafted(ctx: "Context", logits, draft_logits, draft_ids, cu_draft, u_
     return n_branch, n_rows
 
 
+def _of_kind(cache, kind):
+    """The cache, found to be of the kind whose struct the C side will take it for."""
+    if not isinstance(cache, kind):
+        raise ValueError(f"the call takes a {kind.__name__}, not {type(cache).__name__}")
+    return cache
+
+
+def _check_rope(ctx: "Context", n: int, positions, q, q_out, turned: bool) -> int:
+    """The stride of the queries' rows, with the tensors of lr_rope_write found to be what the C side takes them for."""
+    m, dev = ctx.model, ctx.device
+    heads, width = m.n_q_heads, m.head_dim
+    fine = not turned or (positions is not None and _flat(positions, torch.int32, n, dev) and positions.numel() == n)
+    if not fine:
+        raise ValueError(f"lr_rope_write: positions are contiguous int32 [{n}] on device {dev}")
+    if (q is None) != (q_out is None):
+        raise ValueError("lr_rope_write: q and q_out come together")
+    if q is None:
+        return 0
+    if not (q.shape == (n, heads, width) and q.dtype is torch.bfloat16 and q.get_device() == dev and (n == 0 or (q.stride(2) == 1 and q.stride(1) == width))):
+        raise ValueError(f"lr_rope_write: q is bf16 [{n}, {heads}, {width}] on device {dev}, a token's heads side by side: got {tuple(q.shape)} {q.dtype} strides {q.stride()} on {q.device}")
+    if not (q_out.dtype is torch.bfloat16 and q_out.is_contiguous() and q_out.get_device() == dev and q_out.numel() == n * heads * width):
+        raise ValueError(f"lr_rope_write: q_out is contiguous bf16 [{n}, {heads}, {width}] on device {dev}: got {tuple(q_out.shape)} {q_out.dtype} strides {q_out.stride()} on {q_out.device}")
+    return q.stride(0) if n > 1 else heads * width
+
+
 # (These run before every launch, where each look at a tensor takes a twentieth of a microsecond: all of them in one expression, and who is at fault only then.)
-def _check_attention(ctx: "Context", n_q_rows: int, q, out, lse) -> tuple:
+def _check_attention(ctx: "Context", n_q_rows: int, q, out, lse, where: str = "lr_verify_attention_fp8") -> tuple:
     """The addresses of the tensors of an attention call, found to be what the C side takes them for."""
     m, dev = ctx.model, ctx.device
     n = n_q_rows * m.n_q_heads
@@ -311,13 +436,13 @@ def _check_attention(ctx: "Context", n_q_rows: int, q, out, lse) -> tuple:
             and q.numel() >= n * m.head_dim <= out.numel() and lse.numel() >= n):
         return q.data_ptr(), out.data_ptr(), lse.data_ptr()
     shape = f"[{n_q_rows}, {m.n_q_heads}"
-    _refuse("lr_verify_attention_fp8", dev, q=(_flat(q, torch.bfloat16, n * m.head_dim, dev), q, f"contiguous bf16 {shape}, {m.head_dim}]"),
+    _refuse(where, dev, q=(_flat(q, torch.bfloat16, n * m.head_dim, dev), q, f"contiguous bf16 {shape}, {m.head_dim}]"),
             out=(_flat(out, torch.bfloat16, n * m.head_dim, dev), out, f"contiguous bf16 {shape}, {m.head_dim}]"),
             lse=(_flat(lse, torch.float32, n, dev), lse, f"contiguous float32 {shape}]"))
     return _ptr(q), _ptr(out), _ptr(lse)
 
 
-def _check_compact(ctx: "Context", n_req: int, keep_off, keep_pages, keep_valid, new_len, n_pages_kept) -> tuple:
+def _check_compact(ctx: "Context", n_req: int, keep_off, keep_pages, keep_valid, new_len, n_pages_kept, where: str = "lr_compact_fp8") -> tuple:
     # (how much of the lists there is to read the offsets say, which are on the device)
     dev, i32 = ctx.device, torch.int32
     some = keep_off is not None and keep_pages is not None and keep_valid is not None and new_len is not None and n_pages_kept is not None
@@ -326,7 +451,7 @@ def _check_compact(ctx: "Context", n_req: int, keep_off, keep_pages, keep_valid,
             and keep_off.is_contiguous() and keep_pages.is_contiguous() and keep_valid.is_contiguous() and new_len.is_contiguous() and n_pages_kept.is_contiguous()
             and keep_off.numel() > n_req <= new_len.numel() and n_pages_kept.numel() >= n_req and keep_valid.numel() >= keep_pages.numel()):
         return keep_off.data_ptr(), keep_pages.data_ptr(), keep_valid.data_ptr(), new_len.data_ptr(), n_pages_kept.data_ptr()
-    _refuse("lr_compact_fp8", dev, keep_off=(_flat(keep_off, i32, n_req + 1, dev), keep_off, f"int32 [{n_req + 1}]"),
+    _refuse(where, dev, keep_off=(_flat(keep_off, i32, n_req + 1, dev), keep_off, f"int32 [{n_req + 1}]"),
             keep_pages=(_flat(keep_pages, i32, 0, dev), keep_pages, "int32 [page slots]"),
             keep_valid=(_flat(keep_valid, i32, 0 if keep_pages is None else keep_pages.numel(), dev), keep_valid, "int32, as long as keep_pages,"),
             new_len=(_flat(new_len, i32, n_req, dev), new_len, f"int32 [{n_req}]"), n_pages_kept=(_flat(n_pages_kept, i32, n_req, dev), n_pages_kept, f"int32 [{n_req}]"))
@@ -430,16 +555,55 @@ class Context:
                      stream=None) -> None:
         """Quantises rows [tokens, KV heads, head size] (bf16; a slice of a joint projection's output will do) into the cache's token
         slots (int64: page * 16 + place, negative: none); status: two int32 of zeros that a slot beyond the cache sets."""
-        n, k_stride, v_stride = _fp8_rows(self, cache, k, v, slots, status)
+        n, k_stride, v_stride = _cache_rows(self, _of_kind(cache, Fp8Cache), k, v, slots, status)
         _check(lib().lr_fp8_write(self.handle, cache.c, k.data_ptr(), k_stride, v.data_ptr(), v_stride, slots.data_ptr(), n, _ptr(status),
                                   _stream_on(self.device, stream)), "lr_fp8_write")
 
     def lr_fp8_read(self, cache: Fp8Cache, slots: torch.Tensor, k: torch.Tensor, v: torch.Tensor, status: Optional[torch.Tensor] = None,
                     stream=None) -> None:
         """The values at the token slots, into rows as ``lr_fp8_write`` takes them; a row without a slot is left as it was."""
-        n, k_stride, v_stride = _fp8_rows(self, cache, k, v, slots, status)
+        n, k_stride, v_stride = _cache_rows(self, _of_kind(cache, Fp8Cache), k, v, slots, status)
         _check(lib().lr_fp8_read(self.handle, cache.c, slots.data_ptr(), n, k.data_ptr(), k_stride, v.data_ptr(), v_stride, _ptr(status),
                                  _stream_on(self.device, stream)), "lr_fp8_read")
+
+    def lr_fp4_write(self, cache: Fp4Cache, k: torch.Tensor, v: torch.Tensor, slots: torch.Tensor, status: Optional[torch.Tensor] = None,
+                     stream=None) -> None:
+        """``lr_fp8_write`` into a 4-bit cache."""
+        n, k_stride, v_stride = _cache_rows(self, _of_kind(cache, Fp4Cache), k, v, slots, status)
+        _check(lib().lr_fp4_write(self.handle, cache.c, k.data_ptr(), k_stride, v.data_ptr(), v_stride, slots.data_ptr(), n, _ptr(status),
+                                  _stream_on(self.device, stream)), "lr_fp4_write")
+
+    def lr_fp4_read(self, cache: Fp4Cache, slots: torch.Tensor, k: torch.Tensor, v: torch.Tensor, status: Optional[torch.Tensor] = None,
+                    stream=None) -> None:
+        """``lr_fp8_read`` from a 4-bit cache."""
+        n, k_stride, v_stride = _cache_rows(self, _of_kind(cache, Fp4Cache), k, v, slots, status)
+        _check(lib().lr_fp4_read(self.handle, cache.c, slots.data_ptr(), n, k.data_ptr(), k_stride, v.data_ptr(), v_stride, _ptr(status),
+                                 _stream_on(self.device, stream)), "lr_fp4_read")
+
+    def lr_rope_write(self, rope: Optional[Rope], positions: Optional[torch.Tensor], cache, k: torch.Tensor, v: torch.Tensor, slots: torch.Tensor,
+                      q: Optional[torch.Tensor] = None, q_out: Optional[torch.Tensor] = None, status: Optional[torch.Tensor] = None, stream=None) -> None:
+        """Turns the queries q [tokens, q heads, head size] into q_out and the keys k into the cache's slots, V beside them: rows of a joint projection, as
+        ``lr_fp8_write`` takes them.  positions: int32 [tokens].  cache: a ``Bf16Cache``, ``Fp8Cache`` or ``Fp4Cache``.  Without rope nothing is turned."""
+        n, k_stride, v_stride = _cache_rows(self, cache, k, v, slots, status)
+        q_stride = _check_rope(self, n, positions, q, q_out, rope is not None)
+        _check(lib().lr_rope_write(self.handle, None if rope is None else rope.handle, cache.any, _ptr(positions), _ptr(q), q_stride, _ptr(q_out),
+                                   k.data_ptr(), k_stride, v.data_ptr(), v_stride, slots.data_ptr(), n, _ptr(status), _stream_on(self.device, stream)),
+               "lr_rope_write")
+
+    def lr_copy_pages(self, src, dst, src_pages: torch.Tensor, dst_pages: torch.Tensor, status: Optional[torch.Tensor] = None, stream=None) -> None:
+        """Copies pages src_pages[i] of every cache of ``src`` to dst_pages[i] of its counterpart in ``dst`` (a cache or a list of them, a layer each)."""
+        src, dst = ([c] if isinstance(c, (Bf16Cache, Fp8Cache, Fp4Cache)) else list(c) for c in (src, dst))
+        if len(src) != len(dst):
+            raise ValueError(f"lr_copy_pages: {len(src)} caches to copy from, {len(dst)} to copy to")
+        for c in src + dst:
+            _check_cache(c, self)
+        n, dev = src_pages.numel(), self.device
+        _refuse("lr_copy_pages", dev, src_pages=(_flat(src_pages, torch.int32, n, dev), src_pages, f"int32 [{n}]"),
+                dst_pages=(_flat(dst_pages, torch.int32, n, dev) and dst_pages.numel() == n, dst_pages, f"int32 [{n}]"),
+                status=(_flat(status, torch.int32, 2, dev), status, "two int32"))
+        array = lr_kv_cache * len(src)
+        _check(lib().lr_copy_pages(self.handle, array(*(c.kv for c in src)), array(*(c.kv for c in dst)), len(src), src_pages.data_ptr(), dst_pages.data_ptr(), n,
+                                   _ptr(status), _stream_on(dev, stream)), "lr_copy_pages")
 
     def accept_sample_filtered_scratch(self, n_rows: int) -> torch.Tensor:
         n = C.c_size_t()
@@ -538,17 +702,31 @@ class Plan:
 
     def lr_verify_attention_fp8(self, q, cache: Fp8Cache, out, lse=None, softmax_scale: float = 0.0, stream=None) -> None:
         """``lr_verify_attention`` over an 8-bit cache."""
-        _check_cache(cache, self.ctx)
+        _check_cache(_of_kind(cache, Fp8Cache), self.ctx)
         q_at, out_at, lse_at = _check_attention(self.ctx, self.n_q_rows, q, out, lse)
         _check(lib().lr_verify_attention_fp8(self.handle, q_at, cache.c, out_at, lse_at, float(softmax_scale), _stream_on(self.ctx.device, stream)),
                "lr_verify_attention_fp8")
 
     def lr_compact_fp8(self, keep_off, keep_pages, keep_valid, cache: Fp8Cache, new_len, n_pages_kept, stream=None) -> None:
         """``lr_compact`` over an 8-bit cache: codes and scales together."""
-        _check_cache(cache, self.ctx)
+        _check_cache(_of_kind(cache, Fp8Cache), self.ctx)
         off_at, pages_at, valid_at, len_at, kept_at = _check_compact(self.ctx, self.n_req, keep_off, keep_pages, keep_valid, new_len, n_pages_kept)
         _check(lib().lr_compact_fp8(self.handle, off_at, pages_at, valid_at, cache.c, len_at, kept_at, _stream_on(self.ctx.device, stream)),
                "lr_compact_fp8")
+
+    def lr_verify_attention_fp4(self, q, cache: Fp4Cache, out, lse=None, softmax_scale: float = 0.0, stream=None) -> None:
+        """``lr_verify_attention`` over a 4-bit cache."""
+        _check_cache(_of_kind(cache, Fp4Cache), self.ctx)
+        q_at, out_at, lse_at = _check_attention(self.ctx, self.n_q_rows, q, out, lse, "lr_verify_attention_fp4")
+        _check(lib().lr_verify_attention_fp4(self.handle, q_at, cache.c, out_at, lse_at, float(softmax_scale), _stream_on(self.ctx.device, stream)),
+               "lr_verify_attention_fp4")
+
+    def lr_compact_fp4(self, keep_off, keep_pages, keep_valid, cache: Fp4Cache, new_len, n_pages_kept, stream=None) -> None:
+        """``lr_compact`` over a 4-bit cache: codes and scales together."""
+        _check_cache(_of_kind(cache, Fp4Cache), self.ctx)
+        off_at, pages_at, valid_at, len_at, kept_at = _check_compact(self.ctx, self.n_req, keep_off, keep_pages, keep_valid, new_len, n_pages_kept, "lr_compact_fp4")
+        _check(lib().lr_compact_fp4(self.handle, off_at, pages_at, valid_at, cache.c, len_at, kept_at, _stream_on(self.ctx.device, stream)),
+               "lr_compact_fp4")
 
     def lr_poll_status(self, stream=None) -> int:
         d = C.c_int32()

@@ -10,13 +10,14 @@
 //
 // The same sweep serves the 8-bit cache, whose rows have half the bytes: the CTA that owns the first columns of a head moves that
 // head's scale bytes too, each with its row (in rounds of their own, behind the rows' or in another CTA, 0.5 and 1.2 us more for 16 requests).
+// In the 4-bit cache the 16 bytes that a thread moves have a scale byte of their own, 32 channels both, which it takes along.
 //
 // Bytes moved: 2 (K, V) x H_kv x D x 2 B per displaced token, read and written once.  Bound by the chain of dependent
 // reads (list bounds, counts, page ids, data), not by bandwidth.  One launch; as three (scan, gather to a staging area,
 // scatter) with the bytes read and written twice, one layer of 8 ragged requests took 16.3 us on a B200, this takes 4.1.
 #include <algorithm>
 
-#include "fp8_cache.cuh"
+#include "fp4_cache.cuh"
 
 namespace lr {
 
@@ -29,8 +30,9 @@ constexpr int kScan = kThreads * kPerThread;   // pages per step
 constexpr int kRows = 8;                       // 16-byte vectors a thread holds per round
 
 // What a CTA moves at a time: rows of vec_per_row elements, of which it has 1 << shift from column c0 on.  Rounds of kThreads * kRows
-// elements, in token order, over the pages first .. n_here - 1 of a step.  kScales: the thread of a row's first element takes its scale byte along.
-template <bool kScales>
+// elements, in token order, over the pages first .. n_here - 1 of a step.  kBits: of the cache; 8: the thread of a row's first element takes its scale byte along,
+// 4: every thread its element's.
+template <int kBits>
 __device__ __forceinline__ void move_rounds(const DevBatch &d, uint4 *pool, uint8_t *scale, int vec_per_row, int shift, int c0, int h, const int32_t *__restrict__ keep_pages,
                                             const int32_t *s_off, int i0, int base, int first, int n_here) {
   const int tid = threadIdx.x;
@@ -65,9 +67,10 @@ __device__ __forceinline__ void move_rounds(const DevBatch &d, uint4 *pool, uint
         continue;
       }
       const int64_t from = (src_page * d.n_kv_heads + h) * kPage + t;
-      if constexpr (kScales) {
+      if constexpr (kBits != 16) {
         v[u] = __ldcg(pool + from * vec_per_row + c);
-        if (c == 0) byte[u] = ld_scale(scale + from);
+        if constexpr (kBits == 4) byte[u] = ld_scale(scale + from * vec_per_row + c);
+        else if (c == 0) byte[u] = ld_scale(scale + from);
       } else {
         v[u] = pool[from * vec_per_row + c];
       }
@@ -78,15 +81,16 @@ __device__ __forceinline__ void move_rounds(const DevBatch &d, uint4 *pool, uint
     for (int u = 0; u < kRows; ++u)
       if (to[u] >= 0) {
         pool[to[u]] = v[u];
-        if (kScales && (to[u] & (vec_per_row - 1)) == 0) scale[to[u] >> (31 - __clz(vec_per_row))] = (uint8_t)byte[u];  // (4 or 8 to a row)
+        if constexpr (kBits == 4) scale[to[u]] = (uint8_t)byte[u];
+        if (kBits == 8 && (to[u] & (vec_per_row - 1)) == 0) scale[to[u] >> (31 - __clz(vec_per_row))] = (uint8_t)byte[u];  // (4 or 8 to a row)
       }
   }
 }
 
 // blockIdx.x: (KV head, K or V, slice of the row); blockIdx.y: request.  1 << shift 16-byte vectors per slice.  sides: 2, or 1
-// when K and V are the same pool, whose bytes one CTA has to own as well.  kScales: the 8-bit cache,
-// rows of half the size and a scale byte for each.
-template <bool kScales>
+// when K and V are the same pool, whose bytes one CTA has to own as well.  kBits: 16, 8 or 4 of a
+// channel; the latter two have scale bytes.
+template <int kBits>
 __global__ void __launch_bounds__(kThreads)
 compact_kernel(DevBatch d, const int32_t *__restrict__ keep_off, const int32_t *__restrict__ keep_pages,
                const int32_t *__restrict__ keep_valid, int shift, int sides, uint4 *k_pool, uint4 *v_pool, uint8_t *k_scale, uint8_t *v_scale,
@@ -94,7 +98,7 @@ compact_kernel(DevBatch d, const int32_t *__restrict__ keep_off, const int32_t *
   __shared__ int32_t s_off[kScan + 1];  // tokens of the request in front of each page of the step
   __shared__ int32_t warp_sum[kThreads / 32], warp_first[kThreads / 32];
   const int r = blockIdx.y, tid = threadIdx.x, lane = tid & 31, wid = tid >> 5;
-  const int vec_per_row = d.head_dim / (kScales ? 16 : 8), slices = vec_per_row >> shift;
+  const int vec_per_row = d.head_dim * kBits / 128, slices = vec_per_row >> shift;
   const int slice = blockIdx.x % slices, h = blockIdx.x / slices / sides;
   const bool of_v = blockIdx.x / slices % sides != 0;
   uint4 *pool = of_v ? v_pool : k_pool;
@@ -154,7 +158,7 @@ compact_kernel(DevBatch d, const int32_t *__restrict__ keep_off, const int32_t *
       for (int w = 0; w < kThreads / 32; ++w) first = min(first, warp_first[w]);
     }
     moved = moved || first < n_here;
-    move_rounds<kScales>(d, pool, scale, vec_per_row, shift, slice << shift, h, keep_pages, s_off, i0, base, first, n_here);
+    move_rounds<kBits>(d, pool, scale, vec_per_row, shift, slice << shift, h, keep_pages, s_off, i0, base, first, n_here);
     __syncthreads();  // s_off is free again
   }
   if (blockIdx.x == 0 && tid == 0) {
@@ -165,19 +169,19 @@ compact_kernel(DevBatch d, const int32_t *__restrict__ keep_off, const int32_t *
 
 }  // namespace
 
-template <bool kScales>
+template <int kBits>
 static int launch_compact_as(lr_plan *p, const int32_t *keep_off, const int32_t *keep_pages, const int32_t *keep_valid, void *k_pool,
                              void *v_pool, uint8_t *k_scale, uint8_t *v_scale, int32_t *new_len, int32_t *n_pages_kept, cudaStream_t s) {
   const DevBatch &d = p->dev;
   if (d.n_req > kMaxReq) {
-    set_error("%s: more than %d requests in one pass", kScales ? "lr_compact_fp8" : "lr_compact", kMaxReq);
+    set_error("%s: more than %d requests in one pass", kBits == 4 ? "lr_compact_fp4" : kBits == 8 ? "lr_compact_fp8" : "lr_compact", kMaxReq);
     return LR_EUNSUPPORTED;
   }
   // Rows are sliced while that gives idle SMs something to do: down to 64 bytes until there are two CTAs per SM (8 KV heads
   // of 128 channels, whole rows and sliced: one request with 360 displaced tokens 10.8 and 5.5 us, 16 with 160 each 7.6 and
   // 7.0, but sliced in four 8.8), down to one sector for half a CTA per SM (one request 5.5 and 4.5, with 4000 tokens 26 and
   // 17; four requests 4.2 and 5.1).
-  const int vec_per_row = d.head_dim / (kScales ? 16 : 8);
+  const int vec_per_row = d.head_dim * kBits / 128;
   int shift = 0;
   while (2 << shift <= vec_per_row) ++shift;
   const int sides = k_pool == v_pool ? 1 : 2;
@@ -185,19 +189,24 @@ static int launch_compact_as(lr_plan *p, const int32_t *keep_off, const int32_t 
   while (shift > 1 && rows * (vec_per_row >> shift) < (shift > 2 ? 2 * p->ctx->sm_count : p->ctx->sm_count / 2)) --shift;
   const dim3 grid((unsigned)(d.n_kv_heads * sides * (vec_per_row >> shift)), (unsigned)d.n_req);
   p->ctx->launches++;
-  return cuda_fail(launch_dependent(compact_kernel<kScales>, grid, dim3(kThreads), 0, s, d, keep_off, keep_pages, keep_valid, shift, sides,
+  return cuda_fail(launch_dependent(compact_kernel<kBits>, grid, dim3(kThreads), 0, s, d, keep_off, keep_pages, keep_valid, shift, sides,
                                     reinterpret_cast<uint4 *>(k_pool), reinterpret_cast<uint4 *>(v_pool), k_scale, v_scale, new_len, n_pages_kept),
                    "compact_kernel launch");
 }
 
 int launch_compact(lr_plan *p, const int32_t *keep_off, const int32_t *keep_pages, const int32_t *keep_valid, void *k_pool,
                    void *v_pool, int32_t *new_len, int32_t *n_pages_kept, cudaStream_t s) {
-  return launch_compact_as<false>(p, keep_off, keep_pages, keep_valid, k_pool, v_pool, nullptr, nullptr, new_len, n_pages_kept, s);
+  return launch_compact_as<16>(p, keep_off, keep_pages, keep_valid, k_pool, v_pool, nullptr, nullptr, new_len, n_pages_kept, s);
 }
 
 int launch_compact_fp8(lr_plan *p, const int32_t *keep_off, const int32_t *keep_pages, const int32_t *keep_valid, const lr_fp8_cache &c,
                        int32_t *new_len, int32_t *n_pages_kept, cudaStream_t s) {
-  return launch_compact_as<true>(p, keep_off, keep_pages, keep_valid, c.k_d, c.v_d, c.k_scale_d, c.v_scale_d, new_len, n_pages_kept, s);
+  return launch_compact_as<8>(p, keep_off, keep_pages, keep_valid, c.k_d, c.v_d, c.k_scale_d, c.v_scale_d, new_len, n_pages_kept, s);
+}
+
+int launch_compact_fp4(lr_plan *p, const int32_t *keep_off, const int32_t *keep_pages, const int32_t *keep_valid, const lr_fp4_cache &c,
+                       int32_t *new_len, int32_t *n_pages_kept, cudaStream_t s) {
+  return launch_compact_as<4>(p, keep_off, keep_pages, keep_valid, c.k_d, c.v_d, c.k_scale_d, c.v_scale_d, new_len, n_pages_kept, s);
 }
 
 }  // namespace lr

@@ -1,6 +1,7 @@
 // Host side of the C ABI: contexts, batch validation, plan images, launch
 // wrappers and the host-buffer pass.  No device memory is allocated here; every
 // device byte the library touches lies in caller-provided buffers.
+#include <math.h>
 #include <stdarg.h>
 #include <stdio.h>
 #include <string.h>
@@ -312,6 +313,7 @@ extern "C" int lr_create(lr_ctx **out, const lr_model *m, int device) {
   if (int rc = init_attn_tc_kernel()) { delete c; return rc; }
   if (int rc = init_attn_pair_kernel()) { delete c; return rc; }
   if (int rc = init_attn_fp8_kernel()) { delete c; return rc; }
+  if (int rc = init_attn_fp4_kernel()) { delete c; return rc; }
   if (int rc = init_accept_filter_kernels()) { delete c; return rc; }
   SideStream side;
   if (int rc = make_side(side)) { delete c; return rc; }
@@ -996,8 +998,9 @@ extern "C" int lr_compact(lr_plan *p, const int32_t *keep_off, const int32_t *ke
                         reinterpret_cast<cudaStream_t>(stream));
 }
 
-// ---- the 8-bit cache ---------------------------------------------------------------
-static int check_cache(const lr_fp8_cache *c, const char *who) {
+// ---- the caches in 8 and in 4 bits ---------------------------------------------------
+template <class Cache>
+static int check_cache(const Cache *c, const char *who) {
   if (!c || !c->k_d || !c->v_d || !c->k_scale_d || !c->v_scale_d) {
     set_error("%s: null cache", who);
     return LR_EINVAL;
@@ -1017,7 +1020,8 @@ static int check_cache(const lr_fp8_cache *c, const char *who) {
   return LR_OK;
 }
 
-static int check_plan_cache(const lr_plan *p, const lr_fp8_cache *c, const char *who) {
+template <class Cache>
+static int check_plan_cache(const lr_plan *p, const Cache *c, const char *who) {
   if (int rc = check_cache(c, who)) return rc;
   if (!p) {
     set_error("%s: null plan", who);
@@ -1030,10 +1034,9 @@ static int check_plan_cache(const lr_plan *p, const lr_fp8_cache *c, const char 
   return LR_OK;
 }
 
-static int fp8_move(lr_ctx *ctx, const lr_fp8_cache *c, bool write, void *k, int64_t k_stride, void *v, int64_t v_stride, const int64_t *slots,
-                    int32_t n_tokens, int32_t *status, void *stream) {
-  const char *who = write ? "lr_fp8_write" : "lr_fp8_read";
-  if (int rc = check_cache(c, who)) return rc;
+// rows of K and V of n_tokens tokens and their slots, as the calls between a projection and a cache take them
+static int check_rows(const lr_ctx *ctx, const void *k, int64_t k_stride, const void *v, int64_t v_stride, const int64_t *slots, int32_t n_tokens,
+                      const int32_t *status, const char *who) {
   if (!ctx || n_tokens < 0 || (n_tokens > 0 && (!k || !v || !slots))) {
     set_error("%s: null argument or negative count", who);
     return LR_EINVAL;
@@ -1044,58 +1047,240 @@ static int fp8_move(lr_ctx *ctx, const lr_fp8_cache *c, bool write, void *k, int
     set_error("%s: rows must be 16-byte aligned with strides that are multiples of 8 and >= %lld, slots 8-byte aligned", who, (long long)width);
     return LR_EINVAL;
   }
+  return LR_OK;
+}
+
+template <class Cache>
+static int cache_move(lr_ctx *ctx, const Cache *c, bool write, void *k, int64_t k_stride, void *v, int64_t v_stride, const int64_t *slots,
+                      int32_t n_tokens, int32_t *status, void *stream, const char *who,
+                      int (*launch)(lr_ctx *, const Cache &, bool, void *, int64_t, void *, int64_t, const int64_t *, int32_t, int32_t *, cudaStream_t)) {
+  if (int rc = check_cache(c, who)) return rc;
+  if (int rc = check_rows(ctx, k, k_stride, v, v_stride, slots, n_tokens, status, who)) return rc;
   if (n_tokens == 0) return LR_OK;
   OnDevice on(ctx);
   if (on.rc != LR_OK) return on.rc;
-  return launch_fp8_move(ctx, *c, write, k, k_stride, v, v_stride, slots, n_tokens, status, reinterpret_cast<cudaStream_t>(stream));
+  return launch(ctx, *c, write, k, k_stride, v, v_stride, slots, n_tokens, status, reinterpret_cast<cudaStream_t>(stream));
 }
 
 extern "C" int lr_fp8_write(lr_ctx *ctx, const lr_fp8_cache *cache, const void *k, int64_t k_stride, const void *v, int64_t v_stride,
                             const int64_t *slots, int32_t n_tokens, int32_t *status, void *stream) {
-  return fp8_move(ctx, cache, true, const_cast<void *>(k), k_stride, const_cast<void *>(v), v_stride, slots, n_tokens, status, stream);
+  return cache_move(ctx, cache, true, const_cast<void *>(k), k_stride, const_cast<void *>(v), v_stride, slots, n_tokens, status, stream, "lr_fp8_write", launch_fp8_move);
 }
 
 extern "C" int lr_fp8_read(lr_ctx *ctx, const lr_fp8_cache *cache, const int64_t *slots, int32_t n_tokens, void *k, int64_t k_stride, void *v,
                            int64_t v_stride, int32_t *status, void *stream) {
-  return fp8_move(ctx, cache, false, k, k_stride, v, v_stride, slots, n_tokens, status, stream);
+  return cache_move(ctx, cache, false, k, k_stride, v, v_stride, slots, n_tokens, status, stream, "lr_fp8_read", launch_fp8_move);
 }
 
-extern "C" int lr_verify_attention_fp8(lr_plan *p, const void *q, const lr_fp8_cache *cache, void *out, float *lse, float scale, void *stream) {
-  if (int rc = check_plan_cache(p, cache, "lr_verify_attention_fp8")) return rc;
+// an attention call over one of these caches, with the kernels of its kind
+template <class Cache>
+static int cache_attention(lr_plan *p, const void *q, const Cache *cache, void *out, float *lse, float scale, void *stream, const char *who, int bits,
+                           int (*tensor_cores)(lr_plan *, const void *, const Cache &, void *, float *, float, cudaStream_t),
+                           int (*cuda_cores)(lr_plan *, const void *, const Cache &, void *, float *, float, cudaStream_t)) {
+  if (int rc = check_plan_cache(p, cache, who)) return rc;
   if (!q || !out) {
-    set_error("lr_verify_attention_fp8: null argument");
+    set_error("%s: null argument", who);
     return LR_EINVAL;
   }
   if ((((uintptr_t)q | (uintptr_t)out) & 15) != 0 || ((uintptr_t)lse & 3) != 0) {
-    set_error("lr_verify_attention_fp8: q and out must be 16-byte aligned");
+    set_error("%s: q and out must be 16-byte aligned", who);
     return LR_EINVAL;
   }
   if (!(scale > 0.f)) scale = 1.0f / sqrtf((float)p->dev.head_dim);
   if (p->attention_path == 3) {
-    set_error("lr_verify_attention_fp8: there is no CTA-pair kernel for an 8-bit cache");
+    set_error(bits == 8 ? "%s: there is no CTA-pair kernel for an 8-bit cache" : "%s: there is no CTA-pair kernel for a 4-bit cache", who);
     return LR_EUNSUPPORTED;
   }
   const bool use_tc = p->attention_path == 2 || (p->attention_path == 0 && p->tc_ok);
   if (use_tc && !p->tc_ok) {
-    set_error("lr_verify_attention_fp8: the tensor-core path does not support this shape");
+    set_error("%s: the tensor-core path does not support this shape", who);
     return LR_EUNSUPPORTED;
   }
   OnDevice on(p->ctx);
   if (on.rc != LR_OK) return on.rc;
-  if (use_tc) return launch_attn_fp8(p, q, *cache, out, lse, scale, reinterpret_cast<cudaStream_t>(stream));
-  return launch_attn_fp8_generic(p, q, *cache, out, lse, scale, reinterpret_cast<cudaStream_t>(stream));
+  return (use_tc ? tensor_cores : cuda_cores)(p, q, *cache, out, lse, scale, reinterpret_cast<cudaStream_t>(stream));
 }
 
-extern "C" int lr_compact_fp8(lr_plan *p, const int32_t *keep_off, const int32_t *keep_pages, const int32_t *keep_valid, const lr_fp8_cache *cache,
-                              int32_t *new_len, int32_t *n_pages_kept, void *stream) {
-  if (int rc = check_plan_cache(p, cache, "lr_compact_fp8")) return rc;
+extern "C" int lr_verify_attention_fp8(lr_plan *p, const void *q, const lr_fp8_cache *cache, void *out, float *lse, float scale, void *stream) {
+  return cache_attention(p, q, cache, out, lse, scale, stream, "lr_verify_attention_fp8", 8, launch_attn_fp8, launch_attn_fp8_generic);
+}
+
+template <class Cache>
+static int cache_compact(lr_plan *p, const int32_t *keep_off, const int32_t *keep_pages, const int32_t *keep_valid, const Cache *cache, int32_t *new_len,
+                         int32_t *n_pages_kept, void *stream, const char *who,
+                         int (*launch)(lr_plan *, const int32_t *, const int32_t *, const int32_t *, const Cache &, int32_t *, int32_t *, cudaStream_t)) {
+  if (int rc = check_plan_cache(p, cache, who)) return rc;
   if (!keep_off || !keep_pages || !keep_valid || !new_len || !n_pages_kept) {
-    set_error("lr_compact_fp8: null argument");
+    set_error("%s: null argument", who);
     return LR_EINVAL;
   }
   OnDevice on(p->ctx);
   if (on.rc != LR_OK) return on.rc;
-  return launch_compact_fp8(p, keep_off, keep_pages, keep_valid, *cache, new_len, n_pages_kept, reinterpret_cast<cudaStream_t>(stream));
+  return launch(p, keep_off, keep_pages, keep_valid, *cache, new_len, n_pages_kept, reinterpret_cast<cudaStream_t>(stream));
+}
+
+extern "C" int lr_compact_fp8(lr_plan *p, const int32_t *keep_off, const int32_t *keep_pages, const int32_t *keep_valid, const lr_fp8_cache *cache,
+                              int32_t *new_len, int32_t *n_pages_kept, void *stream) {
+  return cache_compact(p, keep_off, keep_pages, keep_valid, cache, new_len, n_pages_kept, stream, "lr_compact_fp8", launch_compact_fp8);
+}
+
+extern "C" int lr_fp4_write(lr_ctx *ctx, const lr_fp4_cache *cache, const void *k, int64_t k_stride, const void *v, int64_t v_stride,
+                            const int64_t *slots, int32_t n_tokens, int32_t *status, void *stream) {
+  return cache_move(ctx, cache, true, const_cast<void *>(k), k_stride, const_cast<void *>(v), v_stride, slots, n_tokens, status, stream, "lr_fp4_write", launch_fp4_move);
+}
+
+extern "C" int lr_fp4_read(lr_ctx *ctx, const lr_fp4_cache *cache, const int64_t *slots, int32_t n_tokens, void *k, int64_t k_stride, void *v,
+                           int64_t v_stride, int32_t *status, void *stream) {
+  return cache_move(ctx, cache, false, k, k_stride, v, v_stride, slots, n_tokens, status, stream, "lr_fp4_read", launch_fp4_move);
+}
+
+extern "C" int lr_verify_attention_fp4(lr_plan *p, const void *q, const lr_fp4_cache *cache, void *out, float *lse, float scale, void *stream) {
+  return cache_attention(p, q, cache, out, lse, scale, stream, "lr_verify_attention_fp4", 4, launch_attn_fp4, launch_attn_fp4_generic);
+}
+
+extern "C" int lr_compact_fp4(lr_plan *p, const int32_t *keep_off, const int32_t *keep_pages, const int32_t *keep_valid, const lr_fp4_cache *cache,
+                              int32_t *new_len, int32_t *n_pages_kept, void *stream) {
+  return cache_compact(p, keep_off, keep_pages, keep_valid, cache, new_len, n_pages_kept, stream, "lr_compact_fp4", launch_compact_fp4);
+}
+
+// ---- a cache of any kind ----------------------------------------------------------------
+static int check_kv_cache(const lr_kv_cache *c, const char *who) {
+  if (!c || c->kind < LR_KV_BF16 || c->kind > LR_KV_FP4) {
+    set_error("%s: a cache is of kind LR_KV_BF16, LR_KV_FP8 or LR_KV_FP4", who);
+    return LR_EINVAL;
+  }
+  if (c->kind != LR_KV_BF16) return check_cache(c, who);
+  if (!c->k_d || !c->v_d) {
+    set_error("%s: null cache", who);
+    return LR_EINVAL;
+  }
+  if ((((uintptr_t)c->k_d | (uintptr_t)c->v_d) & 15) != 0 || c->n_pages < 1 || c->n_pages > ((int64_t)1 << 40) || c->k_d == c->v_d) {
+    set_error("%s: the pools of a cache must be 16-byte aligned, apart and have a page at least", who);
+    return LR_EINVAL;
+  }
+  return LR_OK;
+}
+
+extern "C" int lr_rope_create(lr_rope **out, const lr_rope_spec *spec) {
+  if (!out || !spec) {
+    set_error("lr_rope_create: null argument");
+    return LR_EINVAL;
+  }
+  *out = nullptr;
+  const lr_rope_spec &s = *spec;
+  const int n = s.rot_dim / 2;
+  if (s.rot_dim < 2 || s.rot_dim > LR_ROPE_MAX_DIM || (s.rot_dim & 1) != 0 || s.scaling < LR_ROPE_PLAIN || s.scaling > LR_ROPE_SMOOTH) {
+    set_error("lr_rope_create: rot_dim must be even and within 2 .. %d, scaling one of LR_ROPE_*", LR_ROPE_MAX_DIM);
+    return LR_EINVAL;
+  }
+  const bool turns = s.scaling == LR_ROPE_PARTS || s.scaling == LR_ROPE_SMOOTH;
+  if (!(s.base > 1.0) || !isfinite(s.base) || !isfinite(s.amplitude) || (s.scaling != LR_ROPE_PLAIN && (!(s.factor >= 1.0) || !isfinite(s.factor))) ||
+      (turns && (!(s.original >= 1.0) || !isfinite(s.original) || !(s.lo > 0.0) || !(s.hi > s.lo) || !isfinite(s.hi)))) {
+    set_error("lr_rope_create: base must be above 1, factor and original at least 1, 0 < lo < hi");
+    return LR_EINVAL;
+  }
+  lr_rope *r = new (std::nothrow) lr_rope();
+  if (!r) {
+    set_error("lr_rope_create: out of host memory");
+    return LR_ENOMEM;
+  }
+  constexpr double kTurn = 6.283185307179586476925286766559;
+  // where in i the pair lies that turns so many times over the original length
+  auto place = [&](double times) { return s.rot_dim * log(s.original / (kTurn * times)) / (2.0 * log(s.base)); };
+  double first = 0.0, last = 0.0;
+  if (s.scaling == LR_ROPE_PARTS) {
+    first = std::max(floor(place(s.hi)), 0.0);
+    last = std::min(ceil(place(s.lo)), s.rot_dim - 1.0);
+  }
+  r->rot_dim = s.rot_dim;
+  r->interleaved = s.interleaved != 0;
+  for (int i = 0; i < n; ++i) {
+    const double f = pow(s.base, -2.0 * i / s.rot_dim);
+    double w = s.scaling == LR_ROPE_LINEAR ? 1.0 : 0.0;
+    if (s.scaling == LR_ROPE_SMOOTH) w = (s.hi - s.original * f / kTurn) / (s.hi - s.lo);
+    if (s.scaling == LR_ROPE_PARTS) w = (i - first) / std::max(last - first, 0.001);
+    w = std::min(std::max(w, 0.0), 1.0);
+    r->radians[i] = s.scaling == LR_ROPE_PLAIN ? f : f * (1.0 - w) + f / s.factor * w;
+    r->turns[i] = r->radians[i] / kTurn;
+  }
+  r->amplitude_64 = s.amplitude != 0.0 ? s.amplitude : s.scaling == LR_ROPE_PARTS ? 0.1 * log(s.factor) + 1.0 : 1.0;
+  r->amplitude = (float)r->amplitude_64;
+  *out = r;
+  return LR_OK;
+}
+
+extern "C" int lr_rope_destroy(lr_rope *rope) {
+  if (!rope) {
+    set_error("lr_rope_destroy: null argument");
+    return LR_EINVAL;
+  }
+  delete rope;
+  return LR_OK;
+}
+
+extern "C" int lr_rope_frequencies(const lr_rope *rope, double *radians, double *amplitude) {
+  if (!rope) {
+    set_error("lr_rope_frequencies: null argument");
+    return LR_EINVAL;
+  }
+  if (radians) std::copy(rope->radians, rope->radians + rope->rot_dim / 2, radians);
+  if (amplitude) *amplitude = rope->amplitude_64;
+  return LR_OK;
+}
+
+extern "C" int lr_rope_write(lr_ctx *ctx, const lr_rope *rope, const lr_kv_cache *cache, const int32_t *positions, const void *q, int64_t q_stride, void *q_out,
+                             const void *k, int64_t k_stride, const void *v, int64_t v_stride, const int64_t *slots, int32_t n_tokens, int32_t *status,
+                             void *stream) {
+  const char *who = "lr_rope_write";
+  if (int rc = check_kv_cache(cache, who)) return rc;
+  if (int rc = check_rows(ctx, k, k_stride, v, v_stride, slots, n_tokens, status, who)) return rc;
+  if ((q == nullptr) != (q_out == nullptr) || (rope && !positions && n_tokens > 0)) {
+    set_error("%s: null argument", who);
+    return LR_EINVAL;
+  }
+  const int64_t width = (int64_t)ctx->model.n_q_heads * ctx->model.head_dim;
+  if ((((uintptr_t)q | (uintptr_t)q_out) & 15) != 0 || ((uintptr_t)positions & 3) != 0 || (q && ((q_stride & 7) != 0 || q_stride < width))) {
+    set_error("%s: queries must be 16-byte aligned with a stride that is a multiple of 8 and >= %lld", who, (long long)width);
+    return LR_EINVAL;
+  }
+  if (q && q == q_out && q_stride != width && n_tokens > 1) {
+    set_error("%s: queries can be turned in place only where a row's stride is its width", who);
+    return LR_EINVAL;
+  }
+  if (rope && rope->rot_dim > ctx->model.head_dim) {
+    set_error("%s: rot_dim %d, but heads of %d", who, rope->rot_dim, ctx->model.head_dim);
+    return LR_EINVAL;
+  }
+  if (n_tokens == 0) return LR_OK;
+  OnDevice on(ctx);
+  if (on.rc != LR_OK) return on.rc;
+  return launch_rope_write(ctx, rope, *cache, RopeWrite{positions, q, q_stride, q_out, k, k_stride, v, v_stride, slots, n_tokens, status},
+                           reinterpret_cast<cudaStream_t>(stream));
+}
+
+extern "C" int lr_copy_pages(lr_ctx *ctx, const lr_kv_cache *src, const lr_kv_cache *dst, int32_t n_caches, const int32_t *src_pages, const int32_t *dst_pages,
+                             int32_t n_pairs, int32_t *status, void *stream) {
+  const char *who = "lr_copy_pages";
+  if (!ctx || !src || !dst || n_caches < 0 || n_pairs < 0 || (n_pairs > 0 && (!src_pages || !dst_pages))) {
+    set_error("%s: null argument or negative count", who);
+    return LR_EINVAL;
+  }
+  if ((((uintptr_t)src_pages | (uintptr_t)dst_pages | (uintptr_t)status) & 3) != 0) {
+    set_error("%s: page lists must be 4-byte aligned", who);
+    return LR_EINVAL;
+  }
+  for (int32_t c = 0; c < n_caches; ++c) {
+    if (int rc = check_kv_cache(src + c, who)) return rc;
+    if (int rc = check_kv_cache(dst + c, who)) return rc;
+    if (src[c].kind != src[0].kind || dst[c].kind != src[0].kind) {
+      set_error("%s: all caches must be of one kind", who);
+      return LR_EINVAL;
+    }
+  }
+  if (n_caches == 0 || n_pairs == 0) return LR_OK;
+  OnDevice on(ctx);
+  if (on.rc != LR_OK) return on.rc;
+  return launch_copy_pages(ctx, src, dst, n_caches, src_pages, dst_pages, n_pairs, status, reinterpret_cast<cudaStream_t>(stream));
 }
 
 // ---- status --------------------------------------------------------------------

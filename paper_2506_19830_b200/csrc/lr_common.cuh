@@ -178,6 +178,14 @@ struct lr_ctx {
   std::vector<lr::SideStream> side_free;  // of destroyed plans, kept for the next one
 };
 
+struct lr_rope {
+  int32_t rot_dim, interleaved;
+  float amplitude;
+  double radians[LR_ROPE_MAX_DIM / 2];  // a position
+  double turns[LR_ROPE_MAX_DIM / 2];
+  double amplitude_64;
+};
+
 struct lr_plan {
   lr_ctx *ctx;
   lr::DevBatch dev;
@@ -342,6 +350,7 @@ int init_commit_kernel();
 int init_attn_tc_kernel();
 int init_attn_pair_kernel();
 int init_attn_fp8_kernel();
+int init_attn_fp4_kernel();
 int init_accept_filter_kernels();
 
 int launch_attn_pair(lr_plan *p, const void *q, const void *k, const void *v, void *out, float *lse, float scale,
@@ -387,6 +396,30 @@ int launch_attn_fp8(lr_plan *p, const void *q, const lr_fp8_cache &c, void *out,
 int launch_attn_fp8_generic(lr_plan *p, const void *q, const lr_fp8_cache &c, void *out, float *lse, float scale, cudaStream_t s);
 int launch_compact_fp8(lr_plan *p, const int32_t *keep_off, const int32_t *keep_pages, const int32_t *keep_valid, const lr_fp8_cache &c,
                        int32_t *new_len, int32_t *n_pages_kept, cudaStream_t s);
+// the 4-bit cache
+int launch_fp4_move(lr_ctx *ctx, const lr_fp4_cache &c, bool write, void *k, int64_t k_stride, void *v, int64_t v_stride, const int64_t *slots,
+                    int32_t n_tokens, int32_t *status, cudaStream_t s);
+int launch_attn_fp4(lr_plan *p, const void *q, const lr_fp4_cache &c, void *out, float *lse, float scale, cudaStream_t s);
+int launch_attn_fp4_generic(lr_plan *p, const void *q, const lr_fp4_cache &c, void *out, float *lse, float scale, cudaStream_t s);
+int launch_compact_fp4(lr_plan *p, const int32_t *keep_off, const int32_t *keep_pages, const int32_t *keep_valid, const lr_fp4_cache &c,
+                       int32_t *new_len, int32_t *n_pages_kept, cudaStream_t s);
+// a cache of any kind
+struct RopeWrite {  // the arguments of lr_rope_write
+  const int32_t *positions;
+  const void *q;
+  int64_t q_stride;
+  void *q_out;
+  const void *k;
+  int64_t k_stride;
+  const void *v;
+  int64_t v_stride;
+  const int64_t *slots;
+  int32_t n_tokens;
+  int32_t *status;
+};
+int launch_rope_write(lr_ctx *ctx, const lr_rope *rope, const lr_kv_cache &c, const RopeWrite &a, cudaStream_t s);
+int launch_copy_pages(lr_ctx *ctx, const lr_kv_cache *src, const lr_kv_cache *dst, int32_t n_caches, const int32_t *src_pages, const int32_t *dst_pages,
+                      int32_t n_pairs, int32_t *status, cudaStream_t s);
 // after_accept: the launch before it in the stream is a kernel that does not write the verdicts and that lets its successor start
 // only once everything older has finished -- launch_accept's, which waits in its first line.  The verdicts are then read while it
 // still runs.

@@ -1,0 +1,276 @@
+// Rotary positions between a joint projection and attention: queries turned, keys turned and written with their values into a cache.
+//
+// A CTA takes the heads of a few tokens.  It first works out their angles: a position times a frequency in turns, in 64 bits, of which the whole turns are dropped; what is
+// left, half a turn at most, is exact to 2^-53 of the angle however far the position, and goes to sinpi and cospi in fp32.  All heads of a token share them through shared memory.
+// A thread then has 8 pairs of a head, both channels of each, so that rows may be turned where they are.  With the channels of a pair half a turned
+// part apart these are 8 channels in each half, else 16 side by side: two 16-byte loads and stores; where the halves do not start on 16 bytes
+// (rot_dim no multiple of 16) channel by channel.  For a cache in 8 or 4 bits the turned keys and the values wait in shared memory in fp32, and threads of 32 channels of a
+// row quantise them: one rounding from what was turned.
+//
+// Bound by HBM on prompts, by the launch and the chain position -> angle -> data on a pass's drafts.
+#include <math.h>
+
+#include <algorithm>
+
+#include "fp4_cache.cuh"
+
+namespace lr {
+
+namespace {
+
+constexpr int kThreads = 256;
+constexpr int kHeads = 64;       // of q, k and v together, a CTA's share of a token
+constexpr int kMaxTokens = 4;    // ... and how many tokens it takes
+constexpr int kRowBytes = 40 << 10;  // of shared memory for rows that are to be quantised
+constexpr int kPadded = kFp4Group + 4;  // floats that 32 channels take there: threads next to each other, a group each, read different banks
+
+struct RopeArgs {
+  double turns[LR_ROPE_MAX_DIM / 2];
+  float amplitude;
+  int32_t pairs, interleaved;  // pairs that are turned
+  int32_t q_heads, kv_heads, q0;  // q0: 0, or q_heads where there are no queries: the first head of the row [q | k | v] that is looked at
+  const int32_t *positions;
+  const uint16_t *q, *k, *v;
+  uint16_t *q_out;
+  int64_t q_stride, k_stride, v_stride;
+  const int64_t *slots;
+  int64_t n_slots;
+  int32_t n_tokens, tokens;  // of the call, of a CTA
+  int32_t *status;
+  uint8_t *pool[2], *scale[2];
+};
+
+__device__ __forceinline__ uint32_t bf16_pair(float a, float b) {
+  const __nv_bfloat162 t = __floats2bfloat162_rn(a, b);
+  uint32_t u;
+  memcpy(&u, &t, 4);
+  return u;
+}
+__device__ __forceinline__ float low(uint32_t w) { return __uint_as_float(w << 16); }
+__device__ __forceinline__ float high(uint32_t w) { return __uint_as_float(w & 0xFFFF0000u); }
+
+// kKind: of the cache.  kVector: the pairs of every thread start on 16 bytes.
+template <int kD, int kKind, bool kVector>
+__global__ void __launch_bounds__(kThreads)
+rope_write_kernel(const __grid_constant__ RopeArgs a) {
+  constexpr int kLanes = kD / 16;  // threads a head
+  constexpr int kRow = kD / kFp4Group * kPadded;
+  extern __shared__ __align__(16) float s_rows[];  // [token][K or V row of this CTA][kRow], of a cache in 8 or 4 bits
+  __shared__ float2 s_turn[kMaxTokens][LR_ROPE_MAX_DIM / 2];
+  __shared__ int64_t s_slot[kMaxTokens];
+  asm volatile("griddepcontrol.wait;" ::: "memory");  // the projection may be the kernel launched just before
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  const int t0 = blockIdx.x * a.tokens, n = min(a.tokens, a.n_tokens - t0);
+  const int all = a.q_heads + 2 * a.kv_heads, h0 = a.q0 + blockIdx.y * kHeads, heads = min(kHeads, all - h0);
+  const int rows0 = max(h0, a.q_heads), rows = max(h0 + heads - rows0, 0);  // K and V among them
+  for (int i = threadIdx.x; i < n * a.pairs; i += kThreads) {
+    const int t = i / a.pairs, p = i - t * a.pairs;
+    const double turns = (double)__ldcg(a.positions + t0 + t) * a.turns[p];
+    float sn, cs;
+    sincospif(2.0f * (float)(turns - rint(turns)), &sn, &cs);
+    s_turn[t][p] = make_float2(cs * a.amplitude, sn * a.amplitude);
+  }
+  if (threadIdx.x < n) {
+    int64_t slot = __ldcg(reinterpret_cast<const long long *>(a.slots) + t0 + threadIdx.x);
+    if (slot >= a.n_slots) {
+      if (a.status != nullptr) {
+        a.status[0] = LR_EBOUNDS;
+        a.status[1] = t0 + threadIdx.x;
+      }
+      slot = -1;
+    }
+    s_slot[threadIdx.x] = slot;
+  }
+  __syncthreads();
+  const int items = n * heads * kLanes;
+  for (int i = threadIdx.x; i < items; i += kThreads) {
+    const int part = i % kLanes, th = i / kLanes, t = th / heads, head = h0 + th - t * heads, token = t0 + t;
+    const bool is_q = head < a.q_heads, is_v = head >= a.q_heads + a.kv_heads;
+    const int kv = is_v ? head - a.q_heads - a.kv_heads : head - a.q_heads;
+    const int64_t slot = s_slot[t];
+    if (!is_q && slot < 0) continue;
+    const uint16_t *src = is_q ? a.q + token * a.q_stride + head * kD : is_v ? a.v + token * a.v_stride + kv * kD : a.k + token * a.k_stride + kv * kD;
+    const int p0 = part * 8;
+    const bool turned = !is_v && p0 < a.pairs;
+    // channels of the 8 pairs: c and d and the seven behind them, or the 16 from c on
+    const bool apart = turned && !a.interleaved;
+    const int c = apart ? p0 : 2 * p0, d = apart ? p0 + a.pairs : c + 8;
+    float x[8], y[8];
+    uint32_t r[8];  // as they lie; what is not turned is not touched (a NaN keeps its bits)
+    if constexpr (kVector) {
+      const uint4 u = __ldcg(reinterpret_cast<const uint4 *>(src + c)), w = __ldcg(reinterpret_cast<const uint4 *>(src + d));
+      r[0] = u.x, r[1] = u.y, r[2] = u.z, r[3] = u.w, r[4] = w.x, r[5] = w.y, r[6] = w.z, r[7] = w.w;
+      if (apart) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) x[2 * j] = low(r[j]), x[2 * j + 1] = high(r[j]), y[2 * j] = low(r[4 + j]), y[2 * j + 1] = high(r[4 + j]);
+      } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) x[j] = low(r[j]), y[j] = high(r[j]);
+      }
+    } else {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const bool halves = apart && p0 + j < a.pairs;
+        const uint32_t one = __ldcg(src + (halves ? p0 + j : 2 * (p0 + j))), two = __ldcg(src + (halves ? p0 + j + a.pairs : 2 * (p0 + j) + 1));
+        r[j] = one | two << 16;
+        x[j] = low(r[j]), y[j] = high(r[j]);
+      }
+    }
+    if (turned) {
+#pragma unroll
+      for (int j = 0; j < 8; ++j)
+        if (p0 + j < a.pairs) {
+          const float2 e = s_turn[t][p0 + j];
+          const float to = x[j] * e.x - y[j] * e.y;
+          y[j] = fmaf(x[j], e.y, y[j] * e.x);
+          x[j] = to;
+          if (!kVector || !apart) r[j] = bf16_pair(x[j], y[j]);
+        }
+      if (kVector && apart) {  // all of them are turned
+#pragma unroll
+        for (int j = 0; j < 4; ++j) r[j] = bf16_pair(x[2 * j], x[2 * j + 1]), r[4 + j] = bf16_pair(y[2 * j], y[2 * j + 1]);
+      }
+    }
+    uint16_t *dst;
+    if (is_q) dst = a.q_out + ((int64_t)token * a.q_heads + head) * kD;
+    else if (kKind == LR_KV_BF16) dst = reinterpret_cast<uint16_t *>(a.pool[is_v ? 1 : 0]) + (((slot / kPage) * a.kv_heads + kv) * kPage + slot % kPage) * kD;
+    else dst = nullptr;
+    if (kKind == LR_KV_BF16 || is_q) {
+      if constexpr (kVector) {
+        *reinterpret_cast<uint4 *>(dst + c) = make_uint4(r[0], r[1], r[2], r[3]);
+        *reinterpret_cast<uint4 *>(dst + d) = make_uint4(r[4], r[5], r[6], r[7]);
+      } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          const bool halves = apart && p0 + j < a.pairs;
+          dst[halves ? p0 + j : 2 * (p0 + j)] = (uint16_t)r[j];
+          dst[halves ? p0 + j + a.pairs : 2 * (p0 + j) + 1] = (uint16_t)(r[j] >> 16);
+        }
+      }
+    } else {
+      float *row = s_rows + (t * rows + head - rows0) * kRow;
+      auto at = [](int ch) { return ch / kFp4Group * kPadded + ch % kFp4Group; };
+      if constexpr (kVector) {
+        float4 *to_c = reinterpret_cast<float4 *>(row + at(c)), *to_d = reinterpret_cast<float4 *>(row + at(d));
+        if (apart) {
+          to_c[0] = make_float4(x[0], x[1], x[2], x[3]), to_c[1] = make_float4(x[4], x[5], x[6], x[7]);
+          to_d[0] = make_float4(y[0], y[1], y[2], y[3]), to_d[1] = make_float4(y[4], y[5], y[6], y[7]);
+        } else {
+          to_c[0] = make_float4(x[0], y[0], x[1], y[1]), to_c[1] = make_float4(x[2], y[2], x[3], y[3]);
+          to_d[0] = make_float4(x[4], y[4], x[5], y[5]), to_d[1] = make_float4(x[6], y[6], x[7], y[7]);
+        }
+      } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          const bool halves = apart && p0 + j < a.pairs;
+          row[at(halves ? p0 + j : 2 * (p0 + j))] = x[j];
+          row[at(halves ? p0 + j + a.pairs : 2 * (p0 + j) + 1)] = y[j];
+        }
+      }
+    }
+  }
+  if constexpr (kKind != LR_KV_BF16) {
+    __syncthreads();
+    constexpr int kParts = kD / kFp4Group;  // threads a row, 32 channels each
+    const int work = n * rows * kParts, loops = (work + kThreads - 1) / kThreads;
+    for (int l = 0; l < loops; ++l) {  // (whole warps: a row's threads ask one another)
+      const int i = l * kThreads + threadIdx.x, part = i % kParts, r = i / kParts, t = r / max(rows, 1), head = rows0 + r - t * rows;
+      const bool live = i < work && s_slot[t] >= 0;
+      float x[kFp4Group];
+      uint32_t top = 0;
+#pragma unroll
+      for (int j = 0; j < kFp4Group; j += 4) {
+        const float4 f = live ? *reinterpret_cast<const float4 *>(s_rows + r * kRow + part * kPadded + j) : make_float4(0.f, 0.f, 0.f, 0.f);
+        x[j] = f.x, x[j + 1] = f.y, x[j + 2] = f.z, x[j + 3] = f.w;
+#pragma unroll
+        for (int m = 0; m < 4; ++m) top = max(top, __float_as_uint(x[j + m]) & 0x7FFFFFFFu);
+      }
+      uint32_t most = top;  // of the row
+#pragma unroll
+      for (int o = kParts / 2; o > 0; o >>= 1) most = max(most, __shfl_xor_sync(0xFFFFFFFFu, most, o));
+      if (!live) continue;
+      const bool fine = most < 0x7F800000u;
+      const int side = head >= a.q_heads + a.kv_heads ? 1 : 0, kv = head - a.q_heads - side * a.kv_heads;
+      const int64_t at = ((s_slot[t] / kPage) * a.kv_heads + kv) * kPage + s_slot[t] % kPage;
+      if constexpr (kKind == LR_KV_FP4) {
+        const int byte = fp4_byte(top);
+        const float by = scale_down(byte);
+        const uint4 codes = make_uint4(fp4_codes(x, by), fp4_codes(x + 8, by), fp4_codes(x + 16, by), fp4_codes(x + 24, by));
+        reinterpret_cast<uint4 *>(a.pool[side] + at * (kD / 2))[part] = fine ? codes : make_uint4(0, 0, 0, 0);
+        a.scale[side][at * kParts + part] = (uint8_t)(fine ? (uint32_t)byte : kFp4NanScale);
+      } else {
+        const int byte = fp8_byte(most);
+        const float by = scale_down(byte);
+        uint32_t w[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) w[j] = fp8_codes(x + 4 * j, by);
+        uint4 *dst = reinterpret_cast<uint4 *>(a.pool[side] + at * kD) + part * 2;
+        dst[0] = fine ? make_uint4(w[0], w[1], w[2], w[3]) : make_uint4(0, 0, 0, 0);
+        dst[1] = fine ? make_uint4(w[4], w[5], w[6], w[7]) : make_uint4(0, 0, 0, 0);
+        if (part == 0) a.scale[side][at] = (uint8_t)(fine ? (uint32_t)byte : kFp8NanScale);
+      }
+    }
+  }
+}
+
+template <int kD, int kKind>
+int launch(const RopeArgs &a, bool vector, dim3 grid, size_t smem, cudaStream_t s) {
+  return cuda_fail(launch_dependent(vector ? rope_write_kernel<kD, kKind, true> : rope_write_kernel<kD, kKind, false>, grid, dim3(kThreads), smem, s, a),
+                   "rope_write_kernel launch");
+}
+
+}  // namespace
+
+int launch_rope_write(lr_ctx *ctx, const lr_rope *rope, const lr_kv_cache &c, const RopeWrite &w, cudaStream_t s) {
+  const lr_model &m = ctx->model;
+  RopeArgs a = {};
+  if (rope != nullptr) {
+    a.pairs = rope->rot_dim / 2;
+    a.interleaved = rope->interleaved;
+    a.amplitude = rope->amplitude;
+    std::copy(rope->turns, rope->turns + a.pairs, a.turns);
+  }
+  a.q_heads = m.n_q_heads;
+  a.kv_heads = m.n_kv_heads;
+  a.q0 = w.q != nullptr ? 0 : m.n_q_heads;
+  a.positions = w.positions;
+  a.q = reinterpret_cast<const uint16_t *>(w.q);
+  a.k = reinterpret_cast<const uint16_t *>(w.k);
+  a.v = reinterpret_cast<const uint16_t *>(w.v);
+  a.q_out = reinterpret_cast<uint16_t *>(w.q_out);
+  a.q_stride = w.q_stride;
+  a.k_stride = w.k_stride;
+  a.v_stride = w.v_stride;
+  a.slots = w.slots;
+  a.n_slots = c.n_pages * kPage;
+  a.n_tokens = w.n_tokens;
+  a.status = w.status;
+  a.pool[0] = reinterpret_cast<uint8_t *>(c.k_d);
+  a.pool[1] = reinterpret_cast<uint8_t *>(c.v_d);
+  a.scale[0] = c.k_scale_d;
+  a.scale[1] = c.v_scale_d;
+  const int heads = m.n_q_heads + 2 * m.n_kv_heads - a.q0, share = std::min(heads, kHeads), chunks = (heads + kHeads - 1) / kHeads;
+  const int rows = c.kind == LR_KV_BF16 ? 0 : std::min(share, 2 * m.n_kv_heads);
+  const int row_bytes = rows * (m.head_dim / kFp4Group) * kPadded * 4;  // of a token
+  a.tokens = 1;
+  while (2 * a.tokens <= kMaxTokens && w.n_tokens / (2 * a.tokens) * (int64_t)chunks >= 8 * ctx->sm_count && 2 * a.tokens * row_bytes <= kRowBytes)
+    a.tokens *= 2;
+  const size_t smem = (size_t)a.tokens * row_bytes;
+  const dim3 grid((unsigned)((w.n_tokens + a.tokens - 1) / a.tokens), (unsigned)chunks);
+  if (chunks > 65535) {
+    set_error("lr_rope_write: too many heads");
+    return LR_EUNSUPPORTED;
+  }
+  const bool vector = a.interleaved != 0 || a.pairs % 8 == 0;
+  ctx->launches++;
+  if (m.head_dim == 128) {
+    if (c.kind == LR_KV_BF16) return launch<128, LR_KV_BF16>(a, vector, grid, smem, s);
+    if (c.kind == LR_KV_FP8) return launch<128, LR_KV_FP8>(a, vector, grid, smem, s);
+    return launch<128, LR_KV_FP4>(a, vector, grid, smem, s);
+  }
+  if (c.kind == LR_KV_BF16) return launch<64, LR_KV_BF16>(a, vector, grid, smem, s);
+  if (c.kind == LR_KV_FP8) return launch<64, LR_KV_FP8>(a, vector, grid, smem, s);
+  return launch<64, LR_KV_FP4>(a, vector, grid, smem, s);
+}
+
+}  // namespace lr

@@ -2,8 +2,9 @@
 
 Host bookkeeping only -- which physical pages a request owns, a free list, where new tokens go -- around the
 library calls that do the work: ``lr_plan_create``, ``lr_verify_attention``, ``lr_accept_greedy``, ``lr_commit``
-and ``lr_compact``, or, with the cache in 8 bits, ``lr_fp8_write``, ``lr_verify_attention_fp8``, ``lr_compact_fp8`` and ``lr_fp8_read``; drafts that a
-model sampled are accepted by ``lr_accept_sample_drafted``.  The models are not here: the caller hands in, per cycle, the K/V of the drafted steps and of
+and ``lr_compact``, or, with the cache in 8 or 4 bits, ``lr_fp8_write``, ``lr_verify_attention_fp8``, ``lr_compact_fp8`` and ``lr_fp8_read`` and their ``fp4``
+counterparts; drafts that a model sampled are accepted by ``lr_accept_sample_drafted``.  With rotary positions ``lr_rope_write`` turns queries and keys as they come;
+``lr_copy_pages`` forks a request.  The models are not here: the caller hands in, per cycle, the K/V of the drafted steps and of
 every branch's tail, the queries, the logits and the step verdicts, as a serving engine would after running its
 draft model, target model and verifier.
 
@@ -60,19 +61,23 @@ class _HostBatch:
 
 
 class PagedCycleEngine:
-    def __init__(self, model, n_pool_pages: int, device: str = "cuda:0", kv_dtype: str = "bf16"):
-        """kv_dtype: "bf16", or "fp8" for a cache of half the size (e4m3 codes, a power of two a row)."""
-        if kv_dtype not in ("bf16", "fp8"):
-            raise ValueError(f"kv_dtype is 'bf16' or 'fp8', not {kv_dtype!r}")
+    def __init__(self, model, n_pool_pages: int, device: str = "cuda:0", kv_dtype: str = "bf16", rope: Optional[B.Rope] = None):
+        """kv_dtype: "bf16", "fp8" for a cache of half the size (e4m3 codes, a power of two a row), or "mxfp4" for one of a quarter (e2m1 codes, a power of two
+        for 32 channels).  rope: queries and keys come as the projection leaves them and are turned to their positions, a token's place in its sequence."""
+        if kv_dtype not in ("bf16", "fp8", "mxfp4"):
+            raise ValueError(f"kv_dtype is 'bf16', 'fp8' or 'mxfp4', not {kv_dtype!r}")
         self.model, self.device, self.n_pool_pages = model, device, n_pool_pages
         self.ctx = B.Context(model, torch.device(device).index or 0)
-        self.cache: Optional[B.Fp8Cache] = None
-        if kv_dtype == "fp8":
-            self.cache = B.Fp8Cache.empty(model, n_pool_pages, torch.device("cuda", self.ctx.device))
+        self.rope = rope
+        self.cache = None  # of 8 or 4 bits
+        if kv_dtype != "bf16":
+            kind = B.Fp8Cache if kv_dtype == "fp8" else B.Fp4Cache
+            self.cache = self.any_cache = kind.empty(model, n_pool_pages, torch.device("cuda", self.ctx.device))
         else:
             shape = (n_pool_pages, model.n_kv_heads, PAGE, model.head_dim)
             self.k_pool = torch.zeros(shape, dtype=torch.bfloat16, device=device)
             self.v_pool = torch.zeros(shape, dtype=torch.bfloat16, device=device)
+            self.any_cache = B.Bf16Cache(self.k_pool, self.v_pool)
         self.free: List[int] = list(range(n_pool_pages - 1, -1, -1))  # a stack: pop() hands out the lowest first
         self.pages: List[List[int]] = []
         self.length: List[int] = []
@@ -84,13 +89,24 @@ class PagedCycleEngine:
             raise RuntimeError(f"KV pool exhausted: {n} pages wanted, {len(self.free)} free")
         return [self.free.pop() for _ in range(n)]
 
-    def _write(self, pages: List[int], k_bits: np.ndarray, v_bits: np.ndarray) -> None:
-        """Token t of the span goes to slot t % 16 of pages[t // 16]."""
+    def _write(self, pages: List[int], k_bits: np.ndarray, v_bits: np.ndarray, position: int = 0, q: Optional[torch.Tensor] = None) -> None:
+        """Token t of the span goes to slot t % 16 of pages[t // 16]; it stands at `position` + t.  With rotary positions, q: the queries of its last
+        tokens, turned where they are."""
         n = len(k_bits)
         if n == 0:
             return
+        if self.rope is not None:
+            k, v, slots = R.bf16_tensor(k_bits, self.device), R.bf16_tensor(v_bits, self.device), self._slots(pages, n)
+            at = torch.arange(position, position + n, dtype=torch.int32, device=self.device)
+            behind = n if q is None else n - len(q)  # tokens without queries
+            if behind > 0:
+                self.ctx.lr_rope_write(self.rope, at[:behind], self.any_cache, k[:behind], v[:behind], slots[:behind])
+            if behind < n:
+                self.ctx.lr_rope_write(self.rope, at[behind:], self.any_cache, k[behind:], v[behind:], slots[behind:], q, q)
+            return
         if self.cache is not None:
-            self.ctx.lr_fp8_write(self.cache, R.bf16_tensor(k_bits, self.device), R.bf16_tensor(v_bits, self.device), self._slots(pages, n))
+            write = self.ctx.lr_fp8_write if isinstance(self.cache, B.Fp8Cache) else self.ctx.lr_fp4_write
+            write(self.cache, R.bf16_tensor(k_bits, self.device), R.bf16_tensor(v_bits, self.device), self._slots(pages, n))
             return
         idx_page = torch.tensor([pages[t // PAGE] for t in range(n)], device=self.device)
         idx_slot = torch.arange(n, device=self.device) % PAGE
@@ -108,13 +124,23 @@ class PagedCycleEngine:
         self.length.append(len(k_bits))
         return len(self.pages) - 1
 
+    def fork(self, r: int) -> int:
+        """A new request with the context of request r so far, in pages of its own; returns its index."""
+        pages = self._alloc(self.length[r])
+        i32 = lambda a: torch.tensor(a, dtype=torch.int32, device=self.device)  # noqa: E731
+        self.ctx.lr_copy_pages(self.any_cache, self.any_cache, i32(self.pages[r][:len(pages)]), i32(pages))
+        self.pages.append(pages)
+        self.length.append(self.length[r])
+        return len(self.pages) - 1
+
     def sequence(self, r: int) -> Tuple[np.ndarray, np.ndarray]:
-        """The committed tokens of request r, gathered from its pages: two uint16 arrays [length, H_kv, D] (of an 8-bit cache: the values its rows
-        stand for)."""
+        """The committed tokens of request r, gathered from its pages: two uint16 arrays [length, H_kv, D] (of an 8- or 4-bit cache: the values its
+        rows stand for)."""
         n = self.length[r]
         if self.cache is not None:
             k, v = (torch.empty((n, self.model.n_kv_heads, self.model.head_dim), dtype=torch.bfloat16, device=self.device) for _ in range(2))
-            self.ctx.lr_fp8_read(self.cache, self._slots(self.pages[r], n), k, v)
+            read = self.ctx.lr_fp8_read if isinstance(self.cache, B.Fp8Cache) else self.ctx.lr_fp4_read
+            read(self.cache, self._slots(self.pages[r], n), k, v)
             return R.bf16_bits(k), R.bf16_bits(v)
         idx_page = torch.tensor([self.pages[r][t // PAGE] for t in range(n)], device=self.device, dtype=torch.long)
         idx_slot = torch.arange(n, device=self.device) % PAGE
@@ -132,6 +158,7 @@ class PagedCycleEngine:
         br = {k: [] for k in ("br_req", "br_depth", "br_own_len", "br_own_slot", "br_n_draft")}
         cu_q = [0]
         tree = any(len(x.parents) for x in reqs)
+        q = R.bf16_tensor(q_bits, self.device)
 
         def place(pages: List[int]) -> int:
             first = len(page_ids)
@@ -142,16 +169,19 @@ class PagedCycleEngine:
             span_len.append(self.length[r])
             span_slot.append(place(self.pages[r][: (self.length[r] + PAGE - 1) // PAGE]))
             seg_parent.append(-1)
+            behind = [self.length[r]]  # where what continues a node stands: behind the tokens up to it
             for c, (k, v) in enumerate(x.segs):
                 pages = self._alloc(len(k))
-                self._write(pages, k, v)
+                start = behind[int(x.parents[c]) if len(x.parents) else c]
+                self._write(pages, k, v, start)
+                behind.append(start + len(k))
                 span_len.append(len(k))
                 span_slot.append(place(pages))
                 seg_parent.append(int(x.parents[c]) if len(x.parents) else c)
             req_span_off.append(len(span_len))
             for b in x.branches:
                 pages = self._alloc(len(b.k_tail))
-                self._write(pages, b.k_tail, b.v_tail)
+                self._write(pages, b.k_tail, b.v_tail, behind[b.node], q[cu_q[-1]:cu_q[-1] + b.q_len])
                 br["br_req"].append(r)
                 br["br_depth"].append(b.node)
                 br["br_own_len"].append(len(b.k_tail))
@@ -165,7 +195,6 @@ class PagedCycleEngine:
         n_req, n_branch, n_slots = len(reqs), len(br["br_req"]), len(page_ids)
         plan = B.Plan(self.ctx, batch)
         dev, i32t = self.device, dict(dtype=torch.int32, device=self.device)
-        q = R.bf16_tensor(q_bits, dev)
         vocab = logits_bits.shape[1]
         stride = (vocab + 7) // 8 * 8
 
@@ -184,7 +213,7 @@ class PagedCycleEngine:
         new_len, n_kept = torch.empty(n_req, **i32t), torch.empty(n_req, **i32t)
         v = verdict if len(verdict) else np.zeros(1, dtype=np.uint8)
         if self.cache is not None:
-            plan.lr_verify_attention_fp8(q, self.cache, out)
+            (plan.lr_verify_attention_fp8 if isinstance(self.cache, B.Fp8Cache) else plan.lr_verify_attention_fp4)(q, self.cache, out)
         else:
             plan.lr_verify_attention(q, self.k_pool, self.v_pool, out, None, 0.0, None)
         drafts = torch.from_numpy(i32(draft_ids)).to(dev)
@@ -198,7 +227,8 @@ class PagedCycleEngine:
         plan.lr_commit(torch.from_numpy(np.ascontiguousarray(v, dtype=np.uint8)).to(dev), n_accept, steps, surv, clen,
                        keep_off, keep_pages, keep_valid, free_off, free_pages, None)
         if self.cache is not None:
-            plan.lr_compact_fp8(keep_off, keep_pages, keep_valid, self.cache, new_len, n_kept)
+            compact = plan.lr_compact_fp8 if isinstance(self.cache, B.Fp8Cache) else plan.lr_compact_fp4
+            compact(keep_off, keep_pages, keep_valid, self.cache, new_len, n_kept)
         else:
             plan.lr_compact(keep_off, keep_pages, keep_valid, self.k_pool, self.v_pool, new_len, n_kept, plan.compact_scratch(), None)
         status = plan.lr_poll_status()  # synchronises the stream
