@@ -11,7 +11,7 @@ INCLUDE = os.path.join(os.path.dirname(PKG_DIR), "include")
 LIB_PATH = os.path.join(PKG_DIR, "liblr_verify.so")
 SOURCES = ["lr_api.cu", "accept_greedy.cu", "accept_sample.cu", "accept_filter.cu", "commit.cu", "pass_tail.cu", "compact.cu", "cycle_host.cu", "attn_generic.cu", "attn_tc.cu", "attn_pair.cu",
            "accept_drafted.cu", "fp8_cache.cu", "attn_fp8_generic.cu", "attn_fp8.cu", "fp4_cache.cu", "attn_fp4_generic.cu",
-           "attn_fp4.cu", "rope.cu", "copy_pages.cu"]
+           "attn_fp4.cu", "attn_fp4_few.cu", "rope.cu", "copy_pages.cu"]
 
 
 def _nvcc() -> str:

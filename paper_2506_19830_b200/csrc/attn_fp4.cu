@@ -780,12 +780,15 @@ int encode_q(lr_ctx *ctx, const void *q, int64_t n, CUtensorMap *map) {
 
 template <int kD>
 int launch(lr_plan *p, const CUtensorMap &q_map, const Fp4Pools &in, uint16_t *out, float *lse, float scale_log2, cudaStream_t s) {
-  const DevTcPlan &tc = p->tc;
   p->ctx->launches++;
-  if (int rc = cuda_fail(launch_dependent(attn_fp4_kernel<kD>, dim3((unsigned)tc.n_cta), dim3(kThreads), Shape<kD>::kSmemBytes, s, q_map, p->dev, tc, in, out, lse,
-                                          scale_log2 * (float)(1 << kShift)),
-                         "attn_fp4_kernel launch"))
-    return rc;
+  return cuda_fail(launch_dependent(attn_fp4_kernel<kD>, dim3((unsigned)p->tc.n_cta), dim3(kThreads), Shape<kD>::kSmemBytes, s, q_map, p->dev, p->tc, in, out, lse,
+                                    scale_log2 * (float)(1 << kShift)),
+                   "attn_fp4_kernel launch");
+}
+
+template <int kD>
+int launch_merge(lr_plan *p, uint16_t *out, float *lse, cudaStream_t s) {
+  const DevTcPlan &tc = p->tc;
   if (tc.n_targets == 0) return LR_OK;
   p->ctx->launches++;  // the merge grid is set up while the attention grid drains
   return cuda_fail(launch_dependent(tc.most_slots <= 4 ? attn_fp4_merge_kernel<kD, 4> : attn_fp4_merge_kernel<kD, 8>, dim3((unsigned)tc.n_targets, kD / 8),
@@ -802,10 +805,17 @@ int init_attn_fp4_kernel() {
 }
 
 int launch_attn_fp4(lr_plan *p, const void *q, const lr_fp4_cache &c, void *out, float *lse, float scale, cudaStream_t s) {
-  alignas(64) CUtensorMap q_map;
-  if (int rc = encode_q(p->ctx, q, p->dev.n_q_rows, &q_map)) return rc;
-  const Fp4Pools in = {reinterpret_cast<const uint8_t *>(c.k_d), reinterpret_cast<const uint8_t *>(c.v_d), c.k_scale_d, c.v_scale_d};
-  return (p->dev.head_dim == 128 ? launch<128> : launch<64>)(p, q_map, in, reinterpret_cast<uint16_t *>(out), lse, scale * 1.4426950408889634f, s);
+  const float scale_log2 = scale * 1.4426950408889634f;
+  auto *o = reinterpret_cast<uint16_t *>(out);
+  if (p->tc_most_rows <= kFp4FewRows) {
+    if (int rc = launch_attn_fp4_few(p, q, c, out, lse, scale_log2, s)) return rc;
+  } else {
+    alignas(64) CUtensorMap q_map;
+    if (int rc = encode_q(p->ctx, q, p->dev.n_q_rows, &q_map)) return rc;
+    const Fp4Pools in = {reinterpret_cast<const uint8_t *>(c.k_d), reinterpret_cast<const uint8_t *>(c.v_d), c.k_scale_d, c.v_scale_d};
+    if (int rc = (p->dev.head_dim == 128 ? launch<128> : launch<64>)(p, q_map, in, o, lse, scale_log2, s)) return rc;
+  }
+  return (p->dev.head_dim == 128 ? launch_merge<128> : launch_merge<64>)(p, o, lse, s);
 }
 
 }  // namespace lr

@@ -1,0 +1,403 @@
+// Attention over the 4-bit cache for few query rows (head_dim 64 or 128): single tokens, short drafts.
+//
+// With at most 16 rows to a (request, KV head) the cache's bytes are the work, and a tile of 128 rows for the tensor cores is padding.  Here a warp takes pages of 16 keys
+// by itself, from the cache into registers: codes become the operands of mma.sync where they are, without shared memory, barriers or roles.  The plan is that of attn_tc.cu
+// (pieces, partial results, merge); the warps of a CTA take a piece's pages in turn and join their sums through shared memory at its end.
+//
+//   S^T = K Q^T    16 keys x 8 queries.  A lane of quarter t = lane % 4 has of keys lane / 4 and lane / 4 + 8 the t-th quarter of the channels, one load each (which channels a
+//                  step of the product takes is free, as long as Q's are the same), of one group of 32 or half of one: a key's factor is one number a lane.
+//   O^T += V^T P^T 16 channels x 8 queries over 16 keys.  A lane has of keys 2t, 2t + 1 and the two 8 behind them an eighth of the channels.  The halves of a word of
+//                  codes are its even and its odd channels, so one byte permutation pairs two keys' and fp4_place leaves neighbouring keys of a channel side by side, as the
+//                  product wants them.  P^T comes out of S^T by movmatrix.
+//
+// Numbers are those of attn_fp4.cu: codes times a scale are bf16 numbers, 2^-kShift of what they are; weights are bf16, and the row sums are those of the rounded weights,
+// so that their rounding takes a weight's error out again where one key has most of it.  A row's reference exponent is raised when a score is more than
+// 2^kRescale above it; the lanes that see it so ask the others for the maximum then.  A row of K that stands for NaN, or a row of V, makes the score of its key no number.
+//
+// What bounds it is turning codes into operands: five instructions for a pair of them, some 400 for a page of K and V, 16 of which are products.
+#include <algorithm>
+
+#include "attn_mma.cuh"
+#include "fp4_cache.cuh"
+
+namespace lr {
+
+namespace {
+
+constexpr int kShift = 16;                  // numbers are 2^-kShift of what they are (attn_fp4.cu)
+constexpr uint32_t kMostScale = 128 + kShift;
+constexpr float kRescale = 8.0f;            // log2 units
+constexpr int kHeld = 32;                   // pieces whose records a CTA keeps in shared memory
+
+template <int kD, int kNB>
+struct Shape {
+  static constexpr int kRows = 8 * kNB;     // queries
+  // a lane's sums, queries and two pages take 128 registers for 8 queries of 128 channels, 230 for 16
+  static constexpr int kWarps = kNB == 1 ? 16 : 8, kThreads = kWarps * 32;
+  static constexpr int kStride = kD + 8;    // floats of a query's sums in shared memory: the four quarters of a warp then write to different banks
+  static constexpr int kSmemBytes = kWarps * kRows * kStride * 4;
+};
+
+struct Few {  // the pools
+  const uint16_t *q;
+  const uint8_t *k, *v, *k_scale, *v_scale;
+};
+
+__device__ __forceinline__ void mma16816(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+  asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+      : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+      : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ uint32_t transpose8(uint32_t x) {  // of 8 x 8 bf16 numbers, two a lane
+  uint32_t y;
+  asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
+  return y;
+}
+__device__ __forceinline__ int2 ld_pair(const void *p) {
+  int2 v;
+  asm volatile("ld.global.nc.v2.s32 {%0, %1}, [%2];" : "=r"(v.x), "=r"(v.y) : "l"(p));
+  return v;
+}
+// (asm so that these stay where they are written, a page ahead of their use)
+template <int kWords>
+__device__ __forceinline__ void ld_codes(uint32_t (&w)[kWords], const uint8_t *p) {
+  if constexpr (kWords == 4) asm volatile("ld.global.cg.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]) : "l"(p));
+  else if constexpr (kWords == 2) asm volatile("ld.global.cg.v2.u32 {%0, %1}, [%2];" : "=r"(w[0]), "=r"(w[1]) : "l"(p));
+  else asm volatile("ld.global.cg.u32 %0, [%1];" : "=r"(w[0]) : "l"(p));
+}
+// 2^(byte - 1 - kShift) as bf16, of the largest scales as far as it goes
+__device__ __forceinline__ uint32_t factor(uint32_t byte) { return (min(byte, kMostScale) + (126 - kShift)) << 7; }
+// ... and what is left of it
+__device__ __forceinline__ uint32_t rest(uint32_t byte) { return (byte > kMostScale && byte != kFp4NanScale ? byte - kMostScale + 127u : 127u) << 7; }
+
+template <int kD>
+struct Page {  // of a lane
+  uint32_t k[2][kD / 32], v[4][kD / 64], kb[2], vb[4];
+  uint32_t meta;
+  bool masked, there;
+};
+
+template <int kD, int kNB>
+__global__ void __launch_bounds__(Shape<kD, kNB>::kThreads, 1)
+attn_fp4_few_kernel(DevBatch d, DevTcPlan tc, Few in, uint16_t *__restrict__ out, float *__restrict__ lse, float scale_log2) {
+  using Sh = Shape<kD, kNB>;
+  constexpr int kWarps = Sh::kWarps, kThreads = Sh::kThreads, kRows = Sh::kRows, kStride = Sh::kStride, kKWords = kD / 32, kVWords = kD / 64, kMTiles = kD / 16;
+  extern __shared__ __align__(16) float s_sum[];  // [warp][query][kStride]
+  __shared__ float2 s_ml[kWarps][kRows];
+  __shared__ TcPiece s_piece[kHeld];
+  __shared__ TcReq s_req[kHeld];
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, t = lane & 3, g = lane >> 2;
+  // the plan is uploaded by copies, so it may be read in front of the wait for the kernel before
+  const int piece0 = tc.heads[blockIdx.x].piece0, piece1 = tc.heads[blockIdx.x].piece1;
+  if (threadIdx.x < kHeld && piece0 + (int)threadIdx.x < piece1) {
+    const TcPiece pi = tc.pieces[piece0 + threadIdx.x];
+    s_piece[threadIdx.x] = pi;
+    s_req[threadIdx.x] = tc.reqs[pi.req];
+  }
+  __syncthreads();
+  asm volatile("griddepcontrol.wait;" ::: "memory");  // queries and cache may come from the kernel launched just before
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  auto piece_of = [&](int pc) { return pc - piece0 < kHeld ? s_piece[pc - piece0] : tc.pieces[pc]; };
+  auto req_of = [&](int pc, const TcPiece &pi) { return pc - piece0 < kHeld ? s_req[pc - piece0] : tc.reqs[pi.req]; };
+
+  // what is asked for: entries of the page list first, then the page that the entry of the step before names
+  int ask_pc = piece0 - 1, ask_i = 0, ask_n = 0, ask_head = 0, ask_dense = 0;
+  const TcPage *ask_list = nullptr;
+  int2 entry = make_int2(0, 0);
+  int entry_head = -1;  // KV head of the entry on its way; -1: none
+  bool entry_masked = false;
+  auto ask_entry = [&]() {
+    while (ask_i >= ask_n) {
+      if (ask_pc + 1 >= piece1) {
+        entry_head = -1;
+        return;
+      }
+      ++ask_pc;
+      const TcPiece pi = piece_of(ask_pc);
+      const TcReq rq = req_of(ask_pc, pi);
+      ask_i = warp;
+      ask_n = min(pi.tile_end * kPagesPerTile, rq.n_pages) - pi.tile_begin * kPagesPerTile;
+      ask_dense = (rq.n_dense_tiles - pi.tile_begin) * kPagesPerTile;
+      ask_head = pi.kv_head;
+      ask_list = tc.pages + rq.page_off + pi.tile_begin * kPagesPerTile;
+    }
+    entry = ld_pair(ask_list + ask_i);
+    entry_head = ask_head;
+    entry_masked = ask_i >= ask_dense;
+    ask_i += kWarps;
+  };
+  auto ask_page = [&](Page<kD> &p) {
+    p.there = entry_head >= 0;
+    if (!p.there) return;
+    int32_t page = entry.x;
+    if (page < 0 || page >= d.n_pool_pages) {  // never fetch outside the pool
+      d.status[0] = kDevBounds;
+      d.status[1] = 200;
+      page = 0;
+    }
+    p.meta = (uint32_t)entry.y;
+    p.masked = entry_masked;
+    const int64_t row = (int64_t)(page * d.n_kv_heads + entry_head) * kPage;  // rows of the pools are numbered within 32 bits (tc_plan_structure)
+    const uint8_t *k = in.k + row * (kD / 2) + g * (kD / 2) + t * (kD / 8), *v = in.v + row * (kD / 2) + 2 * t * (kD / 2) + g * (kD / 16);
+    const uint8_t *ks = in.k_scale + row * (kD / kFp4Group) + g * (kD / kFp4Group) + t * (kD / 4) / kFp4Group;
+    const uint8_t *vs = in.v_scale + row * (kD / kFp4Group) + 2 * t * (kD / kFp4Group) + g * (kD / 8) / kFp4Group;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      ld_codes(p.k[i], k + i * 8 * (kD / 2));
+      p.kb[i] = ld_scale(ks + i * 8 * (kD / kFp4Group));
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int key = (i >> 1) * 8 + (i & 1);
+      ld_codes(p.v[i], v + key * (kD / 2));
+      p.vb[i] = ld_scale(vs + key * (kD / kFp4Group));
+    }
+  };
+
+  const int G = d.group;
+  Page<kD> next;
+  ask_entry();
+  ask_page(next);
+  ask_entry();
+  for (int pc = piece0; pc < piece1; ++pc) {
+    const TcPiece pi = piece_of(pc);
+    const TcReq rq = req_of(pc, pi);
+    const int rows = min(rq.n_q * G, kRows), n_pages = min(pi.tile_end * kPagesPerTile, rq.n_pages) - pi.tile_begin * kPagesPerTile;
+    uint32_t qf[kNB][kD / 8];
+    int depth[kNB][2], branch[kNB][2], limit[kNB][2];  // of this lane's columns, queries 2t and 2t + 1
+#pragma unroll
+    for (int b = 0; b < kNB; ++b) {
+      const int r = b * 8 + g;  // this lane's query of the operand
+#pragma unroll
+      for (int i = 0; i < kD / 32; ++i) {
+        uint4 x = make_uint4(0, 0, 0, 0);
+        if (r < rows)
+          x = __ldcg(reinterpret_cast<const uint4 *>(in.q + ((int64_t)(rq.q_row0 + r / G) * d.n_q_heads + pi.kv_head * G + r % G) * kD + t * (kD / 4)) + i);
+        qf[b][4 * i] = x.x, qf[b][4 * i + 1] = x.y, qf[b][4 * i + 2] = x.z, qf[b][4 * i + 3] = x.w;
+      }
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        const RowInfo ri = row_info(d, tc, rq, tc.tokens_per_mtile, pi.mtile0, b * 8 + 2 * t + e, pi.kv_head);
+        depth[b][e] = ri.depth, branch[b][e] = ri.branch, limit[b][e] = ri.limit;
+      }
+    }
+    float o[kNB][kMTiles][4], ref[kNB][2], l[kNB][2];
+#pragma unroll
+    for (int b = 0; b < kNB; ++b) {
+      ref[b][0] = ref[b][1] = -INFINITY;
+      l[b][0] = l[b][1] = 0.f;
+#pragma unroll
+      for (int m = 0; m < kMTiles; ++m) o[b][m][0] = o[b][m][1] = o[b][m][2] = o[b][m][3] = 0.f;
+    }
+#pragma unroll 1
+    for (int i = warp; i < n_pages; i += kWarps) {
+      const Page<kD> p = next;
+      ask_page(next);
+      ask_entry();
+      const uint32_t big = max(max(p.kb[0] == kFp4NanScale ? 0u : p.kb[0], p.kb[1] == kFp4NanScale ? 0u : p.kb[1]),
+                               max(max(p.vb[0] == kFp4NanScale ? 0u : p.vb[0], p.vb[1] == kFp4NanScale ? 0u : p.vb[1]),
+                                   max(p.vb[2] == kFp4NanScale ? 0u : p.vb[2], p.vb[3] == kFp4NanScale ? 0u : p.vb[3])));
+      const bool far = __any_sync(0xFFFFFFFFu, big > kMostScale);
+      const bool nan_v = __any_sync(0xFFFFFFFFu, max(max(p.vb[0], p.vb[1]), max(p.vb[2], p.vb[3])) == kFp4NanScale);
+      // scores
+      float s[kNB][4];
+#pragma unroll
+      for (int b = 0; b < kNB; ++b) s[b][0] = s[b][1] = s[b][2] = s[b][3] = 0.f;
+      {
+        uint32_t f[2], m[2];
+#pragma unroll
+        for (int j = 0; j < 2; ++j) f[j] = twice(p.kb[j] == kFp4NanScale ? 0x7FFFu : factor(p.kb[j])), m[j] = twice(rest(p.kb[j]));
+#pragma unroll
+        for (int w = 0; w < kKWords; ++w) {
+          uint32_t a[2][4];
+#pragma unroll
+          for (int j = 0; j < 2; ++j) {
+            a[j][0] = mul_bf16x2(fp4_place<0>(p.k[j][w]), f[j]);
+            a[j][1] = mul_bf16x2(fp4_place<1>(p.k[j][w]), f[j]);
+            a[j][2] = mul_bf16x2(fp4_place<2>(p.k[j][w]), f[j]);
+            a[j][3] = mul_bf16x2(fp4_place<3>(p.k[j][w]), f[j]);
+            if (far) {
+#pragma unroll
+              for (int x = 0; x < 4; ++x) a[j][x] = mul_bf16x2(a[j][x], m[j]);
+            }
+          }
+#pragma unroll
+          for (int b = 0; b < kNB; ++b) {
+            mma16816(s[b], a[0][0], a[1][0], a[0][1], a[1][1], qf[b][4 * w], qf[b][4 * w + 1]);
+            mma16816(s[b], a[0][2], a[1][2], a[0][3], a[1][3], qf[b][4 * w + 2], qf[b][4 * w + 3]);
+          }
+        }
+      }
+      const int valid = (int)(p.meta & 31u);
+      if (nan_v) {
+        // keys g and g + 8: whether a group of their rows of V stands for NaN, from the lanes that have those (key 2t + e of quarter t, channels of group of lane / 4)
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+          bool bad = false;
+#pragma unroll
+          for (int x = 0; x < 8; ++x) {
+            const uint32_t even = __shfl_sync(0xFFFFFFFFu, p.vb[2 * j], x * 4 + (g >> 1)), odd = __shfl_sync(0xFFFFFFFFu, p.vb[2 * j + 1], x * 4 + (g >> 1));
+            bad = bad || ((g & 1) != 0 ? odd : even) == kFp4NanScale;
+          }
+          if (bad) {
+#pragma unroll
+            for (int b = 0; b < kNB; ++b) s[b][2 * j] = s[b][2 * j + 1] = __uint_as_float(0x7FC00000u);
+          }
+        }
+      }
+      uint32_t pt[kNB][2];
+#pragma unroll
+      for (int b = 0; b < kNB; ++b) {
+#pragma unroll
+        for (int x = 0; x < 4; ++x) s[b][x] *= scale_log2;
+        if (p.masked) {
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+            RowInfo ri;
+            ri.depth = depth[b][e], ri.branch = branch[b][e], ri.limit = limit[b][e];
+            const int n_ok = page_n_ok(p.meta, ri);
+            if (g >= n_ok) s[b][e] = -INFINITY;
+            if (g + 8 >= n_ok) s[b][2 + e] = -INFINITY;
+          }
+        }
+        float top[2];
+        bool grow = false;
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          top[e] = fmaxf(s[b][e], s[b][2 + e]);
+          grow = grow || top[e] > ref[b][e] + kRescale;
+        }
+        if (__any_sync(0xFFFFFFFFu, grow)) {
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+#pragma unroll
+            for (int x = 4; x < 32; x <<= 1) top[e] = fmaxf(top[e], __shfl_xor_sync(0xFFFFFFFFu, top[e], x));
+            if (top[e] > ref[b][e] + kRescale) {
+              const float down = ex2(ref[b][e] - top[e]);
+              ref[b][e] = top[e];
+              l[b][e] *= down;
+#pragma unroll
+              for (int m = 0; m < kMTiles; ++m) o[b][m][e] *= down, o[b][m][2 + e] *= down;
+            }
+          }
+        }
+        const float at[2] = {ref[b][0] == -INFINITY ? 0.f : ref[b][0], ref[b][1] == -INFINITY ? 0.f : ref[b][1]};
+        const uint32_t p0 = pack_bf16(ex2(s[b][0] - at[0]), ex2(s[b][1] - at[1])), p1 = pack_bf16(ex2(s[b][2] - at[0]), ex2(s[b][3] - at[1]));
+        l[b][0] += bits_f(p0 << 16) + bits_f(p1 << 16);
+        l[b][1] += bits_f(p0 & 0xFFFF0000u) + bits_f(p1 & 0xFFFF0000u);
+        pt[b][0] = transpose8(p0);
+        pt[b][1] = transpose8(p1);
+      }
+      // O^T += V^T P^T
+      uint32_t f[2], m[2];
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        uint32_t x[2];
+#pragma unroll
+        for (int e = 0; e < 2; ++e)
+          x[e] = p.vb[2 * j + e] == kFp4NanScale || (p.masked && 2 * t + 8 * j + e >= valid) ? 0u : factor(p.vb[2 * j + e]);
+        f[j] = x[0] | x[1] << 16;
+        m[j] = rest(p.vb[2 * j]) | rest(p.vb[2 * j + 1]) << 16;
+      }
+#pragma unroll
+      for (int w = 0; w < kVWords; ++w) {
+        const uint32_t z[4] = {__byte_perm(p.v[0][w], p.v[1][w], 0x5410), __byte_perm(p.v[0][w], p.v[1][w], 0x7632), __byte_perm(p.v[2][w], p.v[3][w], 0x5410),
+                               __byte_perm(p.v[2][w], p.v[3][w], 0x7632)};
+        uint32_t a[4][4];
+#pragma unroll
+        for (int x = 0; x < 4; ++x) {
+          a[0][x] = mul_bf16x2(fp4_place<0>(z[x]), f[x >> 1]);
+          a[1][x] = mul_bf16x2(fp4_place<1>(z[x]), f[x >> 1]);
+          a[2][x] = mul_bf16x2(fp4_place<2>(z[x]), f[x >> 1]);
+          a[3][x] = mul_bf16x2(fp4_place<3>(z[x]), f[x >> 1]);
+          if (far) {
+#pragma unroll
+            for (int y = 0; y < 4; ++y) a[y][x] = mul_bf16x2(a[y][x], m[x >> 1]);
+          }
+        }
+#pragma unroll
+        for (int y = 0; y < 4; ++y)
+#pragma unroll
+          for (int b = 0; b < kNB; ++b) mma16816(o[b][4 * w + y], a[y][0], a[y][1], a[y][2], a[y][3], pt[b][0], pt[b][1]);
+      }
+    }
+    // the warps' sums, joined
+#pragma unroll
+    for (int b = 0; b < kNB; ++b) {
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+#pragma unroll
+        for (int x = 4; x < 32; x <<= 1) l[b][e] += __shfl_xor_sync(0xFFFFFFFFu, l[b][e], x);
+        const int r = b * 8 + 2 * t + e;
+        if (g == 0) s_ml[warp][r] = make_float2(ref[b][e], l[b][e]);
+        float *to = s_sum + (warp * kRows + r) * kStride + g * 2;
+#pragma unroll
+        for (int m = 0; m < kMTiles; ++m) *reinterpret_cast<float2 *>(to + m * 16) = make_float2(o[b][m][e], o[b][m][2 + e]);
+      }
+    }
+    __syncthreads();
+    const int slot = pi.slot[0];
+    for (int i = threadIdx.x; i < rows * (kD / 2); i += kThreads) {  // a pair of channels: 2m and 2m + 1 of eighth x
+      const int r = i / (kD / 2), c = i % (kD / 2), ch = (c % 8) * (kD / 8) + 2 * (c / 8);
+      float top = -INFINITY, sum = 0.f;
+      float2 acc = make_float2(0.f, 0.f);
+#pragma unroll
+      for (int w = 0; w < kWarps; ++w) top = s_ml[w][r].y != 0.f ? fmaxf(top, s_ml[w][r].x) : top;
+#pragma unroll
+      for (int w = 0; w < kWarps; ++w) {
+        const float2 ml = s_ml[w][r];
+        if (ml.y != 0.f) {  // (a warp that saw no key of the row has a sum of 0)
+          const float by = ex2(ml.x - top);
+          const float2 x = *reinterpret_cast<const float2 *>(s_sum + (w * kRows + r) * kStride + 2 * c);
+          sum = fmaf(by, ml.y, sum);
+          acc.x = fmaf(by, x.x, acc.x);
+          acc.y = fmaf(by, x.y, acc.y);
+        }
+      }
+      constexpr float kUnit = (float)(1 << kShift);
+      const int64_t q_index = (int64_t)(rq.q_row0 + r / G) * d.n_q_heads + pi.kv_head * G + r % G;
+      if (slot < 0) {
+        const float inv = kUnit / sum;
+        *reinterpret_cast<uint32_t *>(out + q_index * kD + ch) = pack_bf16(acc.x * inv, acc.y * inv);
+        if (c == 0 && lse != nullptr) lse[q_index] = (top + log2f(sum)) * 0.6931471805599453f;
+      } else {
+        *reinterpret_cast<float2 *>(tc.partial_o + (((int64_t)slot * (kD / 4) + ch / 4) * 128 + r) * 4 + ch % 4) = make_float2(acc.x * kUnit, acc.y * kUnit);
+        // a sum that is not a number must not look like that of a row that saw nothing: the merge asks whether the sum is above 0
+        if (c == 0) *reinterpret_cast<float2 *>(tc.partial_ml + ((int64_t)slot * 128 + r) * 2) = sum != sum ? make_float2(sum, 1.0f) : make_float2(top, sum);
+      }
+    }
+    __syncthreads();  // the sums have been read
+  }
+}
+
+template <int kD, int kNB>
+int launch(lr_plan *p, const Few &in, uint16_t *out, float *lse, float scale_log2, cudaStream_t s) {
+  p->ctx->launches++;
+  return cuda_fail(launch_dependent(attn_fp4_few_kernel<kD, kNB>, dim3((unsigned)p->tc.n_cta), dim3(Shape<kD, kNB>::kThreads), Shape<kD, kNB>::kSmemBytes, s, p->dev, p->tc, in, out, lse,
+                                    scale_log2 * (float)(1 << kShift)),
+                   "attn_fp4_few_kernel launch");
+}
+
+template <int kD, int kNB>
+cudaError_t allow() {
+  return cudaFuncSetAttribute(attn_fp4_few_kernel<kD, kNB>, cudaFuncAttributeMaxDynamicSharedMemorySize, Shape<kD, kNB>::kSmemBytes);
+}
+
+}  // namespace
+
+int init_attn_fp4_few_kernel() {
+  cudaError_t e = allow<128, 1>();
+  if (e == cudaSuccess) e = allow<128, 2>();
+  if (e == cudaSuccess) e = allow<64, 1>();
+  if (e == cudaSuccess) e = allow<64, 2>();
+  return cuda_fail(e, "attn_fp4_few_kernel shared-memory attribute");
+}
+
+int launch_attn_fp4_few(lr_plan *p, const void *q, const lr_fp4_cache &c, void *out, float *lse, float scale_log2, cudaStream_t s) {
+  const Few in = {reinterpret_cast<const uint16_t *>(q), reinterpret_cast<const uint8_t *>(c.k_d), reinterpret_cast<const uint8_t *>(c.v_d), c.k_scale_d, c.v_scale_d};
+  auto *o = reinterpret_cast<uint16_t *>(out);
+  if (p->dev.head_dim == 128) return p->tc_most_rows <= 8 ? launch<128, 1>(p, in, o, lse, scale_log2, s) : launch<128, 2>(p, in, o, lse, scale_log2, s);
+  return p->tc_most_rows <= 8 ? launch<64, 1>(p, in, o, lse, scale_log2, s) : launch<64, 2>(p, in, o, lse, scale_log2, s);
+}
+
+}  // namespace lr

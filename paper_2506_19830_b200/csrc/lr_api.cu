@@ -314,6 +314,7 @@ extern "C" int lr_create(lr_ctx **out, const lr_model *m, int device) {
   if (int rc = init_attn_pair_kernel()) { delete c; return rc; }
   if (int rc = init_attn_fp8_kernel()) { delete c; return rc; }
   if (int rc = init_attn_fp4_kernel()) { delete c; return rc; }
+  if (int rc = init_attn_fp4_few_kernel()) { delete c; return rc; }
   if (int rc = init_accept_filter_kernels()) { delete c; return rc; }
   SideStream side;
   if (int rc = make_side(side)) { delete c; return rc; }

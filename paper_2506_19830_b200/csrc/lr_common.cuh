@@ -195,6 +195,7 @@ struct lr_plan {
   lr::DevPairPlan pr;
   bool tc_ok;             // shape allows the tensor-core path
   bool tc_few_rows;       // some piece of it shares_keys
+  int tc_most_rows;       // query rows (tokens x heads of a group) of the (request, KV head) that has most
   // The CTA-pair plan is built and uploaded when its path is first selected.  Its tables have a part of the workspace to
   // themselves, so that launches that were captured or queued find them whatever has run since; partial results share
   // theirs with the single-CTA path's (the two never run at the same time).
@@ -351,6 +352,7 @@ int init_attn_tc_kernel();
 int init_attn_pair_kernel();
 int init_attn_fp8_kernel();
 int init_attn_fp4_kernel();
+int init_attn_fp4_few_kernel();
 int init_accept_filter_kernels();
 
 int launch_attn_pair(lr_plan *p, const void *q, const void *k, const void *v, void *out, float *lse, float scale,
@@ -400,6 +402,9 @@ int launch_compact_fp8(lr_plan *p, const int32_t *keep_off, const int32_t *keep_
 int launch_fp4_move(lr_ctx *ctx, const lr_fp4_cache &c, bool write, void *k, int64_t k_stride, void *v, int64_t v_stride, const int64_t *slots,
                     int32_t n_tokens, int32_t *status, cudaStream_t s);
 int launch_attn_fp4(lr_plan *p, const void *q, const lr_fp4_cache &c, void *out, float *lse, float scale, cudaStream_t s);
+// of a plan whose tc_most_rows is kFp4FewRows at most; without the merge
+constexpr int kFp4FewRows = 16;
+int launch_attn_fp4_few(lr_plan *p, const void *q, const lr_fp4_cache &c, void *out, float *lse, float scale_log2, cudaStream_t s);
 int launch_attn_fp4_generic(lr_plan *p, const void *q, const lr_fp4_cache &c, void *out, float *lse, float scale, cudaStream_t s);
 int launch_compact_fp4(lr_plan *p, const int32_t *keep_off, const int32_t *keep_pages, const int32_t *keep_valid, const lr_fp4_cache &c,
                        int32_t *new_len, int32_t *n_pages_kept, cudaStream_t s);
