@@ -544,7 +544,7 @@ def fp4_store_values(x: np.ndarray) -> Tuple[np.ndarray, np.ndarray]:
     g = np.where(fine[..., None], x, 0.0).reshape(*x.shape[:-1], x.shape[-1] // FP4_GROUP, FP4_GROUP)
     top = np.abs(g).max(axis=-1)
     m, x2 = np.frexp(top)  # top = m 2^x2, 1/2 <= m < 1, and 6 = 3/4 2^3
-    e = np.maximum(np.where(m > 0.75, x2 - 2, x2 - 3), -126).astype(np.int64)
+    e = np.where(top > 0, np.maximum(np.where(m > 0.75, x2 - 2, x2 - 3), -126), -126).astype(np.int64)
     y = (g / np.exp2(e.astype(np.float64))[..., None]).reshape(x.shape)
     between = (E2M1[1:] + E2M1[:-1]) / 2
     a = np.abs(y)

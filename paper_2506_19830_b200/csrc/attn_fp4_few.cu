@@ -1,7 +1,7 @@
 // Attention over the 4-bit cache for few query rows (head_dim 64 or 128): single tokens, short drafts.
 //
 // With at most 16 rows to a (request, KV head) the cache's bytes are the work, and a tile of 128 rows for the tensor cores is padding.  Here a warp takes pages of 16 keys
-// by itself, from the cache into registers: codes become the operands of mma.sync where they are, without shared memory, barriers or roles.  The plan is that of attn_tc.cu
+// by itself: codes wait in shared memory, become the operands of mma.sync in registers, and there are no barriers or roles.  The plan is that of attn_tc.cu
 // (pieces, partial results, merge); the warps of a CTA take a piece's pages in turn and join their sums through shared memory at its end.
 //
 //   S^T = K Q^T    16 keys x 8 queries.  A lane of quarter t = lane % 4 has of keys lane / 4 and lane / 4 + 8 the t-th quarter of the channels, one load each (which channels a
@@ -27,6 +27,7 @@ namespace {
 constexpr int kShift = 16;                  // numbers are 2^-kShift of what they are (attn_fp4.cu)
 constexpr uint32_t kMostScale = 128 + kShift;
 constexpr float kRescale = 8.0f;            // log2 units
+constexpr float kNoKey = -3.0e38f;          // a row's reference before its first key: everything is above it, and a score of -infinity less it is no NaN
 constexpr int kHeld = 32;                   // pieces whose records a CTA keeps in shared memory
 
 template <int kD, int kNB>
@@ -35,7 +36,10 @@ struct Shape {
   // a lane's sums, queries and two pages take 128 registers for 8 queries of 128 channels, 230 for 16
   static constexpr int kWarps = kNB == 1 ? 16 : 8, kThreads = kWarps * 32;
   static constexpr int kStride = kD + 8;    // floats of a query's sums in shared memory: the four quarters of a warp then write to different banks
-  static constexpr int kSmemBytes = kWarps * kRows * kStride * 4;
+  static constexpr int kSumBytes = kWarps * kRows * kStride * 4;
+  // pages of a warp on their way or being used: K's codes, V's, their scales, what the keys are
+  static constexpr int kStages = 4, kCodeBytes = kPage * kD / 2, kScaleBytes = kPage * kD / kFp4Group, kPageBytes = 2 * kCodeBytes + 2 * kScaleBytes + 16;
+  static constexpr int kSmemBytes = kSumBytes + kWarps * kStages * kPageBytes;
 };
 
 struct Few {  // the pools
@@ -58,31 +62,40 @@ __device__ __forceinline__ int2 ld_pair(const void *p) {
   asm volatile("ld.global.nc.v2.s32 {%0, %1}, [%2];" : "=r"(v.x), "=r"(v.y) : "l"(p));
   return v;
 }
-// (asm so that these stay where they are written, a page ahead of their use)
-template <int kWords>
-__device__ __forceinline__ void ld_codes(uint32_t (&w)[kWords], const uint8_t *p) {
-  if constexpr (kWords == 4) asm volatile("ld.global.cg.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]) : "l"(p));
-  else if constexpr (kWords == 2) asm volatile("ld.global.cg.v2.u32 {%0, %1}, [%2];" : "=r"(w[0]), "=r"(w[1]) : "l"(p));
-  else asm volatile("ld.global.cg.u32 %0, [%1];" : "=r"(w[0]) : "l"(p));
+// past L1, as everything that reads the cache (fp8_cache.cuh)
+__device__ __forceinline__ void copy16(uint32_t dst, const uint8_t *src) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
 }
-// 2^(byte - 1 - kShift) as bf16, of the largest scales as far as it goes
-__device__ __forceinline__ uint32_t factor(uint32_t byte) { return (min(byte, kMostScale) + (126 - kShift)) << 7; }
-// ... and what is left of it
-__device__ __forceinline__ uint32_t rest(uint32_t byte) { return (byte > kMostScale && byte != kFp4NanScale ? byte - kMostScale + 127u : 127u) << 7; }
-
+template <int kWords>
+__device__ __forceinline__ void ld_codes(uint32_t (&w)[kWords], uint32_t p) {
+  if constexpr (kWords == 4) asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]) : "r"(p) : "memory");
+  else if constexpr (kWords == 2) asm volatile("ld.shared.v2.u32 {%0, %1}, [%2];" : "=r"(w[0]), "=r"(w[1]) : "r"(p) : "memory");
+  else asm volatile("ld.shared.u32 %0, [%1];" : "=r"(w[0]) : "r"(p) : "memory");
+}
+__device__ __forceinline__ uint32_t ld_byte(uint32_t p) {
+  uint32_t v;
+  asm volatile("ld.shared.u8 %0, [%1];" : "=r"(v) : "r"(p) : "memory");
+  return v;
+}
+// Where 16-byte unit c of a key's row of V lies in a stage: even keys first and, with two rows to the banks' width, units swapped from four on, so that what the lanes ask for
+// at once (two units of keys 2t, t = 0 .. 3) is in different banks.
 template <int kD>
-struct Page {  // of a lane
-  uint32_t k[2][kD / 32], v[4][kD / 64], kb[2], vb[4];
-  uint32_t meta;
-  bool masked, there;
-};
+__device__ __forceinline__ uint32_t v_unit(int key, int c) {
+  const int row = (key & 8) | ((key >> 1) & 3) | ((key & 1) << 2);
+  return (uint32_t)(row * (kD / 2) + (kD == 128 ? c ^ (((key >> 2) & 1) << 1) : c) * 16);
+}
+// 2^(byte - 1 - kShift) as bf16
+__device__ __forceinline__ uint32_t factor(uint32_t byte) { return (byte + (126 - kShift)) << 7; }
+// ... as far as bf16 goes, and what is left of it
+__device__ __forceinline__ uint32_t most_of(uint32_t byte) { return factor(min(byte, kMostScale)); }
+__device__ __forceinline__ uint32_t rest_of(uint32_t byte) { return (byte > kMostScale && byte != kFp4NanScale ? byte - kMostScale + 127u : 127u) << 7; }
 
 template <int kD, int kNB>
 __global__ void __launch_bounds__(Shape<kD, kNB>::kThreads, 1)
 attn_fp4_few_kernel(DevBatch d, DevTcPlan tc, Few in, uint16_t *__restrict__ out, float *__restrict__ lse, float scale_log2) {
   using Sh = Shape<kD, kNB>;
   constexpr int kWarps = Sh::kWarps, kThreads = Sh::kThreads, kRows = Sh::kRows, kStride = Sh::kStride, kKWords = kD / 32, kVWords = kD / 64, kMTiles = kD / 16;
-  extern __shared__ __align__(16) float s_sum[];  // [warp][query][kStride]
+  extern __shared__ __align__(16) float s_sum[];  // [warp][query][kStride], then the warps' stages
   __shared__ float2 s_ml[kWarps][kRows];
   __shared__ TcPiece s_piece[kHeld];
   __shared__ TcReq s_req[kHeld];
@@ -126,39 +139,46 @@ attn_fp4_few_kernel(DevBatch d, DevTcPlan tc, Few in, uint16_t *__restrict__ out
     entry_masked = ask_i >= ask_dense;
     ask_i += kWarps;
   };
-  auto ask_page = [&](Page<kD> &p) {
-    p.there = entry_head >= 0;
-    if (!p.there) return;
-    int32_t page = entry.x;
-    if (page < 0 || page >= d.n_pool_pages) {  // never fetch outside the pool
-      d.status[0] = kDevBounds;
-      d.status[1] = 200;
-      page = 0;
-    }
-    p.meta = (uint32_t)entry.y;
-    p.masked = entry_masked;
-    const int64_t row = (int64_t)(page * d.n_kv_heads + entry_head) * kPage;  // rows of the pools are numbered within 32 bits (tc_plan_structure)
-    const uint8_t *k = in.k + row * (kD / 2) + g * (kD / 2) + t * (kD / 8), *v = in.v + row * (kD / 2) + 2 * t * (kD / 2) + g * (kD / 16);
-    const uint8_t *ks = in.k_scale + row * (kD / kFp4Group) + g * (kD / kFp4Group) + t * (kD / 4) / kFp4Group;
-    const uint8_t *vs = in.v_scale + row * (kD / kFp4Group) + 2 * t * (kD / kFp4Group) + g * (kD / 8) / kFp4Group;
+  // A page's codes and scales come by asynchronous copies, kStages - 1 pages ahead: 16 bytes a lane, twice from K and from V (once with head size 64), and 16 of scales from
+  // the first lanes.
+  constexpr int kUnits = kD / 64;  // of K, and of V, a lane copies
+  const uint32_t ring = smem_u32(s_sum) + Sh::kSumBytes + warp * (Sh::kStages * Sh::kPageBytes);
+  const int copy_key = lane / (kD / 32), copy_unit = lane % (kD / 32);
+  const uint8_t *const codes_at[2] = {in.k + lane * 16, in.v + lane * 16};
+  const uint8_t *const scales_at = (lane * 16 < Sh::kScaleBytes ? in.k_scale : in.v_scale) + lane * 16 % Sh::kScaleBytes;
+  uint32_t to_v[kUnits];
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      ld_codes(p.k[i], k + i * 8 * (kD / 2));
-      p.kb[i] = ld_scale(ks + i * 8 * (kD / kFp4Group));
-    }
+  for (int u = 0; u < kUnits; ++u) to_v[u] = Sh::kCodeBytes + v_unit<kD>(copy_key + u * 8, copy_unit);
+  uint32_t asked = 0;  // stage
+  auto ask_page = [&]() {
+    if (entry_head >= 0) {
+      int32_t page = entry.x;
+      if (page < 0 || page >= d.n_pool_pages) {  // never fetch outside the pool
+        d.status[0] = kDevBounds;
+        d.status[1] = 200;
+        page = 0;
+      }
+      const int64_t row = (page * d.n_kv_heads + entry_head) * kPage;  // rows of the pools are numbered within 32 bits (tc_plan_structure)
+      const uint32_t to = ring + asked * Sh::kPageBytes;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const int key = (i >> 1) * 8 + (i & 1);
-      ld_codes(p.v[i], v + key * (kD / 2));
-      p.vb[i] = ld_scale(vs + key * (kD / kFp4Group));
+      for (int u = 0; u < kUnits; ++u) {
+        copy16(to + u * 512 + lane * 16, codes_at[0] + row * (kD / 2) + u * 512);
+        copy16(to + to_v[u], codes_at[1] + row * (kD / 2) + u * 512);
+      }
+      if (lane * 16 < 2 * Sh::kScaleBytes) copy16(to + 2 * Sh::kCodeBytes + lane * 16, scales_at + row * (kD / kFp4Group));
+      if (lane == 0)
+        asm volatile("st.shared.v2.b32 [%0], {%1, %2};" ::"r"(to + 2 * Sh::kCodeBytes + 2 * Sh::kScaleBytes), "r"(entry.y), "r"(entry_masked ? 1 : 0) : "memory");
+      ask_entry();
     }
+    asm volatile("cp.async.commit_group;" ::: "memory");
+    asked = asked + 1 == Sh::kStages ? 0u : asked + 1;
   };
 
   const int G = d.group;
-  Page<kD> next;
   ask_entry();
-  ask_page(next);
-  ask_entry();
+#pragma unroll 1
+  for (int i = 0; i + 1 < Sh::kStages; ++i) ask_page();
+  uint32_t from = 0;  // stage
   for (int pc = piece0; pc < piece1; ++pc) {
     const TcPiece pi = piece_of(pc);
     const TcReq rq = req_of(pc, pi);
@@ -184,59 +204,69 @@ attn_fp4_few_kernel(DevBatch d, DevTcPlan tc, Few in, uint16_t *__restrict__ out
     float o[kNB][kMTiles][4], ref[kNB][2], l[kNB][2];
 #pragma unroll
     for (int b = 0; b < kNB; ++b) {
-      ref[b][0] = ref[b][1] = -INFINITY;
+      ref[b][0] = ref[b][1] = kNoKey;
       l[b][0] = l[b][1] = 0.f;
 #pragma unroll
       for (int m = 0; m < kMTiles; ++m) o[b][m][0] = o[b][m][1] = o[b][m][2] = o[b][m][3] = 0.f;
     }
 #pragma unroll 1
     for (int i = warp; i < n_pages; i += kWarps) {
-      const Page<kD> p = next;
-      ask_page(next);
-      ask_entry();
-      const uint32_t big = max(max(p.kb[0] == kFp4NanScale ? 0u : p.kb[0], p.kb[1] == kFp4NanScale ? 0u : p.kb[1]),
-                               max(max(p.vb[0] == kFp4NanScale ? 0u : p.vb[0], p.vb[1] == kFp4NanScale ? 0u : p.vb[1]),
-                                   max(p.vb[2] == kFp4NanScale ? 0u : p.vb[2], p.vb[3] == kFp4NanScale ? 0u : p.vb[3])));
-      const bool far = __any_sync(0xFFFFFFFFu, big > kMostScale);
-      const bool nan_v = __any_sync(0xFFFFFFFFu, max(max(p.vb[0], p.vb[1]), max(p.vb[2], p.vb[3])) == kFp4NanScale);
-      // scores
+      __syncwarp();  // the stage asked for next has been read
+      ask_page();
+      asm volatile("cp.async.wait_group %0;" ::"n"(Sh::kStages - 1) : "memory");
+      __syncwarp();  // what the other lanes have copied is there
+      const uint32_t at = ring + from * Sh::kPageBytes, scales = at + 2 * Sh::kCodeBytes;
+      from = from + 1 == Sh::kStages ? 0u : from + 1;
+      uint32_t k[2][kKWords], kb[2], v[4][kVWords], vb[4], what[2];
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        ld_codes(k[j], at + (g + 8 * j) * (kD / 2) + t * (kD / 8));
+        kb[j] = ld_byte(scales + (g + 8 * j) * (kD / kFp4Group) + t * (kD / 4) / kFp4Group);
+      }
+#pragma unroll
+      for (int j = 0; j < 4; ++j) vb[j] = ld_byte(scales + Sh::kScaleBytes + (2 * t + (j >> 1) * 8 + (j & 1)) * (kD / kFp4Group) + g * (kD / 8) / kFp4Group);
+      ld_codes(what, scales + 2 * Sh::kScaleBytes);
+      const uint32_t meta = what[0];
+      const bool masked = what[1] != 0u;
+      // scales beyond one factor and rows that stand for NaN: rare
+      const bool rare = __any_sync(0xFFFFFFFFu, max(max(max(kb[0], kb[1]), max(vb[0], vb[1])), max(vb[2], vb[3])) > kMostScale);
       float s[kNB][4];
 #pragma unroll
       for (int b = 0; b < kNB; ++b) s[b][0] = s[b][1] = s[b][2] = s[b][3] = 0.f;
-      {
-        uint32_t f[2], m[2];
+      uint32_t f[2] = {twice(factor(kb[0])), twice(factor(kb[1]))}, more[2] = {0, 0};
+      if (rare) {
 #pragma unroll
-        for (int j = 0; j < 2; ++j) f[j] = twice(p.kb[j] == kFp4NanScale ? 0x7FFFu : factor(p.kb[j])), m[j] = twice(rest(p.kb[j]));
+        for (int j = 0; j < 2; ++j) f[j] = twice(kb[j] == kFp4NanScale ? 0x7FFFu : most_of(kb[j])), more[j] = twice(rest_of(kb[j]));
+      }
 #pragma unroll
-        for (int w = 0; w < kKWords; ++w) {
-          uint32_t a[2][4];
+      for (int w = 0; w < kKWords; ++w) {
+        uint32_t a[2][4];
 #pragma unroll
-          for (int j = 0; j < 2; ++j) {
-            a[j][0] = mul_bf16x2(fp4_place<0>(p.k[j][w]), f[j]);
-            a[j][1] = mul_bf16x2(fp4_place<1>(p.k[j][w]), f[j]);
-            a[j][2] = mul_bf16x2(fp4_place<2>(p.k[j][w]), f[j]);
-            a[j][3] = mul_bf16x2(fp4_place<3>(p.k[j][w]), f[j]);
-            if (far) {
+        for (int j = 0; j < 2; ++j) {
+          a[j][0] = mul_bf16x2(fp4_place<0>(k[j][w]), f[j]);
+          a[j][1] = mul_bf16x2(fp4_place<1>(k[j][w]), f[j]);
+          a[j][2] = mul_bf16x2(fp4_place<2>(k[j][w]), f[j]);
+          a[j][3] = mul_bf16x2(fp4_place<3>(k[j][w]), f[j]);
+        }
+        if (rare) {
 #pragma unroll
-              for (int x = 0; x < 4; ++x) a[j][x] = mul_bf16x2(a[j][x], m[j]);
-            }
-          }
+          for (int x = 0; x < 4; ++x) a[0][x] = mul_bf16x2(a[0][x], more[0]), a[1][x] = mul_bf16x2(a[1][x], more[1]);
+        }
 #pragma unroll
-          for (int b = 0; b < kNB; ++b) {
-            mma16816(s[b], a[0][0], a[1][0], a[0][1], a[1][1], qf[b][4 * w], qf[b][4 * w + 1]);
-            mma16816(s[b], a[0][2], a[1][2], a[0][3], a[1][3], qf[b][4 * w + 2], qf[b][4 * w + 3]);
-          }
+        for (int b = 0; b < kNB; ++b) {
+          mma16816(s[b], a[0][0], a[1][0], a[0][1], a[1][1], qf[b][4 * w], qf[b][4 * w + 1]);
+          mma16816(s[b], a[0][2], a[1][2], a[0][3], a[1][3], qf[b][4 * w + 2], qf[b][4 * w + 3]);
         }
       }
-      const int valid = (int)(p.meta & 31u);
-      if (nan_v) {
+      const int valid = (int)(meta & 31u);
+      if (rare) {
         // keys g and g + 8: whether a group of their rows of V stands for NaN, from the lanes that have those (key 2t + e of quarter t, channels of group of lane / 4)
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
           bool bad = false;
-#pragma unroll
+#pragma unroll 1
           for (int x = 0; x < 8; ++x) {
-            const uint32_t even = __shfl_sync(0xFFFFFFFFu, p.vb[2 * j], x * 4 + (g >> 1)), odd = __shfl_sync(0xFFFFFFFFu, p.vb[2 * j + 1], x * 4 + (g >> 1));
+            const uint32_t even = __shfl_sync(0xFFFFFFFFu, vb[2 * j], x * 4 + (g >> 1)), odd = __shfl_sync(0xFFFFFFFFu, vb[2 * j + 1], x * 4 + (g >> 1));
             bad = bad || ((g & 1) != 0 ? odd : even) == kFp4NanScale;
           }
           if (bad) {
@@ -248,61 +278,62 @@ attn_fp4_few_kernel(DevBatch d, DevTcPlan tc, Few in, uint16_t *__restrict__ out
       uint32_t pt[kNB][2];
 #pragma unroll
       for (int b = 0; b < kNB; ++b) {
-#pragma unroll
-        for (int x = 0; x < 4; ++x) s[b][x] *= scale_log2;
-        if (p.masked) {
+        if (masked) {
 #pragma unroll
           for (int e = 0; e < 2; ++e) {
             RowInfo ri;
             ri.depth = depth[b][e], ri.branch = branch[b][e], ri.limit = limit[b][e];
-            const int n_ok = page_n_ok(p.meta, ri);
+            const int n_ok = page_n_ok(meta, ri);
             if (g >= n_ok) s[b][e] = -INFINITY;
             if (g + 8 >= n_ok) s[b][2 + e] = -INFINITY;
           }
         }
-        float top[2];
-        bool grow = false;
+        float x[4];
 #pragma unroll
-        for (int e = 0; e < 2; ++e) {
-          top[e] = fmaxf(s[b][e], s[b][2 + e]);
-          grow = grow || top[e] > ref[b][e] + kRescale;
-        }
-        if (__any_sync(0xFFFFFFFFu, grow)) {
+        for (int i = 0; i < 4; ++i) x[i] = fmaf(s[b][i], scale_log2, -ref[b][i & 1]);
+        if (__any_sync(0xFFFFFFFFu, fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])) > kRescale)) {
 #pragma unroll
           for (int e = 0; e < 2; ++e) {
+            float top = fmaxf(s[b][e], s[b][2 + e]) * scale_log2;
 #pragma unroll
-            for (int x = 4; x < 32; x <<= 1) top[e] = fmaxf(top[e], __shfl_xor_sync(0xFFFFFFFFu, top[e], x));
-            if (top[e] > ref[b][e] + kRescale) {
-              const float down = ex2(ref[b][e] - top[e]);
-              ref[b][e] = top[e];
+            for (int y = 4; y < 32; y <<= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, y));
+            if (top > ref[b][e] + kRescale) {
+              const float down = ex2(ref[b][e] - top);
+              ref[b][e] = top;
               l[b][e] *= down;
 #pragma unroll
               for (int m = 0; m < kMTiles; ++m) o[b][m][e] *= down, o[b][m][2 + e] *= down;
             }
+            x[e] = fmaf(s[b][e], scale_log2, -ref[b][e]);
+            x[2 + e] = fmaf(s[b][2 + e], scale_log2, -ref[b][e]);
           }
         }
-        const float at[2] = {ref[b][0] == -INFINITY ? 0.f : ref[b][0], ref[b][1] == -INFINITY ? 0.f : ref[b][1]};
-        const uint32_t p0 = pack_bf16(ex2(s[b][0] - at[0]), ex2(s[b][1] - at[1])), p1 = pack_bf16(ex2(s[b][2] - at[0]), ex2(s[b][3] - at[1]));
+        const uint32_t p0 = pack_bf16(ex2(x[0]), ex2(x[1])), p1 = pack_bf16(ex2(x[2]), ex2(x[3]));
         l[b][0] += bits_f(p0 << 16) + bits_f(p1 << 16);
         l[b][1] += bits_f(p0 & 0xFFFF0000u) + bits_f(p1 & 0xFFFF0000u);
         pt[b][0] = transpose8(p0);
         pt[b][1] = transpose8(p1);
       }
       // O^T += V^T P^T
-      uint32_t f[2], m[2];
 #pragma unroll
-      for (int j = 0; j < 2; ++j) {
-        uint32_t x[2];
+      for (int j = 0; j < 4; ++j) ld_codes(v[j], at + Sh::kCodeBytes + v_unit<kD>(2 * t + (j >> 1) * 8 + (j & 1), g * (kD / 16) / 16) + g * (kD / 16) % 16);
 #pragma unroll
-        for (int e = 0; e < 2; ++e)
-          x[e] = p.vb[2 * j + e] == kFp4NanScale || (p.masked && 2 * t + 8 * j + e >= valid) ? 0u : factor(p.vb[2 * j + e]);
-        f[j] = x[0] | x[1] << 16;
-        m[j] = rest(p.vb[2 * j]) | rest(p.vb[2 * j + 1]) << 16;
+      for (int j = 0; j < 2; ++j) f[j] = factor(vb[2 * j]) | factor(vb[2 * j + 1]) << 16;
+      if (rare) {
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+          f[j] = (vb[2 * j] == kFp4NanScale ? 0u : most_of(vb[2 * j])) | (vb[2 * j + 1] == kFp4NanScale ? 0u : most_of(vb[2 * j + 1])) << 16;
+          more[j] = rest_of(vb[2 * j]) | rest_of(vb[2 * j + 1]) << 16;
+        }
+      }
+      if (masked) {  // slots of no valid token
+#pragma unroll
+        for (int j = 0; j < 2; ++j) f[j] &= (2 * t + 8 * j < valid ? 0xFFFFu : 0u) | (2 * t + 8 * j + 1 < valid ? 0xFFFF0000u : 0u);
       }
 #pragma unroll
       for (int w = 0; w < kVWords; ++w) {
-        const uint32_t z[4] = {__byte_perm(p.v[0][w], p.v[1][w], 0x5410), __byte_perm(p.v[0][w], p.v[1][w], 0x7632), __byte_perm(p.v[2][w], p.v[3][w], 0x5410),
-                               __byte_perm(p.v[2][w], p.v[3][w], 0x7632)};
+        const uint32_t z[4] = {__byte_perm(v[0][w], v[1][w], 0x5410), __byte_perm(v[0][w], v[1][w], 0x7632), __byte_perm(v[2][w], v[3][w], 0x5410),
+                               __byte_perm(v[2][w], v[3][w], 0x7632)};
         uint32_t a[4][4];
 #pragma unroll
         for (int x = 0; x < 4; ++x) {
@@ -310,10 +341,12 @@ attn_fp4_few_kernel(DevBatch d, DevTcPlan tc, Few in, uint16_t *__restrict__ out
           a[1][x] = mul_bf16x2(fp4_place<1>(z[x]), f[x >> 1]);
           a[2][x] = mul_bf16x2(fp4_place<2>(z[x]), f[x >> 1]);
           a[3][x] = mul_bf16x2(fp4_place<3>(z[x]), f[x >> 1]);
-          if (far) {
+        }
+        if (rare) {
 #pragma unroll
-            for (int y = 0; y < 4; ++y) a[y][x] = mul_bf16x2(a[y][x], m[x >> 1]);
-          }
+          for (int x = 0; x < 4; ++x)
+#pragma unroll
+            for (int y = 0; y < 4; ++y) a[y][x] = mul_bf16x2(a[y][x], more[x >> 1]);
         }
 #pragma unroll
         for (int y = 0; y < 4; ++y)

@@ -12,11 +12,12 @@ constexpr int kFp4LeastScale = 1;         // 2^-126: the smallest code is 2^-1, 
 
 // A word holds the codes of channels 0 .. 7 as nibbles 0, 2, 4, 6, 1, 3, 5, 7 from the bottom: the four bits of neighbouring channels lie 16 bits apart, as two bf16
 // numbers in a register do.  Nibble J of each half moves to where bf16 has its sign, the last two bits of its exponent and the first of its fraction: the two codes times
-// 2^-126 (the exponent's bias is 127, e2m1's 1; 1/2 is a subnormal number in either).
+// 2^-126 (the exponent's bias is 127, e2m1's 1; 1/2 is a subnormal number in either).  One product puts a copy of the nibble at bits 6 and 12 of its half; shifting and
+// masking the sign and the rest apart would take four instructions, all for the same pipe.
 template <int J>
 __device__ __forceinline__ uint32_t fp4_place(uint32_t w) {
-  constexpr int kUp = 6 - 4 * J;
-  return ((kUp >= 0 ? w << (kUp & 31) : w >> (-kUp & 31)) & 0x01C001C0u) | ((w << (12 - 4 * J)) & 0x80008000u);
+  const uint32_t x = J >= 2 ? w >> 8 : w;
+  return ((J & 1) != 0 ? (x & 0x00F000F0u) * 260u : (x & 0x000F000Fu) * 4160u) & 0x81C081C0u;
 }
 __device__ __forceinline__ uint32_t mul_bf16x2(uint32_t a, uint32_t b) {
   uint32_t d;

@@ -70,7 +70,7 @@ def test_rows_that_are_not_finite_and_the_ends_of_the_range():
     assert (byte[:3] == 255).all() and not codes[:3].any() and np.isnan(O.fp4_load(codes, byte)[:3]).all()
     assert (byte[3] == 1).all() and not O.fp4_load(codes, byte)[3].any()
     assert (byte[4] == 253).all() and (O.fp4_load(codes, byte)[4] == 2.0 ** 128).all()
-    assert (codes[5] == 0x88).all()
+    assert (codes[5] == 0x88).all() and (byte[5] == 1).all()
 
 
 # ---- rotary positions ----------------------------------------------------------------------------------------------------------
