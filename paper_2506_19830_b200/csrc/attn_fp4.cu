@@ -3,27 +3,24 @@
 // The plan, the two streams of a CTA, the ring of tiles and what the issuers and the softmax threads do are those of attn_tc.cu.  What is different is how K and V get
 // into the ring: four warps bring their codes and scales from the cache and leave them there as bf16.
 //
-// Numbers.  A code times its scale has two bits of fraction at most: as bf16 it is exact, and so is its product with a bf16 query in fp32.  Codes become
-// bf16 by moving their bits (fp4_place: the code times 2^-126) and one multiplication with 2^(byte - 1 - kShift), which brings the number to 2^-kShift of what it is; the scale of
-// the softmax and the epilogue take that out again.  With kShift = 16 that factor is a bf16 number for scales up to 2^17 (channels up to 786,432) and what the cache can
-// hold below 2^-117 is lost; groups with a larger scale take a second multiplication, which a warp skips where it has none.
-//
-// A row of K or V that stands for NaN becomes a row of K that is (and zeros in V): the score of its key is no number, nor is the sum of a query that sees it, and one that does
-// not see it has a weight of 0 times finite numbers.  Slots that hold no valid token become zeros in V, whatever they held; their scores are masked.
+// Numbers.  Q, K, V and the weights are halves (attn_fp4.cuh): a code and its scale are one exactly, two instructions for a pair of codes, where bf16 takes twice as many and the
+// converters, one warp to a scheduler, are what a tile waits for.  A row of Q is scaled by a power of two, which the softmax takes out again; eight channels of K
+// and Q lie in the order in which the bytes of a word give them, those of O are put right as they are stored.  Weights lie 2^kLift above what they are when the row's
+// reference is set, and may rise to 2^15: off by 2^-12 of themselves, or by 2^-25 where they are below 2^-14, 2^-29 of the weight that set it.  Rows that this
+// does not serve are worked out once more when their piece is done (exact_row).  Slots that hold no valid token become zeros, whatever they held.
 //
 // One CTA = 16 warps in four warpgroups, registers moved with setmaxnreg (184 x 256 + 72 x 256 = 128 x 512):
-//   warps 8-11  converters, a quarter of every tile each (two pages, 32 keys).  A lane brings the 16 bytes of one group of a key, 32 channels with one scale, by an
-//               asynchronous copy into a place of its own, kRaw tiles ahead, reads them back and stores four 16-byte units of the swizzled operand; lanes are dealt to
-//               keys and groups so that eight neighbours' stores lie in different banks.
-//   warp 12     brings the queries, by TMA.
+//   warps 8-11  converters, a quarter of every tile each (two pages, 32 keys).  A lane has the 16 bytes of one group of a key at a time, 32 channels with one scale, and stores
+//               four 16-byte units of the swizzled operand; lanes are dealt to keys and groups so that eight neighbours' loads and stores lie in different banks.
+//   warp 15     brings codes and scales into shared memory, kRaw tiles ahead, by asynchronous copies of 16 bytes.
+//   warp 12     brings the queries, by TMA; the softmax threads turn them into halves where they lie, a row each.
 //   warps 13, 14  MMA issuers of stream 0 and 1.
 //   warps 0-3, 4-7  softmax of stream 0 and 1, one thread per query row.
 #include <cuda.h>
 
 #include <algorithm>
 
-#include "attn_mma.cuh"
-#include "fp4_cache.cuh"
+#include "attn_fp4.cuh"
 
 namespace lr {
 
@@ -35,8 +32,6 @@ constexpr int kMaxStages = 8;
 constexpr int kThreads = 512;
 constexpr int kTeams = 4;          // converter warps
 constexpr int kKeys = 128 / kTeams;  // of a tile, that a warp converts
-constexpr int kShift = 16;         // numbers in the ring are 2^-kShift of what they are
-constexpr int kMostScale = 128 + kShift;  // the largest scale byte whose factor, 2^(byte - 1 - kShift), is a bf16 number
 
 template <int kD>
 struct Shape {
@@ -49,13 +44,15 @@ struct Shape {
   static constexpr int kScales = kD / kFp4Group;          // scale bytes of a row
   static constexpr int kPasses = kD / 32;                 // 16-byte groups of a lane in a tile
   static constexpr int kPassKeys = kKeys / kPasses;
-  static constexpr int kCodeBytes = kKeys * kD / 2, kScaleBytes = kKeys * kScales;
-  static constexpr int kSlotBytes = kCodeBytes + 2 * kScaleBytes + 16;  // of a warp: codes, scales, V's scales beside K's, what the keys are
-  static constexpr int kRawBytes = kTeams * kRaw * kSlotBytes;
+  static constexpr int kCodeBytes = 128 * kD / 2, kScaleBytes = 128 * kScales;
+  static constexpr int kSlotBytes = kCodeBytes + kScaleBytes + 32;  // of a tile: codes, scales, valid tokens of its pages
+  static constexpr int kRawBytes = kRaw * kSlotBytes;
   static constexpr int kSmemBytes = 2 * kTileBytes + kStages * kTileBytes + kRawBytes + 4096;  // tiles, codes, Ctrl; the base must be 1024-aligned
 };
-constexpr float kRescaleThreshold = 8.0f;  // log2 units: the reference exponent follows the row maximum within 2^8
-constexpr float kRedoThreshold = 64.0f;    // log2 units: beyond this a tile is redone with its own maximum as reference
+constexpr int kMaxRaw = 6;
+constexpr float kLift = 4.0f;              // log2 units: a row's reference is set this much below its maximum so far,
+constexpr float kRescaleThreshold = 10.0f; // ... is set again once that is this much above it,
+constexpr float kRedoThreshold = 15.0f;    // ... and a tile beyond this is done again at once: halves end at 2^16
 
 struct __align__(16) Ctrl {
   TcCtaHead head;         // this CTA's record
@@ -67,7 +64,12 @@ struct __align__(16) Ctrl {
   uint32_t tmem_base;
   int abort_flag;
   uint64_t wait_limit_ns;  // bound of every wait, measured on the global timer
+  uint64_t raw_full[kMaxRaw], raw_empty[kMaxRaw], q_raw;
+  uint64_t alive_ns;      // when a warp was last seen at work that may take longer than a wait (exact_row)
+  int32_t odd_piece[4];   // 1 + the last piece of four in turn that has a scale beyond halves; converters are two pieces ahead at most
+  Fp4Call call;
   float2 ml_xch[128];     // (reference exponent, row sum) of stream 1's rows, for the in-CTA combination
+  float q_unit[2][128];   // of the rows of either M-tile: what a score is worth
 };
 static_assert(sizeof(Ctrl) <= 4096, "Ctrl must fit behind the tiles");
 static_assert(Shape<64>::kSmemBytes <= 227 * 1024 && Shape<128>::kSmemBytes <= 227 * 1024, "shared memory per CTA");
@@ -78,10 +80,6 @@ __device__ __forceinline__ void tma_load_3d(uint32_t dst, const CUtensorMap *map
       "cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5}], [%2];" ::"r"(dst),
       "l"(map), "r"(smem_u32(bar)), "r"(x), "r"(y), "r"(z)
       : "memory");
-}
-// past L1, as everything that reads the cache (fp8_cache.cuh)
-__device__ __forceinline__ void copy16(uint32_t dst, const uint8_t *src) {
-  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
 }
 __device__ __forceinline__ uint4 ld_shared(uint32_t addr) {
   uint4 v;
@@ -96,20 +94,55 @@ __device__ __forceinline__ uint32_t ld_shared_byte(uint32_t addr) {
 __device__ __forceinline__ void st_shared(uint32_t addr, const uint32_t *r) {
   asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(addr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]) : "memory");
 }
-__device__ __forceinline__ int2 ld_pair(const void *p) {
-  int2 v;
-  asm volatile("ld.global.nc.v2.s32 {%0, %1}, [%2];" : "=r"(v.x), "=r"(v.y) : "l"(p));
-  return v;
+
+extern __shared__ __align__(1024) unsigned char smem[];
+template <int kD>
+__device__ __forceinline__ Ctrl *ctrl_at() {
+  return reinterpret_cast<Ctrl *>(smem + Shape<kD>::kSmemBytes - 4096);
 }
 
-// Instruction descriptors: D fp32, A and B bf16, M = 128 (bits 24-28 = M/16), N in bits 17-22 (= N/8).
+// The bounded wait of a whole warp (as wait_bar), in functions of their own: waits that last are rare, and all roles share an SM's instruction cache.  The limit counts from when
+// somebody was last seen at exact_row.  kRole: 0 softmax, 1 the others, whose registers are fewer.
+template <int kD, int kRole>
+__device__ __noinline__ bool wait_long(uint32_t bar, uint32_t parity, int code) {
+  Ctrl *ctrl = ctrl_at<kD>();
+  uint64_t t0 = 0;
+  for (uint32_t i = 0;; ++i) {
+    uint32_t got;
+    asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, %3;\n\tselp.b32 %0, 1, 0, p;\n\t}"
+                 : "=r"(got)
+                 : "r"(bar), "r"(parity), "r"(20000u)  // suspend for at most 20 us per try
+                 : "memory");
+    if (__all_sync(0xFFFFFFFFu, got != 0u)) return true;
+    if (i == 0) t0 = global_ns();
+    if ((i & 31u) == 31u) {
+      const uint64_t since = max(t0, *reinterpret_cast<volatile uint64_t *>(&ctrl->alive_ns)), now = global_ns();
+      const bool out = now > since && now - since > ctrl->wait_limit_ns;
+      if (__any_sync(0xFFFFFFFFu, out || *reinterpret_cast<volatile int *>(&ctrl->abort_flag))) {
+        if (out) {
+          *reinterpret_cast<volatile int *>(&ctrl->abort_flag) = 1;
+          ctrl->call.status[0] = kDevTimeout;
+          ctrl->call.status[1] = code;
+        }
+        return false;
+      }
+    }
+  }
+}
+template <int kD, int kRole>
+__device__ __forceinline__ bool wait(uint64_t *bar, uint32_t parity, int code) {
+  if (__all_sync(0xFFFFFFFFu, mbar_test_wait(bar, parity) != 0u)) return true;
+  return wait_long<kD, kRole>(smem_u32(bar), parity, code);
+}
+
+// Instruction descriptors: D fp32, A and B f16, M = 128 (bits 24-28 = M/16), N in bits 17-22 (= N/8).
 // QK: N = 64 keys of a half-tile, both operands K-major.  PV: N = head size, bit 16 selects the N-major B operand.
-constexpr uint32_t kIdescBase = (1u << 4) | (1u << 7) | (1u << 10) | (8u << 24);
+constexpr uint32_t kIdescBase = (1u << 4) | (8u << 24);
 constexpr uint32_t kIdescQK = kIdescBase | ((64u >> 3) << 17);
 template <int kD>
 constexpr uint32_t kIdescPV = kIdescBase | (((uint32_t)kD >> 3) << 17) | (1u << 16);
 
-// P = exp2(scale * s - m) for 64 scores, as bf16 over the first half of the score buffer; returns the fp32 sum.  With kMax also (in the shadow of the
+// P = exp2(scale * s - m) for 64 scores, as halves over the first half of the score buffer; returns the fp32 sum.  With kMax also (in the shadow of the
 // exponentials) the maximum of the raw scores.
 template <bool kMax>
 __device__ __forceinline__ float exp_half(const uint32_t (&v)[64], uint32_t addr, float scale_log2, float neg_m, float &raw_max) {
@@ -129,8 +162,8 @@ __device__ __forceinline__ float exp_half(const uint32_t (&v)[64], uint32_t addr
     y1.y = ex2(y1.y);
     acc0 = fadd2(acc0, y0);
     acc1 = fadd2(acc1, y1);
-    pk[i >> 1] = pack_bf16(y0.x, y0.y);
-    pk[(i >> 1) + 1] = pack_bf16(y1.x, y1.y);
+    pk[i >> 1] = pack_f16(y0.x, y0.y);
+    pk[(i >> 1) + 1] = pack_f16(y1.x, y1.y);
   }
   tmem_st32(addr, pk);
   if (kMax) raw_max = fmaxf(m0, m1);
@@ -138,9 +171,29 @@ __device__ __forceinline__ float exp_half(const uint32_t (&v)[64], uint32_t addr
   return acc0.x + acc0.y;
 }
 
+// O *= alpha.  The PV product of the previous half-unit must have retired first; the one before it has (its commit precedes the s_full this thread has just
+// seen), so o_done has completed done_needed or done_needed - 1 phases and the parity says which, whether or not this thread has looked at the
+// earlier ones.
+template <int kD>
+__device__ __noinline__ bool rescale_rows(uint32_t o_addr, float alpha, uint64_t *o_done, uint32_t done_needed, int code) {
+  if (!wait<kD, 0>(o_done, (done_needed - 1) & 1u, code)) return false;
+  tc_fence_after();
+#pragma unroll 1
+  for (int ch = 0; ch < kD / 32; ++ch) {
+    uint32_t o[32];
+    tmem_ld32(o_addr + ch * 32, o);
+    tc_wait_ld();
+#pragma unroll
+    for (int c = 0; c < 32; ++c) o[c] = __float_as_uint(bits_f(o[c]) * alpha);
+    tmem_st32(o_addr + ch * 32, o);
+  }
+  tc_wait_st();
+  return true;
+}
+
 // The store epilogue of a softmax thread: row r of the accumulator at o_addr times `self` (and, when the CTA's two streams worked on the same
 // rows, of the other stream's at o_other times `other`) goes out as bf16 (slot < 0) or as an fp32 partial.  Not inlined: its two row
-// buffers must not weigh on the register allocation of the sweep.
+// buffers must not weigh on the register allocation of the sweep.  Of eight channels those that come are 0, 2, 4, 6, 1, 3, 5, 7.
 template <int kD>
 __device__ __noinline__ void store_rows(uint32_t o_addr, uint32_t o_other, int slot, float self, float other, bool other_live, float m_out, float l_out, int r,
                                         int64_t q_index, uint16_t *__restrict__ out, float *__restrict__ lse, float *__restrict__ partial_o,
@@ -172,13 +225,16 @@ __device__ __noinline__ void store_rows(uint32_t o_addr, uint32_t o_other, int s
         uint4 *dst = reinterpret_cast<uint4 *>(out + q_index * kD + ch * 32);
 #pragma unroll
         for (int j = 0; j < 4; ++j)
-          dst[j] = make_uint4(pack_bf16(bits_f(o[8 * j]), bits_f(o[8 * j + 1])), pack_bf16(bits_f(o[8 * j + 2]), bits_f(o[8 * j + 3])),
-                              pack_bf16(bits_f(o[8 * j + 4]), bits_f(o[8 * j + 5])), pack_bf16(bits_f(o[8 * j + 6]), bits_f(o[8 * j + 7])));
+          dst[j] = make_uint4(pack_bf16(bits_f(o[8 * j]), bits_f(o[8 * j + 4])), pack_bf16(bits_f(o[8 * j + 1]), bits_f(o[8 * j + 5])),
+                              pack_bf16(bits_f(o[8 * j + 2]), bits_f(o[8 * j + 6])), pack_bf16(bits_f(o[8 * j + 3]), bits_f(o[8 * j + 7])));
       } else {
         // chunk-major: 16-byte chunk k of row r at [slot][k][r], so a warp's store is 512 contiguous bytes
         uint4 *dst = reinterpret_cast<uint4 *>(partial_o) + ((int64_t)slot * (kD / 4) + ch * 8) * 128 + r;
 #pragma unroll
-        for (int j = 0; j < 8; ++j) dst[j * 128] = make_uint4(o[4 * j], o[4 * j + 1], o[4 * j + 2], o[4 * j + 3]);
+        for (int j = 0; j < 4; ++j) {
+          dst[2 * j * 128] = make_uint4(o[8 * j], o[8 * j + 4], o[8 * j + 1], o[8 * j + 5]);
+          dst[(2 * j + 1) * 128] = make_uint4(o[8 * j + 2], o[8 * j + 6], o[8 * j + 3], o[8 * j + 7]);
+        }
       }
     }
   }
@@ -192,22 +248,47 @@ __device__ __noinline__ void store_rows(uint32_t o_addr, uint32_t o_other, int s
   }
 }
 
-struct Fp4Pools {
-  const uint8_t *k, *v, *k_scale, *v_scale;
-};
-
-// The steps of a CTA's ring, tile after tile: which piece, K or V, which tile.
-struct Walk {
-  int pc, i, n, mode, tile_begin, kv_head;
-  const TcPage *pages;  // of the piece's list
-};
+// Row r of an M-tile of Q, which lies as the copy left it, as halves times a power of two; zeros where no query is.  Returns what a score is worth (NaN for a row that is not finite),
+// negative if the row has a channel too small beside its largest to be a half.
+template <int kD>
+__device__ __noinline__ float convert_row(uint32_t tile, int r, bool live) {
+  uint32_t top2 = 0, least2 = 0xFFFFFFFFu;  // of low and high halves: largest magnitudes, least ones that are not 0, less one
+#pragma unroll 1
+  for (int h = 0; h < kD / 64; ++h)
+#pragma unroll 4
+    for (int u = 0; u < 8; ++u) {
+      const uint4 x = ld_shared(tile + h * kHalfBytes + r * 128 + ((u ^ (r & 7)) << 4));
+      const uint32_t m = 0x7FFF7FFFu, a = x.x & m, b = x.y & m, c = x.z & m, d = x.w & m;
+      top2 = __vmaxu2(top2, __vmaxu2(__vmaxu2(a, b), __vmaxu2(c, d)));
+      least2 = __vminu2(least2, __vminu2(__vminu2(__vsub2(a, 0x00010001u), __vsub2(b, 0x00010001u)), __vminu2(__vsub2(c, 0x00010001u), __vsub2(d, 0x00010001u))));
+    }
+  const uint32_t top = max(top2 & 0xFFFFu, top2 >> 16), least = min(least2 & 0xFFFFu, least2 >> 16);
+  const int e = min(half_exponent(top), (int)kQMostExponent);
+  const float by = live ? __uint_as_float((uint32_t)(127 + e) << 23) : 0.f;
+  const bool odd = live && least != 0xFFFFu && ((least + 1u) >> 7) + e < 127 - 17 && top < 0x7F80u;
+#pragma unroll 1
+  for (int h = 0; h < kD / 64; ++h)
+#pragma unroll 2
+    for (int u = 0; u < 8; ++u) {
+      const uint32_t at = tile + h * kHalfBytes + r * 128 + ((u ^ (r & 7)) << 4);
+      uint4 x = ld_shared(at);
+      if (live) x = as_halves8(x);
+      else x = make_uint4(0, 0, 0, 0);  // (whatever the copy brought along, or left)
+      const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+      uint32_t t[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) t[i] = pack_f16(bits_f(w[i] << 16) * by, bits_f(w[i] & 0xFFFF0000u) * by);
+      st_shared(at, t);
+    }
+  const float worth = top < 0x7F80u ? __uint_as_float((uint32_t)(127 - e) << 23) : __uint_as_float(0x7FC00000u);
+  return !live ? 1.0f : odd ? -worth : worth;
+}
 
 template <int kD>
 __global__ void __launch_bounds__(kThreads, 1)
-attn_fp4_kernel(const __grid_constant__ CUtensorMap q_map, DevBatch d, DevTcPlan tc, Fp4Pools in, uint16_t *__restrict__ out, float *__restrict__ lse, float scale_log2) {
+attn_fp4_kernel(const __grid_constant__ CUtensorMap q_map, DevBatch d, DevTcPlan tc, const __grid_constant__ Fp4Call in) {
   using Sh = Shape<kD>;
   constexpr int kTileBytes = Sh::kTileBytes, kGroupBytes = Sh::kGroupBytes, kStages = Sh::kStages, kHalves = Sh::kHalves, kRaw = Sh::kRaw;
-  extern __shared__ __align__(1024) unsigned char smem[];
   if ((smem_u32(smem) & 1023u) != 0u) {  // the swizzled tiles need a 1024-byte aligned base
     if (threadIdx.x == 0) {
       d.status[0] = kDevBounds;
@@ -217,8 +298,8 @@ attn_fp4_kernel(const __grid_constant__ CUtensorMap q_map, DevBatch d, DevTcPlan
   }
   unsigned char *q_smem = smem;                           // two M-tiles
   unsigned char *kv_smem = smem + 2 * kTileBytes;         // kStages tiles
-  unsigned char *raw_smem = kv_smem + kStages * kTileBytes;  // [team][kRaw] codes and scales
-  Ctrl *ctrl = reinterpret_cast<Ctrl *>(raw_smem + Sh::kRawBytes);
+  unsigned char *raw_smem = kv_smem + kStages * kTileBytes;  // kRaw tiles of codes and scales
+  Ctrl *ctrl = ctrl_at<kD>();
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
 
   // the plan is uploaded by copies, so it may be read in front of the wait for the kernel before
@@ -228,19 +309,18 @@ attn_fp4_kernel(const __grid_constant__ CUtensorMap q_map, DevBatch d, DevTcPlan
     if (lane < (int)(sizeof(TcCtaHead) / 16)) reinterpret_cast<uint4 *>(&ctrl->head)[lane] = __ldg(reinterpret_cast<const uint4 *>(head) + lane);
     if (elect_one()) asm volatile("prefetch.tensormap [%0];" ::"l"(&q_map) : "memory");
     __syncwarp();
-  } else {
-    // rows of a Q tile that no copy writes must hold finite values: those behind the box of T tokens
-    const int live = tc.tokens_per_mtile * d.group, spare = (128 - live) * 8, at = threadIdx.x < 256 ? threadIdx.x : threadIdx.x - 32;  // 16-byte pieces a half-tile
-    for (int i = at; i < spare * 2 * kHalves; i += kThreads - 32)
-      *reinterpret_cast<uint4 *>(q_smem + (i / spare) * kHalfBytes + live * 128 + (i % spare) * 16) = make_uint4(0, 0, 0, 0);
-    fence_proxy_async();
   }
   if (threadIdx.x == 0) {
     for (int s = 0; s < kStages; ++s) {
       mbar_init(&ctrl->kv_full[s], kTeams);
       mbar_init(&ctrl->kv_empty[s], 2);  // one arrival per MMA issuer
     }
-    mbar_init(&ctrl->q_full, 1);
+    for (int s = 0; s < kRaw; ++s) {
+      mbar_init(&ctrl->raw_full[s], 32 + kPagesPerTile);  // the copies of every lane, and what some say of the pages
+      mbar_init(&ctrl->raw_empty[s], kTeams);
+    }
+    mbar_init(&ctrl->q_raw, 1);
+    mbar_init(&ctrl->q_full, 256);
     mbar_init(&ctrl->q_empty, 2);
     for (int s = 0; s < 2; ++s) {
       for (int h = 0; h < 2; ++h) {
@@ -253,9 +333,12 @@ attn_fp4_kernel(const __grid_constant__ CUtensorMap q_map, DevBatch d, DevTcPlan
     mbar_init(&ctrl->epi_done, 256);
     mbar_init(&ctrl->xch, 128);
     ctrl->abort_flag = 0;
+    ctrl->alive_ns = 0;
+    for (int i = 0; i < 4; ++i) ctrl->odd_piece[i] = 0;
     ctrl->wait_limit_ns = (uint64_t)tc.wait_limit_us * 1000ull;
     fence_barrier_init();
   }
+  if (threadIdx.x == 32) ctrl->call = in;
   if (warp == 12) {
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&ctrl->tmem_base)), "r"(512u)
                  : "memory");
@@ -280,113 +363,127 @@ attn_fp4_kernel(const __grid_constant__ CUtensorMap q_map, DevBatch d, DevTcPlan
       constexpr int kPasses = Sh::kPasses, kPassKeys = Sh::kPassKeys, kScales = Sh::kScales;
       // this lane's key within a pass and its group of 32 channels
       const int key0 = (lane >> 1) & (kPassKeys - 1), grp = kD == 128 ? ((lane >> 4) << 1) | (lane & 1) : lane & 1;
-      const uint32_t raw = smem_u32(raw_smem) + team * (kRaw * Sh::kSlotBytes);
+      const int key = team * kKeys + key0;
+      // where they lie in a slot (the units of keys 2 and 3 of four are swapped by two, see the copies)
+      const uint32_t raw = smem_u32(raw_smem), codes = key * (kD / 2) + (kD == 128 ? grp ^ (key0 & 2) : grp) * 16, scales = Sh::kCodeBytes + key * kScales + grp;
       // of pass 0 in a stage; the four units of 16 bytes are this ^ 16, ^ 32, ^ 48 (key0's bits below 8 do not change from pass to pass)
-      const uint32_t to0 = smem_u32(kv_smem) + (team * (kKeys / 8) + (key0 >> 3)) * kGroupBytes + (grp >> 1) * kAtomBytes + (key0 & 7) * 128 + ((((grp & 1) * 4) ^ (key0 & 7)) << 4);
-      Walk at;  // what is asked for next
-      at.pc = piece0 - 1;
-      at.i = at.n = 0;
-      int2 e = make_int2(0, 0);  // page entry of lane & 1 of this warp's two pages, of that step
+      const uint32_t to0 = smem_u32(kv_smem) + (key >> 3) * kGroupBytes + (grp >> 1) * kAtomBytes + (key0 & 7) * 128 + ((((grp & 1) * 4) ^ (key0 & 7)) << 4);
+      uint32_t ring = 0, slot = 0, slot_parity = 0;
+      bool ok = true;
+      for (int pc = piece0; pc < piece1 && ok; ++pc) {
+        const TcPiece *pi = pc == piece0 ? &head->first : tc.pieces + pc;
+        const int steps = 2 * (pi->tile_end - pi->tile_begin);
+#pragma unroll 1
+        for (int i = 0; i < steps; ++i, ++ring) {
+          const uint32_t stage = ring % kStages, parity = ((ring / kStages) & 1u) ^ 1u, from = raw + slot * Sh::kSlotBytes;
+          if (!__all_sync(0xFFFFFFFFu, mbar_test_wait2(&ctrl->raw_full[slot], slot_parity, &ctrl->kv_empty[stage], parity) == 3u)) {
+            ok = wait<kD, 1>(&ctrl->raw_full[slot], slot_parity, 211) && wait<kD, 1>(&ctrl->kv_empty[stage], parity, 210);
+            if (!ok) break;
+          }
+          // valid tokens of this warp's two pages, and whether a scale is beyond halves
+          uint32_t valid[2], word;
+          asm volatile("ld.shared.v2.u32 {%0, %1}, [%2];" : "=r"(valid[0]), "=r"(valid[1]) : "r"(from + Sh::kCodeBytes + Sh::kScaleBytes + team * 8) : "memory");
+          if constexpr (kD == 128) asm volatile("ld.shared.u32 %0, [%1];" : "=r"(word) : "r"(from + Sh::kCodeBytes + (team * kKeys + lane) * 4) : "memory");
+          else asm volatile("ld.shared.u32 %0, [%1];" : "=r"(word) : "r"(from + Sh::kCodeBytes + team * kKeys * 2 + (lane & 15) * 4) : "memory");
+          const bool whole = valid[0] + valid[1] == 2 * kPage;
+          if (__any_sync(0xFFFFFFFFu, any_odd_scale(word))) {  // (among it what a slot of no valid token holds)
+            bool odd = false;
+#pragma unroll
+            for (int x = 0; x < 4; ++x) {
+              const int k = kD == 128 ? lane : (lane & 15) * 2 + (x >> 1);
+              odd = odd || (odd_scale((word >> (8 * x)) & 0xFFu) && (k & (kPage - 1)) < (int)valid[k >> 4]);
+            }
+            if (odd) *reinterpret_cast<volatile int32_t *>(&ctrl->odd_piece[pc & 3]) = pc + 1;
+          }
+          uint32_t to = to0 + stage * kTileBytes;
+#pragma unroll 1
+          for (int p = 0; p < kPasses; ++p, to += (kPassKeys / 8) * kGroupBytes) {
+            const uint4 c = ld_shared(from + codes + p * kPassKeys * (kD / 2));
+            uint32_t f = half_factor(ld_shared_byte(from + scales + p * kPassKeys * kScales));
+            if (!whole) {
+              const int k = p * kPassKeys + key0;
+              if ((k & (kPage - 1)) >= (int)valid[k >> 4]) f = 0u;
+            }
+            uint32_t h[4];
+            halves8(h, c.x, f);
+            st_shared(to, h);
+            halves8(h, c.y, f);
+            st_shared(to ^ 16u, h);
+            halves8(h, c.z, f);
+            st_shared(to ^ 32u, h);
+            halves8(h, c.w, f);
+            st_shared(to ^ 48u, h);
+          }
+          fence_proxy_async();
+          __syncwarp();  // the slot has been read, the tile's part is written
+          if (lane == 0) {
+            mbar_arrive(&ctrl->raw_empty[slot]);
+            if (blockIdx.x == 0 && ring == 0 && team == 0 && tc.phantom_tx_bytes != 0u) mbar_arrive_expect_tx(&ctrl->kv_full[stage], tc.phantom_tx_bytes);
+            else mbar_arrive(&ctrl->kv_full[stage]);
+          }
+          if (++slot == (uint32_t)kRaw) slot = 0, slot_parity ^= 1u;
+        }
+      }
+    } else if (warp == 15) {
+      // ======================= codes and scales =================================================
+      uint32_t slot = 0, parity = 1;
+      bool ok = true;
+      // the entry of page lane & 7 of the tile asked for next, on its way a tile ahead
+      int pc = piece0 - 1, i = 0, n = 0, mode = 1, kv_head = 0;
+      const TcPage *pages = nullptr;
       bool is_v = false, more = true;
-      auto load_entry = [&]() {  // of the step at `at`, or no more
-        while (at.i >= 2 * at.n) {
-          if (++at.pc >= piece1) {
+      int2 e = make_int2(0, 0);
+      auto next_step = [&]() {
+        while (i >= 2 * n) {
+          if (++pc >= piece1) {
             more = false;
             return;
           }
-          const TcPiece *pi = at.pc == piece0 ? &head->first : tc.pieces + at.pc;
-          const TcReq *rq = at.pc == piece0 ? &head->first_req : tc.reqs + pi->req;
-          at.n = pi->tile_end - pi->tile_begin;
-          at.mode = pi->n_mt;
-          at.kv_head = pi->kv_head;
-          at.pages = tc.pages + rq->page_off + pi->tile_begin * kPagesPerTile + team * (kKeys / kPage) + (lane & 1);
-          at.i = 0;
+          const TcPiece *pi = pc == piece0 ? &head->first : tc.pieces + pc;
+          const TcReq *rq = pc == piece0 ? &head->first_req : tc.reqs + pi->req;
+          n = pi->tile_end - pi->tile_begin;
+          mode = pi->n_mt;
+          kv_head = pi->kv_head;
+          pages = tc.pages + rq->page_off + pi->tile_begin * kPagesPerTile + (lane & 7);
+          i = 0;
         }
-        const RingOrder ord(at.n, at.mode);
-        const int t = ord.step(at.i, is_v);
-        ++at.i;
-        e = ld_pair(at.pages + t * kPagesPerTile);
+        const RingOrder ord(n, mode);
+        const int t = ord.step(i, is_v);
+        ++i;
+        e = ld_pair(pages + t * kPagesPerTile);
       };
-      uint32_t asked = 0;
-      auto ask = [&]() {
-        if (more) {
-          int32_t page = e.x;
-          if (page < 0 || page >= d.n_pool_pages) {  // never fetch outside the pool
-            d.status[0] = kDevBounds;
-            d.status[1] = 200;
-            page = 0;
-          }
-          const int32_t row = (page * d.n_kv_heads + at.kv_head) * kPage;  // rows of the pools are numbered within 32 bits (tc_plan_structure)
-          const int32_t row0 = __shfl_sync(0xFFFFFFFFu, row, 0), row1 = __shfl_sync(0xFFFFFFFFu, row, 1);
-          const int32_t valid0 = __shfl_sync(0xFFFFFFFFu, e.y & 31, 0), valid1 = __shfl_sync(0xFFFFFFFFu, e.y & 31, 1);
-          const uint32_t slot = raw + (asked % kRaw) * Sh::kSlotBytes;
-          const uint8_t *codes = (is_v ? in.v : in.k) + key0 * (kD / 2) + grp * 16;
-#pragma unroll
-          for (int p = 0; p < kPasses; ++p)
-            copy16(slot + p * 512 + lane * 16, codes + (int64_t)((p * kPassKeys >= kPage ? row1 : row0) + p * kPassKeys % kPage) * (kD / 2));
-          // a page's scales are kScales units of 16 bytes; V's also beside K's, for rows that stand for NaN
-          const int u = lane & 7;
-          if (u < 2 * kScales && (lane < 8 || (lane < 16 && !is_v)))
-            copy16(slot + Sh::kCodeBytes + (lane >> 3) * Sh::kScaleBytes + u * 16,
-                   (is_v || lane >= 8 ? in.v_scale : in.k_scale) + (int64_t)(u >= kScales ? row1 : row0) * kScales + (u % kScales) * 16);
-          if (lane == 0)
-            asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %3};" ::"r"(slot + Sh::kCodeBytes + 2 * Sh::kScaleBytes), "r"(valid0), "r"(valid1), "r"(is_v ? 1 : 0) : "memory");
-          ++asked;
-          load_entry();
+      next_step();
+#pragma unroll 1
+      while (more) {
+        int32_t page = e.x;
+        if (page < 0 || page >= d.n_pool_pages) {  // never fetch outside the pool
+          d.status[0] = kDevBounds;
+          d.status[1] = 200;
+          page = 0;
         }
-        asm volatile("cp.async.commit_group;" ::: "memory");
-      };
-      load_entry();
-#pragma unroll 1
-      for (int i = 0; i + 1 < kRaw; ++i) ask();
-      bool ok = true;
-#pragma unroll 1
-      for (uint32_t ring = 0;; ++ring) {
-        ask();
-        if (ring == asked) break;
-        const uint32_t stage = ring % kStages, slot = raw + (ring % kRaw) * Sh::kSlotBytes;
-        asm volatile("cp.async.wait_group %0;" ::"n"(kRaw - 1) : "memory");
-        __syncwarp();  // the scales and the word about the keys are other lanes'
-        ok = wait_bar(&ctrl->kv_empty[stage], ((ring / kStages) & 1u) ^ 1u, ctrl, d.status, 210);
+        const int32_t row = (page * d.n_kv_heads + kv_head) * kPage;  // rows of the pools are numbered within 32 bits (tc_plan_structure)
+        const uint32_t valid = (uint32_t)e.y & 31u, to = smem_u32(raw_smem) + slot * Sh::kSlotBytes;
+        const uint8_t *codes = (is_v ? in.v : in.k) + lane * 16, *scales = is_v ? in.v_scale : in.k_scale;
+        next_step();
+        ok = wait<kD, 1>(&ctrl->raw_empty[slot], parity, 212);
         if (!ok) break;
-        const uint4 what = ld_shared(slot + Sh::kCodeBytes + 2 * Sh::kScaleBytes);
-        const bool v_tile = what.z != 0u;
-        uint32_t to = to0 + stage * kTileBytes;
-#pragma unroll 1
-        for (int p = 0; p < kPasses; ++p, to += (kPassKeys / 8) * kGroupBytes) {
-          const uint4 c = ld_shared(slot + p * 512 + lane * 16);
-          const int key = p * kPassKeys + key0;
-          const uint32_t from = slot + Sh::kCodeBytes + key * kScales + grp;
-          const uint32_t byte = ld_shared_byte(from);
-          uint32_t f = twice((min(byte, (uint32_t)kMostScale) + (126 - kShift)) << 7);
-          if (v_tile) {
-            if (byte == kFp4NanScale || (key & (kPage - 1)) >= (int)(key >= kPage ? what.y : what.x)) f = 0u;
-          } else if (byte == kFp4NanScale || ld_shared_byte(from + Sh::kScaleBytes) == kFp4NanScale) {
-            f = 0x7FFF7FFFu;
-          }
-          uint32_t h[16];
-          const uint32_t w[4] = {c.x, c.y, c.z, c.w};
+        constexpr int kCopies = kD / 64;  // of 512 bytes, a page; a key has kD / 32 units, of which those of keys 2 and 3 of four are swapped by two
+        const uint32_t unit = kD == 128 ? (uint32_t)lane ^ ((lane >> 3) & 1) << 1 : (uint32_t)lane;
 #pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            h[4 * j] = mul_bf16x2(fp4_place<0>(w[j]), f);
-            h[4 * j + 1] = mul_bf16x2(fp4_place<1>(w[j]), f);
-            h[4 * j + 2] = mul_bf16x2(fp4_place<2>(w[j]), f);
-            h[4 * j + 3] = mul_bf16x2(fp4_place<3>(w[j]), f);
-          }
-          if (__any_sync(0xFFFFFFFFu, byte > (uint32_t)kMostScale && byte != kFp4NanScale)) {
-            const uint32_t more_f = twice((byte > (uint32_t)kMostScale && byte != kFp4NanScale ? byte - kMostScale + 127u : 127u) << 7);
+        for (int p = 0; p < kPagesPerTile; ++p) {
+          const uint8_t *src = codes + (int64_t)__shfl_sync(0xFFFFFFFFu, row, p) * (kD / 2);
 #pragma unroll
-            for (int j = 0; j < 16; ++j) h[j] = mul_bf16x2(h[j], more_f);
-          }
-#pragma unroll
-          for (int j = 0; j < 4; ++j) st_shared(to ^ (j << 4), h + 4 * j);
+          for (int c = 0; c < kCopies; ++c) copy16(to + (p * kCopies + c) * 512 + unit * 16, src + c * 512);
         }
-        fence_proxy_async();
-        __syncwarp();  // the slot has been read, the tile's part is written
-        if (lane == 0) {
-          if (blockIdx.x == 0 && ring == 0 && team == 0 && tc.phantom_tx_bytes != 0u) mbar_arrive_expect_tx(&ctrl->kv_full[stage], tc.phantom_tx_bytes);
-          else mbar_arrive(&ctrl->kv_full[stage]);
+        constexpr int kScaleUnits = Sh::kScaleBytes / 16, kEach = kScaleUnits / kPagesPerTile;  // units of scales, of a page
+        const int32_t scale_row = __shfl_sync(0xFFFFFFFFu, row, (lane / kEach) & 7);
+        if (lane < kScaleUnits) copy16(to + Sh::kCodeBytes + lane * 16, scales + (int64_t)scale_row * Sh::kScales + lane % kEach * 16);
+        asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(smem_u32(&ctrl->raw_full[slot])) : "memory");
+        if (lane < kPagesPerTile) {
+          asm volatile("st.shared.u32 [%0], %1;" ::"r"(to + Sh::kCodeBytes + Sh::kScaleBytes + lane * 4), "r"(valid) : "memory");
+          mbar_arrive(&ctrl->raw_full[slot]);
         }
+        if (++slot == (uint32_t)kRaw) slot = 0, parity ^= 1u;
       }
       asm volatile("cp.async.wait_all;" ::: "memory");  // (after an abort some are still on their way)
     } else if (warp == 12) {
@@ -398,19 +495,19 @@ attn_fp4_kernel(const __grid_constant__ CUtensorMap q_map, DevBatch d, DevTcPlan
         const TcPiece pi = pc == piece0 ? head->first : tc.pieces[pc];
         const TcReq rq = pc == piece0 ? head->first_req : tc.reqs[pi.req];
         // once the MMAs of the previous piece no longer read the buffers
-        ok = wait_bar(&ctrl->q_empty, (q_count & 1u) ^ 1u, ctrl, d.status, 205);
+        ok = wait<kD, 1>(&ctrl->q_empty, (q_count & 1u) ^ 1u, 205);
         if (!ok) break;
-        if (lane == 0) mbar_arrive_expect_tx(&ctrl->q_full, (uint32_t)(pi.n_mt * kHalves) * q_box_bytes);
+        if (lane == 0) mbar_arrive_expect_tx(&ctrl->q_raw, (uint32_t)(pi.n_mt * kHalves) * q_box_bytes);
         __syncwarp();
         if (lane < kHalves * pi.n_mt)
           tma_load_3d(smem_u32(q_smem) + lane * kHalfBytes, &q_map, (lane % kHalves) * 64, pi.kv_head * G, rq.q_row0 + (pi.mtile0 + lane / kHalves) * T,
-                      &ctrl->q_full);
+                      &ctrl->q_raw);
         ++q_count;
       }
       // copies that nobody waited for, after an abort, must land before the CTA exits
       if (q_count > 0) {
         const uint64_t t0 = global_ns();
-        while (!mbar_try_wait(&ctrl->q_full, (q_count - 1u) & 1u))
+        while (!mbar_try_wait(&ctrl->q_raw, (q_count - 1u) & 1u))
           if (global_ns() - t0 > kDrainLimitNs) break;
       }
       __syncwarp();
@@ -445,9 +542,8 @@ attn_fp4_kernel(const __grid_constant__ CUtensorMap q_map, DevBatch d, DevTcPlan
           mma_ts(o_tmem, s_tmem + half * 64 + k4 * 8, b + (uint64_t)(k4 * (2 * kGroupBytes >> 4)), kIdescPV<kD>, acc || k4 != 0);
       };
       for (int pc = piece0; pc < piece1 && ok; ++pc, ++pc_idx) {
-        const TcPiece pi = pc == piece0 ? head->first : tc.pieces[pc];
-        const TcReq rq = pc == piece0 ? head->first_req : tc.reqs[pi.req];
-        const int n = pi.tile_end - pi.tile_begin, mode = pi.n_mt;
+        const TcPiece *pi = pc == piece0 ? &head->first : tc.pieces + pc;
+        const int n = pi->tile_end - pi->tile_begin, mode = pi->n_mt;
         const RingOrder ord(n, mode);
         const int my_units = mode == 2 ? n : (n - s + 1) / 2;
         const int m_tile = mode == 2 ? s : 0;
@@ -455,7 +551,7 @@ attn_fp4_kernel(const __grid_constant__ CUtensorMap q_map, DevBatch d, DevTcPlan
         // belong to the other stream and are released here
         auto need = [&](uint32_t pos, int code) -> bool {
           while (waited <= pos) {
-            if (!wait_bar(&ctrl->kv_full[waited % kStages], (waited / kStages) & 1u, ctrl, d.status, code)) return false;
+            if (!wait<kD, 1>(&ctrl->kv_full[waited % kStages], (waited / kStages) & 1u, code)) return false;
             if (waited < pos && elect_one()) mbar_arrive(&ctrl->kv_empty[waited % kStages]);
             ++waited;
           }
@@ -463,18 +559,8 @@ attn_fp4_kernel(const __grid_constant__ CUtensorMap q_map, DevBatch d, DevTcPlan
         };
         // after the MMAs that read the stage: arrives when they retire (the other issuer arrives for itself)
         auto release = [&](uint32_t pos) { tc_commit(&ctrl->kv_empty[pos % kStages]); };
-        ok = wait_bar(&ctrl->q_full, pc_idx & 1u, ctrl, d.status, 220);
+        ok = wait<kD, 1>(&ctrl->q_full, pc_idx & 1u, 220);
         if (!ok) break;
-        // the box of a last M-tile brought queries of the next request along: zeros cost the tensor core less power (attn_tc.cu)
-        const int live = min(T, rq.n_q - (pi.mtile0 + m_tile) * T) * d.group;
-        if (my_units > 0 && live < T * d.group) {
-          unsigned char *qs = q_smem + m_tile * kTileBytes;
-          for (int idx = lane; idx < (128 - live) * 8; idx += 32)
-#pragma unroll
-            for (int h = 0; h < kHalves; ++h) *reinterpret_cast<uint4 *>(qs + h * kHalfBytes + live * 128 + idx * 16) = make_uint4(0, 0, 0, 0);
-          fence_proxy_async();
-          __syncwarp();
-        }
         if (my_units > 0) {
           const uint32_t pos = ring_base + ord.pos_k(mode == 2 ? 0 : s);
           ok = need(pos, 221);
@@ -494,7 +580,7 @@ attn_fp4_kernel(const __grid_constant__ CUtensorMap q_map, DevBatch d, DevTcPlan
           // nothing to issue in this piece: still observe the previous piece's epilogue phase, so that the parity
           // wait of a later piece never finds this issuer two phases behind
           if (pc_idx > 0) {
-            ok = wait_bar(&ctrl->epi_done, (pc_idx - 1) & 1u, ctrl, d.status, 228);
+            ok = wait<kD, 1>(&ctrl->epi_done, (pc_idx - 1) & 1u, 228);
             if (!ok) break;
           }
         }
@@ -510,13 +596,13 @@ attn_fp4_kernel(const __grid_constant__ CUtensorMap q_map, DevBatch d, DevTcPlan
             if (!ok) break;
           }
           if (j == 0 && pc_idx > 0) {  // the epilogue of the previous piece has read O_0 and O_1
-            ok = wait_bar(&ctrl->epi_done, (pc_idx - 1) & 1u, ctrl, d.status, 223);
+            ok = wait<kD, 1>(&ctrl->epi_done, (pc_idx - 1) & 1u, 223);
             if (!ok) break;
           }
 #pragma unroll 1
           for (int half = 0; half < 2; ++half) {
             // P of this half is in place: O += P V, then the buffer takes the scores of the next tile's half
-            ok = wait_bar(&ctrl->p_full[s][half], p_cnt & 1u, ctrl, d.status, 224 + s);
+            ok = wait<kD, 1>(&ctrl->p_full[s][half], p_cnt & 1u, 224 + s);
             if (!ok) break;
             tc_fence_after();
             if (elect_one()) {
@@ -570,35 +656,33 @@ attn_fp4_kernel(const __grid_constant__ CUtensorMap q_map, DevBatch d, DevTcPlan
       const TcReq rq = pc == piece0 ? head->first_req : tc.reqs[pi.req];
       const int n = pi.tile_end - pi.tile_begin, mode = pi.n_mt;
       const int my_units = mode == 2 ? n : (n - s + 1) / 2;
+      const RowInfo ri = row_info(d, tc, rq, T, mode == 2 ? pi.mtile0 + s : pi.mtile0, r, pi.kv_head);
+      float sc_row = 0.f;
+      if (ok) {
+        // the queries as halves; those of one M-tile, which both streams use, by stream 0
+        if (mode == 2 || s == 0) {
+          ok = wait<kD, 0>(&ctrl->q_raw, (uint32_t)(pc - piece0) & 1u, 245);
+          if (ok) {
+            ctrl->q_unit[mode == 2 ? s : 0][r] = convert_row<kD>(smem_u32(q_smem) + (mode == 2 ? s : 0) * kTileBytes, r, ri.q_index >= 0);
+            fence_proxy_async();
+          }
+        }
+        if (ok) {
+          mbar_arrive(&ctrl->q_full);
+          ok = wait<kD, 0>(&ctrl->q_full, (uint32_t)(pc - piece0) & 1u, 246);
+          sc_row = in.scale_log2 * fabsf(ctrl->q_unit[mode == 2 ? s : 0][r]);
+        }
+      }
       if (ok && my_units > 0) {
-        const RowInfo ri = row_info(d, tc, rq, T, mode == 2 ? pi.mtile0 + s : pi.mtile0, r, pi.kv_head);
         float m_used = -INFINITY, l = 0.f, m_new = 0.f;
         bool pend = false, s_ready = false;
-        // O *= alpha.  The PV product of the previous half-unit must have retired first; the one before
-        // it has (its commit precedes the s_full this thread has just seen), so o_done has completed done_needed or
-        // done_needed - 1 phases and the parity says which, whether or not this thread has looked at the earlier ones.
-        auto rescale_o = [&](float alpha, uint32_t done_needed) -> bool {
-          if (!wait_bar(&ctrl->o_done[s], (done_needed - 1) & 1u, ctrl, d.status, 235 + s)) return false;
-          tc_fence_after();
-#pragma unroll 1
-          for (int ch = 0; ch < kD / 32; ++ch) {
-            uint32_t o[32];
-            tmem_ld32(o_addr + ch * 32, o);
-            tc_wait_ld();
-#pragma unroll
-            for (int c = 0; c < 32; ++c) o[c] = __float_as_uint(bits_f(o[c]) * alpha);
-            tmem_st32(o_addr + ch * 32, o);
-          }
-          tc_wait_st();
-          return true;
-        };
         // A warp whose 32 rows are all padding only keeps the barriers' counts: what it leaves as weights multiplies into rows
         // of O that nobody reads.
         const bool idle = __all_sync(0xFFFFFFFFu, ri.q_index < 0);
         if (idle) {
           for (int u = 0; u < 2 * my_units && ok; ++u) {
-            ok = wait_bar(&ctrl->s_full[s][u & 1], (s_cnt + (uint32_t)(u >> 1)) & 1u, ctrl, d.status, 230 + s);
-            if (ok && u + 1 == 2 * my_units) ok = wait_bar(&ctrl->o_done[s], (o_cnt + (uint32_t)u - 1) & 1u, ctrl, d.status, 237 + s);
+            ok = wait<kD, 0>(&ctrl->s_full[s][u & 1], (s_cnt + (uint32_t)(u >> 1)) & 1u, 230 + s);
+            if (ok && u + 1 == 2 * my_units) ok = wait<kD, 0>(&ctrl->o_done[s], (o_cnt + (uint32_t)u - 1) & 1u, 237 + s);
             if (ok) mbar_arrive(&ctrl->p_full[s][u & 1]);
           }
           s_cnt += (uint32_t)my_units;
@@ -613,7 +697,18 @@ attn_fp4_kernel(const __grid_constant__ CUtensorMap q_map, DevBatch d, DevTcPlan
             const uint32_t g = o_cnt + (uint32_t)(2 * j + half);  // half-units of this stream before this one
             const bool first = (j | half) == 0;
             if (!s_ready) {
-              ok = wait_bar(&ctrl->s_full[s][half], s_cnt & 1u, ctrl, d.status, 230 + s);
+              ok = wait<kD, 0>(&ctrl->s_full[s][half], s_cnt & 1u, 230 + s);
+              if (!ok) break;
+            }
+            // A growth of the maximum noticed in an earlier half-unit is applied now.
+            if (__any_sync(0xFFFFFFFFu, pend)) {
+              const float alpha = pend ? ex2(m_used - m_new) : 1.0f;
+              if (pend) {
+                l *= alpha;
+                m_used = m_new;
+                pend = false;
+              }
+              ok = rescale_rows<kD>(o_addr, alpha, &ctrl->o_done[s], g, 235 + s);
               if (!ok) break;
             }
             tc_fence_after();
@@ -628,48 +723,35 @@ attn_fp4_kernel(const __grid_constant__ CUtensorMap q_map, DevBatch d, DevTcPlan
               for (int p = 0; p < kPagesPerTile / 2; ++p) n_ok[p] = page_n_ok(__ldg(&pages[half * 4 + p].meta), ri);
               mask_half(v, n_ok);
             }
-            // A growth of the maximum noticed in an earlier half-unit is applied now.
-            if (__any_sync(0xFFFFFFFFu, pend)) {
-              const float alpha = pend ? ex2(m_used - m_new) : 1.0f;
-              if (pend) {
-                l *= alpha;
-                m_used = m_new;
-                pend = false;
-              }
-              ok = rescale_o(alpha, g);
-              if (!ok) break;
-            }
             float sum = 0.f, mx, raw;
             // Fast path: exponentials against the running reference exponent; the maximum of the 64 scores is
             // computed beside them and only checked afterwards.
             bool fast = __all_sync(0xFFFFFFFFu, m_used > -INFINITY);
             if (fast) {
-              sum = exp_half<true>(v, sh_addr, scale_log2, -m_used, raw);
-              mx = raw * scale_log2;
+              sum = exp_half<true>(v, sh_addr, sc_row, -m_used, raw);
+              mx = raw * sc_row;
               if (__any_sync(0xFFFFFFFFu, mx > m_used + kRedoThreshold)) fast = false;  // could overflow: redo exactly
             } else {
-              mx = max_half(v) * scale_log2;
+              mx = max_half(v) * sc_row;
             }
             if (!fast) {
               // Exact path (first half-unit of a stream, rows that have seen no key yet, a jump of the
               // scores): adopt the maximum before the exponentials.
               const bool grow = mx > m_used + kRescaleThreshold;
-              if (__any_sync(0xFFFFFFFFu, grow)) {
-                const float alpha = grow ? ex2(m_used - mx) : 1.0f;
-                if (grow) {
-                  l *= alpha;
-                  m_used = mx;
-                }
-                if (!first) {
-                  ok = rescale_o(alpha, g);
-                  if (!ok) break;
-                }
+              const float alpha = grow ? ex2(m_used - (mx - kLift)) : 1.0f;
+              if (grow) {
+                l *= alpha;
+                m_used = mx - kLift;
               }
               tc_wait_st();
-              sum = exp_half<false>(v, sh_addr, scale_log2, (m_used == -INFINITY) ? 0.f : -m_used, raw);
+              sum = exp_half<false>(v, sh_addr, sc_row, (m_used == -INFINITY) ? 0.f : -m_used, raw);
+              if (!first && __any_sync(0xFFFFFFFFu, grow)) {  // (the scores are no longer held then)
+                ok = rescale_rows<kD>(o_addr, alpha, &ctrl->o_done[s], g, 235 + s);
+                if (!ok) break;
+              }
             } else if (mx > m_used + kRescaleThreshold) {
               pend = true;
-              m_new = mx;
+              m_new = mx - kLift;
             }
             l += sum;
             tc_wait_st();
@@ -678,7 +760,7 @@ attn_fp4_kernel(const __grid_constant__ CUtensorMap q_map, DevBatch d, DevTcPlan
             // The wait at the end must not find o_done two phases back (one parity for both): the last arrive comes
             // after the product before has been seen to retire.
             if (half == 1 && j + 1 == my_units) {
-              ok = wait_bar(&ctrl->o_done[s], (g - 1) & 1u, ctrl, d.status, 237 + s);
+              ok = wait<kD, 0>(&ctrl->o_done[s], (g - 1) & 1u, 237 + s);
               if (!ok) break;
             }
             mbar_arrive(&ctrl->p_full[s][half]);
@@ -688,14 +770,13 @@ attn_fp4_kernel(const __grid_constant__ CUtensorMap q_map, DevBatch d, DevTcPlan
         if (ok) {
           // epilogue: wait for the last PV of this stream, then normalise and store
           o_cnt += 2u * (uint32_t)my_units;
-          ok = wait_bar(&ctrl->o_done[s], (o_cnt - 1) & 1u, ctrl, d.status, 240 + s);
+          ok = wait<kD, 0>(&ctrl->o_done[s], (o_cnt - 1) & 1u, 240 + s);
         }
         // The two streams of a one-M-tile piece hold partial results of the same rows (even and odd tiles).
         // Stream 1 publishes its (m, l); stream 0 reads them and stream 1's accumulator -- the same tensor-memory
         // lanes, so the thread of row r can load both -- and writes one combined result.
-        constexpr float kUnit = (float)(1 << kShift);  // what the accumulator's numbers are worth
         const bool pair = mode == 1 && n >= 2;
-        float m_out = m_used, l_out = l, self = kUnit, other = 0.0f;
+        float m_out = m_used, l_out = l, self = 1.0f, other = 0.0f;
         bool writer = true, other_live = false;
         if (ok && pair) {
           if (s == 1) {
@@ -704,31 +785,36 @@ attn_fp4_kernel(const __grid_constant__ CUtensorMap q_map, DevBatch d, DevTcPlan
             mbar_arrive(&ctrl->xch);
             writer = false;
           } else {
-            ok = wait_bar(&ctrl->xch, x_cnt & 1u, ctrl, d.status, 242);
+            ok = wait<kD, 0>(&ctrl->xch, x_cnt & 1u, 242);
             if (ok) {
               tc_fence_after();
               const float2 o = ctrl->ml_xch[r];
               other_live = o.y != 0.f;  // a stream that saw no key of the row has a sum of 0
               m_out = fmaxf(m_used, o.x);
               const float w_self = l != 0.f ? ex2(m_used - m_out) : 0.f, w_other = other_live ? ex2(o.x - m_out) : 0.f;
-              self = kUnit * w_self;
-              other = kUnit * w_other;
+              self = w_self;
+              other = w_other;
               l_out = w_self * l + w_other * o.y;
             }
           }
         }
         if (pair) ++x_cnt;
         if (ok && writer && !idle) {
+          // rows to be gone through again: those of a piece with scales beyond halves, and of queries that are
+          const int slot = pi.slot[pair ? 0 : s];
+          const bool odd_piece = *reinterpret_cast<volatile int32_t *>(&ctrl->odd_piece[pc & 3]) == pc + 1;
+          uint32_t again = __ballot_sync(0xFFFFFFFFu, ri.q_index >= 0 && (odd_piece || ctrl->q_unit[mode == 2 ? s : 0][r] < 0.f));
           tc_fence_after();
-          store_rows<kD>(o_addr, lane_base + 256 + (1 - s) * 128, pi.slot[pair ? 0 : s], self, other, other_live, m_out, l_out, r, ri.q_index, out, lse,
-                         tc.partial_o, tc.partial_ml);
+          store_rows<kD>(o_addr, lane_base + 256 + (1 - s) * 128, slot, self, other, other_live, m_out, l_out, r, (again >> lane) & 1u ? -1 : ri.q_index, in.out, in.lse,
+                         in.partial_o, in.partial_ml);
           tc_fence_before();
+          for (; again != 0u; again &= again - 1u) exact_row<kD>(ctrl->call, pc, s, quarter * 32 + __ffs(again) - 1, &ctrl->alive_ns);
         }
       }
       // One arrival per thread and piece.  A stream with units in this piece cannot get here before the previous
       // piece's phase is complete (its PV products were issued behind a wait for it); a stream with none must look
       // itself, or its arrival would be counted into the previous phase while the other stream is still storing.
-      if (my_units == 0 && pc > piece0 && ok) ok = wait_bar(&ctrl->epi_done, (uint32_t)(pc - piece0 - 1) & 1u, ctrl, d.status, 243);
+      if (my_units == 0 && pc > piece0 && ok) ok = wait<kD, 0>(&ctrl->epi_done, (uint32_t)(pc - piece0 - 1) & 1u, 243);
       mbar_arrive(&ctrl->epi_done);
     }
   }
@@ -779,10 +865,9 @@ int encode_q(lr_ctx *ctx, const void *q, int64_t n, CUtensorMap *map) {
 }
 
 template <int kD>
-int launch(lr_plan *p, const CUtensorMap &q_map, const Fp4Pools &in, uint16_t *out, float *lse, float scale_log2, cudaStream_t s) {
+int launch(lr_plan *p, const CUtensorMap &q_map, const Fp4Call &in, cudaStream_t s) {
   p->ctx->launches++;
-  return cuda_fail(launch_dependent(attn_fp4_kernel<kD>, dim3((unsigned)p->tc.n_cta), dim3(kThreads), Shape<kD>::kSmemBytes, s, q_map, p->dev, p->tc, in, out, lse,
-                                    scale_log2 * (float)(1 << kShift)),
+  return cuda_fail(launch_dependent(attn_fp4_kernel<kD>, dim3((unsigned)p->tc.n_cta), dim3(kThreads), Shape<kD>::kSmemBytes, s, q_map, p->dev, p->tc, in),
                    "attn_fp4_kernel launch");
 }
 
@@ -805,17 +890,18 @@ int init_attn_fp4_kernel() {
 }
 
 int launch_attn_fp4(lr_plan *p, const void *q, const lr_fp4_cache &c, void *out, float *lse, float scale, cudaStream_t s) {
-  const float scale_log2 = scale * 1.4426950408889634f;
-  auto *o = reinterpret_cast<uint16_t *>(out);
+  const DevTcPlan &tc = p->tc;
+  const Fp4Call in = {reinterpret_cast<const uint16_t *>(q), reinterpret_cast<const uint8_t *>(c.k_d), reinterpret_cast<const uint8_t *>(c.v_d), c.k_scale_d, c.v_scale_d,
+                      reinterpret_cast<uint16_t *>(out), lse, tc.partial_o, tc.partial_ml, tc.pages, tc.rows, tc.pieces, tc.reqs, p->dev.n_pool_pages, p->dev.status,
+                      p->dev.n_q_heads, p->dev.n_kv_heads, p->dev.group, tc.tokens_per_mtile, scale * 1.4426950408889634f};
   if (p->tc_most_rows <= kFp4FewRows) {
-    if (int rc = launch_attn_fp4_few(p, q, c, out, lse, scale_log2, s)) return rc;
+    if (int rc = launch_attn_fp4_few(p, in, s)) return rc;
   } else {
     alignas(64) CUtensorMap q_map;
     if (int rc = encode_q(p->ctx, q, p->dev.n_q_rows, &q_map)) return rc;
-    const Fp4Pools in = {reinterpret_cast<const uint8_t *>(c.k_d), reinterpret_cast<const uint8_t *>(c.v_d), c.k_scale_d, c.v_scale_d};
-    if (int rc = (p->dev.head_dim == 128 ? launch<128> : launch<64>)(p, q_map, in, o, lse, scale_log2, s)) return rc;
+    if (int rc = (p->dev.head_dim == 128 ? launch<128> : launch<64>)(p, q_map, in, s)) return rc;
   }
-  return (p->dev.head_dim == 128 ? launch_merge<128> : launch_merge<64>)(p, o, lse, s);
+  return (p->dev.head_dim == 128 ? launch_merge<128> : launch_merge<64>)(p, in.out, lse, s);
 }
 
 }  // namespace lr

@@ -6,27 +6,24 @@
 //
 //   S^T = K Q^T    16 keys x 8 queries.  A lane of quarter t = lane % 4 has of keys lane / 4 and lane / 4 + 8 the t-th quarter of the channels, one load each (which channels a
 //                  step of the product takes is free, as long as Q's are the same), of one group of 32 or half of one: a key's factor is one number a lane.
-//   O^T += V^T P^T 16 channels x 8 queries over 16 keys.  A lane has of keys 2t, 2t + 1 and the two 8 behind them an eighth of the channels.  The halves of a word of
-//                  codes are its even and its odd channels, so one byte permutation pairs two keys' and fp4_place leaves neighbouring keys of a channel side by side, as the
-//                  product wants them.  P^T comes out of S^T by movmatrix.
+//   O^T += V^T P^T 16 channels x 8 queries over 16 keys.  A lane has of keys 2t, 2t + 1 and the two 8 behind them an eighth of the channels; with the codes of two keys in the
+//                  halves of a byte, neighbouring keys of a channel come out side by side, as the product wants them.  P^T comes out of S^T by movmatrix.
 //
-// Numbers are those of attn_fp4.cu: codes times a scale are bf16 numbers, 2^-kShift of what they are; weights are bf16, and the row sums are those of the rounded weights,
-// so that their rounding takes a weight's error out again where one key has most of it.  A row's reference exponent is raised when a score is more than
-// 2^kRescale above it; the lanes that see it so ask the others for the maximum then.  A row of K that stands for NaN, or a row of V, makes the score of its key no number.
+// Numbers are those of attn_fp4.cu.  A row's reference exponent is set again when a score is more than 2^kRescale above it; the lanes that see it so ask the others for the
+// maximum then.
 //
-// What bounds it is turning codes into operands: five instructions for a pair of them, some 400 for a page of K and V, 16 of which are products.
+// What bounds it is turning codes into operands: nine instructions for a word of eight, some 300 for a page of K and V, 16 of which are products.  As bf16 it took 17
+// for a word: 48 single tokens over 9 K keys each 158 us.
 #include <algorithm>
 
-#include "attn_mma.cuh"
-#include "fp4_cache.cuh"
+#include "attn_fp4.cuh"
 
 namespace lr {
 
 namespace {
 
-constexpr int kShift = 16;                  // numbers are 2^-kShift of what they are (attn_fp4.cu)
-constexpr uint32_t kMostScale = 128 + kShift;
-constexpr float kRescale = 8.0f;            // log2 units
+constexpr float kLift = 4.0f;               // log2 units: a row's reference is set this much below its maximum so far,
+constexpr float kRescale = 14.0f;           // ... and set again once a score is this much above it: halves end at 2^16
 constexpr float kNoKey = -3.0e38f;          // a row's reference before its first key: everything is above it, and a score of -infinity less it is no NaN
 constexpr int kHeld = 32;                   // pieces whose records a CTA keeps in shared memory
 
@@ -42,29 +39,15 @@ struct Shape {
   static constexpr int kSmemBytes = kSumBytes + kWarps * kStages * kPageBytes;
 };
 
-struct Few {  // the pools
-  const uint16_t *q;
-  const uint8_t *k, *v, *k_scale, *v_scale;
-};
-
 __device__ __forceinline__ void mma16816(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
-  asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+  asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
       : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
       : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
-__device__ __forceinline__ uint32_t transpose8(uint32_t x) {  // of 8 x 8 bf16 numbers, two a lane
+__device__ __forceinline__ uint32_t transpose8(uint32_t x) {  // of 8 x 8 halves, two a lane
   uint32_t y;
   asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
   return y;
-}
-__device__ __forceinline__ int2 ld_pair(const void *p) {
-  int2 v;
-  asm volatile("ld.global.nc.v2.s32 {%0, %1}, [%2];" : "=r"(v.x), "=r"(v.y) : "l"(p));
-  return v;
-}
-// past L1, as everything that reads the cache (fp8_cache.cuh)
-__device__ __forceinline__ void copy16(uint32_t dst, const uint8_t *src) {
-  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
 }
 template <int kWords>
 __device__ __forceinline__ void ld_codes(uint32_t (&w)[kWords], uint32_t p) {
@@ -84,21 +67,16 @@ __device__ __forceinline__ uint32_t v_unit(int key, int c) {
   const int row = (key & 8) | ((key >> 1) & 3) | ((key & 1) << 2);
   return (uint32_t)(row * (kD / 2) + (kD == 128 ? c ^ (((key >> 2) & 1) << 1) : c) * 16);
 }
-// 2^(byte - 1 - kShift) as bf16
-__device__ __forceinline__ uint32_t factor(uint32_t byte) { return (byte + (126 - kShift)) << 7; }
-// ... as far as bf16 goes, and what is left of it
-__device__ __forceinline__ uint32_t most_of(uint32_t byte) { return factor(min(byte, kMostScale)); }
-__device__ __forceinline__ uint32_t rest_of(uint32_t byte) { return (byte > kMostScale && byte != kFp4NanScale ? byte - kMostScale + 127u : 127u) << 7; }
-
 template <int kD, int kNB>
 __global__ void __launch_bounds__(Shape<kD, kNB>::kThreads, 1)
-attn_fp4_few_kernel(DevBatch d, DevTcPlan tc, Few in, uint16_t *__restrict__ out, float *__restrict__ lse, float scale_log2) {
+attn_fp4_few_kernel(DevBatch d, DevTcPlan tc, const __grid_constant__ Fp4Call in) {
   using Sh = Shape<kD, kNB>;
   constexpr int kWarps = Sh::kWarps, kThreads = Sh::kThreads, kRows = Sh::kRows, kStride = Sh::kStride, kKWords = kD / 32, kVWords = kD / 64, kMTiles = kD / 16;
   extern __shared__ __align__(16) float s_sum[];  // [warp][query][kStride], then the warps' stages
   __shared__ float2 s_ml[kWarps][kRows];
   __shared__ TcPiece s_piece[kHeld];
   __shared__ TcReq s_req[kHeld];
+  __shared__ int s_odd;  // 1 + the last piece that has a scale beyond halves
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, t = lane & 3, g = lane >> 2;
   // the plan is uploaded by copies, so it may be read in front of the wait for the kernel before
   const int piece0 = tc.heads[blockIdx.x].piece0, piece1 = tc.heads[blockIdx.x].piece1;
@@ -107,6 +85,7 @@ attn_fp4_few_kernel(DevBatch d, DevTcPlan tc, Few in, uint16_t *__restrict__ out
     s_piece[threadIdx.x] = pi;
     s_req[threadIdx.x] = tc.reqs[pi.req];
   }
+  if (threadIdx.x == 0) s_odd = 0;
   __syncthreads();
   asm volatile("griddepcontrol.wait;" ::: "memory");  // queries and cache may come from the kernel launched just before
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
@@ -183,22 +162,45 @@ attn_fp4_few_kernel(DevBatch d, DevTcPlan tc, Few in, uint16_t *__restrict__ out
     const TcPiece pi = piece_of(pc);
     const TcReq rq = req_of(pc, pi);
     const int rows = min(rq.n_q * G, kRows), n_pages = min(pi.tile_end * kPagesPerTile, rq.n_pages) - pi.tile_begin * kPagesPerTile;
-    uint32_t qf[kNB][kD / 8];
+    uint32_t qf[kNB][kD / 8], again = 0;  // again: rows with a channel too small beside their largest to be a half
+    float sc[kNB][2];
     int depth[kNB][2], branch[kNB][2], limit[kNB][2];  // of this lane's columns, queries 2t and 2t + 1
 #pragma unroll
     for (int b = 0; b < kNB; ++b) {
       const int r = b * 8 + g;  // this lane's query of the operand
+      uint4 x[kD / 32];
+      uint32_t top = 0;
 #pragma unroll
       for (int i = 0; i < kD / 32; ++i) {
-        uint4 x = make_uint4(0, 0, 0, 0);
+        x[i] = make_uint4(0, 0, 0, 0);
         if (r < rows)
-          x = __ldcg(reinterpret_cast<const uint4 *>(in.q + ((int64_t)(rq.q_row0 + r / G) * d.n_q_heads + pi.kv_head * G + r % G) * kD + t * (kD / 4)) + i);
-        qf[b][4 * i] = x.x, qf[b][4 * i + 1] = x.y, qf[b][4 * i + 2] = x.z, qf[b][4 * i + 3] = x.w;
+          x[i] = __ldcg(reinterpret_cast<const uint4 *>(in.q + ((int64_t)(rq.q_row0 + r / G) * d.n_q_heads + pi.kv_head * G + r % G) * kD + t * (kD / 4)) + i);
+        const uint32_t m = 0x7FFF7FFFu, two = __vmaxu2(__vmaxu2(x[i].x & m, x[i].y & m), __vmaxu2(x[i].z & m, x[i].w & m));
+        top = max(top, max(two & 0xFFFFu, two >> 16));
       }
 #pragma unroll
-      for (int e = 0; e < 2; ++e) {
-        const RowInfo ri = row_info(d, tc, rq, tc.tokens_per_mtile, pi.mtile0, b * 8 + 2 * t + e, pi.kv_head);
-        depth[b][e] = ri.depth, branch[b][e] = ri.branch, limit[b][e] = ri.limit;
+      for (int y = 1; y < 4; y <<= 1) top = max(top, __shfl_xor_sync(0xFFFFFFFFu, top, y));
+      const int e = min(half_exponent(top), (int)kQMostExponent);
+      const float by = __uint_as_float((uint32_t)(127 + e) << 23);
+      bool odd = false;
+#pragma unroll
+      for (int i = 0; i < kD / 32; ++i) {
+        const uint4 p = as_halves8(x[i]);
+        const uint32_t w[4] = {p.x, p.y, p.z, p.w};
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const float lo = bits_f(w[j] << 16) * by, hi = bits_f(w[j] & 0xFFFF0000u) * by;
+          odd = odd || (lo != 0.f && fabsf(lo) < 0x1p-17f) || (hi != 0.f && fabsf(hi) < 0x1p-17f);
+          qf[b][4 * i + j] = pack_f16(lo, hi);
+        }
+      }
+      again |= __reduce_or_sync(0xFFFFFFFFu, odd && top < 0x7F80u ? 1u << r : 0u);
+      const float unit = in.scale_log2 * (top < 0x7F80u ? __uint_as_float((uint32_t)(127 - e) << 23) : __uint_as_float(0x7FC00000u));
+#pragma unroll
+      for (int y = 0; y < 2; ++y) {
+        sc[b][y] = __shfl_sync(0xFFFFFFFFu, unit, (2 * t + y) * 4);
+        const RowInfo ri = row_info(d, tc, rq, tc.tokens_per_mtile, pi.mtile0, b * 8 + 2 * t + y, pi.kv_head);
+        depth[b][y] = ri.depth, branch[b][y] = ri.branch, limit[b][y] = ri.limit;
       }
     }
     float o[kNB][kMTiles][4], ref[kNB][2], l[kNB][2];
@@ -228,51 +230,29 @@ attn_fp4_few_kernel(DevBatch d, DevTcPlan tc, Few in, uint16_t *__restrict__ out
       ld_codes(what, scales + 2 * Sh::kScaleBytes);
       const uint32_t meta = what[0];
       const bool masked = what[1] != 0u;
-      // scales beyond one factor and rows that stand for NaN: rare
-      const bool rare = __any_sync(0xFFFFFFFFu, max(max(max(kb[0], kb[1]), max(vb[0], vb[1])), max(vb[2], vb[3])) > kMostScale);
+      const int valid = (int)(meta & 31u);
+      if (__any_sync(0xFFFFFFFFu, max(max(max(kb[0], kb[1]), max(vb[0], vb[1])), max(vb[2], vb[3])) > kMostHalf ||
+                                      min(min(min(kb[0], kb[1]), min(vb[0], vb[1])), min(vb[2], vb[3])) < kLeastHalf)) {  // (among it what a slot of no valid token holds)
+        bool odd = false;
+#pragma unroll
+        for (int j = 0; j < 2; ++j) odd = odd || (odd_scale(kb[j]) && g + 8 * j < valid);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) odd = odd || (odd_scale(vb[j]) && 2 * t + (j >> 1) * 8 + (j & 1) < valid);
+        if (odd) *reinterpret_cast<volatile int *>(&s_odd) = pc + 1;
+      }
       float s[kNB][4];
 #pragma unroll
       for (int b = 0; b < kNB; ++b) s[b][0] = s[b][1] = s[b][2] = s[b][3] = 0.f;
-      uint32_t f[2] = {twice(factor(kb[0])), twice(factor(kb[1]))}, more[2] = {0, 0};
-      if (rare) {
-#pragma unroll
-        for (int j = 0; j < 2; ++j) f[j] = twice(kb[j] == kFp4NanScale ? 0x7FFFu : most_of(kb[j])), more[j] = twice(rest_of(kb[j]));
-      }
+      uint32_t f[2] = {half_factor(kb[0]), half_factor(kb[1])};
 #pragma unroll
       for (int w = 0; w < kKWords; ++w) {
         uint32_t a[2][4];
 #pragma unroll
-        for (int j = 0; j < 2; ++j) {
-          a[j][0] = mul_bf16x2(fp4_place<0>(k[j][w]), f[j]);
-          a[j][1] = mul_bf16x2(fp4_place<1>(k[j][w]), f[j]);
-          a[j][2] = mul_bf16x2(fp4_place<2>(k[j][w]), f[j]);
-          a[j][3] = mul_bf16x2(fp4_place<3>(k[j][w]), f[j]);
-        }
-        if (rare) {
-#pragma unroll
-          for (int x = 0; x < 4; ++x) a[0][x] = mul_bf16x2(a[0][x], more[0]), a[1][x] = mul_bf16x2(a[1][x], more[1]);
-        }
+        for (int j = 0; j < 2; ++j) halves8(a[j], k[j][w], f[j]);
 #pragma unroll
         for (int b = 0; b < kNB; ++b) {
           mma16816(s[b], a[0][0], a[1][0], a[0][1], a[1][1], qf[b][4 * w], qf[b][4 * w + 1]);
           mma16816(s[b], a[0][2], a[1][2], a[0][3], a[1][3], qf[b][4 * w + 2], qf[b][4 * w + 3]);
-        }
-      }
-      const int valid = (int)(meta & 31u);
-      if (rare) {
-        // keys g and g + 8: whether a group of their rows of V stands for NaN, from the lanes that have those (key 2t + e of quarter t, channels of group of lane / 4)
-#pragma unroll
-        for (int j = 0; j < 2; ++j) {
-          bool bad = false;
-#pragma unroll 1
-          for (int x = 0; x < 8; ++x) {
-            const uint32_t even = __shfl_sync(0xFFFFFFFFu, vb[2 * j], x * 4 + (g >> 1)), odd = __shfl_sync(0xFFFFFFFFu, vb[2 * j + 1], x * 4 + (g >> 1));
-            bad = bad || ((g & 1) != 0 ? odd : even) == kFp4NanScale;
-          }
-          if (bad) {
-#pragma unroll
-            for (int b = 0; b < kNB; ++b) s[b][2 * j] = s[b][2 * j + 1] = __uint_as_float(0x7FC00000u);
-          }
         }
       }
       uint32_t pt[kNB][2];
@@ -290,27 +270,29 @@ attn_fp4_few_kernel(DevBatch d, DevTcPlan tc, Few in, uint16_t *__restrict__ out
         }
         float x[4];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) x[i] = fmaf(s[b][i], scale_log2, -ref[b][i & 1]);
+        for (int i = 0; i < 4; ++i) x[i] = fmaf(s[b][i], sc[b][i & 1], -ref[b][i & 1]);
         if (__any_sync(0xFFFFFFFFu, fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])) > kRescale)) {
 #pragma unroll
           for (int e = 0; e < 2; ++e) {
-            float top = fmaxf(s[b][e], s[b][2 + e]) * scale_log2;
+            float top = fmaxf(s[b][e], s[b][2 + e]) * sc[b][e];
 #pragma unroll
             for (int y = 4; y < 32; y <<= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, y));
             if (top > ref[b][e] + kRescale) {
-              const float down = ex2(ref[b][e] - top);
-              ref[b][e] = top;
+              const float down = ex2(ref[b][e] - (top - kLift));
+              ref[b][e] = top - kLift;
               l[b][e] *= down;
 #pragma unroll
               for (int m = 0; m < kMTiles; ++m) o[b][m][e] *= down, o[b][m][2 + e] *= down;
             }
-            x[e] = fmaf(s[b][e], scale_log2, -ref[b][e]);
-            x[2 + e] = fmaf(s[b][2 + e], scale_log2, -ref[b][e]);
+            x[e] = fmaf(s[b][e], sc[b][e], -ref[b][e]);
+            x[2 + e] = fmaf(s[b][2 + e], sc[b][e], -ref[b][e]);
           }
         }
-        const uint32_t p0 = pack_bf16(ex2(x[0]), ex2(x[1])), p1 = pack_bf16(ex2(x[2]), ex2(x[3]));
-        l[b][0] += bits_f(p0 << 16) + bits_f(p1 << 16);
-        l[b][1] += bits_f(p0 & 0xFFFF0000u) + bits_f(p1 & 0xFFFF0000u);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) x[i] = ex2(x[i]);
+        l[b][0] += x[0] + x[2];
+        l[b][1] += x[1] + x[3];
+        const uint32_t p0 = pack_f16(x[0], x[1]), p1 = pack_f16(x[2], x[3]);
         pt[b][0] = transpose8(p0);
         pt[b][1] = transpose8(p1);
       }
@@ -318,40 +300,25 @@ attn_fp4_few_kernel(DevBatch d, DevTcPlan tc, Few in, uint16_t *__restrict__ out
 #pragma unroll
       for (int j = 0; j < 4; ++j) ld_codes(v[j], at + Sh::kCodeBytes + v_unit<kD>(2 * t + (j >> 1) * 8 + (j & 1), g * (kD / 16) / 16) + g * (kD / 16) % 16);
 #pragma unroll
-      for (int j = 0; j < 2; ++j) f[j] = factor(vb[2 * j]) | factor(vb[2 * j + 1]) << 16;
-      if (rare) {
-#pragma unroll
-        for (int j = 0; j < 2; ++j) {
-          f[j] = (vb[2 * j] == kFp4NanScale ? 0u : most_of(vb[2 * j])) | (vb[2 * j + 1] == kFp4NanScale ? 0u : most_of(vb[2 * j + 1])) << 16;
-          more[j] = rest_of(vb[2 * j]) | rest_of(vb[2 * j + 1]) << 16;
-        }
-      }
+      for (int j = 0; j < 2; ++j) f[j] = half_factors(vb[2 * j], vb[2 * j + 1]);
       if (masked) {  // slots of no valid token
 #pragma unroll
         for (int j = 0; j < 2; ++j) f[j] &= (2 * t + 8 * j < valid ? 0xFFFFu : 0u) | (2 * t + 8 * j + 1 < valid ? 0xFFFF0000u : 0u);
       }
 #pragma unroll
       for (int w = 0; w < kVWords; ++w) {
-        const uint32_t z[4] = {__byte_perm(v[0][w], v[1][w], 0x5410), __byte_perm(v[0][w], v[1][w], 0x7632), __byte_perm(v[2][w], v[3][w], 0x5410),
-                               __byte_perm(v[2][w], v[3][w], 0x7632)};
-        uint32_t a[4][4];
+        uint32_t a[2][2][4];  // [which two keys][channels 0, 4, 1, 5 or 2, 6, 3, 7]
 #pragma unroll
-        for (int x = 0; x < 4; ++x) {
-          a[0][x] = mul_bf16x2(fp4_place<0>(z[x]), f[x >> 1]);
-          a[1][x] = mul_bf16x2(fp4_place<1>(z[x]), f[x >> 1]);
-          a[2][x] = mul_bf16x2(fp4_place<2>(z[x]), f[x >> 1]);
-          a[3][x] = mul_bf16x2(fp4_place<3>(z[x]), f[x >> 1]);
-        }
-        if (rare) {
-#pragma unroll
-          for (int x = 0; x < 4; ++x)
-#pragma unroll
-            for (int y = 0; y < 4; ++y) a[y][x] = mul_bf16x2(a[y][x], more[x >> 1]);
+        for (int j = 0; j < 2; ++j) {
+          const uint32_t x = v[2 * j][w], y = v[2 * j + 1][w], m = 0x0F0F0F0Fu;
+          halves8(a[j][0], (x & m) | ((y << 4) & ~m), f[j]);
+          halves8(a[j][1], ((x >> 4) & m) | (y & ~m), f[j]);
         }
 #pragma unroll
-        for (int y = 0; y < 4; ++y)
+        for (int y = 0; y < 4; ++y)  // channels 2y and 2y + 1
 #pragma unroll
-          for (int b = 0; b < kNB; ++b) mma16816(o[b][4 * w + y], a[y][0], a[y][1], a[y][2], a[y][3], pt[b][0], pt[b][1]);
+          for (int b = 0; b < kNB; ++b)
+            mma16816(o[b][4 * w + y], a[0][y & 1][y >> 1], a[0][y & 1][2 + (y >> 1)], a[1][y & 1][y >> 1], a[1][y & 1][2 + (y >> 1)], pt[b][0], pt[b][1]);
       }
     }
     // the warps' sums, joined
@@ -370,8 +337,10 @@ attn_fp4_few_kernel(DevBatch d, DevTcPlan tc, Few in, uint16_t *__restrict__ out
     }
     __syncthreads();
     const int slot = pi.slot[0];
+    if (s_odd == pc + 1) again = (1u << kRows) - 1u;
     for (int i = threadIdx.x; i < rows * (kD / 2); i += kThreads) {  // a pair of channels: 2m and 2m + 1 of eighth x
       const int r = i / (kD / 2), c = i % (kD / 2), ch = (c % 8) * (kD / 8) + 2 * (c / 8);
+      if ((again >> r) & 1u) continue;
       float top = -INFINITY, sum = 0.f;
       float2 acc = make_float2(0.f, 0.f);
 #pragma unroll
@@ -387,27 +356,27 @@ attn_fp4_few_kernel(DevBatch d, DevTcPlan tc, Few in, uint16_t *__restrict__ out
           acc.y = fmaf(by, x.y, acc.y);
         }
       }
-      constexpr float kUnit = (float)(1 << kShift);
       const int64_t q_index = (int64_t)(rq.q_row0 + r / G) * d.n_q_heads + pi.kv_head * G + r % G;
       if (slot < 0) {
-        const float inv = kUnit / sum;
-        *reinterpret_cast<uint32_t *>(out + q_index * kD + ch) = pack_bf16(acc.x * inv, acc.y * inv);
-        if (c == 0 && lse != nullptr) lse[q_index] = (top + log2f(sum)) * 0.6931471805599453f;
+        const float inv = 1.0f / sum;
+        *reinterpret_cast<uint32_t *>(in.out + q_index * kD + ch) = pack_bf16(acc.x * inv, acc.y * inv);
+        if (c == 0 && in.lse != nullptr) in.lse[q_index] = (top + log2f(sum)) * 0.6931471805599453f;
       } else {
-        *reinterpret_cast<float2 *>(tc.partial_o + (((int64_t)slot * (kD / 4) + ch / 4) * 128 + r) * 4 + ch % 4) = make_float2(acc.x * kUnit, acc.y * kUnit);
+        *reinterpret_cast<float2 *>(in.partial_o + (((int64_t)slot * (kD / 4) + ch / 4) * 128 + r) * 4 + ch % 4) = acc;
         // a sum that is not a number must not look like that of a row that saw nothing: the merge asks whether the sum is above 0
-        if (c == 0) *reinterpret_cast<float2 *>(tc.partial_ml + ((int64_t)slot * 128 + r) * 2) = sum != sum ? make_float2(sum, 1.0f) : make_float2(top, sum);
+        if (c == 0) *reinterpret_cast<float2 *>(in.partial_ml + ((int64_t)slot * 128 + r) * 2) = sum != sum ? make_float2(sum, 1.0f) : make_float2(top, sum);
       }
     }
+    for (int r = warp; r < rows; r += kWarps)
+      if ((again >> r) & 1u) exact_row<kD>(in, pc, 0, r, nullptr);
     __syncthreads();  // the sums have been read
   }
 }
 
 template <int kD, int kNB>
-int launch(lr_plan *p, const Few &in, uint16_t *out, float *lse, float scale_log2, cudaStream_t s) {
+int launch(lr_plan *p, const Fp4Call &in, cudaStream_t s) {
   p->ctx->launches++;
-  return cuda_fail(launch_dependent(attn_fp4_few_kernel<kD, kNB>, dim3((unsigned)p->tc.n_cta), dim3(Shape<kD, kNB>::kThreads), Shape<kD, kNB>::kSmemBytes, s, p->dev, p->tc, in, out, lse,
-                                    scale_log2 * (float)(1 << kShift)),
+  return cuda_fail(launch_dependent(attn_fp4_few_kernel<kD, kNB>, dim3((unsigned)p->tc.n_cta), dim3(Shape<kD, kNB>::kThreads), Shape<kD, kNB>::kSmemBytes, s, p->dev, p->tc, in),
                    "attn_fp4_few_kernel launch");
 }
 
@@ -426,11 +395,9 @@ int init_attn_fp4_few_kernel() {
   return cuda_fail(e, "attn_fp4_few_kernel shared-memory attribute");
 }
 
-int launch_attn_fp4_few(lr_plan *p, const void *q, const lr_fp4_cache &c, void *out, float *lse, float scale_log2, cudaStream_t s) {
-  const Few in = {reinterpret_cast<const uint16_t *>(q), reinterpret_cast<const uint8_t *>(c.k_d), reinterpret_cast<const uint8_t *>(c.v_d), c.k_scale_d, c.v_scale_d};
-  auto *o = reinterpret_cast<uint16_t *>(out);
-  if (p->dev.head_dim == 128) return p->tc_most_rows <= 8 ? launch<128, 1>(p, in, o, lse, scale_log2, s) : launch<128, 2>(p, in, o, lse, scale_log2, s);
-  return p->tc_most_rows <= 8 ? launch<64, 1>(p, in, o, lse, scale_log2, s) : launch<64, 2>(p, in, o, lse, scale_log2, s);
+int launch_attn_fp4_few(lr_plan *p, const Fp4Call &in, cudaStream_t s) {
+  if (p->dev.head_dim == 128) return p->tc_most_rows <= 8 ? launch<128, 1>(p, in, s) : launch<128, 2>(p, in, s);
+  return p->tc_most_rows <= 8 ? launch<64, 1>(p, in, s) : launch<64, 2>(p, in, s);
 }
 
 }  // namespace lr

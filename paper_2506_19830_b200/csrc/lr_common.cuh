@@ -402,9 +402,6 @@ int launch_compact_fp8(lr_plan *p, const int32_t *keep_off, const int32_t *keep_
 int launch_fp4_move(lr_ctx *ctx, const lr_fp4_cache &c, bool write, void *k, int64_t k_stride, void *v, int64_t v_stride, const int64_t *slots,
                     int32_t n_tokens, int32_t *status, cudaStream_t s);
 int launch_attn_fp4(lr_plan *p, const void *q, const lr_fp4_cache &c, void *out, float *lse, float scale, cudaStream_t s);
-// of a plan whose tc_most_rows is kFp4FewRows at most; without the merge
-constexpr int kFp4FewRows = 16;
-int launch_attn_fp4_few(lr_plan *p, const void *q, const lr_fp4_cache &c, void *out, float *lse, float scale_log2, cudaStream_t s);
 int launch_attn_fp4_generic(lr_plan *p, const void *q, const lr_fp4_cache &c, void *out, float *lse, float scale, cudaStream_t s);
 int launch_compact_fp4(lr_plan *p, const int32_t *keep_off, const int32_t *keep_pages, const int32_t *keep_valid, const lr_fp4_cache &c,
                        int32_t *new_len, int32_t *n_pages_kept, cudaStream_t s);
