@@ -6,7 +6,7 @@
 // Numbers.  Q, K, V and the weights are halves (attn_fp4.cuh): a code and its scale are one exactly, two instructions for a pair of codes, where bf16 takes twice as many and the
 // converters, one warp to a scheduler, are what a tile waits for.  A row of Q is scaled by a power of two, which the softmax takes out again; eight channels of K
 // and Q lie in the order in which the bytes of a word give them, those of O are put right as they are stored.  Weights lie 2^kLift above what they are when the row's
-// reference is set, and may rise to 2^15: off by 2^-12 of themselves, or by 2^-25 where they are below 2^-14, 2^-29 of the weight that set it.  Rows that this
+// reference is set, and may rise to 2^15: off by 2^-12 of themselves, or by 2^-25 where they are below 2^-14, 2^-27 of the weight that set it.  Rows that this
 // does not serve are worked out once more when their piece is done (exact_row).  Slots that hold no valid token become zeros, whatever they held.
 //
 // One CTA = 16 warps in four warpgroups, registers moved with setmaxnreg (184 x 256 + 72 x 256 = 128 x 512):
@@ -50,9 +50,8 @@ struct Shape {
   static constexpr int kSmemBytes = 2 * kTileBytes + kStages * kTileBytes + kRawBytes + 4096;  // tiles, codes, Ctrl; the base must be 1024-aligned
 };
 constexpr int kMaxRaw = 6;
-constexpr float kLift = 4.0f;              // log2 units: a row's reference is set this much below its maximum so far,
-constexpr float kRescaleThreshold = 10.0f; // ... is set again once that is this much above it,
-constexpr float kRedoThreshold = 15.0f;    // ... and a tile beyond this is done again at once: halves end at 2^16
+constexpr float kLift = 2.0f;   // log2 units: a row's reference is set this much below its maximum so far; the more, the smaller the weights that are more than 0,
+constexpr float kGrow = 15.0f;  // ... and keys beyond this are done again with another one: halves end at 2^16
 
 struct __align__(16) Ctrl {
   TcCtaHead head;         // this CTA's record
@@ -674,8 +673,8 @@ attn_fp4_kernel(const __grid_constant__ CUtensorMap q_map, DevBatch d, DevTcPlan
         }
       }
       if (ok && my_units > 0) {
-        float m_used = -INFINITY, l = 0.f, m_new = 0.f;
-        bool pend = false, s_ready = false;
+        float m_used = -INFINITY, l = 0.f;
+        bool s_ready = false;
         // A warp whose 32 rows are all padding only keeps the barriers' counts: what it leaves as weights multiplies into rows
         // of O that nobody reads.
         const bool idle = __all_sync(0xFFFFFFFFu, ri.q_index < 0);
@@ -700,17 +699,6 @@ attn_fp4_kernel(const __grid_constant__ CUtensorMap q_map, DevBatch d, DevTcPlan
               ok = wait<kD, 0>(&ctrl->s_full[s][half], s_cnt & 1u, 230 + s);
               if (!ok) break;
             }
-            // A growth of the maximum noticed in an earlier half-unit is applied now.
-            if (__any_sync(0xFFFFFFFFu, pend)) {
-              const float alpha = pend ? ex2(m_used - m_new) : 1.0f;
-              if (pend) {
-                l *= alpha;
-                m_used = m_new;
-                pend = false;
-              }
-              ok = rescale_rows<kD>(o_addr, alpha, &ctrl->o_done[s], g, 235 + s);
-              if (!ok) break;
-            }
             tc_fence_after();
             uint32_t v[64];
             tmem_ld64(sh_addr, v);
@@ -730,14 +718,13 @@ attn_fp4_kernel(const __grid_constant__ CUtensorMap q_map, DevBatch d, DevTcPlan
             if (fast) {
               sum = exp_half<true>(v, sh_addr, sc_row, -m_used, raw);
               mx = raw * sc_row;
-              if (__any_sync(0xFFFFFFFFu, mx > m_used + kRedoThreshold)) fast = false;  // could overflow: redo exactly
+              if (__any_sync(0xFFFFFFFFu, mx > m_used + kGrow)) fast = false;
             } else {
               mx = max_half(v) * sc_row;
             }
             if (!fast) {
-              // Exact path (first half-unit of a stream, rows that have seen no key yet, a jump of the
-              // scores): adopt the maximum before the exponentials.
-              const bool grow = mx > m_used + kRescaleThreshold;
+              // the first half-unit of a stream, rows that have seen no key yet, scores that rise beyond halves: the maximum first
+              const bool grow = mx > m_used + kGrow;
               const float alpha = grow ? ex2(m_used - (mx - kLift)) : 1.0f;
               if (grow) {
                 l *= alpha;
@@ -749,9 +736,6 @@ attn_fp4_kernel(const __grid_constant__ CUtensorMap q_map, DevBatch d, DevTcPlan
                 ok = rescale_rows<kD>(o_addr, alpha, &ctrl->o_done[s], g, 235 + s);
                 if (!ok) break;
               }
-            } else if (mx > m_used + kRescaleThreshold) {
-              pend = true;
-              m_new = mx - kLift;
             }
             l += sum;
             tc_wait_st();

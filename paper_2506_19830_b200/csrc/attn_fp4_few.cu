@@ -22,8 +22,8 @@ namespace lr {
 
 namespace {
 
-constexpr float kLift = 4.0f;               // log2 units: a row's reference is set this much below its maximum so far,
-constexpr float kRescale = 14.0f;           // ... and set again once a score is this much above it: halves end at 2^16
+constexpr float kLift = 2.0f;               // log2 units: a row's reference is set this much below its maximum so far,
+constexpr float kRescale = 15.0f;           // ... and set again once a score is this much above it: halves end at 2^16
 constexpr float kNoKey = -3.0e38f;          // a row's reference before its first key: everything is above it, and a score of -infinity less it is no NaN
 constexpr int kHeld = 32;                   // pieces whose records a CTA keeps in shared memory
 

@@ -117,11 +117,11 @@ def run_stored(w, pools, path, **kw):
 def bound(w, k, v, o_ref):
     """What an output may be off by: half a step of bf16, and of the weighted sum of |v| half a step of a weight in bf16, 2^-8, and as much for
     scores in fp32 of a few hundred at most (2^-8 of a weight is 2^-8 / ln 2 in its exponent, 2^-16 of 400).  On the tensor cores weights are halves, multiples of 2^-24 at
-    the least, in a row whose sum is 2^4 or more (its largest weight is when its reference is set, and may rise): a key's part of an output may be off by 2^-29 of its V."""
+    the least, in a row whose sum is 2^2 or more (its largest weight is when its reference is set, and may rise): a key's part of an output may be off by 2^-27 of its V."""
     a, _ = O.verify_attention(w.batch, w.tensors.q, k, v & 0x7FFF)
     at = tokens(w.batch)
     sizes = np.abs(bf16_to_f32(v[at[:, 0], :, at[:, 1]])).astype(np.float64)
-    return 2.0 ** -8 * np.abs(o_ref) + 2.0 ** -7 * a + len(at) * 2.0 ** -29 * sizes[np.isfinite(sizes)].max()
+    return 2.0 ** -8 * np.abs(o_ref) + 2.0 ** -7 * a + len(at) * 2.0 ** -27 * sizes[np.isfinite(sizes)].max()
 
 
 def compare(w, pools, path):
