@@ -250,7 +250,7 @@ class Fp8Cache:
         self._c = lr_fp8_cache(k.data_ptr(), v.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr(), shape[0])
         self.c = C.addressof(self._c)
         self.kv = lr_kv_cache(KV_FP8, *(getattr(self._c, n) for n, _ in lr_fp8_cache._fields_))
-        self.any = C.addressof(self.kv)
+        self.any, self.raw = C.addressof(self.kv), bytes(self.kv)
 
     @staticmethod
     def empty(model, n_pages: int, device="cuda:0") -> "Fp8Cache":
@@ -277,7 +277,7 @@ class Fp4Cache:
         self._c = lr_fp4_cache(k.data_ptr(), v.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr(), shape[0])
         self.c = C.addressof(self._c)
         self.kv = lr_kv_cache(KV_FP4, *(getattr(self._c, n) for n, _ in lr_fp8_cache._fields_))
-        self.any = C.addressof(self.kv)
+        self.any, self.raw = C.addressof(self.kv), bytes(self.kv)
 
     @staticmethod
     def empty(model, n_pages: int, device="cuda:0") -> "Fp4Cache":
@@ -298,7 +298,7 @@ class Bf16Cache:
         self.n_pages, self.heads, self.head_dim, self.device = k.shape[0], k.shape[1], k.shape[3], k.device
         self.kind = (self.heads, self.head_dim, k.device.index)
         self.kv = lr_kv_cache(KV_BF16, k.data_ptr(), v.data_ptr(), None, None, k.shape[0])
-        self.any = C.addressof(self.kv)
+        self.any, self.raw = C.addressof(self.kv), bytes(self.kv)
 
 
 class Rope:
@@ -412,18 +412,18 @@ def _check_rope(ctx: "Context", n: int, positions, q, q_out, turned: bool) -> in
     """The stride of the queries' rows, with the tensors of lr_rope_write found to be what the C side takes them for."""
     m, dev = ctx.model, ctx.device
     heads, width = m.n_q_heads, m.head_dim
-    fine = not turned or (positions is not None and _flat(positions, torch.int32, n, dev) and positions.numel() == n)
-    if not fine:
+    if turned and (positions is None or positions.dtype is not torch.int32 or positions.numel() != n or not positions.is_contiguous() or positions.get_device() != dev):
         raise ValueError(f"lr_rope_write: positions are contiguous int32 [{n}] on device {dev}")
-    if (q is None) != (q_out is None):
-        raise ValueError("lr_rope_write: q and q_out come together")
-    if q is None:
+    if q is None or q_out is None:
+        if q is not q_out:
+            raise ValueError("lr_rope_write: q and q_out come together")
         return 0
-    if not (q.shape == (n, heads, width) and q.dtype is torch.bfloat16 and q.get_device() == dev and (n == 0 or (q.stride(2) == 1 and q.stride(1) == width))):
+    row, head, one = q.stride() if q.dim() == 3 else (0, 0, 0)
+    if not (q.shape == (n, heads, width) and q.dtype is torch.bfloat16 and q.get_device() == dev and (n == 0 or (one == 1 and head == width))):
         raise ValueError(f"lr_rope_write: q is bf16 [{n}, {heads}, {width}] on device {dev}, a token's heads side by side: got {tuple(q.shape)} {q.dtype} strides {q.stride()} on {q.device}")
     if not (q_out.dtype is torch.bfloat16 and q_out.is_contiguous() and q_out.get_device() == dev and q_out.numel() == n * heads * width):
         raise ValueError(f"lr_rope_write: q_out is contiguous bf16 [{n}, {heads}, {width}] on device {dev}: got {tuple(q_out.shape)} {q_out.dtype} strides {q_out.stride()} on {q_out.device}")
-    return q.stride(0) if n > 1 else heads * width
+    return row if n > 1 else heads * width
 
 
 # (These run before every launch, where each look at a tensor takes a twentieth of a microsecond: all of them in one expression, and who is at fault only then.)
@@ -592,18 +592,27 @@ class Context:
 
     def lr_copy_pages(self, src, dst, src_pages: torch.Tensor, dst_pages: torch.Tensor, status: Optional[torch.Tensor] = None, stream=None) -> None:
         """Copies pages src_pages[i] of every cache of ``src`` to dst_pages[i] of its counterpart in ``dst`` (a cache or a list of them, a layer each)."""
-        src, dst = ([c] if isinstance(c, (Bf16Cache, Fp8Cache, Fp4Cache)) else list(c) for c in (src, dst))
-        if len(src) != len(dst):
-            raise ValueError(f"lr_copy_pages: {len(src)} caches to copy from, {len(dst)} to copy to")
-        for c in src + dst:
-            _check_cache(c, self)
-        n, dev = src_pages.numel(), self.device
-        _refuse("lr_copy_pages", dev, src_pages=(_flat(src_pages, torch.int32, n, dev), src_pages, f"int32 [{n}]"),
-                dst_pages=(_flat(dst_pages, torch.int32, n, dev) and dst_pages.numel() == n, dst_pages, f"int32 [{n}]"),
-                status=(_flat(status, torch.int32, 2, dev), status, "two int32"))
-        array = lr_kv_cache * len(src)
-        _check(lib().lr_copy_pages(self.handle, array(*(c.kv for c in src)), array(*(c.kv for c in dst)), len(src), src_pages.data_ptr(), dst_pages.data_ptr(), n,
-                                   _ptr(status), _stream_on(dev, stream)), "lr_copy_pages")
+        if isinstance(src, (list, tuple)):
+            if not isinstance(dst, (list, tuple)) or len(src) != len(dst):
+                raise ValueError(f"lr_copy_pages: {len(src)} caches to copy from, and others to copy to")
+            for c in (*src, *dst):
+                _check_cache(c, self)
+            n_caches, src_at, dst_at = len(src), b"".join([c.raw for c in src]), b"".join([c.raw for c in dst])
+        else:
+            if isinstance(dst, (list, tuple)):
+                raise ValueError(f"lr_copy_pages: one cache to copy from, {len(dst)} to copy to")
+            _check_cache(src, self)
+            _check_cache(dst, self)
+            n_caches, src_at, dst_at = 1, src.any, dst.any
+        dev, i32 = self.device, torch.int32
+        n = src_pages.numel()
+        if not (src_pages.dtype is dst_pages.dtype is i32 and dst_pages.numel() == n and src_pages.get_device() == dst_pages.get_device() == dev
+                and src_pages.is_contiguous() and dst_pages.is_contiguous() and (status is None or _flat(status, i32, 2, dev))):
+            _refuse("lr_copy_pages", dev, src_pages=(_flat(src_pages, i32, n, dev), src_pages, f"int32 [{n}]"),
+                    dst_pages=(_flat(dst_pages, i32, n, dev) and dst_pages.numel() == n, dst_pages, f"int32 [{n}]"),
+                    status=(_flat(status, i32, 2, dev), status, "two int32"))
+        _check(lib().lr_copy_pages(self.handle, src_at, dst_at, n_caches, src_pages.data_ptr(), dst_pages.data_ptr(), n, _ptr(status), _stream_on(dev, stream)),
+               "lr_copy_pages")
 
     def accept_sample_filtered_scratch(self, n_rows: int) -> torch.Tensor:
         n = C.c_size_t()

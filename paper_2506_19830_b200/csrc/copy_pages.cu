@@ -12,21 +12,23 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr int kUnits = 4;         // 16-byte units a thread has in flight
-constexpr int kMaxCaches = 32;    // layers in one launch: their pointers are the kernel's arguments
+constexpr int kMaxCaches = 32;    // layers in one launch: their pointers are the kernel's arguments (2.6 KB, which take the host a microsecond more than those of one)
 
 struct Pools {
   uint4 *p[4];  // K, V, scales of K, scales of V
 };
+template <int kCaches>
 struct CopyArgs {
-  Pools src[kMaxCaches], dst[kMaxCaches];
-  int64_t src_pages[kMaxCaches], dst_pages[kMaxCaches];
+  Pools src[kCaches], dst[kCaches];
+  int64_t src_pages[kCaches], dst_pages[kCaches];
   int32_t codes, scales;  // units of a page in a pool of K or V, and in one of scales
   int32_t parts;          // CTAs a pair
   int32_t n_pairs;
 };
 
+template <int kCaches>
 __global__ void __launch_bounds__(kThreads)
-copy_pages_kernel(const __grid_constant__ CopyArgs a, const int32_t *__restrict__ src_pages, const int32_t *__restrict__ dst_pages, int32_t *__restrict__ status) {
+copy_pages_kernel(const __grid_constant__ CopyArgs<kCaches> a, const int32_t *__restrict__ src_pages, const int32_t *__restrict__ dst_pages, int32_t *__restrict__ status) {
   asm volatile("griddepcontrol.wait;" ::: "memory");  // the pages may come from the kernel launched just before
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   const int pair = blockIdx.x / a.parts, part = blockIdx.x % a.parts, c = blockIdx.y;
@@ -73,9 +75,7 @@ int launch_copy_pages(lr_ctx *ctx, const lr_kv_cache *src, const lr_kv_cache *ds
     set_error("lr_copy_pages: too many pages in one call");
     return LR_EUNSUPPORTED;
   }
-  for (int c0 = 0; c0 < n_caches; c0 += kMaxCaches) {
-    CopyArgs a = {};
-    const int n = std::min(kMaxCaches, n_caches - c0);
+  auto launch = [&](auto a, int c0, int n) {
     for (int c = 0; c < n; ++c) {
       const lr_kv_cache &from = src[c0 + c], &to = dst[c0 + c];
       a.src[c] = {{(uint4 *)from.k_d, (uint4 *)from.v_d, (uint4 *)from.k_scale_d, (uint4 *)from.v_scale_d}};
@@ -88,9 +88,13 @@ int launch_copy_pages(lr_ctx *ctx, const lr_kv_cache *src, const lr_kv_cache *ds
     a.parts = (int32_t)parts;
     a.n_pairs = n_pairs;
     ctx->launches++;
-    if (int rc = cuda_fail(launch_dependent(copy_pages_kernel, dim3((unsigned)(parts * n_pairs), (unsigned)n), dim3(kThreads), 0, s, a, src_pages, dst_pages, status),
-                           "copy_pages_kernel launch"))
-      return rc;
+    return cuda_fail(launch_dependent(copy_pages_kernel<(int)(sizeof(a.src) / sizeof(Pools))>, dim3((unsigned)(parts * n_pairs), (unsigned)n), dim3(kThreads), 0, s, a, src_pages,
+                                      dst_pages, status),
+                     "copy_pages_kernel launch");
+  };
+  for (int c0 = 0; c0 < n_caches; c0 += kMaxCaches) {
+    const int n = std::min(kMaxCaches, n_caches - c0);
+    if (int rc = n == 1 ? launch(CopyArgs<1>{}, c0, n) : launch(CopyArgs<kMaxCaches>{}, c0, n)) return rc;
   }
   return LR_OK;
 }

@@ -63,6 +63,115 @@ rope_write_kernel(const __grid_constant__ RopeArgs a) {
   const int t0 = blockIdx.x * a.tokens, n = min(a.tokens, a.n_tokens - t0);
   const int all = a.q_heads + 2 * a.kv_heads, h0 = a.q0 + blockIdx.y * kHeads, heads = min(kHeads, all - h0);
   const int rows0 = max(h0, a.q_heads), rows = max(h0 + heads - rows0, 0);  // K and V among them
+  // An item is the eight pairs of part `threadIdx.x % kLanes` of a head of a token; a thread's items are kStep heads apart.  Two are asked for together, the first ones
+  // before the angles are worked out.
+  constexpr int kStep = kThreads / kLanes;
+  const int part = threadIdx.x % kLanes, p0 = part * 8;
+  struct Item {
+    int t, h;      // token and head of this CTA's
+    uint32_t r[8];
+  } item[2];
+  auto settle = [&](Item &x) {
+    while (x.h >= heads) x.h -= heads, ++x.t;
+  };
+  // channels of the 8 pairs: c and d and the seven behind them where the halves of what is turned lie apart, else the 16 from c on
+  auto halves_apart = [&](int head) { return head < a.q_heads + a.kv_heads && p0 < a.pairs && a.interleaved == 0; };
+  auto load = [&](Item &x) {
+    if (x.t >= n) return;
+    const int head = h0 + x.h, token = t0 + x.t;
+    const uint16_t *src = head < a.q_heads ? a.q + token * a.q_stride + head * kD
+                                           : head < a.q_heads + a.kv_heads ? a.k + token * a.k_stride + (head - a.q_heads) * kD
+                                                                           : a.v + token * a.v_stride + (head - a.q_heads - a.kv_heads) * kD;
+    const bool apart = halves_apart(head);
+    if constexpr (kVector) {
+      const int c = apart ? p0 : 2 * p0, d = apart ? p0 + a.pairs : c + 8;
+      const uint4 u = __ldcg(reinterpret_cast<const uint4 *>(src + c)), w = __ldcg(reinterpret_cast<const uint4 *>(src + d));
+      x.r[0] = u.x, x.r[1] = u.y, x.r[2] = u.z, x.r[3] = u.w, x.r[4] = w.x, x.r[5] = w.y, x.r[6] = w.z, x.r[7] = w.w;
+    } else {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const bool far = apart && p0 + j < a.pairs;
+        x.r[j] = (uint32_t)__ldcg(src + (far ? p0 + j : 2 * (p0 + j))) | (uint32_t)__ldcg(src + (far ? p0 + j + a.pairs : 2 * (p0 + j) + 1)) << 16;
+      }
+    }
+  };
+  auto finish = [&](const Item &it) {
+    const int t = it.t, head = h0 + it.h, token = t0 + t;
+    if (t >= n) return;
+    const bool is_q = head < a.q_heads, is_v = head >= a.q_heads + a.kv_heads, turned = !is_v && p0 < a.pairs, apart = halves_apart(head);
+    const int kv = is_v ? head - a.q_heads - a.kv_heads : head - a.q_heads, c = apart ? p0 : 2 * p0, d = apart ? p0 + a.pairs : c + 8;
+    const int64_t slot = s_slot[t];
+    if (!is_q && slot < 0) return;
+    float x[8], y[8];
+    uint32_t r[8];  // as they lie; what is not turned is not touched (a NaN keeps its bits)
+#pragma unroll
+    for (int j = 0; j < 8; ++j) r[j] = it.r[j];
+    if (kVector && apart) {
+#pragma unroll
+      for (int j = 0; j < 4; ++j) x[2 * j] = low(r[j]), x[2 * j + 1] = high(r[j]), y[2 * j] = low(r[4 + j]), y[2 * j + 1] = high(r[4 + j]);
+    } else {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) x[j] = low(r[j]), y[j] = high(r[j]);
+    }
+    if (turned) {
+#pragma unroll
+      for (int j = 0; j < 8; ++j)
+        if (p0 + j < a.pairs) {
+          const float2 e = s_turn[t][p0 + j];
+          const float to = x[j] * e.x - y[j] * e.y;
+          y[j] = fmaf(x[j], e.y, y[j] * e.x);
+          x[j] = to;
+          if (!kVector || !apart) r[j] = bf16_pair(x[j], y[j]);
+        }
+      if (kVector && apart) {  // all of them are turned
+#pragma unroll
+        for (int j = 0; j < 4; ++j) r[j] = bf16_pair(x[2 * j], x[2 * j + 1]), r[4 + j] = bf16_pair(y[2 * j], y[2 * j + 1]);
+      }
+    }
+    if (kKind == LR_KV_BF16 || is_q) {
+      uint16_t *dst = is_q ? a.q_out + ((int64_t)token * a.q_heads + head) * kD
+                           : reinterpret_cast<uint16_t *>(a.pool[is_v ? 1 : 0]) + (((slot / kPage) * a.kv_heads + kv) * kPage + slot % kPage) * kD;
+      if constexpr (kVector) {
+        *reinterpret_cast<uint4 *>(dst + c) = make_uint4(r[0], r[1], r[2], r[3]);
+        *reinterpret_cast<uint4 *>(dst + d) = make_uint4(r[4], r[5], r[6], r[7]);
+      } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          const bool far = apart && p0 + j < a.pairs;
+          dst[far ? p0 + j : 2 * (p0 + j)] = (uint16_t)r[j];
+          dst[far ? p0 + j + a.pairs : 2 * (p0 + j) + 1] = (uint16_t)(r[j] >> 16);
+        }
+      }
+    } else {
+      float *row = s_rows + (t * rows + head - rows0) * kRow;
+      auto at = [](int ch) { return ch / kFp4Group * kPadded + ch % kFp4Group; };
+      if constexpr (kVector) {
+        float4 *to_c = reinterpret_cast<float4 *>(row + at(c)), *to_d = reinterpret_cast<float4 *>(row + at(d));
+        if (apart) {
+          to_c[0] = make_float4(x[0], x[1], x[2], x[3]), to_c[1] = make_float4(x[4], x[5], x[6], x[7]);
+          to_d[0] = make_float4(y[0], y[1], y[2], y[3]), to_d[1] = make_float4(y[4], y[5], y[6], y[7]);
+        } else {
+          to_c[0] = make_float4(x[0], y[0], x[1], y[1]), to_c[1] = make_float4(x[2], y[2], x[3], y[3]);
+          to_d[0] = make_float4(x[4], y[4], x[5], y[5]), to_d[1] = make_float4(x[6], y[6], x[7], y[7]);
+        }
+      } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          const bool far = apart && p0 + j < a.pairs;
+          row[at(far ? p0 + j : 2 * (p0 + j))] = x[j];
+          row[at(far ? p0 + j + a.pairs : 2 * (p0 + j) + 1)] = y[j];
+        }
+      }
+    }
+  };
+  item[0].t = item[1].t = 0;
+  item[0].h = threadIdx.x / kLanes;
+  item[1].h = item[0].h + kStep;
+#pragma unroll
+  for (int u = 0; u < 2; ++u) {
+    settle(item[u]);
+    load(item[u]);
+  }
   for (int i = threadIdx.x; i < n * a.pairs; i += kThreads) {
     const int t = i / a.pairs, p = i - t * a.pairs;
     const double turns = (double)__ldcg(a.positions + t0 + t) * a.turns[p];
@@ -82,91 +191,14 @@ rope_write_kernel(const __grid_constant__ RopeArgs a) {
     s_slot[threadIdx.x] = slot;
   }
   __syncthreads();
-  const int items = n * heads * kLanes;
-  for (int i = threadIdx.x; i < items; i += kThreads) {
-    const int part = i % kLanes, th = i / kLanes, t = th / heads, head = h0 + th - t * heads, token = t0 + t;
-    const bool is_q = head < a.q_heads, is_v = head >= a.q_heads + a.kv_heads;
-    const int kv = is_v ? head - a.q_heads - a.kv_heads : head - a.q_heads;
-    const int64_t slot = s_slot[t];
-    if (!is_q && slot < 0) continue;
-    const uint16_t *src = is_q ? a.q + token * a.q_stride + head * kD : is_v ? a.v + token * a.v_stride + kv * kD : a.k + token * a.k_stride + kv * kD;
-    const int p0 = part * 8;
-    const bool turned = !is_v && p0 < a.pairs;
-    // channels of the 8 pairs: c and d and the seven behind them, or the 16 from c on
-    const bool apart = turned && !a.interleaved;
-    const int c = apart ? p0 : 2 * p0, d = apart ? p0 + a.pairs : c + 8;
-    float x[8], y[8];
-    uint32_t r[8];  // as they lie; what is not turned is not touched (a NaN keeps its bits)
-    if constexpr (kVector) {
-      const uint4 u = __ldcg(reinterpret_cast<const uint4 *>(src + c)), w = __ldcg(reinterpret_cast<const uint4 *>(src + d));
-      r[0] = u.x, r[1] = u.y, r[2] = u.z, r[3] = u.w, r[4] = w.x, r[5] = w.y, r[6] = w.z, r[7] = w.w;
-      if (apart) {
+  while (item[0].t < n) {
 #pragma unroll
-        for (int j = 0; j < 4; ++j) x[2 * j] = low(r[j]), x[2 * j + 1] = high(r[j]), y[2 * j] = low(r[4 + j]), y[2 * j + 1] = high(r[4 + j]);
-      } else {
+    for (int u = 0; u < 2; ++u) finish(item[u]);
 #pragma unroll
-        for (int j = 0; j < 8; ++j) x[j] = low(r[j]), y[j] = high(r[j]);
-      }
-    } else {
-#pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        const bool halves = apart && p0 + j < a.pairs;
-        const uint32_t one = __ldcg(src + (halves ? p0 + j : 2 * (p0 + j))), two = __ldcg(src + (halves ? p0 + j + a.pairs : 2 * (p0 + j) + 1));
-        r[j] = one | two << 16;
-        x[j] = low(r[j]), y[j] = high(r[j]);
-      }
-    }
-    if (turned) {
-#pragma unroll
-      for (int j = 0; j < 8; ++j)
-        if (p0 + j < a.pairs) {
-          const float2 e = s_turn[t][p0 + j];
-          const float to = x[j] * e.x - y[j] * e.y;
-          y[j] = fmaf(x[j], e.y, y[j] * e.x);
-          x[j] = to;
-          if (!kVector || !apart) r[j] = bf16_pair(x[j], y[j]);
-        }
-      if (kVector && apart) {  // all of them are turned
-#pragma unroll
-        for (int j = 0; j < 4; ++j) r[j] = bf16_pair(x[2 * j], x[2 * j + 1]), r[4 + j] = bf16_pair(y[2 * j], y[2 * j + 1]);
-      }
-    }
-    uint16_t *dst;
-    if (is_q) dst = a.q_out + ((int64_t)token * a.q_heads + head) * kD;
-    else if (kKind == LR_KV_BF16) dst = reinterpret_cast<uint16_t *>(a.pool[is_v ? 1 : 0]) + (((slot / kPage) * a.kv_heads + kv) * kPage + slot % kPage) * kD;
-    else dst = nullptr;
-    if (kKind == LR_KV_BF16 || is_q) {
-      if constexpr (kVector) {
-        *reinterpret_cast<uint4 *>(dst + c) = make_uint4(r[0], r[1], r[2], r[3]);
-        *reinterpret_cast<uint4 *>(dst + d) = make_uint4(r[4], r[5], r[6], r[7]);
-      } else {
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          const bool halves = apart && p0 + j < a.pairs;
-          dst[halves ? p0 + j : 2 * (p0 + j)] = (uint16_t)r[j];
-          dst[halves ? p0 + j + a.pairs : 2 * (p0 + j) + 1] = (uint16_t)(r[j] >> 16);
-        }
-      }
-    } else {
-      float *row = s_rows + (t * rows + head - rows0) * kRow;
-      auto at = [](int ch) { return ch / kFp4Group * kPadded + ch % kFp4Group; };
-      if constexpr (kVector) {
-        float4 *to_c = reinterpret_cast<float4 *>(row + at(c)), *to_d = reinterpret_cast<float4 *>(row + at(d));
-        if (apart) {
-          to_c[0] = make_float4(x[0], x[1], x[2], x[3]), to_c[1] = make_float4(x[4], x[5], x[6], x[7]);
-          to_d[0] = make_float4(y[0], y[1], y[2], y[3]), to_d[1] = make_float4(y[4], y[5], y[6], y[7]);
-        } else {
-          to_c[0] = make_float4(x[0], y[0], x[1], y[1]), to_c[1] = make_float4(x[2], y[2], x[3], y[3]);
-          to_d[0] = make_float4(x[4], y[4], x[5], y[5]), to_d[1] = make_float4(x[6], y[6], x[7], y[7]);
-        }
-      } else {
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          const bool halves = apart && p0 + j < a.pairs;
-          row[at(halves ? p0 + j : 2 * (p0 + j))] = x[j];
-          row[at(halves ? p0 + j + a.pairs : 2 * (p0 + j) + 1)] = y[j];
-        }
-      }
+    for (int u = 0; u < 2; ++u) {
+      item[u].h += 2 * kStep;
+      settle(item[u]);
+      load(item[u]);
     }
   }
   if constexpr (kKind != LR_KV_BF16) {
