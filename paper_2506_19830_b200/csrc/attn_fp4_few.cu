@@ -128,6 +128,7 @@ attn_fp4_few_kernel(DevBatch d, DevTcPlan tc, const __grid_constant__ Fp4Call in
   uint32_t to_v[kUnits];
 #pragma unroll
   for (int u = 0; u < kUnits; ++u) to_v[u] = Sh::kCodeBytes + v_unit<kD>(copy_key + u * 8, copy_unit);
+  const uint32_t v_lane = Sh::kCodeBytes + v_unit<kD>(2 * t, g * (kD / 16) / 16) + g * (kD / 16) % 16;  // where this lane's channels of key 2t lie
   uint32_t asked = 0;  // stage
   auto ask_page = [&]() {
     if (entry_head >= 0) {
@@ -219,25 +220,25 @@ attn_fp4_few_kernel(DevBatch d, DevTcPlan tc, const __grid_constant__ Fp4Call in
       __syncwarp();  // what the other lanes have copied is there
       const uint32_t at = ring + from * Sh::kPageBytes, scales = at + 2 * Sh::kCodeBytes;
       from = from + 1 == Sh::kStages ? 0u : from + 1;
-      uint32_t k[2][kKWords], kb[2], v[4][kVWords], vb[4], what[2];
+      uint32_t k[2][kKWords], kb[2], v[4][kVWords], vb[4], what[2], word[1];
+      const uint32_t k_from = at + g * (kD / 2) + t * (kD / 8), kb_from = scales + g * (kD / kFp4Group) + t * (kD / 4) / kFp4Group;
+      const uint32_t v_from = at + v_lane, vb_from = scales + Sh::kScaleBytes + 2 * t * (kD / kFp4Group) + g * (kD / 8) / kFp4Group;
 #pragma unroll
       for (int j = 0; j < 2; ++j) {
-        ld_codes(k[j], at + (g + 8 * j) * (kD / 2) + t * (kD / 8));
-        kb[j] = ld_byte(scales + (g + 8 * j) * (kD / kFp4Group) + t * (kD / 4) / kFp4Group);
+        ld_codes(k[j], k_from + j * 8 * (kD / 2));
+        kb[j] = ld_byte(kb_from + j * 8 * (kD / kFp4Group));
       }
-#pragma unroll
-      for (int j = 0; j < 4; ++j) vb[j] = ld_byte(scales + Sh::kScaleBytes + (2 * t + (j >> 1) * 8 + (j & 1)) * (kD / kFp4Group) + g * (kD / 8) / kFp4Group);
       ld_codes(what, scales + 2 * Sh::kScaleBytes);
+      ld_codes(word, scales + lane % (Sh::kScaleBytes / 2) * 4);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) vb[j] = ld_byte(vb_from + ((j >> 1) * 8 + (j & 1)) * (kD / kFp4Group));
       const uint32_t meta = what[0];
       const bool masked = what[1] != 0u;
       const int valid = (int)(meta & 31u);
-      if (__any_sync(0xFFFFFFFFu, max(max(max(kb[0], kb[1]), max(vb[0], vb[1])), max(vb[2], vb[3])) > kMostHalf ||
-                                      min(min(min(kb[0], kb[1]), min(vb[0], vb[1])), min(vb[2], vb[3])) < kLeastHalf)) {  // (among it what a slot of no valid token holds)
+      if (__any_sync(0xFFFFFFFFu, any_odd_scale(word[0]))) {  // (among it what a slot of no valid token holds)
         bool odd = false;
 #pragma unroll
-        for (int j = 0; j < 2; ++j) odd = odd || (odd_scale(kb[j]) && g + 8 * j < valid);
-#pragma unroll
-        for (int j = 0; j < 4; ++j) odd = odd || (odd_scale(vb[j]) && 2 * t + (j >> 1) * 8 + (j & 1) < valid);
+        for (int x = 0; x < 4; ++x) odd = odd || (odd_scale((word[0] >> (8 * x)) & 0xFFu) && (lane * 4 + x) % Sh::kScaleBytes / (kD / kFp4Group) < valid);
         if (odd) *reinterpret_cast<volatile int *>(&s_odd) = pc + 1;
       }
       float s[kNB][4];
@@ -298,7 +299,7 @@ attn_fp4_few_kernel(DevBatch d, DevTcPlan tc, const __grid_constant__ Fp4Call in
       }
       // O^T += V^T P^T
 #pragma unroll
-      for (int j = 0; j < 4; ++j) ld_codes(v[j], at + Sh::kCodeBytes + v_unit<kD>(2 * t + (j >> 1) * 8 + (j & 1), g * (kD / 16) / 16) + g * (kD / 16) % 16);
+      for (int j = 0; j < 4; ++j) ld_codes(v[j], v_from + ((j >> 1) * 8 + (j & 1) * 4) * (kD / 2));  // (odd keys four rows behind the even ones)
 #pragma unroll
       for (int j = 0; j < 2; ++j) f[j] = half_factors(vb[2 * j], vb[2 * j + 1]);
       if (masked) {  // slots of no valid token

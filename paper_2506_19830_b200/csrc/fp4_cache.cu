@@ -37,8 +37,11 @@ fp4_write_kernel(CacheRows w, const uint16_t *__restrict__ k, const uint16_t *__
   constexpr int kLanes = kD / 16;  // threads a row
   asm volatile("griddepcontrol.wait;" ::: "memory");  // the projection may be the kernel launched just before
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-  const int64_t row = ((int64_t)blockIdx.x * kThreads + threadIdx.x) / kLanes, token = row / w.heads;
-  const int part = threadIdx.x % kLanes, head = (int)(row - token * w.heads);
+  const int64_t row = (int64_t)blockIdx.x * (kThreads / kLanes) + threadIdx.x / kLanes;
+  const int part = threadIdx.x % kLanes;
+  int64_t token;
+  int head;
+  w.split(row, token, head);
   const int64_t at = row < w.n_rows ? cache_row(__ldcg(reinterpret_cast<const long long *>(w.slots) + token), w.n_slots, w.heads, head, token, w.status) : -1;
   uint4 x[2][2];
 #pragma unroll
@@ -79,8 +82,11 @@ fp4_read_kernel(CacheRows w, uint16_t *__restrict__ k, uint16_t *__restrict__ v,
   constexpr int kLanes = kD / 16;  // threads a row, 8 channels in each half of it
   asm volatile("griddepcontrol.wait;" ::: "memory");
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-  const int64_t row = ((int64_t)blockIdx.x * kThreads + threadIdx.x) / kLanes, token = row / w.heads;
-  const int part = threadIdx.x % kLanes, head = (int)(row - token * w.heads);
+  const int64_t row = (int64_t)blockIdx.x * (kThreads / kLanes) + threadIdx.x / kLanes;
+  const int part = threadIdx.x % kLanes;
+  int64_t token;
+  int head;
+  w.split(row, token, head);
   if (row >= w.n_rows) return;
   const int64_t at = cache_row(__ldcg(reinterpret_cast<const long long *>(w.slots) + token), w.n_slots, w.heads, head, token, w.status);
   if (at < 0) return;

@@ -79,6 +79,8 @@ __device__ __forceinline__ int fp8_byte(uint32_t top) { return max((int)(top >> 
 // 2^(127 - byte), for bytes from 1 to 253: what a row is multiplied by
 __device__ __forceinline__ float scale_down(int byte) { return __uint_as_float((uint32_t)(254 - byte) << 23); }
 
+static_assert(kPage == 16, "slots are taken apart by shifts");
+
 // The rows of a call that moves K and V between a projection's output and the slots of a cache.
 struct CacheRows {
   const int64_t *slots;
@@ -87,10 +89,21 @@ struct CacheRows {
   int64_t k_stride, v_stride;
   int32_t heads;
   int32_t *status;
+  // a thread's token and head; a division of 64 bits, which takes as long as the rest of a thread's work, only where rows are that many
+  __device__ __forceinline__ void split(int64_t row, int64_t &token, int &head) const {
+    if (n_rows <= 0x7FFFFFFF) {
+      const uint32_t t = (uint32_t)row / (uint32_t)heads;
+      token = t;
+      head = (int)((uint32_t)row - t * (uint32_t)heads);
+    } else {
+      token = row / heads;
+      head = (int)(row - token * heads);
+    }
+  }
 };
 // The number of a token's row in a pool, (page * heads + head) * 16 + place; -1: nothing to do.  A slot beyond the cache is reported.
 __device__ __forceinline__ int64_t cache_row(int64_t slot, int64_t n_slots, int32_t heads, int32_t head, int64_t token, int32_t *status) {
-  if (slot >= 0 && slot < n_slots) return ((slot / kPage) * heads + head) * kPage + slot % kPage;
+  if (slot >= 0 && slot < n_slots) return ((slot >> 4) * heads + head) * kPage + (slot & 15);
   if (slot >= 0 && status != nullptr) {
     status[0] = LR_EBOUNDS;
     status[1] = (int32_t)token;

@@ -20,7 +20,7 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr int kHeads = 64;       // of q, k and v together, a CTA's share of a token
-constexpr int kMaxTokens = 4;    // ... and how many tokens it takes
+constexpr int kMaxTokens = 8;    // ... and how many tokens it takes
 constexpr int kRowBytes = 40 << 10;  // of shared memory for rows that are to be quantised
 constexpr int kPadded = kFp4Group + 4;  // floats that 32 channels take there: threads next to each other, a group each, read different banks
 
@@ -51,103 +51,112 @@ __device__ __forceinline__ float high(uint32_t w) { return __uint_as_float(w & 0
 
 // kKind: of the cache.  kVector: the pairs of every thread start on 16 bytes.
 template <int kD, int kKind, bool kVector>
-__global__ void __launch_bounds__(kThreads)
+__global__ void __launch_bounds__(kThreads, 4)  // (three of them without being asked: a prompt of 32 K tokens 161 us instead of 167)
 rope_write_kernel(const __grid_constant__ RopeArgs a) {
   constexpr int kLanes = kD / 16;  // threads a head
   constexpr int kRow = kD / kFp4Group * kPadded;
   extern __shared__ __align__(16) float s_rows[];  // [token][K or V row of this CTA][kRow], of a cache in 8 or 4 bits
-  __shared__ float2 s_turn[kMaxTokens][LR_ROPE_MAX_DIM / 2];
-  __shared__ int64_t s_slot[kMaxTokens];
+  __shared__ float4 s_turn[kMaxTokens][4 * kLanes];  // [pairs 2i, 2i + 1 of a part][part]: cosine and sine of either
+  __shared__ int64_t s_row[kMaxTokens];  // of the token's first head in the pools; -1: none
   asm volatile("griddepcontrol.wait;" ::: "memory");  // the projection may be the kernel launched just before
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   const int t0 = blockIdx.x * a.tokens, n = min(a.tokens, a.n_tokens - t0);
   const int all = a.q_heads + 2 * a.kv_heads, h0 = a.q0 + blockIdx.y * kHeads, heads = min(kHeads, all - h0);
   const int rows0 = max(h0, a.q_heads), rows = max(h0 + heads - rows0, 0);  // K and V among them
-  // An item is the eight pairs of part `threadIdx.x % kLanes` of a head of a token; a thread's items are kStep heads apart.  Two are asked for together, the first ones
-  // before the angles are worked out.
-  constexpr int kStep = kThreads / kLanes;
-  const int part = threadIdx.x % kLanes, p0 = part * 8;
-  struct Item {
-    int t, h;      // token and head of this CTA's
+  // A thread has the eight pairs of part `threadIdx.x % kLanes` of one or two heads, kStep apart, of every token; where there are fewer heads than that, of every so many tokens.
+  constexpr int kStep = kThreads / kLanes, kMine = kHeads / kStep > 0 ? kHeads / kStep : 1;
+  const int part = threadIdx.x % kLanes, p0 = part * 8, seat = threadIdx.x / kLanes, wide = min(heads, kStep), stride = kStep / wide, t_first = seat / wide;
+  struct Mine {
+    const uint16_t *src;  // of the token that is asked for next
+    int64_t src_step;
+    int32_t off;          // of the head in a row of q_out (channels), or of K or V in a page (rows)
+    int32_t row;          // among the rows that are quantised
+    bool live, is_q, is_v, turned, apart;
     uint32_t r[8];
-  } item[2];
-  auto settle = [&](Item &x) {
-    while (x.h >= heads) x.h -= heads, ++x.t;
-  };
+  } mine[kMine];
+#pragma unroll
+  for (int u = 0; u < kMine; ++u) {
+    Mine &x = mine[u];
+    const int h = seat % wide + u * kStep, head = h0 + h;
+    x.live = h < heads && t_first < stride;
+    x.is_q = head < a.q_heads;
+    x.is_v = head >= a.q_heads + a.kv_heads;
+    x.turned = !x.is_v && p0 < a.pairs;
+    x.apart = x.turned && a.interleaved == 0;
+    const int kv = x.is_v ? head - a.q_heads - a.kv_heads : head - a.q_heads;
+    const int64_t step = x.is_q ? a.q_stride : x.is_v ? a.v_stride : a.k_stride;
+    x.src = (x.is_q ? a.q : x.is_v ? a.v : a.k) + (t0 + t_first) * step + (x.is_q ? head : kv) * kD;
+    x.src_step = step * stride;
+    x.off = x.is_q ? head * kD : kv * kPage;
+    x.row = head - rows0;
+  }
   // channels of the 8 pairs: c and d and the seven behind them where the halves of what is turned lie apart, else the 16 from c on
-  auto halves_apart = [&](int head) { return head < a.q_heads + a.kv_heads && p0 < a.pairs && a.interleaved == 0; };
-  auto load = [&](Item &x) {
-    if (x.t >= n) return;
-    const int head = h0 + x.h, token = t0 + x.t;
-    const uint16_t *src = head < a.q_heads ? a.q + token * a.q_stride + head * kD
-                                           : head < a.q_heads + a.kv_heads ? a.k + token * a.k_stride + (head - a.q_heads) * kD
-                                                                           : a.v + token * a.v_stride + (head - a.q_heads - a.kv_heads) * kD;
-    const bool apart = halves_apart(head);
+  auto load = [&](Mine &x) {
     if constexpr (kVector) {
-      const int c = apart ? p0 : 2 * p0, d = apart ? p0 + a.pairs : c + 8;
-      const uint4 u = __ldcg(reinterpret_cast<const uint4 *>(src + c)), w = __ldcg(reinterpret_cast<const uint4 *>(src + d));
+      const int c = x.apart ? p0 : 2 * p0, d = x.apart ? p0 + a.pairs : c + 8;
+      const uint4 u = __ldcg(reinterpret_cast<const uint4 *>(x.src + c)), w = __ldcg(reinterpret_cast<const uint4 *>(x.src + d));
       x.r[0] = u.x, x.r[1] = u.y, x.r[2] = u.z, x.r[3] = u.w, x.r[4] = w.x, x.r[5] = w.y, x.r[6] = w.z, x.r[7] = w.w;
     } else {
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
-        const bool far = apart && p0 + j < a.pairs;
-        x.r[j] = (uint32_t)__ldcg(src + (far ? p0 + j : 2 * (p0 + j))) | (uint32_t)__ldcg(src + (far ? p0 + j + a.pairs : 2 * (p0 + j) + 1)) << 16;
+        const bool far = x.apart && p0 + j < a.pairs;
+        x.r[j] = (uint32_t)__ldcg(x.src + (far ? p0 + j : 2 * (p0 + j))) | (uint32_t)__ldcg(x.src + (far ? p0 + j + a.pairs : 2 * (p0 + j) + 1)) << 16;
       }
     }
+    x.src += x.src_step;
   };
-  auto finish = [&](const Item &it) {
-    const int t = it.t, head = h0 + it.h, token = t0 + t;
-    if (t >= n) return;
-    const bool is_q = head < a.q_heads, is_v = head >= a.q_heads + a.kv_heads, turned = !is_v && p0 < a.pairs, apart = halves_apart(head);
-    const int kv = is_v ? head - a.q_heads - a.kv_heads : head - a.q_heads, c = apart ? p0 : 2 * p0, d = apart ? p0 + a.pairs : c + 8;
-    const int64_t slot = s_slot[t];
-    if (!is_q && slot < 0) return;
+  auto finish = [&](Mine &it, int t) {
+    const int64_t at_row = s_row[t];
+    if (!it.is_q && at_row < 0) return;
+    const int c = it.apart ? p0 : 2 * p0, d = it.apart ? p0 + a.pairs : c + 8;
     float x[8], y[8];
-    uint32_t r[8];  // as they lie; what is not turned is not touched (a NaN keeps its bits)
-#pragma unroll
-    for (int j = 0; j < 8; ++j) r[j] = it.r[j];
-    if (kVector && apart) {
+    uint32_t (&r)[8] = it.r;  // as they lie; what is not turned is not touched (a NaN keeps its bits)
+    if (kVector && it.apart) {
 #pragma unroll
       for (int j = 0; j < 4; ++j) x[2 * j] = low(r[j]), x[2 * j + 1] = high(r[j]), y[2 * j] = low(r[4 + j]), y[2 * j + 1] = high(r[4 + j]);
     } else {
 #pragma unroll
       for (int j = 0; j < 8; ++j) x[j] = low(r[j]), y[j] = high(r[j]);
     }
-    if (turned) {
+    if (it.turned) {
 #pragma unroll
-      for (int j = 0; j < 8; ++j)
-        if (p0 + j < a.pairs) {
-          const float2 e = s_turn[t][p0 + j];
-          const float to = x[j] * e.x - y[j] * e.y;
-          y[j] = fmaf(x[j], e.y, y[j] * e.x);
-          x[j] = to;
-          if (!kVector || !apart) r[j] = bf16_pair(x[j], y[j]);
+      for (int i = 0; i < 4; ++i) {
+        const float4 e2 = s_turn[t][i * kLanes + part];  // of two pairs
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+          const int j = 2 * i + k;
+          const float cs = k == 0 ? e2.x : e2.z, sn = k == 0 ? e2.y : e2.w, to = x[j] * cs - y[j] * sn, other = fmaf(x[j], sn, y[j] * cs);
+          if (p0 + j < a.pairs) {
+            x[j] = to;
+            y[j] = other;
+            if (!kVector || !it.apart) r[j] = bf16_pair(to, other);
+          }
         }
-      if (kVector && apart) {  // all of them are turned
+      }
+      if (kVector && it.apart) {  // all of them are turned
 #pragma unroll
         for (int j = 0; j < 4; ++j) r[j] = bf16_pair(x[2 * j], x[2 * j + 1]), r[4 + j] = bf16_pair(y[2 * j], y[2 * j + 1]);
       }
     }
-    if (kKind == LR_KV_BF16 || is_q) {
-      uint16_t *dst = is_q ? a.q_out + ((int64_t)token * a.q_heads + head) * kD
-                           : reinterpret_cast<uint16_t *>(a.pool[is_v ? 1 : 0]) + (((slot / kPage) * a.kv_heads + kv) * kPage + slot % kPage) * kD;
+    if (kKind == LR_KV_BF16 || it.is_q) {
+      uint16_t *dst = it.is_q ? a.q_out + (int64_t)(t0 + t) * a.q_heads * kD + it.off : reinterpret_cast<uint16_t *>(a.pool[it.is_v ? 1 : 0]) + (at_row + it.off) * kD;
       if constexpr (kVector) {
         *reinterpret_cast<uint4 *>(dst + c) = make_uint4(r[0], r[1], r[2], r[3]);
         *reinterpret_cast<uint4 *>(dst + d) = make_uint4(r[4], r[5], r[6], r[7]);
       } else {
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-          const bool far = apart && p0 + j < a.pairs;
+          const bool far = it.apart && p0 + j < a.pairs;
           dst[far ? p0 + j : 2 * (p0 + j)] = (uint16_t)r[j];
           dst[far ? p0 + j + a.pairs : 2 * (p0 + j) + 1] = (uint16_t)(r[j] >> 16);
         }
       }
     } else {
-      float *row = s_rows + (t * rows + head - rows0) * kRow;
+      float *row = s_rows + (t * rows + it.row) * kRow;
       auto at = [](int ch) { return ch / kFp4Group * kPadded + ch % kFp4Group; };
       if constexpr (kVector) {
         float4 *to_c = reinterpret_cast<float4 *>(row + at(c)), *to_d = reinterpret_cast<float4 *>(row + at(d));
-        if (apart) {
+        if (it.apart) {
           to_c[0] = make_float4(x[0], x[1], x[2], x[3]), to_c[1] = make_float4(x[4], x[5], x[6], x[7]);
           to_d[0] = make_float4(y[0], y[1], y[2], y[3]), to_d[1] = make_float4(y[4], y[5], y[6], y[7]);
         } else {
@@ -157,49 +166,39 @@ rope_write_kernel(const __grid_constant__ RopeArgs a) {
       } else {
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-          const bool far = apart && p0 + j < a.pairs;
+          const bool far = it.apart && p0 + j < a.pairs;
           row[at(far ? p0 + j : 2 * (p0 + j))] = x[j];
           row[at(far ? p0 + j + a.pairs : 2 * (p0 + j) + 1)] = y[j];
         }
       }
     }
   };
-  item[0].t = item[1].t = 0;
-  item[0].h = threadIdx.x / kLanes;
-  item[1].h = item[0].h + kStep;
+  // the first token's rows are on their way while the angles are worked out
 #pragma unroll
-  for (int u = 0; u < 2; ++u) {
-    settle(item[u]);
-    load(item[u]);
-  }
+  for (int u = 0; u < kMine; ++u)
+    if (mine[u].live && t_first < n) load(mine[u]);
   for (int i = threadIdx.x; i < n * a.pairs; i += kThreads) {
     const int t = i / a.pairs, p = i - t * a.pairs;
     const double turns = (double)__ldcg(a.positions + t0 + t) * a.turns[p];
     float sn, cs;
     sincospif(2.0f * (float)(turns - rint(turns)), &sn, &cs);
-    s_turn[t][p] = make_float2(cs * a.amplitude, sn * a.amplitude);
+    // two neighbouring pairs of every part side by side: a thread takes them at once, and its neighbours' lie behind
+    reinterpret_cast<float2 *>(&s_turn[t][(p % 8 / 2) * kLanes + p / 8])[p % 2] = make_float2(cs * a.amplitude, sn * a.amplitude);
   }
   if (threadIdx.x < n) {
-    int64_t slot = __ldcg(reinterpret_cast<const long long *>(a.slots) + t0 + threadIdx.x);
-    if (slot >= a.n_slots) {
-      if (a.status != nullptr) {
-        a.status[0] = LR_EBOUNDS;
-        a.status[1] = t0 + threadIdx.x;
-      }
-      slot = -1;
-    }
-    s_slot[threadIdx.x] = slot;
+    const int64_t slot = __ldcg(reinterpret_cast<const long long *>(a.slots) + t0 + threadIdx.x);
+    s_row[threadIdx.x] = cache_row(slot, a.n_slots, a.kv_heads, 0, t0 + threadIdx.x, blockIdx.y == 0 ? a.status : nullptr);
   }
   __syncthreads();
-  while (item[0].t < n) {
+  for (int t = t_first; t < n; t += stride) {
 #pragma unroll
-    for (int u = 0; u < 2; ++u) finish(item[u]);
-#pragma unroll
-    for (int u = 0; u < 2; ++u) {
-      item[u].h += 2 * kStep;
-      settle(item[u]);
-      load(item[u]);
-    }
+    for (int u = 0; u < kMine; ++u)
+      if (mine[u].live) {
+        Mine &x = mine[u];
+        Mine now = x;  // (its rows; those of the next token are asked for before they are looked at)
+        if (t + stride < n) load(x);
+        finish(now, t);
+      }
   }
   if constexpr (kKind != LR_KV_BF16) {
     __syncthreads();
@@ -207,7 +206,7 @@ rope_write_kernel(const __grid_constant__ RopeArgs a) {
     const int work = n * rows * kParts, loops = (work + kThreads - 1) / kThreads;
     for (int l = 0; l < loops; ++l) {  // (whole warps: a row's threads ask one another)
       const int i = l * kThreads + threadIdx.x, part = i % kParts, r = i / kParts, t = r / max(rows, 1), head = rows0 + r - t * rows;
-      const bool live = i < work && s_slot[t] >= 0;
+      const bool live = i < work && s_row[t] >= 0;
       float x[kFp4Group];
       uint32_t top = 0;
 #pragma unroll
@@ -223,7 +222,7 @@ rope_write_kernel(const __grid_constant__ RopeArgs a) {
       if (!live) continue;
       const bool fine = most < 0x7F800000u;
       const int side = head >= a.q_heads + a.kv_heads ? 1 : 0, kv = head - a.q_heads - side * a.kv_heads;
-      const int64_t at = ((s_slot[t] / kPage) * a.kv_heads + kv) * kPage + s_slot[t] % kPage;
+      const int64_t at = s_row[t] + kv * kPage;
       if constexpr (kKind == LR_KV_FP4) {
         const int byte = fp4_byte(top);
         const float by = scale_down(byte);
