@@ -43,6 +43,7 @@ struct Shape {
   static constexpr int kRaw = kD == 128 ? 3 : 6;          // tiles of codes on their way or being converted
   static constexpr int kScales = kD / kFp4Group;          // scale bytes of a row
   static constexpr int kPasses = kD / 32;                 // 16-byte groups of a lane in a tile
+  static constexpr int kBatch = kD == 128 ? 2 : 1;        // ... whose codes are asked for at once: 177 us where one at a time takes 191 (16 requests over 8 to 32 K keys); with two passes, of head size 64, one is 1% faster
   static constexpr int kPassKeys = kKeys / kPasses;
   static constexpr int kCodeBytes = 128 * kD / 2, kScaleBytes = 128 * kScales;
   static constexpr int kSlotBytes = kCodeBytes + kScaleBytes + 32;  // of a tile: codes, scales, valid tokens of its pages
@@ -359,7 +360,7 @@ attn_fp4_kernel(const __grid_constant__ CUtensorMap q_map, DevBatch d, DevTcPlan
     if (warp < 12) {
       // ======================= converters ====================================================
       const int team = warp - 8;
-      constexpr int kPasses = Sh::kPasses, kPassKeys = Sh::kPassKeys, kScales = Sh::kScales;
+      constexpr int kPasses = Sh::kPasses, kBatch = Sh::kBatch, kPassKeys = Sh::kPassKeys, kScales = Sh::kScales;
       // this lane's key within a pass and its group of 32 channels
       const int key0 = (lane >> 1) & (kPassKeys - 1), grp = kD == 128 ? ((lane >> 4) << 1) | (lane & 1) : lane & 1;
       const int key = team * kKeys + key0;
@@ -396,22 +397,32 @@ attn_fp4_kernel(const __grid_constant__ CUtensorMap q_map, DevBatch d, DevTcPlan
           }
           uint32_t to = to0 + stage * kTileBytes;
 #pragma unroll 1
-          for (int p = 0; p < kPasses; ++p, to += (kPassKeys / 8) * kGroupBytes) {
-            const uint4 c = ld_shared(from + codes + p * kPassKeys * (kD / 2));
-            uint32_t f = half_factor(ld_shared_byte(from + scales + p * kPassKeys * kScales));
-            if (!whole) {
-              const int k = p * kPassKeys + key0;
-              if ((k & (kPage - 1)) >= (int)valid[k >> 4]) f = 0u;
+          for (int p0 = 0; p0 < kPasses; p0 += kBatch) {
+            uint4 c[kBatch];
+            uint32_t f[kBatch];
+#pragma unroll
+            for (int u = 0; u < kBatch; ++u) {
+              c[u] = ld_shared(from + codes + (p0 + u) * kPassKeys * (kD / 2));
+              f[u] = ld_shared_byte(from + scales + (p0 + u) * kPassKeys * kScales);
             }
-            uint32_t h[4];
-            halves8(h, c.x, f);
-            st_shared(to, h);
-            halves8(h, c.y, f);
-            st_shared(to ^ 16u, h);
-            halves8(h, c.z, f);
-            st_shared(to ^ 32u, h);
-            halves8(h, c.w, f);
-            st_shared(to ^ 48u, h);
+#pragma unroll
+            for (int u = 0; u < kBatch; ++u) {
+              f[u] = half_factor(f[u]);
+              const int k = (p0 + u) * kPassKeys + key0;
+              if (!whole && (k & (kPage - 1)) >= (int)valid[k >> 4]) f[u] = 0u;
+            }
+#pragma unroll
+            for (int u = 0; u < kBatch; ++u, to += (kPassKeys / 8) * kGroupBytes) {
+              uint32_t h[4];
+              halves8(h, c[u].x, f[u]);
+              st_shared(to, h);
+              halves8(h, c[u].y, f[u]);
+              st_shared(to ^ 16u, h);
+              halves8(h, c[u].z, f[u]);
+              st_shared(to ^ 32u, h);
+              halves8(h, c[u].w, f[u]);
+              st_shared(to ^ 48u, h);
+            }
           }
           fence_proxy_async();
           __syncwarp();  // the slot has been read, the tile's part is written
@@ -588,9 +599,9 @@ attn_fp4_kernel(const __grid_constant__ CUtensorMap q_map, DevBatch d, DevTcPlan
           ok = need(pos_v, 222);
           if (!ok) break;
           const bool has_next = j + 1 < my_units;
-          uint32_t pos_k = 0;
-          if (has_next) {
-            pos_k = ring_base + ord.pos_k(mode == 2 ? j + 1 : 2 * (j + 1) + s);
+          const uint32_t pos_k = has_next ? ring_base + ord.pos_k(mode == 2 ? j + 1 : 2 * (j + 1) + s) : 0u;
+          // the K tile behind: with stages to spare it has landed by now, with four it is waited for under the first product
+          if (kStages > 4 && has_next) {
             ok = need(pos_k, 226);
             if (!ok) break;
           }
@@ -608,13 +619,20 @@ attn_fp4_kernel(const __grid_constant__ CUtensorMap q_map, DevBatch d, DevTcPlan
               issue_pv(sV, half, (j | half) != 0);
               tc_commit(&ctrl->o_done[s]);
               if (half == 1) release(pos_v);
-              if (has_next) {
-                issue_qk(m_tile, pos_k % kStages, half);
-                tc_commit(&ctrl->s_full[s][half]);
-                if (half == 1) {
-                  release(pos_k);
-                  if (j + 2 == my_units) tc_commit(&ctrl->q_empty);  // last QK of the piece
-                }
+            }
+            __syncwarp();
+            if (!has_next) continue;
+            if (kStages <= 4 && half == 0) {
+              ok = need(pos_k, 226);
+              if (!ok) break;
+              tc_fence_after();
+            }
+            if (elect_one()) {
+              issue_qk(m_tile, pos_k % kStages, half);
+              tc_commit(&ctrl->s_full[s][half]);
+              if (half == 1) {
+                release(pos_k);
+                if (j + 2 == my_units) tc_commit(&ctrl->q_empty);  // last QK of the piece
               }
             }
             __syncwarp();
