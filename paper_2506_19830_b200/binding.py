@@ -585,6 +585,8 @@ class Context:
         """Turns the queries q [tokens, q heads, head size] into q_out and the keys k into the cache's slots, V beside them: rows of a joint projection, as
         ``lr_fp8_write`` takes them.  positions: int32 [tokens].  cache: a ``Bf16Cache``, ``Fp8Cache`` or ``Fp4Cache``.  Without rope nothing is turned."""
         n, k_stride, v_stride = _cache_rows(self, cache, k, v, slots, status)
+        if rope is not None and rope.handle is None:
+            raise ValueError("lr_rope_write: the rope is closed")
         q_stride = _check_rope(self, n, positions, q, q_out, rope is not None)
         _check(lib().lr_rope_write(self.handle, None if rope is None else rope.handle, cache.any, _ptr(positions), _ptr(q), q_stride, _ptr(q_out),
                                    k.data_ptr(), k_stride, v.data_ptr(), v_stride, slots.data_ptr(), n, _ptr(status), _stream_on(self.device, stream)),

@@ -190,3 +190,51 @@ def test_waits_for_rows_gone_through_again_do_not_run_out():
     check_attention(out, lse, o_ref, l_ref, rows, REL_LARGE)
     plan.close()
     ctx.close()
+
+
+@pytest.mark.parametrize("path", PATHS)
+@pytest.mark.parametrize("q", [1, 9])
+@pytest.mark.parametrize("extra", [1, 200])
+def test_rows_behind_the_last_branch_are_neither_read_nor_written(extra, q, path):
+    w = chain([300, 77], 128, q=q, seed=60)
+    b = w.batch
+    pools, k, v = stored(w)
+    ctx = B.Context(b.model, 0)
+    plan = B.Plan(ctx, b)
+    plan.lr_plan_set_attention_path(path)
+    n = w.tensors.q.shape[0]
+    rows = R.bf16_tensor(w.tensors.q, DEV)
+    padded = torch.full((n + extra, *rows.shape[1:]), float("nan"), dtype=torch.bfloat16, device=DEV)
+    padded[:n] = rows
+    out, lse = torch.full_like(padded, -7.0), torch.full(padded.shape[:2], -7.0, device=DEV)
+    plan.lr_verify_attention_fp4(padded, on_device(pools), out, lse)
+    assert plan.lr_poll_status() == 0
+    assert bool((out[n:] == -7.0).all()) and bool((lse[n:] == -7.0).all())
+    check_attention(out[:n], lse[:n], *O.verify_attention(b, w.tensors.q, k, v), None, REL_LARGE)
+    plan.close()
+    ctx.close()
+
+
+@pytest.mark.parametrize("q", [1, 20])
+def test_a_first_call_that_is_captured(q):
+    w = chain([900, 170], 128, q=q, seed=61)
+    b = w.batch
+    pools, k, v = stored(w)
+    ctx = B.Context(b.model, 0)
+    plan = B.Plan(ctx, b)
+    plan.lr_plan_set_attention_path(B.PATH_TENSOR_CORE)
+    rows, cache = R.bf16_tensor(w.tensors.q, DEV), on_device(pools)
+    out, lse = torch.zeros_like(rows), torch.zeros(rows.shape[:2], device=DEV)
+    torch.cuda.synchronize()
+    s, g = torch.cuda.Stream(), torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g, stream=s):
+        plan.lr_verify_attention_fp4(rows, cache, out, lse, 0.0, s)
+    for _ in range(2):
+        out.zero_()
+        g.replay()
+        torch.cuda.synchronize()
+        assert plan.lr_poll_status() == 0
+        check_attention(out, lse, *O.verify_attention(b, w.tensors.q, k, v), None, REL_LARGE)
+    del g
+    plan.close()
+    ctx.close()

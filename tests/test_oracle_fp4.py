@@ -234,3 +234,13 @@ def test_rope_takes_tensors_for_what_they_are():
                  (at, q[:4], out), (at, joint[:, ::2], out), (at, q.transpose(1, 2), out), (at, q, out.half()), (at, q, out[:4]), (at, q, joint[:, :4])):
         with pytest.raises(ValueError, match="lr_rope_write"):
             B._check_rope(ctx, 5, *args, True)
+
+
+def test_a_closed_rope_does_not_leave_rows_as_they_are():
+    cache = B.Fp4Cache.empty(Model(4, 2, 64, 8), 3, "cpu")
+    ctx = SimpleNamespace(model=Model(4, 2, 64, 8), device=-1, cache_kind=cache.kind, handle=None)
+    rows, slots, at = torch.zeros((2, 2, 64), dtype=torch.bfloat16), torch.arange(2), torch.zeros(2, dtype=torch.int32)
+    rope = B.Rope(64)
+    rope.close()
+    with pytest.raises(ValueError, match="closed"):
+        B.Context.lr_rope_write(ctx, rope, at, cache, rows, rows, slots)
