@@ -540,11 +540,15 @@ int lr_fp4_read(lr_ctx *ctx, const lr_fp4_cache *cache, const int64_t *slots_d, 
 /*
  * lr_verify_attention on such a cache (cache->n_pages >= the plan's n_pool_pages, else
  * LR_EINVAL): same plan, queries, outputs and errors, for a chain or a tree of draft
- * steps.  Q, and K and V as the values they stand for, enter the products as bf16, which
- * they are; numbers of K and V below 2^-117 count as 0.  Products are summed and the
- * softmax is done in fp32; its weights enter the second product as bf16.  Slots that hold
- * no token of the plan may hold anything.  A row of K or V that stands for NaN makes
- * output and log-sum of a query that sees it NaN and does not touch the others.
+ * steps.  On the tensor cores Q (a row times a power of two), K, V and the softmax weights
+ * are half-precision numbers; products are summed in fp32, as the softmax is.  Q, K and V
+ * are exact where scales are 2^-23 .. 2^13 (numbers from 2^-24 to 49,152) and a row of Q
+ * has no channel but 0 below 2^-31 of its largest; numbers of K and V with a scale below
+ * 2^-116 count as 0.  What lies outside of that is worked out again on the CUDA cores in
+ * the same call: the same results, some hundred times slower.  A weight is off by 2^-12
+ * of itself at most, or by 2^-27 of the row's sum of weights where that is more.  Slots
+ * that hold no token of the plan may hold anything.  A row of K or V that stands for NaN
+ * makes output and log-sum of a query that sees it NaN and does not touch the others.
  * lr_plan_set_attention_path: 0 automatic, 1 CUDA cores, 2 tensor cores; there is no
  * CTA-pair kernel for this cache (3: LR_EUNSUPPORTED).
  */

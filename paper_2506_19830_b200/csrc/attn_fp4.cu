@@ -1,7 +1,7 @@
 // Tensor-core nested-prefix attention over the 4-bit cache (head_dim 64 or 128).
 //
 // The plan, the two streams of a CTA, the ring of tiles and what the issuers and the softmax threads do are those of attn_tc.cu.  What is different is how K and V get
-// into the ring: four warps bring their codes and scales from the cache and leave them there as bf16.
+// into the ring: one warp brings codes and scales from the cache, four turn them into halves and store those as the operands.
 //
 // Numbers.  Q, K, V and the weights are halves (attn_fp4.cuh): a code and its scale are one exactly, two instructions for a pair of codes, where bf16 takes twice as many and the
 // converters, one warp to a scheduler, are what a tile waits for.  A row of Q is scaled by a power of two, which the softmax takes out again; eight channels of K
