@@ -1204,8 +1204,7 @@ extern "C" int lr_rope_create(lr_rope **out, const lr_rope_spec *spec) {
     r->radians[i] = s.scaling == LR_ROPE_PLAIN ? f : f * (1.0 - w) + f / s.factor * w;
     r->turns[i] = r->radians[i] / kTurn;
   }
-  r->amplitude_64 = s.amplitude != 0.0 ? s.amplitude : s.scaling == LR_ROPE_PARTS ? 0.1 * log(s.factor) + 1.0 : 1.0;
-  r->amplitude = (float)r->amplitude_64;
+  r->amplitude = s.amplitude != 0.0 ? s.amplitude : s.scaling == LR_ROPE_PARTS ? 0.1 * log(s.factor) + 1.0 : 1.0;
   *out = r;
   return LR_OK;
 }
@@ -1225,7 +1224,7 @@ extern "C" int lr_rope_frequencies(const lr_rope *rope, double *radians, double 
     return LR_EINVAL;
   }
   if (radians) std::copy(rope->radians, rope->radians + rope->rot_dim / 2, radians);
-  if (amplitude) *amplitude = rope->amplitude_64;
+  if (amplitude) *amplitude = rope->amplitude;
   return LR_OK;
 }
 

@@ -180,10 +180,9 @@ struct lr_ctx {
 
 struct lr_rope {
   int32_t rot_dim, interleaved;
-  float amplitude;
   double radians[LR_ROPE_MAX_DIM / 2];  // a position
   double turns[LR_ROPE_MAX_DIM / 2];
-  double amplitude_64;
+  double amplitude;
 };
 
 struct lr_plan {

@@ -1,13 +1,15 @@
 // Rotary positions between a joint projection and attention: queries turned, keys turned and written with their values into a cache.
 //
-// A CTA takes the heads of a few tokens.  It first works out their angles: a position times a frequency in turns, in 64 bits, of which the whole turns are dropped; what is
-// left, half a turn at most, is exact to 2^-53 of the angle however far the position, and goes to sinpi and cospi in fp32.  All heads of a token share them through shared memory.
+// A CTA takes the heads of a few tokens.  It first works out their angles: a position times a frequency in turns, in 64 bits, of which the whole quarters are dropped; what is
+// left, an eighth of a turn at most, is exact to 2^-53 of the angle however far the position.  Its sine and cosine are Taylor series in 64 bits, times the amplitude, rounded once: with sinpi
+// and cospi in fp32 twice as many codes of an 8-bit cache came out one off.  All heads of a token share them through shared memory.
 // A thread then has 8 pairs of a head, both channels of each, so that rows may be turned where they are.  With the channels of a pair half a turned
-// part apart these are 8 channels in each half, else 16 side by side: two 16-byte loads and stores; where the halves do not start on 16 bytes
-// (rot_dim no multiple of 16) channel by channel.  For a cache in 8 or 4 bits the turned keys and the values wait in shared memory in fp32, and threads of 32 channels of a
+// part apart these are 8 channels in each half, else 16 side by side: two 16-byte loads and stores.  Where the halves do not start on 16 bytes (rot_dim no multiple of 16) a thread brings
+// 16 channels side by side and the threads of a head find their pairs in shared memory (channel by channel from memory a prompt of 32 K tokens, 90 of 128 channels turned, took 1172 us; now 201).
+// For a cache in 8 or 4 bits the turned keys and the values wait in shared memory in fp32, and threads of 32 channels of a
 // row quantise them: one rounding from what was turned.
 //
-// Bound by HBM on prompts, by the launch and the chain position -> angle -> data on a pass's drafts.
+// Bound by HBM on prompts (32 K tokens of 40 + 8 + 8 heads of 128: 165 us, 940 MB at 5.7 TB/s), by the launch and the chain position -> angle -> data on a pass's drafts.
 #include <math.h>
 
 #include <algorithm>
@@ -20,13 +22,13 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr int kHeads = 64;       // of q, k and v together, a CTA's share of a token
-constexpr int kMaxTokens = 8;    // ... and how many tokens it takes
-constexpr int kRowBytes = 40 << 10;  // of shared memory for rows that are to be quantised
+constexpr int kMaxTokens = 8;    // ... and how many tokens it takes; half as many where heads wait in shared memory
+constexpr int kRowBytes = 36 << 10;  // of shared memory for rows that are to be quantised
 constexpr int kPadded = kFp4Group + 4;  // floats that 32 channels take there: threads next to each other, a group each, read different banks
 
 struct RopeArgs {
   double turns[LR_ROPE_MAX_DIM / 2];
-  float amplitude;
+  double amplitude;
   int32_t pairs, interleaved;  // pairs that are turned
   int32_t q_heads, kv_heads, q0;  // q0: 0, or q_heads where there are no queries: the first head of the row [q | k | v] that is looked at
   const int32_t *positions;
@@ -46,17 +48,29 @@ __device__ __forceinline__ uint32_t bf16_pair(float a, float b) {
   memcpy(&u, &t, 4);
   return u;
 }
+// Cosine and sine of an angle in turns, times an amplitude.  The series of |x| <= pi / 4 end at x^10 and x^11: 2^-31 off at the most.
+__device__ __forceinline__ float2 cos_sin(double turns, double amplitude) {
+  const double fours = 4.0 * turns, whole = rint(fours), x = (fours - whole) * 1.5707963267948966, y = x * x;
+  const double c = 1.0 + y * (-1.0 / 2 + y * (1.0 / 24 + y * (-1.0 / 720 + y * (1.0 / 40320 + y * (-1.0 / 3628800)))));
+  const double s = x * (1.0 + y * (-1.0 / 6 + y * (1.0 / 120 + y * (-1.0 / 5040 + y * (1.0 / 362880 + y * (-1.0 / 39916800))))));
+  const float cs = (float)(c * amplitude), sn = (float)(s * amplitude);
+  const int quarters = (int)whole;  // below 2^31: a frequency is one radian a position at the most
+  const float a = (quarters & 1) != 0 ? -sn : cs, b = (quarters & 1) != 0 ? cs : sn;
+  return (quarters & 2) != 0 ? make_float2(-a, -b) : make_float2(a, b);
+}
 __device__ __forceinline__ float low(uint32_t w) { return __uint_as_float(w << 16); }
 __device__ __forceinline__ float high(uint32_t w) { return __uint_as_float(w & 0xFFFF0000u); }
 
 // kKind: of the cache.  kVector: the pairs of every thread start on 16 bytes.
 template <int kD, int kKind, bool kVector>
-__global__ void __launch_bounds__(kThreads, 4)  // (three of them without being asked: a prompt of 32 K tokens 161 us instead of 167)
+__global__ void __launch_bounds__(kThreads, 4)  // (three of them without being asked: 4 % more for a prompt of 32 K tokens)
 rope_write_kernel(const __grid_constant__ RopeArgs a) {
   constexpr int kLanes = kD / 16;  // threads a head
   constexpr int kRow = kD / kFp4Group * kPadded;
   extern __shared__ __align__(16) float s_rows[];  // [token][K or V row of this CTA][kRow], of a cache in 8 or 4 bits
-  __shared__ float4 s_turn[kMaxTokens][4 * kLanes];  // [pairs 2i, 2i + 1 of a part][part]: cosine and sine of either
+  constexpr int kTokens = kVector ? kMaxTokens : kMaxTokens / 2;
+  __shared__ float4 s_turn[kTokens][4 * kLanes];  // [pairs 2i, 2i + 1 of a part][part]: cosine and sine of either; if not kVector of pair after pair
+  __shared__ __align__(16) uint16_t s_head[kVector ? 1 : kThreads / kLanes][kD + 8];  // of heads whose pairs do not start on 16 bytes; the four of a warp in different banks
   __shared__ int64_t s_row[kMaxTokens];  // of the token's first head in the pools; -1: none
   asm volatile("griddepcontrol.wait;" ::: "memory");  // the projection may be the kernel launched just before
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
@@ -82,7 +96,7 @@ rope_write_kernel(const __grid_constant__ RopeArgs a) {
     x.is_q = head < a.q_heads;
     x.is_v = head >= a.q_heads + a.kv_heads;
     x.turned = !x.is_v && p0 < a.pairs;
-    x.apart = x.turned && a.interleaved == 0;
+    x.apart = kVector && x.turned && a.interleaved == 0;
     const int kv = x.is_v ? head - a.q_heads - a.kv_heads : head - a.q_heads;
     const int64_t step = x.is_q ? a.q_stride : x.is_v ? a.v_stride : a.k_stride;
     x.src = (x.is_q ? a.q : x.is_v ? a.v : a.k) + (t0 + t_first) * step + (x.is_q ? head : kv) * kD;
@@ -92,17 +106,9 @@ rope_write_kernel(const __grid_constant__ RopeArgs a) {
   }
   // channels of the 8 pairs: c and d and the seven behind them where the halves of what is turned lie apart, else the 16 from c on
   auto load = [&](Mine &x) {
-    if constexpr (kVector) {
-      const int c = x.apart ? p0 : 2 * p0, d = x.apart ? p0 + a.pairs : c + 8;
-      const uint4 u = __ldcg(reinterpret_cast<const uint4 *>(x.src + c)), w = __ldcg(reinterpret_cast<const uint4 *>(x.src + d));
-      x.r[0] = u.x, x.r[1] = u.y, x.r[2] = u.z, x.r[3] = u.w, x.r[4] = w.x, x.r[5] = w.y, x.r[6] = w.z, x.r[7] = w.w;
-    } else {
-#pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        const bool far = x.apart && p0 + j < a.pairs;
-        x.r[j] = (uint32_t)__ldcg(x.src + (far ? p0 + j : 2 * (p0 + j))) | (uint32_t)__ldcg(x.src + (far ? p0 + j + a.pairs : 2 * (p0 + j) + 1)) << 16;
-      }
-    }
+    const int c = x.apart ? p0 : 2 * p0, d = x.apart ? p0 + a.pairs : c + 8;
+    const uint4 u = __ldcg(reinterpret_cast<const uint4 *>(x.src + c)), w = __ldcg(reinterpret_cast<const uint4 *>(x.src + d));
+    x.r[0] = u.x, x.r[1] = u.y, x.r[2] = u.z, x.r[3] = u.w, x.r[4] = w.x, x.r[5] = w.y, x.r[6] = w.z, x.r[7] = w.w;
     x.src += x.src_step;
   };
   auto finish = [&](Mine &it, int t) {
@@ -111,14 +117,17 @@ rope_write_kernel(const __grid_constant__ RopeArgs a) {
     const int c = it.apart ? p0 : 2 * p0, d = it.apart ? p0 + a.pairs : c + 8;
     float x[8], y[8];
     uint32_t (&r)[8] = it.r;  // as they lie; what is not turned is not touched (a NaN keeps its bits)
-    if (kVector && it.apart) {
+    const bool as_bf16 = kKind == LR_KV_BF16 || it.is_q;
+    auto at = [](int ch) { return ch / kFp4Group * kPadded + ch % kFp4Group; };
+    float *const row = as_bf16 ? nullptr : s_rows + (t * rows + it.row) * kRow;
+    if (it.apart) {
 #pragma unroll
       for (int j = 0; j < 4; ++j) x[2 * j] = low(r[j]), x[2 * j + 1] = high(r[j]), y[2 * j] = low(r[4 + j]), y[2 * j + 1] = high(r[4 + j]);
     } else {
 #pragma unroll
       for (int j = 0; j < 8; ++j) x[j] = low(r[j]), y[j] = high(r[j]);
     }
-    if (it.turned) {
+    if (kVector && it.turned) {
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         const float4 e2 = s_turn[t][i * kLanes + part];  // of two pairs
@@ -129,61 +138,67 @@ rope_write_kernel(const __grid_constant__ RopeArgs a) {
           if (p0 + j < a.pairs) {
             x[j] = to;
             y[j] = other;
-            if (!kVector || !it.apart) r[j] = bf16_pair(to, other);
+            if (!it.apart) r[j] = bf16_pair(to, other);
           }
         }
       }
-      if (kVector && it.apart) {  // all of them are turned
+      if (it.apart) {  // all of them are turned
 #pragma unroll
         for (int j = 0; j < 4; ++j) r[j] = bf16_pair(x[2 * j], x[2 * j + 1]), r[4 + j] = bf16_pair(y[2 * j], y[2 * j + 1]);
       }
     }
-    if (kKind == LR_KV_BF16 || it.is_q) {
+    // the pairs of a head whose halves lie anywhere, by its threads: pair after pair from where the head waits
+    const unsigned of_head = ((1u << kLanes) - 1u) << (threadIdx.x % 32 / kLanes * kLanes);
+    auto turn_all = [&](auto get, auto set) {
+      __syncwarp(of_head);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const int i = part + j * kLanes;
+        if (i < a.pairs) {
+          const float2 e = reinterpret_cast<const float2 *>(s_turn[t])[i];
+          const float xi = get(i), yi = get(i + a.pairs);
+          set(i, xi * e.x - yi * e.y);
+          set(i + a.pairs, fmaf(xi, e.y, yi * e.x));
+        }
+      }
+      __syncwarp(of_head);
+    };
+    if (as_bf16) {
+      if (!kVector && !it.is_v) {
+        uint16_t *const head = s_head[kVector ? 0 : seat];
+        uint4 *const own = reinterpret_cast<uint4 *>(head + c);
+        own[0] = make_uint4(r[0], r[1], r[2], r[3]);
+        own[1] = make_uint4(r[4], r[5], r[6], r[7]);
+        turn_all([&](int ch) { return low(head[ch]); }, [&](int ch, float to) { head[ch] = (uint16_t)bf16_pair(to, to); });
+        const uint4 u = own[0], w = own[1];
+        r[0] = u.x, r[1] = u.y, r[2] = u.z, r[3] = u.w, r[4] = w.x, r[5] = w.y, r[6] = w.z, r[7] = w.w;
+      }
       uint16_t *dst = it.is_q ? a.q_out + (int64_t)(t0 + t) * a.q_heads * kD + it.off : reinterpret_cast<uint16_t *>(a.pool[it.is_v ? 1 : 0]) + (at_row + it.off) * kD;
-      if constexpr (kVector) {
-        *reinterpret_cast<uint4 *>(dst + c) = make_uint4(r[0], r[1], r[2], r[3]);
-        *reinterpret_cast<uint4 *>(dst + d) = make_uint4(r[4], r[5], r[6], r[7]);
-      } else {
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          const bool far = it.apart && p0 + j < a.pairs;
-          dst[far ? p0 + j : 2 * (p0 + j)] = (uint16_t)r[j];
-          dst[far ? p0 + j + a.pairs : 2 * (p0 + j) + 1] = (uint16_t)(r[j] >> 16);
-        }
-      }
+      *reinterpret_cast<uint4 *>(dst + c) = make_uint4(r[0], r[1], r[2], r[3]);
+      *reinterpret_cast<uint4 *>(dst + d) = make_uint4(r[4], r[5], r[6], r[7]);
     } else {
-      float *row = s_rows + (t * rows + it.row) * kRow;
-      auto at = [](int ch) { return ch / kFp4Group * kPadded + ch % kFp4Group; };
-      if constexpr (kVector) {
-        float4 *to_c = reinterpret_cast<float4 *>(row + at(c)), *to_d = reinterpret_cast<float4 *>(row + at(d));
-        if (it.apart) {
-          to_c[0] = make_float4(x[0], x[1], x[2], x[3]), to_c[1] = make_float4(x[4], x[5], x[6], x[7]);
-          to_d[0] = make_float4(y[0], y[1], y[2], y[3]), to_d[1] = make_float4(y[4], y[5], y[6], y[7]);
-        } else {
-          to_c[0] = make_float4(x[0], y[0], x[1], y[1]), to_c[1] = make_float4(x[2], y[2], x[3], y[3]);
-          to_d[0] = make_float4(x[4], y[4], x[5], y[5]), to_d[1] = make_float4(x[6], y[6], x[7], y[7]);
-        }
+      float4 *to_c = reinterpret_cast<float4 *>(row + at(c)), *to_d = reinterpret_cast<float4 *>(row + at(d));
+      if (it.apart) {
+        to_c[0] = make_float4(x[0], x[1], x[2], x[3]), to_c[1] = make_float4(x[4], x[5], x[6], x[7]);
+        to_d[0] = make_float4(y[0], y[1], y[2], y[3]), to_d[1] = make_float4(y[4], y[5], y[6], y[7]);
       } else {
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          const bool far = it.apart && p0 + j < a.pairs;
-          row[at(far ? p0 + j : 2 * (p0 + j))] = x[j];
-          row[at(far ? p0 + j + a.pairs : 2 * (p0 + j) + 1)] = y[j];
-        }
+        to_c[0] = make_float4(x[0], y[0], x[1], y[1]), to_c[1] = make_float4(x[2], y[2], x[3], y[3]);
+        to_d[0] = make_float4(x[4], y[4], x[5], y[5]), to_d[1] = make_float4(x[6], y[6], x[7], y[7]);
       }
+      if (!kVector && !it.is_v) turn_all([&](int ch) { return row[at(ch)]; }, [&](int ch, float to) { row[at(ch)] = to; });
     }
   };
   // the first token's rows are on their way while the angles are worked out
 #pragma unroll
   for (int u = 0; u < kMine; ++u)
     if (mine[u].live && t_first < n) load(mine[u]);
+#pragma unroll 1
   for (int i = threadIdx.x; i < n * a.pairs; i += kThreads) {
     const int t = i / a.pairs, p = i - t * a.pairs;
-    const double turns = (double)__ldcg(a.positions + t0 + t) * a.turns[p];
-    float sn, cs;
-    sincospif(2.0f * (float)(turns - rint(turns)), &sn, &cs);
+    const float2 e = cos_sin((double)__ldcg(a.positions + t0 + t) * a.turns[p], a.amplitude);
     // two neighbouring pairs of every part side by side: a thread takes them at once, and its neighbours' lie behind
-    reinterpret_cast<float2 *>(&s_turn[t][(p % 8 / 2) * kLanes + p / 8])[p % 2] = make_float2(cs * a.amplitude, sn * a.amplitude);
+    if constexpr (kVector) reinterpret_cast<float2 *>(&s_turn[t][(p % 8 / 2) * kLanes + p / 8])[p % 2] = e;
+    else reinterpret_cast<float2 *>(s_turn[t])[p] = e;
   }
   if (threadIdx.x < n) {
     const int64_t slot = __ldcg(reinterpret_cast<const long long *>(a.slots) + t0 + threadIdx.x);
@@ -283,16 +298,16 @@ int launch_rope_write(lr_ctx *ctx, const lr_rope *rope, const lr_kv_cache &c, co
   const int heads = m.n_q_heads + 2 * m.n_kv_heads - a.q0, share = std::min(heads, kHeads), chunks = (heads + kHeads - 1) / kHeads;
   const int rows = c.kind == LR_KV_BF16 ? 0 : std::min(share, 2 * m.n_kv_heads);
   const int row_bytes = rows * (m.head_dim / kFp4Group) * kPadded * 4;  // of a token
+  const bool vector = a.interleaved != 0 || a.pairs % 8 == 0;
+  const int most = vector ? kMaxTokens : kMaxTokens / 2;
   a.tokens = 1;
-  while (2 * a.tokens <= kMaxTokens && w.n_tokens / (2 * a.tokens) * (int64_t)chunks >= 8 * ctx->sm_count && 2 * a.tokens * row_bytes <= kRowBytes)
-    a.tokens *= 2;
+  while (2 * a.tokens <= most && w.n_tokens / (2 * a.tokens) * (int64_t)chunks >= 8 * ctx->sm_count && 2 * a.tokens * row_bytes <= kRowBytes) a.tokens *= 2;
   const size_t smem = (size_t)a.tokens * row_bytes;
   const dim3 grid((unsigned)((w.n_tokens + a.tokens - 1) / a.tokens), (unsigned)chunks);
   if (chunks > 65535) {
     set_error("lr_rope_write: too many heads");
     return LR_EUNSUPPORTED;
   }
-  const bool vector = a.interleaved != 0 || a.pairs % 8 == 0;
   ctx->launches++;
   if (m.head_dim == 128) {
     if (c.kind == LR_KV_BF16) return launch<128, LR_KV_BF16>(a, vector, grid, smem, s);
