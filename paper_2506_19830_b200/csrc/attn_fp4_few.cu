@@ -74,6 +74,8 @@ attn_fp4_few_kernel(DevBatch d, DevTcPlan tc, const __grid_constant__ Fp4Call in
   constexpr int kWarps = Sh::kWarps, kThreads = Sh::kThreads, kRows = Sh::kRows, kStride = Sh::kStride, kKWords = kD / 32, kVWords = kD / 64, kMTiles = kD / 16;
   extern __shared__ __align__(16) float s_sum[];  // [warp][query][kStride], then the warps' stages
   __shared__ float2 s_ml[kWarps][kRows];
+  __shared__ __align__(16) uint16_t s_q[kRows][kD + 8];  // a piece's queries as halves
+  __shared__ int4 s_info[kRows];  // what they see (RowInfo), and what a score is worth, negative for one with a channel too small beside its largest to be a half
   __shared__ TcPiece s_piece[kHeld];
   __shared__ TcReq s_req[kHeld];
   __shared__ int s_odd;  // 1 + the last piece that has a scale beyond halves
@@ -155,55 +157,72 @@ attn_fp4_few_kernel(DevBatch d, DevTcPlan tc, const __grid_constant__ Fp4Call in
   };
 
   const int G = d.group;
+  // The queries of a piece: eight channels a lane, some rows a warp, asked for while the piece before is joined and left in shared memory for all warps.
+  constexpr int kRowLanes = kD / 8;
+  const int q_row = warp * (32 / kRowLanes) + lane / kRowLanes, q_part = lane % kRowLanes;
+  uint4 q_raw = make_uint4(0, 0, 0, 0);
+  RowInfo q_info;
+  auto ask_queries = [&](int pc) {
+    if (q_row >= kRows || pc >= piece1) return;  // (whole warps)
+    const TcPiece pi = piece_of(pc);
+    const TcReq rq = req_of(pc, pi);
+    q_raw = make_uint4(0, 0, 0, 0);
+    if (q_row < rq.n_q * G)
+      q_raw = __ldcg(reinterpret_cast<const uint4 *>(in.q + ((int64_t)(rq.q_row0 + q_row / G) * d.n_q_heads + pi.kv_head * G + q_row % G) * kD) + q_part);
+    q_info = row_info(d, tc, rq, tc.tokens_per_mtile, pi.mtile0, q_row, pi.kv_head);
+  };
+  auto leave_queries = [&](int pc) {
+    if (q_row >= kRows || pc >= piece1) return;
+    const uint32_t m = 0x7FFF7FFFu, two = __vmaxu2(__vmaxu2(q_raw.x & m, q_raw.y & m), __vmaxu2(q_raw.z & m, q_raw.w & m));
+    uint32_t top = max(two & 0xFFFFu, two >> 16);
+#pragma unroll
+    for (int y = 1; y < kRowLanes; y <<= 1) top = max(top, __shfl_xor_sync(0xFFFFFFFFu, top, y));
+    const int e = min(half_exponent(top), (int)kQMostExponent);
+    const float by = __uint_as_float((uint32_t)(127 + e) << 23);
+    const uint4 p = as_halves8(q_raw);
+    const uint32_t w[4] = {p.x, p.y, p.z, p.w};
+    uint32_t h[4];
+    bool odd = false;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const float lo = bits_f(w[j] << 16) * by, hi = bits_f(w[j] & 0xFFFF0000u) * by;
+      odd = odd || (lo != 0.f && fabsf(lo) < 0x1p-17f) || (hi != 0.f && fabsf(hi) < 0x1p-17f);
+      h[j] = pack_f16(lo, hi);
+    }
+    const unsigned any = __ballot_sync(0xFFFFFFFFu, odd && top < 0x7F80u) >> (lane - q_part) & ((1u << kRowLanes) - 1u);
+    *reinterpret_cast<uint4 *>(&s_q[q_row][q_part * 8]) = make_uint4(h[0], h[1], h[2], h[3]);
+    const float unit = in.scale_log2 * (top < 0x7F80u ? __uint_as_float((uint32_t)(127 - e) << 23) : __uint_as_float(0x7FC00000u));
+    if (q_part == 0) s_info[q_row] = make_int4(q_info.depth, q_info.branch, q_info.limit, __float_as_int(any != 0u ? -unit : unit));
+  };
   ask_entry();
+  ask_queries(piece0);
 #pragma unroll 1
   for (int i = 0; i + 1 < Sh::kStages; ++i) ask_page();
+  leave_queries(piece0);
+  __syncthreads();
   uint32_t from = 0;  // stage
   for (int pc = piece0; pc < piece1; ++pc) {
     const TcPiece pi = piece_of(pc);
     const TcReq rq = req_of(pc, pi);
     const int rows = min(rq.n_q * G, kRows), n_pages = min(pi.tile_end * kPagesPerTile, rq.n_pages) - pi.tile_begin * kPagesPerTile;
-    uint32_t qf[kNB][kD / 8], again = 0;  // again: rows with a channel too small beside their largest to be a half
+    uint32_t qf[kNB][kD / 8];
     float sc[kNB][2];
     int depth[kNB][2], branch[kNB][2], limit[kNB][2];  // of this lane's columns, queries 2t and 2t + 1
 #pragma unroll
     for (int b = 0; b < kNB; ++b) {
-      const int r = b * 8 + g;  // this lane's query of the operand
-      uint4 x[kD / 32];
-      uint32_t top = 0;
 #pragma unroll
       for (int i = 0; i < kD / 32; ++i) {
-        x[i] = make_uint4(0, 0, 0, 0);
-        if (r < rows)
-          x[i] = __ldcg(reinterpret_cast<const uint4 *>(in.q + ((int64_t)(rq.q_row0 + r / G) * d.n_q_heads + pi.kv_head * G + r % G) * kD + t * (kD / 4)) + i);
-        const uint32_t m = 0x7FFF7FFFu, two = __vmaxu2(__vmaxu2(x[i].x & m, x[i].y & m), __vmaxu2(x[i].z & m, x[i].w & m));
-        top = max(top, max(two & 0xFFFFu, two >> 16));
+        const uint4 x = *reinterpret_cast<const uint4 *>(&s_q[b * 8 + g][t * (kD / 4) + i * 8]);
+        qf[b][4 * i] = x.x, qf[b][4 * i + 1] = x.y, qf[b][4 * i + 2] = x.z, qf[b][4 * i + 3] = x.w;
       }
-#pragma unroll
-      for (int y = 1; y < 4; y <<= 1) top = max(top, __shfl_xor_sync(0xFFFFFFFFu, top, y));
-      const int e = min(half_exponent(top), (int)kQMostExponent);
-      const float by = __uint_as_float((uint32_t)(127 + e) << 23);
-      bool odd = false;
-#pragma unroll
-      for (int i = 0; i < kD / 32; ++i) {
-        const uint4 p = as_halves8(x[i]);
-        const uint32_t w[4] = {p.x, p.y, p.z, p.w};
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          const float lo = bits_f(w[j] << 16) * by, hi = bits_f(w[j] & 0xFFFF0000u) * by;
-          odd = odd || (lo != 0.f && fabsf(lo) < 0x1p-17f) || (hi != 0.f && fabsf(hi) < 0x1p-17f);
-          qf[b][4 * i + j] = pack_f16(lo, hi);
-        }
-      }
-      again |= __reduce_or_sync(0xFFFFFFFFu, odd && top < 0x7F80u ? 1u << r : 0u);
-      const float unit = in.scale_log2 * (top < 0x7F80u ? __uint_as_float((uint32_t)(127 - e) << 23) : __uint_as_float(0x7FC00000u));
 #pragma unroll
       for (int y = 0; y < 2; ++y) {
-        sc[b][y] = __shfl_sync(0xFFFFFFFFu, unit, (2 * t + y) * 4);
-        const RowInfo ri = row_info(d, tc, rq, tc.tokens_per_mtile, pi.mtile0, b * 8 + 2 * t + y, pi.kv_head);
-        depth[b][y] = ri.depth, branch[b][y] = ri.branch, limit[b][y] = ri.limit;
+        const int4 x = s_info[b * 8 + 2 * t + y];
+        depth[b][y] = x.x, branch[b][y] = x.y, limit[b][y] = x.z, sc[b][y] = fabsf(__int_as_float(x.w));
       }
     }
+    // rows with a channel too small beside their largest to be a half
+    unsigned again = __ballot_sync(0xFFFFFFFFu, lane < kRows && s_info[lane % kRows].w < 0);
     float o[kNB][kMTiles][4], ref[kNB][2], l[kNB][2];
 #pragma unroll
     for (int b = 0; b < kNB; ++b) {
@@ -323,6 +342,7 @@ attn_fp4_few_kernel(DevBatch d, DevTcPlan tc, const __grid_constant__ Fp4Call in
       }
     }
     // the warps' sums, joined
+    ask_queries(pc + 1);
 #pragma unroll
     for (int b = 0; b < kNB; ++b) {
 #pragma unroll
@@ -370,7 +390,8 @@ attn_fp4_few_kernel(DevBatch d, DevTcPlan tc, const __grid_constant__ Fp4Call in
     }
     for (int r = warp; r < rows; r += kWarps)
       if ((again >> r) & 1u) exact_row<kD>(in, pc, 0, r, nullptr);
-    __syncthreads();  // the sums have been read
+    leave_queries(pc + 1);
+    __syncthreads();  // the sums have been read, the queries are there
   }
 }
 

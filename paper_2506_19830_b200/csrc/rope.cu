@@ -2,7 +2,7 @@
 //
 // A CTA takes the heads of a few tokens.  It first works out their angles: a position times a frequency in turns, in 64 bits, of which the whole quarters are dropped; what is
 // left, an eighth of a turn at most, is exact to 2^-53 of the angle however far the position.  Its sine and cosine are Taylor series in 64 bits, times the amplitude, rounded once: with sinpi
-// and cospi in fp32 twice as many codes of an 8-bit cache came out one off.  All heads of a token share them through shared memory.
+// and cospi in fp32 two and a half times as many codes of an 8-bit cache came out one off.  All heads of a token share them through shared memory.
 // A thread then has 8 pairs of a head, both channels of each, so that rows may be turned where they are.  With the channels of a pair half a turned
 // part apart these are 8 channels in each half, else 16 side by side: two 16-byte loads and stores.  Where the halves do not start on 16 bytes (rot_dim no multiple of 16) a thread brings
 // 16 channels side by side and the threads of a head find their pairs in shared memory (channel by channel from memory a prompt of 32 K tokens, 90 of 128 channels turned, took 1172 us; now 201).
