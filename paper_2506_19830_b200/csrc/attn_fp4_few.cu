@@ -74,6 +74,8 @@ attn_fp4_few_kernel(DevBatch d, DevTcPlan tc, const __grid_constant__ Fp4Call in
   constexpr int kWarps = Sh::kWarps, kThreads = Sh::kThreads, kRows = Sh::kRows, kStride = Sh::kStride, kKWords = kD / 32, kVWords = kD / 64, kMTiles = kD / 16;
   extern __shared__ __align__(16) float s_sum[];  // [warp][query][kStride], then the warps' stages
   __shared__ float2 s_ml[kWarps][kRows];
+  __shared__ uint4 s_raw[kRows][kD / 8];  // the next piece's queries,
+  __shared__ int2 s_sees[kRows];          // and what they see, as the plan has it
   __shared__ __align__(16) uint16_t s_q[kRows][kD + 8];  // a piece's queries as halves
   __shared__ int4 s_info[kRows];  // what they see (RowInfo), and what a score is worth, negative for one with a channel too small beside its largest to be a half
   __shared__ TcPiece s_piece[kHeld];
@@ -94,16 +96,18 @@ attn_fp4_few_kernel(DevBatch d, DevTcPlan tc, const __grid_constant__ Fp4Call in
   auto piece_of = [&](int pc) { return pc - piece0 < kHeld ? s_piece[pc - piece0] : tc.pieces[pc]; };
   auto req_of = [&](int pc, const TcPiece &pi) { return pc - piece0 < kHeld ? s_req[pc - piece0] : tc.reqs[pi.req]; };
 
-  // what is asked for: entries of the page list first, then the page that the entry of the step before names
+  // What is asked for: entries of the page list first, those of the warp's next 32 pages of a piece at once, one a lane and such a set ahead; then the pages that they name.
   int ask_pc = piece0 - 1, ask_i = 0, ask_n = 0, ask_head = 0, ask_dense = 0;
   const TcPage *ask_list = nullptr;
-  int2 entry = make_int2(0, 0);
-  int entry_head = -1;  // KV head of the entry on its way; -1: none
-  bool entry_masked = false;
-  auto ask_entry = [&]() {
+  struct Entries {
+    int2 mine;        // this lane's
+    int n, head;      // how many there are; their KV head
+    uint32_t masked;  // which of them have keys that not every row sees
+  } now, next;
+  auto ask_entries = [&]() {
     while (ask_i >= ask_n) {
       if (ask_pc + 1 >= piece1) {
-        entry_head = -1;
+        next.n = 0;
         return;
       }
       ++ask_pc;
@@ -115,10 +119,12 @@ attn_fp4_few_kernel(DevBatch d, DevTcPlan tc, const __grid_constant__ Fp4Call in
       ask_head = pi.kv_head;
       ask_list = tc.pages + rq.page_off + pi.tile_begin * kPagesPerTile;
     }
-    entry = ld_pair(ask_list + ask_i);
-    entry_head = ask_head;
-    entry_masked = ask_i >= ask_dense;
-    ask_i += kWarps;
+    const int i = ask_i + lane * kWarps;
+    if (i < ask_n) next.mine = ld_pair(ask_list + i);
+    next.n = min((ask_n - ask_i + kWarps - 1) / kWarps, 32);
+    next.head = ask_head;
+    next.masked = __ballot_sync(0xFFFFFFFFu, i >= ask_dense);
+    ask_i += 32 * kWarps;
   };
   // A page's codes and scales come by asynchronous copies, kStages - 1 pages ahead: 16 bytes a lane, twice from K and from V (once with head size 64), and 16 of scales from
   // the first lanes.
@@ -132,15 +138,22 @@ attn_fp4_few_kernel(DevBatch d, DevTcPlan tc, const __grid_constant__ Fp4Call in
   for (int u = 0; u < kUnits; ++u) to_v[u] = Sh::kCodeBytes + v_unit<kD>(copy_key + u * 8, copy_unit);
   const uint32_t v_lane = Sh::kCodeBytes + v_unit<kD>(2 * t, g * (kD / 16) / 16) + g * (kD / 16) % 16;  // where this lane's channels of key 2t lie
   uint32_t asked = 0;  // stage
+  int at_entry = 0;
   auto ask_page = [&]() {
-    if (entry_head >= 0) {
-      int32_t page = entry.x;
+    if (at_entry >= now.n) {
+      now = next;
+      at_entry = 0;
+      if (now.n > 0) ask_entries();
+    }
+    if (at_entry < now.n) {
+      int32_t page = __shfl_sync(0xFFFFFFFFu, now.mine.x, at_entry);
+      const int32_t meta = __shfl_sync(0xFFFFFFFFu, now.mine.y, at_entry);
       if (page < 0 || page >= d.n_pool_pages) {  // never fetch outside the pool
         d.status[0] = kDevBounds;
         d.status[1] = 200;
         page = 0;
       }
-      const int64_t row = (page * d.n_kv_heads + entry_head) * kPage;  // rows of the pools are numbered within 32 bits (tc_plan_structure)
+      const int64_t row = (page * d.n_kv_heads + now.head) * kPage;  // rows of the pools are numbered within 32 bits (tc_plan_structure)
       const uint32_t to = ring + asked * Sh::kPageBytes;
 #pragma unroll
       for (int u = 0; u < kUnits; ++u) {
@@ -149,30 +162,30 @@ attn_fp4_few_kernel(DevBatch d, DevTcPlan tc, const __grid_constant__ Fp4Call in
       }
       if (lane * 16 < 2 * Sh::kScaleBytes) copy16(to + 2 * Sh::kCodeBytes + lane * 16, scales_at + row * (kD / kFp4Group));
       if (lane == 0)
-        asm volatile("st.shared.v2.b32 [%0], {%1, %2};" ::"r"(to + 2 * Sh::kCodeBytes + 2 * Sh::kScaleBytes), "r"(entry.y), "r"(entry_masked ? 1 : 0) : "memory");
-      ask_entry();
+        asm volatile("st.shared.v2.b32 [%0], {%1, %2};" ::"r"(to + 2 * Sh::kCodeBytes + 2 * Sh::kScaleBytes), "r"(meta), "r"(now.masked >> at_entry & 1u) : "memory");
+      ++at_entry;
     }
     asm volatile("cp.async.commit_group;" ::: "memory");
     asked = asked + 1 == Sh::kStages ? 0u : asked + 1;
   };
 
   const int G = d.group;
-  // The queries of a piece: eight channels a lane, some rows a warp, asked for while the piece before is joined and left in shared memory for all warps.
+  // The queries of a piece: eight channels a lane, some rows a warp, on their way under the pages of the piece before; as halves they wait in shared memory for all warps.
   constexpr int kRowLanes = kD / 8;
   const int q_row = warp * (32 / kRowLanes) + lane / kRowLanes, q_part = lane % kRowLanes;
-  uint4 q_raw = make_uint4(0, 0, 0, 0);
-  RowInfo q_info;
   auto ask_queries = [&](int pc) {
     if (q_row >= kRows || pc >= piece1) return;  // (whole warps)
     const TcPiece pi = piece_of(pc);
     const TcReq rq = req_of(pc, pi);
-    q_raw = make_uint4(0, 0, 0, 0);
-    if (q_row < rq.n_q * G)
-      q_raw = __ldcg(reinterpret_cast<const uint4 *>(in.q + ((int64_t)(rq.q_row0 + q_row / G) * d.n_q_heads + pi.kv_head * G + q_row % G) * kD) + q_part);
-    q_info = row_info(d, tc, rq, tc.tokens_per_mtile, pi.mtile0, q_row, pi.kv_head);
+    if (q_row >= rq.n_q * G) return;
+    const int row = rq.q_row0 + q_row / G;
+    copy16(smem_u32(&s_raw[q_row][q_part]), reinterpret_cast<const uint8_t *>(in.q + ((int64_t)row * d.n_q_heads + pi.kv_head * G + q_row % G) * kD + q_part * 8));
+    if (q_part == 0) asm volatile("cp.async.ca.shared.global [%0], [%1], 8;" ::"r"(smem_u32(&s_sees[q_row])), "l"(tc.rows + row) : "memory");
   };
   auto leave_queries = [&](int pc) {
     if (q_row >= kRows || pc >= piece1) return;
+    const bool live = q_row < req_of(pc, piece_of(pc)).n_q * G;
+    const uint4 q_raw = live ? s_raw[q_row][q_part] : make_uint4(0, 0, 0, 0);
     const uint32_t m = 0x7FFF7FFFu, two = __vmaxu2(__vmaxu2(q_raw.x & m, q_raw.y & m), __vmaxu2(q_raw.z & m, q_raw.w & m));
     uint32_t top = max(two & 0xFFFFu, two >> 16);
 #pragma unroll
@@ -192,12 +205,19 @@ attn_fp4_few_kernel(DevBatch d, DevTcPlan tc, const __grid_constant__ Fp4Call in
     const unsigned any = __ballot_sync(0xFFFFFFFFu, odd && top < 0x7F80u) >> (lane - q_part) & ((1u << kRowLanes) - 1u);
     *reinterpret_cast<uint4 *>(&s_q[q_row][q_part * 8]) = make_uint4(h[0], h[1], h[2], h[3]);
     const float unit = in.scale_log2 * (top < 0x7F80u ? __uint_as_float((uint32_t)(127 - e) << 23) : __uint_as_float(0x7FC00000u));
-    if (q_part == 0) s_info[q_row] = make_int4(q_info.depth, q_info.branch, q_info.limit, __float_as_int(any != 0u ? -unit : unit));
+    if (q_part == 0) {
+      const int2 sees = live ? s_sees[q_row] : make_int2(-1, -1);
+      s_info[q_row] = make_int4(live ? sees.x & 0xFFFF : -1, sees.x >> 16, sees.y, __float_as_int(any != 0u ? -unit : unit));
+    }
   };
-  ask_entry();
+  now.n = 0;
+  now.mine = next.mine = make_int2(0, 0);
+  ask_entries();
   ask_queries(piece0);
+  asm volatile("cp.async.commit_group;" ::: "memory");
 #pragma unroll 1
   for (int i = 0; i + 1 < Sh::kStages; ++i) ask_page();
+  asm volatile("cp.async.wait_group %0;" ::"n"(Sh::kStages - 1) : "memory");
   leave_queries(piece0);
   __syncthreads();
   uint32_t from = 0;  // stage
@@ -223,6 +243,7 @@ attn_fp4_few_kernel(DevBatch d, DevTcPlan tc, const __grid_constant__ Fp4Call in
     }
     // rows with a channel too small beside their largest to be a half
     unsigned again = __ballot_sync(0xFFFFFFFFu, lane < kRows && s_info[lane % kRows].w < 0);
+    ask_queries(pc + 1);
     float o[kNB][kMTiles][4], ref[kNB][2], l[kNB][2];
 #pragma unroll
     for (int b = 0; b < kNB; ++b) {
@@ -342,7 +363,6 @@ attn_fp4_few_kernel(DevBatch d, DevTcPlan tc, const __grid_constant__ Fp4Call in
       }
     }
     // the warps' sums, joined
-    ask_queries(pc + 1);
 #pragma unroll
     for (int b = 0; b < kNB; ++b) {
 #pragma unroll
@@ -390,6 +410,8 @@ attn_fp4_few_kernel(DevBatch d, DevTcPlan tc, const __grid_constant__ Fp4Call in
     }
     for (int r = warp; r < rows; r += kWarps)
       if ((again >> r) & 1u) exact_row<kD>(in, pc, 0, r, nullptr);
+    if (q_row < kRows && pc + 1 < piece1 && n_pages - warp <= (Sh::kStages - 1) * kWarps)
+      asm volatile("cp.async.wait_all;" ::: "memory");  // (the queries; with kStages pages or more they have been waited for)
     leave_queries(pc + 1);
     __syncthreads();  // the sums have been read, the queries are there
   }
