@@ -16,6 +16,10 @@
 //   warp 12     brings the queries, by TMA; the softmax threads turn them into halves where they lie, a row each.
 //   warps 13, 14  MMA issuers of stream 0 and 1.
 //   warps 0-3, 4-7  softmax of stream 0 and 1, one thread per query row.
+//
+// What bounds it, in cycles of a half-unit (64 keys of either stream).  96 query tokens over 32 K keys (68 us): 1460 of a softmax warp, in which the exponentials of the two warps that share
+// a unit take 1024, and 390 of waiting: products at N = 64 read Q's tile again for every half, which with the converters' stores is, by count, three quarters of what shared memory gives.  16 requests over 8 to
+// 32 K keys (172 us), whose pieces have one M-tile: converters, 1050 a tile, two of them a half-unit; without them it would take 161.  64-wide heads: the softmax, 1540 of 1710.
 #include <cuda.h>
 
 #include <algorithm>
@@ -43,7 +47,8 @@ struct Shape {
   static constexpr int kRaw = kD == 128 ? 3 : 6;          // tiles of codes on their way or being converted
   static constexpr int kScales = kD / kFp4Group;          // scale bytes of a row
   static constexpr int kPasses = kD / 32;                 // 16-byte groups of a lane in a tile
-  static constexpr int kBatch = kD == 128 ? 2 : 1;        // ... whose codes are asked for at once: 177 us where one at a time takes 191 (16 requests over 8 to 32 K keys); with two passes, of head size 64, one is 1% faster
+  // ... whose codes are asked for at once: 178 us where one at a time takes 188 (16 requests over 8 to 32 K keys, with the launch); with two passes, of head size 64, one is 1% faster
+  static constexpr int kBatch = kD == 128 ? 2 : 1;
   static constexpr int kPassKeys = kKeys / kPasses;
   static constexpr int kCodeBytes = 128 * kD / 2, kScaleBytes = 128 * kScales;
   static constexpr int kSlotBytes = kCodeBytes + kScaleBytes + 32;  // of a tile: codes, scales, valid tokens of its pages

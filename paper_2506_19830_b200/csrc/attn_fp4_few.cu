@@ -12,8 +12,10 @@
 // Numbers are those of attn_fp4.cu.  A row's reference exponent is set again when a score is more than 2^kRescale above it; the lanes that see it so ask the others for the
 // maximum then.
 //
-// What bounds it is turning codes into operands: nine instructions for a word of eight, some 300 for a page of K and V, 16 of which are products.  As bf16 it took 17
-// for a word: 48 single tokens over 9 K keys each 158 us.
+// What bounds it is turning codes into operands: nine instructions for a word of eight, some 350 for a page of K and V, 16 of which are products; a scheduler takes 530 cycles for a page,
+// its issue slots are taken for two thirds of the time and what only every other cycle takes (conversions, shifts, masks) for half of it.  48 single tokens over 2 to 32 K keys,
+// 40 heads of 128 on 8: 128 us, 434 MB at 3.4 TB/s.  As bf16 a word took 17 instructions and the call 158 us; with every warp turning the queries of its pieces by itself
+// (5500 cycles a piece) 142, with one page entry asked for at a time 138.
 #include <algorithm>
 
 #include "attn_fp4.cuh"
@@ -30,7 +32,7 @@ constexpr int kHeld = 32;                   // pieces whose records a CTA keeps 
 template <int kD, int kNB>
 struct Shape {
   static constexpr int kRows = 8 * kNB;     // queries
-  // a lane's sums, queries and two pages take 128 registers for 8 queries of 128 channels, 230 for 16
+  // a lane's sums, queries and a page take 128 registers for 8 queries of 128 channels, 230 for 16
   static constexpr int kWarps = kNB == 1 ? 16 : 8, kThreads = kWarps * 32;
   static constexpr int kStride = kD + 8;    // floats of a query's sums in shared memory: the four quarters of a warp then write to different banks
   static constexpr int kSumBytes = kWarps * kRows * kStride * 4;

