@@ -283,3 +283,38 @@ def test_on_a_stream_of_its_own_and_replayed_with_other_positions():
         check_bf16(bf16_to_f32(R.bf16_bits(out)).astype(np.float64), O.rope(q, p, f), SLACK * pair_size(q, 128, False))
         check_stored("bf16", cache, 0, np.arange(n), O.rope(k, p, f), SLACK * pair_size(k, 128, False))
     ctx.close()
+
+
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("hq,h,d,rot,n", [(8, 2, 128, 90, 5000), (4, 4, 64, 34, 6000), (3, 1, 128, 126, 2500), (96, 48, 128, 90, 7), (96, 48, 128, 128, 7), (96, 48, 64, 2, 5)])
+def test_halves_that_start_anywhere(hq, h, d, rot, n, kind):
+    """Several tokens to a CTA, more heads than it takes, the most shared memory; what is not turned keeps its bits."""
+    rng = np.random.default_rng(rot + n)
+    model, pages = Model(hq, h, d, 8), n // 16 + 1
+    ctx, cache = B.Context(model, 0), empty(kind, model, pages)
+    q, k, v = rows(rng, n, hq, d), rows(rng, n, h, d), rows(rng, n, h, d)
+    at, slots = rng.integers(0, 1 << 20, n).astype(np.int32), rng.permutation(pages * 16)[:n].astype(np.int64)
+    to = lambda a: torch.from_numpy(a).to(DEV)  # noqa: E731
+    out = torch.zeros((n, hq, d), dtype=torch.bfloat16, device=DEV)
+    ctx.lr_rope_write(B.Rope(rot), to(at), cache, R.bf16_tensor(k, DEV), R.bf16_tensor(v, DEV), to(slots), R.bf16_tensor(q, DEV), out)
+    f, _ = O.rope_frequencies(rot, 1e4)
+    assert np.array_equal(R.bf16_bits(out)[:, :, rot:], q[:, :, rot:])
+    qq, kk, vv = (bf16_to_f32(x).astype(np.float64) for x in (q, k, v))
+    check_bf16(bf16_to_f32(R.bf16_bits(out)).astype(np.float64), O.rope(qq, at, f), SLACK * pair_size(qq, rot, False))
+    check_stored(kind, cache, 0, slots, O.rope(kk, at, f), SLACK * pair_size(kk, rot, False))
+    check_stored(kind, cache, 1, slots, vv, np.zeros_like(vv))
+    ctx.close()
+
+
+def test_rows_that_are_not_finite_beside_halves_that_start_anywhere():
+    model = Model(2, 1, 128, 8)
+    ctx, cache = B.Context(model, 0), empty("bf16", model, 1)
+    x = torch.ones((2, 1, 128), dtype=torch.bfloat16, device=DEV)
+    x.view(torch.int16)[0, 0, 100] = 0x7FA5  # a NaN of its own bits, not turned
+    x[1, 0, 3] = float("inf")
+    q = torch.cat([x, x], 1)
+    ctx.lr_rope_write(B.Rope(90), torch.full((2,), 5, dtype=torch.int32, device=DEV), cache, x, x, torch.arange(2, device=DEV), q, q)
+    for got in (cache.k[0, 0, :2], q[:, 0], q[:, 1]):
+        assert got.view(torch.int16)[0, 100] == 0x7FA5 and int(torch.isfinite(got[0].float()).sum()) == 127
+        assert not bool(torch.isfinite(got[1, [3, 48]].float()).any()) and int(torch.isfinite(got[1].float()).sum()) == 126
+    ctx.close()
