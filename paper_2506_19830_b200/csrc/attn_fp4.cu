@@ -19,7 +19,8 @@
 //
 // What bounds it, in cycles of a half-unit (64 keys of either stream).  96 query tokens over 32 K keys (68 us): 1460 of a softmax warp, in which the exponentials of the two warps that share
 // a unit take 1024, and 390 of waiting: products at N = 64 read Q's tile again for every half, which with the converters' stores is, by count, three quarters of what shared memory gives.  16 requests over 8 to
-// 32 K keys (172 us), whose pieces have one M-tile: converters, 1050 a tile, two of them a half-unit; without them it would take 161.  64-wide heads: the softmax, 1540 of 1710.
+// 32 K keys (172 us), whose pieces have one M-tile: converters, 1010 a tile, two of them a half-unit (twice the warps do not help: their stores
+// and the products' reads share a memory); without them it would take 161.  64-wide heads: the softmax, 1540 of 1710.
 #include <cuda.h>
 
 #include <algorithm>
