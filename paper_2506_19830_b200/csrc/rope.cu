@@ -23,7 +23,9 @@ namespace {
 constexpr int kThreads = 256;
 constexpr int kHeads = 64;       // of q, k and v together, a CTA's share of a token
 constexpr int kMaxTokens = 8;    // ... and how many tokens it takes; half as many where heads wait in shared memory
-constexpr int kRowBytes = 36 << 10;  // of shared memory for rows that are to be quantised
+// Of shared memory for rows that are to be quantised, with what else there is below 48 KB.  8 K tokens of 32 + 8 + 8 heads of 128 into an 8-bit cache: 48 us with the four tokens
+// that fit, 51 with two, 67 with one.
+constexpr int kRowBytes = 36 << 10;
 constexpr int kPadded = kFp4Group + 4;  // floats that 32 channels take there: threads next to each other, a group each, read different banks
 
 struct RopeArgs {
