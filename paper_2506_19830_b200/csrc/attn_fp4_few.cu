@@ -32,8 +32,9 @@ constexpr int kHeld = 32;                   // pieces whose records a CTA keeps 
 template <int kD, int kNB>
 struct Shape {
   static constexpr int kRows = 8 * kNB;     // queries
-  // a lane's sums, queries and a page take 128 registers for 8 queries of 128 channels, 230 for 16
-  static constexpr int kWarps = kNB == 1 ? 16 : 8, kThreads = kWarps * 32;
+  // A lane's sums, queries and a page take 128 registers for 8 queries of 128 channels, 230 for 16, 160 for 16 of 64: with more warps than there is room for it spills (48 requests
+  // of 16 rows over 2 to 32 K keys: 128-wide 189 us with 8 warps, 208 with 10; 64-wide 120 with 12, 126 with 16, 140 with 8).
+  static constexpr int kWarps = kNB == 1 ? 16 : kD == 64 ? 12 : 8, kThreads = kWarps * 32;
   static constexpr int kStride = kD + 8;    // floats of a query's sums in shared memory: the four quarters of a warp then write to different banks
   static constexpr int kSumBytes = kWarps * kRows * kStride * 4;
   // pages of a warp on their way or being used: K's codes, V's, their scales, what the keys are
