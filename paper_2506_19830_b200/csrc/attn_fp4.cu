@@ -57,6 +57,10 @@ struct Shape {
   static constexpr int kSmemBytes = 2 * kTileBytes + kStages * kTileBytes + kRawBytes + 4096;  // tiles, codes, Ctrl; the base must be 1024-aligned
 };
 constexpr int kMaxRaw = 6;
+// Marks of pieces with a scale beyond halves, of as many pieces in turn as may be under way.  Softmax threads read that of a piece at its end, and until all of them have, no issuer
+// starts on the next (q_full).  So the ring ends kStages positions behind the piece, two of which are the least that one takes: converters are kStages / 2 pieces ahead at most.
+constexpr int kMarks = 8;
+static_assert((kMarks & (kMarks - 1)) == 0 && kMarks > Shape<64>::kStages / 2 && kMarks > Shape<128>::kStages / 2, "a mark is read before its place is another piece's");
 constexpr float kLift = 2.0f;   // log2 units: a row's reference is set this much below its maximum so far; the more, the smaller the weights that are more than 0,
 constexpr float kGrow = 15.0f;  // ... and keys beyond this are done again with another one: halves end at 2^16
 
@@ -72,7 +76,7 @@ struct __align__(16) Ctrl {
   uint64_t wait_limit_ns;  // bound of every wait, measured on the global timer
   uint64_t raw_full[kMaxRaw], raw_empty[kMaxRaw], q_raw;
   uint64_t alive_ns;      // when a warp was last seen at work that may take longer than a wait (exact_row)
-  int32_t odd_piece[4];   // 1 + the last piece of four in turn that has a scale beyond halves; converters are two pieces ahead at most
+  int32_t odd_piece[kMarks];  // 1 + the last piece of kMarks in turn that has a scale beyond halves
   Fp4Call call;
   float2 ml_xch[128];     // (reference exponent, row sum) of stream 1's rows, for the in-CTA combination
   float q_unit[2][128];   // of the rows of either M-tile: what a score is worth
@@ -340,7 +344,7 @@ attn_fp4_kernel(const __grid_constant__ CUtensorMap q_map, DevBatch d, DevTcPlan
     mbar_init(&ctrl->xch, 128);
     ctrl->abort_flag = 0;
     ctrl->alive_ns = 0;
-    for (int i = 0; i < 4; ++i) ctrl->odd_piece[i] = 0;
+    for (int i = 0; i < kMarks; ++i) ctrl->odd_piece[i] = 0;
     ctrl->wait_limit_ns = (uint64_t)tc.wait_limit_us * 1000ull;
     fence_barrier_init();
   }
@@ -399,7 +403,7 @@ attn_fp4_kernel(const __grid_constant__ CUtensorMap q_map, DevBatch d, DevTcPlan
               const int k = kD == 128 ? lane : (lane & 15) * 2 + (x >> 1);
               odd = odd || (odd_scale((word >> (8 * x)) & 0xFFu) && (k & (kPage - 1)) < (int)valid[k >> 4]);
             }
-            if (odd) *reinterpret_cast<volatile int32_t *>(&ctrl->odd_piece[pc & 3]) = pc + 1;
+            if (odd) *reinterpret_cast<volatile int32_t *>(&ctrl->odd_piece[pc & (kMarks - 1)]) = pc + 1;
           }
           uint32_t to = to0 + stage * kTileBytes;
 #pragma unroll 1
@@ -810,7 +814,7 @@ attn_fp4_kernel(const __grid_constant__ CUtensorMap q_map, DevBatch d, DevTcPlan
         if (ok && writer && !idle) {
           // rows to be gone through again: those of a piece with scales beyond halves, and of queries that are
           const int slot = pi.slot[pair ? 0 : s];
-          const bool odd_piece = *reinterpret_cast<volatile int32_t *>(&ctrl->odd_piece[pc & 3]) == pc + 1;
+          const bool odd_piece = *reinterpret_cast<volatile int32_t *>(&ctrl->odd_piece[pc & (kMarks - 1)]) == pc + 1;
           uint32_t again = __ballot_sync(0xFFFFFFFFu, ri.q_index >= 0 && (odd_piece || ctrl->q_unit[mode == 2 ? s : 0][r] < 0.f));
           tc_fence_after();
           store_rows<kD>(o_addr, lane_base + 256 + (1 - s) * 128, slot, self, other, other_live, m_out, l_out, r, (again >> lane) & 1u ? -1 : ri.q_index, in.out, in.lse,
