@@ -258,10 +258,10 @@ __device__ __noinline__ void store_rows(uint32_t o_addr, uint32_t o_other, int s
   }
 }
 
-// Row r of an M-tile of Q, which lies as the copy left it, as halves times a power of two; zeros where no query is.  Returns what a score is worth (NaN for a row that is not finite),
+// Row r of an M-tile of Q, which lies as the copy left it, as halves times a power of two; zeros where no query is.  Returns what a score is worth (score_unit),
 // negative if the row has a channel too small beside its largest to be a half.
 template <int kD>
-__device__ __noinline__ float convert_row(uint32_t tile, int r, bool live) {
+__device__ __noinline__ float convert_row(uint32_t tile, int r, bool live, float scale_log2) {
   uint32_t top2 = 0, least2 = 0xFFFFFFFFu;  // of low and high halves: largest magnitudes, least ones that are not 0, less one
 #pragma unroll 1
   for (int h = 0; h < kD / 64; ++h)
@@ -275,7 +275,7 @@ __device__ __noinline__ float convert_row(uint32_t tile, int r, bool live) {
   const uint32_t top = max(top2 & 0xFFFFu, top2 >> 16), least = min(least2 & 0xFFFFu, least2 >> 16);
   const int e = min(half_exponent(top), (int)kQMostExponent);
   const float by = live ? __uint_as_float((uint32_t)(127 + e) << 23) : 0.f;
-  const bool odd = live && least != 0xFFFFu && ((least + 1u) >> 7) + e < 127 - 17 && top < 0x7F80u;
+  const bool odd = least != 0xFFFFu && ((least + 1u) >> 7) + e < 127 - 17;
 #pragma unroll 1
   for (int h = 0; h < kD / 64; ++h)
 #pragma unroll 2
@@ -290,8 +290,7 @@ __device__ __noinline__ float convert_row(uint32_t tile, int r, bool live) {
       for (int i = 0; i < 4; ++i) t[i] = pack_f16(bits_f(w[i] << 16) * by, bits_f(w[i] & 0xFFFF0000u) * by);
       st_shared(at, t);
     }
-  const float worth = top < 0x7F80u ? __uint_as_float((uint32_t)(127 - e) << 23) : __uint_as_float(0x7FC00000u);
-  return !live ? 1.0f : odd ? -worth : worth;
+  return live ? score_unit(scale_log2, e, top, odd) : 1.0f;
 }
 
 template <int kD>
@@ -690,14 +689,14 @@ attn_fp4_kernel(const __grid_constant__ CUtensorMap q_map, DevBatch d, DevTcPlan
         if (mode == 2 || s == 0) {
           ok = wait<kD, 0>(&ctrl->q_raw, (uint32_t)(pc - piece0) & 1u, 245);
           if (ok) {
-            ctrl->q_unit[mode == 2 ? s : 0][r] = convert_row<kD>(smem_u32(q_smem) + (mode == 2 ? s : 0) * kTileBytes, r, ri.q_index >= 0);
+            ctrl->q_unit[mode == 2 ? s : 0][r] = convert_row<kD>(smem_u32(q_smem) + (mode == 2 ? s : 0) * kTileBytes, r, ri.q_index >= 0, in.scale_log2);
             fence_proxy_async();
           }
         }
         if (ok) {
           mbar_arrive(&ctrl->q_full);
           ok = wait<kD, 0>(&ctrl->q_full, (uint32_t)(pc - piece0) & 1u, 246);
-          sc_row = in.scale_log2 * fabsf(ctrl->q_unit[mode == 2 ? s : 0][r]);
+          sc_row = fabsf(ctrl->q_unit[mode == 2 ? s : 0][r]);
         }
       }
       if (ok && my_units > 0) {

@@ -85,6 +85,12 @@ __device__ __forceinline__ void copy16(uint32_t dst, const uint8_t *src) {
 // 2^-17, 2^-31 of the largest; a row with a smaller one that is not 0 is gone through again.  (Powers of two beyond what fp32 has: such a row is, too.)
 __device__ __forceinline__ int half_exponent(uint32_t top) { return 141 - (int)(top >> 7); }
 constexpr uint32_t kQMostExponent = 126;
+// What a score of such a row is worth, log2 units; NaN for a row that is not finite, negative for one to be gone through again.  Products are below 2^38 (2^15 of Q, 49,152 of K, 128 channels):
+// with the least normal number in place of a smaller unit scores are below 2^-88, as they would be, and those of keys that the row does not see stay -infinity, which 0 would make NaN.
+__device__ __forceinline__ float score_unit(float scale_log2, int e, uint32_t top, bool odd) {
+  const float unit = fmaxf(scale_log2 * __uint_as_float((uint32_t)(127 - e) << 23), 0x1p-126f);
+  return top >= 0x7F80u ? __uint_as_float(0x7FC00000u) : odd || unit == INFINITY ? -unit : unit;
+}
 
 // Row r of the M-tile that stream s of piece pc has, by a whole warp on the CUDA cores: what the tensor cores would have left for it.  32 keys at a time: a lane scores
 // one, the lanes then share the value rows.  alive: told the time now and then, as this may take longer than a wait.

@@ -80,7 +80,7 @@ attn_fp4_few_kernel(DevBatch d, DevTcPlan tc, const __grid_constant__ Fp4Call in
   __shared__ uint4 s_raw[kRows][kD / 8];  // the next piece's queries,
   __shared__ int2 s_sees[kRows];          // and what they see, as the plan has it
   __shared__ __align__(16) uint16_t s_q[kRows][kD + 8];  // a piece's queries as halves
-  __shared__ int4 s_info[kRows];  // what they see (RowInfo), and what a score is worth, negative for one with a channel too small beside its largest to be a half
+  __shared__ int4 s_info[kRows];  // what they see (RowInfo), and what a score is worth (score_unit)
   __shared__ TcPiece s_piece[kHeld];
   __shared__ TcReq s_req[kHeld];
   __shared__ int s_odd;  // 1 + the last piece that has a scale beyond halves
@@ -205,12 +205,11 @@ attn_fp4_few_kernel(DevBatch d, DevTcPlan tc, const __grid_constant__ Fp4Call in
       odd = odd || (lo != 0.f && fabsf(lo) < 0x1p-17f) || (hi != 0.f && fabsf(hi) < 0x1p-17f);
       h[j] = pack_f16(lo, hi);
     }
-    const unsigned any = __ballot_sync(0xFFFFFFFFu, odd && top < 0x7F80u) >> (lane - q_part) & ((1u << kRowLanes) - 1u);
+    const unsigned any = __ballot_sync(0xFFFFFFFFu, odd) >> (lane - q_part) & ((1u << kRowLanes) - 1u);
     *reinterpret_cast<uint4 *>(&s_q[q_row][q_part * 8]) = make_uint4(h[0], h[1], h[2], h[3]);
-    const float unit = in.scale_log2 * (top < 0x7F80u ? __uint_as_float((uint32_t)(127 - e) << 23) : __uint_as_float(0x7FC00000u));
     if (q_part == 0) {
       const int2 sees = live ? s_sees[q_row] : make_int2(-1, -1);
-      s_info[q_row] = make_int4(live ? sees.x & 0xFFFF : -1, sees.x >> 16, sees.y, __float_as_int(any != 0u ? -unit : unit));
+      s_info[q_row] = make_int4(live ? sees.x & 0xFFFF : -1, sees.x >> 16, sees.y, __float_as_int(score_unit(in.scale_log2, e, top, any != 0u)));
     }
   };
   now.n = 0;
@@ -244,7 +243,7 @@ attn_fp4_few_kernel(DevBatch d, DevTcPlan tc, const __grid_constant__ Fp4Call in
         depth[b][y] = x.x, branch[b][y] = x.y, limit[b][y] = x.z, sc[b][y] = fabsf(__int_as_float(x.w));
       }
     }
-    // rows with a channel too small beside their largest to be a half
+    // rows with a channel too small beside their largest to be a half, or scores beyond fp32
     unsigned again = __ballot_sync(0xFFFFFFFFu, lane < kRows && s_info[lane % kRows].w < 0);
     ask_queries(pc + 1);
     float o[kNB][kMTiles][4], ref[kNB][2], l[kNB][2];
