@@ -98,7 +98,7 @@ class PagedCycleEngine:
         if self.rope is not None:
             k, v, slots = R.bf16_tensor(k_bits, self.device), R.bf16_tensor(v_bits, self.device), self._slots(pages, n)
             at = torch.arange(position, position + n, dtype=torch.int32, device=self.device)
-            behind = n if q is None else n - len(q)  # tokens without queries
+            behind = n if q is None or len(q) > n else n - len(q)  # tokens without queries (more of those than tokens the plan refuses)
             if behind > 0:
                 self.ctx.lr_rope_write(self.rope, at[:behind], self.any_cache, k[:behind], v[:behind], slots[:behind])
             if behind < n:
@@ -170,9 +170,10 @@ class PagedCycleEngine:
             span_slot.append(place(self.pages[r][: (self.length[r] + PAGE - 1) // PAGE]))
             seg_parent.append(-1)
             behind = [self.length[r]]  # where what continues a node stands: behind the tokens up to it
+            start_of = lambda node: behind[node] if 0 <= node < len(behind) else 0  # noqa: E731 (a node that is not there the plan refuses)
             for c, (k, v) in enumerate(x.segs):
                 pages = self._alloc(len(k))
-                start = behind[int(x.parents[c]) if len(x.parents) else c]
+                start = start_of(int(x.parents[c]) if len(x.parents) else c)
                 self._write(pages, k, v, start)
                 behind.append(start + len(k))
                 span_len.append(len(k))
@@ -181,7 +182,7 @@ class PagedCycleEngine:
             req_span_off.append(len(span_len))
             for b in x.branches:
                 pages = self._alloc(len(b.k_tail))
-                self._write(pages, b.k_tail, b.v_tail, behind[b.node], q[cu_q[-1]:cu_q[-1] + b.q_len])
+                self._write(pages, b.k_tail, b.v_tail, start_of(b.node), q[cu_q[-1]:cu_q[-1] + b.q_len])
                 br["br_req"].append(r)
                 br["br_depth"].append(b.node)
                 br["br_own_len"].append(len(b.k_tail))
