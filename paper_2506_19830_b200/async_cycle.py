@@ -135,6 +135,10 @@ class AsyncCycleEngine(PagedCycleEngine, StageExecutor):
         self._source: Optional[Callable[[int], PositionInput]] = None
         self.results: Dict[int, dict] = {}
 
+    def fork(self, r: int) -> int:
+        """Refused: stages are those of one request."""
+        raise NotImplementedError("the asynchronous engine advances one request: it cannot be forked")
+
     # ---- one stage --------------------------------------------------------------------------------------
     def run_stage(self, source: Callable[[int], PositionInput], max_positions: Optional[int] = None) -> dict:
         """Runs one stage of request 0.  ``source(i)`` is asked for position i when the controller starts it (its
