@@ -19,65 +19,34 @@ namespace {
 
 constexpr int kThreads = 256;
 
-struct Fp8Rows {  // the rows of a call
-  const int64_t *slots;
-  int64_t n_rows;      // n_tokens * heads
-  int64_t n_slots;     // of the cache
-  int64_t k_stride, v_stride;
-  int32_t heads;
-  int32_t *status;
-};
-
-struct Fp8Row {
-  int64_t token, at;  // at: (page * heads + head) * 16 + place, the row's number in a pool; -1: nothing to do
-  int32_t head;
-};
-
-__device__ __forceinline__ Fp8Row fp8_row(const Fp8Rows &w, int64_t row) {
-  Fp8Row r;
-  r.token = row / w.heads;
-  r.head = (int32_t)(row - r.token * w.heads);
-  const int64_t slot = w.slots[r.token];
-  r.at = -1;
-  if (slot >= 0 && slot < w.n_slots) r.at = ((slot / kPage) * w.heads + r.head) * kPage + slot % kPage;
-  else if (slot >= 0 && w.status != nullptr) {
-    w.status[0] = LR_EBOUNDS;
-    w.status[1] = (int32_t)r.token;
-  }
-  return r;
-}
-
 // |x| of two bf16 numbers, as integers
 __device__ __forceinline__ uint32_t abs2(uint32_t x) { return x & 0x7FFF7FFFu; }
 
-__device__ __forceinline__ uint32_t codes4(uint32_t a, uint32_t b, float by) {  // four bf16 values times a power of two, as e4m3
-  uint32_t r;
-  asm("{\n\t.reg .b16 lo, hi;\n\t"
-      "cvt.rn.satfinite.e4m3x2.f32 lo, %2, %1;\n\tcvt.rn.satfinite.e4m3x2.f32 hi, %4, %3;\n\tmov.b32 %0, {lo, hi};\n\t}"
-      : "=r"(r)
-      : "f"(__uint_as_float(a << 16) * by), "f"(__uint_as_float(a & 0xFFFF0000u) * by), "f"(__uint_as_float(b << 16) * by),
-        "f"(__uint_as_float(b & 0xFFFF0000u) * by));
-  return r;
+__device__ __forceinline__ uint2 codes8(uint4 a, float by) {  // eight bf16 values times a power of two
+  const float x[8] = {__uint_as_float(a.x << 16), __uint_as_float(a.x & 0xFFFF0000u), __uint_as_float(a.y << 16), __uint_as_float(a.y & 0xFFFF0000u),
+                      __uint_as_float(a.z << 16), __uint_as_float(a.z & 0xFFFF0000u), __uint_as_float(a.w << 16), __uint_as_float(a.w & 0xFFFF0000u)};
+  return make_uint2(fp8_codes(x, by), fp8_codes(x + 4, by));
 }
 
 template <int kD>
 __global__ void __launch_bounds__(kThreads)
-fp8_write_kernel(Fp8Rows w, const uint16_t *__restrict__ k, const uint16_t *__restrict__ v, uint8_t *__restrict__ k_pool, uint8_t *__restrict__ v_pool,
+fp8_write_kernel(CacheRows w, const uint16_t *__restrict__ k, const uint16_t *__restrict__ v, uint8_t *__restrict__ k_pool, uint8_t *__restrict__ v_pool,
                  uint8_t *__restrict__ k_scale, uint8_t *__restrict__ v_scale) {
   constexpr int kLanes = kD / 16;  // threads a row
   asm volatile("griddepcontrol.wait;" ::: "memory");  // the projection may be the kernel launched just before
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   const int64_t row = ((int64_t)blockIdx.x * kThreads + threadIdx.x) / kLanes;
   const int part = threadIdx.x % kLanes;
-  Fp8Row r;
-  r.at = -1;
-  if (row < w.n_rows) r = fp8_row(w, row);
+  int64_t token;
+  int head;
+  w.split(row, token, head);
+  const int64_t at = row < w.n_rows ? cache_row(__ldcg(reinterpret_cast<const long long *>(w.slots) + token), w.n_slots, w.heads, head, token, w.status) : -1;
   uint4 x[2][2];
 #pragma unroll
   for (int side = 0; side < 2; ++side) {
     x[side][0] = x[side][1] = make_uint4(0, 0, 0, 0);
-    if (r.at >= 0) {
-      const uint16_t *src = (side != 0 ? v + r.token * w.v_stride : k + r.token * w.k_stride) + r.head * kD + part * 16;
+    if (at >= 0) {
+      const uint16_t *src = (side != 0 ? v + token * w.v_stride : k + token * w.k_stride) + head * kD + part * 16;
       x[side][0] = __ldg(reinterpret_cast<const uint4 *>(src));
       x[side][1] = __ldg(reinterpret_cast<const uint4 *>(src) + 1);
     }
@@ -91,13 +60,13 @@ fp8_write_kernel(Fp8Rows w, const uint16_t *__restrict__ k, const uint16_t *__re
 #pragma unroll
     for (int o = kLanes / 2; o > 0; o >>= 1) top = max(top, __shfl_xor_sync(0xFFFFFFFFu, top, o));
     const bool fine = top < 0x7F80u;
-    // top = (1 + m / 128) 2^E: E - 8 brings it below 512, one more where that is above 448 = 1.75 x 256
-    const int byte = max((int)(top >> 7) - 8 + ((top & 0x7Fu) > 0x60u ? 1 : 0), kFp8LeastScale);
-    const float by = __uint_as_float((uint32_t)(254 - byte) << 23);  // 2^(127 - byte)
-    const uint4 c = make_uint4(codes4(a.x, a.y, by), codes4(a.z, a.w, by), codes4(b.x, b.y, by), codes4(b.z, b.w, by));
-    if (r.at >= 0) {
-      reinterpret_cast<uint4 *>((side != 0 ? v_pool : k_pool) + r.at * kD)[part] = fine ? c : make_uint4(0, 0, 0, 0);
-      if (part == 0) (side != 0 ? v_scale : k_scale)[r.at] = (uint8_t)(fine ? (uint32_t)byte : kFp8NanScale);
+    const int byte = fp8_byte(top << 16);
+    const float by = scale_down(byte);
+    const uint2 lo = codes8(a, by), hi = codes8(b, by);
+    const uint4 c = make_uint4(lo.x, lo.y, hi.x, hi.y);
+    if (at >= 0) {
+      reinterpret_cast<uint4 *>((side != 0 ? v_pool : k_pool) + at * kD)[part] = fine ? c : make_uint4(0, 0, 0, 0);
+      if (part == 0) (side != 0 ? v_scale : k_scale)[at] = (uint8_t)(fine ? (uint32_t)byte : kFp8NanScale);
     }
   }
 }
@@ -111,7 +80,7 @@ __device__ __forceinline__ uint32_t pack2(float2 x, float by) {  // exact: a pow
 
 template <int kD>
 __global__ void __launch_bounds__(kThreads)
-fp8_read_kernel(Fp8Rows w, uint16_t *__restrict__ k, uint16_t *__restrict__ v, const uint8_t *__restrict__ k_pool, const uint8_t *__restrict__ v_pool,
+fp8_read_kernel(CacheRows w, uint16_t *__restrict__ k, uint16_t *__restrict__ v, const uint8_t *__restrict__ k_pool, const uint8_t *__restrict__ v_pool,
                 const uint8_t *__restrict__ k_scale, const uint8_t *__restrict__ v_scale) {
   constexpr int kLanes = kD / 16;  // threads a row, 8 channels in each half of it
   asm volatile("griddepcontrol.wait;" ::: "memory");
@@ -119,20 +88,23 @@ fp8_read_kernel(Fp8Rows w, uint16_t *__restrict__ k, uint16_t *__restrict__ v, c
   const int64_t row = ((int64_t)blockIdx.x * kThreads + threadIdx.x) / kLanes;
   const int part = threadIdx.x % kLanes;
   if (row >= w.n_rows) return;
-  const Fp8Row r = fp8_row(w, row);
-  if (r.at < 0) return;
+  int64_t token;
+  int head;
+  w.split(row, token, head);
+  const int64_t at = cache_row(__ldcg(reinterpret_cast<const long long *>(w.slots) + token), w.n_slots, w.heads, head, token, w.status);
+  if (at < 0) return;
   uint2 c[2][2];
 #pragma unroll
   for (int side = 0; side < 2; ++side)
 #pragma unroll
-    for (int h = 0; h < 2; ++h) c[side][h] = __ldcg(reinterpret_cast<const uint2 *>((side != 0 ? v_pool : k_pool) + r.at * kD) + part + h * kLanes);
-  const float by[2] = {fp8_scale(ld_scale(k_scale + r.at)), fp8_scale(ld_scale(v_scale + r.at))};
+    for (int h = 0; h < 2; ++h) c[side][h] = __ldcg(reinterpret_cast<const uint2 *>((side != 0 ? v_pool : k_pool) + at * kD) + part + h * kLanes);
+  const float by[2] = {fp8_scale(ld_scale(k_scale + at)), fp8_scale(ld_scale(v_scale + at))};
 #pragma unroll
   for (int side = 0; side < 2; ++side)
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
       const uint2 q = c[side][h];
-      reinterpret_cast<uint4 *>((side != 0 ? v + r.token * w.v_stride : k + r.token * w.k_stride) + r.head * kD)[part + h * kLanes] =
+      reinterpret_cast<uint4 *>((side != 0 ? v + token * w.v_stride : k + token * w.k_stride) + head * kD)[part + h * kLanes] =
           make_uint4(pack2(fp8_float2(q.x & 0xFFFFu), by[side]), pack2(fp8_float2(q.x >> 16), by[side]), pack2(fp8_float2(q.y & 0xFFFFu), by[side]),
                      pack2(fp8_float2(q.y >> 16), by[side]));
     }
@@ -143,7 +115,7 @@ fp8_read_kernel(Fp8Rows w, uint16_t *__restrict__ k, uint16_t *__restrict__ v, c
 int launch_fp8_move(lr_ctx *ctx, const lr_fp8_cache &c, bool write, void *k, int64_t k_stride, void *v, int64_t v_stride, const int64_t *slots,
                     int32_t n_tokens, int32_t *status, cudaStream_t s) {
   const lr_model &m = ctx->model;
-  const Fp8Rows w = {slots, (int64_t)n_tokens * m.n_kv_heads, c.n_pages * kPage, k_stride, v_stride, m.n_kv_heads, status};
+  const CacheRows w = {slots, (int64_t)n_tokens * m.n_kv_heads, c.n_pages * kPage, k_stride, v_stride, m.n_kv_heads, status};
   const int64_t grid = (w.n_rows * (m.head_dim / 16) + kThreads - 1) / kThreads;
   if (grid > 0x7FFFFFFF) {
     set_error("%s: too many rows in one call", write ? "lr_fp8_write" : "lr_fp8_read");

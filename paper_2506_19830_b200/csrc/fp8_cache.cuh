@@ -1,5 +1,5 @@
 // The format of the 8-bit cache, as the kernels that write and read it share it: e4m3 codes with one power-of-two scale byte a row
-// (include/lr_verify.h, lr_fp8_cache).
+// (include/lr_verify.h, lr_fp8_cache); and the rows of a call between a projection and a cache of 8 or 4 bits.
 #pragma once
 
 #include <cuda_fp16.h>
@@ -37,6 +37,53 @@ __device__ __forceinline__ float2 fp8_float2(uint32_t two) {
   __half2 t;
   memcpy(&t, &h, 4);
   return __half22float2(t);
+}
+
+// Four numbers times a power of two as e4m3 codes.
+__device__ __forceinline__ uint32_t fp8_codes(const float *x, float by) {
+  uint32_t w;
+  asm("{\n\t.reg .b16 lo, hi;\n\t"
+      "cvt.rn.satfinite.e4m3x2.f32 lo, %2, %1;\n\tcvt.rn.satfinite.e4m3x2.f32 hi, %4, %3;\n\tmov.b32 %0, {lo, hi};\n\t}"
+      : "=r"(w)
+      : "f"(x[0] * by), "f"(x[1] * by), "f"(x[2] * by), "f"(x[3] * by));
+  return w;
+}
+
+// The scale byte of numbers whose largest magnitude has these fp32 bits: (1 + m) 2^E, E - 8 brings it below 512, one more where that is above 448 = 1.75 x 256.
+__device__ __forceinline__ int fp8_byte(uint32_t top) { return max((int)(top >> 23) - 8 + ((top & 0x7FFFFFu) > 0x600000u ? 1 : 0), kFp8LeastScale); }
+// 2^(127 - byte), for bytes from 1 to 253: what a row is multiplied by
+__device__ __forceinline__ float scale_down(int byte) { return __uint_as_float((uint32_t)(254 - byte) << 23); }
+
+static_assert(kPage == 16, "slots are taken apart by shifts");
+
+// The rows of a call that moves K and V between a projection's output and the slots of a cache.
+struct CacheRows {
+  const int64_t *slots;
+  int64_t n_rows;      // n_tokens * heads
+  int64_t n_slots;     // of the cache
+  int64_t k_stride, v_stride;
+  int32_t heads;
+  int32_t *status;
+  // a thread's token and head; a division of 64 bits, which takes as long as the rest of a thread's work, only where rows are that many
+  __device__ __forceinline__ void split(int64_t row, int64_t &token, int &head) const {
+    if (n_rows <= 0x7FFFFFFF) {
+      const uint32_t t = (uint32_t)row / (uint32_t)heads;
+      token = t;
+      head = (int)((uint32_t)row - t * (uint32_t)heads);
+    } else {
+      token = row / heads;
+      head = (int)(row - token * heads);
+    }
+  }
+};
+// The number of a token's row in a pool, (page * heads + head) * 16 + place; -1: nothing to do.  A slot beyond the cache is reported.
+__device__ __forceinline__ int64_t cache_row(int64_t slot, int64_t n_slots, int32_t heads, int32_t head, int64_t token, int32_t *status) {
+  if (slot >= 0 && slot < n_slots) return ((slot >> 4) * heads + head) * kPage + (slot & 15);
+  if (slot >= 0 && status != nullptr) {
+    status[0] = LR_EBOUNDS;
+    status[1] = (int32_t)token;
+  }
+  return -1;
 }
 
 }  // namespace lr
