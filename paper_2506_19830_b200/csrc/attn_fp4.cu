@@ -18,7 +18,8 @@
 //   warps 0-3, 4-7  softmax of stream 0 and 1, one thread per query row.
 //
 // What bounds it, in cycles of a half-unit (64 keys of either stream).  96 query tokens over 32 K keys (68 us): 1460 of a softmax warp, in which the exponentials of the two warps that share
-// a unit take 1024, and 390 of waiting: products at N = 64 read Q's tile again for every half, which with the converters' stores is, by count, three quarters of what shared memory gives.  16 requests over 8 to
+// a unit take 1024, and 390 of waiting: products at N = 64 read Q's tile again for every half, which with the converters' stores is, by count, three quarters of what shared memory gives (no counter at hand has
+// the products' reads: those of loads and stores show 25 to 29 %).  16 requests over 8 to
 // 32 K keys (172 us), whose pieces have one M-tile: converters, 1010 a tile, two of them a half-unit (twice the warps do not help: their stores
 // and the products' reads share a memory); without them it would take 161.  64-wide heads: the softmax, 1540 of 1710.
 #include <cuda.h>
@@ -79,7 +80,7 @@ struct __align__(16) Ctrl {
   int32_t odd_piece[kMarks];  // 1 + the last piece of kMarks in turn that has a scale beyond halves
   Fp4Call call;
   float2 ml_xch[128];     // (reference exponent, row sum) of stream 1's rows, for the in-CTA combination
-  float q_unit[2][128];   // of the rows of either M-tile: what a score is worth
+  float q_unit[2][128];   // of the rows of either M-tile: what a score is worth (score_unit)
 };
 static_assert(sizeof(Ctrl) <= 4096, "Ctrl must fit behind the tiles");
 static_assert(Shape<64>::kSmemBytes <= 227 * 1024 && Shape<128>::kSmemBytes <= 227 * 1024, "shared memory per CTA");

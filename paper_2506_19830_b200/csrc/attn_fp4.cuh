@@ -27,7 +27,8 @@ struct Fp4Call {  // of the call, what exact_row needs
 };
 
 // Of a plan whose tc_most_rows is kFp4FewRows at most; without the merge.  48 requests of so many rows over 2 to 32 K keys, here and with the tile kernel, which pads rows to 128: 8 rows 130 us and
-// 265, 16 rows 189 and 267 (64-wide heads 87 and 208, 120 and 208).  A third set of eight has no registers left.
+// 265, 16 rows 189 and 267 (64-wide heads 87 and 208, 120 and 208).  A third set of eight has no registers left.  The largest request of a batch decides for all of it: 48 of 5 rows take 121 us,
+// with one of 15 among them 179, with one of 20 255.
 constexpr int kFp4FewRows = 16;
 int launch_attn_fp4_few(lr_plan *p, const Fp4Call &in, cudaStream_t s);
 

@@ -2,7 +2,8 @@
 //
 // A page of a layer is one page of each of its pools -- K, V and, in 8 or 4 bits, their scales -- taken as one run of 16-byte units; a CTA copies a part of one pair's
 // run, every thread kUnits of them at once.  Bound by HBM: a page is read and written once (four layers of bf16 pages, 718 MB
-// read and written: 221 us, 6.5 TB/s).
+// read and written: 221 us, 6.5 TB/s; forks of 64 K tokens in four layers of 8 heads of 128: 327 us in bf16, 170 in 8 bits, 96 in 4 bits, of 332, 168 and 88 at the copy rate).  In 4 bits
+// such a page is 1088 units, and every second CTA has 64 of them.
 #include <algorithm>
 
 #include "lr_common.cuh"

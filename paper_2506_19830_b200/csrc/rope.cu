@@ -9,7 +9,8 @@
 // For a cache in 8 or 4 bits the turned keys and the values wait in shared memory in fp32, and threads of 32 channels of a
 // row quantise them: one rounding from what was turned.
 //
-// Bound by HBM on prompts (32 K tokens of 40 + 8 + 8 heads of 128: 165 us, 940 MB at 5.7 TB/s), by the launch and the chain position -> angle -> data on a pass's drafts.
+// Bound by HBM on prompts (32 K tokens of 40 + 8 + 8 heads of 128, half of each turned: 158 us, 940 MB at 6.0 TB/s; into a cache of 8 or 4 bits, whose rows wait between two barriers, 174 and 169 us,
+// 5.0 TB/s), by the launch and the chain position -> angle -> data on a pass's drafts.
 #include <math.h>
 
 #include <algorithm>
